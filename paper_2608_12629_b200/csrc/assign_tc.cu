@@ -1645,6 +1645,21 @@ int make_tmap_rows16(CUtensorMap* m, const void* base, i64 rows, int box_rows) {
     return r == CUDA_SUCCESS ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
+// bytes viewed as [rows][cols], rows `stride` bytes apart (cols, stride multiples of 16); box = 128 bytes x box_rows rows,
+// 128-byte swizzle, zeros outside
+int make_tmap_bytes(CUtensorMap* m, const void* base, i64 cols, i64 rows, i64 stride, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return CAKE_ERR_CUDA;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride)};
+    cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CAKE_OK : CAKE_ERR_CUDA;
+}
+
 #ifdef CAKE_ASSIGN_ACC
 extern "C" __attribute__((visibility("default"))) int cake_debug_read_acc(long long* host) {
     cudaDeviceSynchronize();

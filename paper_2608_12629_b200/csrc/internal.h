@@ -74,6 +74,8 @@ int launch_assign_pair(const cake_bf16* X, const cake_bf16* C, int B, i64 N, int
 // and bytes viewed as [rows][16], box 16 x box_rows, no swizzle
 int make_tmap_bf16_rows(CUtensorMap* m, const void* base, int D, i64 rows, int batch, int box_rows);
 int make_tmap_rows16(CUtensorMap* m, const void* base, i64 rows, int box_rows);
+// bytes viewed as [rows][cols], rows `stride` bytes apart, box 128 x box_rows, 128-byte swizzle
+int make_tmap_bytes(CUtensorMap* m, const void* base, i64 cols, i64 rows, i64 stride, int box_rows);
 // Fused update (fuse_sums / fuse_counts / fuse_ctas all given, one problem, K <= 128, D <= 128 and room in shared
 // memory): the assign kernel also adds the rows of every tile to per-cluster sums on the tensor core.  On return
 // *fuse_ctas = n > 0 says that it did: fuse_sums then holds n partial sums of [128][round_up(D, 16)] floats (one per

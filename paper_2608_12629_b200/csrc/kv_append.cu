@@ -1,0 +1,258 @@
+// Keys and values of new tokens into a paged cache, keys and queries rotated by their positions on the way.
+//
+//   (a, b) -> (a cos - b sin, b cos + a sin) for the pairs (i, i + rot/2) or (2i, 2i+1) of a head's first `rot` elements
+//
+// Bound by memory: q, k, v are read once and written once.  A thread keeps the cosines and sines of its place in a head
+// and walks over heads, so the table is read once per token and group of threads, not once per head.
+#include "serving.cuh"
+
+namespace cake {
+namespace serving {
+namespace {
+
+struct AppendArgs {
+    cake_paged_cache c;
+    const cake_bf16* k;
+    const cake_bf16* v;
+    const cake_bf16* q;
+    cake_bf16* out_q;
+    const long long* slots;
+    const int* positions;
+    const float* cos_sin;
+    i64 k_stride, v_stride, q_stride, max_positions, T;
+    int Hq, rot;
+    int* status;
+};
+
+// where a token's keys and values go; false: nowhere
+struct Place {
+    bool rotate_ok, kv;
+    i64 page;
+    int off, pos;
+};
+__device__ __forceinline__ Place place_of(const AppendArgs& a, i64 t, bool report) {
+    Place p;
+    p.pos = a.rot ? a.positions[t] : 0;
+    p.rotate_ok = !a.rot || (p.pos >= 0 && p.pos < a.max_positions);
+    const i64 slot = a.slots[t];
+    const i64 page = slot / a.c.page_size;
+    p.kv = p.rotate_ok && slot >= 0 && page < a.c.num_pages;
+    p.page = page;
+    p.off = static_cast<int>(slot - page * a.c.page_size);
+    if (report && (!p.rotate_ok || (slot >= 0 && page >= a.c.num_pages))) raise_bad_index(a.status);
+    return p;
+}
+
+__device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = bf16_lo(w[j]), f[2 * j + 1] = bf16_hi(w[j]);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+template <bool E4M3>
+__device__ __forceinline__ void store8(void* base, i64 at, const float (&f)[8], float scale) {
+    if (E4M3) {
+        *reinterpret_cast<uint2*>(static_cast<cake_e4m3*>(base) + at) =
+            make_uint2(pack4_e4m3(f[0] / scale, f[1] / scale, f[2] / scale, f[3] / scale),
+                       pack4_e4m3(f[4] / scale, f[5] / scale, f[6] / scale, f[7] / scale));
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(base) + at) = pack8(f);
+    }
+}
+
+// Block (units, heads in parallel): thread (u, y) takes unit u of the heads y, y + blockDim.y, ... of the token's
+// Hq query, Hkv key and Hkv value heads.  A unit is 8 neighbouring elements, or two such runs rot/2 apart that rotate into
+// each other (PAIRS false, the first rot/16 units of a head).
+template <bool E4M3, bool PAIRS>
+__global__ void __launch_bounds__(512)
+kv_append_kernel(const AppendArgs a) {
+    const i64 t = blockIdx.x;
+    const int u = threadIdx.x;
+    const Place p = place_of(a, t, threadIdx.x == 0 && threadIdx.y == 0);
+    if (!p.rotate_ok) return;
+    const int D = a.c.D, half = a.rot >> 1;
+    const int turning = PAIRS ? a.rot >> 3 : a.rot >> 4;              // units that rotate
+    const bool turns = u < turning;
+    const int d0 = (PAIRS || turns) ? 8 * u : a.rot + 8 * (u - turning);
+    const bool two = !PAIRS && turns;
+    float cs[8], sn[8];
+    if (turns) {
+        const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
+        constexpr int N = PAIRS ? 4 : 8;
+#pragma unroll
+        for (int j = 0; j < N; ++j) cs[j] = __ldg(row + N * u + j), sn[j] = __ldg(row + half + N * u + j);
+    }
+    const int heads = (a.q ? a.Hq : 0);
+    for (int h = threadIdx.y; h < heads + a.c.Hkv; h += blockDim.y) {
+        const bool is_q = h < heads;
+        if (!is_q && !p.kv) continue;
+        const int g = h - heads;
+        const cake_bf16* src = is_q ? a.q + t * a.q_stride + static_cast<i64>(h) * D : a.k + t * a.k_stride + static_cast<i64>(g) * D;
+        float x[8], y[8];
+        unpack8(*reinterpret_cast<const uint4*>(src + d0), x);
+        if (two) {
+            unpack8(*reinterpret_cast<const uint4*>(src + d0 + half), y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float r = x[j] * cs[j] - y[j] * sn[j];
+                y[j] = y[j] * cs[j] + x[j] * sn[j];
+                x[j] = r;
+            }
+        } else if (turns) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float r = x[2 * j] * cs[j] - x[2 * j + 1] * sn[j];
+                x[2 * j + 1] = x[2 * j + 1] * cs[j] + x[2 * j] * sn[j];
+                x[2 * j] = r;
+            }
+        }
+        if (is_q) {
+            cake_bf16* dst = a.out_q + (t * a.Hq + h) * static_cast<i64>(D) + d0;
+            *reinterpret_cast<uint4*>(dst) = pack8(x);
+            if (two) *reinterpret_cast<uint4*>(dst + half) = pack8(y);
+        } else {
+            const i64 at = p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride + d0;
+            const float sc = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + g) : 1.f;
+            store8<E4M3>(a.c.k, at, x, sc);
+            if (two) store8<E4M3>(a.c.k, at + half, y, sc);
+        }
+    }
+    if (!p.kv) return;
+    // values: plain runs of 8 over all threads of the block
+    const int runs = D >> 3;
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < a.c.Hkv * runs; i += blockDim.x * blockDim.y) {
+        const int g = i / runs, d = 8 * (i - g * runs);
+        float x[8];
+        unpack8(*reinterpret_cast<const uint4*>(a.v + t * a.v_stride + static_cast<i64>(g) * D + d), x);
+        const i64 at = p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d;
+        store8<E4M3>(a.c.v, at, x, E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + g) : 1.f);
+    }
+}
+
+// Any rot, any alignment of q, k, v: one pair of elements (or one element that does not rotate) per thread and step.
+template <bool E4M3>
+__global__ void __launch_bounds__(256)
+kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
+    const i64 t = blockIdx.x;
+    const Place p = place_of(a, t, threadIdx.x == 0);
+    if (!p.rotate_ok) return;
+    const int D = a.c.D, half = a.rot >> 1;
+    const int units = half + (D - a.rot);
+    const int hq = a.q ? a.Hq : 0;
+    auto put = [&](void* base, i64 at, float f, float sc) {
+        if (E4M3) static_cast<cake_e4m3*>(base)[at] = static_cast<cake_e4m3>(pack_e4m3(f / sc, 0.f) & 0xff);
+        else static_cast<cake_bf16*>(base)[at] = to_bf16(f);
+    };
+    for (int i = threadIdx.x; i < (hq + a.c.Hkv) * units; i += blockDim.x) {
+        const int h = i / units, u = i - h * units, g = h - hq;
+        const bool is_q = h < hq, turns = u < half;
+        if (!is_q && !p.kv) continue;
+        const cake_bf16* src = is_q ? a.q + t * a.q_stride + static_cast<i64>(h) * D : a.k + t * a.k_stride + static_cast<i64>(g) * D;
+        const int d = turns ? (pairs ? 2 * u : u) : a.rot + (u - half);
+        const int e = pairs ? d + 1 : d + half;
+        float x = bf16_f(src[d]), y = 0.f;
+        if (turns) {
+            const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
+            const float c = __ldg(row + u), s = __ldg(row + half + u);
+            const float o = bf16_f(src[e]);
+            y = o * c + x * s;
+            x = x * c - o * s;
+        }
+        if (is_q) {
+            cake_bf16* dst = a.out_q + (t * a.Hq + h) * static_cast<i64>(D);
+            dst[d] = to_bf16(x);
+            if (turns) dst[e] = to_bf16(y);
+        } else {
+            const i64 at = p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride;
+            const float sc = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + g) : 1.f;
+            put(a.c.k, at + d, x, sc);
+            if (turns) put(a.c.k, at + e, y, sc);
+        }
+    }
+    if (!p.kv) return;
+    for (int i = threadIdx.x; i < a.c.Hkv * D; i += blockDim.x) {
+        const int g = i / D, d = i - g * D;
+        const i64 at = p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d;
+        put(a.c.v, at, bf16_f(a.v[t * a.v_stride + static_cast<i64>(g) * D + d]), E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + g) : 1.f);
+    }
+}
+
+}  // namespace
+
+int check_cache(const cake_paged_cache* c) {
+    if (!c || !c->k || !c->v) return CAKE_ERR_NULL;
+    if (c->num_pages < 1 || c->page_size < 1 || c->Hkv < 1 || c->D < 1) return CAKE_ERR_SHAPE;
+    if (c->num_pages > INT_MAX || c->num_pages > LLONG_MAX / 2 / c->page_size) return CAKE_ERR_SHAPE;
+    if (c->type != CAKE_KV_BF16 && c->type != CAKE_KV_E4M3) return CAKE_ERR_UNSUPPORTED;
+    if (c->D != 64 && c->D != 96 && c->D != 128 && c->D != 256) return CAKE_ERR_UNSUPPORTED;
+    const i64 per16 = c->type == CAKE_KV_BF16 ? 8 : 16;
+    const i64 st[6] = {c->k_page_stride, c->k_token_stride, c->k_head_stride, c->v_page_stride, c->v_token_stride, c->v_head_stride};
+    for (i64 s : st) {
+        if (s < 0) return CAKE_ERR_SHAPE;
+        if (s % per16 != 0) return CAKE_ERR_ALIGN;
+    }
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return CAKE_ERR_ALIGN;
+    return CAKE_OK;
+}
+
+}  // namespace serving
+}  // namespace cake
+
+using namespace cake;
+using namespace cake::serving;
+
+extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, long long k_stride, const cake_bf16* v,
+                              long long v_stride, const cake_bf16* q, long long q_stride, int Hq, cake_bf16* out_q,
+                              const long long* slots, const int* positions, const float* cos_sin, long long max_positions, int rot,
+                              long long T, void* ws, size_t ws_bytes, cake_stream_t stream, unsigned flags) {
+    int rc = check_cache(cache);
+    if (rc != CAKE_OK) return rc;
+    const i64 kv_row = static_cast<i64>(cache->Hkv) * cache->D;
+    if (T < 0 || T > INT_MAX || rot < 0 || rot % 2 != 0 || rot > cache->D || k_stride < kv_row || v_stride < kv_row) return CAKE_ERR_SHAPE;
+    if (q && (Hq < 1 || q_stride < static_cast<i64>(Hq) * cache->D)) return CAKE_ERR_SHAPE;
+    if (rot && max_positions < 1) return CAKE_ERR_SHAPE;
+    if ((flags & ~CAKE_APPEND_INTERLEAVED) != 0) return CAKE_ERR_UNSUPPORTED;
+    if (!ws) return CAKE_ERR_NULL;
+    if (!aligned(ws, 256)) return CAKE_ERR_ALIGN;
+    if (ws_bytes < kHeaderBytes) return CAKE_ERR_WORKSPACE;
+    if (T == 0) return CAKE_OK;
+    if (!k || !v || !slots || (q && !out_q) || (rot && (!positions || !cos_sin))) return CAKE_ERR_NULL;
+    if (!aligned(k, 2) || !aligned(v, 2) || !aligned(q, 2) || !aligned(out_q, 2) || !aligned(slots, 8) || !aligned(positions, 4) || !aligned(cos_sin, 4))
+        return CAKE_ERR_ALIGN;
+    DeviceInfo di;
+    rc = current_device_info(&di);
+    if (rc != CAKE_OK) return rc;
+    if (di.cc_major != 10) return CAKE_ERR_DEVICE;
+    AppendArgs a;
+    a.c = *cache, a.k = k, a.v = v, a.q = q, a.out_q = out_q, a.slots = slots, a.positions = positions, a.cos_sin = cos_sin;
+    a.k_stride = k_stride, a.v_stride = v_stride, a.q_stride = q_stride, a.max_positions = max_positions, a.T = T, a.Hq = Hq, a.rot = rot;
+    a.status = static_cast<int*>(ws);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const bool pairs = flags & CAKE_APPEND_INTERLEAVED;
+    const bool e4m3 = cache->type == CAKE_KV_E4M3;
+    const int D = cache->D;
+    const bool wide = (pairs ? rot % 8 == 0 : rot % 16 == 0) && k_stride % 8 == 0 && v_stride % 8 == 0 && aligned(k, 16) && aligned(v, 16) &&
+                      (!q || (q_stride % 8 == 0 && aligned(q, 16) && aligned(out_q, 16)));
+    const unsigned blocks = static_cast<unsigned>(T);
+    if (wide) {
+        const int units = pairs ? D / 8 : rot / 16 + (D - rot) / 8;
+        const int heads = (q ? Hq : 0) + cache->Hkv;
+        const int par = heads * units <= 256 ? heads : (256 + units - 1) / units;
+        const dim3 block(units, par);
+        if (e4m3) {
+            if (pairs) kv_append_kernel<true, true><<<blocks, block, 0, s>>>(a);
+            else kv_append_kernel<true, false><<<blocks, block, 0, s>>>(a);
+        } else {
+            if (pairs) kv_append_kernel<false, true><<<blocks, block, 0, s>>>(a);
+            else kv_append_kernel<false, false><<<blocks, block, 0, s>>>(a);
+        }
+    } else if (e4m3) {
+        kv_append_scalar_kernel<true><<<blocks, 256, 0, s>>>(a, pairs);
+    } else {
+        kv_append_scalar_kernel<false><<<blocks, 256, 0, s>>>(a, pairs);
+    }
+    note_launches(1);
+    return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+}

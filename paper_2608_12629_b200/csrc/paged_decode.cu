@@ -1,0 +1,660 @@
+// Attention of one new token per sequence over a paged cache, split over the cache's length and joined, in one launch.
+//
+//   out = sum_t exp(x_t - m) v_t / sum_t exp(x_t - m),   x_t = scale * q . k_t,   m = max_t x_t
+//
+// One pass over the keys and values with the running maximum m, sum l and weighted sum O of a softmax; parts (m, l, O) of
+// the same row join by  m = max m_i,  l = sum l_i e^(m_i - m),  O = sum O_i e^(m_i - m).  Bound by memory: every key and
+// value is read once, so everything here serves to keep loads in flight.
+//
+// Work is the list of 64-key tiles of all (sequence, key-value head) entries, one after the other; CTA c of n takes tiles
+// [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined by the last of
+// them to arrive, from parts in the workspace, in the order of the CTAs.
+//
+// A warp works on 16 keys at a time, with no barrier between warps: every lane copies (cp.async) exactly the bytes that it
+// will itself feed to the matrix instructions, so its ring in shared memory is a private queue, laid out lane by lane.
+//   scores:  S^T[key][head] = K Q^T   (m16n8k16: 16 keys x 8 heads; the contraction's order of elements is permuted the same way
+//            in both operands so that a lane's 16-byte run of a key feeds whole k-steps)
+//   output:  O^T[d][head] += V^T P    (16 values of d x 8 heads x 16 keys; V^T is formed from four keys' runs by byte
+//            permutes, P's operand from S^T's accumulators by an 8x8 transpose between lanes)
+// Query heads that share a key-value head sit side by side in the 8 (or 16) columns, so the group costs one read.
+#include "ptx.cuh"
+#include "serving.cuh"
+
+namespace cake {
+namespace serving {
+
+int check_cache(const cake_paged_cache* c);   // kv_append.cu
+
+namespace {
+
+constexpr int WARPS = 4;
+constexpr int THREADS = WARPS * 32;
+constexpr int KEYS = 16;                 // keys of a warp's step
+constexpr int TILE = WARPS * KEYS;       // keys of a CTA's tile
+constexpr int kPartCtas = 1024;          // CTAs that the workspace has room for parts of (two each)
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr float NEG_INF = -INFINITY;
+
+struct DecodeArgs {
+    cake_paged_cache c;
+    const cake_bf16* q;
+    const int* table;
+    const int* lens;
+    cake_bf16* out;
+    float* lse;
+    int* status;
+    int* counters;
+    float* parts;
+    i64 q_stride, q_head_stride, table_stride, table_head_stride, lens_stride, lens_head_stride;
+    int B, Hq, G, chunks, max_pages, window;   // chunks: runs of at most 8 * NT query heads of a key-value head
+    float scale;
+};
+
+template <int D, bool E4M3>
+struct Layout {
+    static constexpr int ELEM = E4M3 ? 1 : 2;
+    static constexpr int ROW = D * ELEM;                                            // bytes of a key
+    // bytes a lane copies at a time: four lanes share a key's row, eight lanes a value's row
+    static constexpr int VK = ROW % 64 == 0 ? 16 : 8;
+    static constexpr int VV = ROW % 128 == 0 ? 16 : (ROW % 64 == 0 ? 8 : 4);
+    static constexpr int CK = ROW / (4 * VK);                                       // runs of a lane per key
+    static constexpr int CV = ROW / (8 * VV);                                       // runs of a lane per value
+    static constexpr int K_BYTES = 2 * CK * VK * 32;                                // a warp's stage: 2 keys per lane
+    static constexpr int V_BYTES = 4 * CV * VV * 32;                                // 4 values per lane
+    static constexpr int STAGE = K_BYTES + V_BYTES;
+    static_assert(STAGE == 2 * KEYS * ROW, "a stage holds 16 keys and 16 values");
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(ok ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
+    if (N == 16) cp_async16(dst, src, ok);
+    else if (N == 8) cp_async8(dst, src, ok);
+    else cp_async4(dst, src, ok);
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <int N>
+__device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[N / 4]) {
+    if constexpr (N == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+    else if constexpr (N == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+}
+
+template <bool F16>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const uint32_t b0, const uint32_t b1) {
+    if (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// four e4m3 values to two pairs of f16: exact
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    const uint16_t a = static_cast<uint16_t>(w & 0xffffu), b = static_cast<uint16_t>(w >> 16);
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"(a));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(b));
+}
+
+// tokens of sequence b and key-value head g that are attended to: [first, first + count)
+__device__ __forceinline__ void span_of(const DecodeArgs& a, int b, int g, int& first, int& count, bool& cut) {
+    const i64 room = static_cast<i64>(a.max_pages) * a.c.page_size;
+    i64 n = a.lens[b * a.lens_stride + g * a.lens_head_stride];
+    cut = n > room;
+    if (cut) n = room;
+    if (n < 0) n = 0;
+    const i64 w = (a.window > 0 && a.window < n) ? a.window : n;
+    first = static_cast<int>(n - w);
+    count = static_cast<int>(w);
+}
+__device__ __forceinline__ int tiles_of(int count) { return count > 0 ? (count - 1) / TILE + 1 : 1; }   // an empty row still has to be written
+
+// The work list: entries in the order (sequence, key-value head, run of query heads), each of tiles_of(its tokens) tiles.
+struct Cursor {
+    int b, g, run, first, count, tiles;
+    i64 start;        // number of the entry's first tile in the list
+};
+
+template <int D, bool E4M3, int NT, int STAGES>
+__global__ void __launch_bounds__(THREADS)
+paged_decode_kernel(const DecodeArgs a) {
+    using L = Layout<D, E4M3>;
+    constexpr int HEADS = 8 * NT;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ i64 scan[WARPS];
+    __shared__ i64 found_start;
+    __shared__ int found_b;
+    __shared__ float wm[WARPS][HEADS], wl[WARPS][HEADS];
+    __shared__ int last_flag;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
+    const int Hkv = a.c.Hkv;
+    const bool shared_lens = a.lens_head_stride == 0;
+
+    // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
+    const int per = (a.B + THREADS - 1) / THREADS;
+    auto tiles_of_sequence = [&](int b) -> i64 {
+        i64 n = 0;
+        int first, count;
+        bool cut;
+        if (shared_lens) {
+            span_of(a, b, 0, first, count, cut);
+            n = static_cast<i64>(tiles_of(count)) * Hkv;
+        } else {
+            for (int g = 0; g < Hkv; ++g) {
+                span_of(a, b, g, first, count, cut);
+                n += tiles_of(count);
+            }
+        }
+        return n * a.chunks;
+    };
+    i64 mine = 0;
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) mine += tiles_of_sequence(b);
+    i64 before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const i64 u = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += u;
+    }
+    if (lane == 31) scan[warp] = before;
+    __syncthreads();
+    i64 total = 0;
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) before += scan[w];
+        total += scan[w];
+    }
+    before -= mine;
+    const i64 n_ctas = min(static_cast<i64>(gridDim.x), total);     // no CTA without a tile between two of an entry's
+    const i64 cta = blockIdx.x;
+    if (cta >= n_ctas) return;
+    const i64 lo = cta * total / n_ctas, hi = (cta + 1) * total / n_ctas;
+    if (before <= lo && lo < before + mine) {
+        i64 at = before;
+        int b = tid * per;
+        for (;; ++b) {
+            const i64 n = tiles_of_sequence(b);
+            if (lo < at + n) break;
+            at += n;
+        }
+        found_b = b;
+        found_start = at;
+    }
+    __syncthreads();
+    Cursor e;
+    e.b = found_b, e.g = 0, e.run = 0, e.start = found_start;
+    bool cut;
+    auto look = [&]() {
+        span_of(a, e.b, e.g, e.first, e.count, cut);
+        e.tiles = tiles_of(e.count);
+        if (cut && tid == 0) raise_bad_index(a.status);
+    };
+    auto next = [&]() {
+        e.start += e.tiles;
+        if (++e.run == a.chunks) {
+            e.run = 0;
+            if (++e.g == Hkv) e.g = 0, ++e.b;
+        }
+    };
+    look();
+    while (e.start + e.tiles <= lo) next(), look();
+
+    const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * L::STAGE;
+    bool first_segment = true;
+    for (i64 at = lo; at < hi;) {
+        const int tile0 = static_cast<int>(at - e.start);
+        const int n_tiles = static_cast<int>(min(hi - at, static_cast<i64>(e.tiles - tile0)));
+        const int heads = min(HEADS, a.G - e.run * HEADS);        // query heads of this run
+        const int h0 = e.g * a.G + e.run * HEADS;
+        const int* table = a.table + e.b * a.table_stride + e.g * a.table_head_stride;
+
+        // ---- queries: operand b of the score product, lane (head g8, element runs of t4), and their factor
+        uint32_t qf[NT][L::CK * L::VK / L::ELEM / 4][2];
+        float factor[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            constexpr int EL = L::VK / L::ELEM;      // elements of a run
+            const int h = n * 8 + g8;
+            const cake_bf16* src = a.q + e.b * a.q_stride + (h0 + h) * a.q_head_stride;
+            float most = 0.f;
+            float f[L::CK][EL];
+#pragma unroll
+            for (int c = 0; c < L::CK; ++c)
+#pragma unroll
+                for (int j = 0; j < EL; ++j) {
+                    f[c][j] = h < heads ? bf16_f(src[(t4 + 4 * c) * EL + j]) : 0.f;
+                    most = fmaxf(most, fabsf(f[c][j]));
+                }
+            // 8-bit keys are widened to f16 (exact), so the query is too: divided by a power of two that leaves its largest
+            // element in [1, 2), which keeps 11 bits where bf16 has 8; what underflows is below 2^-24 of the largest
+            float unit = 1.f;
+            if (E4M3) {
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                const uint32_t ex = __float_as_uint(most) & 0x7f800000u;
+                if (ex > (2u << 23) && ex < (252u << 23)) unit = __uint_as_float(ex);
+                const float down = __uint_as_float((254u << 23) - __float_as_uint(unit));
+#pragma unroll
+                for (int c = 0; c < L::CK; ++c)
+#pragma unroll
+                    for (int j = 0; j < EL; ++j) f[c][j] *= down;
+            }
+#pragma unroll
+            for (int c = 0; c < L::CK; ++c)
+#pragma unroll
+                for (int j = 0; j < EL / 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        qf[n][c * (EL / 4) + j][i] = E4M3 ? pack_f16(f[c][4 * j + 2 * i], f[c][4 * j + 2 * i + 1])
+                                                          : pack_bf16(f[c][4 * j + 2 * i], f[c][4 * j + 2 * i + 1]);
+            const float ks = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + e.g) : 1.f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                factor[n][i] = a.scale * LOG2E * ks * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
+        }
+
+        // ---- loads: lanes 0-15 look up the pages of the step's keys, every lane copies its own runs
+        const int end = e.first + e.count;
+        const int key0 = e.first + tile0 * TILE + warp * KEYS;     // the warp's first key of the segment
+        auto page_at = [&](int step) -> int {                      // the table entry of key (lane) of a step; -1: no such key
+            const int key = key0 + step * TILE + (lane & 15);
+            return (step < n_tiles && key < end) ? __ldg(table + static_cast<unsigned>(key) / static_cast<unsigned>(a.c.page_size)) : -1;
+        };
+        auto copy = [&](int step, int entry) -> uint32_t {         // returns the step's mask of keys that are there
+            const int key = key0 + step * TILE + (lane & 15);
+            const bool asked = step < n_tiles && key < end;
+            const bool there = asked && entry >= 0 && entry < a.c.num_pages;
+            if (asked && !there) raise_bad_index(a.status);
+            const int off = static_cast<unsigned>(key) % static_cast<unsigned>(a.c.page_size);
+            const uint32_t mask = __ballot_sync(0xffffffffu, there) & 0xffffu;
+            const uint32_t stage = ring + (step % STAGES) * L::STAGE;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int kk = g8 + 8 * r;
+                const i64 p = __shfl_sync(0xffffffffu, entry, kk);
+                const i64 o = __shfl_sync(0xffffffffu, off, kk);
+                const bool ok = (mask >> kk) & 1;
+                const uint8_t* src = static_cast<const uint8_t*>(a.c.k) +
+                                     (ok ? (p * a.c.k_page_stride + o * a.c.k_token_stride + e.g * a.c.k_head_stride) * L::ELEM : 0) + t4 * L::VK;
+#pragma unroll
+                for (int c = 0; c < L::CK; ++c)
+                    cp_async<L::VK>(stage + ((r * L::CK + c) * 32 + lane) * L::VK, src + c * 4 * L::VK, ok);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int kk = 2 * t4 + (r & 1) + 8 * (r >> 1);
+                const i64 p = __shfl_sync(0xffffffffu, entry, kk);
+                const i64 o = __shfl_sync(0xffffffffu, off, kk);
+                const bool ok = (mask >> kk) & 1;
+                const uint8_t* src = static_cast<const uint8_t*>(a.c.v) +
+                                     (ok ? (p * a.c.v_page_stride + o * a.c.v_token_stride + e.g * a.c.v_head_stride) * L::ELEM : 0) + g8 * L::VV;
+#pragma unroll
+                for (int c = 0; c < L::CV; ++c)
+                    cp_async<L::VV>(stage + L::K_BYTES + ((r * L::CV + c) * 32 + lane) * L::VV,
+                                    src + c * 8 * L::VV, ok);
+            }
+            return mask;
+        };
+
+        float o[D / 16][NT][4];      // O^T: per 16 values of d, (d, head 2t4), (d, head 2t4+1), (d', ...), (d', ...)
+        float m[NT][2], l[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) m[n][i] = NEG_INF, l[n][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[j][n][i] = 0.f;
+        }
+        uint32_t masks[STAGES];
+        int entry = page_at(0);
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) {
+            const int following = page_at(s + 1);
+            masks[s] = copy(s, entry);
+            cp_commit();
+            entry = following;
+        }
+        masks[STAGES - 1] = 0;
+        for (int step = 0; step < n_tiles; ++step) {
+            const int following = page_at(step + STAGES);
+            const uint32_t coming = copy(step + STAGES - 1, entry);
+            cp_commit();
+            entry = following;
+            cp_wait<STAGES - 1>();
+            const uint32_t mask = masks[0];
+#pragma unroll
+            for (int s = 0; s + 1 < STAGES - 1; ++s) masks[s] = masks[s + 1];
+            masks[STAGES - 2] = coming;
+            if (mask == 0) continue;
+            const uint32_t stage = ring + (step % STAGES) * L::STAGE;
+
+            // ---- scores of 16 keys
+            float x[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < L::CK; ++c) {
+                uint32_t k0[L::VK / 4], k1[L::VK / 4];
+                lds<L::VK>(stage + (c * 32 + lane) * L::VK, k0);
+                lds<L::VK>(stage + ((L::CK + c) * 32 + lane) * L::VK, k1);
+                if (E4M3) {
+#pragma unroll
+                    for (int j = 0; j < L::VK / 4; ++j) {
+                        uint32_t f[4];
+                        e4m3_to_f16(k0[j], f[0], f[2]);
+                        e4m3_to_f16(k1[j], f[1], f[3]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma<true>(x[n], f, qf[n][c * (L::VK / 4) + j][0], qf[n][c * (L::VK / 4) + j][1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < L::VK / 8; ++j) {
+                        const uint32_t f[4] = {k0[2 * j], k1[2 * j], k0[2 * j + 1], k1[2 * j + 1]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma<false>(x[n], f, qf[n][c * (L::VK / 8) + j][0], qf[n][c * (L::VK / 8) + j][1]);
+                    }
+                }
+            }
+
+            // ---- running maximum and sum; p in [0, 1]
+            uint32_t ph[NT][2], pl[NT][2];
+            const bool ok0 = (mask >> g8) & 1, ok1 = (mask >> (g8 + 8)) & 1;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float p[4], keep[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    p[i] = ok0 ? x[n][i] * factor[n][i] : NEG_INF;
+                    p[2 + i] = ok1 ? x[n][2 + i] * factor[n][i] : NEG_INF;
+                    float top = fmaxf(p[i], p[2 + i]);
+#pragma unroll
+                    for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+                    top = fmaxf(m[n][i], top);
+                    const float base = top == NEG_INF ? 0.f : top;   // every score so far is -inf: they all weigh nothing
+                    keep[i] = exp2f(m[n][i] - base);
+                    m[n][i] = top;
+                    p[i] = exp2f(p[i] - base);
+                    p[2 + i] = exp2f(p[2 + i] - base);
+                    l[n][i] = l[n][i] * keep[i] + (p[i] + p[2 + i]);
+                }
+                if (E4M3) {
+                    // f16 holds 11 bits of p: its rounding is an eighth of the output's
+                    ph[n][0] = transpose8x8(pack_f16(p[0], p[1]));
+                    ph[n][1] = transpose8x8(pack_f16(p[2], p[3]));
+                } else {
+                    // p as the sum of two bf16, so that its rounding (2^-8 in one of them) does not add to the output's own
+                    const uint32_t a0 = pack_bf16(p[0], p[1]), a1 = pack_bf16(p[2], p[3]);
+                    pl[n][0] = transpose8x8(pack_bf16(p[0] - bf16_lo(a0), p[1] - bf16_hi(a0)));
+                    pl[n][1] = transpose8x8(pack_bf16(p[2] - bf16_lo(a1), p[3] - bf16_hi(a1)));
+                    ph[n][0] = transpose8x8(a0);
+                    ph[n][1] = transpose8x8(a1);
+                }
+                if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        o[j][n][0] *= keep[0], o[j][n][1] *= keep[1];
+                        o[j][n][2] *= keep[0], o[j][n][3] *= keep[1];
+                    }
+                }
+            }
+
+            // ---- weighted sum of 16 values
+#pragma unroll
+            for (int c = 0; c < L::CV; ++c) {
+                uint32_t v[4][L::VV / 4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) lds<L::VV>(stage + L::K_BYTES + ((r * L::CV + c) * 32 + lane) * L::VV, v[r]);
+#pragma unroll
+                for (int j = 0; j < L::VV / 4; ++j) {
+                    if (E4M3) {
+                        uint32_t w[4][2];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) e4m3_to_f16(v[r][j], w[r][0], w[r][1]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t f[4] = {__byte_perm(w[0][i], w[1][i], 0x5410), __byte_perm(w[0][i], w[1][i], 0x7632),
+                                                   __byte_perm(w[2][i], w[3][i], 0x5410), __byte_perm(w[2][i], w[3][i], 0x7632)};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma<true>(o[(c * (L::VV / 4) + j) * 2 + i][n], f, ph[n][0], ph[n][1]);
+                        }
+                    } else {
+                        const uint32_t f[4] = {__byte_perm(v[0][j], v[1][j], 0x5410), __byte_perm(v[0][j], v[1][j], 0x7632),
+                                               __byte_perm(v[2][j], v[3][j], 0x5410), __byte_perm(v[2][j], v[3][j], 0x7632)};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma<false>(o[c * (L::VV / 4) + j][n], f, ph[n][0], ph[n][1]);
+                            mma<false>(o[c * (L::VV / 4) + j][n], f, pl[n][0], pl[n][1]);
+                        }
+                    }
+                }
+            }
+        }
+        cp_wait<0>();
+
+        // ---- the warps' parts: maxima and sums first, then the weighted sums through the ring's memory
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int s = 4; s < 32; s <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], s);
+                if (g8 == 0) wm[warp][n * 8 + 2 * t4 + i] = m[n][i], wl[warp][n * 8 + 2 * t4 + i] = l[n][i];
+            }
+        __syncthreads();             // (also: every warp has drained its ring)
+        float* const osum = reinterpret_cast<float*>(smem);      // [WARPS][HEADS][D]
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int h = n * 8 + 2 * t4 + i;
+                float top = NEG_INF;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) top = fmaxf(top, wm[w][h]);
+                const float f = exp2f(m[n][i] - (top == NEG_INF ? 0.f : top));
+                float* dst = osum + (warp * HEADS + h) * D;
+                constexpr int EV = L::VV / L::ELEM;       // neighbouring values of d of a lane
+#pragma unroll
+                for (int c = 0; c < L::CV; ++c)
+#pragma unroll
+                    for (int j = 0; j < EV / 2; ++j) {
+                        const int d = (g8 + 8 * c) * EV + 2 * j;
+                        dst[d] = o[c * (EV / 2) + j][n][i] * f;
+                        dst[d + 1] = o[c * (EV / 2) + j][n][2 + i] * f;
+                    }
+            }
+        __syncthreads();
+        const bool whole = tile0 == 0 && n_tiles == e.tiles;
+        constexpr int PART = HEADS * (D + 2);            // floats of a part: m, l, then O, all of the run's heads
+        float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
+        const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
+        const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
+        for (int i = tid; i < heads * D; i += THREADS) {
+            const int h = i / D, d = i - h * D;
+            float top = NEG_INF;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) top = fmaxf(top, wm[w][h]);
+            const float base = top == NEG_INF ? 0.f : top;
+            float sum = 0.f, acc = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                sum += wl[w][h] * exp2f(wm[w][h] - base);
+                acc += osum[(w * HEADS + h) * D + d];
+            }
+            if (whole) {
+                a.out[(out0 + h) * D + d] = to_bf16(sum == 0.f ? 0.f : acc / sum * vs);     // no token weighs anything: zeros
+                if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
+            } else {
+                part[2 * HEADS + h * D + d] = acc;
+                if (d == 0) part[h] = top, part[HEADS + h] = sum;
+            }
+        }
+        if (!whole) {
+            // ---- the entry's CTAs are neighbours; the last to arrive joins their parts in order
+            const i64 s0 = e.start, s1 = e.start + e.tiles - 1;
+            const i64 c0 = ((s0 + 1) * n_ctas - 1) / total, c1 = ((s1 + 1) * n_ctas - 1) / total;
+            __syncthreads();
+            if (tid == 0) {
+                __threadfence();
+                const int before_me = atomicAdd(a.counters + c0, 1);
+                last_flag = before_me == static_cast<int>(c1 - c0);
+                if (last_flag) a.counters[c0] = 0;       // ready for the next call
+                __threadfence();
+            }
+            __syncthreads();
+            if (last_flag) {
+                for (int i = tid; i < heads * D; i += THREADS) {
+                    const int h = i / D, d = i - h * D;
+                    float top = NEG_INF, sum = 0.f, acc = 0.f;
+                    for (i64 c = c0; c <= c1; ++c) {
+                        const float* p = a.parts + (2 * c + (c * total / n_ctas >= s0 ? 0 : 1)) * static_cast<i64>(PART);
+                        const float mi = __ldcg(p + h), li = __ldcg(p + HEADS + h), oi = __ldcg(p + 2 * HEADS + h * D + d);
+                        const float up = fmaxf(top, mi);
+                        const float base = up == NEG_INF ? 0.f : up;
+                        const float f0 = exp2f(top - base), f1 = exp2f(mi - base);
+                        sum = sum * f0 + li * f1;
+                        acc = acc * f0 + oi * f1;
+                        top = up;
+                    }
+                    a.out[(out0 + h) * D + d] = to_bf16(sum == 0.f ? 0.f : acc / sum * vs);
+                    if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
+                }
+            }
+        }
+        __syncthreads();             // the ring's memory, wm and wl are free again
+        first_segment = false;
+        at += n_tiles;
+        if (at < hi) next(), look();
+    }
+}
+
+struct Shape {
+    int nt, chunks;
+};
+Shape shape_of(int Hq, int Hkv) {
+    const int G = Hq / Hkv;
+    Shape s;
+    s.nt = G <= 8 ? 1 : 2;
+    s.chunks = (G + 8 * s.nt - 1) / (8 * s.nt);
+    return s;
+}
+
+template <int D, bool E4M3, int NT>
+int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
+    using L = Layout<D, E4M3>;
+    constexpr int RING1 = WARPS * L::STAGE;
+    constexpr int STAGES = RING1 * 3 > 100 * 1024 ? 3 : (RING1 * 6 <= 100 * 1024 ? 6 : 100 * 1024 / RING1);
+    constexpr int RING = RING1 * STAGES;
+    constexpr int MERGE = WARPS * 8 * NT * D * 4;
+    constexpr int SMEM = RING > MERGE ? RING : MERGE;
+    static bool set[64] = {};
+    auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES>;
+    if (di.device < 0 || di.device >= 64 || !set[di.device]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
+        if (di.device >= 0 && di.device < 64) set[di.device] = true;
+    }
+    const int per_sm = SMEM > 110 * 1024 ? 1 : 2;
+    const int ctas = min(di.sm_count * per_sm, kPartCtas);
+    kernel<<<ctas, THREADS, SMEM, s>>>(a);
+    note_launches(1);
+    return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+}
+
+template <int D>
+int launch_d(const DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_t s) {
+    if (e4m3) return nt == 1 ? launch<D, true, 1>(a, di, s) : launch<D, true, 2>(a, di, s);
+    return nt == 1 ? launch<D, false, 1>(a, di, s) : launch<D, false, 2>(a, di, s);
+}
+
+int check_heads(long long B, int Hq, int Hkv, int D) {
+    if (B < 0 || B > INT_MAX / 2 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return CAKE_ERR_SHAPE;
+    if (D != 64 && D != 96 && D != 128 && D != 256) return CAKE_ERR_UNSUPPORTED;
+    return CAKE_OK;
+}
+size_t workspace_bytes(int Hq, int Hkv, int D) {
+    const Shape sh = shape_of(Hq, Hkv);
+    return round_up(static_cast<i64>(kHeaderBytes + sizeof(float) * 2 * kPartCtas * 8 * sh.nt * (D + 2)), 256);
+}
+
+}  // namespace
+}  // namespace serving
+}  // namespace cake
+
+using namespace cake;
+using namespace cake::serving;
+
+extern "C" {
+
+int cake_paged_decode_workspace_bytes(long long B, int Hq, int Hkv, int D, size_t* out_bytes) {
+    if (!out_bytes) return CAKE_ERR_NULL;
+    const int rc = check_heads(B, Hq, Hkv, D);
+    if (rc != CAKE_OK) return rc;
+    *out_bytes = workspace_bytes(Hq, Hkv, D);
+    return CAKE_OK;
+}
+
+int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_paged_cache* cache,
+                      const int* page_table, long long table_stride, long long table_head_stride, int max_pages,
+                      const int* seq_lens, long long lens_stride, long long lens_head_stride, long long B, int Hq, float scale,
+                      int window, cake_bf16* out, float* out_lse, void* ws, size_t ws_bytes, cake_stream_t stream) {
+    int rc = check_cache(cache);
+    if (rc != CAKE_OK) return rc;
+    rc = check_heads(B, Hq, cache->Hkv, cache->D);
+    if (rc != CAKE_OK) return rc;
+    if (max_pages < 0 || static_cast<i64>(max_pages) * cache->page_size > INT_MAX - 16 * TILE || window < 0) return CAKE_ERR_SHAPE;
+    if (table_stride < 0 || table_head_stride < 0 || lens_stride < 0 || lens_head_stride < 0 || q_stride < 0 || q_head_stride < 0)
+        return CAKE_ERR_SHAPE;
+    if (!ws) return CAKE_ERR_NULL;
+    if (!aligned(ws, 256)) return CAKE_ERR_ALIGN;
+    if (ws_bytes < workspace_bytes(Hq, cache->Hkv, cache->D)) return CAKE_ERR_WORKSPACE;
+    if (B == 0) return CAKE_OK;
+    if (!q || !seq_lens || !out || (max_pages > 0 && !page_table)) return CAKE_ERR_NULL;
+    if (!aligned(q, 2) || !aligned(out, 2) || !aligned(out_lse, 4) || !aligned(page_table, 4) || !aligned(seq_lens, 4)) return CAKE_ERR_ALIGN;
+    DeviceInfo di;
+    rc = current_device_info(&di);
+    if (rc != CAKE_OK) return rc;
+    if (di.cc_major != 10) return CAKE_ERR_DEVICE;
+    const Shape sh = shape_of(Hq, cache->Hkv);
+    DecodeArgs a;
+    a.c = *cache, a.q = q, a.table = page_table, a.lens = seq_lens, a.out = out, a.lse = out_lse;
+    a.status = static_cast<int*>(ws);
+    a.counters = static_cast<int*>(ws) + 64;
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes);
+    a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.table_stride = table_stride, a.table_head_stride = table_head_stride;
+    a.lens_stride = lens_stride, a.lens_head_stride = lens_head_stride;
+    a.B = static_cast<int>(B), a.Hq = Hq, a.G = Hq / cache->Hkv, a.chunks = sh.chunks, a.max_pages = max_pages, a.window = window;
+    a.scale = scale;
+    const bool e4m3 = cache->type == CAKE_KV_E4M3;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    switch (cache->D) {
+        case 64: return launch_d<64>(a, e4m3, sh.nt, di, s);
+        case 96: return launch_d<96>(a, e4m3, sh.nt, di, s);
+        case 128: return launch_d<128>(a, e4m3, sh.nt, di, s);
+        default: return launch_d<256>(a, e4m3, sh.nt, di, s);
+    }
+}
+
+}  // extern "C"

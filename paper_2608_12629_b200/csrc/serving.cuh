@@ -1,0 +1,45 @@
+// What the serving operators share: bf16 / e4m3 conversions, workspace header, host-side checks.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <limits.h>
+
+#include "../../include/cake_serving.h"
+#include "internal.h"
+
+namespace cake {
+namespace serving {
+
+constexpr float kE4M3Max = 448.0f;
+constexpr float kScaleMin = 7.888609052210118e-31f;   // 2^-100: the scale of a group of zeros; its reciprocal is finite
+
+// Workspace header: 64 status words (word 0 is the sticky status), then arrival counters, one per CTA that can be the first
+// of several to work on one output.  They are zero between calls, whatever sizes the calls have.
+constexpr int kMaxCtas = 4096;
+constexpr size_t kHeaderBytes = 256 + kMaxCtas * 4;
+static_assert(kHeaderBytes == CAKE_SERVING_HEADER_BYTES, "header and ABI constant agree");
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ float bf16_f(cake_bf16 v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // round to nearest even
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ cake_bf16 to_bf16(float v) { return static_cast<cake_bf16>(pack_bf16(v, 0.f) & 0xffffu); }
+// two floats to e4m3, nearest even, values beyond 448 become 448, NaN stays NaN
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+    uint16_t d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
+    return pack_e4m3(a, b) | (pack_e4m3(c, d) << 16);
+}
+__device__ __forceinline__ void raise_bad_index(int* status) { atomicCAS(status, CAKE_OK, CAKE_ERR_BAD_INDEX); }
+
+}  // namespace serving
+}  // namespace cake
