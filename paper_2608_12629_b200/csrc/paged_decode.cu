@@ -10,12 +10,13 @@
 // [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined by the last of
 // them to arrive, from parts in the workspace, in the order of the CTAs.
 //
-// A warp works on 16 keys at a time, with no barrier between warps: every lane copies (cp.async) exactly the bytes that it
-// will itself feed to the matrix instructions, so its ring in shared memory is a private queue, laid out lane by lane.
+// A warp works on 16 keys at a time, with a ring of its own in shared memory and no barrier between warps.  One instruction
+// of the warp fetches a step: each lane copies one row (bulk copy; lanes 0-15 the keys, 16-31 the values) to a pitch at which
+// the reads below meet no bank twice.
 //   scores:  S^T[key][head] = K Q^T   (m16n8k16: 16 keys x 8 heads; the contraction's order of elements is permuted the same way
 //            in both operands so that a lane's 16-byte run of a key feeds whole k-steps)
-//   output:  O^T[d][head] += V^T P    (16 values of d x 8 heads x 16 keys; V^T is formed from four keys' runs by byte
-//            permutes, P's operand from S^T's accumulators by an 8x8 transpose between lanes)
+//   output:  O^T[d][head] += V^T P    (16 values of d x 8 heads x 16 keys; V^T by transposing matrix loads, P's operand from
+//            S^T's accumulators by an 8x8 transpose between lanes)
 // Query heads that share a key-value head sit side by side in the 8 (or 16) columns, so the group costs one read.
 #include "ptx.cuh"
 #include "serving.cuh"
@@ -35,6 +36,8 @@ constexpr int kPartCtas = 1024;          // CTAs that the workspace has room for
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
+constexpr float SLACK = 8.f;
+constexpr int WAIT_TRIES = 100000;       // of 20 us each
 
 struct DecodeArgs {
     cake_paged_cache c;
@@ -47,6 +50,7 @@ struct DecodeArgs {
     int* counters;
     float* parts;
     i64 q_stride, q_head_stride, table_stride, table_head_stride, lens_stride, lens_head_stride;
+    bool q_wide, out_wide;           // 16-byte loads of q, 8-byte stores of out
     int B, Hq, G, chunks, max_pages, window;   // chunks: runs of at most 8 * NT query heads of a key-value head
     float scale;
 };
@@ -55,35 +59,15 @@ template <int D, bool E4M3>
 struct Layout {
     static constexpr int ELEM = E4M3 ? 1 : 2;
     static constexpr int ROW = D * ELEM;                                            // bytes of a key
-    // bytes a lane copies at a time: four lanes share a key's row, eight lanes a value's row
+    // a key's row is read in runs of VK bytes by four lanes, eight rows at a time: 8 rows apart by 64 (32) bytes modulo 128
     static constexpr int VK = ROW % 64 == 0 ? 16 : 8;
-    static constexpr int VV = ROW % 128 == 0 ? 16 : (ROW % 64 == 0 ? 8 : 4);
     static constexpr int CK = ROW / (4 * VK);                                       // runs of a lane per key
-    static constexpr int CV = ROW / (8 * VV);                                       // runs of a lane per value
-    static constexpr int K_BYTES = 2 * CK * VK * 32;                                // a warp's stage: 2 keys per lane
-    static constexpr int V_BYTES = 4 * CV * VV * 32;                                // 4 values per lane
-    static constexpr int STAGE = K_BYTES + V_BYTES;
-    static_assert(STAGE == 2 * KEYS * ROW, "a stage holds 16 keys and 16 values");
+    static constexpr int K_PITCH = VK == 16 ? (ROW % 128 == 64 ? ROW : ROW + 64) : (ROW / 128 * 128 + 160);
+    // a value's row is read 16 bytes at a time, eight rows at once: an odd number of 16-byte units apart
+    static constexpr int V_PITCH = (ROW / 16) % 2 == 1 ? ROW : ROW + 16;
+    static constexpr int K_BYTES = KEYS * K_PITCH;
+    static constexpr int STAGE = KEYS * (K_PITCH + V_PITCH);                        // of a warp
 };
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool ok) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(ok ? 8 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool ok) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
-    if (N == 16) cp_async16(dst, src, ok);
-    else if (N == 8) cp_async8(dst, src, ok);
-    else cp_async4(dst, src, ok);
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <int N>
 __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[N / 4]) {
@@ -101,6 +85,11 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flushed to zero
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
@@ -110,6 +99,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t d;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
+}
+// four 8x8 matrices of 16-bit elements, each transposed; lane i gives the address of row i % 8 of matrix i / 8
+__device__ __forceinline__ void ldmatrix_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 // four e4m3 values to two pairs of f16: exact
 __device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -148,9 +141,14 @@ paged_decode_kernel(const DecodeArgs a) {
     __shared__ int found_b;
     __shared__ float wm[WARPS][HEADS], wl[WARPS][HEADS];
     __shared__ int last_flag;
+    __shared__ uint64_t bars[WARPS][STAGES];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
     const int Hkv = a.c.Hkv;
     const bool shared_lens = a.lens_head_stride == 0;
+    if (lane == 0) {
+        for (int s = 0; s < STAGES; ++s) ptx::mbar_init(ptx::smem_u32(&bars[warp][s]), 1);
+        ptx::fence_mbar_init();
+    }
 
     // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
     const int per = (a.B + THREADS - 1) / THREADS;
@@ -219,7 +217,20 @@ paged_decode_kernel(const DecodeArgs a) {
     look();
     while (e.start + e.tiles <= lo) next(), look();
 
+    // ---- the warp's ring
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * L::STAGE;
+    const uint32_t bar0 = ptx::smem_u32(&bars[warp][0]);
+    uint32_t phases = 0;             // bit s: parity of the next completion of stage s
+    bool dead = false;               // a wait has expired: no more copies, no more waits
+    const int row = lane & 15;
+    const bool is_v = lane >= 16;
+    const uint32_t row_dst = ring + (is_v ? L::K_BYTES + row * L::V_PITCH : row * L::K_PITCH);
+    const i64 page_bytes = (is_v ? a.c.v_page_stride : a.c.k_page_stride) * L::ELEM;
+    const i64 token_bytes = (is_v ? a.c.v_token_stride : a.c.k_token_stride) * L::ELEM;
+    const unsigned page_size = a.c.page_size;
+    const uint32_t v_read = ring + L::K_BYTES + ((lane & 7) + ((lane >> 4) << 3)) * L::V_PITCH + ((lane >> 3) & 1) * 16;
+    const uint32_t k_read = ring + g8 * L::K_PITCH + t4 * L::VK;
+
     bool first_segment = true;
     for (i64 at = lo; at < hi;) {
         const int tile0 = static_cast<int>(at - e.start);
@@ -227,28 +238,84 @@ paged_decode_kernel(const DecodeArgs a) {
         const int heads = min(HEADS, a.G - e.run * HEADS);        // query heads of this run
         const int h0 = e.g * a.G + e.run * HEADS;
         const int* table = a.table + e.b * a.table_stride + e.g * a.table_head_stride;
+        const int end = e.first + e.count;
+        const int key0 = e.first + tile0 * TILE + warp * KEYS + row;       // this lane's key of the segment's first step
+        const uint8_t* const base = is_v ? static_cast<const uint8_t*>(a.c.v) + e.g * a.c.v_head_stride * L::ELEM
+                                         : static_cast<const uint8_t*>(a.c.k) + e.g * a.c.k_head_stride * L::ELEM;
+
+        // the table entry of this lane's key of a step; -1: no such key
+        auto page_at = [&](int step) -> int {
+            const int key = key0 + step * TILE;
+            return (step < n_tiles && key < end) ? __ldg(table + static_cast<unsigned>(key) / page_size) : -1;
+        };
+        // fetches a step; returns the mask of its keys that are there
+        auto copy = [&](int step, int entry, uint32_t s) -> uint32_t {
+            const int key = key0 + step * TILE;
+            const bool asked = step < n_tiles && key < end;
+            const bool there = asked && entry >= 0 && entry < a.c.num_pages;
+            const uint32_t mask = __ballot_sync(0xffffffffu, there) & 0xffffu;
+            if (asked && !there) raise_bad_index(a.status);
+            if (mask == 0 || dead) return 0;
+            const uint32_t bar = bar0 + 8 * s;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2 * __popc(mask) * L::ROW);
+            if (there) {
+                const unsigned off = static_cast<unsigned>(key) % page_size;
+                ptx::bulk_load(row_dst + s * L::STAGE, base + entry * page_bytes + off * token_bytes, L::ROW, bar);
+            } else if (is_v) {
+                // 0 * v has to be 0 for a value that is not there; ordered ahead of a later copy to the same place
+#pragma unroll
+                for (int i = 0; i < L::ROW; i += 16)
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(row_dst + s * L::STAGE + i), "r"(0) : "memory");
+                ptx::fence_proxy_async_smem();
+            }
+            return mask;
+        };
+
+        uint32_t masks[STAGES];      // of the next STAGES - 1 steps
+        int entry;
+        {
+            int entries[STAGES];
+#pragma unroll
+            for (int s = 0; s < STAGES; ++s) entries[s] = page_at(s);
+#pragma unroll
+            for (int s = 0; s < STAGES - 1; ++s) masks[s] = copy(s, entries[s], s);
+            entry = entries[STAGES - 1];
+        }
 
         // ---- queries: operand b of the score product, lane (head g8, element runs of t4), and their factor
-        uint32_t qf[NT][L::CK * L::VK / L::ELEM / 4][2];
+        constexpr int EL = L::VK / L::ELEM;      // elements of a run
+        uint32_t qf[NT][L::CK * EL / 4][2];
         float factor[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            constexpr int EL = L::VK / L::ELEM;      // elements of a run
             const int h = n * 8 + g8;
-            const cake_bf16* src = a.q + e.b * a.q_stride + (h0 + h) * a.q_head_stride;
-            float most = 0.f;
-            float f[L::CK][EL];
+            const cake_bf16* src = a.q + e.b * a.q_stride + (h0 + h) * a.q_head_stride + t4 * EL;
+            uint32_t w[L::CK][EL / 2];
 #pragma unroll
             for (int c = 0; c < L::CK; ++c)
 #pragma unroll
-                for (int j = 0; j < EL; ++j) {
-                    f[c][j] = h < heads ? bf16_f(src[(t4 + 4 * c) * EL + j]) : 0.f;
-                    most = fmaxf(most, fabsf(f[c][j]));
+                for (int j = 0; j < EL / 8; ++j) {
+                    uint4 u = make_uint4(0, 0, 0, 0);
+                    if (h < heads) {
+                        const cake_bf16* from = src + 4 * c * EL + 8 * j;
+                        if (a.q_wide) {
+                            u = __ldg(reinterpret_cast<const uint4*>(from));
+                        } else {
+                            auto two = [&](int i) { return static_cast<uint32_t>(from[i]) | (static_cast<uint32_t>(from[i + 1]) << 16); };
+                            u = make_uint4(two(0), two(2), two(4), two(6));
+                        }
+                    }
+                    w[c][4 * j] = u.x, w[c][4 * j + 1] = u.y, w[c][4 * j + 2] = u.z, w[c][4 * j + 3] = u.w;
                 }
             // 8-bit keys are widened to f16 (exact), so the query is too: divided by a power of two that leaves its largest
             // element in [1, 2), which keeps 11 bits where bf16 has 8; what underflows is below 2^-24 of the largest
             float unit = 1.f;
             if (E4M3) {
+                float most = 0.f;
+#pragma unroll
+                for (int c = 0; c < L::CK; ++c)
+#pragma unroll
+                    for (int j = 0; j < EL / 2; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo(w[c][j])), fabsf(bf16_hi(w[c][j]))));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 const uint32_t ex = __float_as_uint(most) & 0x7f800000u;
@@ -257,64 +324,17 @@ paged_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int c = 0; c < L::CK; ++c)
 #pragma unroll
-                    for (int j = 0; j < EL; ++j) f[c][j] *= down;
+                    for (int j = 0; j < EL / 2; ++j) w[c][j] = pack_f16(bf16_lo(w[c][j]) * down, bf16_hi(w[c][j]) * down);
             }
 #pragma unroll
             for (int c = 0; c < L::CK; ++c)
 #pragma unroll
-                for (int j = 0; j < EL / 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        qf[n][c * (EL / 4) + j][i] = E4M3 ? pack_f16(f[c][4 * j + 2 * i], f[c][4 * j + 2 * i + 1])
-                                                          : pack_bf16(f[c][4 * j + 2 * i], f[c][4 * j + 2 * i + 1]);
+                for (int j = 0; j < EL / 2; ++j) qf[n][c * (EL / 4) + j / 2][j & 1] = w[c][j];
             const float ks = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + e.g) : 1.f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 factor[n][i] = a.scale * LOG2E * ks * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
         }
-
-        // ---- loads: lanes 0-15 look up the pages of the step's keys, every lane copies its own runs
-        const int end = e.first + e.count;
-        const int key0 = e.first + tile0 * TILE + warp * KEYS;     // the warp's first key of the segment
-        auto page_at = [&](int step) -> int {                      // the table entry of key (lane) of a step; -1: no such key
-            const int key = key0 + step * TILE + (lane & 15);
-            return (step < n_tiles && key < end) ? __ldg(table + static_cast<unsigned>(key) / static_cast<unsigned>(a.c.page_size)) : -1;
-        };
-        auto copy = [&](int step, int entry) -> uint32_t {         // returns the step's mask of keys that are there
-            const int key = key0 + step * TILE + (lane & 15);
-            const bool asked = step < n_tiles && key < end;
-            const bool there = asked && entry >= 0 && entry < a.c.num_pages;
-            if (asked && !there) raise_bad_index(a.status);
-            const int off = static_cast<unsigned>(key) % static_cast<unsigned>(a.c.page_size);
-            const uint32_t mask = __ballot_sync(0xffffffffu, there) & 0xffffu;
-            const uint32_t stage = ring + (step % STAGES) * L::STAGE;
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int kk = g8 + 8 * r;
-                const i64 p = __shfl_sync(0xffffffffu, entry, kk);
-                const i64 o = __shfl_sync(0xffffffffu, off, kk);
-                const bool ok = (mask >> kk) & 1;
-                const uint8_t* src = static_cast<const uint8_t*>(a.c.k) +
-                                     (ok ? (p * a.c.k_page_stride + o * a.c.k_token_stride + e.g * a.c.k_head_stride) * L::ELEM : 0) + t4 * L::VK;
-#pragma unroll
-                for (int c = 0; c < L::CK; ++c)
-                    cp_async<L::VK>(stage + ((r * L::CK + c) * 32 + lane) * L::VK, src + c * 4 * L::VK, ok);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int kk = 2 * t4 + (r & 1) + 8 * (r >> 1);
-                const i64 p = __shfl_sync(0xffffffffu, entry, kk);
-                const i64 o = __shfl_sync(0xffffffffu, off, kk);
-                const bool ok = (mask >> kk) & 1;
-                const uint8_t* src = static_cast<const uint8_t*>(a.c.v) +
-                                     (ok ? (p * a.c.v_page_stride + o * a.c.v_token_stride + e.g * a.c.v_head_stride) * L::ELEM : 0) + g8 * L::VV;
-#pragma unroll
-                for (int c = 0; c < L::CV; ++c)
-                    cp_async<L::VV>(stage + L::K_BYTES + ((r * L::CV + c) * 32 + lane) * L::VV,
-                                    src + c * 8 * L::VV, ok);
-            }
-            return mask;
-        };
 
         float o[D / 16][NT][4];      // O^T: per 16 values of d, (d, head 2t4), (d, head 2t4+1), (d', ...), (d', ...)
         float m[NT][2], l[NT][2];
@@ -327,28 +347,30 @@ paged_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[j][n][i] = 0.f;
         }
-        uint32_t masks[STAGES];
-        int entry = page_at(0);
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) {
-            const int following = page_at(s + 1);
-            masks[s] = copy(s, entry);
-            cp_commit();
-            entry = following;
-        }
-        masks[STAGES - 1] = 0;
+        uint32_t s = 0;              // stage of the step
         for (int step = 0; step < n_tiles; ++step) {
             const int following = page_at(step + STAGES);
-            const uint32_t coming = copy(step + STAGES - 1, entry);
-            cp_commit();
+            __syncwarp();            // every lane has read the stage that is filled next
+            const uint32_t s_next = s == 0 ? STAGES - 1 : s - 1;
+            const uint32_t coming = copy(step + STAGES - 1, entry, s_next);
             entry = following;
-            cp_wait<STAGES - 1>();
             const uint32_t mask = masks[0];
 #pragma unroll
-            for (int s = 0; s + 1 < STAGES - 1; ++s) masks[s] = masks[s + 1];
+            for (int i = 0; i + 1 < STAGES - 1; ++i) masks[i] = masks[i + 1];
             masks[STAGES - 2] = coming;
+            const uint32_t here = s;
+            s = s + 1 == STAGES ? 0 : s + 1;
             if (mask == 0) continue;
-            const uint32_t stage = ring + (step % STAGES) * L::STAGE;
+            if (!dead) {
+                const uint32_t bar = bar0 + 8 * here, parity = (phases >> here) & 1;
+                int tries = 0;
+                while (!ptx::mbar_try_wait_hint(bar, parity, 20000) && tries < WAIT_TRIES) ++tries;
+                if (__any_sync(0xffffffffu, tries == WAIT_TRIES)) {
+                    dead = true;
+                    if (lane == 0) atomicCAS(a.status, CAKE_OK, CAKE_ERR_TIMEOUT);
+                }
+                phases ^= 1u << here;
+            }
 
             // ---- scores of 16 keys
             float x[NT][4];
@@ -356,11 +378,12 @@ paged_decode_kernel(const DecodeArgs a) {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
+            const uint32_t k_at = k_read + here * L::STAGE;
 #pragma unroll
             for (int c = 0; c < L::CK; ++c) {
                 uint32_t k0[L::VK / 4], k1[L::VK / 4];
-                lds<L::VK>(stage + (c * 32 + lane) * L::VK, k0);
-                lds<L::VK>(stage + ((L::CK + c) * 32 + lane) * L::VK, k1);
+                lds<L::VK>(k_at + c * 4 * L::VK, k0);
+                lds<L::VK>(k_at + 8 * L::K_PITCH + c * 4 * L::VK, k1);
                 if (E4M3) {
 #pragma unroll
                     for (int j = 0; j < L::VK / 4; ++j) {
@@ -380,26 +403,44 @@ paged_decode_kernel(const DecodeArgs a) {
                 }
             }
 
-            // ---- running maximum and sum; p in [0, 1]
+            // ---- running maximum and sum.  The maximum that is subtracted may lag behind the true one by up to SLACK (p stays below
+            // 2^SLACK, far inside every format it passes through), so it moves, and O is rescaled, only a few times per row
             uint32_t ph[NT][2], pl[NT][2];
             const bool ok0 = (mask >> g8) & 1, ok1 = (mask >> (g8 + 8)) & 1;
+            bool higher = false;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float p[4], keep[2];
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    p[i] = ok0 ? x[n][i] * factor[n][i] : NEG_INF;
-                    p[2 + i] = ok1 ? x[n][2 + i] * factor[n][i] : NEG_INF;
-                    float top = fmaxf(p[i], p[2 + i]);
+                    x[n][i] = ok0 ? x[n][i] * factor[n][i] : NEG_INF;
+                    x[n][2 + i] = ok1 ? x[n][2 + i] * factor[n][i] : NEG_INF;
+                    higher |= fmaxf(x[n][i], x[n][2 + i]) > m[n][i] + SLACK;
+                }
+            if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
-                    for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-                    top = fmaxf(m[n][i], top);
-                    const float base = top == NEG_INF ? 0.f : top;   // every score so far is -inf: they all weigh nothing
-                    keep[i] = exp2f(m[n][i] - base);
-                    m[n][i] = top;
-                    p[i] = exp2f(p[i] - base);
-                    p[2 + i] = exp2f(p[2 + i] - base);
-                    l[n][i] = l[n][i] * keep[i] + (p[i] + p[2 + i]);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float top = fmaxf(x[n][i], x[n][2 + i]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        top = fmaxf(m[n][i], top);
+                        const float keep = ex2(m[n][i] - (top == NEG_INF ? 0.f : top));
+                        m[n][i] = top;
+                        l[n][i] *= keep;
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j) o[j][n][i] *= keep, o[j][n][2 + i] *= keep;
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float base_m = m[n][i] == NEG_INF ? 0.f : m[n][i];     // every score so far is -inf: they all weigh nothing
+                    p[i] = ex2(x[n][i] - base_m);
+                    p[2 + i] = ex2(x[n][2 + i] - base_m);
+                    l[n][i] += p[i] + p[2 + i];
                 }
                 if (E4M3) {
                     // f16 holds 11 bits of p: its rounding is an eighth of the output's
@@ -413,47 +454,32 @@ paged_decode_kernel(const DecodeArgs a) {
                     ph[n][0] = transpose8x8(a0);
                     ph[n][1] = transpose8x8(a1);
                 }
-                if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        o[j][n][0] *= keep[0], o[j][n][1] *= keep[1];
-                        o[j][n][2] *= keep[0], o[j][n][3] *= keep[1];
-                    }
-                }
             }
 
-            // ---- weighted sum of 16 values
+            // ---- weighted sum of 16 values: 32 bytes of each at a time
 #pragma unroll
-            for (int c = 0; c < L::CV; ++c) {
-                uint32_t v[4][L::VV / 4];
+            for (int j = 0; j < L::ROW / 32; ++j) {
+                uint32_t v[4];
+                ldmatrix_trans(v_read + here * L::STAGE + j * 32, v);
+                if (E4M3) {
+                    // v[0], v[2]: elements (d, d+1) of two keys each, d = 32j + 2 g8; v[1], v[3]: 16 further on
 #pragma unroll
-                for (int r = 0; r < 4; ++r) lds<L::VV>(stage + L::K_BYTES + ((r * L::CV + c) * 32 + lane) * L::VV, v[r]);
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t f[4];
+                        e4m3_to_f16(__byte_perm(v[i], 0, 0x3120), f[0], f[1]);
+                        e4m3_to_f16(__byte_perm(v[2 + i], 0, 0x3120), f[2], f[3]);
 #pragma unroll
-                for (int j = 0; j < L::VV / 4; ++j) {
-                    if (E4M3) {
-                        uint32_t w[4][2];
+                        for (int n = 0; n < NT; ++n) mma<true>(o[2 * j + i][n], f, ph[n][0], ph[n][1]);
+                    }
+                } else {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) e4m3_to_f16(v[r][j], w[r][0], w[r][1]);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t f[4] = {__byte_perm(w[0][i], w[1][i], 0x5410), __byte_perm(w[0][i], w[1][i], 0x7632),
-                                                   __byte_perm(w[2][i], w[3][i], 0x5410), __byte_perm(w[2][i], w[3][i], 0x7632)};
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) mma<true>(o[(c * (L::VV / 4) + j) * 2 + i][n], f, ph[n][0], ph[n][1]);
-                        }
-                    } else {
-                        const uint32_t f[4] = {__byte_perm(v[0][j], v[1][j], 0x5410), __byte_perm(v[0][j], v[1][j], 0x7632),
-                                               __byte_perm(v[2][j], v[3][j], 0x5410), __byte_perm(v[2][j], v[3][j], 0x7632)};
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            mma<false>(o[c * (L::VV / 4) + j][n], f, ph[n][0], ph[n][1]);
-                            mma<false>(o[c * (L::VV / 4) + j][n], f, pl[n][0], pl[n][1]);
-                        }
+                    for (int n = 0; n < NT; ++n) {
+                        mma<false>(o[j][n], v, ph[n][0], ph[n][1]);
+                        mma<false>(o[j][n], v, pl[n][0], pl[n][1]);
                     }
                 }
             }
         }
-        cp_wait<0>();
 
         // ---- the warps' parts: maxima and sums first, then the weighted sums through the ring's memory
 #pragma unroll
@@ -461,11 +487,12 @@ paged_decode_kernel(const DecodeArgs a) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
 #pragma unroll
-                for (int s = 4; s < 32; s <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], s);
+                for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], d);
                 if (g8 == 0) wm[warp][n * 8 + 2 * t4 + i] = m[n][i], wl[warp][n * 8 + 2 * t4 + i] = l[n][i];
             }
         __syncthreads();             // (also: every warp has drained its ring)
-        float* const osum = reinterpret_cast<float*>(smem);      // [WARPS][HEADS][D]
+        float* const osum = reinterpret_cast<float*>(smem);      // [WARPS][HEADS][O_PITCH]
+        constexpr int O_PITCH = D + 4;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -474,77 +501,110 @@ paged_decode_kernel(const DecodeArgs a) {
                 float top = NEG_INF;
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) top = fmaxf(top, wm[w][h]);
-                const float f = exp2f(m[n][i] - (top == NEG_INF ? 0.f : top));
-                float* dst = osum + (warp * HEADS + h) * D;
-                constexpr int EV = L::VV / L::ELEM;       // neighbouring values of d of a lane
+                const float f = ex2(m[n][i] - (top == NEG_INF ? 0.f : top));
+                float* dst = osum + (warp * HEADS + h) * O_PITCH;
 #pragma unroll
-                for (int c = 0; c < L::CV; ++c)
-#pragma unroll
-                    for (int j = 0; j < EV / 2; ++j) {
-                        const int d = (g8 + 8 * c) * EV + 2 * j;
-                        dst[d] = o[c * (EV / 2) + j][n][i] * f;
-                        dst[d + 1] = o[c * (EV / 2) + j][n][2 + i] * f;
+                for (int j = 0; j < D / 16; ++j) {
+                    if (E4M3) {
+                        *reinterpret_cast<float2*>(dst + 16 * j + 2 * g8) = make_float2(o[j][n][i] * f, o[j][n][2 + i] * f);
+                    } else {
+                        dst[16 * j + g8] = o[j][n][i] * f;
+                        dst[16 * j + 8 + g8] = o[j][n][2 + i] * f;
                     }
+                }
             }
         __syncthreads();
         const bool whole = tile0 == 0 && n_tiles == e.tiles;
-        constexpr int PART = HEADS * (D + 2);            // floats of a part: m, l, then O, all of the run's heads
+        constexpr int PART = HEADS * (D + 4);            // floats of a part: O of the run's heads, then m and l (and padding)
         float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
         const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
-        for (int i = tid; i < heads * D; i += THREADS) {
-            const int h = i / D, d = i - h * D;
+        auto finish = [&](int h, int d, const float4& acc, float top, float sum) {
+            const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
+            uint2 w = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
+            cake_bf16* dst = a.out + (out0 + h) * D + d;
+            if (a.out_wide) {
+                *reinterpret_cast<uint2*>(dst) = w;
+            } else {
+                dst[0] = w.x & 0xffff, dst[1] = w.x >> 16, dst[2] = w.y & 0xffff, dst[3] = w.y >> 16;
+            }
+            if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
+        };
+        for (int i = tid; i < heads * (D / 4); i += THREADS) {
+            const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
             float top = NEG_INF;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) top = fmaxf(top, wm[w][h]);
-            const float base = top == NEG_INF ? 0.f : top;
-            float sum = 0.f, acc = 0.f;
+            const float base_m = top == NEG_INF ? 0.f : top;
+            float sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                sum += wl[w][h] * exp2f(wm[w][h] - base);
-                acc += osum[(w * HEADS + h) * D + d];
+                sum += wl[w][h] * ex2(wm[w][h] - base_m);
+                const float4 u = *reinterpret_cast<const float4*>(osum + (w * HEADS + h) * O_PITCH + d);
+                acc.x += u.x, acc.y += u.y, acc.z += u.z, acc.w += u.w;
             }
             if (whole) {
-                a.out[(out0 + h) * D + d] = to_bf16(sum == 0.f ? 0.f : acc / sum * vs);     // no token weighs anything: zeros
-                if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
+                finish(h, d, acc, top, sum);
             } else {
-                part[2 * HEADS + h * D + d] = acc;
-                if (d == 0) part[h] = top, part[HEADS + h] = sum;
+                __stcg(reinterpret_cast<float4*>(part + h * D + d), acc);
+                if (d == 0) __stcg(reinterpret_cast<float2*>(part + HEADS * D + 2 * h), make_float2(top, sum));
             }
         }
         if (!whole) {
             // ---- the entry's CTAs are neighbours; the last to arrive joins their parts in order
             const i64 s0 = e.start, s1 = e.start + e.tiles - 1;
-            const i64 c0 = ((s0 + 1) * n_ctas - 1) / total, c1 = ((s1 + 1) * n_ctas - 1) / total;
+            const int c0 = static_cast<int>(((s0 + 1) * n_ctas - 1) / total), c1 = static_cast<int>(((s1 + 1) * n_ctas - 1) / total);
             __syncthreads();
             if (tid == 0) {
                 __threadfence();
                 const int before_me = atomicAdd(a.counters + c0, 1);
-                last_flag = before_me == static_cast<int>(c1 - c0);
+                last_flag = before_me == c1 - c0;
                 if (last_flag) a.counters[c0] = 0;       // ready for the next call
                 __threadfence();
             }
             __syncthreads();
             if (last_flag) {
-                for (int i = tid; i < heads * D; i += THREADS) {
-                    const int h = i / D, d = i - h * D;
-                    float top = NEG_INF, sum = 0.f, acc = 0.f;
-                    for (i64 c = c0; c <= c1; ++c) {
-                        const float* p = a.parts + (2 * c + (c * total / n_ctas >= s0 ? 0 : 1)) * static_cast<i64>(PART);
-                        const float mi = __ldcg(p + h), li = __ldcg(p + HEADS + h), oi = __ldcg(p + 2 * HEADS + h * D + d);
-                        const float up = fmaxf(top, mi);
-                        const float base = up == NEG_INF ? 0.f : up;
-                        const float f0 = exp2f(top - base), f1 = exp2f(mi - base);
-                        sum = sum * f0 + li * f1;
-                        acc = acc * f0 + oi * f1;
+                // the entry is the first of a CTA's segments unless that CTA (the first of them) began before it
+                const int slot0 = c0 * total / n_ctas >= s0 ? 0 : 1;
+                for (int i = tid; i < heads * (D / 4); i += THREADS) {
+                    const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
+                    float top = NEG_INF, sum = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    constexpr int BATCH = 8;             // parts in flight
+                    for (int c = c0; c <= c1; c += BATCH) {
+                        float4 u[BATCH];
+                        float2 ml[BATCH];
+#pragma unroll
+                        for (int k = 0; k < BATCH; ++k) {
+                            u[k] = make_float4(0.f, 0.f, 0.f, 0.f), ml[k] = make_float2(NEG_INF, 0.f);
+                            if (c + k <= c1) {
+                                const float* p = a.parts + (2 * (c + k) + (c + k == c0 ? slot0 : 0)) * static_cast<i64>(PART);
+                                u[k] = __ldcg(reinterpret_cast<const float4*>(p + h * D + d));
+                                ml[k] = __ldcg(reinterpret_cast<const float2*>(p + HEADS * D + 2 * h));
+                            }
+                        }
+                        float up = top;
+#pragma unroll
+                        for (int k = 0; k < BATCH; ++k) up = fmaxf(up, ml[k].x);
+                        const float base_m = up == NEG_INF ? 0.f : up;
+                        const float f0 = ex2(top - base_m);
+                        sum *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+#pragma unroll
+                        for (int k = 0; k < BATCH; ++k) {
+                            const float f = ex2(ml[k].x - base_m);
+                            sum = fmaf(ml[k].y, f, sum);
+                            acc.x = fmaf(u[k].x, f, acc.x), acc.y = fmaf(u[k].y, f, acc.y);
+                            acc.z = fmaf(u[k].z, f, acc.z), acc.w = fmaf(u[k].w, f, acc.w);
+                        }
                         top = up;
                     }
-                    a.out[(out0 + h) * D + d] = to_bf16(sum == 0.f ? 0.f : acc / sum * vs);
-                    if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
+                    finish(h, d, acc, top, sum);
                 }
             }
         }
         __syncthreads();             // the ring's memory, wm and wl are free again
+        ptx::fence_proxy_async_smem();       // plain accesses to the ring's memory come before the next copies into it
         first_segment = false;
         at += n_tiles;
         if (at < hi) next(), look();
@@ -562,13 +622,13 @@ Shape shape_of(int Hq, int Hkv) {
     return s;
 }
 
-template <int D, bool E4M3, int NT>
+template <int D, bool E4M3, int NT, int STAGES_>
 int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     using L = Layout<D, E4M3>;
     constexpr int RING1 = WARPS * L::STAGE;
-    constexpr int STAGES = RING1 * 3 > 100 * 1024 ? 3 : (RING1 * 6 <= 100 * 1024 ? 6 : 100 * 1024 / RING1);
+    constexpr int STAGES = STAGES_;
     constexpr int RING = RING1 * STAGES;
-    constexpr int MERGE = WARPS * 8 * NT * D * 4;
+    constexpr int MERGE = WARPS * 8 * NT * (D + 4) * 4;
     constexpr int SMEM = RING > MERGE ? RING : MERGE;
     static bool set[64] = {};
     auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES>;
@@ -576,7 +636,12 @@ int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
         if (di.device >= 0 && di.device < 64) set[di.device] = true;
     }
-    const int per_sm = SMEM > 110 * 1024 ? 1 : 2;
+    static int per_sm_of[64] = {};
+    int per_sm = di.device >= 0 && di.device < 64 ? per_sm_of[di.device] : 0;
+    if (per_sm == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, SMEM) != cudaSuccess || per_sm < 1) return CAKE_ERR_CUDA;
+        if (di.device >= 0 && di.device < 64) per_sm_of[di.device] = per_sm;
+    }
     const int ctas = min(di.sm_count * per_sm, kPartCtas);
     kernel<<<ctas, THREADS, SMEM, s>>>(a);
     note_launches(1);
@@ -585,8 +650,9 @@ int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
 
 template <int D>
 int launch_d(const DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_t s) {
-    if (e4m3) return nt == 1 ? launch<D, true, 1>(a, di, s) : launch<D, true, 2>(a, di, s);
-    return nt == 1 ? launch<D, false, 1>(a, di, s) : launch<D, false, 2>(a, di, s);
+    constexpr int S16 = D <= 64 ? 4 : 2, S8 = D <= 96 ? 6 : D <= 128 ? 4 : 2;
+    if (e4m3) return nt == 1 ? launch<D, true, 1, S8>(a, di, s) : launch<D, true, 2, S8>(a, di, s);
+    return nt == 1 ? launch<D, false, 1, S16>(a, di, s) : launch<D, false, 2, S16>(a, di, s);
 }
 
 int check_heads(long long B, int Hq, int Hkv, int D) {
@@ -596,7 +662,7 @@ int check_heads(long long B, int Hq, int Hkv, int D) {
 }
 size_t workspace_bytes(int Hq, int Hkv, int D) {
     const Shape sh = shape_of(Hq, Hkv);
-    return round_up(static_cast<i64>(kHeaderBytes + sizeof(float) * 2 * kPartCtas * 8 * sh.nt * (D + 2)), 256);
+    return round_up(static_cast<i64>(kHeaderBytes + sizeof(float) * 2 * kPartCtas * 8 * sh.nt * (D + 4)), 256);
 }
 
 }  // namespace
@@ -647,6 +713,8 @@ int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_s
     a.lens_stride = lens_stride, a.lens_head_stride = lens_head_stride;
     a.B = static_cast<int>(B), a.Hq = Hq, a.G = Hq / cache->Hkv, a.chunks = sh.chunks, a.max_pages = max_pages, a.window = window;
     a.scale = scale;
+    a.q_wide = aligned(q, 16) && q_stride % 8 == 0 && q_head_stride % 8 == 0;
+    a.out_wide = aligned(out, 8);
     const bool e4m3 = cache->type == CAKE_KV_E4M3;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     switch (cache->D) {
