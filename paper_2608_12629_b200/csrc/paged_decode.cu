@@ -28,10 +28,8 @@ int check_cache(const cake_paged_cache* c);   // kv_append.cu
 
 namespace {
 
-constexpr int WARPS = 4;
-constexpr int THREADS = WARPS * 32;
 constexpr int KEYS = 16;                 // keys of a warp's step
-constexpr int TILE = WARPS * KEYS;       // keys of a CTA's tile
+constexpr int MOST_WARPS = 4;
 constexpr int kPartCtas = 1024;          // CTAs that the workspace has room for parts of (two each)
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
@@ -104,11 +102,26 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ void ldmatrix_trans(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-// four e4m3 values to two pairs of f16: exact
-__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    const uint16_t a = static_cast<uint16_t>(w & 0xffffu), b = static_cast<uint16_t>(w >> 16);
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"(a));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(b));
+// Four e4m3 values to two pairs of f16: `even` = bytes 0 and 2, `odd` = bytes 1 and 3.  The seven magnitude bits moved to bits
+// 7..13 are the value / 256 in f16 (its subnormals included; the factor is left to the caller), all in integer instructions: the conversion
+// instruction runs at a fraction of their rate (a pass over 8-bit keys was bound by it: 271 us against 106 us of memory
+// traffic).  NaN (magnitude 0x7f) would read 1.875: `most` keeps the largest magnitudes seen, 0x3f80 tells.
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& even, uint32_t& odd, uint32_t& most) {
+    const uint32_t mo = (w >> 1) & 0x3f803f80u, me = (w << 7) & 0x3f803f80u;
+    odd = mo | (w & 0x80008000u);
+    even = me | ((w << 8) & 0x80008000u);
+    most = __vimax3_u16x2(most, mo, me);
+}
+__device__ __forceinline__ bool holds_nan(uint32_t most) { return (most & 0xffffu) == 0x3f80u || (most >> 16) == 0x3f80u; }
+// the same with NaN kept, for the steps that hold one
+__device__ __forceinline__ void e4m3_to_f16_nan(uint32_t w, uint32_t& even, uint32_t& odd) {
+    uint32_t none = 0;
+    e4m3_to_f16(w, even, odd, none);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (((w >> (16 * h)) & 0x7fu) == 0x7fu) even |= 0x7e00u << (16 * h);
+        if (((w >> (16 * h + 8)) & 0x7fu) == 0x7fu) odd |= 0x7e00u << (16 * h);
+    }
 }
 
 // tokens of sequence b and key-value head g that are attended to: [first, first + count)
@@ -122,6 +135,7 @@ __device__ __forceinline__ void span_of(const DecodeArgs& a, int b, int g, int& 
     first = static_cast<int>(n - w);
     count = static_cast<int>(w);
 }
+template <int TILE>
 __device__ __forceinline__ int tiles_of(int count) { return count > 0 ? (count - 1) / TILE + 1 : 1; }   // an empty row still has to be written
 
 // The work list: entries in the order (sequence, key-value head, run of query heads), each of tiles_of(its tokens) tiles.
@@ -130,11 +144,13 @@ struct Cursor {
     i64 start;        // number of the entry's first tile in the list
 };
 
-template <int D, bool E4M3, int NT, int STAGES>
-__global__ void __launch_bounds__(THREADS)
+template <int D, bool E4M3, int NT, int STAGES, int WARPS, int PER_SM>
+__global__ void __launch_bounds__(WARPS * 32, PER_SM)
 paged_decode_kernel(const DecodeArgs a) {
     using L = Layout<D, E4M3>;
     constexpr int HEADS = 8 * NT;
+    constexpr int THREADS = WARPS * 32;
+    constexpr int TILE = WARPS * KEYS;       // keys of a CTA's tile
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ i64 scan[WARPS];
     __shared__ i64 found_start;
@@ -158,11 +174,11 @@ paged_decode_kernel(const DecodeArgs a) {
         bool cut;
         if (shared_lens) {
             span_of(a, b, 0, first, count, cut);
-            n = static_cast<i64>(tiles_of(count)) * Hkv;
+            n = static_cast<i64>(tiles_of<TILE>(count)) * Hkv;
         } else {
             for (int g = 0; g < Hkv; ++g) {
                 span_of(a, b, g, first, count, cut);
-                n += tiles_of(count);
+                n += tiles_of<TILE>(count);
             }
         }
         return n * a.chunks;
@@ -204,7 +220,7 @@ paged_decode_kernel(const DecodeArgs a) {
     bool cut;
     auto look = [&]() {
         span_of(a, e.b, e.g, e.first, e.count, cut);
-        e.tiles = tiles_of(e.count);
+        e.tiles = tiles_of<TILE>(e.count);
         if (cut && tid == 0) raise_bad_index(a.status);
     };
     auto next = [&]() {
@@ -324,7 +340,12 @@ paged_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int c = 0; c < L::CK; ++c)
 #pragma unroll
-                    for (int j = 0; j < EL / 2; ++j) w[c][j] = pack_f16(bf16_lo(w[c][j]) * down, bf16_hi(w[c][j]) * down);
+                    for (int j = 0; j < EL / 2; j += 2) {
+                    // in the order of the keys' conversion: elements 0 and 2, then 1 and 3, of every four
+                    const uint32_t u = w[c][j], v = w[c][j + 1];
+                    w[c][j] = pack_f16(bf16_lo(u) * down, bf16_lo(v) * down);
+                    w[c][j + 1] = pack_f16(bf16_hi(u) * down, bf16_hi(v) * down);
+                }
             }
 #pragma unroll
             for (int c = 0; c < L::CK; ++c)
@@ -333,7 +354,7 @@ paged_decode_kernel(const DecodeArgs a) {
             const float ks = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + e.g) : 1.f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                factor[n][i] = a.scale * LOG2E * ks * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
+                factor[n][i] = a.scale * LOG2E * ks * (E4M3 ? 256.f : 1.f) * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
         }
 
         float o[D / 16][NT][4];      // O^T: per 16 values of d, (d, head 2t4), (d, head 2t4+1), (d', ...), (d', ...)
@@ -374,33 +395,44 @@ paged_decode_kernel(const DecodeArgs a) {
 
             // ---- scores of 16 keys
             float x[NT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
             const uint32_t k_at = k_read + here * L::STAGE;
+            bool careful = false;        // 8-bit: a NaN among the keys, keep it
+            for (;;) {
+                uint32_t most = 0;
 #pragma unroll
-            for (int c = 0; c < L::CK; ++c) {
-                uint32_t k0[L::VK / 4], k1[L::VK / 4];
-                lds<L::VK>(k_at + c * 4 * L::VK, k0);
-                lds<L::VK>(k_at + 8 * L::K_PITCH + c * 4 * L::VK, k1);
-                if (E4M3) {
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < L::VK / 4; ++j) {
-                        uint32_t f[4];
-                        e4m3_to_f16(k0[j], f[0], f[2]);
-                        e4m3_to_f16(k1[j], f[1], f[3]);
+                    for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma<true>(x[n], f, qf[n][c * (L::VK / 4) + j][0], qf[n][c * (L::VK / 4) + j][1]);
-                    }
-                } else {
+                for (int c = 0; c < L::CK; ++c) {
+                    uint32_t k0[L::VK / 4], k1[L::VK / 4];
+                    lds<L::VK>(k_at + c * 4 * L::VK, k0);
+                    lds<L::VK>(k_at + 8 * L::K_PITCH + c * 4 * L::VK, k1);
+                    if (E4M3) {
 #pragma unroll
-                    for (int j = 0; j < L::VK / 8; ++j) {
-                        const uint32_t f[4] = {k0[2 * j], k1[2 * j], k0[2 * j + 1], k1[2 * j + 1]};
+                        for (int j = 0; j < L::VK / 4; ++j) {
+                            uint32_t f[4];
+                            if (careful) {
+                                e4m3_to_f16_nan(k0[j], f[0], f[2]);
+                                e4m3_to_f16_nan(k1[j], f[1], f[3]);
+                            } else {
+                                e4m3_to_f16(k0[j], f[0], f[2], most);
+                                e4m3_to_f16(k1[j], f[1], f[3], most);
+                            }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma<false>(x[n], f, qf[n][c * (L::VK / 8) + j][0], qf[n][c * (L::VK / 8) + j][1]);
+                            for (int n = 0; n < NT; ++n) mma<true>(x[n], f, qf[n][c * (L::VK / 4) + j][0], qf[n][c * (L::VK / 4) + j][1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < L::VK / 8; ++j) {
+                            const uint32_t f[4] = {k0[2 * j], k1[2 * j], k0[2 * j + 1], k1[2 * j + 1]};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma<false>(x[n], f, qf[n][c * (L::VK / 8) + j][0], qf[n][c * (L::VK / 8) + j][1]);
+                        }
                     }
                 }
+                if (!E4M3 || careful || !__any_sync(0xffffffffu, holds_nan(most))) break;
+                careful = true;
             }
 
             // ---- running maximum and sum.  The maximum that is subtracted may lag behind the true one by up to SLACK (p stays below
@@ -457,21 +489,44 @@ paged_decode_kernel(const DecodeArgs a) {
             }
 
             // ---- weighted sum of 16 values: 32 bytes of each at a time
+            if (E4M3) {
+                // of v: [0], [2] elements (d, d+1) of two keys each, d = 32j + 2 g8; [1], [3] 16 further on; even bytes are d, odd ones d+1
+                constexpr int RUN = L::ROW / 32 < 4 ? L::ROW / 32 : 4;
 #pragma unroll
-            for (int j = 0; j < L::ROW / 32; ++j) {
-                uint32_t v[4];
-                ldmatrix_trans(v_read + here * L::STAGE + j * 32, v);
-                if (E4M3) {
-                    // v[0], v[2]: elements (d, d+1) of two keys each, d = 32j + 2 g8; v[1], v[3]: 16 further on
+                for (int j0 = 0; j0 < L::ROW / 32; j0 += RUN) {
+                    uint32_t v[4], f[RUN][2][4], most = 0;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t f[4];
-                        e4m3_to_f16(__byte_perm(v[i], 0, 0x3120), f[0], f[1]);
-                        e4m3_to_f16(__byte_perm(v[2 + i], 0, 0x3120), f[2], f[3]);
+                    for (int j = 0; j < RUN; ++j) {
+                        ldmatrix_trans(v_read + here * L::STAGE + (j0 + j) * 32, v);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma<true>(o[2 * j + i][n], f, ph[n][0], ph[n][1]);
+                        for (int i = 0; i < 2; ++i) {
+                            e4m3_to_f16(v[i], f[j][i][0], f[j][i][1], most);
+                            e4m3_to_f16(v[2 + i], f[j][i][2], f[j][i][3], most);
+                        }
                     }
-                } else {
+                    if (__any_sync(0xffffffffu, holds_nan(most))) {
+#pragma unroll
+                        for (int j = 0; j < RUN; ++j) {
+                            ldmatrix_trans(v_read + here * L::STAGE + (j0 + j) * 32, v);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                e4m3_to_f16_nan(v[i], f[j][i][0], f[j][i][1]);
+                                e4m3_to_f16_nan(v[2 + i], f[j][i][2], f[j][i][3]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < RUN; ++j)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma<true>(o[2 * (j0 + j) + i][n], f[j][i], ph[n][0], ph[n][1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < L::ROW / 32; ++j) {
+                    uint32_t v[4];
+                    ldmatrix_trans(v_read + here * L::STAGE + j * 32, v);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         mma<false>(o[j][n], v, ph[n][0], ph[n][1]);
@@ -517,7 +572,7 @@ paged_decode_kernel(const DecodeArgs a) {
         const bool whole = tile0 == 0 && n_tiles == e.tiles;
         constexpr int PART = HEADS * (D + 4);            // floats of a part: O of the run's heads, then m and l (and padding)
         float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
-        const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
+        const float vs = !E4M3 ? 1.f : (a.c.v_scale ? 256.f * __ldg(a.c.v_scale + e.g) : 256.f);
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
         auto finish = [&](int h, int d, const float4& acc, float top, float sum) {
             const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
@@ -622,16 +677,15 @@ Shape shape_of(int Hq, int Hkv) {
     return s;
 }
 
-template <int D, bool E4M3, int NT, int STAGES_>
+template <int D, bool E4M3, int NT, int STAGES, int WARPS, int PER_SM>
 int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     using L = Layout<D, E4M3>;
     constexpr int RING1 = WARPS * L::STAGE;
-    constexpr int STAGES = STAGES_;
     constexpr int RING = RING1 * STAGES;
     constexpr int MERGE = WARPS * 8 * NT * (D + 4) * 4;
     constexpr int SMEM = RING > MERGE ? RING : MERGE;
     static bool set[64] = {};
-    auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES>;
+    auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES, WARPS, PER_SM>;
     if (di.device < 0 || di.device >= 64 || !set[di.device]) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
         if (di.device >= 0 && di.device < 64) set[di.device] = true;
@@ -639,20 +693,22 @@ int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     static int per_sm_of[64] = {};
     int per_sm = di.device >= 0 && di.device < 64 ? per_sm_of[di.device] : 0;
     if (per_sm == 0) {
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, SMEM) != cudaSuccess || per_sm < 1) return CAKE_ERR_CUDA;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, WARPS * 32, SMEM) != cudaSuccess || per_sm < 1) return CAKE_ERR_CUDA;
         if (di.device >= 0 && di.device < 64) per_sm_of[di.device] = per_sm;
     }
     const int ctas = min(di.sm_count * per_sm, kPartCtas);
-    kernel<<<ctas, THREADS, SMEM, s>>>(a);
+    kernel<<<ctas, WARPS * 32, SMEM, s>>>(a);
     note_launches(1);
     return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
+// Two stages a warp and as many warps as fit: a warp's step is a chain of dependent instructions, other warps fill its gaps.
 template <int D>
 int launch_d(const DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_t s) {
-    constexpr int S16 = D <= 64 ? 4 : 2, S8 = D <= 96 ? 6 : D <= 128 ? 4 : 2;
-    if (e4m3) return nt == 1 ? launch<D, true, 1, S8>(a, di, s) : launch<D, true, 2, S8>(a, di, s);
-    return nt == 1 ? launch<D, false, 1, S16>(a, di, s) : launch<D, false, 2, S16>(a, di, s);
+    constexpr int W16 = D == 256 ? 2 : 4;
+    constexpr int P8 = D <= 128 ? 4 : 2, P16 = D <= 64 ? 4 : 3;
+    if (e4m3) return nt == 1 ? launch<D, true, 1, 2, 4, P8>(a, di, s) : launch<D, true, 2, 2, 4, D == 256 ? 2 : 3>(a, di, s);
+    return nt == 1 ? launch<D, false, 1, 2, W16, P16>(a, di, s) : launch<D, false, 2, 2, W16, 3>(a, di, s);
 }
 
 int check_heads(long long B, int Hq, int Hkv, int D) {
@@ -690,7 +746,7 @@ int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_s
     if (rc != CAKE_OK) return rc;
     rc = check_heads(B, Hq, cache->Hkv, cache->D);
     if (rc != CAKE_OK) return rc;
-    if (max_pages < 0 || static_cast<i64>(max_pages) * cache->page_size > INT_MAX - 16 * TILE || window < 0) return CAKE_ERR_SHAPE;
+    if (max_pages < 0 || static_cast<i64>(max_pages) * cache->page_size > INT_MAX - 16 * MOST_WARPS * KEYS || window < 0) return CAKE_ERR_SHAPE;
     if (table_stride < 0 || table_head_stride < 0 || lens_stride < 0 || lens_head_stride < 0 || q_stride < 0 || q_head_stride < 0)
         return CAKE_ERR_SHAPE;
     if (!ws) return CAKE_ERR_NULL;

@@ -507,6 +507,30 @@ def test_decode_scores_far_apart_and_infinite():
     assert torch.isnan(out[3]).all() and torch.isnan(lse[3]).all()
 
 
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_decode_every_8_bit_value_and_nan(D):
+    """All 254 finite e4m3 patterns (their subnormals too) through the keys' and the values' conversion; NaN where it is."""
+    q, cache, table, n = decode_problem(4, 1, D, 16, E4M3, [256, 256, 256], 21, poison=False)
+    flat = [c.view(torch.uint8) for c in (cache.k, cache.v)]
+    codes = torch.arange(256, device=DEV)
+    codes = torch.where((codes & 0x7f) == 0x7f, codes - 1, codes).to(torch.uint8)
+    g = gen(2)
+    for b in range(3):
+        for f in flat:                               # every token of a column another code
+            cols = torch.stack([codes[torch.randperm(256, device=DEV, generator=g)] for _ in range(D)], 1)
+            f[table[b].long()] = cols.view(16, 16, 1, D)
+    q.mul_(0.02)
+    out, lse = cake.cake_paged_decode(q, cache, table, n, want_lse=True)
+    check_decode(q, cache, table, n, out, lse)
+    for sign in (0x7f, 0xff):
+        flat[0][table[0, 3].long(), 5, 0, 7] = sign  # a key of the first sequence
+        flat[1][table[1, 9].long(), 2, 0, D - 1] = sign      # one element of a value of the second
+        bad, bad_lse = cake.cake_paged_decode(q, cache, table, n, want_lse=True)
+        assert torch.isnan(bad[0]).all() and torch.isnan(bad_lse[0]).all()
+        assert torch.isnan(bad[1, :, D - 1]).all() and torch.equal(bad[1, :, :D - 1], out[1, :, :D - 1])
+        assert torch.equal(bad[2], out[2]) and torch.equal(bad_lse[1:], lse[1:])
+
+
 def test_decode_scale_strides_streams_and_graphs():
     q, cache, table, n = decode_problem(8, 2, 128, 16, BF16, [500, 33, 0, 70], 12)
     wide = torch.zeros(4, 12, 128, dtype=BF16, device=DEV)
