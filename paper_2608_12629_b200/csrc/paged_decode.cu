@@ -10,9 +10,9 @@
 // [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined by the last of
 // them to arrive, from parts in the workspace, in the order of the CTAs.
 //
-// A warp works on 16 keys at a time, with a ring of its own in shared memory and no barrier between warps.  One instruction
-// of the warp fetches a step: each lane copies one row (bulk copy; lanes 0-15 the keys, 16-31 the values) to a pitch at which
-// the reads below meet no bank twice.
+// A warp works on 16 keys at a time, with a ring of its own in shared memory and no barrier between warps.  Long rows are
+// fetched by one instruction of the warp a step: each lane copies one row (bulk copy; lanes 0-15 the keys, 16-31 the values); short
+// ones 16 bytes per lane and instruction.  They land at a pitch at which the reads below meet no bank twice.
 //   scores:  S^T[key][head] = K Q^T   (m16n8k16: 16 keys x 8 heads; the contraction's order of elements is permuted the same way
 //            in both operands so that a lane's 16-byte run of a key feeds whole k-steps)
 //   output:  O^T[d][head] += V^T P    (16 values of d x 8 heads x 16 keys; V^T by transposing matrix loads, P's operand from
@@ -64,8 +64,19 @@ struct Layout {
     // a value's row is read 16 bytes at a time, eight rows at once: an odd number of 16-byte units apart
     static constexpr int V_PITCH = (ROW / 16) % 2 == 1 ? ROW : ROW + 16;
     static constexpr int K_BYTES = KEYS * K_PITCH;
+    // Rows of 256 bytes and more: one bulk copy per row.  An SM takes about 160 bulk copies a microsecond, whatever their size, so that
+    // shorter rows (128 bytes: 2.8 TB/s) are fetched by 16-byte asynchronous copies of all lanes instead
+    static constexpr bool BULK = ROW >= 256;
+    static constexpr int UNITS = ROW / 16;                                          // 16-byte units of a row
     static constexpr int STAGE = KEYS * (K_PITCH + V_PITCH);                        // of a warp
 };
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {      // zeros where !ok
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <int N>
 __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[N / 4]) {
@@ -271,6 +282,23 @@ paged_decode_kernel(const DecodeArgs a) {
             const bool there = asked && entry >= 0 && entry < a.c.num_pages;
             const uint32_t mask = __ballot_sync(0xffffffffu, there) & 0xffffu;
             if (asked && !there) raise_bad_index(a.status);
+            if (!L::BULK) {
+                if (mask != 0) {
+                    const unsigned off = static_cast<unsigned>(key) % page_size;
+                    const uint64_t mine = reinterpret_cast<uint64_t>(base + (there ? entry * page_bytes + off * token_bytes : 0));
+                    const uint32_t stage = ring + s * L::STAGE;
+#pragma unroll
+                    for (int i = 0; i < L::UNITS; ++i) {          // first the keys' 16 * UNITS units, then the values'
+                        const int v = i >= L::UNITS / 2;
+                        const int unit = (i - v * (L::UNITS / 2)) * 32 + lane;
+                        const int r = unit / L::UNITS, c = unit - r * L::UNITS;
+                        const uint8_t* src = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, mine, r + 16 * v)) + c * 16;
+                        cp_async16(stage + (v ? L::K_BYTES + r * L::V_PITCH : r * L::K_PITCH) + c * 16, src, (mask >> r) & 1);
+                    }
+                }
+                cp_commit();
+                return mask;
+            }
             if (mask == 0 || dead) return 0;
             const uint32_t bar = bar0 + 8 * s;
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2 * __popc(mask) * L::ROW);
@@ -382,7 +410,10 @@ paged_decode_kernel(const DecodeArgs a) {
             const uint32_t here = s;
             s = s + 1 == STAGES ? 0 : s + 1;
             if (mask == 0) continue;
-            if (!dead) {
+            if (!L::BULK) {
+                cp_wait<STAGES - 1>();
+                __syncwarp();
+            } else if (!dead) {
                 const uint32_t bar = bar0 + 8 * here, parity = (phases >> here) & 1;
                 int tries = 0;
                 while (!ptx::mbar_try_wait_hint(bar, parity, 20000) && tries < WAIT_TRIES) ++tries;
@@ -535,6 +566,8 @@ paged_decode_kernel(const DecodeArgs a) {
                 }
             }
         }
+
+        if (!L::BULK) cp_wait<0>();
 
         // ---- the warps' parts: maxima and sums first, then the weighted sums through the ring's memory
 #pragma unroll
