@@ -6,10 +6,14 @@
 // (kind::f8f6f4).  The tensor core starts every block from zero in one of a ring of tensor-memory buffers; the epilogue
 // warps fetch a finished block, scale it and add it to 32-bit sums in their registers, while the next blocks run.
 //
-// The weights are the M side of the instruction (128 rows of W = 128 lanes of tensor memory), the rows of X its columns:
-// a few rows of X (a decode step) then cost a narrow tile instead of a mostly empty one, a tile of W lies in one row of the
-// weights' scales, and 32 lanes store 32 neighbouring outputs.  The scale of an element depends on its column alone
-// (xs * ws, multiplied once per block by a warp of its own and read as a broadcast), so the addition is one FMA.
+// Two kernels, chosen by the rows of X:
+//   up to 64 rows   The weights are the M side of the instruction (128 rows of W = 128 lanes of tensor memory), the rows of X its
+//                   columns: a few rows then cost a narrow tile instead of a mostly empty one.  Bound by reading W.  The scale of an
+//                   element depends on its column (xs * ws, multiplied once per block by a warp of its own, read as a broadcast).
+//   more            X is the M side, two SMs to a 256 x 256 tile (cta_group::2: each loads half of both operands, 32 KiB a block instead
+//                   of the 48 of a 128 x 256 tile of one SM, whose demand of 94 bytes a clock the L2 does not meet).  The scale of an
+//                   element depends on its lane and on its half of the columns: one factor per thread and block, packed FMAs.
+// Where a product has too few tiles for the SMs its contraction is split; the last CTA of a tile to arrive adds up the parts.
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -25,6 +29,7 @@ constexpr int THREADS = 11 * 32;
 constexpr int SCALE_BUFS = 8;                  // blocks of scales ahead
 constexpr uint32_t W_BYTES = TM * KB;
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
+constexpr int NARROW_M = 64;                   // rows of X up to which the narrow kernel is taken
 
 struct GemmArgs {
     const float* xs;
@@ -35,7 +40,7 @@ struct GemmArgs {
     int* status;
     i64 M, out_stride;
     int N, nkb, tiles_m, tiles_n, splits;      // tiles_m: of X's rows
-    bool fp32;
+    bool fp32, out_wide;                       // out_wide: 16-byte stores
 };
 
 struct __align__(16) Ctrl {
@@ -100,8 +105,8 @@ struct Tile {
     static constexpr int COLS = TN / 2;                              // columns of an epilogue thread
     static constexpr int LD = COLS < 32 ? COLS : 32;
     static constexpr uint32_t STAGE = W_BYTES + TN * KB;
-    static constexpr int STAGES = TN == 256 ? 4 : TN == 128 ? 6 : TN == 64 ? 8 : TN == 32 ? 10 : 11;
-    static constexpr int BUFS = TN == 256 ? 2 : 4;
+    static constexpr int STAGES = TN == 64 ? 8 : TN == 32 ? 10 : 11;
+    static constexpr int BUFS = 4;
     static constexpr uint32_t TMEM_COLS = BUFS * TN < 32 ? 32 : BUFS * TN;
     static constexpr uint32_t SMEM = 1024 + STAGES * STAGE + SCALE_BUFS * TN * 4 + sizeof(Ctrl);
     static_assert(SMEM <= 227 * 1024, "");
@@ -334,29 +339,348 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     }
 }
 
+// ------------------------------------------------------------------------------------------------------ more rows: CTA pairs
+namespace wide {
+
+constexpr int BM = 256, BN = 256;              // tile of a pair: rows of X, rows of W
+constexpr int STAGES = 6, BUFS = 2;
+constexpr uint32_t HALF = 128 * KB;            // a CTA's 128 rows of one operand
+constexpr uint32_t STAGE = 2 * HALF;
+constexpr int PAIR_THREADS = 10 * 32;
+constexpr int OUT_PITCH = 80;                  // bytes of a staged row: 64 and a shift of the banks
+constexpr uint32_t OUT_BYTES = EPI_WARPS * 32 * OUT_PITCH;
+constexpr int COLS = 128;                      // columns of an epilogue thread
+constexpr int BAND = 8;                        // tiles of X's rows that are worked on together, for the L2
+
+struct __align__(16) PairCtrl {
+    uint64_t full[STAGES], empty[STAGES], tfull[BUFS], tempty[BUFS];
+    uint32_t tmem;
+    int abort_flag;
+    int last;
+};
+constexpr uint32_t SMEM = 1024 + STAGES * STAGE + OUT_BYTES + sizeof(PairCtrl);
+static_assert(SMEM <= 227 * 1024, "");
+
+__device__ __forceinline__ void pair_wait(uint64_t* bar, uint32_t parity, PairCtrl* ctrl, int* status) {
+    const uint32_t addr = ptx::smem_u32(bar);
+    if (ptx::mbar_try_wait(addr, parity)) return;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (!ptx::mbar_try_wait_hint(addr, parity, 20000)) {
+        if (*reinterpret_cast<volatile int*>(&ctrl->abort_flag)) return;
+        if (ptx::globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+            *reinterpret_cast<volatile int*>(&ctrl->abort_flag) = 1;
+            atomicCAS(status, CAKE_OK, CAKE_ERR_TIMEOUT);
+            return;
+        }
+    }
+}
+__device__ __forceinline__ bool pair_aborted(PairCtrl* ctrl) { return *reinterpret_cast<volatile int*>(&ctrl->abort_flag) != 0; }
+// the same place in rank 0's shared memory
+__device__ __forceinline__ uint32_t at_rank0(const void* p) { return ptx::smem_u32(p) & ~ptx::CLUSTER_PEER_BIT; }
+
+template <bool ACC>
+__device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "n"(ACC ? 1 : 0)
+        : "memory");
+}
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ld_wait(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
+}
+// acc (two floats) += r * s
+__device__ __forceinline__ void fma2(float2& acc, uint32_t r0, uint32_t r1, float s) {
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %4};\n\t"
+        "mov.b64 c, {%0, %1};\n\t"
+        "fma.rn.f32x2 c, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, c;\n\t}"
+        : "+f"(acc.x), "+f"(acc.y) : "r"(r0), "r"(r1), "f"(s));
+}
+
+struct PairItem {
+    int m0, n0, kb0, kb1, split, tile;
+};
+// Tiles in bands of BAND tiles of X's rows, all of W's tiles through a band; the parts of a tile next to each other.
+__device__ __forceinline__ PairItem pair_item(const GemmArgs& a, int i) {
+    PairItem it;
+    it.split = i % a.splits;
+    it.tile = i / a.splits;
+    const int band = it.tile / (BAND * a.tiles_n);
+    const int in_band = it.tile - band * BAND * a.tiles_n;
+    const int high = min(BAND, a.tiles_m - band * BAND);
+    const int nt = in_band / high;
+    it.m0 = (band * BAND + in_band - nt * high) * BM;
+    it.n0 = nt * BN;
+    it.kb0 = static_cast<int>(static_cast<i64>(it.split) * a.nkb / a.splits);
+    it.kb1 = static_cast<int>(static_cast<i64>(it.split + 1) * a.nkb / a.splits);
+    return it;
+}
+
+__global__ void __launch_bounds__(PAIR_THREADS, 1)
+gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const GemmArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t* const staging = tiles + STAGES * STAGE;
+    PairCtrl* const ctrl = reinterpret_cast<PairCtrl*>(staging + OUT_BYTES);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const int items = a.tiles_m * a.tiles_n * a.splits;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctrl->full[i]), 1);          // rank 0's: both CTAs' bytes
+            ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), 1);
+        }
+        for (int i = 0; i < BUFS; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), 2 * EPI_WARPS);   // rank 0's: both CTAs' warps
+        }
+        ctrl->abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tensormap(&map_w);
+        ptx::prefetch_tensormap(&map_x);
+    }
+    if (warp == WARP_MMA) {
+        ptx::tmem_alloc_pair(ptx::smem_u32(&ctrl->tmem), BUFS * BN);
+        ptx::tmem_relinquish_pair();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_sync_all();         // both CTAs' barriers and tensor memory are set up
+    ptx::tc_fence_after();
+    const uint32_t tmem = ctrl->tmem;
+
+    if (warp == WARP_TMA) {
+        if (ptx::elect_one()) {
+            uint32_t n = 0;
+            for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
+                const PairItem it = pair_item(a, i);
+                const int x_row = it.m0 + static_cast<int>(rank) * 128, w_row = it.n0 + static_cast<int>(rank) * 128;
+                for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
+                    const uint32_t s = n % STAGES;
+                    pair_wait(&ctrl->empty[s], ((n / STAGES) & 1) ^ 1, ctrl, a.status);
+                    if (pair_aborted(ctrl)) break;
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctrl->full[s]), 2 * STAGE);
+                    const uint32_t bar = at_rank0(&ctrl->full[s]), dst = ptx::smem_u32(tiles + s * STAGE);
+                    ptx::tma_load_2d_pair(dst, &map_x, bar, kb * KB, x_row);
+                    ptx::tma_load_2d_pair(dst + HALF, &map_w, bar, kb * KB, w_row);
+                }
+            }
+            if (pair_aborted(ctrl)) {        // give copies in flight a bounded time to land
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (ptx::globaltimer_ns() - t0 < 1000000ull) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp == WARP_MMA) {
+        if (rank == 0 && ptx::elect_one()) {
+            uint32_t n = 0;
+            constexpr uint32_t idesc = idesc_e4m3(BM, BN);
+            constexpr uint16_t BOTH = 3;
+            for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
+                const PairItem it = pair_item(a, i);
+                for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
+                    const uint32_t s = n % STAGES, b = n % BUFS;
+                    pair_wait(&ctrl->tempty[b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
+                    pair_wait(&ctrl->full[s], (n / STAGES) & 1, ctrl, a.status);
+                    if (pair_aborted(ctrl)) break;
+                    ptx::tc_fence_after();
+                    const uint32_t base = ptx::smem_u32(tiles + s * STAGE);
+                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + HALF);
+                    const uint32_t d = tmem + b * BN;
+                    umma_pair_e4m3<false>(d, da, db, idesc);
+                    umma_pair_e4m3<true>(d, da + 2, db + 2, idesc);
+                    umma_pair_e4m3<true>(d, da + 4, db + 4, idesc);
+                    umma_pair_e4m3<true>(d, da + 6, db + 6, idesc);
+                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->empty[s]), BOTH);
+                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[b]), BOTH);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int half = warp >> 2, quad = warp & 3;
+        const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * COLS;
+        const int local_row = quad * 32 + lane;                        // of the CTA's 128
+        uint8_t* const stage_out = staging + warp * 32 * OUT_PITCH;
+        const int n_blocks = (a.N + 127) / 128;
+        uint32_t n = 0;
+        for (int i = pair; i < items; i += n_pairs) {                  // (every warp takes every step, also after an expired wait)
+            const PairItem it = pair_item(a, i);
+            const i64 row = static_cast<i64>(it.m0) + rank * 128 + local_row;
+            const int block = it.n0 / 128 + half;
+            const bool live = row < a.M && block < n_blocks;
+            const float* xs = a.xs + row * a.nkb;
+            const float* ws = a.ws + static_cast<i64>(block) * a.nkb;
+            float2 acc[COLS / 2];
+#pragma unroll
+            for (int c = 0; c < COLS / 2; ++c) acc[c] = make_float2(0.f, 0.f);
+            float next = live ? __ldg(xs + it.kb0) * __ldg(ws + it.kb0) : 0.f;
+            for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
+                const uint32_t b = n % BUFS;
+                const float s = next;
+                if (live && kb + 1 < it.kb1) next = __ldg(xs + kb + 1) * __ldg(ws + kb + 1);
+                pair_wait(&ctrl->tfull[b], (n / BUFS) & 1, ctrl, a.status);
+                ptx::tc_fence_after();
+                const uint32_t t = t_lane + b * BN;
+                uint32_t r[2][16];
+                ld16(t, r[0]);
+#pragma unroll
+                for (int c = 0; c < COLS / 16; ++c) {
+                    ld_wait(r[c & 1]);
+                    if (c + 1 < COLS / 16) {
+                        ld16(t + (c + 1) * 16, r[(c + 1) & 1]);
+                    } else {
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[b]));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) fma2(acc[c * 8 + j], r[c & 1][2 * j], r[c & 1][2 * j + 1], s);
+                }
+            }
+            if (a.splits > 1) {
+                // parts as [4 columns][256 rows] of float4: 32 lanes write 512 neighbouring bytes
+                const i64 part = static_cast<i64>(BM) * BN;
+                float4* const mine = reinterpret_cast<float4*>(a.parts + i * part) + (half * (COLS / 4)) * BM + rank * 128 + local_row;
+#pragma unroll
+                for (int c = 0; c < COLS / 4; ++c)
+                    __stcg(mine + c * BM, make_float4(acc[2 * c].x, acc[2 * c].y, acc[2 * c + 1].x, acc[2 * c + 1].y));
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
+                if (threadIdx.x == 0) {
+                    __threadfence();
+                    int* counter = a.counters + 2 * it.tile + rank;
+                    const int seen = atomicAdd(counter, 1);
+                    ctrl->last = seen == a.splits - 1;
+                    if (ctrl->last) *counter = 0;
+                    __threadfence();
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
+                const bool last = ctrl->last;
+                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");     // read by all before the next item writes it
+                if (!last) continue;
+#pragma unroll
+                for (int c = 0; c < COLS / 2; ++c) acc[c] = make_float2(0.f, 0.f);
+                for (int s = 0; s < a.splits; ++s) {
+                    const float4* from = mine + static_cast<i64>(s - it.split) * (part / 4);
+#pragma unroll
+                    for (int c = 0; c < COLS / 4; ++c) {
+                        const float4 u = __ldcg(from + c * BM);
+                        acc[2 * c].x += u.x, acc[2 * c].y += u.y, acc[2 * c + 1].x += u.z, acc[2 * c + 1].y += u.w;
+                    }
+                }
+            }
+            // ---- out: 64 bytes of each of the warp's 32 rows at a time through shared memory, so that a store instruction covers whole
+            // sectors of 8 rows instead of 16 bytes of 32
+            const int col0 = it.n0 + half * COLS;
+            const i64 row0 = static_cast<i64>(it.m0) + rank * 128 + quad * 32;
+            auto flush = [&](int col, int per) {       // `per` elements to a row's 64 bytes
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = k * 8 + (lane >> 2), c = lane & 3;
+                    const uint4 u = *reinterpret_cast<const uint4*>(stage_out + r * OUT_PITCH + c * 16);
+                    const i64 to = row0 + r;
+                    const int e = col + c * (per / 4);
+                    if (to < a.M && e < a.N) {
+                        if (a.out_wide && e + per / 4 <= a.N) {
+                            if (a.fp32) *reinterpret_cast<uint4*>(static_cast<float*>(a.out) + to * a.out_stride + e) = u;
+                            else *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(a.out) + to * a.out_stride + e) = u;
+                        } else {
+                            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                if (a.fp32) {
+                                    if (e + q < a.N) static_cast<uint32_t*>(a.out)[to * a.out_stride + e + q] = w[q];
+                                } else {
+                                    cake_bf16* dst = static_cast<cake_bf16*>(a.out) + to * a.out_stride + e;
+                                    if (e + 2 * q < a.N) dst[2 * q] = w[q] & 0xffff;
+                                    if (e + 2 * q + 1 < a.N) dst[2 * q + 1] = w[q] >> 16;
+                                }
+                            }
+                        }
+                    }
+                }
+                __syncwarp();
+            };
+            uint4* const put = reinterpret_cast<uint4*>(stage_out + lane * OUT_PITCH);
+            if (a.fp32) {
+#pragma unroll
+                for (int c = 0; c < COLS; c += 16) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        put[q] = make_uint4(__float_as_uint(acc[c / 2 + 2 * q].x), __float_as_uint(acc[c / 2 + 2 * q].y),
+                                            __float_as_uint(acc[c / 2 + 2 * q + 1].x), __float_as_uint(acc[c / 2 + 2 * q + 1].y));
+                    flush(col0 + c, 16);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < COLS; c += 32) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float2* f = acc + c / 2 + 4 * q;
+                        put[q] = make_uint4(pack_bf16(f[0].x, f[0].y), pack_bf16(f[1].x, f[1].y), pack_bf16(f[2].x, f[2].y), pack_bf16(f[3].x, f[3].y));
+                    }
+                    flush(col0 + c, 32);
+                }
+            }
+        }
+    }
+    // neither CTA leaves while the other's MMAs, loads or arrivals can still reach it
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::cluster_sync_all();
+    if (warp == WARP_MMA) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc_pair(tmem, BUFS * BN);
+    }
+}
+
+}  // namespace wide
+
 // ---------------------------------------------------------------------------------------------------------------- host
 struct Plan {
+    bool pair;
     int tn, tiles_m, tiles_n, splits, nkb;
     size_t part_bytes;
 };
 Plan plan_of(i64 M, int N, int K, int sms) {
     Plan p;
     p.nkb = (K + KB - 1) / KB;
-    p.tiles_n = (N + TM - 1) / TM;
-    p.tn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-    if (p.tn == 256) {      // 128 columns where they need less time for the last, partly filled round of CTAs
-        const i64 t256 = (M + 255) / 256 * p.tiles_n, t128 = (M + 127) / 128 * p.tiles_n;
-        if ((t128 + sms - 1) / sms < 2 * ((t256 + sms - 1) / sms)) p.tn = 128;
-    }
+    p.pair = M > NARROW_M;
+    p.tn = p.pair ? wide::BM : M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    const int units = p.pair ? sms / 2 : sms;        // that work on a tile each
+    p.tiles_n = (N + (p.pair ? wide::BN : TM) - 1) / (p.pair ? wide::BN : TM);
     p.tiles_m = static_cast<int>((M + p.tn - 1) / p.tn);
     const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
     p.splits = 1;
-    if (tiles > 0 && tiles < sms) {
-        p.splits = static_cast<int>(sms / tiles);
-        if (p.splits > p.nkb / 4) p.splits = p.nkb / 4;
-        if (p.splits < 1) p.splits = 1;
+    // Parts of the contraction: the number that needs the fewest blocks in a row, a tile's start and end counted as 4 blocks and the joining
+    // of parts as 2 and half a block per part
+    if (tiles > 0 && tiles < units) {
+        double least = 1e30;
+        for (int s = 1; s <= p.nkb / 2 && s <= 32 && tiles * s <= 4 * units; ++s) {
+            const double rounds = static_cast<double>((tiles * s + units - 1) / units);
+            const double cost = rounds * ((p.nkb + s - 1) / s + 4) + (s > 1 ? 2 + 0.5 * s : 0);
+            if (s == 1 || cost < least) least = cost, p.splits = s;
+        }
     }
-    p.part_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * TM * p.tn * 4 : 0;
+    p.part_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * (p.pair ? wide::BM * wide::BN : TM * p.tn) * 4 : 0;
     return p;
 }
 
@@ -375,9 +699,37 @@ int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, cons
     return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
+int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, const DeviceInfo& di, cudaStream_t s) {
+    static bool set[64] = {};
+    if (di.device < 0 || di.device >= 64 || !set[di.device]) {
+        if (cudaFuncSetAttribute(wide::gemm_fp8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wide::SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
+        if (di.device >= 0 && di.device < 64) set[di.device] = true;
+    }
+    const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
+    const int pairs = static_cast<int>(items < di.sm_count / 2 ? items : di.sm_count / 2);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * pairs);
+    cfg.blockDim = dim3(wide::PAIR_THREADS);
+    cfg.dynamicSmemBytes = wide::SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel, mw, mx, a) != cudaSuccess) {
+        cudaGetLastError();
+        return CAKE_ERR_CUDA;
+    }
+    note_launches(1);
+    return CAKE_OK;
+}
+
 int check_shape(i64 M, int N, int K) {
     if (M < 0 || N < 1 || K < 1 || M > INT_MAX - 1024 || N > INT_MAX - 1024 || K > INT_MAX - 1024) return CAKE_ERR_SHAPE;
-    if (((M + 127) / 128) * ((static_cast<i64>(N) + TM - 1) / TM) > INT_MAX / 2) return CAKE_ERR_SHAPE;
+    if (((M + 127) / 128) * ((static_cast<i64>(N) + TM - 1) / TM) > INT_MAX / 64) return CAKE_ERR_SHAPE;
     return CAKE_OK;
 }
 constexpr int kMaxSms = 148;      // the plan that sizes the workspace touches no device: that of a B200
@@ -421,20 +773,20 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     CUtensorMap mw, mx;
     rc = make_tmap_bytes(&mw, W, K, N, w_stride, TM);
     if (rc != CAKE_OK) return rc;
-    rc = make_tmap_bytes(&mx, X, K, M, x_stride, p.tn);
+    rc = make_tmap_bytes(&mx, X, K, M, x_stride, p.pair ? 128 : p.tn);
     if (rc != CAKE_OK) return rc;
     GemmArgs a;
     a.xs = x_scale, a.ws = w_scale, a.out = out, a.status = static_cast<int*>(ws), a.counters = static_cast<int*>(ws) + 64;
     a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes);
     a.M = M, a.out_stride = out_stride, a.N = N, a.nkb = p.nkb, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n, a.splits = p.splits;
     a.fp32 = flags & CAKE_GEMM_OUT_FP32;
+    a.out_wide = aligned(out, 16) && out_stride % (a.fp32 ? 4 : 8) == 0;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (p.pair) return launch_pair(a, mw, mx, di, s);
     switch (p.tn) {
         case 16: return launch<16>(a, mw, mx, di, s);
         case 32: return launch<32>(a, mw, mx, di, s);
-        case 64: return launch<64>(a, mw, mx, di, s);
-        case 128: return launch<128>(a, mw, mx, di, s);
-        default: return launch<256>(a, mw, mx, di, s);
+        default: return launch<64>(a, mw, mx, di, s);
     }
 }
 
