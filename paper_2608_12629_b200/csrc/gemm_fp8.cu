@@ -13,7 +13,8 @@
 //   more            X is the M side, two SMs to a 256 x 256 tile (cta_group::2: each loads half of both operands, 32 KiB a block instead
 //                   of the 48 of a 128 x 256 tile of one SM, whose demand of 94 bytes a clock the L2 does not meet).  The scale of an
 //                   element depends on its lane and on its half of the columns: one factor per thread and block, packed FMAs.
-// Where a product has too few tiles for the SMs its contraction is split; the last CTA of a tile to arrive adds up the parts.
+// Where a product has too few tiles for the SMs its contraction is split; the narrow kernel's last CTA of a
+// tile to arrive adds up the parts, the pairs of a tile share that work.
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -40,7 +41,7 @@ struct GemmArgs {
     int* status;
     i64 M, out_stride;
     int N, nkb, tiles_m, tiles_n, splits;      // tiles_m: of X's rows
-    bool fp32, out_wide;                       // out_wide: 16-byte stores
+    bool fp32, out_wide, xs_wide;              // 16-byte stores of out, loads of xs and ws
 };
 
 struct __align__(16) Ctrl {
@@ -344,11 +345,16 @@ namespace wide {
 
 constexpr int BM = 256, BN = 256;              // tile of a pair: rows of X, rows of W
 constexpr int STAGES = 6, BUFS = 2;
+constexpr int PAIR_EPI = 8;                    // epilogue warps
+constexpr int PAIR_TMA = 8, PAIR_MMA = 9, PAIR_MMA1 = 10;
+// registers: 12 warps start with 168 each; the two epilogue warpgroups take what the third gives up (2 * 232 + 40 = 3 * 168)
+constexpr int EPI_REGS = 232, AUX_REGS = 40;
+constexpr int GROUP = 4;                       // blocks whose scales are fetched together
 constexpr uint32_t HALF = 128 * KB;            // a CTA's 128 rows of one operand
 constexpr uint32_t STAGE = 2 * HALF;
-constexpr int PAIR_THREADS = 10 * 32;
+constexpr int PAIR_THREADS = 12 * 32;
 constexpr int OUT_PITCH = 80;                  // bytes of a staged row: 64 and a shift of the banks
-constexpr uint32_t OUT_BYTES = EPI_WARPS * 32 * OUT_PITCH;
+constexpr uint32_t OUT_BYTES = PAIR_EPI * 32 * OUT_PITCH;
 constexpr int COLS = 128;                      // columns of an epilogue thread
 constexpr int BAND = 8;                        // tiles of X's rows that are worked on together, for the L2
 
@@ -356,10 +362,10 @@ struct __align__(16) PairCtrl {
     uint64_t full[STAGES], empty[STAGES], tfull[BUFS], tempty[BUFS];
     uint32_t tmem;
     int abort_flag;
-    int last;
 };
 constexpr uint32_t SMEM = 1024 + STAGES * STAGE + OUT_BYTES + sizeof(PairCtrl);
 static_assert(SMEM <= 227 * 1024, "");
+static_assert(BUFS == 2, "an accumulator per issuing thread");
 
 __device__ __forceinline__ void pair_wait(uint64_t* bar, uint32_t parity, PairCtrl* ctrl, int* status) {
     const uint32_t addr = ptx::smem_u32(bar);
@@ -386,20 +392,6 @@ __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a, uint
         "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "n"(ACC ? 1 : 0)
         : "memory");
-}
-__device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ld_wait(uint32_t (&r)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-                 :: "memory");
 }
 // acc (two floats) += r * s
 __device__ __forceinline__ void fma2(float2& acc, uint32_t r0, uint32_t r1, float s) {
@@ -449,14 +441,14 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         }
         for (int i = 0; i < BUFS; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), 2 * EPI_WARPS);   // rank 0's: both CTAs' warps
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), 2 * PAIR_EPI);   // rank 0's: both CTAs' warps
         }
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&map_w);
         ptx::prefetch_tensormap(&map_x);
     }
-    if (warp == WARP_MMA) {
+    if (warp == PAIR_MMA) {
         ptx::tmem_alloc_pair(ptx::smem_u32(&ctrl->tmem), BUFS * BN);
         ptx::tmem_relinquish_pair();
     }
@@ -466,7 +458,9 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     ptx::tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
 
-    if (warp == WARP_TMA) {
+    if (warp >= PAIR_EPI) {
+    ptx::setmaxnreg_dec<AUX_REGS>();
+    if (warp == PAIR_TMA) {
         if (ptx::elect_one()) {
             uint32_t n = 0;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
@@ -488,33 +482,39 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == WARP_MMA) {
+    } else if (warp == PAIR_MMA || warp == PAIR_MMA1) {
+        // Two issuing threads (rank 0), every other block and one of the two accumulators each: an instruction is accepted at the tensor
+        // core's pace (4 x 128 clocks a block), and one thread's waits and commits on top of that (about 500 clocks) left it idle half of the time
         if (rank == 0 && ptx::elect_one()) {
+            const uint32_t mine = warp == PAIR_MMA ? 0 : 1;
             uint32_t n = 0;
             constexpr uint32_t idesc = idesc_e4m3(BM, BN);
             constexpr uint16_t BOTH = 3;
+            const uint32_t d = tmem + mine * BN;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
                 const PairItem it = pair_item(a, i);
                 for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                    const uint32_t s = n % STAGES, b = n % BUFS;
-                    pair_wait(&ctrl->tempty[b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
+                    if (n % BUFS != mine) continue;
+                    const uint32_t s = n % STAGES;
+                    pair_wait(&ctrl->tempty[mine], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
                     pair_wait(&ctrl->full[s], (n / STAGES) & 1, ctrl, a.status);
                     if (pair_aborted(ctrl)) break;
                     ptx::tc_fence_after();
                     const uint32_t base = ptx::smem_u32(tiles + s * STAGE);
                     const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + HALF);
-                    const uint32_t d = tmem + b * BN;
                     umma_pair_e4m3<false>(d, da, db, idesc);
                     umma_pair_e4m3<true>(d, da + 2, db + 2, idesc);
                     umma_pair_e4m3<true>(d, da + 4, db + 4, idesc);
                     umma_pair_e4m3<true>(d, da + 6, db + 6, idesc);
+                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[mine]), BOTH);
                     ptx::umma_pair_commit(ptx::smem_u32(&ctrl->empty[s]), BOTH);
-                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[b]), BOTH);
                 }
             }
         }
         __syncwarp();
+    }
     } else {
+        ptx::setmaxnreg_inc<EPI_REGS>();
         const int half = warp >> 2, quad = warp & 3;
         const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * COLS;
         const int local_row = quad * 32 + lane;                        // of the CTA's 128
@@ -523,80 +523,95 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         uint32_t n = 0;
         for (int i = pair; i < items; i += n_pairs) {                  // (every warp takes every step, also after an expired wait)
             const PairItem it = pair_item(a, i);
-            const i64 row = static_cast<i64>(it.m0) + rank * 128 + local_row;
-            const int block = it.n0 / 128 + half;
-            const bool live = row < a.M && block < n_blocks;
-            const float* xs = a.xs + row * a.nkb;
-            const float* ws = a.ws + static_cast<i64>(block) * a.nkb;
             float2 acc[COLS / 2];
 #pragma unroll
             for (int c = 0; c < COLS / 2; ++c) acc[c] = make_float2(0.f, 0.f);
-            float next = live ? __ldg(xs + it.kb0) * __ldg(ws + it.kb0) : 0.f;
-            for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                const uint32_t b = n % BUFS;
-                const float s = next;
-                if (live && kb + 1 < it.kb1) next = __ldg(xs + kb + 1) * __ldg(ws + kb + 1);
-                pair_wait(&ctrl->tfull[b], (n / BUFS) & 1, ctrl, a.status);
-                ptx::tc_fence_after();
-                const uint32_t t = t_lane + b * BN;
-                uint32_t r[2][16];
-                ld16(t, r[0]);
+            // The scales of four blocks at a time, one such group ahead and without a barrier: at this thread's pace (about 500 clocks a
+            // block) a wait on a barrier, even a completed one, is dearer than the loads
+            const i64 row = static_cast<i64>(it.m0) + rank * 128 + local_row;
+            const int block = it.n0 / 128 + half;
+            const bool live = row < a.M && block < n_blocks;
+            const float* const xs = a.xs + (live ? row : 0) * a.nkb;
+            const float* const ws = a.ws + static_cast<i64>(live ? block : 0) * a.nkb;
+            float xn[GROUP], wn[GROUP], sc[GROUP];
+            auto fetch = [&](int kb) {
+                if (a.xs_wide && kb % GROUP == 0 && kb + GROUP <= it.kb1) {
+                    const float4 u = __ldg(reinterpret_cast<const float4*>(xs + kb)), v = __ldg(reinterpret_cast<const float4*>(ws + kb));
+                    xn[0] = u.x, xn[1] = u.y, xn[2] = u.z, xn[3] = u.w;
+                    wn[0] = v.x, wn[1] = v.y, wn[2] = v.z, wn[3] = v.w;
+                } else {
 #pragma unroll
-                for (int c = 0; c < COLS / 16; ++c) {
-                    ld_wait(r[c & 1]);
-                    if (c + 1 < COLS / 16) {
-                        ld16(t + (c + 1) * 16, r[(c + 1) & 1]);
-                    } else {
-                        ptx::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[b]));
+                    for (int u = 0; u < GROUP; ++u) {
+                        xn[u] = kb + u < it.kb1 ? __ldg(xs + kb + u) : 0.f;
+                        wn[u] = kb + u < it.kb1 ? __ldg(ws + kb + u) : 0.f;
                     }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) fma2(acc[c * 8 + j], r[c & 1][2 * j], r[c & 1][2 * j + 1], s);
                 }
-            }
-            if (a.splits > 1) {
-                // parts as [4 columns][256 rows] of float4: 32 lanes write 512 neighbouring bytes
-                const i64 part = static_cast<i64>(BM) * BN;
-                float4* const mine = reinterpret_cast<float4*>(a.parts + i * part) + (half * (COLS / 4)) * BM + rank * 128 + local_row;
+            };
+            fetch(it.kb0);
+            // The block's 128 columns in four loads of 32, each in flight while the one before is added up; the first of the next
+            // block as well, if that block is done already
+            uint32_t r0[32], r1[32];
+            auto add = [&](int c, const uint32_t (&r)[32], float s) {
 #pragma unroll
-                for (int c = 0; c < COLS / 4; ++c)
-                    __stcg(mine + c * BM, make_float4(acc[2 * c].x, acc[2 * c].y, acc[2 * c + 1].x, acc[2 * c + 1].y));
-                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
-                if (threadIdx.x == 0) {
-                    __threadfence();
-                    int* counter = a.counters + 2 * it.tile + rank;
-                    const int seen = atomicAdd(counter, 1);
-                    ctrl->last = seen == a.splits - 1;
-                    if (ctrl->last) *counter = 0;
-                    __threadfence();
-                }
-                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
-                const bool last = ctrl->last;
-                asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");     // read by all before the next item writes it
-                if (!last) continue;
+                for (int q = 0; q < 16; ++q) fma2(acc[c * 16 + q], r[2 * q], r[2 * q + 1], s);
+            };
+            pair_wait(&ctrl->tfull[n % BUFS], (n / BUFS) & 1, ctrl, a.status);
+            ptx::tc_fence_after();
+            ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+            for (int kb0 = it.kb0; kb0 < it.kb1; kb0 += GROUP) {
 #pragma unroll
-                for (int c = 0; c < COLS / 2; ++c) acc[c] = make_float2(0.f, 0.f);
-                for (int s = 0; s < a.splits; ++s) {
-                    const float4* from = mine + static_cast<i64>(s - it.split) * (part / 4);
+                for (int u = 0; u < GROUP; ++u) sc[u] = live ? xn[u] * wn[u] : 0.f;
+                if (kb0 + GROUP < it.kb1) fetch(kb0 + GROUP);
 #pragma unroll
-                    for (int c = 0; c < COLS / 4; ++c) {
-                        const float4 u = __ldcg(from + c * BM);
-                        acc[2 * c].x += u.x, acc[2 * c].y += u.y, acc[2 * c + 1].x += u.z, acc[2 * c + 1].y += u.w;
+                for (int u = 0; u < GROUP; ++u) {
+                    const int kb = kb0 + u;
+                    if (kb >= it.kb1) break;
+                    const float s = sc[u];
+                    const uint32_t b = n % BUFS;
+                    const uint32_t t = t_lane + b * BN;
+                    ++n;
+                    uint64_t* const next = &ctrl->tfull[n % BUFS];
+                    const uint32_t parity = (n / BUFS) & 1;
+                    const bool more = kb + 1 < it.kb1;
+                    ptx::tmem_ld_wait(r0);
+                    ptx::tmem_ld_x32(t + 32, r1);
+                    add(0, r0, s);
+                    ptx::tmem_ld_wait(r1);
+                    ptx::tmem_ld_x32(t + 64, r0);
+                    add(1, r1, s);
+                    ptx::tmem_ld_wait(r0);
+                    ptx::tmem_ld_x32(t + 96, r1);
+                    const bool ready = more && ptx::mbar_test_wait(ptx::smem_u32(next), parity);
+                    add(2, r0, s);
+                    ptx::tmem_ld_wait(r1);
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[b]));
+                    if (__all_sync(0xffffffffu, ready)) {
+                        ptx::tc_fence_after();
+                        ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+                        add(3, r1, s);
+                    } else {
+                        add(3, r1, s);
+                        if (more) {
+                            pair_wait(next, parity, ctrl, a.status);
+                            ptx::tc_fence_after();
+                            ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+                        }
                     }
                 }
             }
             // ---- out: 64 bytes of each of the warp's 32 rows at a time through shared memory, so that a store instruction covers whole
             // sectors of 8 rows instead of 16 bytes of 32
-            const int col0 = it.n0 + half * COLS;
-            const i64 row0 = static_cast<i64>(it.m0) + rank * 128 + quad * 32;
+            i64 out_row0 = static_cast<i64>(it.m0) + rank * 128 + quad * 32;      // of the rows in the staging buffer
+            uint4* const put = reinterpret_cast<uint4*>(stage_out + lane * OUT_PITCH);
             auto flush = [&](int col, int per) {       // `per` elements to a row's 64 bytes
                 __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int r = k * 8 + (lane >> 2), c = lane & 3;
                     const uint4 u = *reinterpret_cast<const uint4*>(stage_out + r * OUT_PITCH + c * 16);
-                    const i64 to = row0 + r;
+                    const i64 to = out_row0 + r;
                     const int e = col + c * (per / 4);
                     if (to < a.M && e < a.N) {
                         if (a.out_wide && e + per / 4 <= a.N) {
@@ -619,26 +634,84 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 }
                 __syncwarp();
             };
-            uint4* const put = reinterpret_cast<uint4*>(stage_out + lane * OUT_PITCH);
-            if (a.fp32) {
-#pragma unroll
-                for (int c = 0; c < COLS; c += 16) {
+            // 16 float2 (fp32: 8) of this lane's row to the columns from `col` on
+            auto write = [&](const float2* f, int col) {
+                if (a.fp32) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        put[q] = make_uint4(__float_as_uint(acc[c / 2 + 2 * q].x), __float_as_uint(acc[c / 2 + 2 * q].y),
-                                            __float_as_uint(acc[c / 2 + 2 * q + 1].x), __float_as_uint(acc[c / 2 + 2 * q + 1].y));
-                    flush(col0 + c, 16);
+                        put[q] = make_uint4(__float_as_uint(f[2 * q].x), __float_as_uint(f[2 * q].y), __float_as_uint(f[2 * q + 1].x), __float_as_uint(f[2 * q + 1].y));
+                    flush(col, 16);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        put[q] = make_uint4(pack_bf16(f[4 * q].x, f[4 * q].y), pack_bf16(f[4 * q + 1].x, f[4 * q + 1].y),
+                                            pack_bf16(f[4 * q + 2].x, f[4 * q + 2].y), pack_bf16(f[4 * q + 3].x, f[4 * q + 3].y));
+                    flush(col, 32);
                 }
-            } else {
+            };
+            if (a.splits == 1) {
+                const int col0 = it.n0 + half * COLS;
+                if (a.fp32) {
 #pragma unroll
-                for (int c = 0; c < COLS; c += 32) {
+                    for (int c = 0; c < COLS; c += 16) write(acc + c / 2, col0 + c);
+                } else {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float2* f = acc + c / 2 + 4 * q;
-                        put[q] = make_uint4(pack_bf16(f[0].x, f[0].y), pack_bf16(f[1].x, f[1].y), pack_bf16(f[2].x, f[2].y), pack_bf16(f[3].x, f[3].y));
+                    for (int c = 0; c < COLS; c += 32) write(acc + c / 2, col0 + c);
+                }
+                continue;
+            }
+            // ---- parts of the contraction, as [4 columns][256 rows] of float4 (32 lanes write 512 neighbouring bytes).  The tile's CTAs of this
+            // rank (all resident: a cooperative launch of one round) wait for each other, then each adds up a share of the columns
+            const i64 part = static_cast<i64>(BM) * BN;
+            float* const tile_parts = a.parts + static_cast<i64>(it.tile) * a.splits * part;
+            float4* const mine = reinterpret_cast<float4*>(tile_parts + it.split * part) + (half * (COLS / 4)) * BM + rank * 128 + local_row;
+#pragma unroll
+            for (int c = 0; c < COLS / 4; ++c)
+                __stcg(mine + c * BM, make_float4(acc[2 * c].x, acc[2 * c].y, acc[2 * c + 1].x, acc[2 * c + 1].y));
+            int* const arrived = a.counters + 2 * it.tile + rank;
+            int* const left = arrived + kMaxCtas / 2;
+            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
+            if (threadIdx.x == 0) {
+                __threadfence();
+                atomicAdd(arrived, 1);
+                const uint64_t t0 = ptx::globaltimer_ns();
+                for (;;) {
+                    int seen;
+                    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(arrived) : "memory");
+                    if (seen >= a.splits) break;
+                    if (ptx::globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+                        atomicCAS(a.status, CAKE_OK, CAKE_ERR_TIMEOUT);
+                        break;
                     }
-                    flush(col0 + c, 32);
                 }
+                __threadfence();
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
+            const int width = a.fp32 ? 16 : 32;                            // columns of a share's unit: 64 bytes of output
+            const int units = 4 * (BN / width);
+            for (int u = it.split + a.splits * warp; u < units; u += a.splits * PAIR_EPI) {
+                // unit u: rows of quadrant u % 4, columns u / 4 -- but a warp writes 32 rows of its own staging, whichever they are
+                const int q32 = u & 3, col = (u >> 2) * width;
+                const float4* from = reinterpret_cast<const float4*>(tile_parts) + (col / 4) * BM + rank * 128 + q32 * 32 + lane;
+                float2 sum[16];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) sum[c] = make_float2(0.f, 0.f);
+                for (int s = 0; s < a.splits; ++s) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        if (4 * c < width) {
+                            const float4 v = __ldcg(from + s * (part / 4) + c * BM);
+                            sum[2 * c].x += v.x, sum[2 * c].y += v.y, sum[2 * c + 1].x += v.z, sum[2 * c + 1].y += v.w;
+                        }
+                    }
+                }
+                out_row0 = static_cast<i64>(it.m0) + rank * 128 + q32 * 32;
+                write(sum, it.n0 + col);
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
+            if (threadIdx.x == 0 && atomicAdd(left, 1) == a.splits - 1) {      // the last to leave makes both ready for the next call
+                *left = 0;
+                *arrived = 0;
             }
         }
     }
@@ -646,7 +719,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     ptx::tc_fence_before();
     __syncthreads();
     ptx::cluster_sync_all();
-    if (warp == WARP_MMA) {
+    if (warp == PAIR_MMA) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc_pair(tmem, BUFS * BN);
     }
@@ -670,13 +743,12 @@ Plan plan_of(i64 M, int N, int K, int sms) {
     p.tiles_m = static_cast<int>((M + p.tn - 1) / p.tn);
     const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
     p.splits = 1;
-    // Parts of the contraction: the number that needs the fewest blocks in a row, a tile's start and end counted as 4 blocks and the joining
-    // of parts as 2 and half a block per part
+    // Parts of the contraction, all in one round of CTAs: the number that needs the fewest blocks in a row, the joining of parts
+    // counted as 4 blocks and half a block per part
     if (tiles > 0 && tiles < units) {
         double least = 1e30;
-        for (int s = 1; s <= p.nkb / 2 && s <= 32 && tiles * s <= 4 * units; ++s) {
-            const double rounds = static_cast<double>((tiles * s + units - 1) / units);
-            const double cost = rounds * ((p.nkb + s - 1) / s + 4) + (s > 1 ? 2 + 0.5 * s : 0);
+        for (int s = 1; s <= p.nkb / 2 && s <= 32 && tiles * s <= units; ++s) {
+            const double cost = (p.nkb + s - 1) / s + (s > 1 ? 4 + 0.5 * s : 0);
             if (s == 1 || cost < least) least = cost, p.splits = s;
         }
     }
@@ -712,13 +784,16 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     cfg.blockDim = dim3(wide::PAIR_THREADS);
     cfg.dynamicSmemBytes = wide::SMEM;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeCooperative;       // CTAs that share a tile wait for each other
+    at[1].val.cooperative = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.splits > 1 ? 2 : 1;
+    if (a.splits > 1 && items > pairs) return CAKE_ERR_UNSUPPORTED;      // (a device with fewer SMs than the plan counts on)
     if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel, mw, mx, a) != cudaSuccess) {
         cudaGetLastError();
         return CAKE_ERR_CUDA;
@@ -780,6 +855,7 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes);
     a.M = M, a.out_stride = out_stride, a.N = N, a.nkb = p.nkb, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n, a.splits = p.splits;
     a.fp32 = flags & CAKE_GEMM_OUT_FP32;
+    a.xs_wide = aligned(x_scale, 16) && aligned(w_scale, 16) && p.nkb % 4 == 0;
     a.out_wide = aligned(out, 16) && out_stride % (a.fp32 ? 4 : 8) == 0;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (p.pair) return launch_pair(a, mw, mx, di, s);
