@@ -359,13 +359,13 @@ constexpr int COLS = 128;                      // columns of an epilogue thread
 constexpr int BAND = 8;                        // tiles of X's rows that are worked on together, for the L2
 
 struct __align__(16) PairCtrl {
-    uint64_t full[STAGES], empty[STAGES], tfull[BUFS], tempty[BUFS];
+    uint64_t full[STAGES], empty[STAGES], tfull[2][BUFS], tempty[2][BUFS];
     uint32_t tmem;
     int abort_flag;
 };
 constexpr uint32_t SMEM = 1024 + STAGES * STAGE + OUT_BYTES + sizeof(PairCtrl);
 static_assert(SMEM <= 227 * 1024, "");
-static_assert(BUFS == 2, "an accumulator per issuing thread");
+static_assert(2 * BUFS * (BN / 2) == 512, "all of tensor memory");
 
 __device__ __forceinline__ void pair_wait(uint64_t* bar, uint32_t parity, PairCtrl* ctrl, int* status) {
     const uint32_t addr = ptx::smem_u32(bar);
@@ -437,11 +437,11 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctrl->full[i]), 1);          // rank 0's: both CTAs' bytes
-            ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), 2);         // both issuing threads
         }
-        for (int i = 0; i < BUFS; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), 2 * PAIR_EPI);   // rank 0's: both CTAs' warps
+        for (int i = 0; i < 2 * BUFS; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i & 1][i >> 1]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i & 1][i >> 1]), PAIR_EPI);   // rank 0's: half of both CTAs' warps
         }
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
@@ -465,7 +465,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             uint32_t n = 0;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
                 const PairItem it = pair_item(a, i);
-                const int x_row = it.m0 + static_cast<int>(rank) * 128, w_row = it.n0 + static_cast<int>(rank) * 128;
+                const int x_row = it.m0 + static_cast<int>(rank) * 128, w_row = it.n0 + static_cast<int>(rank) * 64;
                 for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
                     const uint32_t s = n % STAGES;
                     pair_wait(&ctrl->empty[s], ((n / STAGES) & 1) ^ 1, ctrl, a.status);
@@ -474,6 +474,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     const uint32_t bar = at_rank0(&ctrl->full[s]), dst = ptx::smem_u32(tiles + s * STAGE);
                     ptx::tma_load_2d_pair(dst, &map_x, bar, kb * KB, x_row);
                     ptx::tma_load_2d_pair(dst + HALF, &map_w, bar, kb * KB, w_row);
+                    ptx::tma_load_2d_pair(dst + HALF + HALF / 2, &map_w, bar, kb * KB, w_row + 128);
                 }
             }
             if (pair_aborted(ctrl)) {        // give copies in flight a bounded time to land
@@ -483,30 +484,31 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         }
         __syncwarp();
     } else if (warp == PAIR_MMA || warp == PAIR_MMA1) {
-        // Two issuing threads (rank 0), every other block and one of the two accumulators each: an instruction is accepted at the tensor
-        // core's pace (4 x 128 clocks a block), and one thread's waits and commits on top of that (about 500 clocks) left it idle half of the time
+        // Two issuing threads (rank 0), one for each half of the tile's columns: an instruction is accepted at the tensor core's pace,
+        // and one thread's waits and commits on top of that left it idle.  A half of a block has accumulators of its own, so the
+        // tensor core comes back to one as soon as the four warps that read it are done.  A half's 128 rows of W lie in both
+        // CTAs, 64 each
         if (rank == 0 && ptx::elect_one()) {
-            const uint32_t mine = warp == PAIR_MMA ? 0 : 1;
+            const uint32_t half = warp == PAIR_MMA ? 0 : 1;
             uint32_t n = 0;
-            constexpr uint32_t idesc = idesc_e4m3(BM, BN);
+            constexpr uint32_t idesc = idesc_e4m3(BM, BN / 2);
             constexpr uint16_t BOTH = 3;
-            const uint32_t d = tmem + mine * BN;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
                 const PairItem it = pair_item(a, i);
                 for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                    if (n % BUFS != mine) continue;
-                    const uint32_t s = n % STAGES;
-                    pair_wait(&ctrl->tempty[mine], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
+                    const uint32_t s = n % STAGES, b = n % BUFS;
                     pair_wait(&ctrl->full[s], (n / STAGES) & 1, ctrl, a.status);
+                    pair_wait(&ctrl->tempty[half][b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
                     if (pair_aborted(ctrl)) break;
                     ptx::tc_fence_after();
+                    const uint32_t d = tmem + (half * BUFS + b) * (BN / 2);
                     const uint32_t base = ptx::smem_u32(tiles + s * STAGE);
-                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + HALF);
+                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + HALF + half * (HALF / 2));
                     umma_pair_e4m3<false>(d, da, db, idesc);
                     umma_pair_e4m3<true>(d, da + 2, db + 2, idesc);
                     umma_pair_e4m3<true>(d, da + 4, db + 4, idesc);
                     umma_pair_e4m3<true>(d, da + 6, db + 6, idesc);
-                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[mine]), BOTH);
+                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[half][b]), BOTH);
                     ptx::umma_pair_commit(ptx::smem_u32(&ctrl->empty[s]), BOTH);
                 }
             }
@@ -516,7 +518,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     } else {
         ptx::setmaxnreg_inc<EPI_REGS>();
         const int half = warp >> 2, quad = warp & 3;
-        const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * COLS;
+        const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * (BUFS * COLS);
         const int local_row = quad * 32 + lane;                        // of the CTA's 128
         uint8_t* const stage_out = staging + warp * 32 * OUT_PITCH;
         const int n_blocks = (a.N + 127) / 128;
@@ -555,9 +557,9 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 #pragma unroll
                 for (int q = 0; q < 16; ++q) fma2(acc[c * 16 + q], r[2 * q], r[2 * q + 1], s);
             };
-            pair_wait(&ctrl->tfull[n % BUFS], (n / BUFS) & 1, ctrl, a.status);
+            pair_wait(&ctrl->tfull[half][n % BUFS], (n / BUFS) & 1, ctrl, a.status);
             ptx::tc_fence_after();
-            ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+            ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
             for (int kb0 = it.kb0; kb0 < it.kb1; kb0 += GROUP) {
 #pragma unroll
                 for (int u = 0; u < GROUP; ++u) sc[u] = live ? xn[u] * wn[u] : 0.f;
@@ -568,9 +570,9 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     if (kb >= it.kb1) break;
                     const float s = sc[u];
                     const uint32_t b = n % BUFS;
-                    const uint32_t t = t_lane + b * BN;
+                    const uint32_t t = t_lane + b * COLS;
                     ++n;
-                    uint64_t* const next = &ctrl->tfull[n % BUFS];
+                    uint64_t* const next = &ctrl->tfull[half][n % BUFS];
                     const uint32_t parity = (n / BUFS) & 1;
                     const bool more = kb + 1 < it.kb1;
                     ptx::tmem_ld_wait(r0);
@@ -586,17 +588,17 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     ptx::tmem_ld_wait(r1);
                     ptx::tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[b]));
+                    if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[half][b]));
                     if (__all_sync(0xffffffffu, ready)) {
                         ptx::tc_fence_after();
-                        ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+                        ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
                         add(3, r1, s);
                     } else {
                         add(3, r1, s);
                         if (more) {
                             pair_wait(next, parity, ctrl, a.status);
                             ptx::tc_fence_after();
-                            ptx::tmem_ld_x32(t_lane + (n % BUFS) * BN, r0);
+                            ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
                         }
                     }
                 }
@@ -846,7 +848,7 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     if (rc != CAKE_OK) return rc;
     if (di.cc_major != 10) return CAKE_ERR_DEVICE;
     CUtensorMap mw, mx;
-    rc = make_tmap_bytes(&mw, W, K, N, w_stride, TM);
+    rc = make_tmap_bytes(&mw, W, K, N, w_stride, p.pair ? 64 : TM);
     if (rc != CAKE_OK) return rc;
     rc = make_tmap_bytes(&mx, X, K, M, x_stride, p.pair ? 128 : p.tn);
     if (rc != CAKE_OK) return rc;
