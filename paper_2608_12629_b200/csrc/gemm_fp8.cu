@@ -14,7 +14,7 @@
 //                   of the 48 of a 128 x 256 tile of one SM, whose demand of 94 bytes a clock the L2 does not meet).  The scale of an
 //                   element depends on its lane and on its half of the columns: one factor per thread and block, packed FMAs.
 // Where a product has too few tiles for the SMs its contraction is split; the narrow kernel's last CTA of a
-// tile to arrive adds up the parts, the pairs of a tile share that work.
+// tile to arrive adds up its (small) parts, a second kernel those of the pairs.
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -605,7 +605,12 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             }
             // ---- out: 64 bytes of each of the warp's 32 rows at a time through shared memory, so that a store instruction covers whole
             // sectors of 8 rows instead of 16 bytes of 32
-            i64 out_row0 = static_cast<i64>(it.m0) + rank * 128 + quad * 32;      // of the rows in the staging buffer
+            // (a part of a split contraction goes to the workspace instead, as a 256 x 256 matrix of its own)
+            const bool part = a.splits > 1, fp32 = part || a.fp32, wide_out = part || a.out_wide;
+            const i64 row0 = (part ? 0 : static_cast<i64>(it.m0)) + rank * 128 + quad * 32;
+            const i64 n_rows = part ? min(static_cast<i64>(BM), a.M - it.m0) : a.M, out_stride = part ? BN : a.out_stride;
+            const int n_cols = part ? BN : a.N;
+            void* const out = part ? static_cast<void*>(a.parts + static_cast<i64>(i) * (BM * BN)) : a.out;
             uint4* const put = reinterpret_cast<uint4*>(stage_out + lane * OUT_PITCH);
             auto flush = [&](int col, int per) {       // `per` elements to a row's 64 bytes
                 __syncwarp();
@@ -613,22 +618,22 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 for (int k = 0; k < 4; ++k) {
                     const int r = k * 8 + (lane >> 2), c = lane & 3;
                     const uint4 u = *reinterpret_cast<const uint4*>(stage_out + r * OUT_PITCH + c * 16);
-                    const i64 to = out_row0 + r;
+                    const i64 to = row0 + r;
                     const int e = col + c * (per / 4);
-                    if (to < a.M && e < a.N) {
-                        if (a.out_wide && e + per / 4 <= a.N) {
-                            if (a.fp32) *reinterpret_cast<uint4*>(static_cast<float*>(a.out) + to * a.out_stride + e) = u;
-                            else *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(a.out) + to * a.out_stride + e) = u;
+                    if (to < n_rows && e < n_cols) {
+                        if (wide_out && e + per / 4 <= n_cols) {
+                            if (fp32) *reinterpret_cast<uint4*>(static_cast<float*>(out) + to * out_stride + e) = u;
+                            else *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(out) + to * out_stride + e) = u;
                         } else {
                             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                if (a.fp32) {
-                                    if (e + q < a.N) static_cast<uint32_t*>(a.out)[to * a.out_stride + e + q] = w[q];
+                                if (fp32) {
+                                    if (e + q < n_cols) static_cast<uint32_t*>(out)[to * out_stride + e + q] = w[q];
                                 } else {
-                                    cake_bf16* dst = static_cast<cake_bf16*>(a.out) + to * a.out_stride + e;
-                                    if (e + 2 * q < a.N) dst[2 * q] = w[q] & 0xffff;
-                                    if (e + 2 * q + 1 < a.N) dst[2 * q + 1] = w[q] >> 16;
+                                    cake_bf16* dst = static_cast<cake_bf16*>(out) + to * out_stride + e;
+                                    if (e + 2 * q < n_cols) dst[2 * q] = w[q] & 0xffff;
+                                    if (e + 2 * q + 1 < n_cols) dst[2 * q + 1] = w[q] >> 16;
                                 }
                             }
                         }
@@ -638,7 +643,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             };
             // 16 float2 (fp32: 8) of this lane's row to the columns from `col` on
             auto write = [&](const float2* f, int col) {
-                if (a.fp32) {
+                if (fp32) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         put[q] = make_uint4(__float_as_uint(f[2 * q].x), __float_as_uint(f[2 * q].y), __float_as_uint(f[2 * q + 1].x), __float_as_uint(f[2 * q + 1].y));
@@ -651,72 +656,19 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     flush(col, 32);
                 }
             };
-            if (a.splits == 1) {
-                const int col0 = it.n0 + half * COLS;
-                if (a.fp32) {
+            {
+                const int col0 = (a.splits == 1 ? it.n0 : 0) + half * COLS;
+                if (fp32) {
 #pragma unroll
                     for (int c = 0; c < COLS; c += 16) write(acc + c / 2, col0 + c);
                 } else {
 #pragma unroll
                     for (int c = 0; c < COLS; c += 32) write(acc + c / 2, col0 + c);
                 }
-                continue;
-            }
-            // ---- parts of the contraction, as [4 columns][256 rows] of float4 (32 lanes write 512 neighbouring bytes).  The tile's CTAs of this
-            // rank (all resident: a cooperative launch of one round) wait for each other, then each adds up a share of the columns
-            const i64 part = static_cast<i64>(BM) * BN;
-            float* const tile_parts = a.parts + static_cast<i64>(it.tile) * a.splits * part;
-            float4* const mine = reinterpret_cast<float4*>(tile_parts + it.split * part) + (half * (COLS / 4)) * BM + rank * 128 + local_row;
-#pragma unroll
-            for (int c = 0; c < COLS / 4; ++c)
-                __stcg(mine + c * BM, make_float4(acc[2 * c].x, acc[2 * c].y, acc[2 * c + 1].x, acc[2 * c + 1].y));
-            int* const arrived = a.counters + 2 * it.tile + rank;
-            int* const left = arrived + kMaxCtas / 2;
-            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
-            if (threadIdx.x == 0) {
-                __threadfence();
-                atomicAdd(arrived, 1);
-                const uint64_t t0 = ptx::globaltimer_ns();
-                for (;;) {
-                    int seen;
-                    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(arrived) : "memory");
-                    if (seen >= a.splits) break;
-                    if (ptx::globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
-                        atomicCAS(a.status, CAKE_OK, CAKE_ERR_TIMEOUT);
-                        break;
-                    }
-                }
-                __threadfence();
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
-            const int width = a.fp32 ? 16 : 32;                            // columns of a share's unit: 64 bytes of output
-            const int units = 4 * (BN / width);
-            for (int u = it.split + a.splits * warp; u < units; u += a.splits * PAIR_EPI) {
-                // unit u: rows of quadrant u % 4, columns u / 4 -- but a warp writes 32 rows of its own staging, whichever they are
-                const int q32 = u & 3, col = (u >> 2) * width;
-                const float4* from = reinterpret_cast<const float4*>(tile_parts) + (col / 4) * BM + rank * 128 + q32 * 32 + lane;
-                float2 sum[16];
-#pragma unroll
-                for (int c = 0; c < 16; ++c) sum[c] = make_float2(0.f, 0.f);
-                for (int s = 0; s < a.splits; ++s) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        if (4 * c < width) {
-                            const float4 v = __ldcg(from + s * (part / 4) + c * BM);
-                            sum[2 * c].x += v.x, sum[2 * c].y += v.y, sum[2 * c + 1].x += v.z, sum[2 * c + 1].y += v.w;
-                        }
-                    }
-                }
-                out_row0 = static_cast<i64>(it.m0) + rank * 128 + q32 * 32;
-                write(sum, it.n0 + col);
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(PAIR_EPI * 32) : "memory");
-            if (threadIdx.x == 0 && atomicAdd(left, 1) == a.splits - 1) {      // the last to leave makes both ready for the next call
-                *left = 0;
-                *arrived = 0;
             }
         }
     }
+    ptx::grid_dep_launch();
     // neither CTA leaves while the other's MMAs, loads or arrivals can still reach it
     ptx::tc_fence_before();
     __syncthreads();
@@ -724,6 +676,42 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (warp == PAIR_MMA) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc_pair(tmem, BUFS * BN);
+    }
+}
+
+// Sums of the parts of a split contraction, in order; four columns to a thread.
+__global__ void __launch_bounds__(256)
+gemm_join_kernel(const GemmArgs a) {
+    ptx::grid_dep_wait();
+    const int quads = (a.N + 3) / 4;
+    const i64 total = a.M * quads;
+    for (i64 e = static_cast<i64>(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += static_cast<i64>(gridDim.x) * blockDim.x) {
+        const i64 m = e / quads;
+        const int n = 4 * static_cast<int>(e - m * quads);
+        const int tm = static_cast<int>(m / BM), tn = n / BN;
+        const int band = tm / BAND, high = min(BAND, a.tiles_m - band * BAND);
+        const i64 tile = static_cast<i64>(band) * BAND * a.tiles_n + tn * high + (tm - band * BAND);
+        const float4* from = reinterpret_cast<const float4*>(a.parts + tile * a.splits * (BM * BN) + (m - static_cast<i64>(tm) * BM) * BN + (n - tn * BN));
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+            const float4 v = __ldcg(from + static_cast<i64>(s) * (BM * BN / 4));
+            sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+        }
+        const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+        if (a.fp32) {
+            float* dst = static_cast<float*>(a.out) + m * a.out_stride + n;
+            if (a.out_wide && n + 4 <= a.N) *reinterpret_cast<float4*>(dst) = sum;
+            else
+                for (int q = 0; q < 4; ++q)
+                    if (n + q < a.N) dst[q] = f[q];
+        } else {
+            cake_bf16* dst = static_cast<cake_bf16*>(a.out) + m * a.out_stride + n;
+            if (a.out_wide && n + 4 <= a.N) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+            else
+                for (int q = 0; q < 4; ++q)
+                    if (n + q < a.N) dst[q] = to_bf16(f[q]);
+        }
     }
 }
 
@@ -786,17 +774,30 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     cfg.blockDim = dim3(wide::PAIR_THREADS);
     cfg.dynamicSmemBytes = wide::SMEM;
     cfg.stream = s;
-    cudaLaunchAttribute at[2];
+    cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeCooperative;       // CTAs that share a tile wait for each other
-    at[1].val.cooperative = 1;
     cfg.attrs = at;
-    cfg.numAttrs = a.splits > 1 ? 2 : 1;
-    if (a.splits > 1 && items > pairs) return CAKE_ERR_UNSUPPORTED;      // (a device with fewer SMs than the plan counts on)
+    cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel, mw, mx, a) != cudaSuccess) {
+        cudaGetLastError();
+        return CAKE_ERR_CUDA;
+    }
+    note_launches(1);
+    if (a.splits == 1) return CAKE_OK;
+    const i64 threads = a.M * ((a.N + 3) / 4);
+    cudaLaunchConfig_t join = {};
+    join.gridDim = dim3(static_cast<unsigned>(threads / 256 + 1 < 8 * di.sm_count ? threads / 256 + 1 : 8 * di.sm_count));
+    join.blockDim = dim3(256);
+    join.stream = s;
+    cudaLaunchAttribute pdl[1];
+    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    pdl[0].val.programmaticStreamSerializationAllowed = 1;
+    join.attrs = pdl;
+    join.numAttrs = 1;
+    if (cudaLaunchKernelEx(&join, wide::gemm_join_kernel, a) != cudaSuccess) {
         cudaGetLastError();
         return CAKE_ERR_CUDA;
     }
