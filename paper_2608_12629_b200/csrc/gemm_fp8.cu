@@ -343,29 +343,37 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 // ------------------------------------------------------------------------------------------------------ more rows: CTA pairs
 namespace wide {
 
-constexpr int BM = 256, BN = 256;              // tile of a pair: rows of X, rows of W
-constexpr int STAGES = 6, BUFS = 2;
+constexpr int BM = 256;                        // rows of X of a pair's tile
 constexpr int PAIR_EPI = 8;                    // epilogue warps
 constexpr int PAIR_TMA = 8, PAIR_MMA = 9, PAIR_MMA1 = 10;
 // registers: 12 warps start with 168 each; the two epilogue warpgroups take what the third gives up (2 * 232 + 40 = 3 * 168)
 constexpr int EPI_REGS = 232, AUX_REGS = 40;
 constexpr int GROUP = 4;                       // blocks whose scales are fetched together
-constexpr uint32_t HALF = 128 * KB;            // a CTA's 128 rows of one operand
-constexpr uint32_t STAGE = 2 * HALF;
 constexpr int PAIR_THREADS = 12 * 32;
 constexpr int OUT_PITCH = 80;                  // bytes of a staged row: 64 and a shift of the banks
 constexpr uint32_t OUT_BYTES = PAIR_EPI * 32 * OUT_PITCH;
-constexpr int COLS = 128;                      // columns of an epilogue thread
 constexpr int BAND = 8;                        // tiles of X's rows that are worked on together, for the L2
+constexpr int ACC = 128;                       // columns of an accumulator (and of an instruction); four of them fill tensor memory
+
+// BN: rows of W of a pair's tile.  256: an issuing thread and two accumulators for each half of the columns, read by a warpgroup each.
+// 128: the issuing threads take turns block by block, all epilogue warps read every accumulator.
+template <int BN>
+struct Shape {
+    static constexpr bool HALVES = BN == 256;
+    static constexpr uint32_t X_BYTES = 128 * KB, W_PART = 64 * KB;       // a CTA's 128 rows of X; its 64 rows of an instruction's W
+    static constexpr uint32_t STAGE = X_BYTES + (HALVES ? 2 : 1) * W_PART;
+    static constexpr int STAGES = HALVES ? 6 : 8;
+    static constexpr int COLS = BN / 2;                                   // columns of an epilogue thread
+};
 
 struct __align__(16) PairCtrl {
-    uint64_t full[STAGES], empty[STAGES], tfull[2][BUFS], tempty[2][BUFS];
+    uint64_t full[8], empty[8], tfull[4], tempty[4];      // accumulators 0, 1: the first issuing thread's; 2, 3: the second's
     uint32_t tmem;
     int abort_flag;
 };
-constexpr uint32_t SMEM = 1024 + STAGES * STAGE + OUT_BYTES + sizeof(PairCtrl);
-static_assert(SMEM <= 227 * 1024, "");
-static_assert(2 * BUFS * (BN / 2) == 512, "all of tensor memory");
+template <int BN>
+constexpr uint32_t pair_smem() { return 1024 + Shape<BN>::STAGES * Shape<BN>::STAGE + OUT_BYTES + sizeof(PairCtrl); }
+static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "");
 
 __device__ __forceinline__ void pair_wait(uint64_t* bar, uint32_t parity, PairCtrl* ctrl, int* status) {
     const uint32_t addr = ptx::smem_u32(bar);
@@ -384,6 +392,18 @@ __device__ __forceinline__ bool pair_aborted(PairCtrl* ctrl) { return *reinterpr
 // the same place in rank 0's shared memory
 __device__ __forceinline__ uint32_t at_rank0(const void* p) { return ptx::smem_u32(p) & ~ptx::CLUSTER_PEER_BIT; }
 
+// the first `left` elements of 16 bytes; out of line: the edges of a matrix alone take it
+__device__ __noinline__ void store_ragged(const uint4 u, uint8_t* dst, int elem, int left) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    for (int q = 0; q < 4; ++q) {
+        if (elem == 4) {
+            if (q < left) reinterpret_cast<uint32_t*>(dst)[q] = w[q];
+        } else {
+            if (2 * q < left) reinterpret_cast<uint16_t*>(dst)[2 * q] = static_cast<uint16_t>(w[q]);
+            if (2 * q + 1 < left) reinterpret_cast<uint16_t*>(dst)[2 * q + 1] = static_cast<uint16_t>(w[q] >> 16);
+        }
+    }
+}
 template <bool ACC>
 __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc) {
     asm volatile(
@@ -408,6 +428,7 @@ struct PairItem {
     int m0, n0, kb0, kb1, split, tile;
 };
 // Tiles in bands of BAND tiles of X's rows, all of W's tiles through a band; the parts of a tile next to each other.
+template <int BN>
 __device__ __forceinline__ PairItem pair_item(const GemmArgs& a, int i) {
     PairItem it;
     it.split = i % a.splits;
@@ -423,8 +444,12 @@ __device__ __forceinline__ PairItem pair_item(const GemmArgs& a, int i) {
     return it;
 }
 
+template <int BN>
 __global__ void __launch_bounds__(PAIR_THREADS, 1)
 gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const GemmArgs a) {
+    using S = Shape<BN>;
+    constexpr int STAGES = S::STAGES, COLS = S::COLS;
+    constexpr uint32_t STAGE = S::STAGE;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* const staging = tiles + STAGES * STAGE;
@@ -437,11 +462,11 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctrl->full[i]), 1);          // rank 0's: both CTAs' bytes
-            ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), 2);         // both issuing threads
+            ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), S::HALVES ? 2 : 1);     // issuing threads that read a stage
         }
-        for (int i = 0; i < 2 * BUFS; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i & 1][i >> 1]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i & 1][i >> 1]), PAIR_EPI);   // rank 0's: half of both CTAs' warps
+        for (int i = 0; i < 4; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), S::HALVES ? PAIR_EPI : 2 * PAIR_EPI);   // rank 0's: warps of both CTAs
         }
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
@@ -449,7 +474,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         ptx::prefetch_tensormap(&map_x);
     }
     if (warp == PAIR_MMA) {
-        ptx::tmem_alloc_pair(ptx::smem_u32(&ctrl->tmem), BUFS * BN);
+        ptx::tmem_alloc_pair(ptx::smem_u32(&ctrl->tmem), 4 * ACC);
         ptx::tmem_relinquish_pair();
     }
     ptx::tc_fence_before();
@@ -464,7 +489,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         if (ptx::elect_one()) {
             uint32_t n = 0;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
-                const PairItem it = pair_item(a, i);
+                const PairItem it = pair_item<BN>(a, i);
                 const int x_row = it.m0 + static_cast<int>(rank) * 128, w_row = it.n0 + static_cast<int>(rank) * 64;
                 for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
                     const uint32_t s = n % STAGES;
@@ -473,8 +498,8 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                     if (rank == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctrl->full[s]), 2 * STAGE);
                     const uint32_t bar = at_rank0(&ctrl->full[s]), dst = ptx::smem_u32(tiles + s * STAGE);
                     ptx::tma_load_2d_pair(dst, &map_x, bar, kb * KB, x_row);
-                    ptx::tma_load_2d_pair(dst + HALF, &map_w, bar, kb * KB, w_row);
-                    ptx::tma_load_2d_pair(dst + HALF + HALF / 2, &map_w, bar, kb * KB, w_row + 128);
+                    ptx::tma_load_2d_pair(dst + S::X_BYTES, &map_w, bar, kb * KB, w_row);
+                    if (S::HALVES) ptx::tma_load_2d_pair(dst + S::X_BYTES + S::W_PART, &map_w, bar, kb * KB, w_row + 128);
                 }
             }
             if (pair_aborted(ctrl)) {        // give copies in flight a bounded time to land
@@ -484,32 +509,33 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         }
         __syncwarp();
     } else if (warp == PAIR_MMA || warp == PAIR_MMA1) {
-        // Two issuing threads (rank 0), one for each half of the tile's columns: an instruction is accepted at the tensor core's pace,
-        // and one thread's waits and commits on top of that left it idle.  A half of a block has accumulators of its own, so the
-        // tensor core comes back to one as soon as the four warps that read it are done.  A half's 128 rows of W lie in both
-        // CTAs, 64 each
+        // Two issuing threads (rank 0): an instruction is accepted at the tensor core's pace, and one thread's waits and commits on top
+        // of that left it idle.  Each has two accumulators of 128 columns, so the tensor core comes back to one as soon as the warps that
+        // read it are done.  An instruction's 128 rows of W lie in both CTAs, 64 each
         if (rank == 0 && ptx::elect_one()) {
-            const uint32_t half = warp == PAIR_MMA ? 0 : 1;
-            uint32_t n = 0;
-            constexpr uint32_t idesc = idesc_e4m3(BM, BN / 2);
+            const uint32_t who = warp == PAIR_MMA ? 0 : 1;
+            uint32_t n = 0, u = 0;      // blocks; blocks that are this thread's
+            constexpr uint32_t idesc = idesc_e4m3(BM, ACC);
             constexpr uint16_t BOTH = 3;
             for (int i = pair; i < items && !pair_aborted(ctrl); i += n_pairs) {
-                const PairItem it = pair_item(a, i);
+                const PairItem it = pair_item<BN>(a, i);
                 for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                    const uint32_t s = n % STAGES, b = n % BUFS;
+                    if (!S::HALVES && (n & 1) != who) continue;
+                    const uint32_t s = n % STAGES, acc = 2 * who + (u & 1);
                     pair_wait(&ctrl->full[s], (n / STAGES) & 1, ctrl, a.status);
-                    pair_wait(&ctrl->tempty[half][b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
+                    pair_wait(&ctrl->tempty[acc], ((u >> 1) & 1) ^ 1, ctrl, a.status);
                     if (pair_aborted(ctrl)) break;
                     ptx::tc_fence_after();
-                    const uint32_t d = tmem + (half * BUFS + b) * (BN / 2);
+                    const uint32_t d = tmem + acc * ACC;
                     const uint32_t base = ptx::smem_u32(tiles + s * STAGE);
-                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + HALF + half * (HALF / 2));
+                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + S::X_BYTES + (S::HALVES ? who * S::W_PART : 0));
                     umma_pair_e4m3<false>(d, da, db, idesc);
                     umma_pair_e4m3<true>(d, da + 2, db + 2, idesc);
                     umma_pair_e4m3<true>(d, da + 4, db + 4, idesc);
                     umma_pair_e4m3<true>(d, da + 6, db + 6, idesc);
-                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[half][b]), BOTH);
+                    ptx::umma_pair_commit(ptx::smem_u32(&ctrl->tfull[acc]), BOTH);
                     ptx::umma_pair_commit(ptx::smem_u32(&ctrl->empty[s]), BOTH);
+                    ++u;
                 }
             }
         }
@@ -518,24 +544,27 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     } else {
         ptx::setmaxnreg_inc<EPI_REGS>();
         const int half = warp >> 2, quad = warp & 3;
-        const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * (BUFS * COLS);
+        const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (S::HALVES ? 0 : half * COLS);
+        // block n is in accumulator acc_of(n), completed for the round_of(n)-th time
+        auto acc_of = [&](uint32_t n) { return S::HALVES ? 2 * half + (n & 1) : 2 * (n & 1) + ((n >> 1) & 1); };
+        auto round_of = [&](uint32_t n) { return S::HALVES ? n >> 1 : n >> 2; };
         const int local_row = quad * 32 + lane;                        // of the CTA's 128
         uint8_t* const stage_out = staging + warp * 32 * OUT_PITCH;
         const int n_blocks = (a.N + 127) / 128;
         uint32_t n = 0;
         for (int i = pair; i < items; i += n_pairs) {                  // (every warp takes every step, also after an expired wait)
-            const PairItem it = pair_item(a, i);
+            const PairItem it = pair_item<BN>(a, i);
             float2 acc[COLS / 2];
 #pragma unroll
             for (int c = 0; c < COLS / 2; ++c) acc[c] = make_float2(0.f, 0.f);
             // The scales of four blocks at a time, one such group ahead and without a barrier: at this thread's pace (about 500 clocks a
             // block) a wait on a barrier, even a completed one, is dearer than the loads
             const i64 row = static_cast<i64>(it.m0) + rank * 128 + local_row;
-            const int block = it.n0 / 128 + half;
+            const int block = it.n0 / 128 + (S::HALVES ? half : 0);
             const bool live = row < a.M && block < n_blocks;
             const float* const xs = a.xs + (live ? row : 0) * a.nkb;
             const float* const ws = a.ws + static_cast<i64>(live ? block : 0) * a.nkb;
-            float xn[GROUP], wn[GROUP], sc[GROUP];
+            float xn[GROUP], wn[GROUP], sc[GROUP], s_now = 0.f;
             auto fetch = [&](int kb) {
                 if (a.xs_wide && kb % GROUP == 0 && kb + GROUP <= it.kb1) {
                     const float4 u = __ldg(reinterpret_cast<const float4*>(xs + kb)), v = __ldg(reinterpret_cast<const float4*>(ws + kb));
@@ -550,16 +579,17 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 }
             };
             fetch(it.kb0);
-            // The block's 128 columns in four loads of 32, each in flight while the one before is added up; the first of the next
-            // block as well, if that block is done already
-            uint32_t r0[32], r1[32];
-            auto add = [&](int c, const uint32_t (&r)[32], float s) {
+            // The block's columns in loads of 32, each in flight while the one before is added up; the first of the next block as well,
+            // if that block is done already
+            constexpr int LOADS = COLS / 32;
+            uint32_t r[2][32];
+            auto add = [&](int c) {
 #pragma unroll
-                for (int q = 0; q < 16; ++q) fma2(acc[c * 16 + q], r[2 * q], r[2 * q + 1], s);
+                for (int q = 0; q < 16; ++q) fma2(acc[c * 16 + q], r[c & 1][2 * q], r[c & 1][2 * q + 1], s_now);
             };
-            pair_wait(&ctrl->tfull[half][n % BUFS], (n / BUFS) & 1, ctrl, a.status);
+            pair_wait(&ctrl->tfull[acc_of(n)], round_of(n) & 1, ctrl, a.status);
             ptx::tc_fence_after();
-            ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
+            ptx::tmem_ld_x32(t_lane + acc_of(n) * ACC, r[0]);
             for (int kb0 = it.kb0; kb0 < it.kb1; kb0 += GROUP) {
 #pragma unroll
                 for (int u = 0; u < GROUP; ++u) sc[u] = live ? xn[u] * wn[u] : 0.f;
@@ -568,102 +598,86 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 for (int u = 0; u < GROUP; ++u) {
                     const int kb = kb0 + u;
                     if (kb >= it.kb1) break;
-                    const float s = sc[u];
-                    const uint32_t b = n % BUFS;
-                    const uint32_t t = t_lane + b * COLS;
+                    s_now = sc[u];
+                    const uint32_t b = acc_of(n);
+                    const uint32_t t = t_lane + b * ACC;
                     ++n;
-                    uint64_t* const next = &ctrl->tfull[half][n % BUFS];
-                    const uint32_t parity = (n / BUFS) & 1;
+                    const uint32_t nb = acc_of(n);
+                    uint64_t* const next = &ctrl->tfull[nb];
+                    const uint32_t parity = round_of(n) & 1;
                     const bool more = kb + 1 < it.kb1;
-                    ptx::tmem_ld_wait(r0);
-                    ptx::tmem_ld_x32(t + 32, r1);
-                    add(0, r0, s);
-                    ptx::tmem_ld_wait(r1);
-                    ptx::tmem_ld_x32(t + 64, r0);
-                    add(1, r1, s);
-                    ptx::tmem_ld_wait(r0);
-                    ptx::tmem_ld_x32(t + 96, r1);
-                    const bool ready = more && ptx::mbar_test_wait(ptx::smem_u32(next), parity);
-                    add(2, r0, s);
-                    ptx::tmem_ld_wait(r1);
+                    bool ready = false;
+#pragma unroll
+                    for (int c = 0; c < LOADS; ++c) {
+                        ptx::tmem_ld_wait(r[c & 1]);
+                        if (c + 1 < LOADS) {
+                            ptx::tmem_ld_x32(t + 32 * (c + 1), r[(c + 1) & 1]);
+                            if (c + 2 == LOADS) ready = more && ptx::mbar_test_wait(ptx::smem_u32(next), parity);
+                            add(c);
+                        }
+                    }
                     ptx::tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[half][b]));
+                    if (lane == 0) ptx::mbar_arrive_cluster(at_rank0(&ctrl->tempty[b]));
                     if (__all_sync(0xffffffffu, ready)) {
                         ptx::tc_fence_after();
-                        ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
-                        add(3, r1, s);
+                        ptx::tmem_ld_x32(t_lane + nb * ACC, r[0]);
+                        add(LOADS - 1);
                     } else {
-                        add(3, r1, s);
+                        add(LOADS - 1);
                         if (more) {
                             pair_wait(next, parity, ctrl, a.status);
                             ptx::tc_fence_after();
-                            ptx::tmem_ld_x32(t_lane + (n % BUFS) * COLS, r0);
+                            ptx::tmem_ld_x32(t_lane + nb * ACC, r[0]);
                         }
                     }
                 }
             }
             // ---- out: 64 bytes of each of the warp's 32 rows at a time through shared memory, so that a store instruction covers whole
-            // sectors of 8 rows instead of 16 bytes of 32
-            // (a part of a split contraction goes to the workspace instead, as a 256 x 256 matrix of its own)
-            const bool part = a.splits > 1, fp32 = part || a.fp32, wide_out = part || a.out_wide;
-            const i64 row0 = (part ? 0 : static_cast<i64>(it.m0)) + rank * 128 + quad * 32;
-            const i64 n_rows = part ? min(static_cast<i64>(BM), a.M - it.m0) : a.M, out_stride = part ? BN : a.out_stride;
+            // sectors of 8 rows instead of 16 bytes of 32.  (A part of a split contraction goes to the workspace, as a matrix of its own)
+            const bool part = a.splits > 1, fp32 = part || a.fp32;
+            const int elem = fp32 ? 4 : 2, per = 16 / elem;                 // bytes of an element, elements of 16 bytes
+            const int col0 = (part ? 0 : it.n0) + half * COLS + (lane & 3) * per;
             const int n_cols = part ? BN : a.N;
-            void* const out = part ? static_cast<void*>(a.parts + static_cast<i64>(i) * (BM * BN)) : a.out;
+            const i64 row0 = (part ? 0 : static_cast<i64>(it.m0)) + rank * 128 + quad * 32 + (lane >> 2);
+            const i64 n_rows = part ? min(static_cast<i64>(BM), a.M - it.m0) : a.M;
+            const i64 pitch = (part ? BN : a.out_stride) * elem;
+            uint8_t* const to = (part ? reinterpret_cast<uint8_t*>(a.parts + static_cast<i64>(i) * (BM * BN)) : static_cast<uint8_t*>(a.out)) +
+                                row0 * pitch + static_cast<i64>(col0) * elem;
+            const bool whole = (part || a.out_wide) && (part ? 0 : it.n0) + BN <= n_cols;
             uint4* const put = reinterpret_cast<uint4*>(stage_out + lane * OUT_PITCH);
-            auto flush = [&](int col, int per) {       // `per` elements to a row's 64 bytes
+            const uint8_t* const get = stage_out + (lane >> 2) * OUT_PITCH + (lane & 3) * 16;
+            auto flush = [&](int run) {                                     // the run-th 64 bytes of the warp's rows
                 __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int r = k * 8 + (lane >> 2), c = lane & 3;
-                    const uint4 u = *reinterpret_cast<const uint4*>(stage_out + r * OUT_PITCH + c * 16);
-                    const i64 to = row0 + r;
-                    const int e = col + c * (per / 4);
-                    if (to < n_rows && e < n_cols) {
-                        if (wide_out && e + per / 4 <= n_cols) {
-                            if (fp32) *reinterpret_cast<uint4*>(static_cast<float*>(out) + to * out_stride + e) = u;
-                            else *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(out) + to * out_stride + e) = u;
-                        } else {
-                            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                if (fp32) {
-                                    if (e + q < n_cols) static_cast<uint32_t*>(out)[to * out_stride + e + q] = w[q];
-                                } else {
-                                    cake_bf16* dst = static_cast<cake_bf16*>(out) + to * out_stride + e;
-                                    if (e + 2 * q < n_cols) dst[2 * q] = w[q] & 0xffff;
-                                    if (e + 2 * q + 1 < n_cols) dst[2 * q + 1] = w[q] >> 16;
-                                }
-                            }
-                        }
+                    const uint4 u = *reinterpret_cast<const uint4*>(get + k * 8 * OUT_PITCH);
+                    if (row0 + 8 * k < n_rows) {
+                        uint8_t* const dst = to + 8 * k * pitch + run * 64;
+                        if (whole) *reinterpret_cast<uint4*>(dst) = u;
+                        else store_ragged(u, dst, elem, n_cols - col0 - run * 4 * per);
                     }
                 }
                 __syncwarp();
             };
-            // 16 float2 (fp32: 8) of this lane's row to the columns from `col` on
-            auto write = [&](const float2* f, int col) {
+#pragma unroll
+            for (int c = 0; c < COLS / 32; ++c) {
+                const float2* f = acc + 16 * c;
                 if (fp32) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        put[q] = make_uint4(__float_as_uint(f[2 * q].x), __float_as_uint(f[2 * q].y), __float_as_uint(f[2 * q + 1].x), __float_as_uint(f[2 * q + 1].y));
-                    flush(col, 16);
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            put[q] = make_uint4(__float_as_uint(f[8 * h + 2 * q].x), __float_as_uint(f[8 * h + 2 * q].y),
+                                                __float_as_uint(f[8 * h + 2 * q + 1].x), __float_as_uint(f[8 * h + 2 * q + 1].y));
+                        flush(2 * c + h);
+                    }
                 } else {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         put[q] = make_uint4(pack_bf16(f[4 * q].x, f[4 * q].y), pack_bf16(f[4 * q + 1].x, f[4 * q + 1].y),
                                             pack_bf16(f[4 * q + 2].x, f[4 * q + 2].y), pack_bf16(f[4 * q + 3].x, f[4 * q + 3].y));
-                    flush(col, 32);
-                }
-            };
-            {
-                const int col0 = (a.splits == 1 ? it.n0 : 0) + half * COLS;
-                if (fp32) {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 16) write(acc + c / 2, col0 + c);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 32) write(acc + c / 2, col0 + c);
+                    flush(c);
                 }
             }
         }
@@ -675,11 +689,12 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     ptx::cluster_sync_all();
     if (warp == PAIR_MMA) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc_pair(tmem, BUFS * BN);
+        ptx::tmem_dealloc_pair(tmem, 4 * ACC);
     }
 }
 
 // Sums of the parts of a split contraction, in order; four columns to a thread.
+template <int BN>
 __global__ void __launch_bounds__(256)
 gemm_join_kernel(const GemmArgs a) {
     ptx::grid_dep_wait();
@@ -720,7 +735,7 @@ gemm_join_kernel(const GemmArgs a) {
 // ---------------------------------------------------------------------------------------------------------------- host
 struct Plan {
     bool pair;
-    int tn, tiles_m, tiles_n, splits, nkb;
+    int tn, bn, tiles_m, tiles_n, splits, nkb;
     size_t part_bytes;
 };
 Plan plan_of(i64 M, int N, int K, int sms) {
@@ -728,21 +743,26 @@ Plan plan_of(i64 M, int N, int K, int sms) {
     p.nkb = (K + KB - 1) / KB;
     p.pair = M > NARROW_M;
     p.tn = p.pair ? wide::BM : M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    const int units = p.pair ? sms / 2 : sms;        // that work on a tile each
-    p.tiles_n = (N + (p.pair ? wide::BN : TM) - 1) / (p.pair ? wide::BN : TM);
     p.tiles_m = static_cast<int>((M + p.tn - 1) / p.tn);
-    const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
-    p.splits = 1;
-    // Parts of the contraction, all in one round of CTAs: the number that needs the fewest blocks in a row, the joining of parts
-    // counted as 4 blocks and half a block per part
-    if (tiles > 0 && tiles < units) {
-        double least = 1e30;
-        for (int s = 1; s <= p.nkb / 2 && s <= 32 && tiles * s <= units; ++s) {
-            const double cost = (p.nkb + s - 1) / s + (s > 1 ? 4 + 0.5 * s : 0);
-            if (s == 1 || cost < least) least = cost, p.splits = s;
+    const int units = p.pair ? sms / 2 : sms;        // that work on a tile each
+    // The shape of a pair's tile, and parts of the contraction (all of them in one round): what needs the least time, counted in
+    // nanoseconds of a block (measured over 128 blocks: 510 of 256 x 256, 290 of 256 x 128), of a tile's start and end, and of
+    // writing and joining the parts.  517 x 2624 x 5120: 22.3 us in 256 x 256 tiles and two parts, 15.7 - 18.3 in 256 x 128
+    double least = 1e300;
+    for (int bn : {256, 128}) {
+        if (!p.pair && bn == 256) continue;
+        const int tiles_n = (N + bn - 1) / bn;
+        const i64 tiles = static_cast<i64>(p.tiles_m) * tiles_n;
+        const double block = !p.pair ? 150 : bn == 256 ? 510 : 290, tile = p.pair ? (bn == 256 ? 2000 : 1200) : 1000;
+        for (int s = 1; s == 1 || (s <= p.nkb / 2 && s <= 32 && tiles * s <= units); ++s) {
+            const double rounds = static_cast<double>((tiles * s + units - 1) / units);
+            double cost = rounds * ((p.nkb + s - 1) / s * block + tile);
+            if (s > 1) cost += p.pair ? 3000 + (bn == 256 ? 2000 : 1000) + 300 * s : 1500 + 250 * s;
+            if (cost < least) least = cost, p.bn = bn, p.tiles_n = tiles_n, p.splits = s;
         }
     }
-    p.part_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * (p.pair ? wide::BM * wide::BN : TM * p.tn) * 4 : 0;
+    const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
+    p.part_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * (p.pair ? wide::BM * p.bn : TM * p.tn) * 4 : 0;
     return p;
 }
 
@@ -761,10 +781,11 @@ int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, cons
     return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
+template <int BN>
 int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, const DeviceInfo& di, cudaStream_t s) {
     static bool set[64] = {};
     if (di.device < 0 || di.device >= 64 || !set[di.device]) {
-        if (cudaFuncSetAttribute(wide::gemm_fp8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wide::SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
+        if (cudaFuncSetAttribute(wide::gemm_fp8_pair_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, wide::pair_smem<BN>()) != cudaSuccess) return CAKE_ERR_CUDA;
         if (di.device >= 0 && di.device < 64) set[di.device] = true;
     }
     const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
@@ -772,7 +793,7 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * pairs);
     cfg.blockDim = dim3(wide::PAIR_THREADS);
-    cfg.dynamicSmemBytes = wide::SMEM;
+    cfg.dynamicSmemBytes = wide::pair_smem<BN>();
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -781,7 +802,7 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel, mw, mx, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel<BN>, mw, mx, a) != cudaSuccess) {
         cudaGetLastError();
         return CAKE_ERR_CUDA;
     }
@@ -797,7 +818,7 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     pdl[0].val.programmaticStreamSerializationAllowed = 1;
     join.attrs = pdl;
     join.numAttrs = 1;
-    if (cudaLaunchKernelEx(&join, wide::gemm_join_kernel, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&join, wide::gemm_join_kernel<BN>, a) != cudaSuccess) {
         cudaGetLastError();
         return CAKE_ERR_CUDA;
     }
@@ -861,7 +882,7 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     a.xs_wide = aligned(x_scale, 16) && aligned(w_scale, 16) && p.nkb % 4 == 0;
     a.out_wide = aligned(out, 16) && out_stride % (a.fp32 ? 4 : 8) == 0;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (p.pair) return launch_pair(a, mw, mx, di, s);
+    if (p.pair) return p.bn == 256 ? launch_pair<256>(a, mw, mx, di, s) : launch_pair<128>(a, mw, mx, di, s);
     switch (p.tn) {
         case 16: return launch<16>(a, mw, mx, di, s);
         case 32: return launch<32>(a, mw, mx, di, s);
