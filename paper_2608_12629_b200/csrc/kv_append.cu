@@ -35,7 +35,9 @@ __device__ __forceinline__ Place place_of(const AppendArgs& a, i64 t, bool repor
     p.pos = a.rot ? a.positions[t] : 0;
     p.rotate_ok = !a.rot || (p.pos >= 0 && p.pos < a.max_positions);
     const i64 slot = a.slots[t];
-    const i64 page = slot / a.c.page_size;
+    // (32-bit division where it will do: the 64-bit one is a hundred instructions)
+    const i64 page = (static_cast<unsigned long long>(slot) >> 32) == 0 ? static_cast<unsigned>(slot) / static_cast<unsigned>(a.c.page_size)
+                                                                        : slot / a.c.page_size;
     p.kv = p.rotate_ok && slot >= 0 && page < a.c.num_pages;
     p.page = page;
     p.off = static_cast<int>(slot - page * a.c.page_size);
@@ -52,21 +54,21 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 template <bool E4M3>
-__device__ __forceinline__ void store8(void* base, i64 at, const float (&f)[8], float scale) {
+__device__ __forceinline__ void store8(void* base, i64 at, const float (&f)[8], float inv) {      // inv: 1 / scale
     if (E4M3) {
         *reinterpret_cast<uint2*>(static_cast<cake_e4m3*>(base) + at) =
-            make_uint2(pack4_e4m3(f[0] / scale, f[1] / scale, f[2] / scale, f[3] / scale),
-                       pack4_e4m3(f[4] / scale, f[5] / scale, f[6] / scale, f[7] / scale));
+            make_uint2(pack4_e4m3(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                       pack4_e4m3(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
     } else {
         *reinterpret_cast<uint4*>(static_cast<cake_bf16*>(base) + at) = pack8(f);
     }
 }
 
 // Block (units, heads in parallel): thread (u, y) takes unit u of the heads y, y + blockDim.y, ... of the token's
-// Hq query, Hkv key and Hkv value heads.  A unit is 8 neighbouring elements, or two such runs rot/2 apart that rotate into
-// each other (PAIRS false, the first rot/16 units of a head).
+// Hq query, Hkv key and Hkv value heads, four heads' loads in flight.  A unit is 8 neighbouring elements, or two such runs rot/2
+// apart that rotate into each other (PAIRS false, the first rot/16 units of a head).
 template <bool E4M3, bool PAIRS>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(288)
 kv_append_kernel(const AppendArgs a) {
     const i64 t = blockIdx.x;
     const int u = threadIdx.x;
@@ -84,50 +86,61 @@ kv_append_kernel(const AppendArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) cs[j] = __ldg(row + N * u + j), sn[j] = __ldg(row + half + N * u + j);
     }
-    const int heads = (a.q ? a.Hq : 0);
-    for (int h = threadIdx.y; h < heads + a.c.Hkv; h += blockDim.y) {
-        const bool is_q = h < heads;
-        if (!is_q && !p.kv) continue;
-        const int g = h - heads;
-        const cake_bf16* src = is_q ? a.q + t * a.q_stride + static_cast<i64>(h) * D : a.k + t * a.k_stride + static_cast<i64>(g) * D;
-        float x[8], y[8];
-        unpack8(*reinterpret_cast<const uint4*>(src + d0), x);
-        if (two) {
-            unpack8(*reinterpret_cast<const uint4*>(src + d0 + half), y);
+    const int hq = a.q ? a.Hq : 0;
+    const int heads = hq + (p.kv ? 2 * a.c.Hkv : 0);
+    constexpr int BATCH = 4;
+    for (int h0 = threadIdx.y; h0 < heads; h0 += BATCH * blockDim.y) {
+        uint4 lo[BATCH], hi[BATCH];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float r = x[j] * cs[j] - y[j] * sn[j];
-                y[j] = y[j] * cs[j] + x[j] * sn[j];
-                x[j] = r;
+        for (int k = 0; k < BATCH; ++k) {
+            const int h = h0 + k * blockDim.y;
+            if (h >= heads) break;
+            const cake_bf16* src = h < hq ? a.q + t * a.q_stride + static_cast<i64>(h) * D
+                                 : h < hq + a.c.Hkv ? a.k + t * a.k_stride + static_cast<i64>(h - hq) * D
+                                                    : a.v + t * a.v_stride + static_cast<i64>(h - hq - a.c.Hkv) * D;
+            lo[k] = *reinterpret_cast<const uint4*>(src + d0);
+            if (two) hi[k] = *reinterpret_cast<const uint4*>(src + d0 + half);
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int h = h0 + k * blockDim.y;
+            if (h >= heads) break;
+            const bool is_q = h < hq, is_v = h >= hq + a.c.Hkv;
+            const int g = h - hq - (is_v ? a.c.Hkv : 0);
+            float x[8], y[8];
+            unpack8(lo[k], x);
+            if (two) unpack8(hi[k], y);
+            if (turns && !is_v) {
+                if (!PAIRS) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float r = x[j] * cs[j] - y[j] * sn[j];
+                        y[j] = y[j] * cs[j] + x[j] * sn[j];
+                        x[j] = r;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float r = x[2 * j] * cs[j] - x[2 * j + 1] * sn[j];
+                        x[2 * j + 1] = x[2 * j + 1] * cs[j] + x[2 * j] * sn[j];
+                        x[2 * j] = r;
+                    }
+                }
             }
-        } else if (turns) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float r = x[2 * j] * cs[j] - x[2 * j + 1] * sn[j];
-                x[2 * j + 1] = x[2 * j + 1] * cs[j] + x[2 * j] * sn[j];
-                x[2 * j] = r;
+            if (is_q) {
+                cake_bf16* dst = a.out_q + (t * a.Hq + h) * static_cast<i64>(D) + d0;
+                *reinterpret_cast<uint4*>(dst) = pack8(x);
+                if (two) *reinterpret_cast<uint4*>(dst + half) = pack8(y);
+            } else {
+                const i64 at = is_v ? p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d0
+                                    : p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride + d0;
+                const float* scale = is_v ? a.c.v_scale : a.c.k_scale;
+                const float inv = E4M3 && scale ? 1.f / __ldg(scale + g) : 1.f;
+                void* const base = is_v ? a.c.v : a.c.k;
+                store8<E4M3>(base, at, x, inv);
+                if (two) store8<E4M3>(base, at + half, y, inv);
             }
         }
-        if (is_q) {
-            cake_bf16* dst = a.out_q + (t * a.Hq + h) * static_cast<i64>(D) + d0;
-            *reinterpret_cast<uint4*>(dst) = pack8(x);
-            if (two) *reinterpret_cast<uint4*>(dst + half) = pack8(y);
-        } else {
-            const i64 at = p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride + d0;
-            const float sc = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + g) : 1.f;
-            store8<E4M3>(a.c.k, at, x, sc);
-            if (two) store8<E4M3>(a.c.k, at + half, y, sc);
-        }
-    }
-    if (!p.kv) return;
-    // values: plain runs of 8 over all threads of the block
-    const int runs = D >> 3;
-    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < a.c.Hkv * runs; i += blockDim.x * blockDim.y) {
-        const int g = i / runs, d = 8 * (i - g * runs);
-        float x[8];
-        unpack8(*reinterpret_cast<const uint4*>(a.v + t * a.v_stride + static_cast<i64>(g) * D + d), x);
-        const i64 at = p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d;
-        store8<E4M3>(a.c.v, at, x, E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + g) : 1.f);
     }
 }
 
@@ -238,8 +251,10 @@ extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k,
     const unsigned blocks = static_cast<unsigned>(T);
     if (wide) {
         const int units = pairs ? D / 8 : rot / 16 + (D - rot) / 8;
-        const int heads = (q ? Hq : 0) + cache->Hkv;
-        const int par = heads * units <= 256 ? heads : (256 + units - 1) / units;
+        const int heads = (q ? Hq : 0) + 2 * cache->Hkv;
+        // four heads to a thread where that leaves 128 threads or more
+        const int most = (heads + 3) / 4 * units >= 128 ? (heads + 3) / 4 : heads;
+        const int par = most * units <= 256 ? most : (256 + units - 1) / units;
         const dim3 block(units, par);
         if (e4m3) {
             if (pairs) kv_append_kernel<true, true><<<blocks, block, 0, s>>>(a);

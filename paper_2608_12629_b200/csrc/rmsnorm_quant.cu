@@ -26,7 +26,8 @@ struct NormArgs {
     bool by_row, norm;
 };
 
-// sum (or maximum) over the threads of a row: shuffles inside a warp, one word per warp through shared memory
+// sum (or maximum) over the threads of a row: shuffles inside a warp, then one word per warp through shared memory.  The
+// row's warps write `part` and read it after one barrier; callers alternate between two such arrays.
 template <bool MAX>
 __device__ __forceinline__ float row_reduce(float v, float* part, int warp, int first_warp, int warps) {
 #pragma unroll
@@ -35,23 +36,33 @@ __device__ __forceinline__ float row_reduce(float v, float* part, int warp, int 
         v = MAX ? fmaxf(v, u) : v + u;
     }
     if (warps == 1) return v;
-    if ((threadIdx.x & 31) == 0) part[warp] = v;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) part[warp] = v;
     __syncthreads();
-    float a = 0.f;
-    for (int i = 0; i < warps; ++i) a = MAX ? fmaxf(a, part[first_warp + i]) : a + part[first_warp + i];
-    __syncthreads();
-    return a;
+    v = lane < warps ? part[first_warp + lane] : 0.f;       // (maxima are of absolute values)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float u = __shfl_xor_sync(0xffffffffu, v, o);
+        v = MAX ? fmaxf(v, u) : v + u;
+    }
+    return v;
+}
+// 1 / scale, one unit in the last place
+__device__ __forceinline__ float recip(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // WIDE: a lane holds 8 neighbouring elements of a 256-element chunk (two groups of 128 = half a warp each); otherwise 4
 // elements 32 apart of a 128-element chunk (one group), loaded one by one: rows of any length and alignment.
 // NV: chunks per warp.  `tpr` threads (whole warps) share a row; a block holds blockDim.x / tpr rows.
-template <bool WIDE, int NV>
-__global__ void __launch_bounds__(1024)
+template <bool WIDE, int NV, int MOST_THREADS>
+__global__ void __launch_bounds__(MOST_THREADS)
 rmsnorm_quant_kernel(const NormArgs a, int tpr) {
     constexpr int E = WIDE ? 8 : 4;
     constexpr int CHUNK = 32 * E;
-    __shared__ float part[32];
+    __shared__ float part[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int warps = tpr >> 5;
     const int sub = warp / warps, w_in_row = warp - sub * warps;
@@ -92,7 +103,7 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
     }
     float rs = 1.f;
     if (a.norm) {
-        ss = row_reduce<false>(ss, part, warp, sub * warps, warps);
+        ss = row_reduce<false>(ss, part[0], warp, sub * warps, warps);
         rs = rsqrtf(ss / static_cast<float>(a.H) + a.eps);
     }
     if (a.out_r && live) {
@@ -152,8 +163,8 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         // one scale per 128 columns: half a warp (WIDE) or the warp
 #pragma unroll
         for (int o = WIDE ? 8 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const float sc = fmaxf(m / kE4M3Max, kScaleMin);
-        const float inv = 1.f / sc;
+        const float sc = fmaxf(m * (1.f / kE4M3Max), kScaleMin);
+        const float inv = recip(sc);
         if (WIDE) {
             const int c = base + lane * 8;
             if (live && c < a.H) {
@@ -172,9 +183,9 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         }
     }
     if (!a.out_q || !a.by_row) return;
-    most = row_reduce<true>(most, part, warp, sub * warps, warps);
-    const float sc = fmaxf(most / kE4M3Max, kScaleMin);
-    const float inv = 1.f / sc;
+    most = row_reduce<true>(most, part[1], warp, sub * warps, warps);
+    const float sc = fmaxf(most * (1.f / kE4M3Max), kScaleMin);
+    const float inv = recip(sc);
     if (!live) return;
     if (lane == 0 && w_in_row == 0) a.out_scale[row] = sc;
 #pragma unroll
@@ -196,14 +207,14 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
     }
 }
 
-template <bool WIDE, int NV>
+template <bool WIDE, int NV, int MOST_THREADS>
 cudaError_t launch_nv(const NormArgs& a, cudaStream_t s) {
     constexpr int CHUNK = WIDE ? 256 : 128;
     const int chunks = (a.H + CHUNK - 1) / CHUNK;
     const int warps = (chunks + NV - 1) / NV;
     const int rows = warps >= 4 ? 1 : 4 / warps;      // blocks of at least about 128 threads
     const i64 blocks = (a.T + rows - 1) / rows;
-    rmsnorm_quant_kernel<WIDE, NV><<<static_cast<unsigned>(blocks), rows * warps * 32, 0, s>>>(a, warps * 32);
+    rmsnorm_quant_kernel<WIDE, NV, MOST_THREADS><<<static_cast<unsigned>(blocks), rows * warps * 32, 0, s>>>(a, warps * 32);
     note_launches(1);
     return cudaGetLastError();
 }
@@ -240,8 +251,9 @@ extern "C" int cake_rmsnorm_quant(const cake_bf16* x, long long x_stride, const 
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (wide)
-        e = H <= 4096 ? launch_nv<true, 1>(a, s) : H <= 16384 ? launch_nv<true, 2>(a, s) : launch_nv<true, 4>(a, s);
+        e = H <= 2048 ? launch_nv<true, 1, 256>(a, s) : H <= 4096 ? launch_nv<true, 2, 256>(a, s)
+          : H <= 8192 ? launch_nv<true, 4, 256>(a, s) : H <= 16384 ? launch_nv<true, 4, 512>(a, s) : launch_nv<true, 4, 1024>(a, s);
     else
-        e = H <= 1024 ? launch_nv<false, 1>(a, s) : H <= 8192 ? launch_nv<false, 4>(a, s) : launch_nv<false, 8>(a, s);
+        e = H <= 1024 ? launch_nv<false, 1, 256>(a, s) : H <= 8192 ? launch_nv<false, 4, 512>(a, s) : launch_nv<false, 8, 1024>(a, s);
     return e == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
