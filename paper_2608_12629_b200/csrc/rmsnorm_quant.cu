@@ -54,167 +54,205 @@ __device__ __forceinline__ float recip(float x) {
     return y;
 }
 
-// WIDE: a lane holds 8 neighbouring elements of a 256-element chunk (two groups of 128 = half a warp each); otherwise 4
-// elements 32 apart of a 128-element chunk (one group), loaded one by one: rows of any length and alignment.
-// NV: chunks per warp.  `tpr` threads (whole warps) share a row; a block holds blockDim.x / tpr rows.
-template <bool WIDE, int NV, int MOST_THREADS>
-__global__ void __launch_bounds__(MOST_THREADS)
+// LOADS says how a lane's elements lie in a chunk: WIDE, 8 neighbours of a 256-element chunk (two groups of 128 = half a warp each) in one 16-byte
+// load; PAIRS, two pairs 64 apart of a 128-element chunk (one group); SINGLE, four elements 32 apart of one: rows of any length
+// and alignment.
+// NV: chunks per warp.  `tpr` threads (whole warps) share a row; a block holds blockDim.x / tpr rows and walks over
+// the matrix, the next rows' loads in flight while a row is reduced and written.
+enum { SINGLE, PAIRS, WIDE_LOADS };
+template <int LOADS, int NV, int MOST_THREADS, int PER_SM>
+__global__ void __launch_bounds__(MOST_THREADS, PER_SM)
 rmsnorm_quant_kernel(const NormArgs a, int tpr) {
+    constexpr bool WIDE = LOADS == WIDE_LOADS, PAIR = LOADS == PAIRS;
     constexpr int E = WIDE ? 8 : 4;
     constexpr int CHUNK = 32 * E;
     __shared__ float part[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int warps = tpr >> 5;
     const int sub = warp / warps, w_in_row = warp - sub * warps;
-    const i64 row = static_cast<i64>(blockIdx.x) * (blockDim.x / tpr) + sub;
-    const bool live = row < a.T;
-    float s[NV][E];
-    float ss = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int base = (v * warps + w_in_row) * CHUNK;
-        if (WIDE) {
-            const int c = base + lane * 8;
-            uint4 u = make_uint4(0, 0, 0, 0), t = u;
-            if (live && c < a.H) {
-                u = *reinterpret_cast<const uint4*>(a.x + row * a.x_stride + c);
-                if (a.r) t = *reinterpret_cast<const uint4*>(a.r + row * a.r_stride + c);
-            }
-            const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, tw[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[v][2 * j] = bf16_lo(uw[j]) + bf16_lo(tw[j]);
-                s[v][2 * j + 1] = bf16_hi(uw[j]) + bf16_hi(tw[j]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const int c = base + j * 32 + lane;
-                float f = 0.f;
-                if (live && c < a.H) {
-                    f = bf16_f(a.x[row * a.x_stride + c]);
-                    if (a.r) f += bf16_f(a.r[row * a.r_stride + c]);
-                }
-                s[v][j] = f;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < E; ++j) ss = fmaf(s[v][j], s[v][j], ss);
-    }
-    float rs = 1.f;
-    if (a.norm) {
-        ss = row_reduce<false>(ss, part[0], warp, sub * warps, warps);
-        rs = rsqrtf(ss / static_cast<float>(a.H) + a.eps);
-    }
-    if (a.out_r && live) {
+    const int per_block = blockDim.x / tpr;
+    const int col0 = w_in_row * CHUNK + lane * (WIDE ? 8 : PAIR ? 2 : 1);       // of the first chunk
+    const int step = warps * CHUNK;                                   // to the next chunk of this warp
+    uint32_t raw[NV][E];              // WIDE: x in words 0-3, r in 4-7; PAIRS: x in 0-1, r in 2-3; SINGLE: x and r of an element side by side
+    auto load = [&](i64 row) {
+        const bool live = row < a.T;
+        const cake_bf16* x = a.x + (live ? row : 0) * a.x_stride;
+        const cake_bf16* r = a.r ? a.r + (live ? row : 0) * a.r_stride : nullptr;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int base = (v * warps + w_in_row) * CHUNK;
+            const int c = col0 + v * step;
             if (WIDE) {
-                const int c = base + lane * 8;
-                if (c < a.H)
-                    *reinterpret_cast<uint4*>(a.out_r + row * a.H + c) =
-                        make_uint4(pack_bf16(s[v][0], s[v][1]), pack_bf16(s[v][2], s[v][3]), pack_bf16(s[v][4], s[v][5]),
-                                   pack_bf16(s[v][6], s[v][7]));
+                uint4 u = make_uint4(0, 0, 0, 0), t = u;
+                if (live && c < a.H) {
+                    u = *reinterpret_cast<const uint4*>(x + c);
+                    if (r) t = *reinterpret_cast<const uint4*>(r + c);
+                }
+                raw[v][0] = u.x, raw[v][1] = u.y, raw[v][2] = u.z, raw[v][3] = u.w;
+                raw[v][E - 4] = t.x, raw[v][E - 3] = t.y, raw[v][E - 2] = t.z, raw[v][E - 1] = t.w;
+            } else if (PAIR) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bool in = live && c + 64 * j < a.H;
+                    raw[v][j] = in ? *reinterpret_cast<const uint32_t*>(x + c + 64 * j) : 0u;
+                    raw[v][2 + j] = in && r ? *reinterpret_cast<const uint32_t*>(r + c + 64 * j) : 0u;
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    const int c = base + j * 32 + lane;
-                    if (c < a.H) a.out_r[row * a.H + c] = to_bf16(s[v][j]);
+                    const bool in = live && c + 32 * j < a.H;
+                    raw[v][j] = (in ? x[c + 32 * j] : 0u) | ((in && r ? static_cast<uint32_t>(r[c + 32 * j]) : 0u) << 16);
                 }
             }
         }
-    }
-    float most = 0.f;
+    };
+    i64 row = static_cast<i64>(blockIdx.x) * per_block + sub;
+    if (WIDE) load(row);
+    // (the rows of a block leave the loop together: its barriers are for all threads)
+    for (i64 first = static_cast<i64>(blockIdx.x) * per_block; first < a.T; first += static_cast<i64>(gridDim.x) * per_block) {
+        const bool live = row < a.T;
+        if (!WIDE) load(row);
+        float s[NV][E];
+        float ss = 0.f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int base = (v * warps + w_in_row) * CHUNK;
-        float y[E];
-        if (WIDE) {
-            const int c = base + lane * 8;
-            uint4 wv = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-            if (a.w && c < a.H) wv = __ldg(reinterpret_cast<const uint4*>(a.w + c));
-            const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                y[2 * j] = s[v][2 * j] * rs * bf16_lo(ww[j]);
-                y[2 * j + 1] = s[v][2 * j + 1] * rs * bf16_hi(ww[j]);
-            }
-            if (a.out_y && live && c < a.H)
-                *reinterpret_cast<uint4*>(a.out_y + row * a.H + c) =
-                    make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-        } else {
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const int c = base + j * 32 + lane;
-                const float wf = (a.w && c < a.H) ? bf16_f(__ldg(a.w + c)) : 1.f;
-                y[j] = s[v][j] * rs * wf;
-                if (a.out_y && live && c < a.H) a.out_y[row * a.H + c] = to_bf16(y[j]);
+                if (WIDE) s[v][j] = (j & 1) ? bf16_hi(raw[v][j / 2]) + bf16_hi(raw[v][E - 4 + j / 2]) : bf16_lo(raw[v][j / 2]) + bf16_lo(raw[v][E - 4 + j / 2]);
+                else if (PAIR) s[v][j] = (j & 1) ? bf16_hi(raw[v][j / 2]) + bf16_hi(raw[v][2 + j / 2]) : bf16_lo(raw[v][j / 2]) + bf16_lo(raw[v][2 + j / 2]);
+                else s[v][j] = bf16_lo(raw[v][j]) + bf16_hi(raw[v][j]);
+                ss = fmaf(s[v][j], s[v][j], ss);
+            }
+        const i64 now = row;
+        row += static_cast<i64>(gridDim.x) * per_block;
+        if (WIDE && first + static_cast<i64>(gridDim.x) * per_block < a.T) load(row);
+        if (a.out_r && live) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = col0 + v * step;
+                if (WIDE) {
+                    if (c < a.H)
+                        *reinterpret_cast<uint4*>(a.out_r + now * a.H + c) =
+                            make_uint4(pack_bf16(s[v][0], s[v][1]), pack_bf16(s[v][2], s[v][3]), pack_bf16(s[v][E - 4], s[v][E - 3]),
+                                       pack_bf16(s[v][E - 2], s[v][E - 1]));
+                } else if (PAIR) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (c + 64 * j < a.H) *reinterpret_cast<uint32_t*>(a.out_r + now * a.H + c + 64 * j) = pack_bf16(s[v][2 * j], s[v][2 * j + 1]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (c + 32 * j < a.H) a.out_r[now * a.H + c + 32 * j] = to_bf16(s[v][j]);
+                }
             }
         }
-        float m = 0.f;
+        // s becomes s * w; y is that times rs, which is applied to the group's maximum and with the scale instead of element by element
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            m = fmaxf(m, fabsf(y[j]));
-            s[v][j] = y[j];
-        }
-        most = fmaxf(most, m);
-        if (!a.out_q || a.by_row) continue;
-        // one scale per 128 columns: half a warp (WIDE) or the warp
+        for (int v = 0; v < NV; ++v) {
+            const int c = col0 + v * step;
+            if (!a.w) continue;
+            if (WIDE) {
+                uint4 wv = make_uint4(0, 0, 0, 0);
+                if (c < a.H) wv = __ldg(reinterpret_cast<const uint4*>(a.w + c));
+                const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
 #pragma unroll
-        for (int o = WIDE ? 8 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const float sc = fmaxf(m * (1.f / kE4M3Max), kScaleMin);
-        const float inv = recip(sc);
-        if (WIDE) {
-            const int c = base + lane * 8;
-            if (live && c < a.H) {
-                *reinterpret_cast<uint2*>(a.out_q + row * a.H + c) =
-                    make_uint2(pack4_e4m3(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                               pack4_e4m3(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
-                if ((lane & 15) == 0) a.out_scale[row * a.n_scales + (c >> 7)] = sc;
-            }
-        } else if (live && base < a.H) {
+                for (int j = 0; j < E; ++j) s[v][j] *= (j & 1) ? bf16_hi(ww[j / 2]) : bf16_lo(ww[j / 2]);
+            } else if (PAIR) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const int c = base + j * 32 + lane;
-                if (c < a.H) a.out_q[row * a.H + c] = static_cast<cake_e4m3>(pack_e4m3(y[j] * inv, 0.f) & 0xff);
-            }
-            if (lane == 0) a.out_scale[row * a.n_scales + (base >> 7)] = sc;
-        }
-    }
-    if (!a.out_q || !a.by_row) return;
-    most = row_reduce<true>(most, part[1], warp, sub * warps, warps);
-    const float sc = fmaxf(most * (1.f / kE4M3Max), kScaleMin);
-    const float inv = recip(sc);
-    if (!live) return;
-    if (lane == 0 && w_in_row == 0) a.out_scale[row] = sc;
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t w = c + 64 * j < a.H ? __ldg(reinterpret_cast<const uint32_t*>(a.w + c + 64 * j)) : 0u;
+                    s[v][2 * j] *= bf16_lo(w), s[v][2 * j + 1] *= bf16_hi(w);
+                }
+            } else {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int base = (v * warps + w_in_row) * CHUNK;
-        if (WIDE) {
-            const int c = base + lane * 8;
-            if (c < a.H)
-                *reinterpret_cast<uint2*>(a.out_q + row * a.H + c) =
-                    make_uint2(pack4_e4m3(s[v][0] * inv, s[v][1] * inv, s[v][2] * inv, s[v][3] * inv),
-                               pack4_e4m3(s[v][4] * inv, s[v][5] * inv, s[v][6] * inv, s[v][7] * inv));
-        } else {
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const int c = base + j * 32 + lane;
-                if (c < a.H) a.out_q[row * a.H + c] = static_cast<cake_e4m3>(pack_e4m3(s[v][j] * inv, 0.f) & 0xff);
+                for (int j = 0; j < E; ++j) s[v][j] *= c + 32 * j < a.H ? bf16_f(__ldg(a.w + c + 32 * j)) : 0.f;
             }
         }
+        float rs = 1.f;
+        if (a.norm) {
+            ss = row_reduce<false>(ss, part[0], warp, sub * warps, warps);
+            rs = rsqrtf(ss / static_cast<float>(a.H) + a.eps);
+        }
+        float most = 0.f;
+        auto write_q = [&](int v, float f) {           // f: rs / scale
+            const int c = col0 + v * step;
+            if (WIDE) {
+                if (c < a.H)
+                    *reinterpret_cast<uint2*>(a.out_q + now * a.H + c) =
+                        make_uint2(pack4_e4m3(s[v][0] * f, s[v][1] * f, s[v][2] * f, s[v][3] * f),
+                                   pack4_e4m3(s[v][E - 4] * f, s[v][E - 3] * f, s[v][E - 2] * f, s[v][E - 1] * f));
+            } else if (PAIR) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (c + 64 * j < a.H)
+                        *reinterpret_cast<uint16_t*>(a.out_q + now * a.H + c + 64 * j) = static_cast<uint16_t>(pack_e4m3(s[v][2 * j] * f, s[v][2 * j + 1] * f));
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (c + 32 * j < a.H) a.out_q[now * a.H + c + 32 * j] = static_cast<cake_e4m3>(pack_e4m3(s[v][j] * f, 0.f) & 0xff);
+            }
+        };
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col0 + v * step;
+            if (a.out_y && live) {
+                if (WIDE) {
+                    if (c < a.H)
+                        *reinterpret_cast<uint4*>(a.out_y + now * a.H + c) =
+                            make_uint4(pack_bf16(s[v][0] * rs, s[v][1] * rs), pack_bf16(s[v][2] * rs, s[v][3] * rs),
+                                       pack_bf16(s[v][E - 4] * rs, s[v][E - 3] * rs), pack_bf16(s[v][E - 2] * rs, s[v][E - 1] * rs));
+                } else if (PAIR) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (c + 64 * j < a.H)
+                            *reinterpret_cast<uint32_t*>(a.out_y + now * a.H + c + 64 * j) = pack_bf16(s[v][2 * j] * rs, s[v][2 * j + 1] * rs);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (c + 32 * j < a.H) a.out_y[now * a.H + c + 32 * j] = to_bf16(s[v][j] * rs);
+                }
+            }
+            if (!a.out_q) continue;
+            float m = 0.f;
+#pragma unroll
+            for (int j = 0; j < E; ++j) m = fmaxf(m, fabsf(s[v][j]));
+            if (a.by_row) {
+                most = fmaxf(most, m);
+                continue;
+            }
+            // one scale per 128 columns: half a warp (WIDE) or the warp
+#pragma unroll
+            for (int o = WIDE ? 8 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float sc = fmaxf(m * rs * (1.f / kE4M3Max), kScaleMin);
+            if (live) {
+                write_q(v, rs * recip(sc));
+                if (WIDE ? ((lane & 15) == 0 && c < a.H) : (lane == 0 && c < a.H)) a.out_scale[now * a.n_scales + (c >> 7)] = sc;
+            }
+        }
+        if (a.out_q && a.by_row) {
+            most = row_reduce<true>(most, part[1], warp, sub * warps, warps);
+            const float sc = fmaxf(most * rs * (1.f / kE4M3Max), kScaleMin);
+            if (live) {
+                const float f = rs * recip(sc);
+                if (lane == 0 && w_in_row == 0) a.out_scale[now] = sc;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) write_q(v, f);
+            }
+        }
+        // a row's second barrier (by_row) or the next row's first one separates the reads of `part` from its next writes only if there
+        // are two per row; with one, the rows would race
+        if (warps > 1 && !(a.norm && a.out_q && a.by_row)) __syncthreads();
     }
 }
 
-template <bool WIDE, int NV, int MOST_THREADS>
-cudaError_t launch_nv(const NormArgs& a, cudaStream_t s) {
-    constexpr int CHUNK = WIDE ? 256 : 128;
+template <int LOADS, int NV, int MOST_THREADS, int PER_SM>
+cudaError_t launch_nv(const NormArgs& a, const DeviceInfo& di, cudaStream_t s) {
+    constexpr int CHUNK = LOADS == WIDE_LOADS ? 256 : 128;
     const int chunks = (a.H + CHUNK - 1) / CHUNK;
     const int warps = (chunks + NV - 1) / NV;
     const int rows = warps >= 4 ? 1 : 4 / warps;      // blocks of at least about 128 threads
     const i64 blocks = (a.T + rows - 1) / rows;
-    rmsnorm_quant_kernel<WIDE, NV, MOST_THREADS><<<static_cast<unsigned>(blocks), rows * warps * 32, 0, s>>>(a, warps * 32);
+    const i64 resident = static_cast<i64>(di.sm_count) * PER_SM * (MOST_THREADS / (rows * warps * 32));
+    rmsnorm_quant_kernel<LOADS, NV, MOST_THREADS, PER_SM><<<static_cast<unsigned>(blocks < resident ? blocks : resident), rows * warps * 32, 0, s>>>(a, warps * 32);
     note_launches(1);
     return cudaGetLastError();
 }
@@ -249,11 +287,19 @@ extern "C" int cake_rmsnorm_quant(const cake_bf16* x, long long x_stride, const 
     const bool wide = H % 8 == 0 && x_stride % 8 == 0 && aligned(x, 16) && (!residual || (residual_stride % 8 == 0 && aligned(residual, 16))) &&
                       aligned(weight, 16) && aligned(out_residual, 16) && aligned(out_y, 16) && aligned(out_q, 8);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const bool pairs = H % 2 == 0 && x_stride % 2 == 0 && aligned(x, 4) && (!residual || (residual_stride % 2 == 0 && aligned(residual, 4))) &&
+                       aligned(weight, 4) && aligned(out_residual, 4) && aligned(out_y, 4) && aligned(out_q, 2);
     cudaError_t e;
+    // 1,024 threads an SM with 64 registers: two chunks of a row per warp and their successors
     if (wide)
-        e = H <= 2048 ? launch_nv<true, 1, 256>(a, s) : H <= 4096 ? launch_nv<true, 2, 256>(a, s)
-          : H <= 8192 ? launch_nv<true, 4, 256>(a, s) : H <= 16384 ? launch_nv<true, 4, 512>(a, s) : launch_nv<true, 4, 1024>(a, s);
+        e = H <= 1024 ? launch_nv<WIDE_LOADS, 1, 128, 10>(a, di, s) : H <= 4096 ? launch_nv<WIDE_LOADS, 2, 256, 4>(a, di, s)
+          : H <= 8192 ? launch_nv<WIDE_LOADS, 2, 512, 2>(a, di, s) : H <= 16384 ? launch_nv<WIDE_LOADS, 2, 1024, 1>(a, di, s)
+                                                                                : launch_nv<WIDE_LOADS, 4, 1024, 1>(a, di, s);
+    else if (pairs)
+        e = H <= 1024 ? launch_nv<PAIRS, 1, 256, 6>(a, di, s) : H <= 4096 ? launch_nv<PAIRS, 4, 256, 4>(a, di, s)
+          : H <= 8192 ? launch_nv<PAIRS, 4, 512, 2>(a, di, s) : launch_nv<PAIRS, 8, 1024, 1>(a, di, s);
     else
-        e = H <= 1024 ? launch_nv<false, 1, 256>(a, s) : H <= 8192 ? launch_nv<false, 4, 512>(a, s) : launch_nv<false, 8, 1024>(a, s);
+        e = H <= 1024 ? launch_nv<SINGLE, 1, 256, 6>(a, di, s) : H <= 4096 ? launch_nv<SINGLE, 4, 256, 4>(a, di, s)
+          : H <= 8192 ? launch_nv<SINGLE, 4, 512, 2>(a, di, s) : launch_nv<SINGLE, 8, 1024, 1>(a, di, s);
     return e == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
