@@ -113,26 +113,11 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ void ldmatrix_trans(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-// Four e4m3 values to two pairs of f16: `even` = bytes 0 and 2, `odd` = bytes 1 and 3.  The seven magnitude bits moved to bits
-// 7..13 are the value / 256 in f16 (its subnormals included; the factor is left to the caller), all in integer instructions: the conversion
-// instruction runs at a fraction of their rate (a pass over 8-bit keys was bound by it: 271 us against 106 us of memory
-// traffic).  NaN (magnitude 0x7f) would read 1.875: `most` keeps the largest magnitudes seen, 0x3f80 tells.
-__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& even, uint32_t& odd, uint32_t& most) {
-    const uint32_t mo = (w >> 1) & 0x3f803f80u, me = (w << 7) & 0x3f803f80u;
-    odd = mo | (w & 0x80008000u);
-    even = me | ((w << 8) & 0x80008000u);
-    most = __vimax3_u16x2(most, mo, me);
-}
-__device__ __forceinline__ bool holds_nan(uint32_t most) { return (most & 0xffffu) == 0x3f80u || (most >> 16) == 0x3f80u; }
-// the same with NaN kept, for the steps that hold one
-__device__ __forceinline__ void e4m3_to_f16_nan(uint32_t w, uint32_t& even, uint32_t& odd) {
-    uint32_t none = 0;
-    e4m3_to_f16(w, even, odd, none);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (((w >> (16 * h)) & 0x7fu) == 0x7fu) even |= 0x7e00u << (16 * h);
-        if (((w >> (16 * h + 8)) & 0x7fu) == 0x7fu) odd |= 0x7e00u << (16 * h);
-    }
+// four e4m3 values to two pairs of f16: exact
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    const uint16_t a = static_cast<uint16_t>(w & 0xffffu), b = static_cast<uint16_t>(w >> 16);
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"(a));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(b));
 }
 
 // tokens of sequence b and key-value head g that are attended to: [first, first + count)
@@ -255,6 +240,11 @@ paged_decode_kernel(const DecodeArgs a) {
     const i64 page_bytes = (is_v ? a.c.v_page_stride : a.c.k_page_stride) * L::ELEM;
     const i64 token_bytes = (is_v ? a.c.v_token_stride : a.c.k_token_stride) * L::ELEM;
     const unsigned page_size = a.c.page_size;
+    // a token's page and place in it; powers of two (almost every cache) without the division's twenty instructions
+    const bool pow2 = (page_size & (page_size - 1)) == 0;
+    const int page_shift = 31 - __clz(page_size);
+    auto page_of = [&](int key) -> unsigned { return pow2 ? static_cast<unsigned>(key) >> page_shift : static_cast<unsigned>(key) / page_size; };
+    auto place_of = [&](int key) -> unsigned { return pow2 ? static_cast<unsigned>(key) & (page_size - 1) : static_cast<unsigned>(key) % page_size; };
     const uint32_t v_read = ring + L::K_BYTES + ((lane & 7) + ((lane >> 4) << 3)) * L::V_PITCH + ((lane >> 3) & 1) * 16;
     const uint32_t k_read = ring + g8 * L::K_PITCH + t4 * L::VK;
 
@@ -273,7 +263,7 @@ paged_decode_kernel(const DecodeArgs a) {
         // the table entry of this lane's key of a step; -1: no such key
         auto page_at = [&](int step) -> int {
             const int key = key0 + step * TILE;
-            return (step < n_tiles && key < end) ? __ldg(table + static_cast<unsigned>(key) / page_size) : -1;
+            return (step < n_tiles && key < end) ? __ldg(table + page_of(key)) : -1;
         };
         // fetches a step; returns the mask of its keys that are there
         auto copy = [&](int step, int entry, uint32_t s) -> uint32_t {
@@ -284,7 +274,7 @@ paged_decode_kernel(const DecodeArgs a) {
             if (asked && !there) raise_bad_index(a.status);
             if (!L::BULK) {
                 if (mask != 0) {
-                    const unsigned off = static_cast<unsigned>(key) % page_size;
+                    const unsigned off = place_of(key);
                     const uint64_t mine = reinterpret_cast<uint64_t>(base + (there ? entry * page_bytes + off * token_bytes : 0));
                     const uint32_t stage = ring + s * L::STAGE;
 #pragma unroll
@@ -303,7 +293,7 @@ paged_decode_kernel(const DecodeArgs a) {
             const uint32_t bar = bar0 + 8 * s;
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2 * __popc(mask) * L::ROW);
             if (there) {
-                const unsigned off = static_cast<unsigned>(key) % page_size;
+                const unsigned off = place_of(key);
                 ptx::bulk_load(row_dst + s * L::STAGE, base + entry * page_bytes + off * token_bytes, L::ROW, bar);
             } else if (is_v) {
                 // 0 * v has to be 0 for a value that is not there; ordered ahead of a later copy to the same place
@@ -368,12 +358,7 @@ paged_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int c = 0; c < L::CK; ++c)
 #pragma unroll
-                    for (int j = 0; j < EL / 2; j += 2) {
-                    // in the order of the keys' conversion: elements 0 and 2, then 1 and 3, of every four
-                    const uint32_t u = w[c][j], v = w[c][j + 1];
-                    w[c][j] = pack_f16(bf16_lo(u) * down, bf16_lo(v) * down);
-                    w[c][j + 1] = pack_f16(bf16_hi(u) * down, bf16_hi(v) * down);
-                }
+                    for (int j = 0; j < EL / 2; ++j) w[c][j] = pack_f16(bf16_lo(w[c][j]) * down, bf16_hi(w[c][j]) * down);
             }
 #pragma unroll
             for (int c = 0; c < L::CK; ++c)
@@ -382,7 +367,7 @@ paged_decode_kernel(const DecodeArgs a) {
             const float ks = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + e.g) : 1.f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                factor[n][i] = a.scale * LOG2E * ks * (E4M3 ? 256.f : 1.f) * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
+                factor[n][i] = a.scale * LOG2E * ks * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
         }
 
         float o[D / 16][NT][4];      // O^T: per 16 values of d, (d, head 2t4), (d, head 2t4+1), (d', ...), (d', ...)
@@ -427,43 +412,32 @@ paged_decode_kernel(const DecodeArgs a) {
             // ---- scores of 16 keys
             float x[NT][4];
             const uint32_t k_at = k_read + here * L::STAGE;
-            bool careful = false;        // 8-bit: a NaN among the keys, keep it
-            for (;;) {
-                uint32_t most = 0;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
+                for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
 #pragma unroll
-                for (int c = 0; c < L::CK; ++c) {
-                    uint32_t k0[L::VK / 4], k1[L::VK / 4];
-                    lds<L::VK>(k_at + c * 4 * L::VK, k0);
-                    lds<L::VK>(k_at + 8 * L::K_PITCH + c * 4 * L::VK, k1);
-                    if (E4M3) {
+            for (int c = 0; c < L::CK; ++c) {
+                uint32_t k0[L::VK / 4], k1[L::VK / 4];
+                lds<L::VK>(k_at + c * 4 * L::VK, k0);
+                lds<L::VK>(k_at + 8 * L::K_PITCH + c * 4 * L::VK, k1);
+                if (E4M3) {
 #pragma unroll
-                        for (int j = 0; j < L::VK / 4; ++j) {
-                            uint32_t f[4];
-                            if (careful) {
-                                e4m3_to_f16_nan(k0[j], f[0], f[2]);
-                                e4m3_to_f16_nan(k1[j], f[1], f[3]);
-                            } else {
-                                e4m3_to_f16(k0[j], f[0], f[2], most);
-                                e4m3_to_f16(k1[j], f[1], f[3], most);
-                            }
+                    for (int j = 0; j < L::VK / 4; ++j) {
+                        uint32_t f[4];
+                        e4m3_to_f16(k0[j], f[0], f[2]);
+                        e4m3_to_f16(k1[j], f[1], f[3]);
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) mma<true>(x[n], f, qf[n][c * (L::VK / 4) + j][0], qf[n][c * (L::VK / 4) + j][1]);
-                        }
-                    } else {
+                        for (int n = 0; n < NT; ++n) mma<true>(x[n], f, qf[n][c * (L::VK / 4) + j][0], qf[n][c * (L::VK / 4) + j][1]);
+                    }
+                } else {
 #pragma unroll
-                        for (int j = 0; j < L::VK / 8; ++j) {
-                            const uint32_t f[4] = {k0[2 * j], k1[2 * j], k0[2 * j + 1], k1[2 * j + 1]};
+                    for (int j = 0; j < L::VK / 8; ++j) {
+                        const uint32_t f[4] = {k0[2 * j], k1[2 * j], k0[2 * j + 1], k1[2 * j + 1]};
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) mma<false>(x[n], f, qf[n][c * (L::VK / 8) + j][0], qf[n][c * (L::VK / 8) + j][1]);
-                        }
+                        for (int n = 0; n < NT; ++n) mma<false>(x[n], f, qf[n][c * (L::VK / 8) + j][0], qf[n][c * (L::VK / 8) + j][1]);
                     }
                 }
-                if (!E4M3 || careful || !__any_sync(0xffffffffu, holds_nan(most))) break;
-                careful = true;
             }
 
             // ---- running maximum and sum.  The maximum that is subtracted may lag behind the true one by up to SLACK (p stays below
@@ -520,44 +494,21 @@ paged_decode_kernel(const DecodeArgs a) {
             }
 
             // ---- weighted sum of 16 values: 32 bytes of each at a time
-            if (E4M3) {
-                // of v: [0], [2] elements (d, d+1) of two keys each, d = 32j + 2 g8; [1], [3] 16 further on; even bytes are d, odd ones d+1
-                constexpr int RUN = L::ROW / 32 < 4 ? L::ROW / 32 : 4;
 #pragma unroll
-                for (int j0 = 0; j0 < L::ROW / 32; j0 += RUN) {
-                    uint32_t v[4], f[RUN][2][4], most = 0;
+            for (int j = 0; j < L::ROW / 32; ++j) {
+                uint32_t v[4];
+                ldmatrix_trans(v_read + here * L::STAGE + j * 32, v);
+                if (E4M3) {
+                    // v[0], v[2]: elements (d, d+1) of two keys each, d = 32j + 2 g8; v[1], v[3]: 16 further on
 #pragma unroll
-                    for (int j = 0; j < RUN; ++j) {
-                        ldmatrix_trans(v_read + here * L::STAGE + (j0 + j) * 32, v);
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t f[4];
+                        e4m3_to_f16(__byte_perm(v[i], 0, 0x3120), f[0], f[1]);
+                        e4m3_to_f16(__byte_perm(v[2 + i], 0, 0x3120), f[2], f[3]);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            e4m3_to_f16(v[i], f[j][i][0], f[j][i][1], most);
-                            e4m3_to_f16(v[2 + i], f[j][i][2], f[j][i][3], most);
-                        }
+                        for (int n = 0; n < NT; ++n) mma<true>(o[2 * j + i][n], f, ph[n][0], ph[n][1]);
                     }
-                    if (__any_sync(0xffffffffu, holds_nan(most))) {
-#pragma unroll
-                        for (int j = 0; j < RUN; ++j) {
-                            ldmatrix_trans(v_read + here * L::STAGE + (j0 + j) * 32, v);
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                e4m3_to_f16_nan(v[i], f[j][i][0], f[j][i][1]);
-                                e4m3_to_f16_nan(v[2 + i], f[j][i][2], f[j][i][3]);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < RUN; ++j)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) mma<true>(o[2 * (j0 + j) + i][n], f[j][i], ph[n][0], ph[n][1]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < L::ROW / 32; ++j) {
-                    uint32_t v[4];
-                    ldmatrix_trans(v_read + here * L::STAGE + j * 32, v);
+                } else {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         mma<false>(o[j][n], v, ph[n][0], ph[n][1]);
@@ -566,7 +517,6 @@ paged_decode_kernel(const DecodeArgs a) {
                 }
             }
         }
-
         if (!L::BULK) cp_wait<0>();
 
         // ---- the warps' parts: maxima and sums first, then the weighted sums through the ring's memory
@@ -605,7 +555,7 @@ paged_decode_kernel(const DecodeArgs a) {
         const bool whole = tile0 == 0 && n_tiles == e.tiles;
         constexpr int PART = HEADS * (D + 4);            // floats of a part: O of the run's heads, then m and l (and padding)
         float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
-        const float vs = !E4M3 ? 1.f : (a.c.v_scale ? 256.f * __ldg(a.c.v_scale + e.g) : 256.f);
+        const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
         auto finish = [&](int h, int d, const float4& acc, float top, float sum) {
             const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
