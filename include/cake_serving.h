@@ -120,7 +120,8 @@ CAKE_API int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, l
  *   out         [B][Hq][D] bf16 contiguous, out;   out_lse [B][Hq] fp32, out, may be NULL: log of the sum of exponentials
  *   ws          at least cake_paged_decode_workspace_bytes(...) bytes
  * A row without tokens (length zero, or none that weighs anything) gives zeros, and -inf in out_lse.  Scores, their maximum and sum, and the weighted sum of
- * values are held in 32 bits; memory behind the last token is never read.  One launch; the result does not depend on timing.
+ * values are held in 32 bits; memory behind the last token is never read.  One launch, or two where few sequences are split
+ * into many parts; the result does not depend on timing.
  */
 CAKE_API int cake_paged_decode_workspace_bytes(long long B, int Hq, int Hkv, int D, size_t* out_bytes);
 CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_paged_cache* cache,

@@ -1,4 +1,4 @@
-// Attention of one new token per sequence over a paged cache, split over the cache's length and joined, in one launch.
+// Attention of one new token per sequence over a paged cache, split over the cache's length and joined.
 //
 //   out = sum_t exp(x_t - m) v_t / sum_t exp(x_t - m),   x_t = scale * q . k_t,   m = max_t x_t
 //
@@ -7,8 +7,8 @@
 // value is read once, so everything here serves to keep loads in flight.
 //
 // Work is the list of 64-key tiles of all (sequence, key-value head) entries, one after the other; CTA c of n takes tiles
-// [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined by the last of
-// them to arrive, from parts in the workspace, in the order of the CTAs.
+// [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined from parts
+// in the workspace, in the order of the CTAs: by the last of them to arrive, or by a second kernel where that would be many parts for one SM.
 //
 // A warp works on 16 keys at a time, with a ring of its own in shared memory and no barrier between warps.  Long rows are
 // fetched by one instruction of the warp a step: each lane copies one row (bulk copy; lanes 0-15 the keys, 16-31 the values); short
@@ -37,6 +37,12 @@ constexpr float NEG_INF = -INFINITY;
 constexpr float SLACK = 8.f;
 constexpr int WAIT_TRIES = 100000;       // of 20 us each
 
+// an entry that several CTAs share
+struct Split {
+    int b, g, run, c0, c1, slot0;    // the CTAs, and which of the first one's two parts is the entry's (0 of all others)
+    int pad[2];
+};
+
 struct DecodeArgs {
     cake_paged_cache c;
     const cake_bf16* q;
@@ -47,6 +53,9 @@ struct DecodeArgs {
     int* status;
     int* counters;
     float* parts;
+    struct Split* splits;
+    int* n_splits;                   // entries in `splits`; [1]: join blocks that are done
+    bool defer;                      // entries that several CTAs share are joined by a second kernel
     i64 q_stride, q_head_stride, table_stride, table_head_stride, lens_stride, lens_head_stride;
     bool q_wide, out_wide;           // 16-byte loads of q, 8-byte stores of out
     int B, Hq, G, chunks, max_pages, window;   // chunks: runs of at most 8 * NT query heads of a key-value head
@@ -134,11 +143,113 @@ __device__ __forceinline__ void span_of(const DecodeArgs& a, int b, int g, int& 
 template <int TILE>
 __device__ __forceinline__ int tiles_of(int count) { return count > 0 ? (count - 1) / TILE + 1 : 1; }   // an empty row still has to be written
 
+// four values of a finished row: (their sum, the row's maximum and sum of exponentials)
+template <int D>
+__device__ __forceinline__ void write_out(const DecodeArgs& a, i64 row, int d, const float4& acc, float top, float sum, float vs) {
+    const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
+    const uint2 w = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
+    cake_bf16* dst = a.out + row * D + d;
+    if (a.out_wide) {
+        *reinterpret_cast<uint2*>(dst) = w;
+    } else {
+        dst[0] = w.x & 0xffff, dst[1] = w.x >> 16, dst[2] = w.y & 0xffff, dst[3] = w.y >> 16;
+    }
+    if (a.lse && d == 0) a.lse[row] = (top + log2f(sum)) * LN2;
+}
+
 // The work list: entries in the order (sequence, key-value head, run of query heads), each of tiles_of(its tokens) tiles.
 struct Cursor {
     int b, g, run, first, count, tiles;
     i64 start;        // number of the entry's first tile in the list
 };
+
+// parts c, c + step, ... of four values of a row, joined
+struct Joined {
+    float top = NEG_INF, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+
+    __device__ __forceinline__ void rescale(float up) {
+        const float f = ex2(top - (up == NEG_INF ? 0.f : up));
+        sum *= f, acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+        top = up;
+    }
+    template <int D, int HEADS>
+    __device__ __forceinline__ void add(const DecodeArgs& a, int c, int c1, int step, int slot0, int c0, int h, int d) {
+        constexpr int BATCH = 8;             // parts in flight
+        constexpr i64 PART = HEADS * (D + 4);
+        for (; c <= c1; c += BATCH * step) {
+            float4 u[BATCH];
+            float2 ml[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                u[k] = make_float4(0.f, 0.f, 0.f, 0.f), ml[k] = make_float2(NEG_INF, 0.f);
+                const int ck = c + k * step;
+                if (ck <= c1) {
+                    const float* p = a.parts + (2 * ck + (ck == c0 ? slot0 : 0)) * PART;
+                    u[k] = __ldcg(reinterpret_cast<const float4*>(p + h * D + d));
+                    ml[k] = __ldcg(reinterpret_cast<const float2*>(p + HEADS * D + 2 * h));
+                }
+            }
+            float up = top;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) up = fmaxf(up, ml[k].x);
+            rescale(up);
+            const float base = up == NEG_INF ? 0.f : up;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const float f = ex2(ml[k].x - base);
+                sum = fmaf(ml[k].y, f, sum);
+                acc.x = fmaf(u[k].x, f, acc.x), acc.y = fmaf(u[k].y, f, acc.y);
+                acc.z = fmaf(u[k].z, f, acc.z), acc.w = fmaf(u[k].w, f, acc.w);
+            }
+        }
+    }
+};
+
+// One row (an entry's query head) to a block and step: D / 4 threads across the row, four such groups share its parts.
+template <int D, int HEADS>
+__global__ void __launch_bounds__(D)
+paged_join_kernel(const DecodeArgs a, bool e4m3) {
+    ptx::grid_dep_wait();
+    __shared__ float4 accs[4][D / 4];
+    __shared__ float2 mls[4];
+    const int group = threadIdx.x / (D / 4), d = 4 * (threadIdx.x % (D / 4));
+    const int rows = *reinterpret_cast<volatile int*>(a.n_splits) * HEADS;
+    for (int u = blockIdx.x; u < rows; u += gridDim.x) {
+        const Split e = a.splits[u / HEADS];
+        const int h = u % HEADS;
+        if (h >= min(HEADS, a.G - e.run * HEADS)) continue;
+        Joined j;
+        j.add<D, HEADS>(a, e.c0 + group, e.c1, 4, e.slot0, e.c0, h, d);
+        accs[group][d / 4] = j.acc;
+        if (d == 0) mls[group] = make_float2(j.top, j.sum);
+        __syncthreads();
+        if (group == 0) {
+            float up = NEG_INF;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) up = fmaxf(up, mls[k].x);
+            const float base = up == NEG_INF ? 0.f : up;
+            float sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = ex2(mls[k].x - base);
+                const float4 v = accs[k][d / 4];
+                sum = fmaf(mls[k].y, f, sum);
+                acc.x = fmaf(v.x, f, acc.x), acc.y = fmaf(v.y, f, acc.y), acc.z = fmaf(v.z, f, acc.z), acc.w = fmaf(v.w, f, acc.w);
+            }
+            const float vs = e4m3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
+            write_out<D>(a, static_cast<i64>(e.b) * a.Hq + e.g * a.G + e.run * HEADS + h, d, acc, up, sum, vs);
+        }
+        __syncthreads();
+    }
+    // the last block empties the list for the next call
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(a.n_splits + 1, 1) == static_cast<int>(gridDim.x) - 1) a.n_splits[0] = 0, a.n_splits[1] = 0;
+    }
+}
 
 template <int D, bool E4M3, int NT, int STAGES, int WARPS, int PER_SM>
 __global__ void __launch_bounds__(WARPS * 32, PER_SM)
@@ -162,6 +273,7 @@ paged_decode_kernel(const DecodeArgs a) {
         ptx::fence_mbar_init();
     }
 
+    ptx::grid_dep_launch();          // (a joining kernel waits for the end of this one by itself)
     // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
     const int per = (a.B + THREADS - 1) / THREADS;
     auto tiles_of_sequence = [&](int b) -> i64 {
@@ -557,17 +669,7 @@ paged_decode_kernel(const DecodeArgs a) {
         float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
         const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
-        auto finish = [&](int h, int d, const float4& acc, float top, float sum) {
-            const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
-            uint2 w = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
-            cake_bf16* dst = a.out + (out0 + h) * D + d;
-            if (a.out_wide) {
-                *reinterpret_cast<uint2*>(dst) = w;
-            } else {
-                dst[0] = w.x & 0xffff, dst[1] = w.x >> 16, dst[2] = w.y & 0xffff, dst[3] = w.y >> 16;
-            }
-            if (a.lse && d == 0) a.lse[out0 + h] = (top + log2f(sum)) * LN2;
-        };
+        auto finish = [&](int h, int d, const float4& acc, float top, float sum) { write_out<D>(a, out0 + h, d, acc, top, sum, vs); };
         for (int i = tid; i < heads * (D / 4); i += THREADS) {
             const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
             float top = NEG_INF;
@@ -590,54 +692,31 @@ paged_decode_kernel(const DecodeArgs a) {
             }
         }
         if (!whole) {
-            // ---- the entry's CTAs are neighbours; the last to arrive joins their parts in order
+            // ---- the entry's CTAs are neighbours.  A few parts are joined, in order, by the last of them to arrive; many by a second kernel,
+            // for which the first of them notes the entry
             const i64 s0 = e.start, s1 = e.start + e.tiles - 1;
             const int c0 = static_cast<int>(((s0 + 1) * n_ctas - 1) / total), c1 = static_cast<int>(((s1 + 1) * n_ctas - 1) / total);
-            __syncthreads();
-            if (tid == 0) {
-                __threadfence();
-                const int before_me = atomicAdd(a.counters + c0, 1);
-                last_flag = before_me == c1 - c0;
-                if (last_flag) a.counters[c0] = 0;       // ready for the next call
-                __threadfence();
-            }
-            __syncthreads();
-            if (last_flag) {
-                // the entry is the first of a CTA's segments unless that CTA (the first of them) began before it
-                const int slot0 = c0 * total / n_ctas >= s0 ? 0 : 1;
-                for (int i = tid; i < heads * (D / 4); i += THREADS) {
-                    const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
-                    float top = NEG_INF, sum = 0.f;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    constexpr int BATCH = 8;             // parts in flight
-                    for (int c = c0; c <= c1; c += BATCH) {
-                        float4 u[BATCH];
-                        float2 ml[BATCH];
-#pragma unroll
-                        for (int k = 0; k < BATCH; ++k) {
-                            u[k] = make_float4(0.f, 0.f, 0.f, 0.f), ml[k] = make_float2(NEG_INF, 0.f);
-                            if (c + k <= c1) {
-                                const float* p = a.parts + (2 * (c + k) + (c + k == c0 ? slot0 : 0)) * static_cast<i64>(PART);
-                                u[k] = __ldcg(reinterpret_cast<const float4*>(p + h * D + d));
-                                ml[k] = __ldcg(reinterpret_cast<const float2*>(p + HEADS * D + 2 * h));
-                            }
-                        }
-                        float up = top;
-#pragma unroll
-                        for (int k = 0; k < BATCH; ++k) up = fmaxf(up, ml[k].x);
-                        const float base_m = up == NEG_INF ? 0.f : up;
-                        const float f0 = ex2(top - base_m);
-                        sum *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
-#pragma unroll
-                        for (int k = 0; k < BATCH; ++k) {
-                            const float f = ex2(ml[k].x - base_m);
-                            sum = fmaf(ml[k].y, f, sum);
-                            acc.x = fmaf(u[k].x, f, acc.x), acc.y = fmaf(u[k].y, f, acc.y);
-                            acc.z = fmaf(u[k].z, f, acc.z), acc.w = fmaf(u[k].w, f, acc.w);
-                        }
-                        top = up;
+            // the entry is the first of a CTA's segments unless that CTA (the first of them) began before it
+            const int slot0 = c0 * total / n_ctas >= s0 ? 0 : 1;
+            if (a.defer) {
+                if (tid == 0 && cta == c0) a.splits[atomicAdd(a.n_splits, 1)] = Split{e.b, e.g, e.run, c0, c1, slot0, {0, 0}};
+            } else {
+                __syncthreads();
+                if (tid == 0) {
+                    __threadfence();
+                    const int before_me = atomicAdd(a.counters + c0, 1);
+                    last_flag = before_me == c1 - c0;
+                    if (last_flag) a.counters[c0] = 0;       // ready for the next call
+                    __threadfence();
+                }
+                __syncthreads();
+                if (last_flag) {
+                    for (int i = tid; i < heads * (D / 4); i += THREADS) {
+                        const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
+                        Joined j;
+                        j.add<D, HEADS>(a, c0, c1, 1, slot0, c0, h, d);
+                        finish(h, d, j.acc, j.top, j.sum);
                     }
-                    finish(h, d, acc, top, sum);
                 }
             }
         }
@@ -661,7 +740,7 @@ Shape shape_of(int Hq, int Hkv) {
 }
 
 template <int D, bool E4M3, int NT, int STAGES, int WARPS, int PER_SM>
-int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
+int launch(DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     using L = Layout<D, E4M3>;
     constexpr int RING1 = WARPS * L::STAGE;
     constexpr int RING = RING1 * STAGES;
@@ -680,14 +759,36 @@ int launch(const DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
         if (di.device >= 0 && di.device < 64) per_sm_of[di.device] = per_sm;
     }
     const int ctas = min(di.sm_count * per_sm, kPartCtas);
+    // Parts of one row if all are about as long: few are joined by the last CTA, from 64 KiB on (about 2 us of one SM's
+    // bandwidth) by a kernel of its own
+    const i64 entries = static_cast<i64>(a.B) * a.c.Hkv * a.chunks;
+    const i64 most_tiles = (static_cast<i64>(a.max_pages) * a.c.page_size + WARPS * KEYS - 1) / (WARPS * KEYS);
+    const i64 share = (ctas + entries - 1) / entries, parts = share < most_tiles ? share : most_tiles;
+    a.defer = parts * min(8 * NT, a.G) * D * 4 > 64 * 1024;
     kernel<<<ctas, WARPS * 32, SMEM, s>>>(a);
     note_launches(1);
-    return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    if (cudaGetLastError() != cudaSuccess) return CAKE_ERR_CUDA;
+    if (!a.defer) return CAKE_OK;
+    cudaLaunchConfig_t join = {};
+    join.gridDim = dim3(2 * di.sm_count);
+    join.blockDim = dim3(D);
+    join.stream = s;
+    cudaLaunchAttribute pdl[1];
+    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    pdl[0].val.programmaticStreamSerializationAllowed = 1;
+    join.attrs = pdl;
+    join.numAttrs = 1;
+    if (cudaLaunchKernelEx(&join, paged_join_kernel<D, 8 * NT>, static_cast<const DecodeArgs>(a), E4M3) != cudaSuccess) {
+        cudaGetLastError();
+        return CAKE_ERR_CUDA;
+    }
+    note_launches(1);
+    return CAKE_OK;
 }
 
 // Two stages a warp and as many warps as fit: a warp's step is a chain of dependent instructions, other warps fill its gaps.
 template <int D>
-int launch_d(const DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_t s) {
+int launch_d(DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_t s) {
     constexpr int W16 = D == 256 ? 2 : 4;
     constexpr int P8 = D <= 128 ? 4 : 2, P16 = D <= 64 ? 4 : 3;
     if (e4m3) return nt == 1 ? launch<D, true, 1, 2, 4, P8>(a, di, s) : launch<D, true, 2, 2, 4, D == 256 ? 2 : 3>(a, di, s);
@@ -701,7 +802,7 @@ int check_heads(long long B, int Hq, int Hkv, int D) {
 }
 size_t workspace_bytes(int Hq, int Hkv, int D) {
     const Shape sh = shape_of(Hq, Hkv);
-    return round_up(static_cast<i64>(kHeaderBytes + sizeof(float) * 2 * kPartCtas * 8 * sh.nt * (D + 4)), 256);
+    return round_up(static_cast<i64>(kHeaderBytes + kPartCtas * sizeof(Split) + sizeof(float) * 2 * kPartCtas * 8 * sh.nt * (D + 4)), 256);
 }
 
 }  // namespace
@@ -747,7 +848,9 @@ int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_s
     a.c = *cache, a.q = q, a.table = page_table, a.lens = seq_lens, a.out = out, a.lse = out_lse;
     a.status = static_cast<int*>(ws);
     a.counters = static_cast<int*>(ws) + 64;
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes);
+    a.n_splits = static_cast<int*>(ws) + 16;
+    a.splits = reinterpret_cast<Split*>(static_cast<char*>(ws) + kHeaderBytes);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes + kPartCtas * sizeof(Split));
     a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.table_stride = table_stride, a.table_head_stride = table_head_stride;
     a.lens_stride = lens_stride, a.lens_head_stride = lens_head_stride;
     a.B = static_cast<int>(B), a.Hq = Hq, a.G = Hq / cache->Hkv, a.chunks = sh.chunks, a.max_pages = max_pages, a.window = window;

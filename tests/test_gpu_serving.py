@@ -479,6 +479,21 @@ def test_decode_many_sequences_and_one_workspace_for_many_shapes():
     assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,D,kv,length", [(1, 16, 1, 256, BF16, 30000), (2, 6, 1, 128, E4M3, 40000), (1, 20, 1, 96, BF16, 20000),
+                                                  (1, 3, 1, 64, BF16, 70001), (3, 40, 2, 64, E4M3, 9000)])
+def test_decode_few_sequences_in_many_parts(B, Hq, Hkv, D, kv, length):
+    """Rows split over hundreds of CTAs (the parts are joined by a kernel of their own), between calls that are not split."""
+    ws = cake.alloc_decode_workspace(B, Hq, Hkv, D, DEV)
+    for lens in ([length] * B, [7] * B, [length - 11 * i for i in range(B)], [0] * B, [length // (i + 1) for i in range(B)]):
+        q, cache, table, n = decode_problem(Hq, Hkv, D, 16, kv, lens, length)
+        wide = torch.full((B, -(-length // 16)), -1, dtype=torch.int32, device=DEV)      # the table's width says how long rows may be
+        wide[:, :table.shape[1]] = table
+        out, lse = cake.cake_paged_decode(q, cache, wide, n, want_lse=True, ws=ws)
+        check_decode(q, cache, table, n, out, lse)
+        assert torch.equal(cake.cake_paged_decode(q, cache, wide, n, ws=ws)[0], out)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
+
+
 def test_decode_scores_far_apart_and_infinite():
     """A maximum that arrives late, scores of -inf beside finite ones, and a row that is nothing but -inf or NaN."""
     q, cache, table, n = decode_problem(8, 1, 64, 16, BF16, [600, 600, 200, 200], 3, poison=False)
