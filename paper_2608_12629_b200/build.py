@@ -3,12 +3,14 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcake_kmeans.so")
+EXT = os.path.join(HERE, "_serving.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--shared",
@@ -45,5 +47,33 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def extension_sources():
+    return [os.path.join(CSRC, "ext", "serving_ext.cpp"), os.path.join(os.path.dirname(HERE), "include", "cake_serving.h"),
+            os.path.join(os.path.dirname(HERE), "include", "cake_kmeans.h")]
+
+
+def build_extension(force: bool = False) -> str:
+    """Compile the serving operators' marshalling module (csrc/ext) against torch's headers and the library; returns its path."""
+    src = extension_sources()
+    if not force and os.path.exists(EXT) and os.path.getmtime(EXT) >= max(os.path.getmtime(f) for f in src):
+        return EXT
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
+    tmp = EXT + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"),
+           "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
+           src[0], "-o", tmp, "-L" + HERE, "-l:" + os.path.basename(LIB), "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           "-Wl,-rpath,$ORIGIN"]
+    subprocess.check_call(cmd)
+    os.replace(tmp, EXT)
+    return EXT
+
+
 if __name__ == "__main__":
     print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_extension(force="--force" in sys.argv))

@@ -31,6 +31,23 @@ def test_header_library_and_binding_agree(L):
     assert int(re.search(r"CAKE_SERVING_HEADER_BYTES (\d+)", header()).group(1)) == cake.CAKE_SERVING_HEADER_BYTES
 
 
+def test_marshalling_module_refuses_what_is_no_cuda_tensor(L):
+    import torch
+    cake_build.build_extension()
+    x = torch.zeros(2, 8, dtype=torch.bfloat16)
+    for bad in (x, x.float(), None, 3, x.view(-1)):
+        with pytest.raises((TypeError, AttributeError, IndexError)):
+            cake.cake_rmsnorm_quant(bad)
+    with pytest.raises(TypeError):
+        serving._native().gemm_fp8(x, x)                 # a wrong number of arguments
+    with pytest.raises(TypeError):
+        serving._native().rmsnorm_quant(*[x] * 11)
+    with pytest.raises(TypeError):
+        cake.PagedCache(x, x)
+    with pytest.raises(TypeError):
+        cake.PagedCache(*[torch.zeros(2, 16, 1, 64, dtype=torch.bfloat16)] * 2)
+
+
 def test_workspace_sizes_need_no_device():
     assert cake.cake_gemm_fp8_workspace_bytes(1, 128, 128) >= cake.CAKE_SERVING_HEADER_BYTES
     assert cake.cake_gemm_fp8_workspace_bytes(0, 1, 16) >= cake.CAKE_SERVING_HEADER_BYTES
