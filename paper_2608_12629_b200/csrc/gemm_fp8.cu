@@ -166,6 +166,8 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
 
     if (warp == WARP_TMA) {
         if (ptx::elect_one()) {
@@ -482,6 +484,8 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     ptx::cluster_sync_all();         // both CTAs' barriers and tensor memory are set up
     ptx::tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
 
     if (warp >= PAIR_EPI) {
     ptx::setmaxnreg_dec<AUX_REGS>();
@@ -682,7 +686,6 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             }
         }
     }
-    ptx::grid_dep_launch();
     // neither CTA leaves while the other's MMAs, loads or arrivals can still reach it
     ptx::tc_fence_before();
     __syncthreads();
@@ -697,6 +700,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 template <int BN>
 __global__ void __launch_bounds__(256)
 gemm_join_kernel(const GemmArgs a) {
+    ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     const int quads = (a.N + 3) / 4;
     const i64 total = a.M * quads;
@@ -776,9 +780,7 @@ int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, cons
     }
     const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
     const int ctas = static_cast<int>(items < di.sm_count ? items : di.sm_count);
-    gemm_fp8_kernel<TN><<<ctas, THREADS, T::SMEM, s>>>(mw, mx, a);
-    note_launches(1);
-    return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    return launch_early(gemm_fp8_kernel<TN>, dim3(ctas), dim3(THREADS), T::SMEM, s, mw, mx, a) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
 template <int BN>
@@ -795,13 +797,15 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     cfg.blockDim = dim3(wide::PAIR_THREADS);
     cfg.dynamicSmemBytes = wide::pair_smem<BN>();
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // as launch_early
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, wide::gemm_fp8_pair_kernel<BN>, mw, mx, a) != cudaSuccess) {
         cudaGetLastError();
         return CAKE_ERR_CUDA;
@@ -809,21 +813,9 @@ int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx,
     note_launches(1);
     if (a.splits == 1) return CAKE_OK;
     const i64 threads = a.M * ((a.N + 3) / 4);
-    cudaLaunchConfig_t join = {};
-    join.gridDim = dim3(static_cast<unsigned>(threads / 256 + 1 < 8 * di.sm_count ? threads / 256 + 1 : 8 * di.sm_count));
-    join.blockDim = dim3(256);
-    join.stream = s;
-    cudaLaunchAttribute pdl[1];
-    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    pdl[0].val.programmaticStreamSerializationAllowed = 1;
-    join.attrs = pdl;
-    join.numAttrs = 1;
-    if (cudaLaunchKernelEx(&join, wide::gemm_join_kernel<BN>, a) != cudaSuccess) {
-        cudaGetLastError();
-        return CAKE_ERR_CUDA;
-    }
-    note_launches(1);
-    return CAKE_OK;
+    const i64 blocks = threads / 256 + 1;
+    return launch_early(wide::gemm_join_kernel<BN>, dim3(static_cast<unsigned>(blocks < 8 * di.sm_count ? blocks : 8 * di.sm_count)), dim3(256), 0, s, a) ==
+                   cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
 int check_shape(i64 M, int N, int K) {

@@ -72,6 +72,8 @@ __global__ void __launch_bounds__(288)
 kv_append_kernel(const AppendArgs a) {
     const i64 t = blockIdx.x;
     const int u = threadIdx.x;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
     const Place p = place_of(a, t, threadIdx.x == 0 && threadIdx.y == 0);
     if (!p.rotate_ok) return;
     const int D = a.c.D, half = a.rot >> 1;
@@ -149,6 +151,8 @@ template <bool E4M3>
 __global__ void __launch_bounds__(256)
 kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
     const i64 t = blockIdx.x;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
     const Place p = place_of(a, t, threadIdx.x == 0);
     if (!p.rotate_ok) return;
     const int D = a.c.D, half = a.rot >> 1;
@@ -249,25 +253,18 @@ extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k,
     const bool wide = (pairs ? rot % 8 == 0 : rot % 16 == 0) && k_stride % 8 == 0 && v_stride % 8 == 0 && aligned(k, 16) && aligned(v, 16) &&
                       (!q || (q_stride % 8 == 0 && aligned(q, 16) && aligned(out_q, 16)));
     const unsigned blocks = static_cast<unsigned>(T);
+    cudaError_t e;
     if (wide) {
         const int units = pairs ? D / 8 : rot / 16 + (D - rot) / 8;
         const int heads = (q ? Hq : 0) + 2 * cache->Hkv;
         // four heads to a thread where that leaves 128 threads or more
         const int most = (heads + 3) / 4 * units >= 128 ? (heads + 3) / 4 : heads;
         const int par = most * units <= 256 ? most : (256 + units - 1) / units;
-        const dim3 block(units, par);
-        if (e4m3) {
-            if (pairs) kv_append_kernel<true, true><<<blocks, block, 0, s>>>(a);
-            else kv_append_kernel<true, false><<<blocks, block, 0, s>>>(a);
-        } else {
-            if (pairs) kv_append_kernel<false, true><<<blocks, block, 0, s>>>(a);
-            else kv_append_kernel<false, false><<<blocks, block, 0, s>>>(a);
-        }
-    } else if (e4m3) {
-        kv_append_scalar_kernel<true><<<blocks, 256, 0, s>>>(a, pairs);
+        void (*const kernel)(const AppendArgs) = e4m3 ? (pairs ? kv_append_kernel<true, true> : kv_append_kernel<true, false>)
+                                                      : (pairs ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
+        e = launch_early(kernel, dim3(blocks), dim3(units, par), 0, s, a);
     } else {
-        kv_append_scalar_kernel<false><<<blocks, 256, 0, s>>>(a, pairs);
+        e = launch_early(e4m3 ? kv_append_scalar_kernel<true> : kv_append_scalar_kernel<false>, dim3(blocks), dim3(256), 0, s, a, pairs);
     }
-    note_launches(1);
-    return cudaGetLastError() == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    return e == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }

@@ -210,6 +210,7 @@ struct Joined {
 template <int D, int HEADS>
 __global__ void __launch_bounds__(D)
 paged_join_kernel(const DecodeArgs a, bool e4m3) {
+    ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     __shared__ float4 accs[4][D / 4];
     __shared__ float2 mls[4];
@@ -273,7 +274,8 @@ paged_decode_kernel(const DecodeArgs a) {
         ptx::fence_mbar_init();
     }
 
-    ptx::grid_dep_launch();          // (a joining kernel waits for the end of this one by itself)
+    ptx::grid_dep_launch();          // (the next kernel, a joining one too, waits for the end of this one by itself)
+    ptx::grid_dep_wait();
     // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
     const int per = (a.B + THREADS - 1) / THREADS;
     auto tiles_of_sequence = [&](int b) -> i64 {
@@ -765,25 +767,9 @@ int launch(DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     const i64 most_tiles = (static_cast<i64>(a.max_pages) * a.c.page_size + WARPS * KEYS - 1) / (WARPS * KEYS);
     const i64 share = (ctas + entries - 1) / entries, parts = share < most_tiles ? share : most_tiles;
     a.defer = parts * min(8 * NT, a.G) * D * 4 > 64 * 1024;
-    kernel<<<ctas, WARPS * 32, SMEM, s>>>(a);
-    note_launches(1);
-    if (cudaGetLastError() != cudaSuccess) return CAKE_ERR_CUDA;
+    if (launch_early(kernel, dim3(ctas), dim3(WARPS * 32), SMEM, s, a) != cudaSuccess) return CAKE_ERR_CUDA;
     if (!a.defer) return CAKE_OK;
-    cudaLaunchConfig_t join = {};
-    join.gridDim = dim3(2 * di.sm_count);
-    join.blockDim = dim3(D);
-    join.stream = s;
-    cudaLaunchAttribute pdl[1];
-    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    pdl[0].val.programmaticStreamSerializationAllowed = 1;
-    join.attrs = pdl;
-    join.numAttrs = 1;
-    if (cudaLaunchKernelEx(&join, paged_join_kernel<D, 8 * NT>, static_cast<const DecodeArgs>(a), E4M3) != cudaSuccess) {
-        cudaGetLastError();
-        return CAKE_ERR_CUDA;
-    }
-    note_launches(1);
-    return CAKE_OK;
+    return launch_early(paged_join_kernel<D, 8 * NT>, dim3(2 * di.sm_count), dim3(D), 0, s, a, E4M3) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
 // Two stages a warp and as many warps as fit: a warp's step is a chain of dependent instructions, other warps fill its gaps.

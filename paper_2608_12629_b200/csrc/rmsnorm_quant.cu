@@ -106,6 +106,8 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         }
     };
     i64 row = static_cast<i64>(blockIdx.x) * per_block + sub;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
     if (WIDE) load(row);
     // (the rows of a block leave the loop together: its barriers are for all threads)
     for (i64 first = static_cast<i64>(blockIdx.x) * per_block; first < a.T; first += static_cast<i64>(gridDim.x) * per_block) {
@@ -252,9 +254,8 @@ cudaError_t launch_nv(const NormArgs& a, const DeviceInfo& di, cudaStream_t s) {
     const int rows = warps >= 4 ? 1 : 4 / warps;      // blocks of at least about 128 threads
     const i64 blocks = (a.T + rows - 1) / rows;
     const i64 resident = static_cast<i64>(di.sm_count) * PER_SM * (MOST_THREADS / (rows * warps * 32));
-    rmsnorm_quant_kernel<LOADS, NV, MOST_THREADS, PER_SM><<<static_cast<unsigned>(blocks < resident ? blocks : resident), rows * warps * 32, 0, s>>>(a, warps * 32);
-    note_launches(1);
-    return cudaGetLastError();
+    return launch_early(rmsnorm_quant_kernel<LOADS, NV, MOST_THREADS, PER_SM>, dim3(static_cast<unsigned>(blocks < resident ? blocks : resident)),
+                        dim3(rows * warps * 32), 0, s, a, warps * 32);
 }
 
 }  // namespace

@@ -6,6 +6,7 @@
 
 #include "../../include/cake_serving.h"
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace cake {
 namespace serving {
@@ -20,6 +21,26 @@ constexpr size_t kHeaderBytes = 256 + kMaxCtas * 4;
 static_assert(kHeaderBytes == CAKE_SERVING_HEADER_BYTES, "header and ABI constant agree");
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// Launch that may begin while the kernel ahead of it in the stream drains: the kernel waits for that one itself (ptx::grid_dep_wait,
+// before its first access to global memory).  In a stream of short kernels this hides their launch.
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    if (e != cudaSuccess) cudaGetLastError();
+    note_launches(1);
+    return e;
+}
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
