@@ -109,6 +109,27 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
     ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     if (WIDE) load(row);
+    // a thread has the same columns in every row: where the registers allow, its weights stay in them
+    constexpr bool KEEP = NV <= 2;
+    uint32_t wr[NV][4];
+    auto weights = [&]() {
+        if (!a.w) return;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col0 + v * step;
+            if (WIDE) {
+                const uint4 u = c < a.H ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : make_uint4(0, 0, 0, 0);
+                wr[v][0] = u.x, wr[v][1] = u.y, wr[v][2] = u.z, wr[v][3] = u.w;
+            } else if (PAIR) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) wr[v][j] = c + 64 * j < a.H ? __ldg(reinterpret_cast<const uint32_t*>(a.w + c + 64 * j)) : 0u;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) wr[v][j] = c + 32 * j < a.H ? __ldg(a.w + c + 32 * j) : 0u;
+            }
+        }
+    };
+    if (KEEP) weights();
     // (the rows of a block leave the loop together: its barriers are for all threads)
     for (i64 first = static_cast<i64>(blockIdx.x) * per_block; first < a.T; first += static_cast<i64>(gridDim.x) * per_block) {
         const bool live = row < a.T;
@@ -148,26 +169,12 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
             }
         }
         // s becomes s * w; y is that times rs, which is applied to the group's maximum and with the scale instead of element by element
+        if (!KEEP) weights();
+        if (a.w) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = col0 + v * step;
-            if (!a.w) continue;
-            if (WIDE) {
-                uint4 wv = make_uint4(0, 0, 0, 0);
-                if (c < a.H) wv = __ldg(reinterpret_cast<const uint4*>(a.w + c));
-                const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
+            for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int j = 0; j < E; ++j) s[v][j] *= (j & 1) ? bf16_hi(ww[j / 2]) : bf16_lo(ww[j / 2]);
-            } else if (PAIR) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t w = c + 64 * j < a.H ? __ldg(reinterpret_cast<const uint32_t*>(a.w + c + 64 * j)) : 0u;
-                    s[v][2 * j] *= bf16_lo(w), s[v][2 * j + 1] *= bf16_hi(w);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) s[v][j] *= c + 32 * j < a.H ? bf16_f(__ldg(a.w + c + 32 * j)) : 0.f;
-            }
+                for (int j = 0; j < E; ++j) s[v][j] *= (WIDE || PAIR) ? ((j & 1) ? bf16_hi(wr[v][j / 2]) : bf16_lo(wr[v][j / 2])) : bf16_lo(wr[v][j % 4]);
         }
         float rs = 1.f;
         if (a.norm) {
@@ -253,8 +260,10 @@ cudaError_t launch_nv(const NormArgs& a, const DeviceInfo& di, cudaStream_t s) {
     const int warps = (chunks + NV - 1) / NV;
     const int rows = warps >= 4 ? 1 : 4 / warps;      // blocks of at least about 128 threads
     const i64 blocks = (a.T + rows - 1) / rows;
-    const i64 resident = static_cast<i64>(di.sm_count) * PER_SM * (MOST_THREADS / (rows * warps * 32));
-    return launch_early(rmsnorm_quant_kernel<LOADS, NV, MOST_THREADS, PER_SM>, dim3(static_cast<unsigned>(blocks < resident ? blocks : resident)),
+    // no more blocks than are resident, the rows spread evenly over their rounds
+    const i64 resident = static_cast<i64>(di.sm_count) * (PER_SM * MOST_THREADS / (rows * warps * 32));
+    const i64 rounds = (blocks + resident - 1) / resident;
+    return launch_early(rmsnorm_quant_kernel<LOADS, NV, MOST_THREADS, PER_SM>, dim3(static_cast<unsigned>((blocks + rounds - 1) / rounds)),
                         dim3(rows * warps * 32), 0, s, a, warps * 32);
 }
 
