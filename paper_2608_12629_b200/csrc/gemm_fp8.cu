@@ -25,9 +25,12 @@ namespace {
 constexpr int TM = 128;                        // rows of W per tile
 constexpr int KB = 128;                        // columns of a block
 constexpr int EPI_WARPS = 8;                   // two warpgroups, half of the tile's columns each
-constexpr int WARP_TMA = 8, WARP_MMA = 9, WARP_SCALE = 10;
-constexpr int THREADS = 11 * 32;
-constexpr int SCALE_BUFS = 8;                  // blocks of scales ahead
+constexpr int WARP_TMA = 8, WARP_MMA = 9, WARP_SCALE = 10, WARP_MMA1 = 11;
+constexpr int THREADS = 12 * 32;
+constexpr int BUFS = 4;                        // steps whose accumulators, and whose scales, are in flight
+// Blocks of a step.  A block of a narrow tile is less work (64 to 256 clocks) than its barriers: about 100 clocks to issue an instruction, 120
+// for a commit, 200 for a wait.  So two blocks share them, and two threads issue every other step
+constexpr int PER_STEP = 2;
 constexpr uint32_t W_BYTES = TM * KB;
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 constexpr int NARROW_M = 64;                   // rows of X up to which the narrow kernel is taken
@@ -45,7 +48,7 @@ struct GemmArgs {
 };
 
 struct __align__(16) Ctrl {
-    uint64_t full[16], empty[16], tfull[4], tempty[4], sfull[SCALE_BUFS], sempty[SCALE_BUFS];
+    uint64_t full[8], empty[8], tfull[BUFS], tempty[BUFS], sfull[BUFS], sempty[BUFS];
     uint32_t tmem;
     int abort_flag;
     int last;
@@ -104,13 +107,14 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[N]) {
 template <int TN>
 struct Tile {
     static constexpr int COLS = TN / 2;                              // columns of an epilogue thread
-    static constexpr int LD = COLS < 32 ? COLS : 32;
-    static constexpr uint32_t STAGE = W_BYTES + TN * KB;
-    static constexpr int STAGES = TN == 64 ? 8 : TN == 32 ? 10 : 11;
-    static constexpr int BUFS = 4;
-    static constexpr uint32_t TMEM_COLS = BUFS * TN < 32 ? 32 : BUFS * TN;
-    static constexpr uint32_t SMEM = 1024 + STAGES * STAGE + SCALE_BUFS * TN * 4 + sizeof(Ctrl);
-    static_assert(SMEM <= 227 * 1024, "");
+    static constexpr int LD = COLS;
+    static_assert(COLS == 8 || COLS == 16 || COLS == 32, "one load of tensor memory");
+    static constexpr uint32_t BLOCK = W_BYTES + TN * KB;
+    static constexpr uint32_t STAGE = PER_STEP * BLOCK;
+    static constexpr int STAGES = TN == 64 ? 4 : TN == 32 ? 5 : 6;
+    static constexpr uint32_t TMEM_COLS = BUFS * PER_STEP * TN;
+    static constexpr uint32_t SMEM = 1024 + STAGES * STAGE + BUFS * PER_STEP * TN * 4 + sizeof(Ctrl);
+    static_assert(SMEM <= 227 * 1024 && TMEM_COLS <= 512, "");
 };
 
 struct Item {
@@ -136,7 +140,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     float* const scales = reinterpret_cast<float*>(tiles + T::STAGES * T::STAGE);
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(scales + SCALE_BUFS * TN);
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(scales + BUFS * PER_STEP * TN);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int items = a.tiles_m * a.tiles_n * a.splits;
 
@@ -145,11 +149,9 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             ptx::mbar_init(ptx::smem_u32(&ctrl->full[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctrl->empty[i]), 1);
         }
-        for (int i = 0; i < T::BUFS; ++i) {
+        for (int i = 0; i < BUFS; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctrl->tfull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctrl->tempty[i]), EPI_WARPS);
-        }
-        for (int i = 0; i < SCALE_BUFS; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctrl->sfull[i]), 32);
             ptx::mbar_init(ptx::smem_u32(&ctrl->sempty[i]), EPI_WARPS);
         }
@@ -171,17 +173,21 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 
     if (warp == WARP_TMA) {
         if (ptx::elect_one()) {
-            uint32_t n = 0;      // blocks so far
+            uint32_t n = 0;      // steps so far
             for (int i = blockIdx.x; i < items && !aborted(ctrl); i += gridDim.x) {
                 const Item it = item_of(a, i, TN);
-                for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
+                for (int kb = it.kb0; kb < it.kb1; kb += PER_STEP, ++n) {
                     const uint32_t s = n % T::STAGES, round = n / T::STAGES;
                     wait_bar(&ctrl->empty[s], (round & 1) ^ 1, ctrl, a.status);
                     if (aborted(ctrl)) break;
-                    const uint32_t bar = ptx::smem_u32(&ctrl->full[s]), dst = ptx::smem_u32(tiles + s * T::STAGE);
-                    ptx::mbar_arrive_expect_tx(bar, T::STAGE);
-                    tma_load_2d(dst, &map_w, bar, kb * KB, it.n0);
-                    tma_load_2d(dst + W_BYTES, &map_x, bar, kb * KB, it.m0);
+                    const int blocks = min(PER_STEP, it.kb1 - kb);
+                    const uint32_t bar = ptx::smem_u32(&ctrl->full[s]);
+                    ptx::mbar_arrive_expect_tx(bar, blocks * T::BLOCK);
+                    for (int j = 0; j < blocks; ++j) {
+                        const uint32_t dst = ptx::smem_u32(tiles + s * T::STAGE + j * T::BLOCK);
+                        tma_load_2d(dst, &map_w, bar, (kb + j) * KB, it.n0);
+                        tma_load_2d(dst + W_BYTES, &map_x, bar, (kb + j) * KB, it.m0);
+                    }
                 }
             }
             // copies in flight land before the CTA gives up its shared memory (they have, unless a wait has expired)
@@ -193,35 +199,40 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
         }
         __syncwarp();
-    } else if (warp == WARP_MMA) {
+    } else if (warp == WARP_MMA || warp == WARP_MMA1) {
         if (ptx::elect_one()) {
+            const uint32_t who = warp == WARP_MMA ? 0 : 1;
             uint32_t n = 0;
             constexpr uint32_t idesc = idesc_e4m3(TM, TN);
             for (int i = blockIdx.x; i < items && !aborted(ctrl); i += gridDim.x) {
                 const Item it = item_of(a, i, TN);
-                for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                    const uint32_t s = n % T::STAGES, b = n % T::BUFS;
-                    wait_bar(&ctrl->tempty[b], ((n / T::BUFS) & 1) ^ 1, ctrl, a.status);
+                for (int kb = it.kb0; kb < it.kb1; kb += PER_STEP, ++n) {
+                    if ((n & 1) != who) continue;
+                    const uint32_t s = n % T::STAGES, b = n % BUFS;
+                    wait_bar(&ctrl->tempty[b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
                     wait_bar(&ctrl->full[s], (n / T::STAGES) & 1, ctrl, a.status);
                     if (aborted(ctrl)) break;
                     ptx::tc_fence_after();
-                    const uint32_t base = ptx::smem_u32(tiles + s * T::STAGE);
-                    const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + W_BYTES);
-                    const uint32_t d = tmem + b * TN;
-                    umma_e4m3<false>(d, da, db, idesc);          // 32 columns (32 bytes) a step
-                    umma_e4m3<true>(d, da + 2, db + 2, idesc);
-                    umma_e4m3<true>(d, da + 4, db + 4, idesc);
-                    umma_e4m3<true>(d, da + 6, db + 6, idesc);
-                    ptx::umma_commit(ptx::smem_u32(&ctrl->empty[s]));
+                    const int blocks = min(PER_STEP, it.kb1 - kb);
+                    for (int j = 0; j < blocks; ++j) {
+                        const uint32_t base = ptx::smem_u32(tiles + s * T::STAGE + j * T::BLOCK);
+                        const uint64_t da = ptx::umma_desc_sw128(base), db = ptx::umma_desc_sw128(base + W_BYTES);
+                        const uint32_t d = tmem + (b * PER_STEP + j) * TN;
+                        umma_e4m3<false>(d, da, db, idesc);          // 32 columns (32 bytes) a step
+                        umma_e4m3<true>(d, da + 2, db + 2, idesc);
+                        umma_e4m3<true>(d, da + 4, db + 4, idesc);
+                        umma_e4m3<true>(d, da + 6, db + 6, idesc);
+                    }
                     ptx::umma_commit(ptx::smem_u32(&ctrl->tfull[b]));
+                    ptx::umma_commit(ptx::smem_u32(&ctrl->empty[s]));
                 }
             }
         }
         __syncwarp();
     } else if (warp == WARP_SCALE) {
-        // one product xs * ws per column and block; the loads of four blocks run together, ahead of the waits
+        // one product xs * ws per column and block; the loads of two steps run together, ahead of the waits
         constexpr int PER = (TN + 31) / 32;
-        constexpr int AHEAD = 4;
+        constexpr int AHEAD = 2 * PER_STEP;
         uint32_t n = 0;
         for (int i = blockIdx.x; i < items; i += gridDim.x) {
             const Item it = item_of(a, i, TN);
@@ -245,13 +256,15 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     for (int j = 0; j < PER; ++j) cur[u][j] = next[u][j];
                 if (kb + AHEAD < it.kb1) fetch(kb + AHEAD);
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    if (kb + u >= it.kb1) break;
-                    const uint32_t b = n % SCALE_BUFS;
-                    wait_bar(&ctrl->sempty[b], ((n / SCALE_BUFS) & 1) ^ 1, ctrl, a.status);
+                for (int h = 0; h < 2; ++h) {
+                    if (kb + h * PER_STEP >= it.kb1) break;
+                    const uint32_t b = n % BUFS;
+                    wait_bar(&ctrl->sempty[b], ((n / BUFS) & 1) ^ 1, ctrl, a.status);
 #pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (j * 32 + lane < TN) scales[b * TN + j * 32 + lane] = cur[u][j];
+                    for (int u = 0; u < PER_STEP; ++u)
+#pragma unroll
+                        for (int j = 0; j < PER; ++j)
+                            if (j * 32 + lane < TN) scales[(b * PER_STEP + u) * TN + j * 32 + lane] = cur[h * PER_STEP + u][j];
                     ptx::mbar_arrive(ptx::smem_u32(&ctrl->sfull[b]));
                     ++n;
                 }
@@ -268,30 +281,31 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             float acc[T::COLS];
 #pragma unroll
             for (int c = 0; c < T::COLS; ++c) acc[c] = 0.f;
-            for (int kb = it.kb0; kb < it.kb1; ++kb, ++n) {
-                const uint32_t b = n % T::BUFS, sb = n % SCALE_BUFS;
-                wait_bar(&ctrl->sfull[sb], (n / SCALE_BUFS) & 1, ctrl, a.status);
-                wait_bar(&ctrl->tfull[b], (n / T::BUFS) & 1, ctrl, a.status);
+            for (int kb = it.kb0; kb < it.kb1; kb += PER_STEP, ++n) {
+                const uint32_t b = n % BUFS;
+                wait_bar(&ctrl->sfull[b], (n / BUFS) & 1, ctrl, a.status);
+                wait_bar(&ctrl->tfull[b], (n / BUFS) & 1, ctrl, a.status);
                 ptx::tc_fence_after();
-                const float* sc = scales + sb * TN + half * T::COLS;
 #pragma unroll
-                for (int c0 = 0; c0 < T::COLS; c0 += T::LD) {
+                for (int j = 0; j < PER_STEP; ++j) {
+                    if (j > 0 && kb + j >= it.kb1) break;
+                    const float* sc = scales + (b * PER_STEP + j) * TN + half * T::COLS;
                     uint32_t r[T::LD];
-                    tmem_load<T::LD>(t_lane + b * TN + c0, r);
+                    tmem_load<T::LD>(t_lane + (b * PER_STEP + j) * TN, r);
 #pragma unroll
                     for (int c = 0; c < T::LD; c += 4) {
-                        const float4 f = *reinterpret_cast<const float4*>(sc + c0 + c);
-                        acc[c0 + c] = fmaf(__uint_as_float(r[c]), f.x, acc[c0 + c]);
-                        acc[c0 + c + 1] = fmaf(__uint_as_float(r[c + 1]), f.y, acc[c0 + c + 1]);
-                        acc[c0 + c + 2] = fmaf(__uint_as_float(r[c + 2]), f.z, acc[c0 + c + 2]);
-                        acc[c0 + c + 3] = fmaf(__uint_as_float(r[c + 3]), f.w, acc[c0 + c + 3]);
+                        const float4 f = *reinterpret_cast<const float4*>(sc + c);
+                        acc[c] = fmaf(__uint_as_float(r[c]), f.x, acc[c]);
+                        acc[c + 1] = fmaf(__uint_as_float(r[c + 1]), f.y, acc[c + 1]);
+                        acc[c + 2] = fmaf(__uint_as_float(r[c + 2]), f.z, acc[c + 2]);
+                        acc[c + 3] = fmaf(__uint_as_float(r[c + 3]), f.w, acc[c + 3]);
                     }
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     ptx::mbar_arrive(ptx::smem_u32(&ctrl->tempty[b]));
-                    ptx::mbar_arrive(ptx::smem_u32(&ctrl->sempty[sb]));
+                    ptx::mbar_arrive(ptx::smem_u32(&ctrl->sempty[b]));
                 }
             }
             const int col = it.n0 + quad * 32 + lane;              // column of the output
