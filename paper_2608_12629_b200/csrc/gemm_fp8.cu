@@ -13,8 +13,8 @@
 //   more            X is the M side, two SMs to a 256 x 256 tile (cta_group::2: each loads half of both operands, 32 KiB a block instead
 //                   of the 48 of a 128 x 256 tile of one SM, whose demand of 94 bytes a clock the L2 does not meet).  The scale of an
 //                   element depends on its lane and on its half of the columns: one factor per thread and block, packed FMAs.
-// Where a product has too few tiles for the SMs its contraction is split; the narrow kernel's last CTA of a
-// tile to arrive adds up its (small) parts, a second kernel those of the pairs.
+// Where a product has too few tiles for the SMs its contraction is split; the parts of a narrow tile are added up
+// through the shared memory of a cluster, those of the pairs by a second kernel.
 #include "ptx.cuh"
 #include "serving.cuh"
 
@@ -40,7 +40,6 @@ struct GemmArgs {
     const float* ws;
     void* out;
     float* parts;
-    int* counters;
     int* status;
     i64 M, out_stride;
     int N, nkb, tiles_m, tiles_n, splits;      // tiles_m: of X's rows
@@ -51,7 +50,6 @@ struct __align__(16) Ctrl {
     uint64_t full[8], empty[8], tfull[BUFS], tempty[BUFS], sfull[BUFS], sempty[BUFS];
     uint32_t tmem;
     int abort_flag;
-    int last;
 };
 
 __device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* ctrl, int* status) {
@@ -117,6 +115,12 @@ struct Tile {
     static_assert(SMEM <= 227 * 1024 && TMEM_COLS <= 512, "");
 };
 
+__device__ __forceinline__ void store_one(const GemmArgs& a, i64 row, int col, float v) {
+    if (row >= a.M || col >= a.N) return;
+    if (a.fp32) static_cast<float*>(a.out)[row * a.out_stride + col] = v;
+    else static_cast<cake_bf16*>(a.out)[row * a.out_stride + col] = to_bf16(v);
+}
+
 struct Item {
     int m0, n0, kb0, kb1, split, tile;
 };
@@ -139,6 +143,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     using T = Tile<TN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    float* const part = reinterpret_cast<float*>(tiles);      // [TN][TM], after the loop
     float* const scales = reinterpret_cast<float*>(tiles + T::STAGES * T::STAGE);
     Ctrl* const ctrl = reinterpret_cast<Ctrl*>(scales + BUFS * PER_STEP * TN);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -274,8 +279,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const int half = warp >> 2, quad = warp & 3;      // a warp reads the 32 lanes of its place in its warpgroup
         const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * T::COLS;
         uint32_t n = 0;
-        // (after an expired wait this loop and the scales' run on with waits that return at once: its warps meet at a
-        // barrier below, so all of them have to take every step)
+        // (after an expired wait this loop and the scales' run on with waits that return at once)
         for (int i = blockIdx.x; i < items; i += gridDim.x) {
             const Item it = item_of(a, i, TN);
             float acc[T::COLS];
@@ -308,45 +312,38 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     ptx::mbar_arrive(ptx::smem_u32(&ctrl->sempty[b]));
                 }
             }
-            const int col = it.n0 + quad * 32 + lane;              // column of the output
-            const i64 row0 = static_cast<i64>(it.m0) + half * T::COLS;
-            auto store = [&](int c, float v) {
-                const i64 row = row0 + c;
-                if (row >= a.M || col >= a.N) return;
-                if (a.fp32) static_cast<float*>(a.out)[row * a.out_stride + col] = v;
-                else static_cast<cake_bf16*>(a.out)[row * a.out_stride + col] = to_bf16(v);
-            };
             if (a.splits == 1) {
 #pragma unroll
-                for (int c = 0; c < T::COLS; ++c) store(c, acc[c]);
-                continue;
+                for (int c = 0; c < T::COLS; ++c) store_one(a, static_cast<i64>(it.m0) + half * T::COLS + c, it.n0 + quad * 32 + lane, acc[c]);
+            } else {
+                // (the ring is free: every copy has landed and every instruction that read it is complete)
+#pragma unroll
+                for (int c = 0; c < T::COLS; ++c) part[(half * T::COLS + c) * TM + quad * 32 + lane] = acc[c];
             }
-            // ---- parts of the contraction: the last of the tile's CTAs adds them up in order
-            float* const mine = a.parts + static_cast<i64>(i) * (TM * TN) + (half * T::COLS) * TM + quad * 32 + lane;
-#pragma unroll
-            for (int c = 0; c < T::COLS; ++c) __stcg(mine + c * TM, acc[c]);
-            asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
-            if (threadIdx.x == 0) {
-                __threadfence();
-                const int seen = atomicAdd(a.counters + it.tile, 1);
-                ctrl->last = seen == a.splits - 1;
-                if (ctrl->last) a.counters[it.tile] = 0;
-                __threadfence();
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");
-            if (ctrl->last) {
-#pragma unroll
-                for (int c = 0; c < T::COLS; ++c) acc[c] = 0.f;
-                for (int s = 0; s < a.splits; ++s) {
-                    const float* from = mine + static_cast<i64>(s - it.split) * (TM * TN);
-#pragma unroll
-                    for (int c = 0; c < T::COLS; ++c) acc[c] += __ldcg(from + c * TM);
-                }
-#pragma unroll
-                for (int c = 0; c < T::COLS; ++c) store(c, acc[c]);
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(EPI_WARPS * 32) : "memory");     // ctrl->last is read by all before the next item
         }
+    }
+    if (a.splits > 1) {
+        // ---- The parts of a tile's contraction lie in the shared memories of the CTAs of a cluster (a tile each, in one round): every CTA
+        // adds up its share of the columns, in the order of the parts, and stores it
+        __syncwarp();
+        ptx::cluster_sync_all();
+        const Item it = item_of(a, blockIdx.x, TN);
+        const int c0 = it.split * TN / a.splits, c1 = (it.split + 1) * TN / a.splits;
+        const uint32_t mine = ptx::smem_u32(part);
+        const int lane_w = threadIdx.x % TM;               // row of W
+        for (int c = c0 + threadIdx.x / TM; c < c1; c += THREADS / TM) {
+            float sum = 0.f;
+#pragma unroll 4
+            for (int s = 0; s < a.splits; ++s) {
+                uint32_t from;
+                float v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(mine + (c * TM + lane_w) * 4), "r"(s));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(from) : "memory");
+                sum += v;
+            }
+            store_one(a, static_cast<i64>(it.m0) + c, it.n0 + lane_w, sum);
+        }
+        ptx::cluster_sync_all();                           // no CTA leaves while another reads its part
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -751,12 +748,14 @@ gemm_join_kernel(const GemmArgs a) {
 }  // namespace wide
 
 // ---------------------------------------------------------------------------------------------------------------- host
+constexpr int MOST_PARTS = 8;      // CTAs of a cluster
 struct Plan {
     bool pair;
     int tn, bn, tiles_m, tiles_n, splits, nkb;
     size_t part_bytes;
 };
-Plan plan_of(i64 M, int N, int K, int sms) {
+// clusters[s]: clusters of s CTAs of the narrow kernel that fit the device at once (nullptr: not asked yet; no matter for the workspace)
+Plan plan_of(i64 M, int N, int K, int sms, const int* clusters) {
     Plan p;
     p.nkb = (K + KB - 1) / KB;
     p.pair = M > NARROW_M;
@@ -772,16 +771,53 @@ Plan plan_of(i64 M, int N, int K, int sms) {
         const int tiles_n = (N + bn - 1) / bn;
         const i64 tiles = static_cast<i64>(p.tiles_m) * tiles_n;
         const double block = !p.pair ? 150 : bn == 256 ? 510 : 290, tile = p.pair ? (bn == 256 ? 2000 : 1200) : 1000;
-        for (int s = 1; s == 1 || (s <= p.nkb / 2 && s <= 32 && tiles * s <= units); ++s) {
+        for (int s = 1; s == 1 || (s <= p.nkb / 2 && s <= (p.pair ? 32 : MOST_PARTS) && tiles * s <= units); ++s) {
+            if (s > 1 && !p.pair && clusters && tiles > clusters[s]) continue;
             const double rounds = static_cast<double>((tiles * s + units - 1) / units);
             double cost = rounds * ((p.nkb + s - 1) / s * block + tile);
-            if (s > 1) cost += p.pair ? 3000 + (bn == 256 ? 2000 : 1000) + 300 * s : 1500 + 250 * s;
+            if (s > 1) cost += p.pair ? 3000 + (bn == 256 ? 2000 : 1000) + 300 * s : 700 + 30 * s;
             if (cost < least) least = cost, p.bn = bn, p.tiles_n = tiles_n, p.splits = s;
         }
     }
     const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
-    p.part_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * (p.pair ? wide::BM * p.bn : TM * p.tn) * 4 : 0;
+    p.part_bytes = p.pair && p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * wide::BM * p.bn * 4 : 0;
     return p;
+}
+
+// clusters of 2 .. MOST_PARTS CTAs that are resident at once: fewer than the SMs divided by their size, since a cluster stays inside one
+// group of SMs (asked once per device)
+template <int TN>
+int clusters_of(const DeviceInfo& di, int (&out)[MOST_PARTS + 1]) {
+    static int known[64][MOST_PARTS + 1] = {};
+    const bool keep = di.device >= 0 && di.device < 64;
+    if (!keep || known[di.device][1] == 0) {
+        if (cudaFuncSetAttribute(gemm_fp8_kernel<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<TN>::SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
+        for (int s = 2; s <= MOST_PARTS; ++s) {
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = s;
+            at[0].val.clusterDim.y = 1;
+            at[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(s);
+            cfg.blockDim = dim3(THREADS);
+            cfg.dynamicSmemBytes = Tile<TN>::SMEM;
+            cfg.attrs = at;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, gemm_fp8_kernel<TN>, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                n = 0;
+            }
+            out[s] = n;
+        }
+        out[0] = 0, out[1] = di.sm_count;
+        if (keep)
+            for (int s = MOST_PARTS; s >= 0; --s) known[di.device][s] = out[s];
+        return CAKE_OK;
+    }
+    for (int s = 0; s <= MOST_PARTS; ++s) out[s] = known[di.device][s];
+    return CAKE_OK;
 }
 
 template <int TN>
@@ -793,8 +829,30 @@ int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, cons
         if (di.device >= 0 && di.device < 64) set[di.device] = true;
     }
     const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
-    const int ctas = static_cast<int>(items < di.sm_count ? items : di.sm_count);
-    return launch_early(gemm_fp8_kernel<TN>, dim3(ctas), dim3(THREADS), T::SMEM, s, mw, mx, a) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    if (a.splits == 1) {
+        const int ctas = static_cast<int>(items < di.sm_count ? items : di.sm_count);
+        return launch_early(gemm_fp8_kernel<TN>, dim3(ctas), dim3(THREADS), T::SMEM, s, mw, mx, a) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    }
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;      // the parts of a tile
+    at[0].val.clusterDim.x = a.splits;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // as launch_early
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(items));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = T::SMEM;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<TN>, mw, mx, a) != cudaSuccess) {
+        cudaGetLastError();
+        return CAKE_ERR_CUDA;
+    }
+    note_launches(1);
+    return CAKE_OK;
 }
 
 template <int BN>
@@ -852,7 +910,7 @@ int cake_gemm_fp8_workspace_bytes(long long M, int N, int K, size_t* out_bytes) 
     if (!out_bytes) return CAKE_ERR_NULL;
     const int rc = check_shape(M, N, K);
     if (rc != CAKE_OK) return rc;
-    *out_bytes = kHeaderBytes + plan_of(M, N, K, kMaxSms).part_bytes;
+    *out_bytes = kHeaderBytes + plan_of(M, N, K, kMaxSms, nullptr).part_bytes;
     return CAKE_OK;
 }
 
@@ -869,19 +927,25 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     if (!X || !W || !x_scale || !w_scale || !out) return CAKE_ERR_NULL;
     if (K % 16 != 0 || x_stride % 16 != 0 || w_stride % 16 != 0 || !aligned(X, 16) || !aligned(W, 16)) return CAKE_ERR_ALIGN;
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(out, (flags & CAKE_GEMM_OUT_FP32) ? 4 : 2)) return CAKE_ERR_ALIGN;
-    const Plan p = plan_of(M, N, K, kMaxSms);
+    Plan p = plan_of(M, N, K, kMaxSms, nullptr);
     if (ws_bytes < kHeaderBytes + p.part_bytes) return CAKE_ERR_WORKSPACE;
     DeviceInfo di;
     rc = current_device_info(&di);
     if (rc != CAKE_OK) return rc;
     if (di.cc_major != 10) return CAKE_ERR_DEVICE;
+    if (!p.pair) {
+        int clusters[MOST_PARTS + 1];
+        rc = p.tn == 16 ? clusters_of<16>(di, clusters) : p.tn == 32 ? clusters_of<32>(di, clusters) : clusters_of<64>(di, clusters);
+        if (rc != CAKE_OK) return rc;
+        p = plan_of(M, N, K, kMaxSms, clusters);
+    }
     CUtensorMap mw, mx;
     rc = make_tmap_bytes(&mw, W, K, N, w_stride, p.pair ? 64 : TM);
     if (rc != CAKE_OK) return rc;
     rc = make_tmap_bytes(&mx, X, K, M, x_stride, p.pair ? 128 : p.tn);
     if (rc != CAKE_OK) return rc;
     GemmArgs a;
-    a.xs = x_scale, a.ws = w_scale, a.out = out, a.status = static_cast<int*>(ws), a.counters = static_cast<int*>(ws) + 64;
+    a.xs = x_scale, a.ws = w_scale, a.out = out, a.status = static_cast<int*>(ws);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes);
     a.M = M, a.out_stride = out_stride, a.N = N, a.nkb = p.nkb, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n, a.splits = p.splits;
     a.fp32 = flags & CAKE_GEMM_OUT_FP32;

@@ -230,11 +230,12 @@ def test_gemm_nan_stays_in_its_row_and_column():
 def test_gemm_refusals():
     x, xs, w, ws = gemm_inputs(8, 32, 128, 2)
     assert cake.cake_gemm_fp8(x[:0], xs[:0], w, ws).shape == (0, 32)
-    small = torch.zeros(cake.CAKE_SERVING_HEADER_BYTES, dtype=torch.uint8, device=DEV)
-    x2, xs2, w2, ws2 = gemm_inputs(8, 128, 4096, 2)
-    with pytest.raises(cake.CakeError) as e:
-        cake.cake_gemm_fp8(x2, xs2, w2, ws2, ws=small)
-    assert e.value.code == cake.CAKE_ERR_WORKSPACE
+    for M in (8, 200):
+        x2, xs2, w2, ws2 = gemm_inputs(M, 128, 4096, 2)
+        small = torch.zeros(cake.cake_gemm_fp8_workspace_bytes(M, 128, 4096) - 1, dtype=torch.uint8, device=DEV)
+        with pytest.raises(cake.CakeError) as e:
+            cake.cake_gemm_fp8(x2, xs2, w2, ws2, ws=small)
+        assert e.value.code == cake.CAKE_ERR_WORKSPACE
     x3, xs3, w3, ws3 = gemm_inputs(8, 32, 120, 2)
     with pytest.raises(cake.CakeError) as e:
         cake.cake_gemm_fp8(x3, xs3, w3, ws3)
