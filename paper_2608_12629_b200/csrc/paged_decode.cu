@@ -705,11 +705,11 @@ paged_decode_kernel(const DecodeArgs a) {
             } else {
                 __syncthreads();
                 if (tid == 0) {
-                    __threadfence();
-                    const int before_me = atomicAdd(a.counters + c0, 1);
+                    // releases the CTA's part (ordered before this thread by the barrier) and acquires those of the CTAs ahead
+                    int before_me;
+                    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before_me) : "l"(a.counters + c0) : "memory");
                     last_flag = before_me == c1 - c0;
                     if (last_flag) a.counters[c0] = 0;       // ready for the next call
-                    __threadfence();
                 }
                 __syncthreads();
                 if (last_flag) {
