@@ -36,8 +36,9 @@ typedef unsigned char cake_e4m3;
  *   residual     [T][H] bf16, rows residual_stride apart, in, may be NULL
  *   weight       [H] bf16, in, may be NULL (all ones)
  *   group        128: one scale per 128 columns (the last group may be shorter); 0: one scale per row
- *   out_residual [T][H] bf16 contiguous, out, may be NULL: s rounded.  May be the buffer of x or of residual
- *   out_y        [T][H] bf16 contiguous, out, may be NULL: y rounded.  May be the buffer of x
+ *   out_residual [T][H] bf16 contiguous, out, may be NULL: s rounded.  May be the buffer of x or of residual where that is
+ *                contiguous too (a row is read before it is written; no other overlap)
+ *   out_y        [T][H] bf16 contiguous, out, may be NULL: y rounded.  May be the buffer of x likewise
  *   out_q        [T][H] e4m3 contiguous, out, may be NULL;  out_scale [T][ceil(H/128) or 1] fp32, with out_q
  *   flags        CAKE_RMSNORM_NONE: no norm (y = s * weight): quantises alone
  * H <= 32768 (CAKE_ERR_UNSUPPORTED beyond).  Pointers are aligned to their elements; rows and bases that are multiples of

@@ -249,7 +249,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 #pragma unroll
                     for (int j = 0; j < PER; ++j) {
                         const i64 m = static_cast<i64>(it.m0) + j * 32 + lane;
-                        next[u][j] = (kb + u < it.kb1 && m < a.M) ? __ldg(a.xs + m * a.nkb + kb + u) * __ldg(wrow + kb + u) : 0.f;
+                        next[u][j] = (kb + u < it.kb1 && m < a.M) ? a.xs[m * a.nkb + kb + u] * wrow[kb + u] : 0.f;
                     }
             };
             fetch(it.kb0);
@@ -582,14 +582,14 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             float xn[GROUP], wn[GROUP], sc[GROUP], s_now = 0.f;
             auto fetch = [&](int kb) {
                 if (a.xs_wide && kb % GROUP == 0 && kb + GROUP <= it.kb1) {
-                    const float4 u = __ldg(reinterpret_cast<const float4*>(xs + kb)), v = __ldg(reinterpret_cast<const float4*>(ws + kb));
+                    const float4 u = *reinterpret_cast<const float4*>(xs + kb), v = *reinterpret_cast<const float4*>(ws + kb);
                     xn[0] = u.x, xn[1] = u.y, xn[2] = u.z, xn[3] = u.w;
                     wn[0] = v.x, wn[1] = v.y, wn[2] = v.z, wn[3] = v.w;
                 } else {
 #pragma unroll
                     for (int u = 0; u < GROUP; ++u) {
-                        xn[u] = kb + u < it.kb1 ? __ldg(xs + kb + u) : 0.f;
-                        wn[u] = kb + u < it.kb1 ? __ldg(ws + kb + u) : 0.f;
+                        xn[u] = kb + u < it.kb1 ? xs[kb + u] : 0.f;
+                        wn[u] = kb + u < it.kb1 ? ws[kb + u] : 0.f;
                     }
                 }
             };

@@ -86,7 +86,7 @@ kv_append_kernel(const AppendArgs a) {
         const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
         constexpr int N = PAIRS ? 4 : 8;
 #pragma unroll
-        for (int j = 0; j < N; ++j) cs[j] = __ldg(row + N * u + j), sn[j] = __ldg(row + half + N * u + j);
+        for (int j = 0; j < N; ++j) cs[j] = row[N * u + j], sn[j] = row[half + N * u + j];
     }
     const int hq = a.q ? a.Hq : 0;
     const int heads = hq + (p.kv ? 2 * a.c.Hkv : 0);
@@ -137,7 +137,7 @@ kv_append_kernel(const AppendArgs a) {
                 const i64 at = is_v ? p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d0
                                     : p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride + d0;
                 const float* scale = is_v ? a.c.v_scale : a.c.k_scale;
-                const float inv = E4M3 && scale ? 1.f / __ldg(scale + g) : 1.f;
+                const float inv = E4M3 && scale ? 1.f / scale[g] : 1.f;
                 void* const base = is_v ? a.c.v : a.c.k;
                 store8<E4M3>(base, at, x, inv);
                 if (two) store8<E4M3>(base, at + half, y, inv);
@@ -172,7 +172,7 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
         float x = bf16_f(src[d]), y = 0.f;
         if (turns) {
             const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
-            const float c = __ldg(row + u), s = __ldg(row + half + u);
+            const float c = row[u], s = row[half + u];
             const float o = bf16_f(src[e]);
             y = o * c + x * s;
             x = x * c - o * s;
@@ -183,7 +183,7 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
             if (turns) dst[e] = to_bf16(y);
         } else {
             const i64 at = p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride;
-            const float sc = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + g) : 1.f;
+            const float sc = E4M3 && a.c.k_scale ? a.c.k_scale[g] : 1.f;
             put(a.c.k, at + d, x, sc);
             if (turns) put(a.c.k, at + e, y, sc);
         }
@@ -192,7 +192,7 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
     for (int i = threadIdx.x; i < a.c.Hkv * D; i += blockDim.x) {
         const int g = i / D, d = i - g * D;
         const i64 at = p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d;
-        put(a.c.v, at, bf16_f(a.v[t * a.v_stride + static_cast<i64>(g) * D + d]), E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + g) : 1.f);
+        put(a.c.v, at, bf16_f(a.v[t * a.v_stride + static_cast<i64>(g) * D + d]), E4M3 && a.c.v_scale ? a.c.v_scale[g] : 1.f);
     }
 }
 

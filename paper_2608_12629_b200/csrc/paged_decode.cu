@@ -239,7 +239,7 @@ paged_join_kernel(const DecodeArgs a, bool e4m3) {
                 sum = fmaf(mls[k].y, f, sum);
                 acc.x = fmaf(v.x, f, acc.x), acc.y = fmaf(v.y, f, acc.y), acc.z = fmaf(v.z, f, acc.z), acc.w = fmaf(v.w, f, acc.w);
             }
-            const float vs = e4m3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
+            const float vs = e4m3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
             write_out<D>(a, static_cast<i64>(e.b) * a.Hq + e.g * a.G + e.run * HEADS + h, d, acc, up, sum, vs);
         }
         __syncthreads();
@@ -377,7 +377,7 @@ paged_decode_kernel(const DecodeArgs a) {
         // the table entry of this lane's key of a step; -1: no such key
         auto page_at = [&](int step) -> int {
             const int key = key0 + step * TILE;
-            return (step < n_tiles && key < end) ? __ldg(table + page_of(key)) : -1;
+            return (step < n_tiles && key < end) ? table[page_of(key)] : -1;
         };
         // fetches a step; returns the mask of its keys that are there
         auto copy = [&](int step, int entry, uint32_t s) -> uint32_t {
@@ -447,7 +447,7 @@ paged_decode_kernel(const DecodeArgs a) {
                     if (h < heads) {
                         const cake_bf16* from = src + 4 * c * EL + 8 * j;
                         if (a.q_wide) {
-                            u = __ldg(reinterpret_cast<const uint4*>(from));
+                            u = *reinterpret_cast<const uint4*>(from);
                         } else {
                             auto two = [&](int i) { return static_cast<uint32_t>(from[i]) | (static_cast<uint32_t>(from[i + 1]) << 16); };
                             u = make_uint4(two(0), two(2), two(4), two(6));
@@ -478,7 +478,7 @@ paged_decode_kernel(const DecodeArgs a) {
             for (int c = 0; c < L::CK; ++c)
 #pragma unroll
                 for (int j = 0; j < EL / 2; ++j) qf[n][c * (EL / 4) + j / 2][j & 1] = w[c][j];
-            const float ks = E4M3 && a.c.k_scale ? __ldg(a.c.k_scale + e.g) : 1.f;
+            const float ks = E4M3 && a.c.k_scale ? a.c.k_scale[e.g] : 1.f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 factor[n][i] = a.scale * LOG2E * ks * __shfl_sync(0xffffffffu, unit, (2 * t4 + i) * 4);
@@ -669,7 +669,7 @@ paged_decode_kernel(const DecodeArgs a) {
         const bool whole = tile0 == 0 && n_tiles == e.tiles;
         constexpr int PART = HEADS * (D + 4);            // floats of a part: O of the run's heads, then m and l (and padding)
         float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
-        const float vs = E4M3 && a.c.v_scale ? __ldg(a.c.v_scale + e.g) : 1.f;
+        const float vs = E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
         auto finish = [&](int h, int d, const float4& acc, float top, float sum) { write_out<D>(a, out0 + h, d, acc, top, sum, vs); };
         for (int i = tid; i < heads * (D / 4); i += THREADS) {

@@ -118,14 +118,14 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         for (int v = 0; v < NV; ++v) {
             const int c = col0 + v * step;
             if (WIDE) {
-                const uint4 u = c < a.H ? __ldg(reinterpret_cast<const uint4*>(a.w + c)) : make_uint4(0, 0, 0, 0);
+                const uint4 u = c < a.H ? *reinterpret_cast<const uint4*>(a.w + c) : make_uint4(0, 0, 0, 0);
                 wr[v][0] = u.x, wr[v][1] = u.y, wr[v][2] = u.z, wr[v][3] = u.w;
             } else if (PAIR) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) wr[v][j] = c + 64 * j < a.H ? __ldg(reinterpret_cast<const uint32_t*>(a.w + c + 64 * j)) : 0u;
+                for (int j = 0; j < 2; ++j) wr[v][j] = c + 64 * j < a.H ? *reinterpret_cast<const uint32_t*>(a.w + c + 64 * j) : 0u;
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) wr[v][j] = c + 32 * j < a.H ? __ldg(a.w + c + 32 * j) : 0u;
+                for (int j = 0; j < 4; ++j) wr[v][j] = c + 32 * j < a.H ? a.w[c + 32 * j] : 0u;
             }
         }
     };

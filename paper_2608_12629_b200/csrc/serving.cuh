@@ -23,7 +23,8 @@ static_assert(kHeaderBytes == CAKE_SERVING_HEADER_BYTES, "header and ABI constan
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // Launch that may begin while the kernel ahead of it in the stream drains: the kernel waits for that one itself (ptx::grid_dep_wait,
-// before its first access to global memory).  In a stream of short kernels this hides their launch.
+// before its first access to global memory).  In a stream of short kernels this hides their launch.  Such a kernel runs while its
+// inputs are still written, so it reads them by plain loads: none of them is constant for the kernel's whole life.
 template <class... P, class... A>
 cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
     cudaLaunchAttribute at[1];

@@ -331,6 +331,28 @@ def test_append_places_that_do_not_exist():
     assert (out[3] == 9.0).all()                     # a position without a row in the table: nothing of the token is written
 
 
+@pytest.mark.parametrize("pairs", [False, True])
+def test_append_unaligned_sources(pairs):
+    """Keys, values and queries at odd addresses and strides: the element-wise kernel, against the wide one bit for bit."""
+    g = gen(8)
+    T, Hq, Hkv, D = 9, 3, 2, 128
+    q, k, v = normal(g, T, Hq, D), normal(g, T, Hkv, D), normal(g, T, Hkv, D)
+    slots, pos, table = torch.arange(T, device=DEV), torch.arange(T, dtype=torch.int32, device=DEV) * 7, rotary_table(64, 64)
+    caches = [[torch.zeros(2, 8, Hkv, D, dtype=kv, device=DEV) for _ in range(2)] for kv in (BF16, BF16)]
+    outs = []
+    for i, c in enumerate(caches):
+        args = (k, v, q)
+        if i:
+            args = []
+            for t in (k, v, q):
+                buf = torch.zeros(T * (t[0].numel() + 1) + 1, dtype=BF16, device=DEV)
+                odd = torch.as_strided(buf, t.shape, (t[0].numel() + 1, D, 1), 1)
+                odd.copy_(t)
+                args.append(odd)
+        outs.append(cake.cake_kv_append(cake.PagedCache(*c), args[0], args[1], slots, pos, table, q=args[2], interleaved=pairs))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
+
+
 def test_append_in_place_queries_and_refusals():
     g = gen(6)
     kc = torch.zeros(4, 8, 2, 128, dtype=BF16, device=DEV)
@@ -571,6 +593,21 @@ def test_decode_scale_strides_streams_and_graphs():
     graph.replay()
     torch.cuda.synchronize()
     check_decode(q, cache, table, n, mine, None, scale=0.3)
+
+
+@pytest.mark.parametrize("kv", [BF16, E4M3])
+def test_decode_unaligned_queries_and_output(kv):
+    """Queries and output on odd addresses take element-wise accesses; a table of no pages leaves every row empty."""
+    q, cache, table, n = decode_problem(6, 2, 128, 16, kv, [90, 0, 300], 31)
+    buf = torch.zeros(3 * 7 * 129 + 1, dtype=BF16, device=DEV)
+    odd = torch.as_strided(buf, (3, 6, 128), (7 * 129, 129, 1), 1)
+    odd.copy_(q)
+    out = torch.zeros(q.numel() + 1, dtype=BF16, device=DEV)[1:].view(q.shape)
+    want, _ = cake.cake_paged_decode(q, cache, table, n)
+    cake.cake_paged_decode(odd, cache, table, n, out=out)
+    assert torch.equal(out, want)
+    none, lse = cake.cake_paged_decode(q, cache, table[:, :0], torch.zeros_like(n), want_lse=True)
+    assert (none == 0).all() and (lse == -math.inf).all()
 
 
 def test_decode_pages_that_do_not_exist():
