@@ -72,7 +72,6 @@ __global__ void __launch_bounds__(288)
 kv_append_kernel(const AppendArgs a) {
     const i64 t = blockIdx.x;
     const int u = threadIdx.x;
-    ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     const Place p = place_of(a, t, threadIdx.x == 0 && threadIdx.y == 0);
     if (!p.rotate_ok) return;
@@ -86,7 +85,11 @@ kv_append_kernel(const AppendArgs a) {
         const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
         constexpr int N = PAIRS ? 4 : 8;
 #pragma unroll
-        for (int j = 0; j < N; ++j) cs[j] = row[N * u + j], sn[j] = row[half + N * u + j];
+        for (int j = 0; j < N; j += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(row + N * u + j), w = *reinterpret_cast<const float4*>(row + half + N * u + j);
+            cs[j] = c.x, cs[j + 1] = c.y, cs[j + 2] = c.z, cs[j + 3] = c.w;
+            sn[j] = w.x, sn[j + 1] = w.y, sn[j + 2] = w.z, sn[j + 3] = w.w;
+        }
     }
     const int hq = a.q ? a.Hq : 0;
     const int heads = hq + (p.kv ? 2 * a.c.Hkv : 0);
@@ -151,7 +154,6 @@ template <bool E4M3>
 __global__ void __launch_bounds__(256)
 kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
     const i64 t = blockIdx.x;
-    ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     const Place p = place_of(a, t, threadIdx.x == 0);
     if (!p.rotate_ok) return;
@@ -250,7 +252,7 @@ extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k,
     const bool pairs = flags & CAKE_APPEND_INTERLEAVED;
     const bool e4m3 = cache->type == CAKE_KV_E4M3;
     const int D = cache->D;
-    const bool wide = (pairs ? rot % 8 == 0 : rot % 16 == 0) && k_stride % 8 == 0 && v_stride % 8 == 0 && aligned(k, 16) && aligned(v, 16) &&
+    const bool wide = (pairs ? rot % 8 == 0 : rot % 16 == 0) && aligned(cos_sin, 16) && k_stride % 8 == 0 && v_stride % 8 == 0 && aligned(k, 16) && aligned(v, 16) &&
                       (!q || (q_stride % 8 == 0 && aligned(q, 16) && aligned(out_q, 16)));
     const unsigned blocks = static_cast<unsigned>(T);
     cudaError_t e;

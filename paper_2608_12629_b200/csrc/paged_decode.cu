@@ -274,7 +274,7 @@ paged_decode_kernel(const DecodeArgs a) {
         ptx::fence_mbar_init();
     }
 
-    ptx::grid_dep_launch();          // (the next kernel, a joining one too, waits for the end of this one by itself)
+
     ptx::grid_dep_wait();
     // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
     const int per = (a.B + THREADS - 1) / THREADS;

@@ -106,7 +106,6 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         }
     };
     i64 row = static_cast<i64>(blockIdx.x) * per_block + sub;
-    ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     if (WIDE) load(row);
     // a thread has the same columns in every row: where the registers allow, its weights stay in them
