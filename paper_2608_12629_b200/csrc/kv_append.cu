@@ -64,13 +64,24 @@ __device__ __forceinline__ void store8(void* base, i64 at, const float (&f)[8], 
     }
 }
 
-// Block (units, heads in parallel): thread (u, y) takes unit u of the heads y, y + blockDim.y, ... of the token's
+// (a, b) -> (a c - b s, b c + a s) for two pairs at a time (packed instructions: issue is half of what bounds the kernel)
+__device__ __forceinline__ void turn2(float& a0, float& a1, float& b0, float& b1, float c0, float c1, float s0, float s1) {
+    asm("{\n\t.reg .b64 a, b, c, s, t, u, n;\n\t"
+        "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tmov.b64 c, {%4, %5};\n\tmov.b64 s, {%6, %7};\n\tmov.b64 n, {%8, %9};\n\t"
+        "mul.rn.f32x2 t, b, n;\n\tfma.rn.f32x2 t, a, c, t;\n\t"
+        "mul.rn.f32x2 u, a, s;\n\tfma.rn.f32x2 u, b, c, u;\n\t"
+        "mov.b64 {%0, %1}, t;\n\tmov.b64 {%2, %3}, u;\n\t}"
+        : "+f"(a0), "+f"(a1), "+f"(b0), "+f"(b1) : "f"(c0), "f"(c1), "f"(s0), "f"(s1), "f"(-s0), "f"(-s1));
+}
+
+// Block (units, heads in parallel, tokens): thread (u, y, z) takes of token z unit u of the heads y, y + blockDim.y, ... of the token's
 // Hq query, Hkv key and Hkv value heads, four heads' loads in flight.  A unit is 8 neighbouring elements, or two such runs rot/2
 // apart that rotate into each other (PAIRS false, the first rot/16 units of a head).
 template <bool E4M3, bool PAIRS>
 __global__ void __launch_bounds__(288)
 kv_append_kernel(const AppendArgs a) {
-    const i64 t = blockIdx.x;
+    const i64 t = static_cast<i64>(blockIdx.x) * blockDim.z + threadIdx.z;
+    if (t >= a.T) return;
     const int u = threadIdx.x;
     ptx::grid_dep_wait();
     const Place p = place_of(a, t, threadIdx.x == 0 && threadIdx.y == 0);
@@ -118,11 +129,7 @@ kv_append_kernel(const AppendArgs a) {
             if (turns && !is_v) {
                 if (!PAIRS) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float r = x[j] * cs[j] - y[j] * sn[j];
-                        y[j] = y[j] * cs[j] + x[j] * sn[j];
-                        x[j] = r;
-                    }
+                    for (int j = 0; j < 8; j += 2) turn2(x[j], x[j + 1], y[j], y[j + 1], cs[j], cs[j + 1], sn[j], sn[j + 1]);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -259,12 +266,21 @@ extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k,
     if (wide) {
         const int units = pairs ? D / 8 : rot / 16 + (D - rot) / 8;
         const int heads = (q ? Hq : 0) + 2 * cache->Hkv;
-        // four heads to a thread where that leaves 128 threads or more
-        const int most = (heads + 3) / 4 * units >= 128 ? (heads + 3) / 4 : heads;
-        const int par = most * units <= 256 ? most : (256 + units - 1) / units;
+        // Few tokens: a head to a thread (latency).  More: four heads to a thread, whose loads overlap and share the token's row of the
+        // table, in blocks of 128 threads (one or more tokens) and, where those are plenty, of a single warp: 16,001 tokens of 32 + 2 * 8 heads
+        // into an 8-bit cache 78 us with 128 threads, 63 with 32; 300 tokens 3.1 us with 128, 4.9 with 32
+        int par, tokens = 1;
+        if (T <= 128) {
+            par = heads * units <= 256 ? heads : (256 + units - 1) / units;
+        } else {
+            const int target = T >= 2048 ? 32 : 128;
+            const int most = target / units > 0 ? target / units : 1;
+            par = (heads + 3) / 4 <= most ? (heads + 3) / 4 : most;
+            tokens = target / (units * par) > 0 ? target / (units * par) : 1;
+        }
         void (*const kernel)(const AppendArgs) = e4m3 ? (pairs ? kv_append_kernel<true, true> : kv_append_kernel<true, false>)
                                                       : (pairs ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
-        e = launch_early(kernel, dim3(blocks), dim3(units, par), 0, s, a);
+        e = launch_early(kernel, dim3((blocks + tokens - 1) / tokens), dim3(units, par, tokens), 0, s, a);
     } else {
         e = launch_early(e4m3 ? kv_append_scalar_kernel<true> : kv_append_scalar_kernel<false>, dim3(blocks), dim3(256), 0, s, a, pairs);
     }

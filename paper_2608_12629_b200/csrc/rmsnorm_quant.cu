@@ -54,6 +54,21 @@ __device__ __forceinline__ float recip(float x) {
     return y;
 }
 
+// two floats at a time (one instruction): the kernel is bound by issue as much as by memory
+__device__ __forceinline__ void mul2(float& a, float& b, float x, float y) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmul.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tadd.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+// (a, b) += (x^2, y^2)
+__device__ __forceinline__ void square2(float& a, float& b, float x, float y) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tfma.rn.f32x2 u, v, v, u;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
 // LOADS says how a lane's elements lie in a chunk: WIDE, 8 neighbours of a 256-element chunk (two groups of 128 = half a warp each) in one 16-byte
 // load; PAIRS, two pairs 64 apart of a 128-element chunk (one group); SINGLE, four elements 32 apart of one: rows of any length
 // and alignment.
@@ -134,16 +149,26 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         const bool live = row < a.T;
         if (!WIDE) load(row);
         float s[NV][E];
-        float ss = 0.f;
+        float ss = 0.f, ss_odd = 0.f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            if (WIDE) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                if (WIDE) s[v][j] = (j & 1) ? bf16_hi(raw[v][j / 2]) + bf16_hi(raw[v][E - 4 + j / 2]) : bf16_lo(raw[v][j / 2]) + bf16_lo(raw[v][E - 4 + j / 2]);
-                else if (PAIR) s[v][j] = (j & 1) ? bf16_hi(raw[v][j / 2]) + bf16_hi(raw[v][2 + j / 2]) : bf16_lo(raw[v][j / 2]) + bf16_lo(raw[v][2 + j / 2]);
-                else s[v][j] = bf16_lo(raw[v][j]) + bf16_hi(raw[v][j]);
-                ss = fmaf(s[v][j], s[v][j], ss);
+                for (int j = 0; j < E; j += 2) {
+                    s[v][j] = bf16_lo(raw[v][j / 2]), s[v][j + 1] = bf16_hi(raw[v][j / 2]);
+                    add2(s[v][j], s[v][j + 1], bf16_lo(raw[v][E - 4 + j / 2]), bf16_hi(raw[v][E - 4 + j / 2]));
+                    square2(ss, ss_odd, s[v][j], s[v][j + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    if (PAIR) s[v][j] = (j & 1) ? bf16_hi(raw[v][j / 2]) + bf16_hi(raw[v][2 + j / 2]) : bf16_lo(raw[v][j / 2]) + bf16_lo(raw[v][2 + j / 2]);
+                    else s[v][j] = bf16_lo(raw[v][j]) + bf16_hi(raw[v][j]);
+                    ss = fmaf(s[v][j], s[v][j], ss);
+                }
             }
+        }
+        ss += ss_odd;
         const i64 now = row;
         row += static_cast<i64>(gridDim.x) * per_block;
         if (WIDE && first + static_cast<i64>(gridDim.x) * per_block < a.T) load(row);
@@ -173,7 +198,10 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int j = 0; j < E; ++j) s[v][j] *= (WIDE || PAIR) ? ((j & 1) ? bf16_hi(wr[v][j / 2]) : bf16_lo(wr[v][j / 2])) : bf16_lo(wr[v][j % 4]);
+                for (int j = 0; j < E; ++j)
+                    if (WIDE) {
+                        if (!(j & 1)) mul2(s[v][j], s[v][(j + 1) % E], bf16_lo(wr[v][j / 2]), bf16_hi(wr[v][j / 2]));
+                    } else s[v][j] *= (WIDE || PAIR) ? ((j & 1) ? bf16_hi(wr[v][j / 2]) : bf16_lo(wr[v][j / 2])) : bf16_lo(wr[v][j % 4]);
         }
         float rs = 1.f;
         if (a.norm) {
@@ -184,10 +212,11 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         auto write_q = [&](int v, float f) {           // f: rs / scale
             const int c = col0 + v * step;
             if (WIDE) {
+#pragma unroll
+                for (int j = 0; j < E; j += 2) mul2(s[v][j], s[v][(j + 1) % E], f, f);
                 if (c < a.H)
                     *reinterpret_cast<uint2*>(a.out_q + now * a.H + c) =
-                        make_uint2(pack4_e4m3(s[v][0] * f, s[v][1] * f, s[v][2] * f, s[v][3] * f),
-                                   pack4_e4m3(s[v][E - 4] * f, s[v][E - 3] * f, s[v][E - 2] * f, s[v][E - 1] * f));
+                        make_uint2(pack4_e4m3(s[v][0], s[v][1], s[v][2], s[v][3]), pack4_e4m3(s[v][E - 4], s[v][E - 3], s[v][E - 2], s[v][E - 1]));
             } else if (PAIR) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
