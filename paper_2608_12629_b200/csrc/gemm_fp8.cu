@@ -330,18 +330,25 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const Item it = item_of(a, blockIdx.x, TN);
         const int c0 = it.split * TN / a.splits, c1 = (it.split + 1) * TN / a.splits;
         const uint32_t mine = ptx::smem_u32(part);
-        const int lane_w = threadIdx.x % TM;               // row of W
-        for (int c = c0 + threadIdx.x / TM; c < c1; c += THREADS / TM) {
-            float sum = 0.f;
+        const int w4 = 4 * (threadIdx.x % (TM / 4));       // four rows of W
+        for (int c = c0 + threadIdx.x / (TM / 4); c < c1; c += THREADS / (TM / 4)) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
             for (int s = 0; s < a.splits; ++s) {
                 uint32_t from;
-                float v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(mine + (c * TM + lane_w) * 4), "r"(s));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(from) : "memory");
-                sum += v;
+                float4 v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(mine + (c * TM + w4) * 4), "r"(s));
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(from) : "memory");
+                sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
             }
-            store_one(a, static_cast<i64>(it.m0) + c, it.n0 + lane_w, sum);
+            const i64 row = static_cast<i64>(it.m0) + c;
+            const int col = it.n0 + w4;
+            if (a.out_wide && row < a.M && col + 4 <= a.N) {
+                if (a.fp32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + row * a.out_stride + col) = sum;
+                else *reinterpret_cast<uint2*>(static_cast<cake_bf16*>(a.out) + row * a.out_stride + col) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
+            } else {
+                store_one(a, row, col, sum.x), store_one(a, row, col + 1, sum.y), store_one(a, row, col + 2, sum.z), store_one(a, row, col + 3, sum.w);
+            }
         }
         ptx::cluster_sync_all();                           // no CTA leaves while another reads its part
     }
@@ -405,18 +412,6 @@ __device__ __forceinline__ bool pair_aborted(PairCtrl* ctrl) { return *reinterpr
 // the same place in rank 0's shared memory
 __device__ __forceinline__ uint32_t at_rank0(const void* p) { return ptx::smem_u32(p) & ~ptx::CLUSTER_PEER_BIT; }
 
-// the first `left` elements of 16 bytes; out of line: the edges of a matrix alone take it
-__device__ __noinline__ void store_ragged(const uint4 u, uint8_t* dst, int elem, int left) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    for (int q = 0; q < 4; ++q) {
-        if (elem == 4) {
-            if (q < left) reinterpret_cast<uint32_t*>(dst)[q] = w[q];
-        } else {
-            if (2 * q < left) reinterpret_cast<uint16_t*>(dst)[2 * q] = static_cast<uint16_t>(w[q]);
-            if (2 * q + 1 < left) reinterpret_cast<uint16_t*>(dst)[2 * q + 1] = static_cast<uint16_t>(w[q] >> 16);
-        }
-    }
-}
 template <bool ACC>
 __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc) {
     asm volatile(
@@ -664,13 +659,24 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             const uint8_t* const get = stage_out + (lane >> 2) * OUT_PITCH + (lane & 3) * 16;
             auto flush = [&](int run) {                                     // the run-th 64 bytes of the warp's rows
                 __syncwarp();
+                if (whole) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(get + k * 8 * OUT_PITCH);
-                    if (row0 + 8 * k < n_rows) {
-                        uint8_t* const dst = to + 8 * k * pitch + run * 64;
-                        if (whole) *reinterpret_cast<uint4*>(dst) = u;
-                        else store_ragged(u, dst, elem, n_cols - col0 - run * 4 * per);
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(get + k * 8 * OUT_PITCH);
+                        if (row0 + 8 * k < n_rows) *reinterpret_cast<uint4*>(to + 8 * k * pitch + run * 64) = u;
+                    }
+                } else {        // edges, and rows that are no multiple of 16 bytes apart: element by element, a row's next to each other
+                    const int wide = 64 / elem, c = lane % wide, col = it.n0 + half * COLS + run * wide + c;
+                    const i64 first = static_cast<i64>(it.m0) + rank * 128 + quad * 32;
+                    if (col < n_cols) {
+#pragma unroll 4
+                        for (int r = lane / wide; r < 32; r += 32 / wide) {
+                            if (first + r >= n_rows) break;
+                            const uint8_t* from = stage_out + r * OUT_PITCH + c * elem;
+                            uint8_t* dst = static_cast<uint8_t*>(a.out) + (first + r) * pitch + static_cast<i64>(col) * elem;
+                            if (fp32) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(from);
+                            else *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(from);
+                        }
                     }
                 }
                 __syncwarp();

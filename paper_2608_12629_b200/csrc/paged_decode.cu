@@ -276,25 +276,19 @@ paged_decode_kernel(const DecodeArgs a) {
 
 
     ptx::grid_dep_wait();
-    // ---- the number of tiles of all entries, and the sequence that holds this CTA's first tile
-    const int per = (a.B + THREADS - 1) / THREADS;
-    auto tiles_of_sequence = [&](int b) -> i64 {
-        i64 n = 0;
+    // ---- the number of tiles of all entries, and the one that holds this CTA's first tile
+    // A unit is a sequence (all heads alike) or, where heads have lengths of their own, one head of a sequence
+    const int units = shared_lens ? a.B : a.B * Hkv;
+    const int per = (units + THREADS - 1) / THREADS;
+    const int repeats = (shared_lens ? Hkv : 1) * a.chunks;          // entries of a unit, all of as many tiles
+    auto tiles_of_unit = [&](int u) -> int {
         int first, count;
         bool cut;
-        if (shared_lens) {
-            span_of(a, b, 0, first, count, cut);
-            n = static_cast<i64>(tiles_of<TILE>(count)) * Hkv;
-        } else {
-            for (int g = 0; g < Hkv; ++g) {
-                span_of(a, b, g, first, count, cut);
-                n += tiles_of<TILE>(count);
-            }
-        }
-        return n * a.chunks;
+        span_of(a, shared_lens ? u : u / Hkv, shared_lens ? 0 : u % Hkv, first, count, cut);
+        return tiles_of<TILE>(count);
     };
     i64 mine = 0;
-    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) mine += tiles_of_sequence(b);
+    for (int u = tid * per; u < min(units, (tid + 1) * per); ++u) mine += static_cast<i64>(tiles_of_unit(u)) * repeats;
     i64 before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -315,18 +309,17 @@ paged_decode_kernel(const DecodeArgs a) {
     const i64 lo = cta * total / n_ctas, hi = (cta + 1) * total / n_ctas;
     if (before <= lo && lo < before + mine) {
         i64 at = before;
-        int b = tid * per;
-        for (;; ++b) {
-            const i64 n = tiles_of_sequence(b);
+        int u = tid * per;
+        i64 n;
+        for (;; ++u, at += n) {
+            n = static_cast<i64>(tiles_of_unit(u)) * repeats;
             if (lo < at + n) break;
-            at += n;
         }
-        found_b = b;
+        found_b = u;
         found_start = at;
     }
     __syncthreads();
-    Cursor e;
-    e.b = found_b, e.g = 0, e.run = 0, e.start = found_start;
+    Cursor e{};
     bool cut;
     auto look = [&]() {
         span_of(a, e.b, e.g, e.first, e.count, cut);
@@ -340,8 +333,13 @@ paged_decode_kernel(const DecodeArgs a) {
             if (++e.g == Hkv) e.g = 0, ++e.b;
         }
     };
+    e.b = shared_lens ? found_b : found_b / Hkv, e.g = shared_lens ? 0 : found_b % Hkv;
     look();
-    while (e.start + e.tiles <= lo) next(), look();
+    {
+        const int skip = static_cast<int>((lo - found_start) / e.tiles);      // entries of the unit ahead of the CTA's first
+        e.g += skip / a.chunks, e.run = skip % a.chunks;
+        e.start = found_start + static_cast<i64>(skip) * e.tiles;
+    }
 
     // ---- the warp's ring
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * L::STAGE;
@@ -782,7 +780,7 @@ int launch_d(DecodeArgs& a, bool e4m3, int nt, const DeviceInfo& di, cudaStream_
 }
 
 int check_heads(long long B, int Hq, int Hkv, int D) {
-    if (B < 0 || B > INT_MAX / 2 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return CAKE_ERR_SHAPE;
+    if (B < 0 || Hkv < 1 || B > INT_MAX / 2 / Hkv || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return CAKE_ERR_SHAPE;
     if (D != 64 && D != 96 && D != 128 && D != 256) return CAKE_ERR_UNSUPPORTED;
     return CAKE_OK;
 }
