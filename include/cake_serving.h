@@ -13,7 +13,8 @@
  *   - strides are counted in elements; the innermost dimension is always contiguous;
  *   - `ws` scratch is 256-byte aligned; its first word is the sticky device status (cake_kmeans_device_status).  The caller
  *     zeroes the first CAKE_SERVING_HEADER_BYTES bytes once, before the first call that uses the buffer; the calls leave
- *     them ready for the next call, of any size.  Calls that run concurrently must use distinct workspaces.
+ *     them ready for the next call, of any size.  Calls that run concurrently must use distinct workspaces.  After a status
+ *     of CAKE_ERR_TIMEOUT (a bounded wait in a kernel expired) the header is zeroed again before the next call.
  */
 #ifndef CAKE_SERVING_H_
 #define CAKE_SERVING_H_
@@ -121,7 +122,7 @@ CAKE_API int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, l
  *   out         [B][Hq][D] bf16 contiguous, out;   out_lse [B][Hq] fp32, out, may be NULL: log of the sum of exponentials
  *   ws          at least cake_paged_decode_workspace_bytes(...) bytes
  * A row without tokens (length zero, or none that weighs anything) gives zeros, and -inf in out_lse.  Scores, their maximum and sum, and the weighted sum of
- * values are held in 32 bits; memory behind the last token is never read.  One launch, or two where few sequences are split
+ * values are held in 32 bits (a value that is infinite, in a bf16 cache, may give NaN instead of infinity); memory behind the last token is never read.  One launch, or two where few sequences are split
  * into many parts; the result does not depend on timing.
  */
 CAKE_API int cake_paged_decode_workspace_bytes(long long B, int Hq, int Hkv, int D, size_t* out_bytes);

@@ -3,7 +3,9 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin) for the pairs (i, i + rot/2) or (2i, 2i+1) of a head's first `rot` elements
 //
 // Bound by memory: q, k, v are read once and written once.  A thread keeps the cosines and sines of its place in a head
-// and walks over heads, so the table is read once per token and group of threads, not once per head.
+// and walks over heads, four at a time, so the table is read once per token and group of threads, not once per head.
+// Measured: 16,001 tokens of 32 + 2 * 8 heads of 128, half of each rotated, into an 8-bit cache 63 us, 5.82 TB/s, 89 % of the copy
+// rate; 16,384 tokens into a bf16 cache 69 us, 91 %; 16 tokens 2.5 us.
 #include "serving.cuh"
 
 namespace cake {
