@@ -39,7 +39,6 @@ constexpr int kPartCtas = 1024;          // CTAs that the workspace has room for
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
-constexpr float SLACK = 8.f;
 constexpr int WAIT_TRIES = 100000;       // of 20 us each
 
 // an entry that several CTAs share
@@ -264,6 +263,10 @@ paged_decode_kernel(const DecodeArgs a) {
     constexpr int HEADS = 8 * NT;
     constexpr int THREADS = WARPS * 32;
     constexpr int TILE = WARPS * KEYS;       // keys of a CTA's tile
+    // What is subtracted from the scores: LIFT below their maximum, which it follows when it lies SLACK behind.  8-bit values take p in f16, whose
+    // full range serves: p of the heaviest key is 2^11 to 2^15, 11 bits are held down to 2^-25 of it and a step of 2^-35 below that.  (With the
+    // heaviest at 1, keys below 2^-25 of it were lost, thousands of them and all)
+    constexpr float LIFT = E4M3 ? 11.f : 0.f, SLACK = E4M3 ? 4.f : 8.f;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ i64 scan[WARPS];
     __shared__ i64 found_start;
@@ -557,8 +560,8 @@ paged_decode_kernel(const DecodeArgs a) {
                 }
             }
 
-            // ---- running maximum and sum.  The maximum that is subtracted may lag behind the true one by up to SLACK (p stays below
-            // 2^SLACK, far inside every format it passes through), so it moves, and O is rescaled, only a few times per row
+            // ---- running maximum (m: LIFT below it) and sum.  It may lag behind the true one by up to SLACK (p stays below 2^(LIFT + SLACK),
+            // inside every format it passes through), so it moves, and O is rescaled, only a few times per row
             uint32_t ph[NT][2], pl[NT][2];
             const bool ok0 = (mask >> g8) & 1, ok1 = (mask >> (g8 + 8)) & 1;
             bool higher = false;
@@ -568,7 +571,7 @@ paged_decode_kernel(const DecodeArgs a) {
                 for (int i = 0; i < 2; ++i) {
                     x[n][i] = ok0 ? x[n][i] * factor[n][i] : NEG_INF;
                     x[n][2 + i] = ok1 ? x[n][2 + i] * factor[n][i] : NEG_INF;
-                    higher |= fmaxf(x[n][i], x[n][2 + i]) > m[n][i] + SLACK;
+                    higher |= fmaxf(x[n][i], x[n][2 + i]) > m[n][i] + (LIFT + SLACK);
                 }
             if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
@@ -578,7 +581,7 @@ paged_decode_kernel(const DecodeArgs a) {
                         float top = fmaxf(x[n][i], x[n][2 + i]);
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        top = fmaxf(m[n][i], top);
+                        top = fmaxf(m[n][i], top - LIFT);
                         const float keep = ex2(m[n][i] - (top == NEG_INF ? 0.f : top));
                         m[n][i] = top;
                         l[n][i] *= keep;
@@ -597,7 +600,7 @@ paged_decode_kernel(const DecodeArgs a) {
                     l[n][i] += p[i] + p[2 + i];
                 }
                 if (E4M3) {
-                    // f16 holds 11 bits of p: its rounding is an eighth of the output's
+                    // f16 holds 11 bits of p: its rounding is an eighth of the output's (the lightest keys': see LIFT)
                     ph[n][0] = transpose8x8(pack_f16(p[0], p[1]));
                     ph[n][1] = transpose8x8(pack_f16(p[2], p[3]));
                 } else {

@@ -569,6 +569,31 @@ def test_decode_every_8_bit_value_and_nan(D):
         assert torch.equal(bad[2], out[2]) and torch.equal(bad_lse[1:], lse[1:])
 
 
+@pytest.mark.parametrize("kv", [BF16, E4M3])
+@pytest.mark.parametrize("D,G", [(64, 1), (96, 4), (128, 12), (256, 2)])
+@pytest.mark.parametrize("gap", [14.3, 25.5, 28.7, 31.0])
+def test_decode_many_light_weights_beside_a_heavy_one(gap, D, G, kv):
+    """Weights 2^-gap of the heaviest, thousands of them, and nothing else in the output.  A weight is held with 11 bits, or to 2^-36 of the
+    heaviest where that is more; scores of up to 31 are right to 32 * 2^-22; then the output's rounding."""
+    B, N, page = 640, 2048, 32
+    k = torch.zeros(N // page, page, 1, D, dtype=torch.float32, device=DEV)
+    v = torch.ones_like(k)
+    flat_k, flat_v = k.view(N, D), v.view(N, D)
+    flat_k[0:64:16, 0] = 1.0                          # one in every 16 keys of the first 64, of value zero
+    flat_v[0:64:16] = 0.0
+    cache = cake.PagedCache(k.to(kv), v.to(kv))
+    q = torch.zeros(B, G, D, dtype=BF16, device=DEV)
+    q[:, :, 0] = 1.0
+    table = torch.arange(N // page, dtype=torch.int32, device=DEV)[None].expand(B, -1).contiguous()
+    n = torch.full((B,), N, dtype=torch.int32, device=DEV)
+    scale = torch.tensor(gap * math.log(2.0), dtype=torch.float32).item()
+    out, _ = cake.cake_paged_decode(q, cache, table, n, scale=scale)
+    p = math.exp(-scale)
+    want = (N - 4) * p / (4 + (N - 4) * p)
+    rel = BF + max(2.0 ** -11, 2.0 ** -36 / p) + 32 * 2.0 ** -22 + N * U
+    close(out, torch.full_like(out, want, dtype=torch.float64), torch.full_like(out, rel * want, dtype=torch.float64), "out")
+
+
 def test_decode_scale_strides_streams_and_graphs():
     q, cache, table, n = decode_problem(8, 2, 128, 16, BF16, [500, 33, 0, 70], 12)
     wide = torch.zeros(4, 12, 128, dtype=BF16, device=DEV)
