@@ -3,6 +3,8 @@
 Each function has the name of the C entry point it calls; PyTorch supplies device memory and the stream.  The checks and the call
 are native (csrc/ext/serving_ext.cpp): a program makes these calls for kernels of a few microseconds.  As in `binding`, there is
 no fallback: a missing library, a wrong type or a refused shape raises.
+
+With `stream`, the outputs and the scratch that a call allocates belong to that stream, as if it were the current one.
 """
 from __future__ import annotations
 
@@ -75,7 +77,17 @@ def _native():
     return _ext
 
 
-def _workspace(n, device):
+def _empty(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(n, device, stream=None):
+    if stream is not None:               # zeroed ahead of the call, and not handed out again before its kernels are done
+        with torch.cuda.stream(stream):
+            return _workspace(n, device)
     ws = torch.empty(n, dtype=torch.uint8, device=device)
     ws[:CAKE_SERVING_HEADER_BYTES].zero_()
     return ws
@@ -90,13 +102,13 @@ def cake_rmsnorm_quant(x, weight=None, residual=None, eps=1e-6, group=128, out_r
     None.  out_residual may be `residual` or `x` themselves.
     """
     if want_q and out_q is None:
-        out_q = torch.empty(x.shape, dtype=_E4M3, device=x.device)
+        out_q = _empty(x.shape, _E4M3, x.device, stream)
     if out_q is not None and out_scale is None:
-        out_scale = torch.empty(x.shape[0], 1 if group == 0 else -(-x.shape[1] // 128), dtype=torch.float32, device=x.device)
+        out_scale = _empty((x.shape[0], 1 if group == 0 else -(-x.shape[1] // 128)), torch.float32, x.device, stream)
     if out_residual is None and (residual is not None if want_residual is None else want_residual):
-        out_residual = torch.empty(x.shape, dtype=_BF16, device=x.device)
+        out_residual = _empty(x.shape, _BF16, x.device, stream)
     if want_y and out_y is None:
-        out_y = torch.empty(x.shape, dtype=_BF16, device=x.device)
+        out_y = _empty(x.shape, _BF16, x.device, stream)
     rc = (_ext or _native()).rmsnorm_quant(x, weight, residual, eps, group, out_residual, out_y, out_q, out_scale,
                                            None if stream is None else stream.cuda_stream, flags)
     if rc:
@@ -122,9 +134,9 @@ def cake_gemm_fp8(X, x_scale, W, w_scale, out=None, out_dtype=_BF16, ws=None, st
     if out is None:
         if out_dtype not in (_BF16, torch.float32):
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-        out = torch.empty(X.shape[0], W.shape[0], dtype=out_dtype, device=X.device)
+        out = _empty((X.shape[0], W.shape[0]), out_dtype, X.device, stream)
     if ws is None:
-        ws = alloc_gemm_workspace(X.shape[0], W.shape[0], X.shape[1], X.device)
+        ws = _workspace(cake_gemm_fp8_workspace_bytes(X.shape[0], W.shape[0], X.shape[1]), X.device, stream)
     rc = (_ext or _native()).gemm_fp8(X, x_scale, W, w_scale, out, ws, None if stream is None else stream.cuda_stream)
     if rc:
         raise CakeError(rc, "cake_gemm_fp8")
@@ -174,9 +186,9 @@ def cake_kv_append(cache, k, v, slots, positions=None, cos_sin=None, q=None, out
     if q is None:
         out_q = None
     elif out_q is None:
-        out_q = torch.empty(q.shape, dtype=_BF16, device=q.device)
+        out_q = _empty(q.shape, _BF16, q.device, stream)
     if ws is None:
-        ws = alloc_append_workspace(k.device)
+        ws = _workspace(CAKE_SERVING_HEADER_BYTES, k.device, stream)
     rc = (_ext or _native()).kv_append(cache._address, cache.k, k, v, slots, positions, cos_sin, q, out_q, interleaved, ws,
                                        None if stream is None else stream.cuda_stream)
     if rc:
@@ -204,11 +216,11 @@ def cake_paged_decode(q, cache, page_table, seq_lens, scale=None, window=0, out=
     scale defaults to 1/sqrt(D); window > 0 attends to the last `window` tokens.
     """
     if out is None:
-        out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+        out = _empty(q.shape, _BF16, q.device, stream)
     if want_lse and out_lse is None:
-        out_lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        out_lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     if ws is None:
-        ws = alloc_decode_workspace(q.shape[0], q.shape[1], cache.Hkv, cache.D, q.device)
+        ws = _workspace(cake_paged_decode_workspace_bytes(q.shape[0], q.shape[1], cache.Hkv, cache.D), q.device, stream)
     rc = (_ext or _native()).paged_decode(q, cache._address, cache.k, page_table, seq_lens, cache.D ** -0.5 if scale is None else scale, window, out, out_lse,
                                           ws, None if stream is None else stream.cuda_stream)
     if rc:

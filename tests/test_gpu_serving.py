@@ -688,3 +688,39 @@ def test_decode_refusals():
     with pytest.raises(cake.CakeError) as e:
         cake.cake_paged_decode(q, cache, table, n, ws=torch.zeros(cake.CAKE_SERVING_HEADER_BYTES, dtype=torch.uint8, device=DEV))
     assert e.value.code == cake.CAKE_ERR_WORKSPACE
+
+
+def test_scratch_and_outputs_of_another_stream():
+    """Calls on a stream that is not the current one: what they allocate is zeroed on theirs and stays theirs until their kernels are done,
+    whatever the current stream does meanwhile with the memory it frees."""
+    g = gen(77)
+    q, cache, table, n = decode_problem(32, 8, 128, 16, BF16, [3000, 17], 4)
+    x, w = normal(g, 70, 1024), normal(g, 1024)
+    X, xs, W, wsc = gemm_inputs(100, 256, 4096, 5)
+    k, v, slots = normal(g, 9, 8, 128), normal(g, 9, 8, 128), torch.arange(9, dtype=torch.int64, device=DEV)
+    qs = normal(g, 9, 32, 128)
+    spare = cake.PagedCache(torch.zeros(4, 16, 8, 128, dtype=BF16, device=DEV), torch.zeros(4, 16, 8, 128, dtype=BF16, device=DEV))
+
+    def run(stream):
+        a = cake.cake_rmsnorm_quant(x, w, stream=stream)
+        b = cake.cake_gemm_fp8(X, xs, W, wsc, stream=stream)
+        c = cake.cake_kv_append(spare, k, v, slots, q=qs, stream=stream)
+        d = cake.cake_paged_decode(q, cache, table, n, want_lse=True, stream=stream)
+        return [a[0].view(torch.uint8), a[1], b, c, d[0], d[1]]
+
+    want = run(None)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    sizes = [cake.cake_paged_decode_workspace_bytes(2, 32, 8, 128), cake.cake_gemm_fp8_workspace_bytes(100, 256, 4096), cake.CAKE_SERVING_HEADER_BYTES]
+    for _ in range(3):
+        dirty = [torch.full((m,), 85, dtype=torch.uint8, device=DEV) for m in sizes]      # what the current stream's allocator hands out next
+        torch.cuda.synchronize()
+        del dirty
+        torch.cuda._sleep(20_000_000)                 # about 10 ms, in which nothing that is queued behind it runs
+        got = run(side)
+        scribble = [torch.full((m,), 85, dtype=torch.uint8, device=DEV) for m in sizes]
+        side.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
+        del scribble
