@@ -70,8 +70,8 @@ CAKE_API int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* 
  * A paged cache of keys and values: page p, token t of the page, head h: k + p*k_page_stride + t*k_token_stride +
  * h*k_head_stride, D contiguous elements there (the order of tokens and heads inside a page is the caller's).  Slot
  * s is token s % page_size of page s / page_size.
- *   type     CAKE_KV_BF16 or CAKE_KV_E4M3 (an element x of head h is held as e4m3(x / scale[h]))
- *   k_scale, v_scale  [Hkv] fp32, device, may be NULL (all ones)
+ *   type     CAKE_KV_BF16 or CAKE_KV_E4M3 (an element x of head h is held as e4m3(x / scale[h]), the quotient taken as x * (1 / scale[h]))
+ *   k_scale, v_scale  [Hkv] fp32, device, normal numbers, may be NULL (all ones)
  * Base pointers are 16-byte aligned and every stride is a multiple of 16 bytes (CAKE_ERR_ALIGN).
  * D: 64, 96, 128 or 256 (CAKE_ERR_UNSUPPORTED otherwise).
  */
@@ -121,9 +121,11 @@ CAKE_API int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, l
  *   window      0: all tokens; w > 0: the last w of them
  *   out         [B][Hq][D] bf16 contiguous, out;   out_lse [B][Hq] fp32, out, may be NULL: log of the sum of exponentials
  *   ws          at least cake_paged_decode_workspace_bytes(...) bytes
- * A row without tokens (length zero, or none that weighs anything) gives zeros, and -inf in out_lse.  Scores, their maximum and sum, and the weighted sum of
- * values are held in 32 bits (a value that is infinite, in a bf16 cache, may give NaN instead of infinity); memory behind the last token is never read.  One launch, or two where few sequences are split
- * into many parts; the result does not depend on timing.
+ * A row without tokens (length zero, or none that weighs anything) gives zeros, and -inf in out_lse.  Scores, their maximum and
+ * sum, and the weighted sum of values are held in 32 bits (a value that is infinite, in a bf16 cache, may give NaN instead of
+ * infinity); memory behind the last token is never read.  Weights are held with 11 bits or more; with an 8-bit cache, those
+ * below 2^-25 of the row's heaviest to 2^-36 of it, and elements of a query below 2^-14 of its largest to 2^-25 of that.
+ * One launch, or two where few sequences are split into many parts; the result does not depend on timing.
  */
 CAKE_API int cake_paged_decode_workspace_bytes(long long B, int Hq, int Hkv, int D, size_t* out_bytes);
 CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_paged_cache* cache,

@@ -66,7 +66,13 @@ __device__ __forceinline__ void store8(void* base, i64 at, const float (&f)[8], 
     }
 }
 
-// (a, b) -> (a c - b s, b c + a s) for two pairs at a time (packed instructions: issue is half of what bounds the kernel)
+// (a, b) -> (a c - b s, b c + a s): the roundings of turn2, so that a token's bits do not depend on the alignment of its sources
+__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
+    const float t = fmaf(a, c, __fmul_rn(b, -s));
+    b = fmaf(b, c, __fmul_rn(a, s));
+    a = t;
+}
+// the same for two pairs at a time (packed instructions: issue is half of what bounds the kernel)
 __device__ __forceinline__ void turn2(float& a0, float& a1, float& b0, float& b1, float c0, float c1, float s0, float s1) {
     asm("{\n\t.reg .b64 a, b, c, s, t, u, n;\n\t"
         "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tmov.b64 c, {%4, %5};\n\tmov.b64 s, {%6, %7};\n\tmov.b64 n, {%8, %9};\n\t"
@@ -134,11 +140,7 @@ kv_append_kernel(const AppendArgs a) {
                     for (int j = 0; j < 8; j += 2) turn2(x[j], x[j + 1], y[j], y[j + 1], cs[j], cs[j + 1], sn[j], sn[j + 1]);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float r = x[2 * j] * cs[j] - x[2 * j + 1] * sn[j];
-                        x[2 * j + 1] = x[2 * j + 1] * cs[j] + x[2 * j] * sn[j];
-                        x[2 * j] = r;
-                    }
+                    for (int j = 0; j < 4; ++j) turn(x[2 * j], x[2 * j + 1], cs[j], sn[j]);
                 }
             }
             if (is_q) {
@@ -169,8 +171,8 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
     const int D = a.c.D, half = a.rot >> 1;
     const int units = half + (D - a.rot);
     const int hq = a.q ? a.Hq : 0;
-    auto put = [&](void* base, i64 at, float f, float sc) {
-        if (E4M3) static_cast<cake_e4m3*>(base)[at] = static_cast<cake_e4m3>(pack_e4m3(f / sc, 0.f) & 0xff);
+    auto put = [&](void* base, i64 at, float f, float inv) {      // inv: 1 / scale
+        if (E4M3) static_cast<cake_e4m3*>(base)[at] = static_cast<cake_e4m3>(pack_e4m3(f * inv, 0.f) & 0xff);
         else static_cast<cake_bf16*>(base)[at] = to_bf16(f);
     };
     for (int i = threadIdx.x; i < (hq + a.c.Hkv) * units; i += blockDim.x) {
@@ -183,10 +185,8 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
         float x = bf16_f(src[d]), y = 0.f;
         if (turns) {
             const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
-            const float c = row[u], s = row[half + u];
-            const float o = bf16_f(src[e]);
-            y = o * c + x * s;
-            x = x * c - o * s;
+            y = bf16_f(src[e]);
+            turn(x, y, row[u], row[half + u]);
         }
         if (is_q) {
             cake_bf16* dst = a.out_q + (t * a.Hq + h) * static_cast<i64>(D);
@@ -194,16 +194,16 @@ kv_append_scalar_kernel(const AppendArgs a, bool pairs) {
             if (turns) dst[e] = to_bf16(y);
         } else {
             const i64 at = p.page * a.c.k_page_stride + p.off * a.c.k_token_stride + g * a.c.k_head_stride;
-            const float sc = E4M3 && a.c.k_scale ? a.c.k_scale[g] : 1.f;
-            put(a.c.k, at + d, x, sc);
-            if (turns) put(a.c.k, at + e, y, sc);
+            const float inv = E4M3 && a.c.k_scale ? 1.f / a.c.k_scale[g] : 1.f;
+            put(a.c.k, at + d, x, inv);
+            if (turns) put(a.c.k, at + e, y, inv);
         }
     }
     if (!p.kv) return;
     for (int i = threadIdx.x; i < a.c.Hkv * D; i += blockDim.x) {
         const int g = i / D, d = i - g * D;
         const i64 at = p.page * a.c.v_page_stride + p.off * a.c.v_token_stride + g * a.c.v_head_stride + d;
-        put(a.c.v, at, bf16_f(a.v[t * a.v_stride + static_cast<i64>(g) * D + d]), E4M3 && a.c.v_scale ? a.c.v_scale[g] : 1.f);
+        put(a.c.v, at, bf16_f(a.v[t * a.v_stride + static_cast<i64>(g) * D + d]), E4M3 && a.c.v_scale ? 1.f / a.c.v_scale[g] : 1.f);
     }
 }
 

@@ -462,7 +462,7 @@ paged_decode_kernel(const DecodeArgs a) {
                     w[c][4 * j] = u.x, w[c][4 * j + 1] = u.y, w[c][4 * j + 2] = u.z, w[c][4 * j + 3] = u.w;
                 }
             // 8-bit keys are widened to f16 (exact), so the query is too: divided by a power of two that leaves its largest
-            // element in [1, 2), which keeps 11 bits where bf16 has 8; what underflows is below 2^-24 of the largest
+            // element in [1, 2), which keeps 11 bits where bf16 has 8; elements below 2^-14 of the largest are held to 2^-25 of it
             float unit = 1.f;
             if (E4M3) {
                 float most = 0.f;

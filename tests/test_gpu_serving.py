@@ -353,6 +353,33 @@ def test_append_unaligned_sources(pairs):
     assert torch.equal(outs[0], outs[1]) and torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
 
 
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("kv", [BF16, E4M3])
+def test_append_bits_do_not_depend_on_alignment(kv, pairs):
+    T, Hq, Hkv, D, rot = 300, 8, 4, 128, 64
+    g = gen(31)
+    q, k, v = normal(g, T, Hq, D), normal(g, T, Hkv, D), normal(g, T, Hkv, D)
+    ang = torch.empty(500, rot // 2, device=DEV).uniform_(0, 6.28, generator=g)
+    table = torch.cat([ang.cos(), ang.sin()], 1).contiguous()
+    pos = torch.randint(0, 500, (T,), generator=g, device=DEV, dtype=torch.int32)
+    slots = torch.randperm(20 * 16, generator=g, device=DEV)[:T]
+    ks, vs = torch.empty(2, Hkv, device=DEV).uniform_(0.001, 0.02, generator=g)
+
+    def odd(t):                                       # the same elements, two bytes off
+        room = torch.empty(t.numel() + 1, dtype=BF16, device=DEV)
+        room[1:] = t.flatten()
+        return room[1:].view(t.shape)
+
+    results = []
+    for change in (lambda t: t, odd):
+        kc, vc = (torch.zeros(20, 16, Hkv, D, dtype=kv, device=DEV) for _ in range(2))
+        cache = cake.PagedCache(kc, vc, ks, vs) if kv == E4M3 else cake.PagedCache(kc, vc)
+        out = cake.cake_kv_append(cache, change(k), change(v), slots, pos, table, change(q), interleaved=pairs)
+        results.append((out, kc.view(torch.uint8), vc.view(torch.uint8)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_append_in_place_queries_and_refusals():
     g = gen(6)
     kc = torch.zeros(4, 8, 2, 128, dtype=BF16, device=DEV)
