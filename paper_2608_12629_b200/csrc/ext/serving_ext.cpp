@@ -256,7 +256,7 @@ PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t out_shape[3] = {B, Hq, D};
         void* out_at = call.dense(out, at::kBFloat16, {out_shape, 3}, "out");
         void* lse_at = call.dense(lse, at::kFloat, {out_shape, 2}, "out_lse");
-        return cake_paged_decode(static_cast<const cake_bf16*>(call.at(q, "q")), q.stride(0), q.stride(1), cache,
+        return cake_paged_decode(static_cast<const cake_bf16*>(call.at(q, "q")), B > 1 ? q.stride(0) : 0, Hq > 1 ? q.stride(1) : 0, cache,
                                  static_cast<const int*>(call.at(table, "page_table")), table.stride(0), td == 3 ? table.stride(1) : 0,
                                  static_cast<int>(table.size(-1)), static_cast<const int*>(call.at(lens, "seq_lens")), lens.stride(0),
                                  ld == 2 ? lens.stride(1) : 0, B, static_cast<int>(Hq), real(a[5]), small(a[6]), static_cast<cake_bf16*>(out_at),

@@ -165,9 +165,11 @@ class PagedCache:
                 raise ValueError(f"{name} is on {t.device}, not on {k.device}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_pages, self.page_size, self.Hkv, self.D = pages, page, Hkv, D
+        # (the stride of a dimension of one element says nothing, and may be any number)
+        strides = [t.stride(i) if t.size(i) > 1 else 0 for t in (k, v) for i in range(3)]
         self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-                                    None if v_scale is None else v_scale.data_ptr(), pages, k.stride(0), k.stride(1), k.stride(2), v.stride(0),
-                                    v.stride(1), v.stride(2), page, Hkv, D, CAKE_KV_E4M3 if k.dtype == _E4M3 else CAKE_KV_BF16)
+                                    None if v_scale is None else v_scale.data_ptr(), pages, *strides, page, Hkv, D,
+                                    CAKE_KV_E4M3 if k.dtype == _E4M3 else CAKE_KV_BF16)
         self._address = ctypes.addressof(self._struct)
 
     @property

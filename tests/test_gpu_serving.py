@@ -698,6 +698,22 @@ def test_offsets_beyond_32_bits():
     check_decode(q, cache, table, n, out, lse)
 
 
+def test_strides_of_single_elements_say_nothing():
+    """One page, one head: their strides may be any number, one that is no multiple of 16 bytes too."""
+    g = gen(8)
+    room_k, room_v = normal(g, 16 * 64 + 9), normal(g, 16 * 64 + 9)
+    k, v = (torch.as_strided(t, (1, 16, 1, 64), (1033, 64, 13, 1)) for t in (room_k, room_v))
+    plain = cake.PagedCache(k.contiguous(), v.contiguous())
+    cache = cake.PagedCache(k, v)
+    q = normal(g, 1, 1, 64)
+    table, n = torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.tensor([11], dtype=torch.int32, device=DEV)
+    out, lse = cake.cake_paged_decode(torch.as_strided(q, (1, 1, 64), (77, 3, 1)), cache, table, n, want_lse=True)
+    check_decode(q, plain, table, n, out, lse)
+    new_k, new_v = normal(g, 1, 1, 64), normal(g, 1, 1, 64)
+    cake.cake_kv_append(cache, new_k, new_v, torch.tensor([15], dtype=torch.int64, device=DEV))
+    assert torch.equal(k[0, 15], new_k[0]) and torch.equal(v[0, 15], new_v[0])
+
+
 def test_decode_refusals():
     q, cache, table, n = decode_problem(4, 2, 64, 16, BF16, [20], 5)
     assert cake.cake_paged_decode(q[:0], cache, table[:0], n[:0])[0].shape == (0, 4, 64)
