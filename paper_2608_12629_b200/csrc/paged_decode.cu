@@ -43,8 +43,8 @@ constexpr int WAIT_TRIES = 100000;       // of 20 us each
 
 // an entry that several CTAs share
 struct Split {
-    int b, g, run, c0, c1, slot0;    // the CTAs, and which of the first one's two parts is the entry's (0 of all others)
-    int pad[2];
+    int b, g, run, c0, c1;           // the CTAs
+    int pad[3];
 };
 
 struct DecodeArgs {
@@ -178,7 +178,7 @@ struct Joined {
         top = up;
     }
     template <int D, int HEADS>
-    __device__ __forceinline__ void add(const DecodeArgs& a, int c, int c1, int step, int slot0, int c0, int h, int d) {
+    __device__ __forceinline__ void add(const DecodeArgs& a, int c, int c1, int step, int c0, int h, int d) {
         constexpr int BATCH = 8;             // parts in flight
         constexpr i64 PART = HEADS * (D + 4);
         for (; c <= c1; c += BATCH * step) {
@@ -189,7 +189,7 @@ struct Joined {
                 u[k] = make_float4(0.f, 0.f, 0.f, 0.f), ml[k] = make_float2(NEG_INF, 0.f);
                 const int ck = c + k * step;
                 if (ck <= c1) {
-                    const float* p = a.parts + (2 * ck + (ck == c0 ? slot0 : 0)) * PART;
+                    const float* p = a.parts + (2 * ck + (ck == c0 ? 1 : 0)) * PART;      // an entry's beginning is the second of its CTA's parts
                     u[k] = __ldcg(reinterpret_cast<const float4*>(p + h * D + d));
                     ml[k] = __ldcg(reinterpret_cast<const float2*>(p + HEADS * D + 2 * h));
                 }
@@ -225,7 +225,7 @@ paged_join_kernel(const DecodeArgs a, bool e4m3) {
         const int h = u % HEADS;
         if (h >= min(HEADS, a.G - e.run * HEADS)) continue;
         Joined j;
-        j.add<D, HEADS>(a, e.c0 + group, e.c1, 4, e.slot0, e.c0, h, d);
+        j.add<D, HEADS>(a, e.c0 + group, e.c1, 4, e.c0, h, d);
         accs[group][d / 4] = j.acc;
         if (d == 0) mls[group] = make_float2(j.top, j.sum);
         __syncthreads();
@@ -368,7 +368,6 @@ paged_decode_kernel(const DecodeArgs a) {
     const uint32_t v_read = ring + L::K_BYTES + ((lane & 7) + ((lane >> 4) << 3)) * L::V_PITCH + ((lane >> 3) & 1) * 16;
     const uint32_t k_read = ring + g8 * L::K_PITCH + t4 * L::VK;
 
-    bool first_segment = true;
     for (i64 at = lo; at < hi;) {
         const int tile0 = static_cast<int>(at - e.start);
         const int n_tiles = static_cast<int>(min(hi - at, static_cast<i64>(e.tiles - tile0)));
@@ -674,7 +673,7 @@ paged_decode_kernel(const DecodeArgs a) {
         __syncthreads();
         const bool whole = tile0 == 0 && n_tiles == e.tiles;
         constexpr int PART = HEADS * (D + 4);            // floats of a part: O of the run's heads, then m and l (and padding)
-        float* const part = a.parts + (2 * cta + (first_segment ? 0 : 1)) * static_cast<i64>(PART);
+        float* const part = a.parts + (2 * cta + (tile0 == 0 ? 1 : 0)) * static_cast<i64>(PART);
         const float vs = E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
         auto finish = [&](int h, int d, const float4& acc, float top, float sum) { write_out<D>(a, out0 + h, d, acc, top, sum, vs); };
@@ -704,10 +703,8 @@ paged_decode_kernel(const DecodeArgs a) {
             // for which the first of them notes the entry
             const i64 s0 = e.start, s1 = e.start + e.tiles - 1;
             const int c0 = static_cast<int>(((s0 + 1) * n_ctas - 1) / total), c1 = static_cast<int>(((s1 + 1) * n_ctas - 1) / total);
-            // the entry is the first of a CTA's segments unless that CTA (the first of them) began before it
-            const int slot0 = c0 * total / n_ctas >= s0 ? 0 : 1;
             if (a.defer) {
-                if (tid == 0 && cta == c0) a.splits[atomicAdd(a.n_splits, 1)] = Split{e.b, e.g, e.run, c0, c1, slot0, {0, 0}};
+                if (tid == 0 && cta == c0) a.splits[atomicAdd(a.n_splits, 1)] = Split{e.b, e.g, e.run, c0, c1, {0, 0, 0}};
             } else {
                 __syncthreads();
                 if (tid == 0) {
@@ -722,7 +719,7 @@ paged_decode_kernel(const DecodeArgs a) {
                     for (int i = tid; i < heads * (D / 4); i += THREADS) {
                         const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
                         Joined j;
-                        j.add<D, HEADS>(a, c0, c1, 1, slot0, c0, h, d);
+                        j.add<D, HEADS>(a, c0, c1, 1, c0, h, d);
                         finish(h, d, j.acc, j.top, j.sum);
                     }
                 }
@@ -730,7 +727,6 @@ paged_decode_kernel(const DecodeArgs a) {
         }
         __syncthreads();             // the ring's memory, wm and wl are free again
         ptx::fence_proxy_async_smem();       // plain accesses to the ring's memory come before the next copies into it
-        first_segment = false;
         at += n_tiles;
         if (at < hi) next(), look();
     }
