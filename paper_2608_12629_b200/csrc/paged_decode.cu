@@ -21,7 +21,7 @@
 //
 // Measured (32 query, 8 key-value heads of 128, bf16): 64 sequences of 512 to 8,192 tokens 187 us, 6.18 TB/s, 94 % of the copy rate, bound by
 // memory.  Four of up to 131,072 tokens, 64 query heads, 8-bit: 140 us, 4.96 TB/s, 76 %: 16-byte copies, conversions and the softmax of
-// twice the keys per byte keep the schedulers half busy and a warp's chain of steps is what is left.  One of 777 tokens: 7.8 us, all latency (lengths, table,
+// twice the keys per byte keep the schedulers half busy and a warp's chain of steps is what is left.  One of 777 tokens: 7.7 us, all latency (lengths, table,
 // keys, join).  First form (lane-wise 16-byte copies everywhere, maximum exact at every step): 301, 253 and 30 us.
 #include "ptx.cuh"
 #include "serving.cuh"
