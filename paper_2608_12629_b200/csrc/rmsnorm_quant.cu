@@ -211,6 +211,15 @@ rmsnorm_quant_kernel(const NormArgs a, int tpr) {
         if (a.norm) {
             ss = row_reduce<false>(ss, part[0], warp, sub * warps, warps);
             rs = rsqrtf(ss / static_cast<float>(a.H) + a.eps);
+            // rs / scale stays finite up to here (the smallest scale is 2^-100).  Beyond, for rows of next to nothing under an eps as small, the
+            // elements take rs themselves; else the zeros of such a row would become 0 * infinity
+            if (rs > 0x1p27f && rs < INFINITY) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int j = 0; j < E; ++j) s[v][j] *= rs;
+                rs = 1.f;
+            }
         }
         float most = 0.f;
         auto write_q = [&](int v, float f) {           // f: rs / scale

@@ -119,6 +119,21 @@ def test_norm_zero_rows_and_values_that_are_not_finite():
     assert torch.isfinite(q.float()).all() and (scale == 2.0 ** -100).all()
 
 
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("H,eps", [(256, 0.0), (256, 1e-30), (258, 1e-22), (257, 1e-30), (9000, 1e-30)])
+def test_norm_rows_of_next_to_nothing_under_a_tiny_eps(H, eps, group):
+    """1 / rms of 2^30 and more: the zeros among such a row's elements, and a row of zeros, stay zeros."""
+    x = normal(gen(H), 5, H)
+    x = (x.float() * torch.tensor([1.0, 2.0 ** -27, 2.0 ** -32, 2.0 ** -40, 0.0], device=DEV)[:, None]).to(BF16)
+    x[:, :128] = 0.0                                 # a group of zeros
+    if eps == 0.0:
+        x = x[:4].contiguous()                       # (a row of zeros has no norm)
+    w = normal(gen(1), H, std=0.3) + 1
+    q, scale, y, _ = cake.cake_rmsnorm_quant(x, w, eps=eps, group=group, want_y=True)
+    check_norm(x, None, w, group, q, scale, y, None, eps=eps)
+    assert (q[:, :128].float() == 0).all()
+
+
 def test_norm_no_rows_and_refusals():
     x = torch.zeros(0, 64, dtype=BF16, device=DEV)
     q, scale, _, _ = cake.cake_rmsnorm_quant(x)
