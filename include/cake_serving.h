@@ -125,7 +125,9 @@ CAKE_API int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, l
  * sum, and the weighted sum of values are held in 32 bits (a value that is infinite, in a bf16 cache, may give NaN instead of
  * infinity); memory behind the last token is never read.  Weights are held with 11 bits or more; with an 8-bit cache, those
  * below 2^-25 of the row's heaviest to 2^-36 of it, and elements of a query below 2^-14 of its largest to 2^-25 of that.
- * One launch, or two where few sequences are split into many parts; the result does not depend on timing.
+ * One launch; two where the query heads of a key-value head have more than 512 elements in all (256 with bf16 heads of 256) and
+ * the page table's width, cut by the window, leaves room for rows in many parts: a max_pages no larger than the longest row
+ * needs saves the second.  The result depends on the inputs and their sizes, not on timing.
  */
 CAKE_API int cake_paged_decode_workspace_bytes(long long B, int Hq, int Hkv, int D, size_t* out_bytes);
 CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_paged_cache* cache,

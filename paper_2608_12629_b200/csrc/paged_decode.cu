@@ -8,7 +8,7 @@
 //
 // Work is the list of 64-key tiles of all (sequence, key-value head) entries, one after the other; CTA c of n takes tiles
 // [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined from parts
-// in the workspace, in the order of the CTAs: by the last of them to arrive, or by a second kernel where that would be many parts for one SM.
+// in the workspace, in the order of the CTAs: by the last of them to arrive, in two levels, or by a second kernel where either would be much for one SM.
 //
 // A warp works on 16 keys at a time, with a ring of its own in shared memory and no barrier between warps.  Long rows are
 // fetched by one instruction of the warp a step: each lane copies one row (bulk copy; lanes 0-15 the keys, 16-31 the values); short
@@ -36,6 +36,8 @@ namespace {
 constexpr int KEYS = 16;                 // keys of a warp's step
 constexpr int MOST_WARPS = 4;
 constexpr int kPartCtas = 1024;          // CTAs that the workspace has room for parts of (two each)
+static_assert(3 * kPartCtas <= kMaxCtas, "arrival counters: of entries, of groups, of entries' first groups");
+constexpr int PART_BATCH = 8;            // parts that a join has in flight
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
@@ -47,21 +49,28 @@ struct Split {
     int pad[3];
 };
 
+// where finished rows go
+struct Rows {
+    cake_bf16* out;
+    float* lse;
+    bool wide;                       // 8-byte stores
+};
+
 struct DecodeArgs {
     cake_paged_cache c;
     const cake_bf16* q;
     const int* table;
     const int* lens;
-    cake_bf16* out;
-    float* lse;
+    Rows rows;
     int* status;
     int* counters;
     float* parts;
     struct Split* splits;
     int* n_splits;                   // entries in `splits`; [1]: join blocks that are done
     bool defer;                      // entries that several CTAs share are joined by a second kernel
+    int few;                         // else: parts that the last CTA joins by itself
     i64 q_stride, q_head_stride, table_stride, table_head_stride, lens_stride, lens_head_stride;
-    bool q_wide, out_wide;           // 16-byte loads of q, 8-byte stores of out
+    bool q_wide;                     // 16-byte loads
     int B, Hq, G, chunks, max_pages, window;   // chunks: runs of at most 8 * NT query heads of a key-value head
     float scale;
 };
@@ -149,16 +158,16 @@ __device__ __forceinline__ int tiles_of(int count) { return count > 0 ? (count -
 
 // four values of a finished row: (their sum, the row's maximum and sum of exponentials)
 template <int D>
-__device__ __forceinline__ void write_out(const DecodeArgs& a, i64 row, int d, const float4& acc, float top, float sum, float vs) {
+__device__ __forceinline__ void write_out(const Rows& r, i64 row, int d, const float4& acc, float top, float sum, float vs) {
     const float f = sum == 0.f ? 0.f : vs / sum;                    // no token weighs anything: zeros
     const uint2 w = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
-    cake_bf16* dst = a.out + row * D + d;
-    if (a.out_wide) {
+    cake_bf16* dst = r.out + row * D + d;
+    if (r.wide) {
         *reinterpret_cast<uint2*>(dst) = w;
     } else {
         dst[0] = w.x & 0xffff, dst[1] = w.x >> 16, dst[2] = w.y & 0xffff, dst[3] = w.y >> 16;
     }
-    if (a.lse && d == 0) a.lse[row] = (top + log2f(sum)) * LN2;
+    if (r.lse && d == 0) r.lse[row] = (top + log2f(sum)) * LN2;
 }
 
 // The work list: entries in the order (sequence, key-value head, run of query heads), each of tiles_of(its tokens) tiles.
@@ -177,9 +186,10 @@ struct Joined {
         sum *= f, acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
         top = up;
     }
+    // ml_at: where a part's m and l are
     template <int D, int HEADS>
-    __device__ __forceinline__ void add(const DecodeArgs& a, int c, int c1, int step, int c0, int h, int d) {
-        constexpr int BATCH = 8;             // parts in flight
+    __device__ __forceinline__ void add(const float* parts, int c, int c1, int step, int c0, int h, int d, int ml_at = HEADS * D) {
+        constexpr int BATCH = PART_BATCH;
         constexpr i64 PART = HEADS * (D + 4);
         for (; c <= c1; c += BATCH * step) {
             float4 u[BATCH];
@@ -189,9 +199,9 @@ struct Joined {
                 u[k] = make_float4(0.f, 0.f, 0.f, 0.f), ml[k] = make_float2(NEG_INF, 0.f);
                 const int ck = c + k * step;
                 if (ck <= c1) {
-                    const float* p = a.parts + (2 * ck + (ck == c0 ? 1 : 0)) * PART;      // an entry's beginning is the second of its CTA's parts
+                    const float* p = parts + (2 * ck + (ck == c0 ? 1 : 0)) * PART;      // an entry's beginning is the second of its CTA's parts
                     u[k] = __ldcg(reinterpret_cast<const float4*>(p + h * D + d));
-                    ml[k] = __ldcg(reinterpret_cast<const float2*>(p + HEADS * D + 2 * h));
+                    ml[k] = __ldcg(reinterpret_cast<const float2*>(p + ml_at + 2 * h));
                 }
             }
             float up = top;
@@ -210,9 +220,51 @@ struct Joined {
     }
 };
 
+// true for the last of `others` + 1 CTAs to arrive: releases what the CTA wrote (ordered before thread 0 by the barrier) and acquires what
+// those ahead of it did.  The counter is zero again then, ready for the next call
+__device__ __forceinline__ bool arrive(int* counter, int others, int* flag) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int before_me;
+        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before_me) : "l"(counter) : "memory");
+        *flag = before_me == others;
+        if (*flag) *counter = 0;
+    }
+    __syncthreads();
+    return *flag;
+}
+
+// An entry of many parts without a second kernel: groups of neighbouring parts are joined by the last CTA of each group, the groups' sums by the
+// last group's.  One row of 131,072 tokens beside 255 of 100, 16 heads of 256: 98 us, and 370 by a single CTA; 8 heads of 128 beside 511: 28 and 61.
+// (Out of line, all arguments by value: inside the kernel it made rows of 64 bytes 7 % slower)
+template <int D, int HEADS>
+__device__ __noinline__ void join_in_groups(Rows rows, float* parts, int* counters, int cta, int c0, int c1, int heads, i64 out0, float vs, int* flag) {
+    constexpr int ML_AT = HEADS * D + 2 * HEADS;         // of a group's sum: beside the first part's m and l, which other threads still read
+    int step = 1;
+    while (step * step <= c1 - c0) ++step;
+    const int first = c0 + (cta - c0) / step * step, last = min(first + step - 1, c1);
+    // (a CTA may begin the last group of one entry and the first of the next)
+    if (!arrive(counters + (first == c0 ? 2 : 1) * kPartCtas + first, last - first, flag)) return;
+    float* const sum = parts + (2 * first + (first == c0 ? 1 : 0)) * static_cast<i64>(HEADS * (D + 4));
+    for (int i = threadIdx.x; i < heads * (D / 4); i += blockDim.x) {
+        const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
+        Joined j;
+        j.add<D, HEADS>(parts, first, last, 1, c0, h, d);
+        __stcg(reinterpret_cast<float4*>(sum + h * D + d), j.acc);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(sum + ML_AT + 2 * h), make_float2(j.top, j.sum));
+    }
+    if (!arrive(counters + c0, (c1 - c0) / step, flag)) return;
+    for (int i = threadIdx.x; i < heads * (D / 4); i += blockDim.x) {
+        const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
+        Joined j;
+        j.add<D, HEADS>(parts, c0, c1, step, c0, h, d, ML_AT);
+        write_out<D>(rows, out0 + h, d, j.acc, j.top, j.sum, vs);
+    }
+}
+
 // One row (an entry's query head) to a block and step: D / 4 threads across the row, four such groups share its parts.
 template <int D, int HEADS>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(D, 2)
 paged_join_kernel(const DecodeArgs a, bool e4m3) {
     ptx::grid_dep_launch();
     ptx::grid_dep_wait();
@@ -220,12 +272,13 @@ paged_join_kernel(const DecodeArgs a, bool e4m3) {
     __shared__ float2 mls[4];
     const int group = threadIdx.x / (D / 4), d = 4 * (threadIdx.x % (D / 4));
     const int rows = *reinterpret_cast<volatile int*>(a.n_splits) * HEADS;
+    if (rows == 0) return;           // (for all blocks alike: the list is emptied when all of them are done)
     for (int u = blockIdx.x; u < rows; u += gridDim.x) {
         const Split e = a.splits[u / HEADS];
         const int h = u % HEADS;
         if (h >= min(HEADS, a.G - e.run * HEADS)) continue;
         Joined j;
-        j.add<D, HEADS>(a, e.c0 + group, e.c1, 4, e.c0, h, d);
+        j.add<D, HEADS>(a.parts, e.c0 + group, e.c1, 4, e.c0, h, d);
         accs[group][d / 4] = j.acc;
         if (d == 0) mls[group] = make_float2(j.top, j.sum);
         __syncthreads();
@@ -244,7 +297,7 @@ paged_join_kernel(const DecodeArgs a, bool e4m3) {
                 acc.x = fmaf(v.x, f, acc.x), acc.y = fmaf(v.y, f, acc.y), acc.z = fmaf(v.z, f, acc.z), acc.w = fmaf(v.w, f, acc.w);
             }
             const float vs = e4m3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
-            write_out<D>(a, static_cast<i64>(e.b) * a.Hq + e.g * a.G + e.run * HEADS + h, d, acc, up, sum, vs);
+            write_out<D>(a.rows, static_cast<i64>(e.b) * a.Hq + e.g * a.G + e.run * HEADS + h, d, acc, up, sum, vs);
         }
         __syncthreads();
     }
@@ -281,7 +334,6 @@ paged_decode_kernel(const DecodeArgs a) {
         for (int s = 0; s < STAGES; ++s) ptx::mbar_init(ptx::smem_u32(&bars[warp][s]), 1);
         ptx::fence_mbar_init();
     }
-
 
     ptx::grid_dep_wait();
     // ---- the number of tiles of all entries, and the one that holds this CTA's first tile
@@ -676,7 +728,7 @@ paged_decode_kernel(const DecodeArgs a) {
         float* const part = a.parts + (2 * cta + (tile0 == 0 ? 1 : 0)) * static_cast<i64>(PART);
         const float vs = E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
         const i64 out0 = static_cast<i64>(e.b) * a.Hq + h0;
-        auto finish = [&](int h, int d, const float4& acc, float top, float sum) { write_out<D>(a, out0 + h, d, acc, top, sum, vs); };
+        auto finish = [&](int h, int d, const float4& acc, float top, float sum) { write_out<D>(a.rows, out0 + h, d, acc, top, sum, vs); };
         for (int i = tid; i < heads * (D / 4); i += THREADS) {
             const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
             float top = NEG_INF;
@@ -699,29 +751,20 @@ paged_decode_kernel(const DecodeArgs a) {
             }
         }
         if (!whole) {
-            // ---- the entry's CTAs are neighbours.  A few parts are joined, in order, by the last of them to arrive; many by a second kernel,
-            // for which the first of them notes the entry
+            // ---- The entry's CTAs are neighbours.  A few parts are joined, in order, by the last of them to arrive; more in two levels; or
+            // all of them by a second kernel, for which the first of them notes the entry
             const i64 s0 = e.start, s1 = e.start + e.tiles - 1;
             const int c0 = static_cast<int>(((s0 + 1) * n_ctas - 1) / total), c1 = static_cast<int>(((s1 + 1) * n_ctas - 1) / total);
             if (a.defer) {
                 if (tid == 0 && cta == c0) a.splits[atomicAdd(a.n_splits, 1)] = Split{e.b, e.g, e.run, c0, c1, {0, 0, 0}};
-            } else {
-                __syncthreads();
-                if (tid == 0) {
-                    // releases the CTA's part (ordered before this thread by the barrier) and acquires those of the CTAs ahead
-                    int before_me;
-                    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before_me) : "l"(a.counters + c0) : "memory");
-                    last_flag = before_me == c1 - c0;
-                    if (last_flag) a.counters[c0] = 0;       // ready for the next call
-                }
-                __syncthreads();
-                if (last_flag) {
-                    for (int i = tid; i < heads * (D / 4); i += THREADS) {
-                        const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
-                        Joined j;
-                        j.add<D, HEADS>(a, c0, c1, 1, c0, h, d);
-                        finish(h, d, j.acc, j.top, j.sum);
-                    }
+            } else if (c1 - c0 >= a.few) {
+                join_in_groups<D, HEADS>(a.rows, a.parts, a.counters, static_cast<int>(cta), c0, c1, heads, out0, vs, &last_flag);
+            } else if (arrive(a.counters + c0, c1 - c0, &last_flag)) {
+                for (int i = tid; i < heads * (D / 4); i += THREADS) {
+                    const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
+                    Joined j;
+                    j.add<D, HEADS>(a.parts, c0, c1, 1, c0, h, d);
+                    finish(h, d, j.acc, j.top, j.sum);
                 }
             }
         }
@@ -763,12 +806,22 @@ int launch(DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
         if (di.device >= 0 && di.device < 64) per_sm_of[di.device] = per_sm;
     }
     const int ctas = min(di.sm_count * per_sm, kPartCtas);
-    // Parts of one row if all are about as long: few are joined by the last CTA, from 64 KiB on (about 2 us of one SM's
-    // bandwidth) by a kernel of its own
+    // Whether a second kernel joins the parts has to be said here, where the lengths are not known: from the parts of an entry if all are about as
+    // long, no more than the page table and the window leave room for.  Behind short rows it is 1.2 - 1.8 us for nothing (one row of 777 tokens, a
+    // table for 16,384: 9.2 us with it, 7.7 without).  Two levels in this kernel lose less than that where a CTA has a thread for each four values of
+    // a part (32 query, 8 key-value heads of 128, one row of 4,000 tokens 11.4 -> 12.3 us, of 30,000 30.4 -> 31.8; 4 heads to a single
+    // key-value head 17.3 -> 14.1), but more in several passes (8 heads, 4,000 tokens: 9.2 and 10.1; 16 heads, 30,000: 19.1 and 24.9), from
+    // 64 KiB of parts on (about 2 us of one SM's reads).  One CTA joins up to `few` parts of an entry by itself: batches of eight, 0.6 us each and pass;
+    // two levels are an arrival (about two batches) more
     const i64 entries = static_cast<i64>(a.B) * a.c.Hkv * a.chunks;
-    const i64 most_tiles = (static_cast<i64>(a.max_pages) * a.c.page_size + WARPS * KEYS - 1) / (WARPS * KEYS);
+    i64 most = static_cast<i64>(a.max_pages) * a.c.page_size;
+    if (a.window > 0 && a.window < most) most = a.window;
+    const i64 most_tiles = (most + WARPS * KEYS - 1) / (WARPS * KEYS);
     const i64 share = (ctas + entries - 1) / entries, parts = share < most_tiles ? share : most_tiles;
-    a.defer = parts * min(8 * NT, a.G) * D * 4 > 64 * 1024;
+    const int part_bytes = min(8 * NT, a.G) * D * 4;
+    const int passes = (part_bytes / 16 + WARPS * 32 - 1) / (WARPS * 32);
+    a.defer = passes > 1 && parts * part_bytes > 64 * 1024;
+    a.few = passes == 1 ? 32 : 16;
     if (launch_early(kernel, dim3(ctas), dim3(WARPS * 32), SMEM, s, a) != cudaSuccess) return CAKE_ERR_CUDA;
     if (!a.defer) return CAKE_OK;
     return launch_early(paged_join_kernel<D, 8 * NT>, dim3(2 * di.sm_count), dim3(D), 0, s, a, E4M3) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
@@ -833,7 +886,7 @@ int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_s
     if (di.cc_major != 10) return CAKE_ERR_DEVICE;
     const Shape sh = shape_of(Hq, cache->Hkv);
     DecodeArgs a;
-    a.c = *cache, a.q = q, a.table = page_table, a.lens = seq_lens, a.out = out, a.lse = out_lse;
+    a.c = *cache, a.q = q, a.table = page_table, a.lens = seq_lens, a.rows = Rows{out, out_lse, aligned(out, 8)};
     a.status = static_cast<int*>(ws);
     a.counters = static_cast<int*>(ws) + 64;
     a.n_splits = static_cast<int*>(ws) + 16;
@@ -844,7 +897,6 @@ int cake_paged_decode(const cake_bf16* q, long long q_stride, long long q_head_s
     a.B = static_cast<int>(B), a.Hq = Hq, a.G = Hq / cache->Hkv, a.chunks = sh.chunks, a.max_pages = max_pages, a.window = window;
     a.scale = scale;
     a.q_wide = aligned(q, 16) && q_stride % 8 == 0 && q_head_stride % 8 == 0;
-    a.out_wide = aligned(out, 8);
     const bool e4m3 = cache->type == CAKE_KV_E4M3;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     switch (cache->D) {

@@ -559,6 +559,56 @@ def test_decode_few_sequences_in_many_parts(B, Hq, Hkv, D, kv, length):
     assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,lens,width,window", [
+    (32, 8, 128, [777], 1024, 0),                    # a table with room for 16,384 tokens
+    (4, 1, 128, [5], 8192, 0), (16, 1, 64, [16000], 1024, 100), (64, 8, 128, [16000, 300], 1024, 300), (16, 1, 256, [30000], 1875, 60)])
+def test_decode_short_rows_take_one_launch_whatever_the_table_has_room_for(Hq, Hkv, D, lens, width, window):
+    q, cache, table, n = decode_problem(Hq, Hkv, D, 16, BF16, lens, 41)
+    wide = torch.full((len(lens), width), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    ws = cake.alloc_decode_workspace(len(lens), Hq, Hkv, D, DEV)
+    before = cake.cake_kmeans_kernel_launches()
+    out, lse = cake.cake_paged_decode(q, cache, wide, n, window=window, want_lse=True, ws=ws)
+    assert cake.cake_kmeans_kernel_launches() == before + 1
+    check_decode(q, cache, table, n, out, lse, window)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,kv,page,lens,window", [
+    (4, 1, 128, BF16, 16, [40000], 0),               # 444 parts in two levels: one row
+    (8, 2, 64, E4M3, 16, [30000, 11], 0),            # a CTA ends one row's last group and begins the next's first
+    (3, 1, 128, BF16, 7, [9000, 20001, 5], 9500),    # and a window
+    (16, 1, 256, BF16, 16, [30000] + [40] * 149, 0), (32, 2, 128, E4M3, 32, [5] * 80 + [60000] + [90] * 79, 0),
+    (12, 1, 96, BF16, 16, [17] * 199 + [25000], 20000), (20, 1, 64, E4M3, 16, [30000] * 2 + [1] * 160, 0)])
+def test_decode_rows_of_many_parts_joined_in_two_levels(Hq, Hkv, D, kv, page, lens, window):
+    """Long rows, alone or beside many short ones, that no second kernel joins: between calls of other lengths in the same workspace."""
+    ws = cake.alloc_decode_workspace(len(lens), Hq, Hkv, D, DEV)
+    for change in (lambda x: x, lambda x: [min(n, 50) for n in x], lambda x: x[::-1], lambda x: [n // 3 for n in x], lambda x: x):
+        q, cache, table, n = decode_problem(Hq, Hkv, D, page, kv, change(lens), 43)
+        before = cake.cake_kmeans_kernel_launches()
+        out, lse = cake.cake_paged_decode(q, cache, table, n, window=window, want_lse=True, ws=ws)
+        assert cake.cake_kmeans_kernel_launches() == before + 1
+        check_decode(q, cache, table, n, out, lse, window)
+        for _ in range(3):
+            assert torch.equal(cake.cake_paged_decode(q, cache, table, n, window=window, ws=ws)[0], out)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,kv,lens,window", [
+    (16, 1, 128, BF16, [30000], 9000), (32, 2, 64, E4M3, [[20000, 9], [0, 12345]], 0), (32, 2, 256, BF16, [[15000, 4000]], 5001),
+    (6, 2, 128, E4M3, [[8000, 30000]], 0), (4, 4, 64, BF16, [[500, 0, 20000, 64]] * 3, 333)])
+def test_decode_windows_and_tables_per_head_in_many_parts(Hq, Hkv, D, kv, lens, window):
+    """The join's kernel, and two levels, with windows and with lengths and tables per head."""
+    per_head = isinstance(lens[0], list)
+    page = 1 if D == 64 else 16
+    q, cache, table, n = decode_problem(Hq, Hkv, D, page, kv, lens, 47, per_head=per_head)
+    ws = cake.alloc_decode_workspace(len(lens), Hq, Hkv, D, DEV)
+    for w in (window, 0, 17):
+        out, lse = cake.cake_paged_decode(q, cache, table, n, window=w, want_lse=True, ws=ws)
+        check_decode(q, cache, table, n, out, lse, w)
+        assert torch.equal(cake.cake_paged_decode(q, cache, table, n, window=w, ws=ws)[0], out)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
+
+
 def test_decode_scores_far_apart_and_infinite():
     """A maximum that arrives late, scores of -inf beside finite ones, and a row that is nothing but -inf or NaN."""
     q, cache, table, n = decode_problem(8, 1, 64, 16, BF16, [600, 600, 200, 200], 3, poison=False)
