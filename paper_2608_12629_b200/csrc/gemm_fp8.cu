@@ -760,20 +760,24 @@ gemm_join_kernel(const GemmArgs a) {
 }  // namespace wide
 
 // ---------------------------------------------------------------------------------------------------------------- host
+// The plan of a product, its workspace and the order of its sums follow from the sizes alone: it asks no device, but has a B200's figures
+constexpr int SMS = 148;
 constexpr int MOST_PARTS = 8;      // CTAs of a cluster
+// Clusters of so many CTAs of the narrow kernel (one to an SM) that a B200 runs at once, as the occupancy query counts them: fewer than
+// the SMs divided by their size, since a cluster stays inside one group of SMs.  A chip grouped otherwise runs some of them later
+constexpr int CLUSTERS[MOST_PARTS + 1] = {0, SMS, 74, 45, 33, 26, 22, 15, 15};
 struct Plan {
     bool pair;
     int tn, bn, tiles_m, tiles_n, splits, nkb;
     size_t part_bytes;
 };
-// clusters[s]: clusters of s CTAs of the narrow kernel that fit the device at once (nullptr: not asked yet; no matter for the workspace)
-Plan plan_of(i64 M, int N, int K, int sms, const int* clusters) {
+Plan plan_of(i64 M, int N, int K) {
     Plan p;
     p.nkb = (K + KB - 1) / KB;
     p.pair = M > NARROW_M;
     p.tn = p.pair ? wide::BM : M <= 16 ? 16 : M <= 32 ? 32 : 64;
     p.tiles_m = static_cast<int>((M + p.tn - 1) / p.tn);
-    const int units = p.pair ? sms / 2 : sms;        // that work on a tile each
+    const int units = p.pair ? SMS / 2 : SMS;        // that work on a tile each
     // The shape of a pair's tile, and parts of the contraction (all of them in one round): what needs the least time, counted in
     // nanoseconds of a block (measured over 128 blocks: 510 of 256 x 256, 290 of 256 x 128), of a tile's start and end, and of
     // writing and joining the parts.  517 x 2624 x 5120: 22.3 us in 256 x 256 tiles and two parts, 15.7 - 18.3 in 256 x 128
@@ -784,7 +788,7 @@ Plan plan_of(i64 M, int N, int K, int sms, const int* clusters) {
         const i64 tiles = static_cast<i64>(p.tiles_m) * tiles_n;
         const double block = !p.pair ? 150 : bn == 256 ? 510 : 290, tile = p.pair ? (bn == 256 ? 2000 : 1200) : 1000;
         for (int s = 1; s == 1 || (s <= p.nkb / 2 && s <= (p.pair ? 32 : MOST_PARTS) && tiles * s <= units); ++s) {
-            if (s > 1 && !p.pair && clusters && tiles > clusters[s]) continue;
+            if (!p.pair && tiles > CLUSTERS[s] && s > 1) continue;
             const double rounds = static_cast<double>((tiles * s + units - 1) / units);
             double cost = rounds * ((p.nkb + s - 1) / s * block + tile);
             if (s > 1) cost += p.pair ? 3000 + (bn == 256 ? 2000 : 1000) + 300 * s : 700 + 30 * s;
@@ -794,42 +798,6 @@ Plan plan_of(i64 M, int N, int K, int sms, const int* clusters) {
     const i64 tiles = static_cast<i64>(p.tiles_m) * p.tiles_n;
     p.part_bytes = p.pair && p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * wide::BM * p.bn * 4 : 0;
     return p;
-}
-
-// clusters of 2 .. MOST_PARTS CTAs that are resident at once: fewer than the SMs divided by their size, since a cluster stays inside one
-// group of SMs (asked once per device)
-template <int TN>
-int clusters_of(const DeviceInfo& di, int (&out)[MOST_PARTS + 1]) {
-    static int known[64][MOST_PARTS + 1] = {};
-    const bool keep = di.device >= 0 && di.device < 64;
-    if (!keep || known[di.device][1] == 0) {
-        if (cudaFuncSetAttribute(gemm_fp8_kernel<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<TN>::SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
-        for (int s = 2; s <= MOST_PARTS; ++s) {
-            cudaLaunchAttribute at[1];
-            at[0].id = cudaLaunchAttributeClusterDimension;
-            at[0].val.clusterDim.x = s;
-            at[0].val.clusterDim.y = 1;
-            at[0].val.clusterDim.z = 1;
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(s);
-            cfg.blockDim = dim3(THREADS);
-            cfg.dynamicSmemBytes = Tile<TN>::SMEM;
-            cfg.attrs = at;
-            cfg.numAttrs = 1;
-            int n = 0;
-            if (cudaOccupancyMaxActiveClusters(&n, gemm_fp8_kernel<TN>, &cfg) != cudaSuccess) {
-                cudaGetLastError();
-                n = 0;
-            }
-            out[s] = n;
-        }
-        out[0] = 0, out[1] = di.sm_count;
-        if (keep)
-            for (int s = MOST_PARTS; s >= 0; --s) known[di.device][s] = out[s];
-        return CAKE_OK;
-    }
-    for (int s = 0; s <= MOST_PARTS; ++s) out[s] = known[di.device][s];
-    return CAKE_OK;
 }
 
 template <int TN>
@@ -907,7 +875,6 @@ int check_shape(i64 M, int N, int K) {
     if (((M + 127) / 128) * ((static_cast<i64>(N) + TM - 1) / TM) > INT_MAX / 64) return CAKE_ERR_SHAPE;
     return CAKE_OK;
 }
-constexpr int kMaxSms = 148;      // the plan that sizes the workspace touches no device: that of a B200
 
 }  // namespace
 }  // namespace serving
@@ -922,7 +889,7 @@ int cake_gemm_fp8_workspace_bytes(long long M, int N, int K, size_t* out_bytes) 
     if (!out_bytes) return CAKE_ERR_NULL;
     const int rc = check_shape(M, N, K);
     if (rc != CAKE_OK) return rc;
-    *out_bytes = kHeaderBytes + plan_of(M, N, K, kMaxSms, nullptr).part_bytes;
+    *out_bytes = kHeaderBytes + plan_of(M, N, K).part_bytes;
     return CAKE_OK;
 }
 
@@ -939,18 +906,12 @@ int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, 
     if (!X || !W || !x_scale || !w_scale || !out) return CAKE_ERR_NULL;
     if (K % 16 != 0 || x_stride % 16 != 0 || w_stride % 16 != 0 || !aligned(X, 16) || !aligned(W, 16)) return CAKE_ERR_ALIGN;
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(out, (flags & CAKE_GEMM_OUT_FP32) ? 4 : 2)) return CAKE_ERR_ALIGN;
-    Plan p = plan_of(M, N, K, kMaxSms, nullptr);
+    const Plan p = plan_of(M, N, K);
     if (ws_bytes < kHeaderBytes + p.part_bytes) return CAKE_ERR_WORKSPACE;
     DeviceInfo di;
     rc = current_device_info(&di);
     if (rc != CAKE_OK) return rc;
     if (di.cc_major != 10) return CAKE_ERR_DEVICE;
-    if (!p.pair) {
-        int clusters[MOST_PARTS + 1];
-        rc = p.tn == 16 ? clusters_of<16>(di, clusters) : p.tn == 32 ? clusters_of<32>(di, clusters) : clusters_of<64>(di, clusters);
-        if (rc != CAKE_OK) return rc;
-        p = plan_of(M, N, K, kMaxSms, clusters);
-    }
     CUtensorMap mw, mx;
     rc = make_tmap_bytes(&mw, W, K, N, w_stride, p.pair ? 64 : TM);
     if (rc != CAKE_OK) return rc;

@@ -233,6 +233,27 @@ def test_gemm_integer_data_is_exact():
     assert torch.equal(out.double(), xd @ wd.t())
 
 
+@pytest.mark.parametrize("M,N,K,parts", [
+    (16, 128, 4096, 8), (3, 1920, 4096, 8), (3, 2048, 4096, 6), (16, 2816, 4096, 6), (16, 2944, 4096, 5), (33, 4224, 2048, 4),
+    (33, 4352, 2048, 3), (1, 5760, 4096, 3), (1, 5888, 4096, 2), (64, 9472, 2048, 2), (64, 9600, 2048, 1), (5, 128, 384, 1)])
+def test_gemm_order_of_sums_follows_from_the_sizes(M, N, K, parts):
+    """Blocks of which each contributes its scale alone: fp32 sums of random numbers show in what order they were added.  The parts of a contraction
+    (up to 64 rows) are those that the sizes say, whatever the device's SMs are grouped like."""
+    nk = K // 128
+    x, w = (torch.zeros(r, K, device=DEV) for r in (M, N))
+    x[:, ::128] = 1.0
+    w[:, ::128] = 1.0
+    xs = torch.empty(M, nk, device=DEV).uniform_(0.1, 1.0, generator=gen(N))
+    out = cake.cake_gemm_fp8(x.to(E4M3), xs, w.to(E4M3), torch.ones(N // 128, nk, device=DEV), out_dtype=torch.float32)
+    want = torch.zeros(M, device=DEV)
+    for s in range(parts):
+        part = torch.zeros(M, device=DEV)
+        for kb in range(s * nk // parts, (s + 1) * nk // parts):
+            part = part + xs[:, kb]
+        want = want + part
+    assert torch.equal(out, want[:, None].expand(M, N))
+
+
 def test_gemm_nan_stays_in_its_row_and_column():
     x, xs, w, ws = gemm_inputs(20, 140, 256, 1)
     x.view(torch.uint8)[3, 200] = 0x7f
