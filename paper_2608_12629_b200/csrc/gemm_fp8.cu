@@ -803,11 +803,8 @@ Plan plan_of(i64 M, int N, int K) {
 template <int TN>
 int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, const DeviceInfo& di, cudaStream_t s) {
     using T = Tile<TN>;
-    static bool set[64] = {};
-    if (di.device < 0 || di.device >= 64 || !set[di.device]) {
-        if (cudaFuncSetAttribute(gemm_fp8_kernel<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
-        if (di.device >= 0 && di.device < 64) set[di.device] = true;
-    }
+    static PerDevice ready;
+    if (!ready.get(di.device, [] { return allow_smem(gemm_fp8_kernel<TN>, T::SMEM); })) return CAKE_ERR_CUDA;
     const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
     if (a.splits == 1) {
         const int ctas = static_cast<int>(items < di.sm_count ? items : di.sm_count);
@@ -837,11 +834,8 @@ int launch(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, cons
 
 template <int BN>
 int launch_pair(const GemmArgs& a, const CUtensorMap& mw, const CUtensorMap& mx, const DeviceInfo& di, cudaStream_t s) {
-    static bool set[64] = {};
-    if (di.device < 0 || di.device >= 64 || !set[di.device]) {
-        if (cudaFuncSetAttribute(wide::gemm_fp8_pair_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, wide::pair_smem<BN>()) != cudaSuccess) return CAKE_ERR_CUDA;
-        if (di.device >= 0 && di.device < 64) set[di.device] = true;
-    }
+    static PerDevice ready;
+    if (!ready.get(di.device, [] { return allow_smem(wide::gemm_fp8_pair_kernel<BN>, wide::pair_smem<BN>()); })) return CAKE_ERR_CUDA;
     const i64 items = static_cast<i64>(a.tiles_m) * a.tiles_n * a.splits;
     const int pairs = static_cast<int>(items < di.sm_count / 2 ? items : di.sm_count / 2);
     cudaLaunchConfig_t cfg = {};

@@ -793,18 +793,16 @@ int launch(DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     constexpr int RING = RING1 * STAGES;
     constexpr int MERGE = WARPS * 8 * NT * (D + 4) * 4;
     constexpr int SMEM = RING > MERGE ? RING : MERGE;
-    static bool set[64] = {};
-    auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES, WARPS, PER_SM>;
-    if (di.device < 0 || di.device >= 64 || !set[di.device]) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return CAKE_ERR_CUDA;
-        if (di.device >= 0 && di.device < 64) set[di.device] = true;
-    }
-    static int per_sm_of[64] = {};
-    int per_sm = di.device >= 0 && di.device < 64 ? per_sm_of[di.device] : 0;
-    if (per_sm == 0) {
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, WARPS * 32, SMEM) != cudaSuccess || per_sm < 1) return CAKE_ERR_CUDA;
-        if (di.device >= 0 && di.device < 64) per_sm_of[di.device] = per_sm;
-    }
+    const auto kernel = paged_decode_kernel<D, E4M3, NT, STAGES, WARPS, PER_SM>;
+    static PerDevice resident;
+    const int per_sm = resident.get(di.device, [kernel]() -> int {
+        int n = 0;
+        if (!allow_smem(kernel, SMEM)) return 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, WARPS * 32, SMEM) == cudaSuccess) return n;
+        cudaGetLastError();
+        return 0;
+    });
+    if (per_sm < 1) return CAKE_ERR_CUDA;
     const int ctas = min(di.sm_count * per_sm, kPartCtas);
     // Whether a second kernel joins the parts has to be said here, where the lengths are not known: from the parts of an entry if all are about as
     // long, no more than the page table and the window leave room for.  Behind short rows it is 1.2 - 1.8 us for nothing (one row of 777 tokens, a

@@ -4,6 +4,8 @@
 #include <cuda_fp16.h>
 #include <limits.h>
 
+#include <atomic>
+
 #include "../../include/cake_serving.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -21,6 +23,30 @@ constexpr size_t kHeaderBytes = 256 + kMaxCtas * 4;
 static_assert(kHeaderBytes == CAKE_SERVING_HEADER_BYTES, "header and ABI constant agree");
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// A number about a kernel on a device, asked for by the first launch there and kept.  Host threads that launch for the first time at once all ask,
+// and get the same answer; an answer of 0 (the query failed) is not kept.
+class PerDevice {
+public:
+    template <class Ask>
+    int get(int device, Ask&& ask) {
+        if (device < 0 || device >= kDevices) return ask();
+        int v = known_[device].load(std::memory_order_acquire);
+        if (v == 0 && (v = ask()) != 0) known_[device].store(v, std::memory_order_release);
+        return v;
+    }
+
+private:
+    static constexpr int kDevices = 64;
+    std::atomic<int> known_[kDevices] = {};
+};
+// Room in shared memory for a kernel: 1, or 0 where the device refuses it.
+template <class Kernel>
+int allow_smem(Kernel kernel, size_t bytes) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess) return 1;
+    cudaGetLastError();
+    return 0;
+}
 
 // Launch that may begin while the kernel ahead of it in the stream drains: the kernel waits for that one itself (ptx::grid_dep_wait,
 // before its first access to global memory).  In a stream of short kernels this hides their launch.  Such a kernel runs while its
