@@ -57,10 +57,13 @@ CAKE_API int cake_rmsnorm_quant(const cake_bf16* x, long long x_stride, const ca
  *   X        [M][K] e4m3, rows x_stride apart, in        x_scale [M][ceil(K/128)] fp32 contiguous, in
  *   W        [N][K] e4m3, rows w_stride apart, in        w_scale [ceil(N/128)][ceil(K/128)] fp32 contiguous, in
  *   out      [M][N] rows out_stride apart, bf16, or fp32 with CAKE_GEMM_OUT_FP32, out
- *   ws       at least cake_gemm_fp8_workspace_bytes(M, N, K) bytes
+ *   ws       at least cake_gemm_fp8_workspace_bytes(M, N, K) bytes.  That number does not grow with M (a product of fewer rows may
+ *            split its contraction where one of more does not): a buffer for products of several sizes has the largest
+ *            of their numbers, or CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES, which no size exceeds
  * K % 16 == 0, x_stride % 16 == 0, w_stride % 16 == 0, X and W 16-byte aligned (CAKE_ERR_ALIGN).  M = 0 does nothing.
  */
 enum { CAKE_GEMM_OUT_FP32 = 1 };
+#define CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES 19415296   /* the header and 74 tiles of 256 x 256 fp32 */
 CAKE_API int cake_gemm_fp8_workspace_bytes(long long M, int N, int K, size_t* out_bytes);
 CAKE_API int cake_gemm_fp8(const cake_e4m3* X, long long x_stride, const float* x_scale, const cake_e4m3* W, long long w_stride,
                            const float* w_scale, long long M, int N, int K, void* out, long long out_stride, void* ws,

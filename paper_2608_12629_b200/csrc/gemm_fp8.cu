@@ -37,6 +37,8 @@ constexpr int BUFS = 4;                        // steps whose accumulators, and 
 constexpr int PER_STEP = 2;
 constexpr uint32_t W_BYTES = TM * KB;
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
+// The plan of a product, its workspace and the order of its sums follow from the sizes alone: it asks no device, but has a B200's figures
+constexpr int SMS = 148;
 // Rows of X up to which the narrow kernel is taken: 64 rows against 8192 x 8192, 16.8 us there and 20.8 us by pairs; 40 against 5000 x 5120,
 // 9.4 and 14.2; beyond 64 the narrow tile would read W more than once
 constexpr int NARROW_M = 64;
@@ -719,6 +721,9 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     }
 }
 
+// (the parts of a split contraction are no more than the pairs of SMs: one round)
+static_assert(kHeaderBytes + static_cast<size_t>(SMS / 2) * BM * 256 * 4 == CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES, "the most that a plan asks for, and the ABI's constant");
+
 // Sums of the parts of a split contraction, in order; four columns to a thread.
 template <int BN>
 __global__ void __launch_bounds__(256)
@@ -760,8 +765,6 @@ gemm_join_kernel(const GemmArgs a) {
 }  // namespace wide
 
 // ---------------------------------------------------------------------------------------------------------------- host
-// The plan of a product, its workspace and the order of its sums follow from the sizes alone: it asks no device, but has a B200's figures
-constexpr int SMS = 148;
 constexpr int MOST_PARTS = 8;      // CTAs of a cluster
 // Clusters of so many CTAs of the narrow kernel (one to an SM) that a B200 runs at once, as the occupancy query counts them: fewer than
 // the SMs divided by their size, since a cluster stays inside one group of SMs.  A chip grouped otherwise runs some of them later

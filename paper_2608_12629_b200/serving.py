@@ -20,6 +20,7 @@ CAKE_RMSNORM_NONE = 1
 CAKE_GEMM_OUT_FP32 = 1
 CAKE_APPEND_INTERLEAVED = 1
 CAKE_SERVING_HEADER_BYTES = 16640
+CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES = 19415296
 
 SERVING_EXPORTS = [
     "cake_rmsnorm_quant", "cake_gemm_fp8_workspace_bytes", "cake_gemm_fp8", "cake_kv_append",
@@ -124,8 +125,8 @@ def cake_gemm_fp8_workspace_bytes(M, N, K) -> int:
 
 
 def alloc_gemm_workspace(M, N, K, device) -> torch.Tensor:
-    """A workspace for cake_gemm_fp8 of this size, its header zeroed."""
-    return _workspace(cake_gemm_fp8_workspace_bytes(M, N, K), device)
+    """A workspace for cake_gemm_fp8 of this size, its header zeroed; with M None, of any number of rows (fewer may need more)."""
+    return _workspace(CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES if M is None else cake_gemm_fp8_workspace_bytes(M, N, K), device)
 
 
 def cake_gemm_fp8(X, x_scale, W, w_scale, out=None, out_dtype=_BF16, ws=None, stream=None):

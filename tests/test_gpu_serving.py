@@ -219,6 +219,17 @@ def test_gemm_strides_and_one_workspace_for_many_sizes():
     assert cake.cake_kmeans_device_status(big) == cake.CAKE_OK
 
 
+def test_gemm_one_workspace_for_any_number_of_rows():
+    """Plans with a split contraction and without one in turn, sizes that need less and more than the one before."""
+    N, K = 1024, 4096
+    buf = cake.alloc_gemm_workspace(None, N, K, DEV)
+    assert len({cake.cake_gemm_fp8_workspace_bytes(m, N, K) for m in (4096, 300, 128, 64)}) > 2
+    for M in (4096, 300, 128, 64, 1, 256, 5000, 65, 2048, 129):
+        x, xs, w, ws = gemm_inputs(M, N, K, M)
+        check_gemm(x, xs, w, ws, cake.cake_gemm_fp8(x, xs, w, ws, ws=buf))
+    assert cake.cake_kmeans_device_status(buf) == cake.CAKE_OK
+
+
 def test_gemm_integer_data_is_exact():
     """Small whole numbers, scales that are powers of two: every product and sum is exact, so a wrong block or row shows."""
     g = gen(9)

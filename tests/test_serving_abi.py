@@ -64,6 +64,17 @@ def test_workspace_sizes_need_no_device():
         assert e.value.code == code
 
 
+def test_no_product_needs_more_than_the_most(L):
+    """A buffer for any number of rows: the size needed is no growing function of them."""
+    most = cake.CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES
+    assert int(re.search(r"CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES (\d+)", header()).group(1)) == most
+    assert cake.cake_gemm_fp8_workspace_bytes(256, 4096, 4096) > cake.cake_gemm_fp8_workspace_bytes(8192, 4096, 4096)
+    ms = [1, 16, 64, 65, 128, 200, 256, 257, 384, 512, 517, 768, 1000, 1024, 2048, 4096, 5000, 18944, 100000]
+    ns = [1, 127, 128, 129, 256, 300, 512, 640, 1000, 1024, 1280, 2048, 2624, 4096, 6144, 8192, 9472, 18944, 18945, 100000]
+    sizes = [cake.cake_gemm_fp8_workspace_bytes(m, n, k) for m in ms for n in ns for k in (16, 128, 512, 1024, 4096, 8192, 14336, 131072)]
+    assert max(sizes) <= most and max(sizes) > 0.9 * most
+
+
 def cache(**more):
     c = serving._CacheStruct(4096, 4096, None, None, 4, 16 * 128, 128, 128, 16 * 128, 128, 128, 16, 1, 128, cake.CAKE_KV_BF16)
     for k, v in more.items():
