@@ -102,7 +102,8 @@ typedef struct cake_paged_cache {
  *              queries are).  A slot beyond the cache: not written, and the device status becomes CAKE_ERR_BAD_INDEX
  *   positions  [T] int32, in;  cos_sin [max_positions][rot] fp32 contiguous, in.  rot = 0: no rotation, both may be NULL.
  *              A position outside [0, max_positions): nothing of the token is written, device status CAKE_ERR_BAD_INDEX
- * Slots that occur twice among the T leave either of the two tokens.  ws: CAKE_SERVING_HEADER_BYTES bytes.
+ * A slot that occurs twice among the T is left with elements of both tokens, in no particular mixture (the key of one beside the
+ * value of the other, or parts of heads); no other slot is touched.  ws: CAKE_SERVING_HEADER_BYTES bytes.
  */
 enum { CAKE_APPEND_INTERLEAVED = 1 };
 CAKE_API int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k, long long k_stride, const cake_bf16* v,

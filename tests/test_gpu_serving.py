@@ -427,6 +427,29 @@ def test_append_bits_do_not_depend_on_alignment(kv, pairs):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T", [20, 3000])
+def test_append_a_slot_named_twice(T):
+    """Its elements are of the one or the other token; every other slot is what it would be without the second."""
+    g = gen(T)
+    Hkv, D, page = 3, 64, 16
+    k, v = normal(g, T, Hkv, D), normal(g, T, Hkv, D)
+    slots = torch.randperm(2 * T, generator=g, device=DEV)[:T]
+    twin = torch.randperm(T, generator=g, device=DEV)[:T // 4 * 2].view(2, -1)
+    slots[twin[1]] = slots[twin[0]]
+    kc, vc = (torch.full((-(-2 * T // page), page, Hkv, D), 7.0, dtype=BF16, device=DEV) for _ in range(2))
+    cake.cake_kv_append(cake.PagedCache(kc, vc), k, v, slots)
+    for cache, new in ((kc, k), (vc, v)):
+        flat = cache.view(-1, Hkv, D)
+        here = flat[slots[twin[0]]]
+        assert ((here == new[twin[0]]) | (here == new[twin[1]])).all()
+        once = torch.ones(T, dtype=torch.bool, device=DEV)
+        once[twin.flatten()] = False
+        assert torch.equal(flat[slots[once]], new[once])
+        rest = torch.ones(flat.shape[0], dtype=torch.bool, device=DEV)
+        rest[slots] = False
+        assert (flat[rest] == 7.0).all()
+
+
 def test_append_in_place_queries_and_refusals():
     g = gen(6)
     kc = torch.zeros(4, 8, 2, 128, dtype=BF16, device=DEV)
