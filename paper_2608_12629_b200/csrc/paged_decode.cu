@@ -405,7 +405,7 @@ paged_decode_kernel(const DecodeArgs a) {
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * L::STAGE;
     const uint32_t bar0 = ptx::smem_u32(&bars[warp][0]);
     uint32_t phases = 0;             // bit s: parity of the next completion of stage s
-    bool dead = false;               // a wait has expired: no more copies, no more waits
+    bool dead = false;               // a wait has expired: no more copies, and a bounded wait for each that is under way
     const int row = lane & 15;
     const bool is_v = lane >= 16;
     const uint32_t row_dst = ring + (is_v ? L::K_BYTES + row * L::V_PITCH : row * L::K_PITCH);
@@ -569,7 +569,7 @@ paged_decode_kernel(const DecodeArgs a) {
             if (!L::BULK) {
                 cp_wait<STAGES - 1>();
                 __syncwarp();
-            } else if (!dead) {
+            } else {                 // (also after a wait that expired: no copy in flight is left behind unwaited for)
                 const uint32_t bar = bar0 + 8 * here, parity = (phases >> here) & 1;
                 int tries = 0;
                 while (!ptx::mbar_try_wait_hint(bar, parity, 20000) && tries < WAIT_TRIES) ++tries;
