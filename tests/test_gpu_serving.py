@@ -887,3 +887,90 @@ def test_scratch_and_outputs_of_another_stream():
             assert torch.equal(a, b)
         torch.cuda.synchronize()
         del scribble
+
+
+@pytest.mark.parametrize("kv", [BF16, E4M3])
+def test_keys_and_values_of_different_stride_orders(kv):
+    """Keys token by token inside a page, values head by head (and rows further apart than they are long)."""
+    g = gen(15)
+    pages, page, Hkv, D = 12, 16, 4, 128
+    k = torch.zeros(pages, page, Hkv, D + 16, device=DEV).to(kv)[..., :D]
+    v = torch.zeros(pages, Hkv, page + 1, D, device=DEV).to(kv)[:, :, :page].transpose(1, 2)
+    ks, vs = (torch.empty(Hkv, device=DEV).uniform_(0.01, 0.03, generator=g) if kv == E4M3 else None for _ in range(2))
+    cache, plain = cake.PagedCache(k, v, ks, vs), cake.PagedCache(k.clone(memory_format=torch.contiguous_format), v.clone(memory_format=torch.contiguous_format), ks, vs)
+    T = 150
+    new_k, new_v = normal(g, T, Hkv, D), normal(g, T, Hkv, D)
+    slots = torch.randperm(pages * page, generator=g, device=DEV)[:T]
+    for c in (cache, plain):
+        cake.cake_kv_append(c, new_k, new_v, slots)
+    for a, b in ((cache.k, plain.k), (cache.v, plain.v)):
+        assert torch.equal(a.float(), b.float())
+    q = normal(g, 3, 12, D)
+    table = torch.randperm(pages, generator=g, device=DEV).to(torch.int32).view(3, 4)
+    n = torch.tensor([64, 1, 39], dtype=torch.int32, device=DEV)
+    out, lse = cake.cake_paged_decode(q, cache, table, n, want_lse=True)
+    check_decode(q, cache, table, n, out, lse)
+    assert torch.equal(out, cake.cake_paged_decode(q, plain, table, n)[0])
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,kv,start", [(16, 8, 2, 64, BF16, 40), (3, 16, 1, 128, E4M3, 9000), (150, 4, 4, 64, E4M3, 3)])
+def test_calls_back_to_back_give_the_bits_of_calls_one_by_one(B, Hq, Hkv, D, kv, start):
+    """Every kernel may start before the one ahead of it ends: steps of a layer, each call writing what calls ahead of it still read, over the same few
+    buffers; 60 steps with nothing between the launches, and as a graph, against the same steps with a wait after every call."""
+    H, page, steps = 512, 16, 60
+    g = gen(B)
+    rows = (Hq + 2 * Hkv) * D
+    w_in, w_out = normal(g, rows, H, std=1.0, dtype=E4M3), normal(g, H, Hq * D, std=1.0, dtype=E4M3)
+    s_in = torch.full((-(-rows // 128), H // 128), 0.04, device=DEV)
+    s_out = torch.full((H // 128, -(-Hq * D // 128)), 0.04, device=DEV)
+    norm_w = normal(g, H, std=0.1) + 1
+    width = -(-(start + steps) // page)
+    table = torch.randperm(B * width, generator=g, device=DEV).to(torch.int32).view(B, width)
+    at = start + torch.arange(steps, device=DEV)
+    slots = (table[:, at // page].long() * page + at % page).t().contiguous()          # [steps, B]
+    lens = (at + 1).to(torch.int32)[:, None].expand(steps, B).contiguous()
+    pos, cos_sin = at.to(torch.int32)[:, None].expand(steps, B).contiguous(), rotary_table(start + steps, D)
+    hidden = normal(g, B, H)
+    old_k, old_v = (normal(g, B * width, page, Hkv, D, std=40.0 if kv == E4M3 else 1.0, dtype=kv) for _ in range(2))
+    scale = torch.full((Hkv,), 0.02, device=DEV) if kv == E4M3 else None
+
+    def run(wait, graph=False):
+        cache = cake.PagedCache(old_k.clone(), old_v.clone(), scale, scale)
+        x, res = hidden.clone(), torch.zeros_like(hidden)
+        q8, sc = torch.empty(B, H, dtype=E4M3, device=DEV), torch.empty(B, H // 128, device=DEV)
+        a8, asc = torch.empty(B, Hq * D, dtype=E4M3, device=DEV), torch.empty(B, -(-Hq * D // 128), device=DEV)
+        proj = torch.empty(B, rows, dtype=BF16, device=DEV)
+        heads = proj.view(B, Hq + 2 * Hkv, D)
+        q, att = (torch.empty(B, Hq, D, dtype=BF16, device=DEV) for _ in range(2))
+        ws, gws = cake.alloc_decode_workspace(B, Hq, Hkv, D, DEV), cake.alloc_gemm_workspace(None, rows, H, DEV)
+
+        def step(t):
+            for call in (lambda: cake.cake_rmsnorm_quant(x, norm_w, res, out_residual=res, out_q=q8, out_scale=sc),
+                         lambda: cake.cake_gemm_fp8(q8, sc, w_in, s_in, out=proj, ws=gws),
+                         lambda: cake.cake_kv_append(cache, heads[:, Hq:Hq + Hkv], heads[:, Hq + Hkv:], slots[t], pos[t], cos_sin, q=heads[:, :Hq], out_q=q, ws=ws),
+                         lambda: cake.cake_paged_decode(q, cache, table, lens[t], out=att, ws=ws),
+                         lambda: cake.cake_rmsnorm_quant(att.view(B, -1), out_q=a8, out_scale=asc, flags=cake.CAKE_RMSNORM_NONE, want_residual=False),
+                         lambda: cake.cake_gemm_fp8(a8, asc, w_out, s_out, out=x, ws=gws)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+
+        if graph:
+            torch.cuda.synchronize()
+            captured = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(captured):
+                for t in range(steps):
+                    step(t)
+            captured.replay()
+        else:
+            for t in range(steps):
+                step(t)
+        torch.cuda.synchronize()
+        assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK and cake.cake_kmeans_device_status(gws) == cake.CAKE_OK
+        return [x, res, att, cache.k.view(torch.uint8), cache.v.view(torch.uint8)]
+
+    want = run(True)
+    assert torch.isfinite(want[0].float()).all() and (want[2] != 0).any()
+    for got in (run(False), run(False), run(False, graph=True)):
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
