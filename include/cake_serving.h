@@ -5,7 +5,8 @@
  *   gemm_fp8        product of two 8-bit matrices with scales per 128-column block (and 128 x 128 block of the weights);
  *   kv_append       rotation of queries and keys by position, keys and values written to a paged cache;
  *   paged_decode    attention of one new token per sequence over the paged cache.
- * The paper has no counterpart of these calls.
+ * The paper names a grouped-query decode and a block-scaled 8-bit product among its other kernels, without their source or interface;
+ * these calls follow neither.
  *
  * Conventions are those of cake_kmeans.h (device pointers, caller-owned buffers, asynchronous on `stream`, CAKE_* return
  * codes, nothing allocated), and
@@ -32,7 +33,8 @@ typedef unsigned char cake_e4m3;
 /*
  * Per row t of T:  s = x[t] + residual[t];  y = s * rsqrt(mean(s^2) + eps) * weight;  then an 8-bit copy of y with scales:
  * scale_g = max(max|y over group g| / 448, 2^-100), q = y / scale_g rounded to nearest even.  Sums are held in 32 bits; y is
- * not rounded before it is quantised, and the norm is that of the unrounded s.
+ * not rounded before it is quantised, and the norm is that of the unrounded s.  (The quotient is formed as (s * weight) * (factor /
+ * scale), with an approximate reciprocal: q may be the neighbouring e4m3 value where y / scale lies within the roundings of its factors of a tie)
  *   x            [T][H] bf16, rows x_stride apart, in
  *   residual     [T][H] bf16, rows residual_stride apart, in, may be NULL
  *   weight       [H] bf16, in, may be NULL (all ones)
@@ -57,7 +59,7 @@ CAKE_API int cake_rmsnorm_quant(const cake_bf16* x, long long x_stride, const ca
  *   X        [M][K] e4m3, rows x_stride apart, in        x_scale [M][ceil(K/128)] fp32 contiguous, in
  *   W        [N][K] e4m3, rows w_stride apart, in        w_scale [ceil(N/128)][ceil(K/128)] fp32 contiguous, in
  *   out      [M][N] rows out_stride apart, bf16, or fp32 with CAKE_GEMM_OUT_FP32, out
- *   ws       at least cake_gemm_fp8_workspace_bytes(M, N, K) bytes.  That number does not grow with M (a product of fewer rows may
+ *   ws       at least cake_gemm_fp8_workspace_bytes(M, N, K) bytes.  That number is not monotonic in M (a product of fewer rows may
  *            split its contraction where one of more does not): a buffer for products of several sizes has the largest
  *            of their numbers, or CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES, which no size exceeds
  * K % 16 == 0, x_stride % 16 == 0, w_stride % 16 == 0, X and W 16-byte aligned (CAKE_ERR_ALIGN).  M = 0 does nothing.

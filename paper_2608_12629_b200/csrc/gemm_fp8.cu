@@ -13,10 +13,11 @@
 //   more            X is the M side, two SMs to a 256 x 256 tile (cta_group::2: each loads half of both operands, 32 KiB a block instead
 //                   of the 48 of a 128 x 256 tile of one SM, whose demand of 94 bytes a clock the L2 does not meet).  The scale of an
 //                   element depends on its lane and on its half of the columns: one factor per thread and block, packed FMAs.
-// Measured: 8192 x 8192 x 8192 504 - 540 us (2.04 - 2.18 PFLOP/s, 62 - 66 % of twice the bf16 burst rate; 480 us in a single launch at full clock,
-// tensor pipe 65 % busy): an accumulator's round trip (product, signal, 128 columns added by the epilogue, signal) is what bounds
-// a block, and the operands' 96 KiB of shared-memory traffic is close behind.  16 x 6144 x 4096 7.4 us (3.4 TB/s of weights, 53 %), 64 x 8192 x 8192
-// 16.8 us (4.1 TB/s, 62 %): start, first loads and join are about 4 us of each.
+// Measured: 8192 x 8192 x 8192 526 - 556 us repeated (1.98 - 2.09 PFLOP/s, 60 - 63 % of twice the bf16 burst rate; under the power cap, clocks of 1.4 to
+// 1.9 GHz), 504 in short bursts, 478 in a single launch at full clock (tensor pipe 65 % busy): an accumulator's round trip (product, signal, 128 columns added by the epilogue, signal) is what bounds
+// a block, and the operands' 96 KiB of shared-memory traffic is close behind.  16 x 6144 x 4096 9.1 us with weights from memory (2.8 TB/s, 43 % of the copy
+// rate; 6.8 - 7.6 us where they lie in the L2), 64 x 8192 x 8192 16.8 - 21.5 us (3.2 - 4.1 TB/s, 49 - 63 %, from one device to the next; 13.9 in the
+// L2): start, first loads and join are about 4 us of each.
 // Where a product has too few tiles for the SMs its contraction is split; the parts of a narrow tile are added up
 // through the shared memory of a cluster, those of the pairs by a second kernel.
 #include "ptx.cuh"
@@ -39,7 +40,7 @@ constexpr uint32_t W_BYTES = TM * KB;
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 // The plan of a product, its workspace and the order of its sums follow from the sizes alone: it asks no device, but has a B200's figures
 constexpr int SMS = 148;
-// Rows of X up to which the narrow kernel is taken: 64 rows against 8192 x 8192, 16.8 us there and 20.8 us by pairs; 40 against 5000 x 5120,
+// Rows of X up to which the narrow kernel is taken: 64 rows against 8192 x 8192, 16.8 us there and 20.8 us by pairs (same device); 40 against 5000 x 5120,
 // 9.4 and 14.2; beyond 64 the narrow tile would read W more than once
 constexpr int NARROW_M = 64;
 

@@ -5,7 +5,8 @@
 // Bound by memory: q, k, v are read once and written once.  A thread keeps the cosines and sines of its place in a head
 // and walks over heads, four at a time, so the table is read once per token and group of threads, not once per head.
 // Measured: 16,001 tokens of 32 + 2 * 8 heads of 128, half of each rotated, into an 8-bit cache 63 us, 5.82 TB/s, 89 % of the copy
-// rate; 16,384 tokens into a bf16 cache 69 us, 91 %; 16 tokens 2.5 us.
+// rate; 16,384 tokens into a bf16 cache 69 us, 91 %; 16 tokens 2.5 us.  A value goes into an 8-bit cache as x * (1 / scale): a rounding of 2^-24 more than
+// x / scale, far below the format's 2^-4, and one division for eight elements.
 #include "serving.cuh"
 
 namespace cake {
@@ -269,8 +270,9 @@ extern "C" int cake_kv_append(const cake_paged_cache* cache, const cake_bf16* k,
         const int units = pairs ? D / 8 : rot / 16 + (D - rot) / 8;
         const int heads = (q ? Hq : 0) + 2 * cache->Hkv;
         // Few tokens: a head to a thread (latency).  More: four heads to a thread, whose loads overlap and share the token's row of the
-        // table, in blocks of 128 threads (one or more tokens) and, where those are plenty, of a single warp: 16,001 tokens of 32 + 2 * 8 heads
-        // into an 8-bit cache 78 us with 128 threads, 63 with 32; 300 tokens 3.1 us with 128, 4.9 with 32
+        // table, in blocks of 128 threads (one or more tokens) and, where those are plenty, of a single warp: 32 + 2 * 8 heads, half rotated in
+        // pairs, into an 8-bit cache, 128 threads and 32: 500 tokens 3.9 and 7.7 us, 1,000 5.4 and 9.6, 2,048 12.6 and 13.6, 4,096 22.7 and 18.6, 16,001
+        // 78 and 63; all rotated into a bf16 cache, 1,000 tokens 6.2 and 6.4 us, 2,048 14.1 and 11.2, 4,096 25.2 and 20.2; 8 + 2 heads, 8,192 14.2 and 16.1
         int par, tokens = 1;
         if (T <= 128) {
             par = heads * units <= 256 ? heads : (256 + units - 1) / units;

@@ -6,7 +6,7 @@
 // the same row join by  m = max m_i,  l = sum l_i e^(m_i - m),  O = sum O_i e^(m_i - m).  Bound by memory: every key and
 // value is read once, so everything here serves to keep loads in flight.
 //
-// Work is the list of 64-key tiles of all (sequence, key-value head) entries, one after the other; CTA c of n takes tiles
+// Work is the list of tiles (16 keys for each of a CTA's warps: 64; 32 for bf16 heads of 256) of all (sequence, key-value head) entries, one after the other; CTA c of n takes tiles
 // [c T / n, (c+1) T / n): equal shares whatever the lengths are.  An entry that several CTAs share is joined from parts
 // in the workspace, in the order of the CTAs: by the last of them to arrive, in two levels, or by a second kernel where either would be much for one SM.
 //
@@ -19,9 +19,9 @@
 //            S^T's accumulators by an 8x8 transpose between lanes)
 // Query heads that share a key-value head sit side by side in the 8 (or 16) columns, so the group costs one read.
 //
-// Measured (32 query, 8 key-value heads of 128, bf16): 64 sequences of 512 to 8,192 tokens 187 us, 6.18 TB/s, 94 % of the copy rate, bound by
-// memory.  Four of up to 131,072 tokens, 64 query heads, 8-bit: 140 us, 4.96 TB/s, 76 %: 16-byte copies, conversions and the softmax of
-// twice the keys per byte keep the schedulers half busy and a warp's chain of steps is what is left.  One of 777 tokens: 7.7 us, all latency (lengths, table,
+// Measured (32 query, 8 key-value heads of 128, bf16): 64 sequences of 512 to 8,192 tokens 187 us, 6.20 TB/s, 95 % of the copy rate, bound by
+// memory.  Four of up to 131,072 tokens, 64 query heads, 8-bit: 141 us, 4.93 TB/s, 75 %: 16-byte copies, conversions and the softmax of
+// twice the keys per byte keep the schedulers half busy and a warp's chain of steps is what is left.  One of 777 tokens: 7.8 us, all latency (lengths, table,
 // keys, join).  First form (lane-wise 16-byte copies everywhere, maximum exact at every step): 301, 253 and 30 us.
 #include "ptx.cuh"
 #include "serving.cuh"

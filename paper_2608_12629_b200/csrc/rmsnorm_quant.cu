@@ -4,10 +4,13 @@
 //
 // Bound by memory, and nearly as much by issue: x and r are read once (4 bytes an element), s and q written once (3 bytes).  A row lives
 // in the registers of the threads that read it, so nothing is read twice; blocks walk over the rows with the next rows' loads in
-// flight, so a row's reductions (one or two barriers) cost no bandwidth; the arithmetic is packed, two floats to an instruction.  64
-// registers and 1,024 threads an SM: blocks of one row without the loads ahead took 25 % longer, half the threads with twice the registers 14 %.
-// Measured: 8192 x 8192 with residual and scales per 128 columns 83 us, 5.67 TB/s, 87 % of the copy rate; 16,384 x 4096 89 %; 16 x 4096
-// 2.5 us.  Rows of odd length are loaded element by element, at 30 % of the copy rate.
+// flight, so a row's reductions (one or two barriers) cost no bandwidth; the arithmetic is packed, two floats to an instruction.  Rows of
+// more than 1,024 columns have 64 registers and 1,024 threads an SM: blocks of one row without the loads ahead took 25 % longer, half the threads with twice
+// the registers 14 %.  (Shorter rows: 38 to 46 registers, 1,280 or 1,536 threads.)
+// Measured: 8192 x 8192 with residual and scales per 128 columns 83.5 us, 5.65 TB/s, 86 % of the copy rate; 16,384 x 1024 83 %; 16 x 4096
+// 2.5 us.  Above 16,384 columns four chunks and their successors do not fit 64 registers (492 bytes of spills): 2,048 x 32,768 140 us, 52 %.  Rows
+// of even length that is no multiple of 8 are loaded by pairs (4,096 x 5,122 46 us, 49 %), of odd length element by element (4,096 x 5,121
+// 112 us, 20 %).
 #include "serving.cuh"
 
 namespace cake {
