@@ -235,14 +235,14 @@ __device__ __forceinline__ bool arrive(int* counter, int others, int* flag) {
 }
 
 // An entry of many parts without a second kernel: groups of neighbouring parts are joined by the last CTA of each group, the groups' sums by the
-// last group's.  One row of 131,072 tokens beside 255 of 100, 16 heads of 256: 98 us, and 370 by a single CTA; 8 heads of 128 beside 511: 28 and 61.
+// last group's.  One row of 131,072 tokens beside 255 of 100, 16 heads of 256: 99 us, and 375 by a single CTA; 8 heads of 128 beside 511: 28 and 61.
 // (Out of line, all arguments by value: inside the kernel it made rows of 64 bytes 7 % slower)
 template <int D, int HEADS>
 __device__ __noinline__ void join_in_groups(Rows rows, float* parts, int* counters, int cta, int c0, int c1, int heads, i64 out0, float vs, int* flag) {
     constexpr int ML_AT = HEADS * D + 2 * HEADS;         // of a group's sum: beside the first part's m and l, which other threads still read
-    int step = 1;
-    while (step * step <= c1 - c0) ++step;
-    const int first = c0 + (cta - c0) / step * step, last = min(first + step - 1, c1);
+    // groups of about the square root of the parts, a power of two, at least a batch
+    const int parts_n = c1 - c0 + 1, shift = parts_n <= 64 ? 3 : parts_n <= 256 ? 4 : 5, step = 1 << shift;
+    const int first = c0 + ((cta - c0) >> shift << shift), last = min(first + step - 1, c1);
     // (a CTA may begin the last group of one entry and the first of the next)
     if (!arrive(counters + (first == c0 ? 2 : 1) * kPartCtas + first, last - first, flag)) return;
     float* const sum = parts + (2 * first + (first == c0 ? 1 : 0)) * static_cast<i64>(HEADS * (D + 4));
@@ -253,7 +253,7 @@ __device__ __noinline__ void join_in_groups(Rows rows, float* parts, int* counte
         __stcg(reinterpret_cast<float4*>(sum + h * D + d), j.acc);
         if (d == 0) __stcg(reinterpret_cast<float2*>(sum + ML_AT + 2 * h), make_float2(j.top, j.sum));
     }
-    if (!arrive(counters + c0, (c1 - c0) / step, flag)) return;
+    if (!arrive(counters + c0, (c1 - c0) >> shift, flag)) return;
     for (int i = threadIdx.x; i < heads * (D / 4); i += blockDim.x) {
         const int h = i / (D / 4), d = 4 * (i - h * (D / 4));
         Joined j;
@@ -758,6 +758,7 @@ paged_decode_kernel(const DecodeArgs a) {
             if (a.defer) {
                 if (tid == 0 && cta == c0) a.splits[atomicAdd(a.n_splits, 1)] = Split{e.b, e.g, e.run, c0, c1, {0, 0, 0}};
             } else if (c1 - c0 >= a.few) {
+                if (at + n_tiles >= hi) ptx::grid_dep_launch();      // the CTA's last: the next kernel may start beside the join
                 join_in_groups<D, HEADS>(a.rows, a.parts, a.counters, static_cast<int>(cta), c0, c1, heads, out0, vs, &last_flag);
             } else if (arrive(a.counters + c0, c1 - c0, &last_flag)) {
                 for (int i = tid; i < heads * (D / 4); i += THREADS) {
@@ -807,8 +808,8 @@ int launch(DecodeArgs& a, const DeviceInfo& di, cudaStream_t s) {
     // Whether a second kernel joins the parts has to be said here, where the lengths are not known: from the parts of an entry if all are about as
     // long, no more than the page table and the window leave room for.  Behind short rows it is 1.2 - 1.8 us for nothing (one row of 777 tokens, a
     // table for 16,384: 9.2 us with it, 7.7 without).  Two levels in this kernel lose less than that where a CTA has a thread for each four values of
-    // a part (32 query, 8 key-value heads of 128, one row of 4,000 tokens 11.4 -> 12.3 us, of 30,000 30.4 -> 31.8; 4 heads to a single
-    // key-value head 17.3 -> 14.1), but more in several passes (8 heads, 4,000 tokens: 9.2 and 10.1; 16 heads, 30,000: 19.1 and 24.9), from
+    // a part (32 query, 8 key-value heads of 128, one row of 4,000 tokens 11.4 -> 11.3 us, of 30,000 30.4 -> 31.0; 4 heads to a single
+    // key-value head 17.2 -> 13.6), but more in several passes (8 heads, 4,000 tokens: 9.2 and 10.1; 16 heads, 30,000: 19.1 and 24.9), from
     // 64 KiB of parts on (about 2 us of one SM's reads).  One CTA joins up to `few` parts of an entry by itself: batches of eight, 0.6 us each and pass;
     // two levels are an arrival (about two batches) more
     const i64 entries = static_cast<i64>(a.B) * a.c.Hkv * a.chunks;
