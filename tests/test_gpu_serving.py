@@ -913,7 +913,8 @@ def test_keys_and_values_of_different_stride_orders(kv):
     assert torch.equal(out, cake.cake_paged_decode(q, plain, table, n)[0])
 
 
-@pytest.mark.parametrize("B,Hq,Hkv,D,kv,start", [(16, 8, 2, 64, BF16, 40), (3, 16, 1, 128, E4M3, 9000), (150, 4, 4, 64, E4M3, 3)])
+@pytest.mark.parametrize("B,Hq,Hkv,D,kv,start", [(16, 8, 2, 64, BF16, 40), (3, 16, 1, 128, E4M3, 9000), (150, 4, 4, 64, E4M3, 3),
+                                                 (2, 4, 1, 128, BF16, 20000)])
 def test_calls_back_to_back_give_the_bits_of_calls_one_by_one(B, Hq, Hkv, D, kv, start):
     """Every kernel may start before the one ahead of it ends: steps of a layer, each call writing what calls ahead of it still read, over the same few
     buffers; 60 steps with nothing between the launches, and as a graph, against the same steps with a wait after every call."""
