@@ -4,7 +4,11 @@
  *   rmsnorm_quant   residual addition, root-mean-square norm, 8-bit output with scales;
  *   gemm_fp8        product of two 8-bit matrices with scales per 128-column block (and 128 x 128 block of the weights);
  *   kv_append       rotation of queries and keys by position, keys and values written to a paged cache;
- *   paged_decode    attention of one new token per sequence over the paged cache.
+ *   qk_norm_append  the same with a norm of each query and key head ahead of the rotation;
+ *   kv_read         cached keys and values read back by slots;
+ *   paged_decode    attention of one new token per sequence over the paged cache;
+ *   paged_chunk     attention of a chunk of new tokens per sequence over the paged cache;
+ *   prompt_attention  attention of whole prompts, packed one behind the other.
  * The paper names a grouped-query decode and a block-scaled 8-bit product among its other kernels, without their source or interface;
  * these calls follow neither.
  *
@@ -141,6 +145,83 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
                                const int* seq_lens, long long lens_stride, long long lens_head_stride, long long B, int Hq,
                                float scale, int window, cake_bf16* out, float* out_lse, void* ws, size_t ws_bytes,
                                cake_stream_t stream);
+
+/*
+ * Attention of many query tokens.  A sequence b has the query tokens starts[b] up to starts[b + 1] of the T that lie one behind the
+ * other; with n of them and L keys, token i is at position p = L - n + i among the keys and sees
+ *   causal:      the keys up to its own position, [0, p + 1)
+ *   window w>0:  the last w of those, [max(0, p - w + 1), p + 1)
+ *   otherwise:   all L keys
+ *   out[token][h] = sum_t p_t v_t,  p = softmax over the keys t that it sees of  scale * q[token][h] . k_t,
+ * query head h reads key-value head h / (Hq / Hkv).
+ *   q          [T][Hq][D] bf16, tokens q_stride apart, heads q_head_stride apart, in
+ *   starts     [B + 1] int32, device, in: 0 <= starts[b] <= starts[b + 1] <= T; a sequence for which that does not hold is left out
+ *              (device status CAKE_ERR_BAD_INDEX).  Tokens of no sequence are left as they were in out and out_lse
+ *   out        [T][Hq][D] bf16 contiguous, out;   out_lse [T][Hq] fp32 contiguous, out, may be NULL: log of the sum of exponentials
+ *   ws         at least cake_attention_workspace_bytes(Hq, Hkv, D) bytes: any number of sequences and tokens
+ * A token that sees nothing (or nothing that weighs anything) gives zeros, and -inf in out_lse.  Keys and values that a token does
+ * not see do not touch its row, infinities and NaN among them (a row that meets such values beside its own is computed again, key by
+ * key: slow, and right).  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are
+ * rounded to bf16 for the product with the values (8-bit caches: to f16), their sum is not.  D: 64, 96, 128 or 256
+ * (CAKE_ERR_UNSUPPORTED otherwise).  Pointers to q, k and v are 16-byte aligned and their strides multiples of 8 elements, at least D
+ * (CAKE_ERR_ALIGN, CAKE_ERR_SHAPE); the stride of a dimension of one element is not looked at.  Two launches.  The result depends
+ * on the inputs and their sizes, not on timing.
+ */
+CAKE_API int cake_attention_workspace_bytes(int Hq, int Hkv, int D, size_t* out_bytes);
+/*
+ * Packed prompts: keys and values lie one sequence behind the other.
+ *   k, v       [Tk][Hkv][D] bf16, in, strides as for q
+ *   k_starts   [B + 1] int32, device, in: as starts, of the keys (<= Tk); NULL: starts (Tk >= T then, or sequences are left out)
+ *   flags      CAKE_ATTENTION_CAUSAL; window needs it (CAKE_ERR_UNSUPPORTED)
+ */
+enum { CAKE_ATTENTION_CAUSAL = 1 };
+CAKE_API int cake_prompt_attention(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_bf16* k, long long k_stride,
+                                   long long k_head_stride, const cake_bf16* v, long long v_stride, long long v_head_stride,
+                                   const int* starts, const int* k_starts, long long B, long long T, long long Tk, int Hq, int Hkv, int D,
+                                   float scale, int window, cake_bf16* out, float* out_lse, void* ws, size_t ws_bytes,
+                                   cake_stream_t stream, unsigned flags);
+/*
+ * A chunk of new tokens per sequence over a paged cache that holds their keys and values already (causal).
+ *   page_table, seq_lens   as for cake_paged_decode: seq_lens counts the chunk's tokens too (they are the last ones); per key-value
+ *              head with table_head_stride, lens_head_stride.  Only entries of keys that some token of the chunk's block of
+ *              neighbouring tokens sees are read, and no memory of other keys.  A page outside [0, num_pages): its keys are left
+ *              out, device status CAKE_ERR_BAD_INDEX; a length beyond max_pages * page_size is cut to it (likewise)
+ */
+CAKE_API int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_stride, const cake_paged_cache* cache,
+                              const int* page_table, long long table_stride, long long table_head_stride, int max_pages,
+                              const int* seq_lens, long long lens_stride, long long lens_head_stride, const int* starts, long long B,
+                              long long T, int Hq, float scale, int window, cake_bf16* out, float* out_lse, void* ws, size_t ws_bytes,
+                              cake_stream_t stream);
+
+/*
+ * The norm of each query and key head, the rotation of cake_kv_append, and its write to the cache, in one pass:
+ *   y = x * rsqrt(mean over the head's D elements of x^2 + eps) * weight, then rotated as there.  Values are neither.  Arithmetic
+ * in 32 bits, one rounding at the store.
+ *   q          [T][Hq][D] bf16, tokens q_stride apart, heads D apart, in;  k, v [T][Hkv][D] likewise
+ *   q_weight, k_weight  [D] bf16, in, may be NULL (all ones)
+ *   out_q      [T][Hq][D] bf16 contiguous, out (may be q's buffer where that is contiguous too)
+ *   out_k      [T][Hkv][D] bf16 contiguous, out, may be NULL (may be k's buffer likewise): the keys beside the cache, of tokens with a
+ *              negative slot too, for the attention of a prompt whose keys need not be read back
+ * cache, slots, positions, cos_sin, rot, flags and what an index out of range does: as for cake_kv_append.  A position out of range
+ * leaves out_q and out_k of that token as they were.  ws: CAKE_SERVING_HEADER_BYTES bytes.
+ */
+CAKE_API int cake_qk_norm_append(const cake_paged_cache* cache, const cake_bf16* q, long long q_stride, int Hq, const cake_bf16* k,
+                                 long long k_stride, const cake_bf16* v, long long v_stride, const cake_bf16* q_weight,
+                                 const cake_bf16* k_weight, float eps, cake_bf16* out_q, cake_bf16* out_k, const long long* slots,
+                                 const int* positions, const float* cos_sin, long long max_positions, int rot, long long T, void* ws,
+                                 size_t ws_bytes, cake_stream_t stream, unsigned flags);
+
+/*
+ * Reads keys and values of N tokens back from their slots: out[n][h] = bf16(cache[slots[n]][h] * scale[h]) (a bf16 cache's as they are).
+ *   slots      [N] int64, in, any order, repeats allowed.  A negative slot gives zeros; a slot beyond the cache likewise, and the
+ *              device status becomes CAKE_ERR_BAD_INDEX
+ *   out_k, out_v  bf16, out, either may be NULL: token n and head h at n * out_stride + h * out_head_stride, D contiguous elements
+ *              (tokens outermost, or a matrix [N][D] for each head, as the clustering takes them).  16-byte aligned, strides
+ *              multiples of 8 elements and at least D
+ * ws: CAKE_SERVING_HEADER_BYTES bytes.
+ */
+CAKE_API int cake_kv_read(const cake_paged_cache* cache, const long long* slots, long long N, cake_bf16* out_k, cake_bf16* out_v,
+                          long long out_stride, long long out_head_stride, void* ws, size_t ws_bytes, cake_stream_t stream);
 
 #ifdef __cplusplus
 }

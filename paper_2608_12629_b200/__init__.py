@@ -14,7 +14,8 @@ from .binding import (  # noqa: F401
 )
 from .sharded import cake_kmeans_lloyd_sharded, shard_rows  # noqa: F401
 from .serving import (  # noqa: F401
-    CAKE_APPEND_INTERLEAVED, CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES, CAKE_GEMM_OUT_FP32, CAKE_KV_BF16, CAKE_KV_E4M3, CAKE_RMSNORM_NONE, CAKE_SERVING_HEADER_BYTES,
-    SERVING_EXPORTS, PagedCache, alloc_append_workspace, alloc_decode_workspace, alloc_gemm_workspace, cake_gemm_fp8,
-    cake_gemm_fp8_workspace_bytes, cake_kv_append, cake_paged_decode, cake_paged_decode_workspace_bytes, cake_rmsnorm_quant,
+    CAKE_APPEND_INTERLEAVED, CAKE_ATTENTION_CAUSAL, CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES, CAKE_GEMM_OUT_FP32, CAKE_KV_BF16, CAKE_KV_E4M3, CAKE_RMSNORM_NONE, CAKE_SERVING_HEADER_BYTES,
+    SERVING_EXPORTS, PagedCache, alloc_append_workspace, alloc_attention_workspace, alloc_decode_workspace, alloc_gemm_workspace,
+    cake_attention_workspace_bytes, cake_gemm_fp8, cake_gemm_fp8_workspace_bytes, cake_kv_append, cake_kv_read, cake_paged_chunk, cake_paged_decode,
+    cake_paged_decode_workspace_bytes, cake_prompt_attention, cake_qk_norm_append, cake_rmsnorm_quant,
 )

@@ -1,0 +1,1277 @@
+// Attention of many query tokens: softmax(scale Q K^T) V, keys and values packed by sequence or in a paged cache.
+//
+//   out_i = sum_t exp(x_it - m_i) v_t / sum_t exp(x_it - m_i),   x_it = scale * q_i . k_t  over the keys t that token i sees
+//
+// One pass over the keys with the running maximum m, sum l and weighted sum O of a softmax.  Both products run on the tensor cores:
+//   S = Q K^T   [128 rows x 128 keys], Q and K from shared memory, S in tensor memory
+//   O += P V    P (16-bit, over S's columns in tensor memory) times V from shared memory, O in tensor memory
+// and the threads between them have a row of S each (tensor memory's lanes): no exchange between threads for maximum and sum.
+//
+// Rows are (token, query head of the key-value head's group) pairs, tokens outermost, so a key-value head is read once for its
+// whole group, whatever the group's size; a tile of 128 rows holds 128 / group tokens.
+//
+// A CTA works on two tiles of rows at a time (heads of 256: one, its O fills tensor memory), so that the tensor cores multiply for
+// one while the other's exponentials are taken: both need about as long (128 x 128 scores: 1,024 clocks of two products at
+// D = 128, 1,024 clocks of 2^x).  Two tiles are either
+//   different rows that share each tile of keys (DUAL), or, where an item has no more than 128 rows,
+//   the same rows over every other tile of keys (ALT), joined at the end.
+//
+// Work is the list of all tiles of keys of all items (sequence, key-value head, block of rows), one after the other; CTA c of n
+// takes the c-th of n equal shares, whatever the lengths are, moved to the end of an item where that is near.  Items that several
+// CTAs share are joined from parts in the workspace by a second kernel, in the order of the CTAs.
+//
+// Warps: two warpgroups of softmax rows, one that loads pages (paged caches only), one with a scheduler, a TMA and an MMA thread.
+#pragma once
+#include "ptx.cuh"
+#include "serving.cuh"
+
+namespace cake {
+namespace serving {
+
+int check_cache(const cake_paged_cache* c);   // kv_append.cu
+
+namespace attn {
+
+constexpr int KT = 128;                        // keys of a tile
+constexpr int MT = 128;                        // rows of a tile
+constexpr int MOST_CTAS = 148;                 // that the workspace has room for parts of (two each)
+constexpr int SEGS = 4;                        // segments of work that the scheduler is ahead
+constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags are kept
+constexpr int OVERHEAD = 1;                    // tiles of keys that an item's start and end cost
+constexpr int SNAP = 2;                        // a share's end within so many tiles of an item's is moved there (> OVERHEAD)
+constexpr int MIN_SHARE = 2;                   // tiles
+static_assert(SNAP > OVERHEAD, "a part has at least one tile of keys");
+constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr float NEG_INF = -INFINITY;
+
+enum Kind { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
+
+// An item that several CTAs share: `cta` has the beginning, the ones up to c1 the rest; count = 0: none.
+struct Split {
+    i64 tok;                                   // first token among all queries'
+    int head0, heads, ntok, c1, valid, g;
+};
+
+struct Args {
+    cake_paged_cache c;                        // paged
+    const cake_bf16 *q, *k, *v;
+    const int *starts, *k_starts;              // of the sequences' queries; of their keys (packed)
+    const int *table, *lens;                   // paged
+    cake_bf16* out;
+    float* lse;
+    int* status;
+    float* parts;
+    Split* splits;
+    i64 T, Tk, q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+    i64 table_stride, table_head_stride, lens_stride, lens_head_stride;
+    i64 entries;                               // sequences * key-value heads * runs
+    int B, Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
+    int max_pages, window;
+    float scale_log2;                          // |scale| log2 e
+    bool negative, causal, wide;               // sign of the scale; 16-byte stores of out
+};
+
+// A share of an item: what every role of a CTA is told of it.
+struct Seg {
+    i64 tok;                                   // first token among all queries'
+    i64 k0;                                    // first key among all keys (packed); the table's row (paged)
+    int g, head0, heads, ntok, pos, klen, ja, jb;   // pos: position of the first token; tiles of keys [ja, jb)
+    int part;                                  // slot among the parts, -1: the whole item
+    int negative, done;
+};
+
+template <int D_, int KIND_>
+struct Traits {
+    static constexpr int D = D_;
+    static constexpr int KIND = KIND_;
+    static constexpr bool PAGED = KIND != PACKED, F16 = KIND == PAGED_E4M3;
+    static constexpr int TILES = D == 256 ? 1 : 2;
+    static constexpr int NU = D == 256 ? 2 : 1;              // units of 128 columns that a tile of keys is loaded in
+    static constexpr int DU = D / NU;
+    static constexpr int SLABS = (DU + 63) / 64;             // of 64 columns: 128-byte rows, 128-byte swizzle
+    static constexpr uint32_t SLAB = MT * 128;
+    static constexpr uint32_t UNIT = SLABS * SLAB;
+    static constexpr int WARPS_SM = 4 * TILES, WARPS_LD = PAGED ? 4 : 0;
+    static constexpr int WARP_SCHED = WARPS_SM + WARPS_LD, WARP_TMA = WARP_SCHED + 1, WARP_MMA = WARP_SCHED + 2;
+    static constexpr int WARPS = WARP_SCHED + 4, THREADS = 32 * WARPS;
+    static constexpr uint32_t Q_BYTES = TILES * NU * UNIT;
+    static constexpr int STAGES = DU == 64 ? 8 : 4;
+    // registers: what a block starts with (65,536 / threads), shared out again between the warpgroups
+    static constexpr bool SPLIT_REGS = TILES == 2 || PAGED;
+    static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 184 : 232) : 232;
+    static constexpr int REGS_LD = TILES == 2 ? 96 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 40) : 80;
+    static constexpr int REGS_START = 65536 / THREADS / 8 * 8 > 255 ? 255 : 65536 / THREADS / 8 * 8;
+    static_assert(!SPLIT_REGS || TILES * REGS_SM + (PAGED ? REGS_LD : 0) + REGS_AUX <= REGS_START * (THREADS / 128), "registers of the block");
+    static constexpr int PART_ROWS = TILES * MT;
+    static constexpr i64 PART = static_cast<i64>(PART_ROWS) * (D + 2);       // floats
+};
+
+struct __align__(16) Ctrl {
+    uint64_t seg_full[SEGS], seg_empty[SEGS];
+    uint64_t q_full[2], q_empty[2], q_conv[2];
+    uint64_t kv_full[8], kv_empty[8];
+    uint64_t s_full[2], p_ready[2], o_done[2], o_free[2], x_full, drained;
+    Seg seg[SEGS];
+    i64 sums[16];
+    uint4 flags[FLAGS_AHEAD];                  // a bit for each key of a tile: its page exists
+    float2 ml[2][MT];                          // maximum and sum of the second tile (ALT)
+    float q_scale[2][MT];                      // powers of two that 16-bit queries were divided by
+    uint32_t tmem;
+    int abort_flag;
+};
+
+template <class T>
+constexpr uint32_t smem_bytes() { return 1024 + T::Q_BYTES + T::STAGES * T::UNIT + sizeof(Ctrl); }
+
+__device__ __forceinline__ bool aborted(Ctrl* ctrl) { return *reinterpret_cast<volatile int*>(&ctrl->abort_flag) != 0; }
+// the same for all lanes of a warp
+__device__ __forceinline__ bool any_aborted(Ctrl* ctrl) { return __any_sync(0xffffffffu, aborted(ctrl)); }
+__device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* ctrl, int* status) {
+    const uint32_t addr = ptx::smem_u32(bar);
+    if (ptx::mbar_try_wait(addr, parity & 1)) return;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (!ptx::mbar_try_wait_hint(addr, parity & 1, 20000)) {
+        if (aborted(ctrl)) return;
+        if (ptx::globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+            *reinterpret_cast<volatile int*>(&ctrl->abort_flag) = 1;
+            atomicCAS(status, CAKE_OK, CAKE_ERR_TIMEOUT);
+            return;
+        }
+    }
+}
+__device__ __forceinline__ void arrive(uint64_t* bar) { ptx::mbar_arrive(ptx::smem_u32(bar)); }
+__device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flushed to zero
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// four e4m3 values to two pairs of f16: exact
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    const uint16_t a = static_cast<uint16_t>(w & 0xffffu), b = static_cast<uint16_t>(w >> 16);
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"(a));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(b));
+}
+// (a, b) * c - d
+__device__ __forceinline__ void scale_sub2(float& a, float& b, float c, float minus_d) {
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(minus_d));
+}
+__device__ __forceinline__ void add2(float2& s, float a, float b) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(s.x), "+f"(s.y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {      // zeros where !ok
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ------------------------------------------------------------------------------------------------- who sees what
+__device__ __forceinline__ int first_key(const Args& a, int pos, int klen) {
+    return a.window > 0 && pos >= a.window ? min(pos - a.window + 1, klen) : 0;
+}
+__device__ __forceinline__ int end_key(const Args& a, int pos, int klen) { return a.causal ? max(0, min(pos + 1, klen)) : klen; }
+
+// An entry: a sequence's new tokens, a key-value head and a run of its query heads.
+struct Entry {
+    i64 q0, k0;
+    int qlen, klen, g, run;
+};
+template <bool PAGED>
+__device__ __forceinline__ Entry entry_of(const Args& a, i64 e, bool report) {
+    Entry n;
+    const int per = a.Hkv * a.runs;
+    const int b = static_cast<int>(e / per), r = static_cast<int>(e - static_cast<i64>(b) * per);
+    n.g = r / a.runs, n.run = r - n.g * a.runs;
+    const int s0 = a.starts[b], s1 = a.starts[b + 1];
+    bool bad = s0 < 0 || s1 < s0 || s1 > a.T;
+    n.q0 = s0, n.qlen = bad ? 0 : s1 - s0;
+    if (PAGED) {
+        n.k0 = b * a.table_stride + n.g * a.table_head_stride;
+        const i64 room = min(static_cast<i64>(a.max_pages) * a.c.page_size, static_cast<i64>(INT_MAX - 2 * KT));
+        i64 len = a.lens[b * a.lens_stride + n.g * a.lens_head_stride];
+        if (len > room) bad = true, len = room;
+        n.klen = static_cast<int>(len < 0 ? 0 : len);
+    } else {
+        const int k0 = a.k_starts[b], k1 = a.k_starts[b + 1];
+        const bool wrong = k0 < 0 || k1 < k0 || k1 > a.Tk;
+        bad |= wrong;
+        n.k0 = wrong ? 0 : k0, n.klen = wrong ? 0 : k1 - k0;
+    }
+    if (bad && report) raise_bad_index(a.status);
+    return n;
+}
+// tiles of keys [ja, jb) that tokens [tok, tok + n) of an entry see
+__device__ __forceinline__ void tiles_of(const Args& a, int pos, int n, int klen, int& ja, int& jb) {
+    ja = first_key(a, pos, klen) / KT;
+    jb = (end_key(a, pos + n - 1, klen) + KT - 1) / KT;
+    if (jb < ja) jb = ja;
+}
+template <int TILES>
+__device__ __forceinline__ int blocks_of(const Args& a, int qlen) { return (qlen + TILES * a.tokens - 1) / (TILES * a.tokens); }
+template <int TILES>
+__device__ __forceinline__ int cost_of(const Args& a, int qlen, int klen, int block) {
+    const int per = TILES * a.tokens, tok = block * per;
+    int ja, jb;
+    tiles_of(a, klen - qlen + tok, min(per, qlen - tok), klen, ja, jb);
+    return jb - ja + OVERHEAD;
+}
+// the cost of the lane's entry (lanes without one: qlen = 0); long ones are added up by the whole warp
+template <int TILES>
+__device__ __forceinline__ i64 entry_cost(const Args& a, int qlen, int klen) {
+    const int lane = threadIdx.x & 31;
+    const int blocks = blocks_of<TILES>(a, qlen);
+    i64 sum = 0;
+    if (blocks <= 4)
+        for (int i = 0; i < blocks; ++i) sum += cost_of<TILES>(a, qlen, klen, i);
+    for (unsigned todo = __ballot_sync(0xffffffffu, blocks > 4); todo; todo &= todo - 1) {
+        const int who = __ffs(todo) - 1;
+        const int ql = __shfl_sync(0xffffffffu, qlen, who), kl = __shfl_sync(0xffffffffu, klen, who), n = __shfl_sync(0xffffffffu, blocks, who);
+        i64 s = 0;
+        for (int i = lane; i < n; i += 32) s += cost_of<TILES>(a, ql, kl, i);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == who) sum = s;
+    }
+    return sum;
+}
+__device__ __forceinline__ i64 inclusive_scan(i64 v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const i64 u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+// a share's end p tiles into an item of this cost, moved to the item's ends where they are near
+__device__ __forceinline__ int snap(int p, int cost) { return p <= SNAP ? 0 : cost - p <= SNAP ? cost : p; }
+
+// ------------------------------------------------------------------------------------------------------ scheduler
+// One warp: finds the CTA's share of the list and tells the others of its segments.
+template <class T>
+__device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl) {
+    constexpr int TILES = T::TILES;
+    const int lane = threadIdx.x & 31;
+    const unsigned all = 0xffffffffu;
+    i64 total = 0;
+#pragma unroll
+    for (int w = 0; w < T::WARPS; ++w) total += ctrl->sums[w];
+    const i64 fit = total / MIN_SHARE;
+    const int n = static_cast<int>(fit < 1 ? 1 : fit < static_cast<i64>(gridDim.x) ? fit : static_cast<i64>(gridDim.x));
+    const int cta = blockIdx.x;
+    uint32_t count = 0;      // segments so far
+    auto post = [&](const Seg& s) {
+        const int slot = count % SEGS;
+        wait_bar(&ctrl->seg_empty[slot], (count / SEGS + 1) & 1, ctrl, a.status);
+        if (any_aborted(ctrl)) return;      // (others may still read the place)
+        if (lane == 0) {
+            ctrl->seg[slot] = s;
+            arrive(&ctrl->seg_full[slot]);
+        }
+        ++count;
+    };
+    Split split = {};
+    if (cta < n && total > 0) {
+        const i64 x0 = total * cta / n, x1 = cta == n - 1 ? total : total * (cta + 1) / n;
+        // the entry that x0 is in
+        i64 before = 0, e = 0, e_end = 0;
+        for (int w = 0; w < T::WARPS; ++w) {
+            const i64 s = ctrl->sums[w];
+            if (x0 < before + s) {
+                e = a.entries * w / T::WARPS, e_end = a.entries * (w + 1) / T::WARPS;
+                break;
+            }
+            before += s;
+        }
+        for (;; e += 32) {
+            Entry en = {};
+            if (e + lane < e_end) en = entry_of<T::PAGED>(a, e + lane, false);
+            const i64 cost = entry_cost<TILES>(a, en.qlen, en.klen);
+            const i64 upto = inclusive_scan(cost);
+            const unsigned hit = __ballot_sync(all, x0 < before + upto);
+            if (hit) {
+                const int who = __ffs(hit) - 1;
+                e += who;
+                before += __shfl_sync(all, upto - cost, who);
+                break;
+            }
+            before += __shfl_sync(all, upto, 31);
+            if (e + 32 >= e_end) break;      // (cannot be: the sums say that it is here)
+        }
+        Entry en = entry_of<T::PAGED>(a, e, false);
+        int blocks = blocks_of<TILES>(a, en.qlen), block = 0;
+        for (; block < blocks; block += 32) {      // the item of the entry
+            const i64 cost = block + lane < blocks ? cost_of<TILES>(a, en.qlen, en.klen, block + lane) : 0;
+            const i64 upto = inclusive_scan(cost);
+            const unsigned hit = __ballot_sync(all, x0 < before + upto);
+            if (hit) {
+                const int who = __ffs(hit) - 1;
+                block += who;
+                before += __shfl_sync(all, upto - cost, who);
+                break;
+            }
+            before += __shfl_sync(all, upto, 31);
+        }
+        int start = -1;
+        while (x1 > before && block < blocks) {
+            const int per = TILES * a.tokens, tok = block * per, ntok = min(per, en.qlen - tok);
+            const int pos = en.klen - en.qlen + tok;
+            int ja, jb;
+            tiles_of(a, pos, ntok, en.klen, ja, jb);
+            const int cost = jb - ja + OVERHEAD;
+            if (start < 0) start = snap(static_cast<int>(x0 - before), cost);      // the share's first item
+            const int end = x1 >= before + cost ? cost : snap(static_cast<int>(x1 - before), cost);
+            if (start < end) {
+                Seg s;
+                s.tok = en.q0 + tok, s.k0 = en.k0, s.g = en.g;
+                s.head0 = en.g * a.G + en.run * a.heads, s.heads = min(a.heads, a.G - en.run * a.heads);
+                s.ntok = ntok, s.pos = pos, s.klen = en.klen;
+                s.ja = start ? ja + start - OVERHEAD : ja;
+                s.jb = end == cost ? jb : ja + end - OVERHEAD;
+                s.part = start == 0 && end == cost ? -1 : 2 * cta + (start == 0 ? 1 : 0);
+                s.negative = a.negative;
+                if (T::F16 && a.c.k_scale && a.c.k_scale[en.g] < 0.f) s.negative ^= 1;
+                s.done = 0;
+                post(s);
+                if (any_aborted(ctrl)) break;
+                if (start == 0 && end < cost) {      // the CTAs behind this one have the rest
+                    int c1 = cta;
+                    for (int c = cta + 1; c < n; c += 32) {
+                        const i64 x = c + lane < n ? total * (c + lane) / n : total;
+                        const unsigned in = __ballot_sync(all, before + cost - x > SNAP);
+                        c1 += __popc(in);
+                        if (in != all) break;
+                    }
+                    split.tok = s.tok, split.head0 = s.head0, split.heads = s.heads, split.ntok = ntok, split.c1 = c1, split.g = en.g;
+                    split.valid = 1;
+                }
+            }
+            if (end < cost) break;
+            before += cost;
+            start = 0;
+            if (++block == blocks) {
+                block = 0, blocks = 0;
+                while (blocks == 0 && ++e < a.entries) {
+                    en = entry_of<T::PAGED>(a, e, false);
+                    blocks = blocks_of<TILES>(a, en.qlen);
+                }
+            }
+        }
+    }
+    if (lane == 0) a.splits[cta] = split;
+    Seg last = {};
+    last.done = 1;
+    post(last);
+}
+
+// The roles' side of it: reads the next segment (whole warps, or one thread with `alone`).  False: no more.
+__device__ __forceinline__ bool next_seg(const Args& a, Ctrl* ctrl, uint32_t& count, Seg& s, bool alone) {
+    const int slot = count % SEGS;
+    wait_bar(&ctrl->seg_full[slot], (count / SEGS) & 1, ctrl, a.status);
+    if (alone ? aborted(ctrl) : any_aborted(ctrl)) return false;
+    s = ctrl->seg[slot];
+    if (!alone) __syncwarp();
+    if (alone || (threadIdx.x & 31) == 0) arrive(&ctrl->seg_empty[slot]);
+    ++count;
+    return !s.done;
+}
+
+// the tiles of keys of a segment that its row tile t sees (DUAL), or all of them
+template <class T>
+__device__ __forceinline__ bool is_dual(const Args& a, const Seg& s) { return T::TILES == 2 && s.ntok > a.tokens; }
+__device__ __forceinline__ void range_of(const Args& a, const Seg& s, bool dual, int t, int& ra, int& rb) {
+    ra = s.ja, rb = s.jb;
+    if (dual) {
+        int ja, jb;
+        const int first = t * a.tokens;
+        tiles_of(a, s.pos + first, min(a.tokens, s.ntok - first), s.klen, ja, jb);
+        ra = max(ra, ja), rb = min(rb, jb);
+        if (rb < ra) rb = ra;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------ rows
+// A row whose O holds something that is not finite: if that comes from values that the row does not see (they weigh nothing, but
+// zero times infinity is NaN), the row is computed again without them, key by key.  Returns false where nothing has to be mended.
+struct RowAt {
+    i64 row;                  // of out and lse: token * Hq + head
+    const cake_bf16* q;
+    int k0, k1;               // the keys that it sees in this segment
+    int from, to;             // the keys that were multiplied
+    int g, part_row, part;
+    i64 base;                 // Seg::k0
+};
+template <class T>
+__device__ __forceinline__ float key_at(const Args& a, const void* p, int d) {
+    if (T::F16) {
+        uint32_t lo, hi;
+        e4m3_to_f16(static_cast<const cake_e4m3*>(p)[d], lo, hi);
+        return __half2float(__ushort_as_half(static_cast<unsigned short>(lo & 0xffff)));
+    }
+    return bf16_f(static_cast<const cake_bf16*>(p)[d]);
+}
+// where a key and its value are; false: nowhere
+template <class T>
+__device__ __forceinline__ bool locate(const Args& a, const RowAt& r, int key, const void*& k, const void*& v) {
+    if (T::PAGED) {
+        const int page = a.table[r.base + key / a.c.page_size];
+        if (page < 0 || page >= a.c.num_pages) return false;
+        const i64 off = key % a.c.page_size, size = T::F16 ? 1 : 2;
+        k = static_cast<const char*>(a.c.k) + (page * a.c.k_page_stride + off * a.c.k_token_stride + r.g * a.c.k_head_stride) * size;
+        v = static_cast<const char*>(a.c.v) + (page * a.c.v_page_stride + off * a.c.v_token_stride + r.g * a.c.v_head_stride) * size;
+    } else {
+        if (r.base + key >= a.Tk) return false;
+        k = a.k + (r.base + key) * a.k_stride + r.g * a.k_head_stride;
+        v = a.v + (r.base + key) * a.v_stride + r.g * a.v_head_stride;
+    }
+    return true;
+}
+template <class T>
+__device__ __noinline__ bool mend_row(const Args& a, RowAt r, float c, float top, float vs) {
+    constexpr int D = T::D;
+    const void *k = nullptr, *v = nullptr;
+    bool wrong = false;
+    for (int key = r.from; key < r.to && !wrong; ++key) {
+        if (key >= r.k0 && key < r.k1) {
+            key = r.k1 - 1;
+            continue;
+        }
+        if (!locate<T>(a, r, key, k, v)) continue;
+        for (int d = 0; d < D; ++d) wrong |= !isfinite(key_at<T>(a, v, d));
+    }
+    if (!wrong) return false;
+    float o[D], l = 0.f;
+    for (int d = 0; d < D; ++d) o[d] = 0.f;
+    for (int key = r.k0; key < r.k1; ++key) {
+        if (!locate<T>(a, r, key, k, v)) continue;
+        float dot = 0.f;
+        for (int d = 0; d < D; ++d) dot = fmaf(bf16_f(r.q[d]), key_at<T>(a, k, d), dot);
+        const float p = ex2(fmaf(dot, c, -top));
+        l += p;
+        for (int d = 0; d < D; ++d) o[d] = fmaf(p, key_at<T>(a, v, d), o[d]);
+    }
+    if (r.part < 0) {
+        const float f = l == 0.f ? 0.f : vs / l;
+        for (int d = 0; d < D; ++d) a.out[r.row * D + d] = to_bf16(o[d] * f);
+        if (a.lse) a.lse[r.row] = (top + log2f(l)) * LN2;
+    } else {
+        float* const to = a.parts + r.part * T::PART;
+        for (int d = 0; d < D; ++d) to[static_cast<i64>(r.part_row) * D + d] = o[d];
+        to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row] = top, to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row + 1] = l;
+    }
+    return true;
+}
+
+// Warpgroup t of softmax rows: thread r has row r of the tile.
+template <class T>
+__device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t* q_smem, uint32_t tmem, int t) {
+    constexpr int D = T::D;
+    // What is subtracted from the scores: LIFT below their maximum, which it follows when it lies SLACK behind (a smaller step would
+    // rescale O more often than it gains).  bf16 weights: any range will do.  f16 weights (8-bit values, which widen to f16 exactly): the
+    // heaviest is 2^11 to 2^15, so 11 bits are held down to 2^-25 of it
+    constexpr float LIFT = T::F16 ? 11.f : 0.f, SLACK = T::F16 ? 4.f : 8.f;
+    const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
+    const uint32_t t_lane = tmem + (static_cast<uint32_t>(r & 96) << 16);
+    const int tok = r / a.heads, h = r - tok * a.heads;
+    uint32_t segs = 0, s_count[2] = {0, 0}, o_count[2] = {0, 0}, q_count[2] = {0, 0}, x_count = 0, tiles = 0;
+    Seg s;
+    while (next_seg(a, ctrl, segs, s, false)) {
+        const bool dual = is_dual<T>(a, s);
+        int ra, rb;
+        range_of(a, s, dual, t, ra, rb);
+        const bool alt = T::TILES == 2 && !dual;
+        const int step = alt ? 2 : 1, first = alt ? ra + t : ra;
+        const int n_mine = first < rb ? (rb - first + step - 1) / step : 0;
+        const int my_tok = (dual ? t * a.tokens : 0) + tok;                 // of the segment's tokens
+        const bool valid = tok < a.tokens && my_tok < s.ntok && h < s.heads;
+        const int pos = s.pos + my_tok;
+        // (rows that are none see what the last one does: their scores are computed, but go nowhere)
+        const int k0 = first_key(a, pos, s.klen), k1 = end_key(a, pos, s.klen);
+        const int tile_first = s.pos + (dual ? t * a.tokens : 0);
+        const int tile_last = s.pos + min(s.ntok, (dual ? (t + 1) * a.tokens : s.ntok)) - 1;
+        const int inner0 = first_key(a, tile_last, s.klen), inner1 = end_key(a, tile_first, s.klen);   // every row sees [inner0, inner1)
+        float c = a.scale_log2;
+        if (T::F16) {
+            if (a.c.k_scale) c *= fabsf(a.c.k_scale[s.g]);
+            // queries to f16, in place: divided by a power of two that brings a row's largest to [1, 2)
+            const int qt = dual ? t : 0;
+            const bool used = dual ? n_mine > 0 : s.jb > s.ja;
+            if (used && (dual || t == 0)) {
+                wait_bar(&ctrl->q_full[qt], q_count[qt], ctrl, a.status);
+                uint8_t* const row = q_smem + qt * (T::NU * T::UNIT) + r * 128;
+                float most = 0.f;
+#pragma unroll 1
+                for (int i = 0; i < T::NU * T::SLABS * 8; ++i) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
+                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+                }
+                uint32_t e = __float_as_uint(most) >> 23;                   // a power of two, 2^(e - 127)
+                e = most == 0.f || e == 255 ? 127 : e < 1 ? 1 : e > 253 ? 253 : e;
+                const float inv = __uint_as_float((254 - e) << 23);
+#pragma unroll 1
+                for (int i = 0; i < T::NU * T::SLABS * 8; ++i) {
+                    uint4* const at = reinterpret_cast<uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
+                    const uint4 u = *at;
+                    *at = make_uint4(pack_f16(bf16_lo(u.x) * inv, bf16_hi(u.x) * inv), pack_f16(bf16_lo(u.y) * inv, bf16_hi(u.y) * inv),
+                                     pack_f16(bf16_lo(u.z) * inv, bf16_hi(u.z) * inv), pack_f16(bf16_lo(u.w) * inv, bf16_hi(u.w) * inv));
+                }
+                ctrl->q_scale[qt][r] = __uint_as_float(e << 23);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) arrive(&ctrl->q_conv[qt]);
+            }
+            if (used) {
+                wait_bar(&ctrl->q_conv[qt], q_count[qt], ctrl, a.status);
+                c *= ctrl->q_scale[qt][r];
+            }
+            if (dual) {      // (both warpgroups count both tiles' loads)
+                for (int u = 0; u < 2; ++u) {
+                    int ua, ub;
+                    range_of(a, s, dual, u, ua, ub);
+                    q_count[u] += ub > ua;
+                }
+            } else {
+                q_count[0] += used;
+            }
+        }
+        float m = NEG_INF, l = 0.f;                // m: the maximum that is subtracted, without LIFT
+        for (int i = 0; i < n_mine; ++i) {
+            const int j = first + i * step;
+            const int buf = T::TILES == 2 ? t : i & 1;
+            wait_bar(&ctrl->s_full[buf], s_count[buf], ctrl, a.status);
+            ++s_count[buf];
+            ptx::tc_fence_after();
+            uint32_t x[4][32];
+            const uint32_t at = t_lane + buf * KT;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) ptx::tmem_ld_x32(at + 32 * w, x[w]);
+            ptx::tmem_ld_wait(x[0]);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) ptx::reg_dep(x[w]);
+            bool masked = KT * j < inner0 || KT * (j + 1) > inner1;
+            uint4 pages = make_uint4(~0u, ~0u, ~0u, ~0u);
+            if (T::PAGED) {
+                pages = ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD];
+                masked |= (pages.x & pages.y & pages.z & pages.w) != ~0u;
+            }
+            if (masked) {
+                const int lo = k0 - KT * j, hi = k1 - KT * j;
+                const uint32_t seen[4] = {pages.x, pages.y, pages.z, pages.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int b0 = min(max(lo - 32 * w, 0), 32), b1 = min(max(hi - 32 * w, 0), 32);
+                    // bits [b0, b1)
+                    const uint32_t below1 = b1 == 32 ? ~0u : (1u << b1) - 1, below0 = b0 == 32 ? ~0u : (1u << b0) - 1;
+                    const uint32_t bits = seen[w] & below1 & ~below0;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (!(bits & (1u << k))) x[w][k] = __float_as_uint(NEG_INF);
+                }
+            }
+            float top[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                top[w] = __uint_as_float(x[w][0]);
+#pragma unroll
+                for (int k = 1; k < 31; k += 2) top[w] = ptx::fmax3(top[w], __uint_as_float(x[w][k]), __uint_as_float(x[w][k + 1]));
+                top[w] = fmaxf(top[w], __uint_as_float(x[w][31]));
+            }
+            const float up = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+            const bool higher = up > m + SLACK;                // (the first keys that are seen: m is -inf)
+            if (__any_sync(0xffffffffu, higher)) {
+                const float f = higher ? ex2(m - up) : 1.f;
+                if (higher) m = up;
+                l *= f;
+                if (i > 0) {
+                    const int ob = T::TILES == 2 ? t : 0;
+                    wait_bar(&ctrl->o_done[ob], o_count[ob] - 1, ctrl, a.status);
+                    ptx::tc_fence_after();
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        const uint32_t oa = t_lane + 2 * KT + ob * KT + d;
+                        ptx::tmem_ld_x32(oa, o);
+                        ptx::tmem_ld_wait(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                        ptx::tmem_st_x32(oa, o);
+                    }
+                }
+            }
+            const float base = m == NEG_INF ? 0.f : m - LIFT;
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t p[16];
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    float u = __uint_as_float(x[w][k]), v = __uint_as_float(x[w][k + 1]);
+                    scale_sub2(u, v, c, -base);
+                    u = ex2(u), v = ex2(v);
+                    add2(sum[(k >> 1) & 1], u, v);
+                    // Weights are rounded to 16 bits for the tensor core (bf16: half a step of 2^-8, about what the output's own
+                    // rounding is; it is the operand type that the values have), their sum is that of the unrounded ones
+                    p[k >> 1] = T::F16 ? pack_f16(u, v) : pack_bf16(u, v);
+                }
+                ptx::tmem_st_x16(at + 16 * w, p);
+            }
+            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&ctrl->p_ready[buf]);
+            ++o_count[T::TILES == 2 ? t : 0];
+        }
+        tiles += s.jb - s.ja;
+        if (dual && t == 0) {      // (the first warpgroup counts the second tile's products too)
+            int ua, ub;
+            range_of(a, s, dual, 1, ua, ub);
+            o_count[1] += ub - ua;
+        }
+        const int n_other = alt ? (s.jb - s.ja) / 2 : 0;       // the second tile's steps
+        if (alt && t == 1) {
+            // the first warpgroup joins (x_count: two places in turn, so that one is not written before it has been read)
+            if (n_mine) {
+                ctrl->ml[x_count & 1][r] = make_float2(m, l);
+                __syncwarp();
+                if (lane == 0) arrive(&ctrl->x_full);
+                ++x_count;
+            }
+            continue;
+        }
+        // ---- the end of the segment
+        float f0 = 1.f, f1 = 0.f, top = m;
+        if (n_other) {
+            wait_bar(&ctrl->x_full, x_count, ctrl, a.status);
+            const float2 other = ctrl->ml[x_count & 1][r];
+            ++x_count;
+            top = fmaxf(m, other.x);
+            const float from = top == NEG_INF ? 0.f : top;
+            f0 = ex2(m - from), f1 = ex2(other.x - from);
+            l = l * f0 + other.y * f1;
+            o_count[1] += n_other;
+            wait_bar(&ctrl->o_done[1], o_count[1] - 1, ctrl, a.status);
+        }
+        const int ob = T::TILES == 2 ? t : 0;
+        // (one O for both score buffers: the last scores say only that the product before the last but one is done, and a parity names every
+        // other product)
+        if (T::TILES == 1 && n_mine > 1) wait_bar(&ctrl->o_done[ob], o_count[ob] - 2, ctrl, a.status);
+        if (n_mine) wait_bar(&ctrl->o_done[ob], o_count[ob] - 1, ctrl, a.status);
+        ptx::tc_fence_after();
+        const float sub = top == NEG_INF ? NEG_INF : top - LIFT;      // what was subtracted
+        const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[s.g] : 1.f;
+        const bool empty = l == 0.f;               // sees nothing that weighs anything: zeros, whatever the values are
+        const float inv = s.part >= 0 ? 1.f : vs / l;
+        f0 *= inv, f1 *= inv;
+        const i64 row = (s.tok + my_tok) * a.Hq + s.head0 + h;
+        const int part_row = (dual ? t * MT : 0) + r;
+        float* const part = a.parts + s.part * T::PART;
+        float odd = 0.f;                           // NaN once something is not finite
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+            uint32_t o[32], o1[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = 0u;
+            if (n_mine) {
+                ptx::tmem_ld_x32(t_lane + 2 * KT + ob * KT + d, o);
+                ptx::tmem_ld_wait(o);
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
+            if (n_other) {
+                ptx::tmem_ld_x32(t_lane + 3 * KT + d, o1);
+                ptx::tmem_ld_wait(o1);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) odd = fmaf(__uint_as_float(o[k]), 0.f, odd);
+            if (!valid) continue;
+            if (empty) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = 0u;
+            }
+            if (s.part >= 0) {
+                float4* const to = reinterpret_cast<float4*>(part + static_cast<i64>(part_row) * D + d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    to[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+            } else {
+                uint32_t w[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) w[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                cake_bf16* const to = a.out + row * D + d;
+                if (a.wide) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(to)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) to[2 * k] = w[k] & 0xffff, to[2 * k + 1] = w[k] >> 16;
+                }
+            }
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (n_mine) arrive(&ctrl->o_free[ob]);
+            if (n_other) arrive(&ctrl->o_free[1]);
+        }
+        if (valid) {
+            bool mended = false;
+            if (isnan(odd) && isfinite(l) && !empty) {
+                RowAt at;
+                at.row = row, at.g = s.g, at.part_row = part_row, at.part = s.part, at.base = s.k0;
+                at.q = a.q + (s.tok + my_tok) * a.q_stride + (s.head0 + h) * a.q_head_stride;
+                at.from = KT * ra, at.to = KT * rb;
+                if (T::PAGED) {                    // (what no row of the segment sees was not loaded)
+                    at.from = max(at.from, first_key(a, s.pos, s.klen)), at.to = min(at.to, end_key(a, s.pos + s.ntok - 1, s.klen));
+                }
+                at.k0 = max(k0, KT * ra), at.k1 = min(k1, KT * rb);
+                float cc = s.negative ? -a.scale_log2 : a.scale_log2;
+                if (T::F16 && a.c.k_scale) cc *= fabsf(a.c.k_scale[s.g]);
+                mended = mend_row<T>(a, at, cc, sub, vs);
+            }
+            if (!mended) {
+                if (s.part >= 0) {
+                    *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
+                } else if (a.lse) {
+                    a.lse[row] = l == 0.f ? NEG_INF : (sub + log2f(l)) * LN2;
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------ loads
+// The order of a segment's loads, which is that of their use: keys of the first tile (ALT: two), then values of tile i, keys of the next.
+// load(values, tile)
+template <class T, class F>
+__device__ __forceinline__ void loads_of(const Args& a, const Seg& s, F&& load) {
+    const int ahead = is_dual<T>(a, s) ? 1 : 2;
+    for (int i = 0; i < ahead && s.ja + i < s.jb; ++i) load(false, s.ja + i);
+    for (int j = s.ja; j < s.jb; ++j) {
+        load(true, j);
+        if (j + ahead < s.jb) load(false, j + ahead);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void load_thread(const Args& a, Ctrl* ctrl, const CUtensorMap* mq, const CUtensorMap* mk, const CUtensorMap* mv,
+                                            uint32_t q_smem, uint32_t kv_smem) {
+    uint32_t segs = 0, q_count[2] = {0, 0}, n = 0;
+    const uint32_t q_bytes = T::NU * T::SLABS * static_cast<uint32_t>(a.tokens * a.heads) * 128u;
+    Seg s;
+    while (next_seg(a, ctrl, segs, s, true)) {
+        const bool dual = is_dual<T>(a, s);
+        for (int t = 0; t < (dual ? 2 : 1); ++t) {
+            int ra, rb;
+            range_of(a, s, dual, t, ra, rb);
+            if (ra == rb) continue;
+            wait_bar(&ctrl->q_empty[t], q_count[t] + 1, ctrl, a.status);
+            if (aborted(ctrl)) break;
+            ++q_count[t];
+            const uint32_t bar = ptx::smem_u32(&ctrl->q_full[t]);
+            ptx::mbar_arrive_expect_tx(bar, q_bytes);
+#pragma unroll
+            for (int x = 0; x < T::NU * T::SLABS; ++x)
+                ptx::tma_load_3d(q_smem + (t * T::NU * T::SLABS + x) * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
+        }
+        if (!T::PAGED) {
+            loads_of<T>(a, s, [&](bool values, int j) {
+                for (int u = 0; u < T::NU; ++u, ++n) {
+                    const uint32_t st = n % T::STAGES;
+                    wait_bar(&ctrl->kv_empty[st], n / T::STAGES + 1, ctrl, a.status);
+                    if (aborted(ctrl)) return;
+                    const uint32_t bar = ptx::smem_u32(&ctrl->kv_full[st]);
+                    ptx::mbar_arrive_expect_tx(bar, T::UNIT);
+#pragma unroll
+                    for (int x = 0; x < T::SLABS; ++x)
+                        ptx::tma_load_3d(kv_smem + st * T::UNIT + x * T::SLAB, values ? mv : mk, bar, 128 * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+                }
+            });
+        }
+        if (aborted(ctrl)) break;
+    }
+    // copies in flight land before the CTA gives up its shared memory (they have, unless a wait has expired)
+    if (aborted(ctrl)) {
+        const uint64_t t0 = ptx::globaltimer_ns();
+        auto landed = [&](uint64_t* bar, uint32_t parity) {
+            while (!ptx::mbar_try_wait(ptx::smem_u32(bar), parity & 1) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
+        };
+        for (int t = 0; t < 2; ++t)
+            if (q_count[t]) landed(&ctrl->q_full[t], q_count[t] - 1);
+        for (uint32_t i = n > T::STAGES ? n - T::STAGES : 0; i < n; ++i) landed(&ctrl->kv_full[i % T::STAGES], i / T::STAGES);
+    }
+}
+
+// Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile; a row's 16-byte pieces are then copied by neighbouring lanes.
+template <class T>
+__device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* kv_smem) {
+    constexpr int ELEM = T::F16 ? 1 : 2;
+    constexpr int PIECES = T::DU * ELEM / 16;               // of a key's part in a unit
+    constexpr int ITERS = PIECES;                           // 32 keys x PIECES / 32 lanes
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+    uint32_t segs = 0, n = 0, signalled = 0, tiles = 0;
+    // bf16: copies of LAG units are in flight.  A unit's place may wait for two more units (values are released behind the next keys' scores, or
+    // a tile's two units together), which have to be signalled by then
+    constexpr uint32_t LAG = T::STAGES - 2 < 4 ? T::STAGES - 2 : 4;
+    auto signal = [&](uint32_t unit) {
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) arrive(&ctrl->kv_full[unit % T::STAGES]);
+    };
+    uint4 held[T::F16 ? ITERS : 1];                         // e4m3: the unit before
+    auto settle = [&](uint32_t unit) {                      // e4m3: widens the unit held into its place
+        uint8_t* const place = kv_smem + (unit % T::STAGES) * T::UNIT;
+        wait_bar(&ctrl->kv_empty[unit % T::STAGES], unit / T::STAGES + 1, ctrl, a.status);
+#pragma unroll
+        for (int i = 0; i < (T::F16 ? ITERS : 0); ++i) {
+            const int flat = i * 32 + lane, key = 32 * warp + flat / PIECES, piece = flat % PIECES;      // 16 elements
+            const uint32_t w[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
+            uint32_t f[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e4m3_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+            uint8_t* const row = place + (piece >> 2) * T::SLAB + key * 128;
+            const int c = (piece & 3) * 2;
+            *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+        }
+        signal(unit);
+    };
+    auto flush = [&]() {
+        if (T::F16) {
+            if (signalled < n) settle(signalled), ++signalled;
+        } else {
+            cp_wait<0>();
+            for (; signalled < n; ++signalled) signal(signalled);
+        }
+    };
+    Seg s;
+    for (;;) {
+        // (what is still under way is waited for before the warp waits for more work)
+        if (!__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(&ctrl->seg_full[segs % SEGS]), (segs / SEGS) & 1))) flush();
+        if (!next_seg(a, ctrl, segs, s, false)) break;
+        // keys that some row of the item sees; no others are read
+        const int from = first_key(a, s.pos, s.klen), to = end_key(a, s.pos + s.ntok - 1, s.klen);
+        auto page_of = [&](int j) {
+            const int key = KT * j + 32 * warp + lane;
+            return j < s.jb && key >= from && key < to ? max(a.table[s.k0 + key / a.c.page_size], -1) : INT_MIN;
+        };
+        // the pages of the next tiles' keys are looked up ahead: [0] the tile whose values come next, [2] the furthest
+        int page[4] = {page_of(s.ja), page_of(s.ja + 1), page_of(s.ja + 2), INT_MIN};
+        int base = s.ja;
+        loads_of<T>(a, s, [&](bool values, int j) {
+            if (any_aborted(ctrl)) return;
+            const int p = j == base ? page[0] : j == base + 1 ? page[1] : page[2];
+            const int key = KT * j + 32 * warp + lane;
+            const bool ok = p >= 0 && p < a.c.num_pages;
+            if (!values) {
+                const unsigned bits = __ballot_sync(0xffffffffu, ok || p == INT_MIN);
+                if (lane == 0) reinterpret_cast<uint32_t*>(&ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD])[warp] = bits;
+                if (!ok && p != INT_MIN) raise_bad_index(a.status);
+            }
+            const i64 off = key % a.c.page_size;
+            const char* row = nullptr;
+            if (ok)
+                row = values ? static_cast<const char*>(a.c.v) + (p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride) * ELEM
+                             : static_cast<const char*>(a.c.k) + (p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride) * ELEM;
+            for (int u = 0; u < T::NU; ++u, ++n) {
+                if (T::F16) {
+                    uint4 got[ITERS];
+#pragma unroll
+                    for (int i = 0; i < ITERS; ++i) {
+                        const int flat = i * 32 + lane;
+                        const char* const from_row = reinterpret_cast<const char*>(
+                            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), flat / PIECES));
+                        got[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (from_row) got[i] = *reinterpret_cast<const uint4*>(from_row + u * T::DU * ELEM + flat % PIECES * 16);
+                    }
+                    if (signalled < n) settle(signalled), ++signalled;
+#pragma unroll
+                    for (int i = 0; i < ITERS; ++i) held[i] = got[i];
+                } else {
+                    const uint32_t st = n % T::STAGES;
+                    wait_bar(&ctrl->kv_empty[st], n / T::STAGES + 1, ctrl, a.status);
+                    const uint32_t place = ptx::smem_u32(kv_smem + st * T::UNIT);
+#pragma unroll
+                    for (int i = 0; i < ITERS; ++i) {
+                        const int flat = i * 32 + lane, k = flat / PIECES, piece = flat % PIECES;      // 8 elements
+                        const char* const from_row = reinterpret_cast<const char*>(
+                            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
+                        const uint32_t dst = place + (piece >> 3) * T::SLAB + (32 * warp + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                        cp_async16(dst, from_row ? from_row + u * T::DU * ELEM + piece * 16 : static_cast<const char*>(a.c.k), from_row != nullptr);
+                    }
+                    cp_commit();
+                    if (n - signalled >= LAG) {
+                        cp_wait<LAG>();
+                        signal(signalled);
+                        ++signalled;
+                    }
+                }
+            }
+            if (values) {      // on to the next tile
+                page[0] = page[1], page[1] = page[2], page[2] = page_of(j + 3);
+                base = j + 1;
+            }
+        });
+        tiles += s.jb - s.ja;
+        if (any_aborted(ctrl)) break;
+    }
+    if (!any_aborted(ctrl)) flush();
+    cp_wait<0>();
+}
+
+// ---------------------------------------------------------------------------------------------------------- products
+template <class T>
+__device__ __forceinline__ void mma_thread(const Args& a, Ctrl* ctrl, uint32_t q_smem, uint32_t kv_smem, uint32_t tmem) {
+    constexpr uint32_t F = T::F16 ? ptx::UMMA_IDESC_F16 : 0u;
+    constexpr uint32_t idesc_s = ptx::umma_idesc_bf16(MT, KT) & ~F;
+    constexpr uint32_t idesc_o = (ptx::umma_idesc_bf16(MT, T::DU) & ~F) | ptx::UMMA_IDESC_B_MN_MAJOR;
+    uint32_t segs = 0, n = 0, q_count[2] = {0, 0}, p_count[2] = {0, 0}, o_uses[2] = {0, 0};
+    Seg s = {};
+    auto full = [&](uint32_t first) {      // a tile's units have landed
+        for (uint32_t u = first; u < first + T::NU; ++u) wait_bar(&ctrl->kv_full[u % T::STAGES], u / T::STAGES, ctrl, a.status);
+        ptx::tc_fence_after();
+    };
+    auto release = [&](uint32_t first) {
+        for (uint32_t u = first; u < first + T::NU; ++u) ptx::umma_commit(ptx::smem_u32(&ctrl->kv_empty[u % T::STAGES]));
+    };
+    auto scores = [&](int qt, int buf, uint32_t first) {
+        const uint32_t idesc = idesc_s | (s.negative ? ptx::UMMA_IDESC_NEGATE_B : 0u);
+#pragma unroll
+        for (int u = 0; u < T::NU; ++u) {
+            const uint32_t qa = ptx::umma_desc_lo_sw128(q_smem + (qt * T::NU + u) * T::UNIT);
+            const uint32_t ka = ptx::umma_desc_lo_sw128(kv_smem + ((first + u) % T::STAGES) * T::UNIT);
+#pragma unroll
+            for (int k = 0; k < T::DU / 16; ++k) {
+                const uint32_t add = (k >> 2) * (T::SLAB >> 4) + (k & 3) * 2;
+                if (u == 0 && k == 0) ptx::umma_bf16_lohi<false>(tmem + buf * KT, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
+                else ptx::umma_bf16_lohi<true>(tmem + buf * KT, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
+            }
+        }
+        ptx::umma_commit(ptx::smem_u32(&ctrl->s_full[buf]));
+    };
+    auto weighted = [&](int buf, int ob, uint32_t first, bool fresh) {
+        wait_bar(&ctrl->p_ready[buf], p_count[buf], ctrl, a.status);
+        ++p_count[buf];
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int u = 0; u < T::NU; ++u) {
+            // values as they lie there: 64-column slabs (leading offset), groups of eight keys 1024 bytes apart
+            const uint32_t lo = (((kv_smem + ((first + u) % T::STAGES) * T::UNIT) & 0x3FFFFu) >> 4) | ((T::SLAB >> 4) << 16);
+#pragma unroll
+            for (int k = 0; k < KT / 16; ++k) {
+                const uint64_t desc = (static_cast<uint64_t>(ptx::UMMA_DESC_HI_SW128) << 32) | (lo + k * (2048u >> 4));
+                ptx::umma_f16_ta(tmem + 2 * KT + ob * KT + u * 128, tmem + buf * KT + k * 8, desc, idesc_o, !fresh || k > 0);
+            }
+        }
+        ptx::umma_commit(ptx::smem_u32(&ctrl->o_done[ob]));
+    };
+    auto q_in = [&](int qt) {
+        wait_bar(T::F16 ? &ctrl->q_conv[qt] : &ctrl->q_full[qt], q_count[qt], ctrl, a.status);
+        ++q_count[qt];
+        ptx::tc_fence_after();
+    };
+    auto q_out = [&](int qt) { ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[qt])); };
+    auto o_in = [&](int ob) {              // the rows of the segment before have been read
+        if (o_uses[ob]) wait_bar(&ctrl->o_free[ob], o_uses[ob] - 1, ctrl, a.status);
+        ++o_uses[ob];
+    };
+    while (next_seg(a, ctrl, segs, s, true)) {
+        if (s.ja == s.jb) continue;
+        if (is_dual<T>(a, s)) {
+            int ra[2], rb[2];
+            range_of(a, s, true, 0, ra[0], rb[0]);
+            range_of(a, s, true, 1, ra[1], rb[1]);
+            auto start = [&](int t, int j, uint32_t keys) {
+                if (j == ra[t]) q_in(t);
+                scores(t, t, keys);
+                if (j == rb[t] - 1) q_out(t);
+            };
+            uint32_t keys = n;
+            n += T::NU;
+            full(keys);
+            for (int t = 0; t < 2; ++t)
+                if (s.ja >= ra[t] && s.ja < rb[t]) start(t, s.ja, keys);
+            release(keys);
+            for (int j = s.ja; j < s.jb && !aborted(ctrl); ++j) {
+                const uint32_t values = n;
+                const bool more = j + 1 < s.jb;
+                keys = n + T::NU;
+                n += more ? 2 * T::NU : T::NU;
+                full(values);
+                bool keys_in = false;
+                for (int t = 0; t < 2; ++t) {
+                    if (j >= ra[t] && j < rb[t]) {
+                        if (j == ra[t]) o_in(t);
+                        weighted(t, t, values, j == ra[t]);
+                    }
+                    if (more && j + 1 >= ra[t] && j + 1 < rb[t]) {
+                        if (!keys_in) full(keys), keys_in = true;
+                        start(t, j + 1, keys);
+                    }
+                }
+                release(values);
+                if (more) {
+                    if (!keys_in) full(keys);
+                    release(keys);
+                }
+            }
+        } else {
+            const int steps = s.jb - s.ja;
+            uint32_t keys;
+            q_in(0);
+            for (int i = 0; i < 2 && i < steps; ++i) {
+                keys = n, n += T::NU;
+                full(keys);
+                scores(0, i, keys);
+                release(keys);
+                if (i == steps - 1) q_out(0);
+            }
+            for (int i = 0; i < steps && !aborted(ctrl); ++i) {
+                const int buf = i & 1, ob = T::TILES == 2 ? buf : 0;
+                const uint32_t values = n;
+                n += T::NU;
+                full(values);
+                const bool fresh = i < T::TILES;
+                if (fresh) o_in(ob);
+                weighted(buf, ob, values, fresh);
+                release(values);
+                if (i + 2 < steps) {
+                    keys = n, n += T::NU;
+                    full(keys);
+                    scores(0, buf, keys);
+                    release(keys);
+                    if (i + 2 == steps - 1) q_out(0);
+                }
+            }
+        }
+        if (aborted(ctrl)) break;
+    }
+    if (aborted(ctrl)) {      // products under way end before shared and tensor memory are given up
+        ptx::umma_commit(ptx::smem_u32(&ctrl->drained));
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (!ptx::mbar_try_wait(ptx::smem_u32(&ctrl->drained), 0) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(T::THREADS, 1)
+attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Args a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t* const kv_smem = q_smem + T::Q_BYTES;
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(kv_smem + T::STAGES * T::UNIT);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        auto init = [](uint64_t* bar, int n) { ptx::mbar_init(ptx::smem_u32(bar), n); };
+        for (int i = 0; i < SEGS; ++i) {
+            init(&ctrl->seg_full[i], 1);
+            init(&ctrl->seg_empty[i], 2 + T::WARPS_SM + T::WARPS_LD);
+        }
+        for (int i = 0; i < 2; ++i) {
+            init(&ctrl->q_full[i], 1), init(&ctrl->q_empty[i], 1), init(&ctrl->q_conv[i], 4);
+            init(&ctrl->s_full[i], 1), init(&ctrl->p_ready[i], 4), init(&ctrl->o_done[i], 1), init(&ctrl->o_free[i], 4);
+        }
+        for (int i = 0; i < T::STAGES; ++i) init(&ctrl->kv_full[i], T::PAGED ? 4 : 1), init(&ctrl->kv_empty[i], 1);
+        init(&ctrl->x_full, 4), init(&ctrl->drained, 1);
+        ctrl->abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tensormap(&mq);
+        if (!T::PAGED) ptx::prefetch_tensormap(&mk), ptx::prefetch_tensormap(&mv);
+    }
+    if (warp == T::WARP_MMA) {
+        ptx::tmem_alloc(ptx::smem_u32(&ctrl->tmem), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::grid_dep_wait();
+    {   // the list's length: every warp adds up a stretch of entries
+        const i64 e0 = a.entries * warp / T::WARPS, e1 = a.entries * (warp + 1) / T::WARPS;
+        i64 sum = 0;
+        for (i64 e = e0; e < e1; e += 32) {
+            Entry en = {};
+            if (e + lane < e1) en = entry_of<T::PAGED>(a, e + lane, blockIdx.x == 0);
+            sum += entry_cost<T::TILES>(a, en.qlen, en.klen);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) ctrl->sums[warp] = sum;
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = ctrl->tmem;
+
+    if (warp >= T::WARP_SCHED) {
+        if (T::SPLIT_REGS) ptx::setmaxnreg_dec<T::REGS_AUX>();
+        if (warp == T::WARP_SCHED) {
+            schedule<T>(a, ctrl);
+        } else if (warp == T::WARP_TMA) {
+            if (ptx::elect_one()) load_thread<T>(a, ctrl, &mq, &mk, &mv, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem));
+            __syncwarp();
+        } else if (warp == T::WARP_MMA) {
+            if (ptx::elect_one()) mma_thread<T>(a, ctrl, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem), tmem);
+            __syncwarp();
+        }
+    } else if (T::PAGED && warp >= T::WARPS_SM) {
+        if constexpr (T::SPLIT_REGS) {
+            if constexpr (T::REGS_LD < T::REGS_START) ptx::setmaxnreg_dec<T::REGS_LD>();
+            else ptx::setmaxnreg_inc<T::REGS_LD>();
+        }
+        if constexpr (T::PAGED) load_pages<T>(a, ctrl, kv_smem);
+    } else {
+        if (T::SPLIT_REGS) ptx::setmaxnreg_inc<T::REGS_SM>();
+        softmax_rows<T>(a, ctrl, q_smem, tmem, warp >> 2);
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == T::WARP_MMA) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- join
+// out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m), m = max m_i, over the parts of an item, in order.  A warp to a row; where an
+// item has more than 8 parts, a block to a row (its warps share the parts).
+constexpr int JOIN_SLICES = 16, JOIN_WARPS = 8;
+template <int D, int ROWS, int TILES>
+__global__ void __launch_bounds__(32 * JOIN_WARPS)
+attention_join_kernel(const Args a) {
+    constexpr int V = (D + 127) / 128;           // float4 of a lane
+    constexpr i64 PART = static_cast<i64>(ROWS) * (D + 2);
+    __shared__ float4 accs[JOIN_WARPS][V][32];
+    __shared__ float2 mls[JOIN_WARPS];
+    ptx::grid_dep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = blockIdx.x / JOIN_SLICES, slice = blockIdx.x % JOIN_SLICES;
+    const Split e = a.splits[c0];
+    if (!e.valid) return;
+    const bool many = e.c1 - c0 + 1 > JOIN_WARPS;
+    const int rows = e.ntok * e.heads;
+    const float vs = a.c.type == CAKE_KV_E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
+    const bool dual = TILES == 2 && e.ntok > a.tokens;
+    for (int i = many ? slice : slice * JOIN_WARPS + warp; i < rows; i += many ? JOIN_SLICES : JOIN_SLICES * JOIN_WARPS) {
+        const int tok = i / e.heads, h = i - tok * e.heads;
+        const int t = dual && tok >= a.tokens ? 1 : 0;
+        const int row = t * MT + (tok - t * a.tokens) * a.heads + h;
+        float m = NEG_INF, l = 0.f;
+        float4 acc[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float pm, float pl, const float4 (&u)[V]) {
+            const float up = fmaxf(m, pm), from = up == NEG_INF ? 0.f : up;
+            const float f = ex2(m - from), g = ex2(pm - from);
+            m = up, l = l * f + pl * g;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                acc[v].x = acc[v].x * f + u[v].x * g, acc[v].y = acc[v].y * f + u[v].y * g;
+                acc[v].z = acc[v].z * f + u[v].z * g, acc[v].w = acc[v].w * f + u[v].w * g;
+            }
+        };
+        const int step = many ? JOIN_WARPS : 1;
+        constexpr int BATCH = 4;
+        for (int c = c0 + (many ? warp : 0); c <= e.c1; c += BATCH * step) {
+            float4 u[BATCH][V];
+            float2 ml[BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int cb = c + b * step;
+                ml[b] = make_float2(NEG_INF, 0.f);
+#pragma unroll
+                for (int v = 0; v < V; ++v) u[b][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (cb <= e.c1) {
+                    const float* p = a.parts + (2 * cb + (cb == c0 ? 1 : 0)) * PART;
+                    ml[b] = *reinterpret_cast<const float2*>(p + static_cast<i64>(ROWS) * D + 2 * row);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (128 * v + 4 * lane < D) u[b][v] = *reinterpret_cast<const float4*>(p + static_cast<i64>(row) * D + 128 * v + 4 * lane);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) add(ml[b].x, ml[b].y, u[b]);
+        }
+        if (many) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) accs[warp][v][lane] = acc[v];
+            if (lane == 0) mls[warp] = make_float2(m, l);
+            __syncthreads();
+            if (warp != 0) continue;
+            for (int w = 1; w < JOIN_WARPS; ++w) {
+                float4 u[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) u[v] = accs[w][v][lane];
+                add(mls[w].x, mls[w].y, u);
+            }
+        }
+        const float f = l == 0.f ? 0.f : vs / l;
+        const i64 out_row = (e.tok + tok) * a.Hq + e.head0 + h;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int d = 128 * v + 4 * lane;
+            if (d >= D) continue;
+            const uint2 w = make_uint2(pack_bf16(acc[v].x * f, acc[v].y * f), pack_bf16(acc[v].z * f, acc[v].w * f));
+            cake_bf16* const to = a.out + out_row * D + d;
+            if (a.wide) *reinterpret_cast<uint2*>(to) = w;
+            else to[0] = w.x & 0xffff, to[1] = w.x >> 16, to[2] = w.y & 0xffff, to[3] = w.y >> 16;
+        }
+        if (a.lse && lane == 0) a.lse[out_row] = l == 0.f ? NEG_INF : (m + log2f(l)) * LN2;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+struct Maps {
+    CUtensorMap q, k, v;
+};
+int launch_64(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
+int launch_96(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
+int launch_128(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
+int launch_256(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
+
+template <class T>
+int launch(const Args& a, const Maps& m, const DeviceInfo& di, cudaStream_t s) {
+    constexpr uint32_t SMEM = smem_bytes<T>();
+    static_assert(SMEM <= 227 * 1024, "");
+    static PerDevice ready;
+    const bool ok = ready.get(di.device, [] {
+        // the split of the registers counts on what the block starts with
+        cudaFuncAttributes at;
+        if (cudaFuncGetAttributes(&at, attention_kernel<T>) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        const int sum = 128 * (T::TILES * T::REGS_SM + (T::PAGED ? T::REGS_LD : 0) + T::REGS_AUX);
+        if (T::SPLIT_REGS && at.numRegs * T::THREADS < sum) return 0;
+        return allow_smem(attention_kernel<T>, SMEM);
+    });
+    if (!ok) return CAKE_ERR_CUDA;
+    const int ctas = di.sm_count < MOST_CTAS ? di.sm_count : MOST_CTAS;
+    if (launch_early(attention_kernel<T>, dim3(ctas), dim3(T::THREADS), SMEM, s, m.q, m.k, m.v, a) != cudaSuccess) return CAKE_ERR_CUDA;
+    return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * JOIN_SLICES), dim3(32 * JOIN_WARPS), 0, s, a) == cudaSuccess
+               ? CAKE_OK : CAKE_ERR_CUDA;
+}
+template <int D>
+int launch_kind(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s) {
+    switch (kind) {
+        case PACKED: return launch<Traits<D, PACKED>>(a, m, di, s);
+        case PAGED_BF16: return launch<Traits<D, PAGED_BF16>>(a, m, di, s);
+        default: return launch<Traits<D, PAGED_E4M3>>(a, m, di, s);
+    }
+}
+
+}  // namespace attn
+}  // namespace serving
+}  // namespace cake

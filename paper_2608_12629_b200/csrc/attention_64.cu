@@ -1,0 +1,12 @@
+// Attention of many query tokens, heads of 64 elements (attention.cuh).
+#include "attention.cuh"
+
+namespace cake {
+namespace serving {
+namespace attn {
+
+int launch_64(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s) { return launch_kind<64>(a, m, kind, di, s); }
+
+}  // namespace attn
+}  // namespace serving
+}  // namespace cake

@@ -19,12 +19,14 @@ CAKE_KV_BF16, CAKE_KV_E4M3 = 0, 1
 CAKE_RMSNORM_NONE = 1
 CAKE_GEMM_OUT_FP32 = 1
 CAKE_APPEND_INTERLEAVED = 1
+CAKE_ATTENTION_CAUSAL = 1
 CAKE_SERVING_HEADER_BYTES = 16640
 CAKE_GEMM_FP8_MOST_WORKSPACE_BYTES = 19415296
 
 SERVING_EXPORTS = [
     "cake_rmsnorm_quant", "cake_gemm_fp8_workspace_bytes", "cake_gemm_fp8", "cake_kv_append",
-    "cake_paged_decode_workspace_bytes", "cake_paged_decode",
+    "cake_paged_decode_workspace_bytes", "cake_paged_decode", "cake_qk_norm_append", "cake_kv_read", "cake_attention_workspace_bytes",
+    "cake_prompt_attention", "cake_paged_chunk",
 ]
 
 _E4M3 = torch.float8_e4m3fn
@@ -56,6 +58,11 @@ def _load() -> ctypes.CDLL:
         L.cake_kv_append.argtypes = [cache, vp, ll, vp, ll, vp, ll, i, vp, vp, vp, vp, ll, i, ll, vp, sz, vp, u]
         L.cake_paged_decode_workspace_bytes.argtypes = [ll, i, i, i, ctypes.POINTER(sz)]
         L.cake_paged_decode.argtypes = [vp, ll, ll, cache, vp, ll, ll, i, vp, ll, ll, ll, i, f, i, vp, vp, vp, sz, vp]
+        L.cake_qk_norm_append.argtypes = [cache, vp, ll, i, vp, ll, vp, ll, vp, vp, f, vp, vp, vp, vp, vp, ll, i, ll, vp, sz, vp, u]
+        L.cake_kv_read.argtypes = [cache, vp, ll, vp, vp, ll, ll, vp, sz, vp]
+        L.cake_attention_workspace_bytes.argtypes = [i, i, i, ctypes.POINTER(sz)]
+        L.cake_prompt_attention.argtypes = [vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, ll, ll, ll, i, i, i, f, i, vp, vp, vp, sz, vp, u]
+        L.cake_paged_chunk.argtypes = [vp, ll, ll, cache, vp, ll, ll, i, vp, ll, ll, vp, ll, ll, i, f, i, vp, vp, vp, sz, vp]
         for name in SERVING_EXPORTS:
             getattr(L, name).restype = i
         _lib = L
@@ -179,7 +186,7 @@ class PagedCache:
 
 
 def alloc_append_workspace(device) -> torch.Tensor:
-    """A workspace for cake_kv_append (its device status), zeroed."""
+    """A workspace for cake_kv_append, cake_qk_norm_append and cake_kv_read (their device status), zeroed."""
     return _workspace(CAKE_SERVING_HEADER_BYTES, device)
 
 
@@ -197,6 +204,41 @@ def cake_kv_append(cache, k, v, slots, positions=None, cos_sin=None, q=None, out
     if rc:
         raise CakeError(rc, "cake_kv_append")
     return out_q
+
+
+# ------------------------------------------------------------------------------------------- qk_norm_append, kv_read
+def cake_qk_norm_append(cache, q, k, v, slots, q_weight=None, k_weight=None, positions=None, cos_sin=None, eps=1e-6, interleaved=False,
+                        out_q=None, out_k=None, want_k=False, ws=None, stream=None):
+    """RMS norm of each head of q bf16 [T,Hq,D] and k [T,Hkv,D] (weights bf16 [D] or None), the rotation of cake_kv_append, and k and
+    v [T,Hkv,D] to `slots` of the cache.  Returns (queries, keys): the keys beside the cache with want_k or out_k, else None."""
+    if out_q is None:
+        out_q = _empty(q.shape, _BF16, q.device, stream)
+    if want_k and out_k is None:
+        out_k = _empty(k.shape, _BF16, k.device, stream)
+    if ws is None:
+        ws = _workspace(CAKE_SERVING_HEADER_BYTES, k.device, stream)
+    rc = (_ext or _native()).qk_norm_append(cache._address, cache.k, q, k, v, slots, q_weight, k_weight, positions, cos_sin, eps, interleaved,
+                                            out_q, out_k, ws, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise CakeError(rc, "cake_qk_norm_append")
+    return out_q, out_k
+
+
+def cake_kv_read(cache, slots, out_k=None, out_v=None, by_head=False, want_k=True, want_v=True, ws=None, stream=None):
+    """Keys and values of `slots` (int64 [N], negative: zeros) back from the cache, bf16 (8-bit ones times their scales) ->
+    (k, v), each [N,Hkv,D], or with by_head [Hkv,N,D]: a matrix of tokens for each head, as the clustering takes it.  What is
+    not wanted (and has no buffer) comes back as None."""
+    shape = (cache.Hkv, slots.shape[0], cache.D) if by_head else (slots.shape[0], cache.Hkv, cache.D)
+    if want_k and out_k is None:
+        out_k = _empty(shape, _BF16, cache.device, stream)
+    if want_v and out_v is None:
+        out_v = _empty(shape, _BF16, cache.device, stream)
+    if ws is None:
+        ws = _workspace(CAKE_SERVING_HEADER_BYTES, cache.device, stream)
+    rc = (_ext or _native()).kv_read(cache._address, cache.k, slots, out_k, out_v, by_head, ws, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise CakeError(rc, "cake_kv_read")
+    return out_k, out_v
 
 
 # -------------------------------------------------------------------------------------------------------- paged_decode
@@ -228,4 +270,57 @@ def cake_paged_decode(q, cache, page_table, seq_lens, scale=None, window=0, out=
                                           ws, None if stream is None else stream.cuda_stream)
     if rc:
         raise CakeError(rc, "cake_paged_decode")
+    return out, out_lse
+
+
+# -------------------------------------------------------------------------------------------- attention of many tokens
+def cake_attention_workspace_bytes(Hq, Hkv, D) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_load().cake_attention_workspace_bytes(Hq, Hkv, D, ctypes.byref(out)), "cake_attention_workspace_bytes")
+    return int(out.value)
+
+
+def alloc_attention_workspace(Hq, Hkv, D, device) -> torch.Tensor:
+    """A workspace for cake_prompt_attention and cake_paged_chunk with these heads, any number of tokens; its header zeroed."""
+    return _workspace(cake_attention_workspace_bytes(Hq, Hkv, D), device)
+
+
+def cake_prompt_attention(q, k, v, starts, k_starts=None, scale=None, causal=True, window=0, out=None, out_lse=None, want_lse=False,
+                          ws=None, stream=None):
+    """Attention of packed prompts: q bf16 [T,Hq,D], k and v [Tk,Hkv,D], sequence b the tokens starts[b] up to starts[b+1] (int32 [B+1];
+    k_starts likewise for the keys, by default the same) -> (out bf16 [T,Hq,D], lse fp32 [T,Hq] or None).
+
+    The last token of a sequence is at its last key's position.  causal: a token sees the keys up to its own position, with window > 0 the
+    last `window` of them.  scale defaults to 1/sqrt(D).  Tokens of no sequence are left as they were.
+    """
+    if out is None:
+        out = _empty(q.shape, _BF16, q.device, stream)
+    if want_lse and out_lse is None:
+        out_lse = _empty(q.shape[:2], torch.float32, q.device, stream)
+    if ws is None:
+        ws = _workspace(cake_attention_workspace_bytes(q.shape[1], k.shape[1], q.shape[2]), q.device, stream)
+    rc = (_ext or _native()).prompt_attention(q, k, v, starts, k_starts, q.shape[2] ** -0.5 if scale is None else scale, causal, window, out, out_lse, ws,
+                                              None if stream is None else stream.cuda_stream)
+    if rc:
+        raise CakeError(rc, "cake_prompt_attention")
+    return out, out_lse
+
+
+def cake_paged_chunk(q, cache, page_table, seq_lens, starts, scale=None, window=0, out=None, out_lse=None, want_lse=False, ws=None, stream=None):
+    """Causal attention of a chunk of new tokens per sequence over the cache, which holds them already: q bf16 [T,Hq,D], sequence b the
+    tokens starts[b] up to starts[b+1] (int32 [B+1]), the last of its seq_lens[b] cached ones -> (out bf16 [T,Hq,D], lse fp32 [T,Hq] or None).
+
+    page_table int32 [B,max_pages] and seq_lens int32 [B], or one per key-value head: [B,Hkv,max_pages] and [B,Hkv].
+    scale defaults to 1/sqrt(D); window > 0: the last `window` tokens up to a token's own.
+    """
+    if out is None:
+        out = _empty(q.shape, _BF16, q.device, stream)
+    if want_lse and out_lse is None:
+        out_lse = _empty(q.shape[:2], torch.float32, q.device, stream)
+    if ws is None:
+        ws = _workspace(cake_attention_workspace_bytes(q.shape[1], cache.Hkv, cache.D), q.device, stream)
+    rc = (_ext or _native()).paged_chunk(q, cache._address, cache.k, page_table, seq_lens, starts, cache.D ** -0.5 if scale is None else scale, window, out,
+                                         out_lse, ws, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise CakeError(rc, "cake_paged_chunk")
     return out, out_lse
