@@ -46,6 +46,11 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
 
+// Tensor memory: scores of one row tile between the weights (16 bits) of two, then the weighted sums (of the one row tile: both places)
+constexpr uint32_t S_COL = KT / 2, O_COL = 2 * KT;
+__device__ __forceinline__ uint32_t p_col(int pb) { return pb ? KT / 2 + KT : 0; }
+constexpr int AHEAD = 2;                       // tiles of keys that are loaded ahead of the first values
+
 enum Kind { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
 
 // An item that several CTAs share: `cta` has the beginning, the ones up to c1 the rest; count = 0: none.
@@ -88,22 +93,28 @@ struct Traits {
     static constexpr int KIND = KIND_;
     static constexpr bool PAGED = KIND != PACKED, F16 = KIND == PAGED_E4M3;
     static constexpr int TILES = D == 256 ? 1 : 2;
-    static constexpr int NU = D == 256 ? 2 : 1;              // units of 128 columns that a tile of keys is loaded in
-    static constexpr int DU = D / NU;
-    static constexpr int SLABS = (DU + 63) / 64;             // of 64 columns: 128-byte rows, 128-byte swizzle
+    // Keys and values have a ring of places each (64 KiB), a tile of them comes in units of KC (VC) columns, in slabs of 64: 128-byte rows,
+    // 128-byte swizzle.  Heads of 256: smaller units of keys, so that the next tile's come in behind this one's products
     static constexpr uint32_t SLAB = MT * 128;
-    static constexpr uint32_t UNIT = SLABS * SLAB;
+    static constexpr int SLABS = (D + 63) / 64;
+    static constexpr int KC = D == 256 ? 64 : D, VC = D == 256 ? 128 : D;
+    static constexpr int NKU = D / KC, NVU = D / VC;
+    static constexpr int K_SLABS = (KC + 63) / 64, V_SLABS = (VC + 63) / 64;
+    static constexpr uint32_t K_UNIT = K_SLABS * SLAB, V_UNIT = V_SLABS * SLAB;
+    static constexpr int K_STAGES = 4 * SLAB / K_UNIT, V_STAGES = 4 * SLAB / V_UNIT;
     static constexpr int WARPS_SM = 4 * TILES, WARPS_LD = PAGED ? 4 : 0;
     static constexpr int WARP_SCHED = WARPS_SM + WARPS_LD, WARP_TMA = WARP_SCHED + 1, WARP_MMA = WARP_SCHED + 2;
     static constexpr int WARPS = WARP_SCHED + 4, THREADS = 32 * WARPS;
-    static constexpr uint32_t Q_BYTES = TILES * NU * UNIT;
-    static constexpr int STAGES = DU == 64 ? 8 : 4;
+    static constexpr uint32_t Q_TILE = SLABS * SLAB, Q_BYTES = TILES * Q_TILE, KV_BYTES = 8 * SLAB;
     // registers: what a block starts with (65,536 / threads), shared out again between the warpgroups
     static constexpr bool SPLIT_REGS = TILES == 2 || PAGED;
     static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 184 : 232) : 232;
     static constexpr int REGS_LD = TILES == 2 ? 96 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 40) : 80;
     static constexpr int REGS_START = 65536 / THREADS / 8 * 8 > 255 ? 255 : 65536 / THREADS / 8 * 8;
     static_assert(!SPLIT_REGS || TILES * REGS_SM + (PAGED ? REGS_LD : 0) + REGS_AUX <= REGS_START * (THREADS / 128), "registers of the block");
+    // Who says that a tile's queries are done with.  A barrier's parity names every other load, so nobody who looks at a load may miss it:
+    // the issuing warp and, of 16-bit copies, the second warpgroup look at every load of the first tile
+    static __host__ __device__ constexpr int q_readers(int t) { return TILES == 2 && t == 0 && F16 ? 5 : 1; }
     static constexpr int PART_ROWS = TILES * MT;
     static constexpr i64 PART = static_cast<i64>(PART_ROWS) * (D + 2);       // floats
 };
@@ -111,19 +122,19 @@ struct Traits {
 struct __align__(16) Ctrl {
     uint64_t seg_full[SEGS], seg_empty[SEGS];
     uint64_t q_full[2], q_empty[2], q_conv[2];
-    uint64_t kv_full[8], kv_empty[8];
-    uint64_t s_full[2], p_ready[2], o_done[2], o_free[2], x_full, drained;
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t s_full[2], p_ready[2], o_done[2], o_free[2], s_free, x_full, x_empty, drained[2];
     Seg seg[SEGS];
     i64 sums[16];
     uint4 flags[FLAGS_AHEAD];                  // a bit for each key of a tile: its page exists
-    float2 ml[2][MT];                          // maximum and sum of the second tile (ALT)
+    float2 ml[MT];                             // maximum and sum of the second tile (ALT)
     float q_scale[2][MT];                      // powers of two that 16-bit queries were divided by
     uint32_t tmem;
     int abort_flag;
 };
 
 template <class T>
-constexpr uint32_t smem_bytes() { return 1024 + T::Q_BYTES + T::STAGES * T::UNIT + sizeof(Ctrl); }
+constexpr uint32_t smem_bytes() { return 1024 + T::Q_BYTES + T::KV_BYTES + sizeof(Ctrl); }
 
 __device__ __forceinline__ bool aborted(Ctrl* ctrl) { return *reinterpret_cast<volatile int*>(&ctrl->abort_flag) != 0; }
 // the same for all lanes of a warp
@@ -482,7 +493,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
     const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(r & 96) << 16);
     const int tok = r / a.heads, h = r - tok * a.heads;
-    uint32_t segs = 0, s_count[2] = {0, 0}, o_count[2] = {0, 0}, q_count[2] = {0, 0}, x_count = 0, tiles = 0;
+    uint32_t segs = 0, s_count = 0, o_count[2] = {0, 0}, q_count[2] = {0, 0}, x_count = 0, tiles = 0;      // o: products on a place of P
     Seg s;
     while (next_seg(a, ctrl, segs, s, false)) {
         const bool dual = is_dual<T>(a, s);
@@ -507,10 +518,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
             const bool used = dual ? n_mine > 0 : s.jb > s.ja;
             if (used && (dual || t == 0)) {
                 wait_bar(&ctrl->q_full[qt], q_count[qt], ctrl, a.status);
-                uint8_t* const row = q_smem + qt * (T::NU * T::UNIT) + r * 128;
+                uint8_t* const row = q_smem + qt * T::Q_TILE + r * 128;
                 float most = 0.f;
 #pragma unroll 1
-                for (int i = 0; i < T::NU * T::SLABS * 8; ++i) {
+                for (int i = 0; i < T::SLABS * 8; ++i) {
                     const uint4 u = *reinterpret_cast<const uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
                     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -520,7 +531,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                 e = most == 0.f || e == 255 ? 127 : e < 1 ? 1 : e > 253 ? 253 : e;
                 const float inv = __uint_as_float((254 - e) << 23);
 #pragma unroll 1
-                for (int i = 0; i < T::NU * T::SLABS * 8; ++i) {
+                for (int i = 0; i < T::SLABS * 8; ++i) {
                     uint4* const at = reinterpret_cast<uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
                     const uint4 u = *at;
                     *at = make_uint4(pack_f16(bf16_lo(u.x) * inv, bf16_hi(u.x) * inv), pack_f16(bf16_lo(u.y) * inv, bf16_hi(u.y) * inv),
@@ -534,31 +545,36 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
             if (used) {
                 wait_bar(&ctrl->q_conv[qt], q_count[qt], ctrl, a.status);
                 c *= ctrl->q_scale[qt][r];
+                ++q_count[qt];
             }
-            if (dual) {      // (both warpgroups count both tiles' loads)
-                for (int u = 0; u < 2; ++u) {
+            if (t == 1) {      // looks at every load of the first tile
+                bool other = !dual && used;
+                if (dual) {
                     int ua, ub;
-                    range_of(a, s, dual, u, ua, ub);
-                    q_count[u] += ub > ua;
+                    range_of(a, s, dual, 0, ua, ub);
+                    other = ub > ua;
+                    if (other) wait_bar(&ctrl->q_conv[0], q_count[0], ctrl, a.status), ++q_count[0];
                 }
-            } else {
-                q_count[0] += used;
+                __syncwarp();
+                if (other && lane == 0) arrive(&ctrl->q_empty[0]);
             }
         }
         float m = NEG_INF, l = 0.f;                // m: the maximum that is subtracted, without LIFT
         for (int i = 0; i < n_mine; ++i) {
             const int j = first + i * step;
-            const int buf = T::TILES == 2 ? t : i & 1;
-            wait_bar(&ctrl->s_full[buf], s_count[buf], ctrl, a.status);
-            ++s_count[buf];
+            const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
+            wait_bar(&ctrl->s_full[t], s_count, ctrl, a.status);
+            ++s_count;
             ptx::tc_fence_after();
             uint32_t x[4][32];
-            const uint32_t at = t_lane + buf * KT;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) ptx::tmem_ld_x32(at + 32 * w, x[w]);
+            for (int w = 0; w < 4; ++w) ptx::tmem_ld_x32(t_lane + S_COL + 32 * w, x[w]);
             ptx::tmem_ld_wait(x[0]);
 #pragma unroll
             for (int w = 1; w < 4; ++w) ptx::reg_dep(x[w]);
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&ctrl->s_free);
             bool masked = KT * j < inner0 || KT * (j + 1) > inner1;
             uint4 pages = make_uint4(~0u, ~0u, ~0u, ~0u);
             if (T::PAGED) {
@@ -594,13 +610,13 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                 if (higher) m = up;
                 l *= f;
                 if (i > 0) {
-                    const int ob = T::TILES == 2 ? t : 0;
-                    wait_bar(&ctrl->o_done[ob], o_count[ob] - 1, ctrl, a.status);
+                    const int ob = T::TILES == 2 ? t : 0, last = T::TILES == 2 ? t : pb ^ 1;      // the product before has to be complete
+                    wait_bar(&ctrl->o_done[last], o_count[last] - 1, ctrl, a.status);
                     ptx::tc_fence_after();
 #pragma unroll 1
                     for (int d = 0; d < D; d += 32) {
                         uint32_t o[32];
-                        const uint32_t oa = t_lane + 2 * KT + ob * KT + d;
+                        const uint32_t oa = t_lane + O_COL + ob * KT + d;
                         ptx::tmem_ld_x32(oa, o);
                         ptx::tmem_ld_wait(o);
 #pragma unroll
@@ -610,6 +626,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                 }
             }
             const float base = m == NEG_INF ? 0.f : m - LIFT;
+            // the product that read the place of the weights before is complete (looked at every time: a parity names every other one)
+            if (o_count[pb]) wait_bar(&ctrl->o_done[pb], o_count[pb] - 1, ctrl, a.status);
+            ++o_count[pb];
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -624,14 +643,13 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                     // rounding is; it is the operand type that the values have), their sum is that of the unrounded ones
                     p[k >> 1] = T::F16 ? pack_f16(u, v) : pack_bf16(u, v);
                 }
-                ptx::tmem_st_x16(at + 16 * w, p);
+                ptx::tmem_st_x16(t_lane + p_col(pb) + 16 * w, p);
             }
             l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive(&ctrl->p_ready[buf]);
-            ++o_count[T::TILES == 2 ? t : 0];
+            if (lane == 0) arrive(&ctrl->p_ready[pb]);
         }
         tiles += s.jb - s.ja;
         if (dual && t == 0) {      // (the first warpgroup counts the second tile's products too)
@@ -641,9 +659,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
         }
         const int n_other = alt ? (s.jb - s.ja) / 2 : 0;       // the second tile's steps
         if (alt && t == 1) {
-            // the first warpgroup joins (x_count: two places in turn, so that one is not written before it has been read)
+            // the first warpgroup joins
             if (n_mine) {
-                ctrl->ml[x_count & 1][r] = make_float2(m, l);
+                if (x_count) wait_bar(&ctrl->x_empty, x_count - 1, ctrl, a.status);
+                ctrl->ml[r] = make_float2(m, l);
                 __syncwarp();
                 if (lane == 0) arrive(&ctrl->x_full);
                 ++x_count;
@@ -654,7 +673,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
         float f0 = 1.f, f1 = 0.f, top = m;
         if (n_other) {
             wait_bar(&ctrl->x_full, x_count, ctrl, a.status);
-            const float2 other = ctrl->ml[x_count & 1][r];
+            const float2 other = ctrl->ml[r];
+            __syncwarp();
+            if (lane == 0) arrive(&ctrl->x_empty);
             ++x_count;
             top = fmaxf(m, other.x);
             const float from = top == NEG_INF ? 0.f : top;
@@ -664,10 +685,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
             wait_bar(&ctrl->o_done[1], o_count[1] - 1, ctrl, a.status);
         }
         const int ob = T::TILES == 2 ? t : 0;
-        // (one O for both score buffers: the last scores say only that the product before the last but one is done, and a parity names every
-        // other product)
-        if (T::TILES == 1 && n_mine > 1) wait_bar(&ctrl->o_done[ob], o_count[ob] - 2, ctrl, a.status);
-        if (n_mine) wait_bar(&ctrl->o_done[ob], o_count[ob] - 1, ctrl, a.status);
+        if (n_mine) {
+            const int last = T::TILES == 2 ? t : (n_mine - 1) & 1;
+            wait_bar(&ctrl->o_done[last], o_count[last] - 1, ctrl, a.status);
+        }
         ptx::tc_fence_after();
         const float sub = top == NEG_INF ? NEG_INF : top - LIFT;      // what was subtracted
         const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[s.g] : 1.f;
@@ -684,13 +705,13 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0u;
             if (n_mine) {
-                ptx::tmem_ld_x32(t_lane + 2 * KT + ob * KT + d, o);
+                ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o);
                 ptx::tmem_ld_wait(o);
             }
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
             if (n_other) {
-                ptx::tmem_ld_x32(t_lane + 3 * KT + d, o1);
+                ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
                 ptx::tmem_ld_wait(o1);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
@@ -754,23 +775,22 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
 }
 
 // ------------------------------------------------------------------------------------------------------------ loads
-// The order of a segment's loads, which is that of their use: keys of the first tile (ALT: two), then values of tile i, keys of the next.
+// The order of a segment's loads, which is about that of their use: keys of the first two tiles, then values of tile i, keys of i + 2.
 // load(values, tile)
 template <class T, class F>
 __device__ __forceinline__ void loads_of(const Args& a, const Seg& s, F&& load) {
-    const int ahead = is_dual<T>(a, s) ? 1 : 2;
-    for (int i = 0; i < ahead && s.ja + i < s.jb; ++i) load(false, s.ja + i);
+    for (int i = 0; i < AHEAD && s.ja + i < s.jb; ++i) load(false, s.ja + i);
     for (int j = s.ja; j < s.jb; ++j) {
         load(true, j);
-        if (j + ahead < s.jb) load(false, j + ahead);
+        if (j + AHEAD < s.jb) load(false, j + AHEAD);
     }
 }
 
 template <class T>
 __device__ __forceinline__ void load_thread(const Args& a, Ctrl* ctrl, const CUtensorMap* mq, const CUtensorMap* mk, const CUtensorMap* mv,
                                             uint32_t q_smem, uint32_t kv_smem) {
-    uint32_t segs = 0, q_count[2] = {0, 0}, n = 0;
-    const uint32_t q_bytes = T::NU * T::SLABS * static_cast<uint32_t>(a.tokens * a.heads) * 128u;
+    uint32_t segs = 0, q_count[2] = {0, 0}, nk = 0, nv = 0;
+    const uint32_t q_bytes = T::SLABS * static_cast<uint32_t>(a.tokens * a.heads) * 128u;
     Seg s;
     while (next_seg(a, ctrl, segs, s, true)) {
         const bool dual = is_dual<T>(a, s);
@@ -784,20 +804,34 @@ __device__ __forceinline__ void load_thread(const Args& a, Ctrl* ctrl, const CUt
             const uint32_t bar = ptx::smem_u32(&ctrl->q_full[t]);
             ptx::mbar_arrive_expect_tx(bar, q_bytes);
 #pragma unroll
-            for (int x = 0; x < T::NU * T::SLABS; ++x)
-                ptx::tma_load_3d(q_smem + (t * T::NU * T::SLABS + x) * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
+            for (int x = 0; x < T::SLABS; ++x)
+                ptx::tma_load_3d(q_smem + t * T::Q_TILE + x * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
         }
         if (!T::PAGED) {
             loads_of<T>(a, s, [&](bool values, int j) {
-                for (int u = 0; u < T::NU; ++u, ++n) {
-                    const uint32_t st = n % T::STAGES;
-                    wait_bar(&ctrl->kv_empty[st], n / T::STAGES + 1, ctrl, a.status);
-                    if (aborted(ctrl)) return;
-                    const uint32_t bar = ptx::smem_u32(&ctrl->kv_full[st]);
-                    ptx::mbar_arrive_expect_tx(bar, T::UNIT);
+                const int z = static_cast<int>(s.k0) + KT * j;
+                if (values) {
+                    for (int u = 0; u < T::NVU; ++u, ++nv) {
+                        const uint32_t st = nv % T::V_STAGES;
+                        wait_bar(&ctrl->v_empty[st], nv / T::V_STAGES + 1, ctrl, a.status);
+                        if (aborted(ctrl)) return;
+                        const uint32_t bar = ptx::smem_u32(&ctrl->v_full[st]);
+                        ptx::mbar_arrive_expect_tx(bar, T::V_UNIT);
 #pragma unroll
-                    for (int x = 0; x < T::SLABS; ++x)
-                        ptx::tma_load_3d(kv_smem + st * T::UNIT + x * T::SLAB, values ? mv : mk, bar, 128 * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+                        for (int x = 0; x < T::V_SLABS; ++x)
+                            ptx::tma_load_3d(kv_smem + 4 * T::SLAB + st * T::V_UNIT + x * T::SLAB, mv, bar, T::VC * u + 64 * x, s.g, z);
+                    }
+                } else {
+                    for (int u = 0; u < T::NKU; ++u, ++nk) {
+                        const uint32_t st = nk % T::K_STAGES;
+                        wait_bar(&ctrl->k_empty[st], nk / T::K_STAGES + 1, ctrl, a.status);
+                        if (aborted(ctrl)) return;
+                        const uint32_t bar = ptx::smem_u32(&ctrl->k_full[st]);
+                        ptx::mbar_arrive_expect_tx(bar, T::K_UNIT);
+#pragma unroll
+                        for (int x = 0; x < T::K_SLABS; ++x)
+                            ptx::tma_load_3d(kv_smem + st * T::K_UNIT + x * T::SLAB, mk, bar, T::KC * u + 64 * x, s.g, z);
+                    }
                 }
             });
         }
@@ -811,50 +845,102 @@ __device__ __forceinline__ void load_thread(const Args& a, Ctrl* ctrl, const CUt
         };
         for (int t = 0; t < 2; ++t)
             if (q_count[t]) landed(&ctrl->q_full[t], q_count[t] - 1);
-        for (uint32_t i = n > T::STAGES ? n - T::STAGES : 0; i < n; ++i) landed(&ctrl->kv_full[i % T::STAGES], i / T::STAGES);
+        for (uint32_t i = nk > T::K_STAGES ? nk - T::K_STAGES : 0; i < nk; ++i) landed(&ctrl->k_full[i % T::K_STAGES], i / T::K_STAGES);
+        for (uint32_t i = nv > T::V_STAGES ? nv - T::V_STAGES : 0; i < nv; ++i) landed(&ctrl->v_full[i % T::V_STAGES], i / T::V_STAGES);
     }
 }
+
+template <int N>
+struct Pieces {
+    static constexpr int value = N;
+};
 
 // Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile; a row's 16-byte pieces are then copied by neighbouring lanes.
 template <class T>
 __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* kv_smem) {
     constexpr int ELEM = T::F16 ? 1 : 2;
-    constexpr int PIECES = T::DU * ELEM / 16;               // of a key's part in a unit
-    constexpr int ITERS = PIECES;                           // 32 keys x PIECES / 32 lanes
+    constexpr int MOST = (T::KC > T::VC ? T::KC : T::VC) * ELEM / 16;      // 16-byte pieces of a key in a unit; 32 keys x pieces / 32 lanes
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
-    uint32_t segs = 0, n = 0, signalled = 0, tiles = 0;
-    // bf16: copies of LAG units are in flight.  A unit's place may wait for two more units (values are released behind the next keys' scores, or
-    // a tile's two units together), which have to be signalled by then
-    constexpr uint32_t LAG = T::STAGES - 2 < 4 ? T::STAGES - 2 : 4;
-    auto signal = [&](uint32_t unit) {
+    uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;
+    // Units whose copies are under way (bf16), or that are in registers (e4m3), oldest first: a bit for each says that it is of values
+    constexpr int LAG = T::F16 ? 1 : 2;
+    uint32_t waiting = 0, kinds = 0;
+    uint4 held[T::F16 ? MOST : 1];
+    auto settle = [&]() {                               // the oldest one is in its place
+        const bool values = (kinds >> (waiting - 1)) & 1;
+        // (the ones behind it, of the same kind, have been counted already)
+        const uint32_t later = values ? __popc(kinds & ((1u << (waiting - 1)) - 1)) : waiting - 1 - __popc(kinds & ((1u << (waiting - 1)) - 1));
+        const uint32_t unit = (values ? nv : nk) - 1 - later;
+        if (T::F16) {                                       // widened into its place
+            auto put = [&](auto pieces, uint8_t* place) {
+                constexpr int PIECES = decltype(pieces)::value;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    const int flat = i * 32 + lane, key = 32 * warp + flat / PIECES, piece = flat % PIECES;      // 16 elements
+                    const uint32_t w[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
+                    uint32_t f[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) e4m3_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+                    uint8_t* const row = place + (piece >> 2) * T::SLAB + key * 128;
+                    const int c = (piece & 3) * 2;
+                    *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
+                    *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+                }
+            };
+            if (values) {
+                wait_bar(&ctrl->v_empty[unit % T::V_STAGES], unit / T::V_STAGES + 1, ctrl, a.status);
+                put(Pieces<T::VC * ELEM / 16>(), kv_smem + 4 * T::SLAB + unit % T::V_STAGES * T::V_UNIT);
+            } else {
+                wait_bar(&ctrl->k_empty[unit % T::K_STAGES], unit / T::K_STAGES + 1, ctrl, a.status);
+                put(Pieces<T::KC * ELEM / 16>(), kv_smem + unit % T::K_STAGES * T::K_UNIT);
+            }
+        }
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) arrive(&ctrl->kv_full[unit % T::STAGES]);
-    };
-    uint4 held[T::F16 ? ITERS : 1];                         // e4m3: the unit before
-    auto settle = [&](uint32_t unit) {                      // e4m3: widens the unit held into its place
-        uint8_t* const place = kv_smem + (unit % T::STAGES) * T::UNIT;
-        wait_bar(&ctrl->kv_empty[unit % T::STAGES], unit / T::STAGES + 1, ctrl, a.status);
-#pragma unroll
-        for (int i = 0; i < (T::F16 ? ITERS : 0); ++i) {
-            const int flat = i * 32 + lane, key = 32 * warp + flat / PIECES, piece = flat % PIECES;      // 16 elements
-            const uint32_t w[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
-            uint32_t f[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e4m3_to_f16(w[j], f[2 * j], f[2 * j + 1]);
-            uint8_t* const row = place + (piece >> 2) * T::SLAB + key * 128;
-            const int c = (piece & 3) * 2;
-            *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-            *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
-        }
-        signal(unit);
+        if (lane == 0) arrive(values ? &ctrl->v_full[unit % T::V_STAGES] : &ctrl->k_full[unit % T::K_STAGES]);
+        --waiting;
     };
     auto flush = [&]() {
+        if (!T::F16) cp_wait<0>();
+        while (waiting) settle();
+    };
+    auto load = [&](auto pieces, bool values, const char* row, int u) {      // unit u of a tile; row: the lane's key
+        constexpr int PIECES = decltype(pieces)::value;
+        auto row_of = [&](int k) { return reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k)); };
         if (T::F16) {
-            if (signalled < n) settle(signalled), ++signalled;
+            uint4 got[PIECES];
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int flat = i * 32 + lane;
+                const char* const from = row_of(flat / PIECES);
+                got[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (from) got[i] = *reinterpret_cast<const uint4*>(from + u * PIECES * 16 + flat % PIECES * 16);
+            }
+            if (waiting) settle();
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) held[T::F16 ? i : 0] = got[i];
         } else {
-            cp_wait<0>();
-            for (; signalled < n; ++signalled) signal(signalled);
+            uint64_t* const empty = values ? &ctrl->v_empty[nv % T::V_STAGES] : &ctrl->k_empty[nk % T::K_STAGES];
+            const uint32_t parity = (values ? nv / T::V_STAGES : nk / T::K_STAGES) + 1;
+            // (what waits for a place may itself be waited for)
+            if (waiting && !__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(empty), parity & 1))) flush();
+            wait_bar(empty, parity, ctrl, a.status);
+            const uint32_t place = ptx::smem_u32(kv_smem) + (values ? 4 * T::SLAB + nv % T::V_STAGES * T::V_UNIT : nk % T::K_STAGES * T::K_UNIT);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int flat = i * 32 + lane, k = flat / PIECES, piece = flat % PIECES;      // 8 elements
+                const char* const from = row_of(k);
+                const uint32_t dst = place + (piece >> 3) * T::SLAB + (32 * warp + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                cp_async16(dst, from ? from + u * PIECES * 16 + piece * 16 : static_cast<const char*>(a.c.k), from != nullptr);
+            }
+            cp_commit();
+        }
+        kinds = kinds << 1 | (values ? 1u : 0u), ++waiting;
+        if (values) ++nv;
+        else ++nk;
+        if (!T::F16 && waiting > LAG) {
+            cp_wait<LAG>();
+            settle();
         }
     };
     Seg s;
@@ -886,40 +972,10 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* k
             if (ok)
                 row = values ? static_cast<const char*>(a.c.v) + (p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride) * ELEM
                              : static_cast<const char*>(a.c.k) + (p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride) * ELEM;
-            for (int u = 0; u < T::NU; ++u, ++n) {
-                if (T::F16) {
-                    uint4 got[ITERS];
-#pragma unroll
-                    for (int i = 0; i < ITERS; ++i) {
-                        const int flat = i * 32 + lane;
-                        const char* const from_row = reinterpret_cast<const char*>(
-                            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), flat / PIECES));
-                        got[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (from_row) got[i] = *reinterpret_cast<const uint4*>(from_row + u * T::DU * ELEM + flat % PIECES * 16);
-                    }
-                    if (signalled < n) settle(signalled), ++signalled;
-#pragma unroll
-                    for (int i = 0; i < ITERS; ++i) held[i] = got[i];
-                } else {
-                    const uint32_t st = n % T::STAGES;
-                    wait_bar(&ctrl->kv_empty[st], n / T::STAGES + 1, ctrl, a.status);
-                    const uint32_t place = ptx::smem_u32(kv_smem + st * T::UNIT);
-#pragma unroll
-                    for (int i = 0; i < ITERS; ++i) {
-                        const int flat = i * 32 + lane, k = flat / PIECES, piece = flat % PIECES;      // 8 elements
-                        const char* const from_row = reinterpret_cast<const char*>(
-                            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
-                        const uint32_t dst = place + (piece >> 3) * T::SLAB + (32 * warp + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
-                        cp_async16(dst, from_row ? from_row + u * T::DU * ELEM + piece * 16 : static_cast<const char*>(a.c.k), from_row != nullptr);
-                    }
-                    cp_commit();
-                    if (n - signalled >= LAG) {
-                        cp_wait<LAG>();
-                        signal(signalled);
-                        ++signalled;
-                    }
-                }
-            }
+            if (values)
+                for (int u = 0; u < T::NVU; ++u) load(Pieces<T::VC * ELEM / 16>(), true, row, u);
+            else
+                for (int u = 0; u < T::NKU; ++u) load(Pieces<T::KC * ELEM / 16>(), false, row, u);
             if (values) {      // on to the next tile
                 page[0] = page[1], page[1] = page[2], page[2] = page_of(j + 3);
                 base = j + 1;
@@ -933,137 +989,158 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* k
 }
 
 // ---------------------------------------------------------------------------------------------------------- products
+// One warp issues the scores' products, another the weighted sums': neither waits for what the other's operands wait for.  The whole warp
+// walks through its loop, so that addresses and descriptors are the same in all lanes as the compiler sees it (a tensor instruction
+// takes them from uniform registers); one lane issues.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+__device__ __forceinline__ void drain(Ctrl* ctrl, int who) {      // products under way end before shared and tensor memory are given up
+    ptx::umma_commit(ptx::smem_u32(&ctrl->drained[who]));
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (!ptx::mbar_try_wait(ptx::smem_u32(&ctrl->drained[who]), 0) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
+}
+
+// S = Q K^T for the row tiles in turn, all into one place of tensor memory, which is free again as soon as a row tile's threads have
+// their scores in registers: the next scores are there when they are done with these.
 template <class T>
-__device__ __forceinline__ void mma_thread(const Args& a, Ctrl* ctrl, uint32_t q_smem, uint32_t kv_smem, uint32_t tmem) {
-    constexpr uint32_t F = T::F16 ? ptx::UMMA_IDESC_F16 : 0u;
-    constexpr uint32_t idesc_s = ptx::umma_idesc_bf16(MT, KT) & ~F;
-    constexpr uint32_t idesc_o = (ptx::umma_idesc_bf16(MT, T::DU) & ~F) | ptx::UMMA_IDESC_B_MN_MAJOR;
-    uint32_t segs = 0, n = 0, q_count[2] = {0, 0}, p_count[2] = {0, 0}, o_uses[2] = {0, 0};
+__device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t q_smem, uint32_t kv_smem, uint32_t tmem) {
+    const bool lead = ptx::elect_one();
+    uint32_t segs = 0, n = 0, q_count[2] = {0, 0}, uses = 0;      // n: units of keys
     Seg s = {};
-    auto full = [&](uint32_t first) {      // a tile's units have landed
-        for (uint32_t u = first; u < first + T::NU; ++u) wait_bar(&ctrl->kv_full[u % T::STAGES], u / T::STAGES, ctrl, a.status);
-        ptx::tc_fence_after();
-    };
-    auto release = [&](uint32_t first) {
-        for (uint32_t u = first; u < first + T::NU; ++u) ptx::umma_commit(ptx::smem_u32(&ctrl->kv_empty[u % T::STAGES]));
-    };
-    auto scores = [&](int qt, int buf, uint32_t first) {
-        const uint32_t idesc = idesc_s | (s.negative ? ptx::UMMA_IDESC_NEGATE_B : 0u);
-#pragma unroll
-        for (int u = 0; u < T::NU; ++u) {
-            const uint32_t qa = ptx::umma_desc_lo_sw128(q_smem + (qt * T::NU + u) * T::UNIT);
-            const uint32_t ka = ptx::umma_desc_lo_sw128(kv_smem + ((first + u) % T::STAGES) * T::UNIT);
-#pragma unroll
-            for (int k = 0; k < T::DU / 16; ++k) {
-                const uint32_t add = (k >> 2) * (T::SLAB >> 4) + (k & 3) * 2;
-                if (u == 0 && k == 0) ptx::umma_bf16_lohi<false>(tmem + buf * KT, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
-                else ptx::umma_bf16_lohi<true>(tmem + buf * KT, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
+    while (next_seg(a, ctrl, segs, s, false)) {
+        const int ja = uniform(s.ja), steps = uniform(s.jb) - ja;
+        if (steps == 0) continue;
+        const uint32_t idesc = (ptx::umma_idesc_bf16(MT, KT) & ~(T::F16 ? ptx::UMMA_IDESC_F16 : 0u)) | (uniform(s.negative) ? ptx::UMMA_IDESC_NEGATE_B : 0u);
+        const bool dual = uniform(is_dual<T>(a, s));
+        int ra[2] = {0, 0}, rb[2] = {steps, steps};
+        if (dual) {
+            for (int t = 0; t < 2; ++t) {
+                range_of(a, s, true, t, ra[t], rb[t]);
+                ra[t] = uniform(ra[t]) - ja, rb[t] = uniform(rb[t]) - ja;
             }
         }
-        ptx::umma_commit(ptx::smem_u32(&ctrl->s_full[buf]));
-    };
-    auto weighted = [&](int buf, int ob, uint32_t first, bool fresh) {
-        wait_bar(&ctrl->p_ready[buf], p_count[buf], ctrl, a.status);
-        ++p_count[buf];
-        ptx::tc_fence_after();
+        auto product = [&](int qt, int t, bool loaded) {      // loaded: the tile's keys have been waited for
+            if (uses) wait_bar(&ctrl->s_free, uses - 1, ctrl, a.status);
+            ++uses;
+            ptx::tc_fence_after();
 #pragma unroll
-        for (int u = 0; u < T::NU; ++u) {
-            // values as they lie there: 64-column slabs (leading offset), groups of eight keys 1024 bytes apart
-            const uint32_t lo = (((kv_smem + ((first + u) % T::STAGES) * T::UNIT) & 0x3FFFFu) >> 4) | ((T::SLAB >> 4) << 16);
+            for (int u = 0; u < T::NKU; ++u) {
+                const uint32_t st = (n + u) % T::K_STAGES;
+                if (!loaded) {
+                    wait_bar(&ctrl->k_full[st], (n + u) / T::K_STAGES, ctrl, a.status);
+                    ptx::tc_fence_after();
+                }
+                const uint32_t qa = ptx::umma_desc_lo_sw128(q_smem + qt * T::Q_TILE + u * T::K_UNIT);
+                const uint32_t ka = ptx::umma_desc_lo_sw128(kv_smem + st * T::K_UNIT);
+                if (lead) {
 #pragma unroll
-            for (int k = 0; k < KT / 16; ++k) {
-                const uint64_t desc = (static_cast<uint64_t>(ptx::UMMA_DESC_HI_SW128) << 32) | (lo + k * (2048u >> 4));
-                ptx::umma_f16_ta(tmem + 2 * KT + ob * KT + u * 128, tmem + buf * KT + k * 8, desc, idesc_o, !fresh || k > 0);
+                    for (int k = 0; k < T::KC / 16; ++k) {
+                        const uint32_t add = (k >> 2) * (T::SLAB >> 4) + (k & 3) * 2;
+                        if (u == 0 && k == 0) ptx::umma_bf16_lohi<false>(tmem + S_COL, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
+                        else ptx::umma_bf16_lohi<true>(tmem + S_COL, qa + add, ptx::UMMA_DESC_HI_SW128, ka + add, ptx::UMMA_DESC_HI_SW128, idesc);
+                    }
+                    if (T::NKU > 1) ptx::umma_commit(ptx::smem_u32(&ctrl->k_empty[st]));
+                }
             }
-        }
-        ptx::umma_commit(ptx::smem_u32(&ctrl->o_done[ob]));
-    };
-    auto q_in = [&](int qt) {
-        wait_bar(T::F16 ? &ctrl->q_conv[qt] : &ctrl->q_full[qt], q_count[qt], ctrl, a.status);
-        ++q_count[qt];
-        ptx::tc_fence_after();
-    };
-    auto q_out = [&](int qt) { ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[qt])); };
-    auto o_in = [&](int ob) {              // the rows of the segment before have been read
-        if (o_uses[ob]) wait_bar(&ctrl->o_free[ob], o_uses[ob] - 1, ctrl, a.status);
-        ++o_uses[ob];
-    };
-    while (next_seg(a, ctrl, segs, s, true)) {
-        if (s.ja == s.jb) continue;
-        if (is_dual<T>(a, s)) {
-            int ra[2], rb[2];
-            range_of(a, s, true, 0, ra[0], rb[0]);
-            range_of(a, s, true, 1, ra[1], rb[1]);
-            auto start = [&](int t, int j, uint32_t keys) {
-                if (j == ra[t]) q_in(t);
-                scores(t, t, keys);
-                if (j == rb[t] - 1) q_out(t);
-            };
-            uint32_t keys = n;
-            n += T::NU;
-            full(keys);
-            for (int t = 0; t < 2; ++t)
-                if (s.ja >= ra[t] && s.ja < rb[t]) start(t, s.ja, keys);
-            release(keys);
-            for (int j = s.ja; j < s.jb && !aborted(ctrl); ++j) {
-                const uint32_t values = n;
-                const bool more = j + 1 < s.jb;
-                keys = n + T::NU;
-                n += more ? 2 * T::NU : T::NU;
-                full(values);
-                bool keys_in = false;
+            if (lead) ptx::umma_commit(ptx::smem_u32(&ctrl->s_full[t]));
+        };
+        auto q_in = [&](int qt) {
+            wait_bar(T::F16 ? &ctrl->q_conv[qt] : &ctrl->q_full[qt], q_count[qt], ctrl, a.status);
+            ++q_count[qt];
+            ptx::tc_fence_after();
+        };
+        for (int i = 0; i < steps; ++i) {
+            if (any_aborted(ctrl)) break;
+            if (dual) {
+                bool loaded = false;
+#pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (j >= ra[t] && j < rb[t]) {
-                        if (j == ra[t]) o_in(t);
-                        weighted(t, t, values, j == ra[t]);
-                    }
-                    if (more && j + 1 >= ra[t] && j + 1 < rb[t]) {
-                        if (!keys_in) full(keys), keys_in = true;
-                        start(t, j + 1, keys);
-                    }
+                    if (i < ra[t] || i >= rb[t]) continue;
+                    if (i == ra[t]) q_in(t);
+                    product(t, t, loaded);
+                    loaded = true;
+                    if (i == rb[t] - 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[t]));
                 }
-                release(values);
-                if (more) {
-                    if (!keys_in) full(keys);
-                    release(keys);
-                }
+                if (!loaded) wait_bar(&ctrl->k_full[n % T::K_STAGES], n / T::K_STAGES, ctrl, a.status);      // (no row tile sees them)
+            } else {
+                if (i == 0) q_in(0);
+                product(0, T::TILES == 2 ? i & 1 : 0, false);
+                if (i == steps - 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[0]));
             }
-        } else {
-            const int steps = s.jb - s.ja;
-            uint32_t keys;
-            q_in(0);
-            for (int i = 0; i < 2 && i < steps; ++i) {
-                keys = n, n += T::NU;
-                full(keys);
-                scores(0, i, keys);
-                release(keys);
-                if (i == steps - 1) q_out(0);
-            }
-            for (int i = 0; i < steps && !aborted(ctrl); ++i) {
-                const int buf = i & 1, ob = T::TILES == 2 ? buf : 0;
-                const uint32_t values = n;
-                n += T::NU;
-                full(values);
-                const bool fresh = i < T::TILES;
-                if (fresh) o_in(ob);
-                weighted(buf, ob, values, fresh);
-                release(values);
-                if (i + 2 < steps) {
-                    keys = n, n += T::NU;
-                    full(keys);
-                    scores(0, buf, keys);
-                    release(keys);
-                    if (i + 2 == steps - 1) q_out(0);
-                }
+            if (T::NKU == 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->k_empty[n % T::K_STAGES]));
+            n += T::NKU;
+        }
+        if (any_aborted(ctrl)) break;
+    }
+    if (lead && aborted(ctrl)) drain(ctrl, 0);
+    __syncwarp();
+}
+
+// O += P V
+template <class T>
+__device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t kv_smem, uint32_t tmem) {
+    constexpr uint32_t idesc = (ptx::umma_idesc_bf16(MT, T::VC) & ~(T::F16 ? ptx::UMMA_IDESC_F16 : 0u)) | ptx::UMMA_IDESC_B_MN_MAJOR;
+    const bool lead = ptx::elect_one();
+    uint32_t segs = 0, n = 0, p_count[2] = {0, 0}, o_uses[2] = {0, 0};
+    Seg s = {};
+    while (next_seg(a, ctrl, segs, s, false)) {
+        const int ja = uniform(s.ja), steps = uniform(s.jb) - ja;
+        if (steps == 0) continue;
+        const bool dual = uniform(is_dual<T>(a, s));
+        int ra[2] = {0, 0}, rb[2] = {steps, steps};
+        if (dual) {
+            for (int t = 0; t < 2; ++t) {
+                range_of(a, s, true, t, ra[t], rb[t]);
+                ra[t] = uniform(ra[t]) - ja, rb[t] = uniform(rb[t]) - ja;
             }
         }
-        if (aborted(ctrl)) break;
+        auto product = [&](int pb, int ob, bool fresh, bool loaded) {
+            if (fresh) {                       // the rows of the segment before have been read
+                if (o_uses[ob]) wait_bar(&ctrl->o_free[ob], o_uses[ob] - 1, ctrl, a.status);
+                ++o_uses[ob];
+            }
+            wait_bar(&ctrl->p_ready[pb], p_count[pb], ctrl, a.status);
+            ++p_count[pb];
+            ptx::tc_fence_after();
+#pragma unroll
+            for (int u = 0; u < T::NVU; ++u) {
+                const uint32_t st = (n + u) % T::V_STAGES;
+                if (!loaded) {
+                    wait_bar(&ctrl->v_full[st], (n + u) / T::V_STAGES, ctrl, a.status);
+                    ptx::tc_fence_after();
+                }
+                // values as they lie there: 64-column slabs (leading offset), groups of eight keys 1024 bytes apart
+                const uint32_t lo = (((kv_smem + 4 * T::SLAB + st * T::V_UNIT) & 0x3FFFFu) >> 4) | ((T::SLAB >> 4) << 16);
+                if (lead) {
+#pragma unroll
+                    for (int k = 0; k < KT / 16; ++k)
+                        ptx::umma_f16_ta(tmem + O_COL + ob * KT + u * T::VC, tmem + p_col(pb) + k * 8, lo + k * (2048u >> 4), ptx::UMMA_DESC_HI_SW128, idesc, !fresh || k > 0);
+                    if (T::NVU > 1) ptx::umma_commit(ptx::smem_u32(&ctrl->v_empty[st]));
+                }
+            }
+            if (lead) ptx::umma_commit(ptx::smem_u32(&ctrl->o_done[pb]));
+        };
+        for (int i = 0; i < steps; ++i) {
+            if (any_aborted(ctrl)) break;
+            if (dual) {
+                bool loaded = false;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (i < ra[t] || i >= rb[t]) continue;
+                    product(t, t, i == ra[t], loaded);
+                    loaded = true;
+                }
+                if (!loaded) wait_bar(&ctrl->v_full[n % T::V_STAGES], n / T::V_STAGES, ctrl, a.status);
+            } else {
+                product(i & 1, T::TILES == 2 ? i & 1 : 0, i < T::TILES, false);
+            }
+            if (T::NVU == 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->v_empty[n % T::V_STAGES]));
+            n += T::NVU;
+        }
+        if (any_aborted(ctrl)) break;
     }
-    if (aborted(ctrl)) {      // products under way end before shared and tensor memory are given up
-        ptx::umma_commit(ptx::smem_u32(&ctrl->drained));
-        const uint64_t t0 = ptx::globaltimer_ns();
-        while (!ptx::mbar_try_wait(ptx::smem_u32(&ctrl->drained), 0) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
-    }
+    if (lead && aborted(ctrl)) drain(ctrl, 1);
+    __syncwarp();
 }
 
 template <class T>
@@ -1072,21 +1149,22 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* const kv_smem = q_smem + T::Q_BYTES;
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(kv_smem + T::STAGES * T::UNIT);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(kv_smem + T::KV_BYTES);
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         auto init = [](uint64_t* bar, int n) { ptx::mbar_init(ptx::smem_u32(bar), n); };
         for (int i = 0; i < SEGS; ++i) {
             init(&ctrl->seg_full[i], 1);
-            init(&ctrl->seg_empty[i], 2 + T::WARPS_SM + T::WARPS_LD);
+            init(&ctrl->seg_empty[i], 3 + T::WARPS_SM + T::WARPS_LD);
         }
         for (int i = 0; i < 2; ++i) {
-            init(&ctrl->q_full[i], 1), init(&ctrl->q_empty[i], 1), init(&ctrl->q_conv[i], 4);
+            init(&ctrl->q_full[i], 1), init(&ctrl->q_empty[i], T::q_readers(i)), init(&ctrl->q_conv[i], 4);
             init(&ctrl->s_full[i], 1), init(&ctrl->p_ready[i], 4), init(&ctrl->o_done[i], 1), init(&ctrl->o_free[i], 4);
         }
-        for (int i = 0; i < T::STAGES; ++i) init(&ctrl->kv_full[i], T::PAGED ? 4 : 1), init(&ctrl->kv_empty[i], 1);
-        init(&ctrl->x_full, 4), init(&ctrl->drained, 1);
+        for (int i = 0; i < T::K_STAGES; ++i) init(&ctrl->k_full[i], T::PAGED ? 4 : 1), init(&ctrl->k_empty[i], 1);
+        for (int i = 0; i < T::V_STAGES; ++i) init(&ctrl->v_full[i], T::PAGED ? 4 : 1), init(&ctrl->v_empty[i], 1);
+        init(&ctrl->x_full, 4), init(&ctrl->x_empty, 4), init(&ctrl->s_free, 4), init(&ctrl->drained[0], 1), init(&ctrl->drained[1], 1);
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&mq);
@@ -1122,8 +1200,9 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             if (ptx::elect_one()) load_thread<T>(a, ctrl, &mq, &mk, &mv, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem));
             __syncwarp();
         } else if (warp == T::WARP_MMA) {
-            if (ptx::elect_one()) mma_thread<T>(a, ctrl, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem), tmem);
-            __syncwarp();
+            scores_warp<T>(a, ctrl, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem), tmem);
+        } else {
+            sums_warp<T>(a, ctrl, ptx::smem_u32(kv_smem), tmem);
         }
     } else if (T::PAGED && warp >= T::WARPS_SM) {
         if constexpr (T::SPLIT_REGS) {
