@@ -163,7 +163,7 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
  * not see do not touch its row, infinities and NaN among them (a row that meets such values beside its own is computed again, key by
  * key: slow, and right).  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are
  * rounded to bf16 for the product with the values (8-bit caches: to f16), their sum is not.  D: 64, 96, 128 or 256
- * (CAKE_ERR_UNSUPPORTED otherwise).  Pointers to q, k and v are 16-byte aligned and their strides multiples of 8 elements, at least D
+ * (CAKE_ERR_UNSUPPORTED otherwise).  q, k, v and out are 16-byte aligned and strides multiples of 8 elements, at least D
  * (CAKE_ERR_ALIGN, CAKE_ERR_SHAPE); the stride of a dimension of one element is not looked at.  Two launches.  The result depends
  * on the inputs and their sizes, not on timing.
  */

@@ -20,6 +20,13 @@ int make_map(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride
     return make_tmap_heads(m, base, D, heads, head_stride * 2, tokens, stride * 2, box_heads, box_tokens);
 }
 
+int make_map_pages(CUtensorMap* m, const void* base, const cake_paged_cache& c, i64 head, i64 token, i64 page, int box) {
+    if (c.Hkv == 1) head = c.D;
+    if (c.num_pages == 1) page = c.D;
+    if (head < c.D || token < c.D || page < c.D) return CAKE_ERR_UNSUPPORTED;      // (strides of zero: expanded tensors)
+    return make_tmap_pages(m, base, c.D, c.Hkv, head * 2, c.page_size, token * 2, c.num_pages, page * 2, box);
+}
+
 bool strides_ok(int D, i64 heads, i64 head_stride, i64 tokens, i64 stride) {
     return (heads == 1 || head_stride >= D) && (tokens <= 1 || stride >= D);
 }
@@ -36,7 +43,7 @@ int check_heads(int Hq, int Hkv, int D) {
 int prepare(Args& a, Maps& maps, int D, float scale, void* ws, size_t ws_bytes, DeviceInfo* di) {
     if (!a.q || !a.starts || !a.out) return CAKE_ERR_NULL;
     if (!aligned(a.q, 16) || !strides_aligned(a.Hq, a.q_head_stride, a.T, a.q_stride)) return CAKE_ERR_ALIGN;
-    if (!aligned(a.out, 2) || !aligned(a.lse, 4) || !aligned(a.starts, 4)) return CAKE_ERR_ALIGN;
+    if (!aligned(a.out, 16) || !aligned(a.lse, 4) || !aligned(a.starts, 4)) return CAKE_ERR_ALIGN;
     if (ws_bytes < kHeaderBytes + kSplitBytes + 2 * MOST_CTAS * part_floats(D) * 4) return CAKE_ERR_WORKSPACE;
     const int rc = current_device_info(di);
     if (rc != CAKE_OK) return rc;
@@ -48,7 +55,6 @@ int prepare(Args& a, Maps& maps, int D, float scale, void* ws, size_t ws_bytes, 
     a.entries = static_cast<i64>(a.B) * a.Hkv * a.runs;
     a.negative = scale < 0.f;
     a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
-    a.wide = aligned(a.out, 16);
     a.status = static_cast<int*>(ws);
     a.splits = reinterpret_cast<Split*>(static_cast<char*>(ws) + kHeaderBytes);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes + kSplitBytes);
@@ -149,7 +155,13 @@ int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_st
     a.B = static_cast<int>(B), a.Hq = Hq, a.Hkv = cache->Hkv, a.window = window, a.causal = true;
     rc = prepare(a, maps, cache->D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
-    maps.k = maps.v = maps.q;      // (pages are not loaded through maps)
+    // Pages come in boxes where a warp's 32 keys are whole boxes of a page: 8, 16 or 32 tokens, or 32 of a page of several times that
+    const cake_paged_cache& c = *cache;
+    a.box = c.page_size < 32 ? c.page_size : 32;
+    a.maps = c.type == CAKE_KV_BF16 && (c.page_size % 32 == 0 || c.page_size == 16 || c.page_size == 8) &&
+             make_map_pages(&maps.k, c.k, c, c.k_head_stride, c.k_token_stride, c.k_page_stride, a.box) == CAKE_OK &&
+             make_map_pages(&maps.v, c.v, c, c.v_head_stride, c.v_token_stride, c.v_page_stride, a.box) == CAKE_OK;
+    if (!a.maps) maps.k = maps.v = maps.q;      // (not used)
     return launch_any(a, maps, cache->D, cache->type == CAKE_KV_E4M3 ? PAGED_E4M3 : PAGED_BF16, di, reinterpret_cast<cudaStream_t>(stream));
 }
 

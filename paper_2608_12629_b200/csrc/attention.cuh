@@ -75,7 +75,9 @@ struct Args {
     int B, Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
-    bool negative, causal, wide;               // sign of the scale; 16-byte stores of out
+    bool negative, causal;                     // sign of the scale
+    bool maps;                                 // paged bf16: mk and mv are maps of the pages, boxes of `box` tokens
+    int box;
 };
 
 // A share of an item: what every role of a CTA is told of it.
@@ -101,15 +103,21 @@ struct Traits {
     static constexpr int NKU = D / KC, NVU = D / VC;
     static constexpr int K_SLABS = (KC + 63) / 64, V_SLABS = (VC + 63) / 64;
     static constexpr uint32_t K_UNIT = K_SLABS * SLAB, V_UNIT = V_SLABS * SLAB;
-    static constexpr int K_STAGES = 4 * SLAB / K_UNIT, V_STAGES = 4 * SLAB / V_UNIT;
+    // (8-bit caches: what has come from memory and is not widened yet takes half of the values' room)
+    static constexpr uint32_t K_BYTES = 4 * SLAB, V_BYTES = (F16 ? 2 : 4) * SLAB;
+    static constexpr int K_STAGES = K_BYTES / K_UNIT, V_STAGES = V_BYTES / V_UNIT;
+    static constexpr uint32_t RAW = SLAB;                    // 128 bytes of 128 keys
+    static constexpr int RAW_STAGES = F16 ? (TILES == 2 ? 2 : 3) : 0;
+    static constexpr uint32_t OUT_PITCH = 80;                // of a row's bytes on their way out (64, and a shift of the banks)
+    static constexpr uint32_t OUT_WARP = 32 * OUT_PITCH;
     static constexpr int WARPS_SM = 4 * TILES, WARPS_LD = PAGED ? 4 : 0;
-    static constexpr int WARP_SCHED = WARPS_SM + WARPS_LD, WARP_TMA = WARP_SCHED + 1, WARP_MMA = WARP_SCHED + 2;
+    static constexpr int WARP_SCHED = WARPS_SM + WARPS_LD, WARP_VALUES = WARP_SCHED + 1, WARP_MMA = WARP_SCHED + 2;
     static constexpr int WARPS = WARP_SCHED + 4, THREADS = 32 * WARPS;
-    static constexpr uint32_t Q_TILE = SLABS * SLAB, Q_BYTES = TILES * Q_TILE, KV_BYTES = 8 * SLAB;
+    static constexpr uint32_t Q_TILE = SLABS * SLAB, Q_BYTES = TILES * Q_TILE;
     // registers: what a block starts with (65,536 / threads), shared out again between the warpgroups
     static constexpr bool SPLIT_REGS = TILES == 2 || PAGED;
-    static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 184 : 232) : 232;
-    static constexpr int REGS_LD = TILES == 2 ? 96 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 40) : 80;
+    static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 200 : 224) : 232;
+    static constexpr int REGS_LD = TILES == 2 ? 64 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 56) : 80;
     static constexpr int REGS_START = 65536 / THREADS / 8 * 8 > 255 ? 255 : 65536 / THREADS / 8 * 8;
     static_assert(!SPLIT_REGS || TILES * REGS_SM + (PAGED ? REGS_LD : 0) + REGS_AUX <= REGS_START * (THREADS / 128), "registers of the block");
     // Who says that a tile's queries are done with.  A barrier's parity names every other load, so nobody who looks at a load may miss it:
@@ -134,16 +142,20 @@ struct __align__(16) Ctrl {
 };
 
 template <class T>
-constexpr uint32_t smem_bytes() { return 1024 + T::Q_BYTES + T::KV_BYTES + sizeof(Ctrl); }
+constexpr uint32_t smem_bytes() {
+    return 1024 + T::Q_BYTES + T::K_BYTES + T::V_BYTES + T::RAW_STAGES * T::RAW + T::WARPS_SM * T::OUT_WARP + sizeof(Ctrl);
+}
+// what a CTA's shared memory holds
+struct Room {
+    uint8_t *q, *k, *v, *raw, *out;
+};
 
 __device__ __forceinline__ bool aborted(Ctrl* ctrl) { return *reinterpret_cast<volatile int*>(&ctrl->abort_flag) != 0; }
 // the same for all lanes of a warp
 __device__ __forceinline__ bool any_aborted(Ctrl* ctrl) { return __any_sync(0xffffffffu, aborted(ctrl)); }
-__device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* ctrl, int* status) {
-    const uint32_t addr = ptx::smem_u32(bar);
-    if (ptx::mbar_try_wait(addr, parity & 1)) return;
+__device__ __forceinline__ void wait_more(uint32_t addr, uint32_t parity, Ctrl* ctrl, int* status) {
     const uint64_t t0 = ptx::globaltimer_ns();
-    while (!ptx::mbar_try_wait_hint(addr, parity & 1, 20000)) {
+    while (!ptx::mbar_try_wait_hint(addr, parity, 20000)) {
         if (aborted(ctrl)) return;
         if (ptx::globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
             *reinterpret_cast<volatile int*>(&ctrl->abort_flag) = 1;
@@ -151,6 +163,10 @@ __device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* c
             return;
         }
     }
+}
+__device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* ctrl, int* status) {
+    const uint32_t addr = ptx::smem_u32(bar);
+    if (!ptx::mbar_try_wait(addr, parity & 1)) wait_more(addr, parity & 1, ctrl, status);
 }
 __device__ __forceinline__ void arrive(uint64_t* bar) { ptx::mbar_arrive(ptx::smem_u32(bar)); }
 __device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flushed to zero
@@ -178,6 +194,11 @@ __device__ __forceinline__ void add2(float2& s, float a, float b) {
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
         : "+f"(s.x), "+f"(s.y) : "f"(a), "f"(b));
 }
+// s += 0 * (a, b): NaN once one of them is not finite
+__device__ __forceinline__ void check2(float2& s, float a, float b) {
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %4};\n\tfma.rn.f32x2 x, y, z, x;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(s.x), "+f"(s.y) : "f"(a), "f"(b), "f"(0.f));
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {      // zeros where !ok
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
@@ -197,7 +218,7 @@ struct Entry {
     int qlen, klen, g, run;
 };
 template <bool PAGED>
-__device__ __forceinline__ Entry entry_of(const Args& a, i64 e, bool report) {
+__device__ __noinline__ Entry entry_of(const Args& a, i64 e, bool report) {
     Entry n;
     const int per = a.Hkv * a.runs;
     const int b = static_cast<int>(e / per), r = static_cast<int>(e - static_cast<i64>(b) * per);
@@ -229,7 +250,7 @@ __device__ __forceinline__ void tiles_of(const Args& a, int pos, int n, int klen
 template <int TILES>
 __device__ __forceinline__ int blocks_of(const Args& a, int qlen) { return (qlen + TILES * a.tokens - 1) / (TILES * a.tokens); }
 template <int TILES>
-__device__ __forceinline__ int cost_of(const Args& a, int qlen, int klen, int block) {
+__device__ __noinline__ int cost_of(const Args& a, int qlen, int klen, int block) {
     const int per = TILES * a.tokens, tok = block * per;
     int ja, jb;
     tiles_of(a, klen - qlen + tok, min(per, qlen - tok), klen, ja, jb);
@@ -242,11 +263,13 @@ __device__ __forceinline__ i64 entry_cost(const Args& a, int qlen, int klen) {
     const int blocks = blocks_of<TILES>(a, qlen);
     i64 sum = 0;
     if (blocks <= 4)
+#pragma unroll 1
         for (int i = 0; i < blocks; ++i) sum += cost_of<TILES>(a, qlen, klen, i);
     for (unsigned todo = __ballot_sync(0xffffffffu, blocks > 4); todo; todo &= todo - 1) {
         const int who = __ffs(todo) - 1;
         const int ql = __shfl_sync(0xffffffffu, qlen, who), kl = __shfl_sync(0xffffffffu, klen, who), n = __shfl_sync(0xffffffffu, blocks, who);
         i64 s = 0;
+#pragma unroll 1
         for (int i = lane; i < n; i += 32) s += cost_of<TILES>(a, ql, kl, i);
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -266,10 +289,64 @@ __device__ __forceinline__ i64 inclusive_scan(i64 v) {
 // a share's end p tiles into an item of this cost, moved to the item's ends where they are near
 __device__ __forceinline__ int snap(int p, int cost) { return p <= SNAP ? 0 : cost - p <= SNAP ? cost : p; }
 
-// ------------------------------------------------------------------------------------------------------ scheduler
-// One warp: finds the CTA's share of the list and tells the others of its segments.
+// the tiles of keys of a segment that its row tile t sees (DUAL), or all of them
 template <class T>
-__device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl) {
+__device__ __forceinline__ bool is_dual(const Args& a, const Seg& s) { return T::TILES == 2 && s.ntok > a.tokens; }
+__device__ __forceinline__ void range_of(const Args& a, const Seg& s, bool dual, int t, int& ra, int& rb) {
+    ra = s.ja, rb = s.jb;
+    if (dual) {
+        int ja, jb;
+        const int first = t * a.tokens;
+        tiles_of(a, s.pos + first, min(a.tokens, s.ntok - first), s.klen, ja, jb);
+        ra = max(ra, ja), rb = min(rb, jb);
+        if (rb < ra) rb = ra;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ scheduler
+// One warp: finds the CTA's share of the list, tells the others of its segments, and loads their queries and (packed) keys.
+template <class T>
+__device__ __forceinline__ void load_queries_keys(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mq, const CUtensorMap* mk, const Seg& s,
+                                                  uint32_t (&q_count)[2], uint32_t& nk) {
+    const uint32_t q_bytes = T::SLABS * static_cast<uint32_t>(a.tokens * a.heads) * 128u;
+    const bool dual = is_dual<T>(a, s);
+#pragma unroll 1
+    for (int t = 0; t < (dual ? 2 : 1); ++t) {
+        int ra, rb;
+        range_of(a, s, dual, t, ra, rb);
+        if (ra == rb) continue;
+        wait_bar(&ctrl->q_empty[t], q_count[t] + 1, ctrl, a.status);
+        if (aborted(ctrl)) return;
+        ++q_count[t];
+        const uint32_t bar = ptx::smem_u32(&ctrl->q_full[t]);
+        ptx::mbar_arrive_expect_tx(bar, q_bytes);
+#pragma unroll
+        for (int x = 0; x < T::SLABS; ++x)
+            ptx::tma_load_3d(ptx::smem_u32(room.q) + t * T::Q_TILE + x * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
+    }
+    if (T::PAGED) return;
+#pragma unroll 1
+    for (int j = s.ja; j < s.jb; ++j)
+#pragma unroll 1
+        for (int u = 0; u < T::NKU; ++u, ++nk) {
+            const uint32_t st = nk % T::K_STAGES;
+            wait_bar(&ctrl->k_empty[st], nk / T::K_STAGES + 1, ctrl, a.status);
+            if (aborted(ctrl)) return;
+            const uint32_t bar = ptx::smem_u32(&ctrl->k_full[st]);
+            ptx::mbar_arrive_expect_tx(bar, T::K_UNIT);
+#pragma unroll
+            for (int x = 0; x < T::K_SLABS; ++x)
+                ptx::tma_load_3d(ptx::smem_u32(room.k) + st * T::K_UNIT + x * T::SLAB, mk, bar, T::KC * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+        }
+}
+// copies in flight land before the CTA gives up its shared memory (they have, unless a wait has expired)
+__device__ __forceinline__ void landed(uint64_t* bars, uint32_t n, uint32_t stages) {
+    const uint64_t t0 = ptx::globaltimer_ns();
+    for (uint32_t i = n > stages ? n - stages : 0; i < n; ++i)
+        while (!ptx::mbar_try_wait(ptx::smem_u32(&bars[i % stages]), (i / stages) & 1) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
+}
+template <class T>
+__device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mq, const CUtensorMap* mk) {
     constexpr int TILES = T::TILES;
     const int lane = threadIdx.x & 31;
     const unsigned all = 0xffffffffu;
@@ -279,7 +356,8 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl) {
     const i64 fit = total / MIN_SHARE;
     const int n = static_cast<int>(fit < 1 ? 1 : fit < static_cast<i64>(gridDim.x) ? fit : static_cast<i64>(gridDim.x));
     const int cta = blockIdx.x;
-    uint32_t count = 0;      // segments so far
+    uint32_t count = 0, q_count[2] = {0, 0}, nk = 0;      // segments, loads of queries, units of keys so far
+    const bool lead = ptx::elect_one();
     auto post = [&](const Seg& s) {
         const int slot = count % SEGS;
         wait_bar(&ctrl->seg_empty[slot], (count / SEGS + 1) & 1, ctrl, a.status);
@@ -353,6 +431,8 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl) {
                 if (T::F16 && a.c.k_scale && a.c.k_scale[en.g] < 0.f) s.negative ^= 1;
                 s.done = 0;
                 post(s);
+                if (lead && !aborted(ctrl)) load_queries_keys<T>(a, ctrl, room, mq, mk, s, q_count, nk);
+                __syncwarp();
                 if (any_aborted(ctrl)) break;
                 if (start == 0 && end < cost) {      // the CTAs behind this one have the rest
                     int c1 = cta;
@@ -382,6 +462,11 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl) {
     Seg last = {};
     last.done = 1;
     post(last);
+    if (lead && aborted(ctrl)) {
+        for (int t = 0; t < 2; ++t) landed(&ctrl->q_full[t], q_count[t], 1);
+        if (!T::PAGED) landed(ctrl->k_full, nk, T::K_STAGES);
+    }
+    __syncwarp();
 }
 
 // The roles' side of it: reads the next segment (whole warps, or one thread with `alone`).  False: no more.
@@ -394,20 +479,6 @@ __device__ __forceinline__ bool next_seg(const Args& a, Ctrl* ctrl, uint32_t& co
     if (alone || (threadIdx.x & 31) == 0) arrive(&ctrl->seg_empty[slot]);
     ++count;
     return !s.done;
-}
-
-// the tiles of keys of a segment that its row tile t sees (DUAL), or all of them
-template <class T>
-__device__ __forceinline__ bool is_dual(const Args& a, const Seg& s) { return T::TILES == 2 && s.ntok > a.tokens; }
-__device__ __forceinline__ void range_of(const Args& a, const Seg& s, bool dual, int t, int& ra, int& rb) {
-    ra = s.ja, rb = s.jb;
-    if (dual) {
-        int ja, jb;
-        const int first = t * a.tokens;
-        tiles_of(a, s.pos + first, min(a.tokens, s.ntok - first), s.klen, ja, jb);
-        ra = max(ra, ja), rb = min(rb, jb);
-        if (rb < ra) rb = ra;
-    }
 }
 
 // ------------------------------------------------------------------------------------------------------------ rows
@@ -447,97 +518,114 @@ __device__ __forceinline__ bool locate(const Args& a, const RowAt& r, int key, c
     return true;
 }
 template <class T>
-__device__ __noinline__ bool mend_row(const Args& a, RowAt r, float c, float top, float vs) {
+__device__ __forceinline__ bool mend_row(const Args& a, RowAt r, float c, float top, float vs) {
     constexpr int D = T::D;
     const void *k = nullptr, *v = nullptr;
     bool wrong = false;
+#pragma unroll 1
     for (int key = r.from; key < r.to && !wrong; ++key) {
         if (key >= r.k0 && key < r.k1) {
             key = r.k1 - 1;
             continue;
         }
         if (!locate<T>(a, r, key, k, v)) continue;
+#pragma unroll 1
         for (int d = 0; d < D; ++d) wrong |= !isfinite(key_at<T>(a, v, d));
     }
     if (!wrong) return false;
     float o[D], l = 0.f;
+#pragma unroll 1
     for (int d = 0; d < D; ++d) o[d] = 0.f;
+#pragma unroll 1
     for (int key = r.k0; key < r.k1; ++key) {
         if (!locate<T>(a, r, key, k, v)) continue;
         float dot = 0.f;
+#pragma unroll 1
         for (int d = 0; d < D; ++d) dot = fmaf(bf16_f(r.q[d]), key_at<T>(a, k, d), dot);
         const float p = ex2(fmaf(dot, c, -top));
         l += p;
+#pragma unroll 1
         for (int d = 0; d < D; ++d) o[d] = fmaf(p, key_at<T>(a, v, d), o[d]);
     }
     if (r.part < 0) {
         const float f = l == 0.f ? 0.f : vs / l;
+#pragma unroll 1
         for (int d = 0; d < D; ++d) a.out[r.row * D + d] = to_bf16(o[d] * f);
         if (a.lse) a.lse[r.row] = (top + log2f(l)) * LN2;
     } else {
         float* const to = a.parts + r.part * T::PART;
+#pragma unroll 1
         for (int d = 0; d < D; ++d) to[static_cast<i64>(r.part_row) * D + d] = o[d];
         to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row] = top, to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row + 1] = l;
     }
     return true;
 }
 
+// Queries of a row to f16, in place: divided by a power of two that brings its largest to [1, 2).  Returns that power.
+template <class T>
+__device__ __forceinline__ float narrow_queries(uint8_t* row, int r) {
+    float most = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < T::SLABS * 8; ++i) {
+        const uint4 u = *reinterpret_cast<const uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+    }
+    uint32_t e = __float_as_uint(most) >> 23;                   // a power of two, 2^(e - 127)
+    e = most == 0.f || e == 255 ? 127 : e < 1 ? 1 : e > 253 ? 253 : e;
+    const float inv = __uint_as_float((254 - e) << 23);
+#pragma unroll 1
+    for (int i = 0; i < T::SLABS * 8; ++i) {
+        uint4* const at = reinterpret_cast<uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
+        const uint4 u = *at;
+        *at = make_uint4(pack_f16(bf16_lo(u.x) * inv, bf16_hi(u.x) * inv), pack_f16(bf16_lo(u.y) * inv, bf16_hi(u.y) * inv),
+                         pack_f16(bf16_lo(u.z) * inv, bf16_hi(u.z) * inv), pack_f16(bf16_lo(u.w) * inv, bf16_hi(u.w) * inv));
+    }
+    return __uint_as_float(e << 23);
+}
+
 // Warpgroup t of softmax rows: thread r has row r of the tile.
 template <class T>
-__device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t* q_smem, uint32_t tmem, int t) {
+__device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Room& room, uint32_t tmem, int t) {
     constexpr int D = T::D;
-    // What is subtracted from the scores: LIFT below their maximum, which it follows when it lies SLACK behind (a smaller step would
-    // rescale O more often than it gains).  bf16 weights: any range will do.  f16 weights (8-bit values, which widen to f16 exactly): the
-    // heaviest is 2^11 to 2^15, so 11 bits are held down to 2^-25 of it
-    constexpr float LIFT = T::F16 ? 11.f : 0.f, SLACK = T::F16 ? 4.f : 8.f;
+    // What is subtracted from a row's scores, m, is the maximum of the first tile in which it sees anything; it is raised to the maximum so far
+    // only when a tile's weights add up to more than LIMIT.  So the maximum of most tiles is never looked for, and O is hardly ever
+    // rescaled: weights above 1 do no harm in 32 bits, nor rounded to bf16.  Weights in f16 (8-bit values, which widen to f16 exactly) lie LIFT higher, so
+    // that 11 bits are held down to 2^-21 of the heaviest and steps of 2^-31 below; each is at most LIMIT, which f16 holds
+    constexpr float LIFT = T::F16 ? 7.f : 0.f, LIMIT = T::F16 ? 65000.f : 1048576.f;
     const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(r & 96) << 16);
-    const int tok = r / a.heads, h = r - tok * a.heads;
+    const int tok = r / a.heads;
     uint32_t segs = 0, s_count = 0, o_count[2] = {0, 0}, q_count[2] = {0, 0}, x_count = 0, tiles = 0;      // o: products on a place of P
-    Seg s;
-    while (next_seg(a, ctrl, segs, s, false)) {
-        const bool dual = is_dual<T>(a, s);
-        int ra, rb;
-        range_of(a, s, dual, t, ra, rb);
-        const bool alt = T::TILES == 2 && !dual;
-        const int step = alt ? 2 : 1, first = alt ? ra + t : ra;
+    for (;; ++segs) {
+        // (the segment stays where it is until its end: registers are for the scores)
+        const Seg* const sp = &ctrl->seg[segs % SEGS];
+        wait_bar(&ctrl->seg_full[segs % SEGS], segs / SEGS, ctrl, a.status);
+        if (any_aborted(ctrl) || sp->done) break;
+        const bool dual = is_dual<T>(a, *sp), alt = T::TILES == 2 && !dual;
+        int first, rb;
+        range_of(a, *sp, dual, t, first, rb);
+        const int ra = first, step = alt ? 2 : 1;
+        if (alt) first += t;
         const int n_mine = first < rb ? (rb - first + step - 1) / step : 0;
         const int my_tok = (dual ? t * a.tokens : 0) + tok;                 // of the segment's tokens
-        const bool valid = tok < a.tokens && my_tok < s.ntok && h < s.heads;
-        const int pos = s.pos + my_tok;
-        // (rows that are none see what the last one does: their scores are computed, but go nowhere)
-        const int k0 = first_key(a, pos, s.klen), k1 = end_key(a, pos, s.klen);
-        const int tile_first = s.pos + (dual ? t * a.tokens : 0);
-        const int tile_last = s.pos + min(s.ntok, (dual ? (t + 1) * a.tokens : s.ntok)) - 1;
-        const int inner0 = first_key(a, tile_last, s.klen), inner1 = end_key(a, tile_first, s.klen);   // every row sees [inner0, inner1)
+        int k0, k1, inner0, inner1;                                         // the row sees [k0, k1), every row of the tile [inner0, inner1)
+        {
+            // (rows that are none see what the last one does: their scores are computed, but go nowhere)
+            const int klen = sp->klen, pos = sp->pos;
+            k0 = first_key(a, pos + my_tok, klen), k1 = end_key(a, pos + my_tok, klen);
+            inner0 = first_key(a, pos + min(sp->ntok, (dual ? (t + 1) * a.tokens : sp->ntok)) - 1, klen);
+            inner1 = end_key(a, pos + (dual ? t * a.tokens : 0), klen);
+        }
         float c = a.scale_log2;
         if (T::F16) {
-            if (a.c.k_scale) c *= fabsf(a.c.k_scale[s.g]);
-            // queries to f16, in place: divided by a power of two that brings a row's largest to [1, 2)
+            if (a.c.k_scale) c *= fabsf(a.c.k_scale[sp->g]);
             const int qt = dual ? t : 0;
-            const bool used = dual ? n_mine > 0 : s.jb > s.ja;
+            const bool used = dual ? n_mine > 0 : sp->jb > sp->ja;
             if (used && (dual || t == 0)) {
                 wait_bar(&ctrl->q_full[qt], q_count[qt], ctrl, a.status);
-                uint8_t* const row = q_smem + qt * T::Q_TILE + r * 128;
-                float most = 0.f;
-#pragma unroll 1
-                for (int i = 0; i < T::SLABS * 8; ++i) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
-                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
-                }
-                uint32_t e = __float_as_uint(most) >> 23;                   // a power of two, 2^(e - 127)
-                e = most == 0.f || e == 255 ? 127 : e < 1 ? 1 : e > 253 ? 253 : e;
-                const float inv = __uint_as_float((254 - e) << 23);
-#pragma unroll 1
-                for (int i = 0; i < T::SLABS * 8; ++i) {
-                    uint4* const at = reinterpret_cast<uint4*>(row + (i >> 3) * T::SLAB + (((i & 7) ^ (r & 7)) << 4));
-                    const uint4 u = *at;
-                    *at = make_uint4(pack_f16(bf16_lo(u.x) * inv, bf16_hi(u.x) * inv), pack_f16(bf16_lo(u.y) * inv, bf16_hi(u.y) * inv),
-                                     pack_f16(bf16_lo(u.z) * inv, bf16_hi(u.z) * inv), pack_f16(bf16_lo(u.w) * inv, bf16_hi(u.w) * inv));
-                }
-                ctrl->q_scale[qt][r] = __uint_as_float(e << 23);
+                ctrl->q_scale[qt][r] = narrow_queries<T>(room.q + qt * T::Q_TILE + r * 128, r);
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) arrive(&ctrl->q_conv[qt]);
@@ -551,7 +639,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                 bool other = !dual && used;
                 if (dual) {
                     int ua, ub;
-                    range_of(a, s, dual, 0, ua, ub);
+                    range_of(a, *sp, dual, 0, ua, ub);
                     other = ub > ua;
                     if (other) wait_bar(&ctrl->q_conv[0], q_count[0], ctrl, a.status), ++q_count[0];
                 }
@@ -561,7 +649,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
         }
         float m = NEG_INF, l = 0.f;                // m: the maximum that is subtracted, without LIFT
         for (int i = 0; i < n_mine; ++i) {
-            const int j = first + i * step;
+            const int key0 = KT * (first + i * step);
             const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
             wait_bar(&ctrl->s_full[t], s_count, ctrl, a.status);
             ++s_count;
@@ -575,18 +663,19 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive(&ctrl->s_free);
-            bool masked = KT * j < inner0 || KT * (j + 1) > inner1;
+            bool masked = key0 < inner0 || key0 + KT > inner1;
             uint4 pages = make_uint4(~0u, ~0u, ~0u, ~0u);
             if (T::PAGED) {
-                pages = ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD];
+                pages = ctrl->flags[(tiles + first + i * step - ra) % FLAGS_AHEAD];
                 masked |= (pages.x & pages.y & pages.z & pages.w) != ~0u;
             }
+            // Which rows look for their maximum: it is theirs alone to say, so that a row's bits do not depend on its neighbours
+            bool search = m == NEG_INF;
             if (masked) {
-                const int lo = k0 - KT * j, hi = k1 - KT * j;
                 const uint32_t seen[4] = {pages.x, pages.y, pages.z, pages.w};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const int b0 = min(max(lo - 32 * w, 0), 32), b1 = min(max(hi - 32 * w, 0), 32);
+                    const int b0 = min(max(k0 - key0 - 32 * w, 0), 32), b1 = min(max(k1 - key0 - 32 * w, 0), 32);
                     // bits [b0, b1)
                     const uint32_t below1 = b1 == 32 ? ~0u : (1u << b1) - 1, below0 = b0 == 32 ? ~0u : (1u << b0) - 1;
                     const uint32_t bits = seen[w] & below1 & ~below0;
@@ -595,69 +684,76 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                         if (!(bits & (1u << k))) x[w][k] = __float_as_uint(NEG_INF);
                 }
             }
-            float top[4];
+            float total;
+            for (int pass = 0;; ++pass) {
+                if (__any_sync(0xffffffffu, search)) {
+                    float top[4];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                top[w] = __uint_as_float(x[w][0]);
+                    for (int w = 0; w < 4; ++w) {
+                        top[w] = __uint_as_float(x[w][0]);
 #pragma unroll
-                for (int k = 1; k < 31; k += 2) top[w] = ptx::fmax3(top[w], __uint_as_float(x[w][k]), __uint_as_float(x[w][k + 1]));
-                top[w] = fmaxf(top[w], __uint_as_float(x[w][31]));
-            }
-            const float up = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
-            const bool higher = up > m + SLACK;                // (the first keys that are seen: m is -inf)
-            if (__any_sync(0xffffffffu, higher)) {
-                const float f = higher ? ex2(m - up) : 1.f;
-                if (higher) m = up;
-                l *= f;
-                if (i > 0) {
-                    const int ob = T::TILES == 2 ? t : 0, last = T::TILES == 2 ? t : pb ^ 1;      // the product before has to be complete
-                    wait_bar(&ctrl->o_done[last], o_count[last] - 1, ctrl, a.status);
-                    ptx::tc_fence_after();
+                        for (int k = 1; k < 31; k += 2) top[w] = ptx::fmax3(top[w], __uint_as_float(x[w][k]), __uint_as_float(x[w][k + 1]));
+                        top[w] = fmaxf(top[w], __uint_as_float(x[w][31]));
+                    }
+                    const float up = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                    const bool higher = search && up > m;
+                    const float f = higher ? ex2(m - up) : 1.f;
+                    if (higher) m = up;
+                    l *= f;
+                    if (i > 0) {
+                        const int ob = T::TILES == 2 ? t : 0, last = T::TILES == 2 ? t : pb ^ 1;      // the product before has to be complete
+                        wait_bar(&ctrl->o_done[last], o_count[last] - 1, ctrl, a.status);
+                        ptx::tc_fence_after();
 #pragma unroll 1
-                    for (int d = 0; d < D; d += 32) {
-                        uint32_t o[32];
-                        const uint32_t oa = t_lane + O_COL + ob * KT + d;
-                        ptx::tmem_ld_x32(oa, o);
-                        ptx::tmem_ld_wait(o);
+                        for (int d = 0; d < D; d += 16) {
+                            uint32_t o[16];
+                            const uint32_t oa = t_lane + O_COL + ob * KT + d;
+                            ptx::tmem_ld_x16(oa, o);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                        ptx::tmem_st_x32(oa, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            ptx::tmem_st_x16(oa, o);
+                        }
                     }
                 }
-            }
-            const float base = m == NEG_INF ? 0.f : m - LIFT;
-            // the product that read the place of the weights before is complete (looked at every time: a parity names every other one)
-            if (o_count[pb]) wait_bar(&ctrl->o_done[pb], o_count[pb] - 1, ctrl, a.status);
-            ++o_count[pb];
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const float minus = m == NEG_INF ? 0.f : LIFT - m;
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t p[16];
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    float u = __uint_as_float(x[w][k]), v = __uint_as_float(x[w][k + 1]);
-                    scale_sub2(u, v, c, -base);
-                    u = ex2(u), v = ex2(v);
-                    add2(sum[(k >> 1) & 1], u, v);
-                    // Weights are rounded to 16 bits for the tensor core (bf16: half a step of 2^-8, about what the output's own
-                    // rounding is; it is the operand type that the values have), their sum is that of the unrounded ones
-                    p[k >> 1] = T::F16 ? pack_f16(u, v) : pack_bf16(u, v);
+                    for (int k = 0; k < 16; ++k) {
+                        float u = __uint_as_float(x[w][2 * k]), v = __uint_as_float(x[w][2 * k + 1]);
+                        scale_sub2(u, v, c, minus);
+                        u = ex2(u), v = ex2(v);
+                        add2(sum[k & 1], u, v);
+                        // Weights are rounded to 16 bits for the tensor core (bf16: half a step of 2^-8, about what the output's own
+                        // rounding is; it is the operand type that the values have), their sum is that of the unrounded ones
+                        p[k] = T::F16 ? pack_f16(u, v) : pack_bf16(u, v);
+                    }
+                    // the product that read the place of the weights before is complete (looked at every time: a parity names every other one)
+                    if (w == 0 && o_count[pb]) wait_bar(&ctrl->o_done[pb], o_count[pb] - 1, ctrl, a.status);
+                    ptx::tmem_st_x16(t_lane + p_col(pb) + 16 * w, p);
                 }
-                ptx::tmem_st_x16(t_lane + p_col(pb) + 16 * w, p);
+                total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                // (the second time m is the maximum: no more than that can be done for scores so large that their differences are lost)
+                search = !search && total > LIMIT;
+                if (pass > 0 || !__any_sync(0xffffffffu, search)) break;
             }
-            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            ++o_count[pb];
+            l += total;
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive(&ctrl->p_ready[pb]);
         }
-        tiles += s.jb - s.ja;
+        const int ja = sp->ja, jb = sp->jb;
+        tiles += jb - ja;
         if (dual && t == 0) {      // (the first warpgroup counts the second tile's products too)
             int ua, ub;
-            range_of(a, s, dual, 1, ua, ub);
+            range_of(a, *sp, dual, 1, ua, ub);
             o_count[1] += ub - ua;
         }
-        const int n_other = alt ? (s.jb - s.ja) / 2 : 0;       // the second tile's steps
+        const int n_other = alt ? (jb - ja) / 2 : 0;       // the second tile's steps
         if (alt && t == 1) {
             // the first warpgroup joins
             if (n_mine) {
@@ -667,6 +763,8 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
                 if (lane == 0) arrive(&ctrl->x_full);
                 ++x_count;
             }
+            __syncwarp();
+            if (lane == 0) arrive(&ctrl->seg_empty[segs % SEGS]);
             continue;
         }
         // ---- the end of the segment
@@ -690,55 +788,85 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
             wait_bar(&ctrl->o_done[last], o_count[last] - 1, ctrl, a.status);
         }
         ptx::tc_fence_after();
+        const int g = sp->g, part_at = sp->part, h = r - tok * a.heads;
+        const bool valid = tok < a.tokens && my_tok < sp->ntok && h < sp->heads;
+        const i64 row = (sp->tok + my_tok) * a.Hq + sp->head0 + h;
         const float sub = top == NEG_INF ? NEG_INF : top - LIFT;      // what was subtracted
-        const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[s.g] : 1.f;
+        const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[g] : 1.f;
         const bool empty = l == 0.f;               // sees nothing that weighs anything: zeros, whatever the values are
-        const float inv = s.part >= 0 ? 1.f : vs / l;
+        const float inv = part_at >= 0 ? 1.f : vs / l;
         f0 *= inv, f1 *= inv;
-        const i64 row = (s.tok + my_tok) * a.Hq + s.head0 + h;
+        // Out by way of shared memory, 64 bytes of each of the warp's 32 rows at a time, so that a store covers whole sectors (16 bytes of 32
+        // rows each cost four times as much); the next 32 columns are on their way from tensor memory meanwhile
+        uint8_t* const stage = room.out + (threadIdx.x >> 5) * T::OUT_WARP;
         const int part_row = (dual ? t * MT : 0) + r;
-        float* const part = a.parts + s.part * T::PART;
-        float odd = 0.f;                           // NaN once something is not finite
+        float* const part = a.parts + part_at * T::PART;
+        uint8_t* dst[4];                           // of the rows 8 k + lane / 4, whose 16 bytes lane % 4 this lane stores
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int from = 8 * k + (lane >> 2);
+            const i64 to_row = __shfl_sync(0xffffffffu, valid ? row : -1, from);
+            uint8_t* const to = part_at >= 0 ? reinterpret_cast<uint8_t*>(part + static_cast<i64>(part_row - lane + from) * D) : reinterpret_cast<uint8_t*>(a.out + to_row * D);
+            dst[k] = to_row < 0 ? nullptr : to + (lane & 3) * 16;
+        }
+        float2 odd = make_float2(0.f, 0.f);        // NaN once something is not finite
+        uint32_t o[2][32];
+        auto fetch = [&](int d, int b) {
+            if (n_mine) ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o[b]);
+        };
+        if (!n_mine) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[0][k] = o[1][k] = 0u;
+        }
+        fetch(0, 0);
 #pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
-            uint32_t o[32], o1[32];
+        for (int d0 = 0; d0 < D; d0 += 64) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = 0u;
-            if (n_mine) {
-                ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o);
-                ptx::tmem_ld_wait(o);
-            }
+            for (int b = 0; b < 2; ++b) {
+                const int d = d0 + 32 * b;
+                if (b == 1 && d >= D) break;
+                ptx::tmem_ld_wait(o[b]);
+                if (d + 32 < D) fetch(d + 32, b ^ 1);
+                float (&f)[32] = reinterpret_cast<float (&)[32]>(o[b]);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
-            if (n_other) {
-                ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
-                ptx::tmem_ld_wait(o1);
+                for (int k = 0; k < 32; ++k) f[k] *= f0;
+                if (n_other) {
+                    uint32_t o1[32];
+                    ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
+                    ptx::tmem_ld_wait(o1);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
-            }
+                    for (int k = 0; k < 32; ++k) f[k] = fmaf(__uint_as_float(o1[k]), f1, f[k]);
+                }
 #pragma unroll
-            for (int k = 0; k < 32; ++k) odd = fmaf(__uint_as_float(o[k]), 0.f, odd);
-            if (!valid) continue;
-            if (empty) {
+                for (int k = 0; k < 32; k += 2) {
+                    check2(odd, f[k], f[k + 1]);
+                    if (empty) f[k] = f[k + 1] = 0.f;
+                }
+                uint4* const put = reinterpret_cast<uint4*>(stage + lane * T::OUT_PITCH);
+                const uint8_t* const get = stage + (lane >> 2) * T::OUT_PITCH + (lane & 3) * 16;
+                auto flush = [&](int at) {
+                    __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = 0u;
-            }
-            if (s.part >= 0) {
-                float4* const to = reinterpret_cast<float4*>(part + static_cast<i64>(part_row) * D + d);
+                    for (int k = 0; k < 4; ++k)
+                        if (dst[k]) *reinterpret_cast<uint4*>(dst[k] + at) = *reinterpret_cast<const uint4*>(get + 8 * k * T::OUT_PITCH);
+                    __syncwarp();
+                };
+                if (part_at >= 0) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    to[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
-            } else {
-                uint32_t w[16];
+                    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
-                cake_bf16* const to = a.out + row * D + d;
-                if (a.wide) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(to)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+                        for (int k = 0; k < 4; ++k) {
+                            const int e = 16 * half + 4 * k;
+                            put[k] = make_uint4(__float_as_uint(f[e]), __float_as_uint(f[e + 1]), __float_as_uint(f[e + 2]), __float_as_uint(f[e + 3]));
+                        }
+                        flush(4 * d + 64 * half);
+                    }
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) to[2 * k] = w[k] & 0xffff, to[2 * k + 1] = w[k] >> 16;
+                    for (int k = 0; k < 4; ++k)
+                        put[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]), pack_bf16(f[8 * k + 4], f[8 * k + 5]),
+                                            pack_bf16(f[8 * k + 6], f[8 * k + 7]));
+                    flush(2 * d);
                 }
             }
         }
@@ -750,32 +878,31 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, uint8_t*
         }
         if (valid) {
             bool mended = false;
-            if (isnan(odd) && isfinite(l) && !empty) {
+            if (isnan(odd.x + odd.y) && isfinite(l) && !empty) {
                 RowAt at;
-                at.row = row, at.g = s.g, at.part_row = part_row, at.part = s.part, at.base = s.k0;
-                at.q = a.q + (s.tok + my_tok) * a.q_stride + (s.head0 + h) * a.q_head_stride;
+                const int klen = sp->klen, pos = sp->pos, ntok = sp->ntok;
+                at.row = row, at.g = g, at.part_row = part_row, at.part = part_at, at.base = sp->k0;
+                at.q = a.q + (sp->tok + my_tok) * a.q_stride + (sp->head0 + h) * a.q_head_stride;
                 at.from = KT * ra, at.to = KT * rb;
-                if (T::PAGED) {                    // (what no row of the segment sees was not loaded)
-                    at.from = max(at.from, first_key(a, s.pos, s.klen)), at.to = min(at.to, end_key(a, s.pos + s.ntok - 1, s.klen));
-                }
+                if (T::PAGED)                      // (what no row of the segment sees was not loaded)
+                    at.from = max(at.from, first_key(a, pos, klen)), at.to = min(at.to, end_key(a, pos + ntok - 1, klen));
                 at.k0 = max(k0, KT * ra), at.k1 = min(k1, KT * rb);
-                float cc = s.negative ? -a.scale_log2 : a.scale_log2;
-                if (T::F16 && a.c.k_scale) cc *= fabsf(a.c.k_scale[s.g]);
+                float cc = sp->negative ? -a.scale_log2 : a.scale_log2;
+                if (T::F16 && a.c.k_scale) cc *= fabsf(a.c.k_scale[g]);
                 mended = mend_row<T>(a, at, cc, sub, vs);
             }
             if (!mended) {
-                if (s.part >= 0) {
-                    *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
-                } else if (a.lse) {
-                    a.lse[row] = l == 0.f ? NEG_INF : (sub + log2f(l)) * LN2;
-                }
+                if (part_at >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
+                else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + log2f(l)) * LN2;
             }
         }
+        __syncwarp();
+        if (lane == 0) arrive(&ctrl->seg_empty[segs % SEGS]);
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------ loads
-// The order of a segment's loads, which is about that of their use: keys of the first two tiles, then values of tile i, keys of i + 2.
+// The order in which pages are loaded, which is about that of their use: keys of the first two tiles, then values of tile i, keys of i + 2.
 // load(values, tile)
 template <class T, class F>
 __device__ __forceinline__ void loads_of(const Args& a, const Seg& s, F&& load) {
@@ -786,113 +913,85 @@ __device__ __forceinline__ void loads_of(const Args& a, const Seg& s, F&& load) 
     }
 }
 
+// Values of packed prompts: one thread
 template <class T>
-__device__ __forceinline__ void load_thread(const Args& a, Ctrl* ctrl, const CUtensorMap* mq, const CUtensorMap* mk, const CUtensorMap* mv,
-                                            uint32_t q_smem, uint32_t kv_smem) {
-    uint32_t segs = 0, q_count[2] = {0, 0}, nk = 0, nv = 0;
-    const uint32_t q_bytes = T::SLABS * static_cast<uint32_t>(a.tokens * a.heads) * 128u;
+__device__ __forceinline__ void load_values(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mv) {
+    uint32_t segs = 0, nv = 0;
     Seg s;
     while (next_seg(a, ctrl, segs, s, true)) {
-        const bool dual = is_dual<T>(a, s);
-        for (int t = 0; t < (dual ? 2 : 1); ++t) {
-            int ra, rb;
-            range_of(a, s, dual, t, ra, rb);
-            if (ra == rb) continue;
-            wait_bar(&ctrl->q_empty[t], q_count[t] + 1, ctrl, a.status);
-            if (aborted(ctrl)) break;
-            ++q_count[t];
-            const uint32_t bar = ptx::smem_u32(&ctrl->q_full[t]);
-            ptx::mbar_arrive_expect_tx(bar, q_bytes);
-#pragma unroll
-            for (int x = 0; x < T::SLABS; ++x)
-                ptx::tma_load_3d(q_smem + t * T::Q_TILE + x * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
-        }
-        if (!T::PAGED) {
-            loads_of<T>(a, s, [&](bool values, int j) {
-                const int z = static_cast<int>(s.k0) + KT * j;
-                if (values) {
-                    for (int u = 0; u < T::NVU; ++u, ++nv) {
-                        const uint32_t st = nv % T::V_STAGES;
-                        wait_bar(&ctrl->v_empty[st], nv / T::V_STAGES + 1, ctrl, a.status);
-                        if (aborted(ctrl)) return;
-                        const uint32_t bar = ptx::smem_u32(&ctrl->v_full[st]);
-                        ptx::mbar_arrive_expect_tx(bar, T::V_UNIT);
-#pragma unroll
-                        for (int x = 0; x < T::V_SLABS; ++x)
-                            ptx::tma_load_3d(kv_smem + 4 * T::SLAB + st * T::V_UNIT + x * T::SLAB, mv, bar, T::VC * u + 64 * x, s.g, z);
-                    }
-                } else {
-                    for (int u = 0; u < T::NKU; ++u, ++nk) {
-                        const uint32_t st = nk % T::K_STAGES;
-                        wait_bar(&ctrl->k_empty[st], nk / T::K_STAGES + 1, ctrl, a.status);
-                        if (aborted(ctrl)) return;
-                        const uint32_t bar = ptx::smem_u32(&ctrl->k_full[st]);
-                        ptx::mbar_arrive_expect_tx(bar, T::K_UNIT);
-#pragma unroll
-                        for (int x = 0; x < T::K_SLABS; ++x)
-                            ptx::tma_load_3d(kv_smem + st * T::K_UNIT + x * T::SLAB, mk, bar, T::KC * u + 64 * x, s.g, z);
-                    }
+#pragma unroll 1
+        for (int j = s.ja; j < s.jb; ++j)
+#pragma unroll 1
+            for (int u = 0; u < T::NVU; ++u, ++nv) {
+                const uint32_t st = nv % T::V_STAGES;
+                wait_bar(&ctrl->v_empty[st], nv / T::V_STAGES + 1, ctrl, a.status);
+                if (aborted(ctrl)) {
+                    landed(ctrl->v_full, nv, T::V_STAGES);
+                    return;
                 }
-            });
-        }
-        if (aborted(ctrl)) break;
+                const uint32_t bar = ptx::smem_u32(&ctrl->v_full[st]);
+                ptx::mbar_arrive_expect_tx(bar, T::V_UNIT);
+#pragma unroll
+                for (int x = 0; x < T::V_SLABS; ++x)
+                    ptx::tma_load_3d(ptx::smem_u32(room.v) + st * T::V_UNIT + x * T::SLAB, mv, bar, T::VC * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+            }
     }
-    // copies in flight land before the CTA gives up its shared memory (they have, unless a wait has expired)
-    if (aborted(ctrl)) {
-        const uint64_t t0 = ptx::globaltimer_ns();
-        auto landed = [&](uint64_t* bar, uint32_t parity) {
-            while (!ptx::mbar_try_wait(ptx::smem_u32(bar), parity & 1) && ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS / 4) {}
-        };
-        for (int t = 0; t < 2; ++t)
-            if (q_count[t]) landed(&ctrl->q_full[t], q_count[t] - 1);
-        for (uint32_t i = nk > T::K_STAGES ? nk - T::K_STAGES : 0; i < nk; ++i) landed(&ctrl->k_full[i % T::K_STAGES], i / T::K_STAGES);
-        for (uint32_t i = nv > T::V_STAGES ? nv - T::V_STAGES : 0; i < nv; ++i) landed(&ctrl->v_full[i % T::V_STAGES], i / T::V_STAGES);
-    }
+    if (aborted(ctrl)) landed(ctrl->v_full, nv, T::V_STAGES);
 }
 
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
 template <int N>
 struct Pieces {
     static constexpr int value = N;
 };
 
-// Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile; a row's 16-byte pieces are then copied by neighbouring lanes.
+// Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile.  bf16: 32 keys that are all there come in boxes of up to 32 tokens of a
+// page; others (the sequence's end, a window's begin, pages that are no multiple of 8) by 16-byte copies, zeros where nothing is to be
+// read.  e4m3: by 16-byte copies into a ring of their own, from where the warp that fetched them widens them.
 template <class T>
-__device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* kv_smem) {
+__device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mk, const CUtensorMap* mv) {
     constexpr int ELEM = T::F16 ? 1 : 2;
-    constexpr int MOST = (T::KC > T::VC ? T::KC : T::VC) * ELEM / 16;      // 16-byte pieces of a key in a unit; 32 keys x pieces / 32 lanes
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
     uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;
-    // Units whose copies are under way (bf16), or that are in registers (e4m3), oldest first: a bit for each says that it is of values
-    constexpr int LAG = T::F16 ? 1 : 2;
-    uint32_t waiting = 0, kinds = 0;
-    uint4 held[T::F16 ? MOST : 1];
-    auto settle = [&]() {                               // the oldest one is in its place
+    // Units whose copies are under way, oldest first: a bit for each says that it is of values
+    constexpr int LAG = T::F16 ? T::RAW_STAGES - 1 : 2;
+    uint32_t waiting = 0, kinds = 0, raw = 0;               // raw: units that were fetched into the ring
+    uint8_t* const mine = room.raw + warp * (T::RAW / 4);
+    auto settle = [&]() {                                   // the oldest one has come
         const bool values = (kinds >> (waiting - 1)) & 1;
         // (the ones behind it, of the same kind, have been counted already)
-        const uint32_t later = values ? __popc(kinds & ((1u << (waiting - 1)) - 1)) : waiting - 1 - __popc(kinds & ((1u << (waiting - 1)) - 1));
+        const uint32_t newer = __popc(kinds & ((1u << (waiting - 1)) - 1)), later = values ? newer : waiting - 1 - newer;
         const uint32_t unit = (values ? nv : nk) - 1 - later;
-        if (T::F16) {                                       // widened into its place
-            auto put = [&](auto pieces, uint8_t* place) {
+        if (T::F16) {
+            __syncwarp();
+            const uint8_t* const from = mine + (raw - waiting) % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
+            auto widen = [&](auto pieces, uint8_t* place) {
                 constexpr int PIECES = decltype(pieces)::value;
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {
                     const int flat = i * 32 + lane, key = 32 * warp + flat / PIECES, piece = flat % PIECES;      // 16 elements
-                    const uint32_t w[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
+                    const uint4 u = *reinterpret_cast<const uint4*>(from + flat * 16);
                     uint32_t f[8];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) e4m3_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+                    e4m3_to_f16(u.x, f[0], f[1]), e4m3_to_f16(u.y, f[2], f[3]), e4m3_to_f16(u.z, f[4], f[5]), e4m3_to_f16(u.w, f[6], f[7]);
+                    // (the second slab's lanes store their halves in the other order: eight lanes then meet every bank once)
+                    const int c = (piece & 3) * 2, odd = piece >> 2 & 1;
                     uint8_t* const row = place + (piece >> 2) * T::SLAB + key * 128;
-                    const int c = (piece & 3) * 2;
-                    *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(f[0], f[1], f[2], f[3]);
-                    *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(f[4], f[5], f[6], f[7]);
+                    const uint4 lo = make_uint4(f[0], f[1], f[2], f[3]), hi = make_uint4(f[4], f[5], f[6], f[7]);
+                    *reinterpret_cast<uint4*>(row + (((c + odd) ^ (key & 7)) << 4)) = odd ? hi : lo;
+                    *reinterpret_cast<uint4*>(row + (((c + 1 - odd) ^ (key & 7)) << 4)) = odd ? lo : hi;
                 }
             };
             if (values) {
                 wait_bar(&ctrl->v_empty[unit % T::V_STAGES], unit / T::V_STAGES + 1, ctrl, a.status);
-                put(Pieces<T::VC * ELEM / 16>(), kv_smem + 4 * T::SLAB + unit % T::V_STAGES * T::V_UNIT);
+                widen(Pieces<T::VC * ELEM / 16>(), room.v + unit % T::V_STAGES * T::V_UNIT);
             } else {
                 wait_bar(&ctrl->k_empty[unit % T::K_STAGES], unit / T::K_STAGES + 1, ctrl, a.status);
-                put(Pieces<T::KC * ELEM / 16>(), kv_smem + unit % T::K_STAGES * T::K_UNIT);
+                widen(Pieces<T::KC * ELEM / 16>(), room.k + unit % T::K_STAGES * T::K_UNIT);
             }
         }
         ptx::fence_proxy_async_smem();
@@ -901,44 +1000,56 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* k
         --waiting;
     };
     auto flush = [&]() {
-        if (!T::F16) cp_wait<0>();
+        cp_wait<0>();
         while (waiting) settle();
     };
-    auto load = [&](auto pieces, bool values, const char* row, int u) {      // unit u of a tile; row: the lane's key
+    // unit u of a tile; row: the lane's key; whole: all of the warp's keys are there, page and off say where
+    auto load = [&](auto pieces, bool values, const char* row, int u, bool whole, int page, int off, int g) {
         constexpr int PIECES = decltype(pieces)::value;
         auto row_of = [&](int k) { return reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k)); };
         if (T::F16) {
-            uint4 got[PIECES];
+            const uint32_t place = ptx::smem_u32(mine) + raw % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int flat = i * 32 + lane;
                 const char* const from = row_of(flat / PIECES);
-                got[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (from) got[i] = *reinterpret_cast<const uint4*>(from + u * PIECES * 16 + flat % PIECES * 16);
+                cp_async16(place + flat * 16, from ? from + u * PIECES * 16 + flat % PIECES * 16 : static_cast<const char*>(a.c.k), from != nullptr);
             }
-            if (waiting) settle();
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) held[T::F16 ? i : 0] = got[i];
+            ++raw;
         } else {
             uint64_t* const empty = values ? &ctrl->v_empty[nv % T::V_STAGES] : &ctrl->k_empty[nk % T::K_STAGES];
             const uint32_t parity = (values ? nv / T::V_STAGES : nk / T::K_STAGES) + 1;
             // (what waits for a place may itself be waited for)
             if (waiting && !__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(empty), parity & 1))) flush();
             wait_bar(empty, parity, ctrl, a.status);
-            const uint32_t place = ptx::smem_u32(kv_smem) + (values ? 4 * T::SLAB + nv % T::V_STAGES * T::V_UNIT : nk % T::K_STAGES * T::K_UNIT);
+            const uint32_t place = ptx::smem_u32(values ? room.v + nv % T::V_STAGES * T::V_UNIT : room.k + nk % T::K_STAGES * T::K_UNIT) + 32 * warp * 128;
+            if (whole) {
+                if (waiting) flush();
+                constexpr int SLABS = (PIECES + 7) / 8;
+                const uint32_t bar = ptx::smem_u32(values ? &ctrl->v_full[nv % T::V_STAGES] : &ctrl->k_full[nk % T::K_STAGES]);
+                if (lane == 0) ptx::mbar_arrive_expect_tx(bar, SLABS * 32 * 128);
+                __syncwarp();
+                const int first = lane / SLABS * a.box, x = lane % SLABS;      // of the warp's keys; slab
+                const int p = __shfl_sync(0xffffffffu, page, first & 31), o = __shfl_sync(0xffffffffu, off, first & 31);
+                if (first < 32)
+                    tma_load_4d(place + x * T::SLAB + first * 128, values ? mv : mk, bar, u * (PIECES * 8) + 64 * x, g, o, p);
+                if (values) ++nv;
+                else ++nk;
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int flat = i * 32 + lane, k = flat / PIECES, piece = flat % PIECES;      // 8 elements
                 const char* const from = row_of(k);
-                const uint32_t dst = place + (piece >> 3) * T::SLAB + (32 * warp + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                const uint32_t dst = place + (piece >> 3) * T::SLAB + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
                 cp_async16(dst, from ? from + u * PIECES * 16 + piece * 16 : static_cast<const char*>(a.c.k), from != nullptr);
             }
-            cp_commit();
         }
+        cp_commit();
         kinds = kinds << 1 | (values ? 1u : 0u), ++waiting;
         if (values) ++nv;
         else ++nk;
-        if (!T::F16 && waiting > LAG) {
+        if (waiting > LAG) {
             cp_wait<LAG>();
             settle();
         }
@@ -967,15 +1078,16 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* k
                 if (lane == 0) reinterpret_cast<uint32_t*>(&ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD])[warp] = bits;
                 if (!ok && p != INT_MIN) raise_bad_index(a.status);
             }
-            const i64 off = key % a.c.page_size;
+            const int off = key % a.c.page_size;
+            const bool whole = !T::F16 && a.maps && __all_sync(0xffffffffu, ok);
             const char* row = nullptr;
             if (ok)
                 row = values ? static_cast<const char*>(a.c.v) + (p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride) * ELEM
                              : static_cast<const char*>(a.c.k) + (p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride) * ELEM;
             if (values)
-                for (int u = 0; u < T::NVU; ++u) load(Pieces<T::VC * ELEM / 16>(), true, row, u);
+                for (int u = 0; u < T::NVU; ++u) load(Pieces<T::VC * ELEM / 16>(), true, row, u, whole, p, off, s.g);
             else
-                for (int u = 0; u < T::NKU; ++u) load(Pieces<T::KC * ELEM / 16>(), false, row, u);
+                for (int u = 0; u < T::NKU; ++u) load(Pieces<T::KC * ELEM / 16>(), false, row, u, whole, p, off, s.g);
             if (values) {      // on to the next tile
                 page[0] = page[1], page[1] = page[2], page[2] = page_of(j + 3);
                 base = j + 1;
@@ -986,6 +1098,8 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, uint8_t* k
     }
     if (!any_aborted(ctrl)) flush();
     cp_wait<0>();
+    if (!T::F16 && lane == 0 && aborted(ctrl)) landed(ctrl->k_full, nk, T::K_STAGES), landed(ctrl->v_full, nv, T::V_STAGES);
+    __syncwarp();
 }
 
 // ---------------------------------------------------------------------------------------------------------- products
@@ -1003,21 +1117,19 @@ __device__ __forceinline__ void drain(Ctrl* ctrl, int who) {      // products un
 // S = Q K^T for the row tiles in turn, all into one place of tensor memory, which is free again as soon as a row tile's threads have
 // their scores in registers: the next scores are there when they are done with these.
 template <class T>
-__device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t q_smem, uint32_t kv_smem, uint32_t tmem) {
+__device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t q_smem, uint32_t k_smem, uint32_t tmem) {
     const bool lead = ptx::elect_one();
-    uint32_t segs = 0, n = 0, q_count[2] = {0, 0}, uses = 0;      // n: units of keys
+    uint32_t segs = 0, n = 0, q0_count = 0, q1_count = 0, uses = 0;      // n: units of keys
     Seg s = {};
     while (next_seg(a, ctrl, segs, s, false)) {
         const int ja = uniform(s.ja), steps = uniform(s.jb) - ja;
         if (steps == 0) continue;
         const uint32_t idesc = (ptx::umma_idesc_bf16(MT, KT) & ~(T::F16 ? ptx::UMMA_IDESC_F16 : 0u)) | (uniform(s.negative) ? ptx::UMMA_IDESC_NEGATE_B : 0u);
         const bool dual = uniform(is_dual<T>(a, s));
-        int ra[2] = {0, 0}, rb[2] = {steps, steps};
+        int ra0 = 0, rb0 = steps, ra1 = 0, rb1 = 0;
         if (dual) {
-            for (int t = 0; t < 2; ++t) {
-                range_of(a, s, true, t, ra[t], rb[t]);
-                ra[t] = uniform(ra[t]) - ja, rb[t] = uniform(rb[t]) - ja;
-            }
+            range_of(a, s, true, 0, ra0, rb0), range_of(a, s, true, 1, ra1, rb1);
+            ra0 = uniform(ra0) - ja, rb0 = uniform(rb0) - ja, ra1 = uniform(ra1) - ja, rb1 = uniform(rb1) - ja;
         }
         auto product = [&](int qt, int t, bool loaded) {      // loaded: the tile's keys have been waited for
             if (uses) wait_bar(&ctrl->s_free, uses - 1, ctrl, a.status);
@@ -1031,7 +1143,7 @@ __device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t 
                     ptx::tc_fence_after();
                 }
                 const uint32_t qa = ptx::umma_desc_lo_sw128(q_smem + qt * T::Q_TILE + u * T::K_UNIT);
-                const uint32_t ka = ptx::umma_desc_lo_sw128(kv_smem + st * T::K_UNIT);
+                const uint32_t ka = ptx::umma_desc_lo_sw128(k_smem + st * T::K_UNIT);
                 if (lead) {
 #pragma unroll
                     for (int k = 0; k < T::KC / 16; ++k) {
@@ -1044,29 +1156,24 @@ __device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t 
             }
             if (lead) ptx::umma_commit(ptx::smem_u32(&ctrl->s_full[t]));
         };
-        auto q_in = [&](int qt) {
-            wait_bar(T::F16 ? &ctrl->q_conv[qt] : &ctrl->q_full[qt], q_count[qt], ctrl, a.status);
-            ++q_count[qt];
-            ptx::tc_fence_after();
-        };
+#pragma unroll 1
         for (int i = 0; i < steps; ++i) {
             if (any_aborted(ctrl)) break;
-            if (dual) {
-                bool loaded = false;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (i < ra[t] || i >= rb[t]) continue;
-                    if (i == ra[t]) q_in(t);
-                    product(t, t, loaded);
-                    loaded = true;
-                    if (i == rb[t] - 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[t]));
+            bool loaded = false;
+#pragma unroll 1
+            for (int t = 0; t < (dual ? 2 : 1); ++t) {
+                const int ra = t ? ra1 : ra0, rb = t ? rb1 : rb0;
+                if (i < ra || i >= rb) continue;
+                if (i == ra) {
+                    wait_bar(T::F16 ? &ctrl->q_conv[t] : &ctrl->q_full[t], t ? q1_count : q0_count, ctrl, a.status);
+                    if (t) ++q1_count;
+                    else ++q0_count;
                 }
-                if (!loaded) wait_bar(&ctrl->k_full[n % T::K_STAGES], n / T::K_STAGES, ctrl, a.status);      // (no row tile sees them)
-            } else {
-                if (i == 0) q_in(0);
-                product(0, T::TILES == 2 ? i & 1 : 0, false);
-                if (i == steps - 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[0]));
+                product(t, dual ? t : T::TILES == 2 ? i & 1 : 0, loaded);
+                loaded = true;
+                if (i == rb - 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->q_empty[t]));
             }
+            if (!loaded) wait_bar(&ctrl->k_full[n % T::K_STAGES], n / T::K_STAGES, ctrl, a.status);      // (no row tile sees them)
             if (T::NKU == 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->k_empty[n % T::K_STAGES]));
             n += T::NKU;
         }
@@ -1078,29 +1185,30 @@ __device__ __forceinline__ void scores_warp(const Args& a, Ctrl* ctrl, uint32_t 
 
 // O += P V
 template <class T>
-__device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t kv_smem, uint32_t tmem) {
+__device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t v_smem, uint32_t tmem) {
     constexpr uint32_t idesc = (ptx::umma_idesc_bf16(MT, T::VC) & ~(T::F16 ? ptx::UMMA_IDESC_F16 : 0u)) | ptx::UMMA_IDESC_B_MN_MAJOR;
     const bool lead = ptx::elect_one();
-    uint32_t segs = 0, n = 0, p_count[2] = {0, 0}, o_uses[2] = {0, 0};
+    uint32_t segs = 0, n = 0, p0_count = 0, p1_count = 0, o0_uses = 0, o1_uses = 0;      // n: units of values
     Seg s = {};
     while (next_seg(a, ctrl, segs, s, false)) {
         const int ja = uniform(s.ja), steps = uniform(s.jb) - ja;
         if (steps == 0) continue;
         const bool dual = uniform(is_dual<T>(a, s));
-        int ra[2] = {0, 0}, rb[2] = {steps, steps};
+        int ra0 = 0, rb0 = steps, ra1 = 0, rb1 = 0;
         if (dual) {
-            for (int t = 0; t < 2; ++t) {
-                range_of(a, s, true, t, ra[t], rb[t]);
-                ra[t] = uniform(ra[t]) - ja, rb[t] = uniform(rb[t]) - ja;
-            }
+            range_of(a, s, true, 0, ra0, rb0), range_of(a, s, true, 1, ra1, rb1);
+            ra0 = uniform(ra0) - ja, rb0 = uniform(rb0) - ja, ra1 = uniform(ra1) - ja, rb1 = uniform(rb1) - ja;
         }
         auto product = [&](int pb, int ob, bool fresh, bool loaded) {
             if (fresh) {                       // the rows of the segment before have been read
-                if (o_uses[ob]) wait_bar(&ctrl->o_free[ob], o_uses[ob] - 1, ctrl, a.status);
-                ++o_uses[ob];
+                const uint32_t uses = ob ? o1_uses : o0_uses;
+                if (uses) wait_bar(&ctrl->o_free[ob], uses - 1, ctrl, a.status);
+                if (ob) ++o1_uses;
+                else ++o0_uses;
             }
-            wait_bar(&ctrl->p_ready[pb], p_count[pb], ctrl, a.status);
-            ++p_count[pb];
+            wait_bar(&ctrl->p_ready[pb], pb ? p1_count : p0_count, ctrl, a.status);
+            if (pb) ++p1_count;
+            else ++p0_count;
             ptx::tc_fence_after();
 #pragma unroll
             for (int u = 0; u < T::NVU; ++u) {
@@ -1110,7 +1218,7 @@ __device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t kv
                     ptx::tc_fence_after();
                 }
                 // values as they lie there: 64-column slabs (leading offset), groups of eight keys 1024 bytes apart
-                const uint32_t lo = (((kv_smem + 4 * T::SLAB + st * T::V_UNIT) & 0x3FFFFu) >> 4) | ((T::SLAB >> 4) << 16);
+                const uint32_t lo = (((v_smem + st * T::V_UNIT) & 0x3FFFFu) >> 4) | ((T::SLAB >> 4) << 16);
                 if (lead) {
 #pragma unroll
                     for (int k = 0; k < KT / 16; ++k)
@@ -1120,20 +1228,19 @@ __device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t kv
             }
             if (lead) ptx::umma_commit(ptx::smem_u32(&ctrl->o_done[pb]));
         };
+#pragma unroll 1
         for (int i = 0; i < steps; ++i) {
             if (any_aborted(ctrl)) break;
-            if (dual) {
-                bool loaded = false;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (i < ra[t] || i >= rb[t]) continue;
-                    product(t, t, i == ra[t], loaded);
-                    loaded = true;
-                }
-                if (!loaded) wait_bar(&ctrl->v_full[n % T::V_STAGES], n / T::V_STAGES, ctrl, a.status);
-            } else {
-                product(i & 1, T::TILES == 2 ? i & 1 : 0, i < T::TILES, false);
+            bool loaded = false;
+#pragma unroll 1
+            for (int t = 0; t < (dual ? 2 : 1); ++t) {
+                const int ra = t ? ra1 : ra0, rb = t ? rb1 : rb0;
+                if (i < ra || i >= rb) continue;
+                const int at = dual ? t : i & 1;
+                product(at, T::TILES == 2 ? at : 0, dual ? i == ra : i < T::TILES, loaded);
+                loaded = true;
             }
+            if (!loaded) wait_bar(&ctrl->v_full[n % T::V_STAGES], n / T::V_STAGES, ctrl, a.status);
             if (T::NVU == 1 && lead) ptx::umma_commit(ptx::smem_u32(&ctrl->v_empty[n % T::V_STAGES]));
             n += T::NVU;
         }
@@ -1147,16 +1254,17 @@ template <class T>
 __global__ void __launch_bounds__(T::THREADS, 1)
 attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Args a) {
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* const q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    uint8_t* const kv_smem = q_smem + T::Q_BYTES;
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(kv_smem + T::KV_BYTES);
+    Room room;
+    room.q = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    room.k = room.q + T::Q_BYTES, room.v = room.k + T::K_BYTES, room.raw = room.v + T::V_BYTES, room.out = room.raw + T::RAW_STAGES * T::RAW;
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(room.out + T::WARPS_SM * T::OUT_WARP);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         auto init = [](uint64_t* bar, int n) { ptx::mbar_init(ptx::smem_u32(bar), n); };
         for (int i = 0; i < SEGS; ++i) {
             init(&ctrl->seg_full[i], 1);
-            init(&ctrl->seg_empty[i], 3 + T::WARPS_SM + T::WARPS_LD);
+            init(&ctrl->seg_empty[i], 2 + T::WARPS_SM + (T::PAGED ? T::WARPS_LD : 1));
         }
         for (int i = 0; i < 2; ++i) {
             init(&ctrl->q_full[i], 1), init(&ctrl->q_empty[i], T::q_readers(i)), init(&ctrl->q_conv[i], 4);
@@ -1168,7 +1276,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&mq);
-        if (!T::PAGED) ptx::prefetch_tensormap(&mk), ptx::prefetch_tensormap(&mv);
+        if (!T::PAGED || a.maps) ptx::prefetch_tensormap(&mk), ptx::prefetch_tensormap(&mv);
     }
     if (warp == T::WARP_MMA) {
         ptx::tmem_alloc(ptx::smem_u32(&ctrl->tmem), 512);
@@ -1195,24 +1303,24 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     if (warp >= T::WARP_SCHED) {
         if (T::SPLIT_REGS) ptx::setmaxnreg_dec<T::REGS_AUX>();
         if (warp == T::WARP_SCHED) {
-            schedule<T>(a, ctrl);
-        } else if (warp == T::WARP_TMA) {
-            if (ptx::elect_one()) load_thread<T>(a, ctrl, &mq, &mk, &mv, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem));
+            schedule<T>(a, ctrl, room, &mq, &mk);
+        } else if (warp == T::WARP_VALUES) {
+            if (!T::PAGED && ptx::elect_one()) load_values<T>(a, ctrl, room, &mv);
             __syncwarp();
         } else if (warp == T::WARP_MMA) {
-            scores_warp<T>(a, ctrl, ptx::smem_u32(q_smem), ptx::smem_u32(kv_smem), tmem);
+            scores_warp<T>(a, ctrl, ptx::smem_u32(room.q), ptx::smem_u32(room.k), tmem);
         } else {
-            sums_warp<T>(a, ctrl, ptx::smem_u32(kv_smem), tmem);
+            sums_warp<T>(a, ctrl, ptx::smem_u32(room.v), tmem);
         }
     } else if (T::PAGED && warp >= T::WARPS_SM) {
         if constexpr (T::SPLIT_REGS) {
             if constexpr (T::REGS_LD < T::REGS_START) ptx::setmaxnreg_dec<T::REGS_LD>();
             else ptx::setmaxnreg_inc<T::REGS_LD>();
         }
-        if constexpr (T::PAGED) load_pages<T>(a, ctrl, kv_smem);
+        if constexpr (T::PAGED) load_pages<T>(a, ctrl, room, &mk, &mv);
     } else {
         if (T::SPLIT_REGS) ptx::setmaxnreg_inc<T::REGS_SM>();
-        softmax_rows<T>(a, ctrl, q_smem, tmem, warp >> 2);
+        softmax_rows<T>(a, ctrl, room, tmem, warp >> 2);
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -1304,8 +1412,7 @@ attention_join_kernel(const Args a) {
             if (d >= D) continue;
             const uint2 w = make_uint2(pack_bf16(acc[v].x * f, acc[v].y * f), pack_bf16(acc[v].z * f, acc[v].w * f));
             cake_bf16* const to = a.out + out_row * D + d;
-            if (a.wide) *reinterpret_cast<uint2*>(to) = w;
-            else to[0] = w.x & 0xffff, to[1] = w.x >> 16, to[2] = w.y & 0xffff, to[3] = w.y >> 16;
+            *reinterpret_cast<uint2*>(to) = w;
         }
         if (a.lse && lane == 0) a.lse[out_row] = l == 0.f ? NEG_INF : (m + log2f(l)) * LN2;
     }
