@@ -37,8 +37,8 @@ constexpr int MT = 128;                        // rows of a tile
 constexpr int MOST_CTAS = 148;                 // that the workspace has room for parts of (two each)
 constexpr int SEGS = 4;                        // segments of work that the scheduler is ahead
 constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags are kept
-constexpr int OVERHEAD = 1;                    // tiles of keys that an item's start and end cost
-constexpr int SNAP = 2;                        // a share's end within so many tiles of an item's is moved there (> OVERHEAD)
+constexpr int OVERHEAD = 4;                    // tiles of keys that an item's start and end cost
+constexpr int SNAP = 5;                        // a share's end within so many tiles of an item's is moved there (> OVERHEAD)
 constexpr int MIN_SHARE = 2;                   // tiles
 static_assert(SNAP > OVERHEAD, "a part has at least one tile of keys");
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
@@ -107,9 +107,7 @@ struct Traits {
     static constexpr uint32_t K_BYTES = 4 * SLAB, V_BYTES = (F16 ? 2 : 4) * SLAB;
     static constexpr int K_STAGES = K_BYTES / K_UNIT, V_STAGES = V_BYTES / V_UNIT;
     static constexpr uint32_t RAW = SLAB;                    // 128 bytes of 128 keys
-    static constexpr int RAW_STAGES = F16 ? (TILES == 2 ? 2 : 3) : 0;
-    static constexpr uint32_t OUT_PITCH = 80;                // of a row's bytes on their way out (64, and a shift of the banks)
-    static constexpr uint32_t OUT_WARP = 32 * OUT_PITCH;
+    static constexpr int RAW_STAGES = F16 ? 3 : 0;
     static constexpr int WARPS_SM = 4 * TILES, WARPS_LD = PAGED ? 4 : 0;
     static constexpr int WARP_SCHED = WARPS_SM + WARPS_LD, WARP_VALUES = WARP_SCHED + 1, WARP_MMA = WARP_SCHED + 2;
     static constexpr int WARPS = WARP_SCHED + 4, THREADS = 32 * WARPS;
@@ -143,11 +141,11 @@ struct __align__(16) Ctrl {
 
 template <class T>
 constexpr uint32_t smem_bytes() {
-    return 1024 + T::Q_BYTES + T::K_BYTES + T::V_BYTES + T::RAW_STAGES * T::RAW + T::WARPS_SM * T::OUT_WARP + sizeof(Ctrl);
+    return 1024 + T::Q_BYTES + T::K_BYTES + T::V_BYTES + T::RAW_STAGES * T::RAW + sizeof(Ctrl);
 }
 // what a CTA's shared memory holds
 struct Room {
-    uint8_t *q, *k, *v, *raw, *out;
+    uint8_t *q, *k, *v, *raw;
 };
 
 __device__ __forceinline__ bool aborted(Ctrl* ctrl) { return *reinterpret_cast<volatile int*>(&ctrl->abort_flag) != 0; }
@@ -796,20 +794,11 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         const bool empty = l == 0.f;               // sees nothing that weighs anything: zeros, whatever the values are
         const float inv = part_at >= 0 ? 1.f : vs / l;
         f0 *= inv, f1 *= inv;
-        // Out by way of shared memory, 64 bytes of each of the warp's 32 rows at a time, so that a store covers whole sectors (16 bytes of 32
-        // rows each cost four times as much); the next 32 columns are on their way from tensor memory meanwhile
-        uint8_t* const stage = room.out + (threadIdx.x >> 5) * T::OUT_WARP;
         const int part_row = (dual ? t * MT : 0) + r;
         float* const part = a.parts + part_at * T::PART;
-        uint8_t* dst[4];                           // of the rows 8 k + lane / 4, whose 16 bytes lane % 4 this lane stores
+        float2 odd[4];                             // NaN once something is not finite
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int from = 8 * k + (lane >> 2);
-            const i64 to_row = __shfl_sync(0xffffffffu, valid ? row : -1, from);
-            uint8_t* const to = part_at >= 0 ? reinterpret_cast<uint8_t*>(part + static_cast<i64>(part_row - lane + from) * D) : reinterpret_cast<uint8_t*>(a.out + to_row * D);
-            dst[k] = to_row < 0 ? nullptr : to + (lane & 3) * 16;
-        }
-        float2 odd = make_float2(0.f, 0.f);        // NaN once something is not finite
+        for (int k = 0; k < 4; ++k) odd[k] = make_float2(0.f, 0.f);
         uint32_t o[2][32];
         auto fetch = [&](int d, int b) {
             if (n_mine) ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o[b]);
@@ -839,34 +828,21 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 }
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) {
-                    check2(odd, f[k], f[k + 1]);
+                    check2(odd[(k >> 1) & 3], f[k], f[k + 1]);
                     if (empty) f[k] = f[k + 1] = 0.f;
                 }
-                uint4* const put = reinterpret_cast<uint4*>(stage + lane * T::OUT_PITCH);
-                const uint8_t* const get = stage + (lane >> 2) * T::OUT_PITCH + (lane & 3) * 16;
-                auto flush = [&](int at) {
-                    __syncwarp();
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (dst[k]) *reinterpret_cast<uint4*>(dst[k] + at) = *reinterpret_cast<const uint4*>(get + 8 * k * T::OUT_PITCH);
-                    __syncwarp();
-                };
+                // (by way of shared memory, in whole sectors: no faster)
+                if (!valid) continue;
                 if (part_at >= 0) {
+                    float4* const to = reinterpret_cast<float4*>(part + static_cast<i64>(part_row) * D + d);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int e = 16 * half + 4 * k;
-                            put[k] = make_uint4(__float_as_uint(f[e]), __float_as_uint(f[e + 1]), __float_as_uint(f[e + 2]), __float_as_uint(f[e + 3]));
-                        }
-                        flush(4 * d + 64 * half);
-                    }
+                    for (int k = 0; k < 8; ++k) to[k] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
                 } else {
+                    uint4* const to = reinterpret_cast<uint4*>(a.out + row * D + d);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        put[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]), pack_bf16(f[8 * k + 4], f[8 * k + 5]),
-                                            pack_bf16(f[8 * k + 6], f[8 * k + 7]));
-                    flush(2 * d);
+                        to[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]), pack_bf16(f[8 * k + 4], f[8 * k + 5]),
+                                           pack_bf16(f[8 * k + 6], f[8 * k + 7]));
                 }
             }
         }
@@ -878,7 +854,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         }
         if (valid) {
             bool mended = false;
-            if (isnan(odd.x + odd.y) && isfinite(l) && !empty) {
+            if (isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y)) && isfinite(l) && !empty) {
                 RowAt at;
                 const int klen = sp->klen, pos = sp->pos, ntok = sp->ntok;
                 at.row = row, at.g = g, at.part_row = part_row, at.part = part_at, at.base = sp->k0;
@@ -893,7 +869,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             }
             if (!mended) {
                 if (part_at >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
-                else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + log2f(l)) * LN2;
+                else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + __log2f(l)) * LN2;
             }
         }
         __syncwarp();
@@ -1256,8 +1232,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     Room room;
     room.q = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    room.k = room.q + T::Q_BYTES, room.v = room.k + T::K_BYTES, room.raw = room.v + T::V_BYTES, room.out = room.raw + T::RAW_STAGES * T::RAW;
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(room.out + T::WARPS_SM * T::OUT_WARP);
+    room.k = room.q + T::Q_BYTES, room.v = room.k + T::K_BYTES, room.raw = room.v + T::V_BYTES;
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(room.raw + T::RAW_STAGES * T::RAW);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
