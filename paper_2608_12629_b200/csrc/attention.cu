@@ -40,7 +40,7 @@ int check_heads(int Hq, int Hkv, int D) {
 }
 
 // what both entry points share: everything of a but the keys
-int prepare(Args& a, Maps& maps, int D, float scale, void* ws, size_t ws_bytes, DeviceInfo* di) {
+int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_bytes, DeviceInfo* di) {
     if (!a.q || !a.starts || !a.out) return CAKE_ERR_NULL;
     if (!aligned(a.q, 16) || !strides_aligned(a.Hq, a.q_head_stride, a.T, a.q_stride)) return CAKE_ERR_ALIGN;
     if (!aligned(a.out, 16) || !aligned(a.lse, 4) || !aligned(a.starts, 4)) return CAKE_ERR_ALIGN;
@@ -52,7 +52,8 @@ int prepare(Args& a, Maps& maps, int D, float scale, void* ws, size_t ws_bytes, 
     a.runs = (a.G + MT - 1) / MT;
     a.heads = (a.G + a.runs - 1) / a.runs;
     a.tokens = MT / a.heads;
-    a.entries = static_cast<i64>(a.B) * a.Hkv * a.runs;
+    if (B > INT_MAX / 64 / (static_cast<i64>(a.Hkv) * a.runs)) return CAKE_ERR_SHAPE;
+    a.entries = static_cast<int>(B) * a.Hkv * a.runs;
     a.negative = scale < 0.f;
     a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
     a.status = static_cast<int*>(ws);
@@ -113,8 +114,8 @@ int cake_prompt_attention(const cake_bf16* q, long long q_stride, long long q_he
     a.q = q, a.k = k, a.v = v, a.starts = starts, a.k_starts = k_starts ? k_starts : starts, a.out = out, a.lse = out_lse;
     a.T = T, a.Tk = Tk, a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.k_stride = k_stride, a.k_head_stride = k_head_stride;
     a.v_stride = v_stride, a.v_head_stride = v_head_stride;
-    a.B = static_cast<int>(B), a.Hq = Hq, a.Hkv = Hkv, a.window = window, a.causal = flags & CAKE_ATTENTION_CAUSAL;
-    rc = prepare(a, maps, D, scale, ws, ws_bytes, &di);
+    a.Hq = Hq, a.Hkv = Hkv, a.window = window, a.causal = flags & CAKE_ATTENTION_CAUSAL;
+    rc = prepare(a, maps, B, D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
     if (Tk == 0) {      // (no keys at all: nothing is loaded, any map will do)
         maps.k = maps.v = maps.q;
@@ -152,8 +153,8 @@ int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_st
     a.q = q, a.starts = starts, a.table = page_table, a.lens = seq_lens, a.out = out, a.lse = out_lse;
     a.T = T, a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.table_stride = table_stride, a.table_head_stride = table_head_stride;
     a.lens_stride = lens_stride, a.lens_head_stride = lens_head_stride, a.max_pages = max_pages;
-    a.B = static_cast<int>(B), a.Hq = Hq, a.Hkv = cache->Hkv, a.window = window, a.causal = true;
-    rc = prepare(a, maps, cache->D, scale, ws, ws_bytes, &di);
+    a.Hq = Hq, a.Hkv = cache->Hkv, a.window = window, a.causal = true;
+    rc = prepare(a, maps, B, cache->D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
     // Pages come in boxes where a warp's 32 keys are whole boxes of a page: 8, 16 or 32 tokens, or 32 of a page of several times that
     const cake_paged_cache& c = *cache;

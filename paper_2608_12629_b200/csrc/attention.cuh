@@ -49,7 +49,6 @@ constexpr float NEG_INF = -INFINITY;
 // Tensor memory: scores of one row tile between the weights (16 bits) of two, then the weighted sums (of the one row tile: both places)
 constexpr uint32_t S_COL = KT / 2, O_COL = 2 * KT;
 __device__ __forceinline__ uint32_t p_col(int pb) { return pb ? KT / 2 + KT : 0; }
-constexpr int AHEAD = 2;                       // tiles of keys that are loaded ahead of the first values
 
 enum Kind { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
 
@@ -71,8 +70,8 @@ struct Args {
     Split* splits;
     i64 T, Tk, q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
     i64 table_stride, table_head_stride, lens_stride, lens_head_stride;
-    i64 entries;                               // sequences * key-value heads * runs
-    int B, Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
+    int entries;                               // sequences * key-value heads * runs
+    int Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
     bool negative, causal;                     // sign of the scale
@@ -114,8 +113,8 @@ struct Traits {
     static constexpr uint32_t Q_TILE = SLABS * SLAB, Q_BYTES = TILES * Q_TILE;
     // registers: what a block starts with (65,536 / threads), shared out again between the warpgroups
     static constexpr bool SPLIT_REGS = TILES == 2 || PAGED;
-    static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 200 : 224) : 232;
-    static constexpr int REGS_LD = TILES == 2 ? 64 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 56) : 80;
+    static constexpr int REGS_SM = TILES == 2 ? (PAGED ? 184 : 224) : 232;
+    static constexpr int REGS_LD = TILES == 2 ? 96 : 192, REGS_AUX = TILES == 2 ? (PAGED ? 48 : 56) : 80;
     static constexpr int REGS_START = 65536 / THREADS / 8 * 8 > 255 ? 255 : 65536 / THREADS / 8 * 8;
     static_assert(!SPLIT_REGS || TILES * REGS_SM + (PAGED ? REGS_LD : 0) + REGS_AUX <= REGS_START * (THREADS / 128), "registers of the block");
     // Who says that a tile's queries are done with.  A barrier's parity names every other load, so nobody who looks at a load may miss it:
@@ -216,10 +215,10 @@ struct Entry {
     int qlen, klen, g, run;
 };
 template <bool PAGED>
-__device__ __noinline__ Entry entry_of(const Args& a, i64 e, bool report) {
+__device__ __noinline__ Entry entry_of(const Args& a, int e, bool report) {
     Entry n;
     const int per = a.Hkv * a.runs;
-    const int b = static_cast<int>(e / per), r = static_cast<int>(e - static_cast<i64>(b) * per);
+    const int b = e / per, r = e - b * per;
     n.g = r / a.runs, n.run = r - n.g * a.runs;
     const int s0 = a.starts[b], s1 = a.starts[b + 1];
     bool bad = s0 < 0 || s1 < s0 || s1 > a.T;
@@ -302,6 +301,8 @@ __device__ __forceinline__ void range_of(const Args& a, const Seg& s, bool dual,
 }
 
 // ------------------------------------------------------------------------------------------------------ scheduler
+template <class T>
+__device__ __forceinline__ int stretch_of(const Args& a) { return (a.entries + T::WARPS - 1) / T::WARPS; }      // entries that a warp adds up
 // One warp: finds the CTA's share of the list, tells the others of its segments, and loads their queries and (packed) keys.
 template <class T>
 __device__ __forceinline__ void load_queries_keys(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mq, const CUtensorMap* mk, const Seg& s,
@@ -348,11 +349,13 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     constexpr int TILES = T::TILES;
     const int lane = threadIdx.x & 31;
     const unsigned all = 0xffffffffu;
-    i64 total = 0;
-#pragma unroll
-    for (int w = 0; w < T::WARPS; ++w) total += ctrl->sums[w];
-    const i64 fit = total / MIN_SHARE;
-    const int n = static_cast<int>(fit < 1 ? 1 : fit < static_cast<i64>(gridDim.x) ? fit : static_cast<i64>(gridDim.x));
+    // the stretches' sums, added up
+    const i64 sums = inclusive_scan(lane < T::WARPS ? ctrl->sums[lane] : 0);
+    const i64 total = __shfl_sync(all, sums, 31);
+    const int n = total < static_cast<i64>(MIN_SHARE) * gridDim.x ? max(static_cast<int>(total) / MIN_SHARE, 1) : static_cast<int>(gridDim.x);
+    const i64 whole = total / n;
+    const int over = static_cast<int>(total - whole * n);
+    auto begin_of = [&](int c) { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(n); };      // of CTA c's share: floor(total c / n)
     const int cta = blockIdx.x;
     uint32_t count = 0, q_count[2] = {0, 0}, nk = 0;      // segments, loads of queries, units of keys so far
     const bool lead = ptx::elect_one();
@@ -368,46 +371,33 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     };
     Split split = {};
     if (cta < n && total > 0) {
-        const i64 x0 = total * cta / n, x1 = cta == n - 1 ? total : total * (cta + 1) / n;
-        // the entry that x0 is in
-        i64 before = 0, e = 0, e_end = 0;
-        for (int w = 0; w < T::WARPS; ++w) {
-            const i64 s = ctrl->sums[w];
-            if (x0 < before + s) {
-                e = a.entries * w / T::WARPS, e_end = a.entries * (w + 1) / T::WARPS;
-                break;
-            }
-            before += s;
-        }
-        for (;; e += 32) {
-            Entry en = {};
-            if (e + lane < e_end) en = entry_of<T::PAGED>(a, e + lane, false);
-            const i64 cost = entry_cost<TILES>(a, en.qlen, en.klen);
+        const i64 x0 = begin_of(cta), x1 = begin_of(cta + 1);
+        // the entry that x0 is in: its stretch first
+        const unsigned behind = __ballot_sync(all, x0 < sums);
+        const int w = __ffs(behind) - 1;
+        i64 before = w > 0 ? __shfl_sync(all, sums, (w - 1) & 31) : 0;
+        const int stretch = stretch_of<T>(a), e_end = min(stretch * (w + 1), a.entries);
+        int e = stretch * w, block = 0;
+        Entry en = {};
+        // lanes look at 32 entries, then at 32 items of one, at a time
+        auto find = [&](i64 cost) {
             const i64 upto = inclusive_scan(cost);
             const unsigned hit = __ballot_sync(all, x0 < before + upto);
-            if (hit) {
-                const int who = __ffs(hit) - 1;
-                e += who;
-                before += __shfl_sync(all, upto - cost, who);
-                break;
-            }
-            before += __shfl_sync(all, upto, 31);
-            if (e + 32 >= e_end) break;      // (cannot be: the sums say that it is here)
+            const int who = hit ? __ffs(hit) - 1 : 32;
+            before += __shfl_sync(all, hit ? upto - cost : upto, hit ? who : 31);
+            return who;
+        };
+#pragma unroll 1
+        for (int who = 32; who == 32 && e < e_end; e += who) {
+            Entry one = {};
+            if (e + lane < e_end) one = entry_of<T::PAGED>(a, e + lane, false);
+            who = find(entry_cost<TILES>(a, one.qlen, one.klen));
         }
-        Entry en = entry_of<T::PAGED>(a, e, false);
-        int blocks = blocks_of<TILES>(a, en.qlen), block = 0;
-        for (; block < blocks; block += 32) {      // the item of the entry
-            const i64 cost = block + lane < blocks ? cost_of<TILES>(a, en.qlen, en.klen, block + lane) : 0;
-            const i64 upto = inclusive_scan(cost);
-            const unsigned hit = __ballot_sync(all, x0 < before + upto);
-            if (hit) {
-                const int who = __ffs(hit) - 1;
-                block += who;
-                before += __shfl_sync(all, upto - cost, who);
-                break;
-            }
-            before += __shfl_sync(all, upto, 31);
-        }
+        en = entry_of<T::PAGED>(a, e, false);
+        int blocks = blocks_of<TILES>(a, en.qlen);
+#pragma unroll 1
+        for (int who = blocks > 1 ? 32 : 0; who == 32 && block < blocks; block += who)
+            who = find(block + lane < blocks ? cost_of<TILES>(a, en.qlen, en.klen, block + lane) : 0);
         int start = -1;
         while (x1 > before && block < blocks) {
             const int per = TILES * a.tokens, tok = block * per, ntok = min(per, en.qlen - tok);
@@ -434,8 +424,9 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
                 if (any_aborted(ctrl)) break;
                 if (start == 0 && end < cost) {      // the CTAs behind this one have the rest
                     int c1 = cta;
+#pragma unroll 1
                     for (int c = cta + 1; c < n; c += 32) {
-                        const i64 x = c + lane < n ? total * (c + lane) / n : total;
+                        const i64 x = c + lane < n ? begin_of(c + lane) : total;
                         const unsigned in = __ballot_sync(all, before + cost - x > SNAP);
                         c1 += __popc(in);
                         if (in != all) break;
@@ -683,6 +674,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 }
             }
             float total;
+#pragma unroll 1                               // (one copy of this: the loops are about what the instruction caches hold)
             for (int pass = 0;; ++pass) {
                 if (__any_sync(0xffffffffu, search)) {
                     float top[4];
@@ -878,17 +870,6 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
 }
 
 // ------------------------------------------------------------------------------------------------------------ loads
-// The order in which pages are loaded, which is about that of their use: keys of the first two tiles, then values of tile i, keys of i + 2.
-// load(values, tile)
-template <class T, class F>
-__device__ __forceinline__ void loads_of(const Args& a, const Seg& s, F&& load) {
-    for (int i = 0; i < AHEAD && s.ja + i < s.jb; ++i) load(false, s.ja + i);
-    for (int j = s.ja; j < s.jb; ++j) {
-        load(true, j);
-        if (j + AHEAD < s.jb) load(false, j + AHEAD);
-    }
-}
-
 // Values of packed prompts: one thread
 template <class T>
 __device__ __forceinline__ void load_values(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mv) {
@@ -921,11 +902,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
-template <int N>
-struct Pieces {
-    static constexpr int value = N;
-};
-
 // Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile.  bf16: 32 keys that are all there come in boxes of up to 32 tokens of a
 // page; others (the sequence's end, a window's begin, pages that are no multiple of 8) by 16-byte copies, zeros where nothing is to be
 // read.  e4m3: by 16-byte copies into a ring of their own, from where the warp that fetched them widens them.
@@ -933,146 +909,132 @@ template <class T>
 __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mk, const CUtensorMap* mv) {
     constexpr int ELEM = T::F16 ? 1 : 2;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
-    uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;
-    // Units whose copies are under way, oldest first: a bit for each says that it is of values
-    constexpr int LAG = T::F16 ? T::RAW_STAGES - 1 : 2;
-    uint32_t waiting = 0, kinds = 0, raw = 0;               // raw: units that were fetched into the ring
+    uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;           // segments, units of keys and of values, tiles so far
+    // e4m3: units that were fetched into the ring and are not widened yet, oldest first: a bit for each says that it is of values
+    constexpr int LAG = T::F16 ? T::RAW_STAGES - 1 : 0;
+    uint32_t waiting = 0, kinds = 0, raw = 0;               // raw: units that were fetched
     uint8_t* const mine = room.raw + warp * (T::RAW / 4);
-    auto settle = [&]() {                                   // the oldest one has come
-        const bool values = (kinds >> (waiting - 1)) & 1;
-        // (the ones behind it, of the same kind, have been counted already)
-        const uint32_t newer = __popc(kinds & ((1u << (waiting - 1)) - 1)), later = values ? newer : waiting - 1 - newer;
-        const uint32_t unit = (values ? nv : nk) - 1 - later;
-        if (T::F16) {
-            __syncwarp();
-            const uint8_t* const from = mine + (raw - waiting) % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
-            auto widen = [&](auto pieces, uint8_t* place) {
-                constexpr int PIECES = decltype(pieces)::value;
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) {
-                    const int flat = i * 32 + lane, key = 32 * warp + flat / PIECES, piece = flat % PIECES;      // 16 elements
-                    const uint4 u = *reinterpret_cast<const uint4*>(from + flat * 16);
-                    uint32_t f[8];
-                    e4m3_to_f16(u.x, f[0], f[1]), e4m3_to_f16(u.y, f[2], f[3]), e4m3_to_f16(u.z, f[4], f[5]), e4m3_to_f16(u.w, f[6], f[7]);
-                    // (the second slab's lanes store their halves in the other order: eight lanes then meet every bank once)
-                    const int c = (piece & 3) * 2, odd = piece >> 2 & 1;
-                    uint8_t* const row = place + (piece >> 2) * T::SLAB + key * 128;
-                    const uint4 lo = make_uint4(f[0], f[1], f[2], f[3]), hi = make_uint4(f[4], f[5], f[6], f[7]);
-                    *reinterpret_cast<uint4*>(row + (((c + odd) ^ (key & 7)) << 4)) = odd ? hi : lo;
-                    *reinterpret_cast<uint4*>(row + (((c + 1 - odd) ^ (key & 7)) << 4)) = odd ? lo : hi;
-                }
-            };
-            if (values) {
-                wait_bar(&ctrl->v_empty[unit % T::V_STAGES], unit / T::V_STAGES + 1, ctrl, a.status);
-                widen(Pieces<T::VC * ELEM / 16>(), room.v + unit % T::V_STAGES * T::V_UNIT);
-            } else {
-                wait_bar(&ctrl->k_empty[unit % T::K_STAGES], unit / T::K_STAGES + 1, ctrl, a.status);
-                widen(Pieces<T::KC * ELEM / 16>(), room.k + unit % T::K_STAGES * T::K_UNIT);
-            }
-        }
-        ptx::fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) arrive(values ? &ctrl->v_full[unit % T::V_STAGES] : &ctrl->k_full[unit % T::K_STAGES]);
-        --waiting;
+    Seg s = {};
+    int from = 0, to = 0, ik = 0, iv = 0, u = 0;            // keys that some row of the item sees; tiles whose keys, values come next; unit of the tile
+    int page[3] = {INT_MIN, INT_MIN, INT_MIN};              // of the lane's key in tiles iv, iv + 1, iv + 2; INT_MIN: not to be read
+    bool more = true;
+    auto page_of = [&](int j) {
+        const int key = KT * j + 32 * warp + lane;
+        return j < s.jb && key >= from && key < to ? max(a.table[s.k0 + key / a.c.page_size], -1) : INT_MIN;
     };
-    auto flush = [&]() {
-        cp_wait<0>();
-        while (waiting) settle();
-    };
-    // unit u of a tile; row: the lane's key; whole: all of the warp's keys are there, page and off say where
-    auto load = [&](auto pieces, bool values, const char* row, int u, bool whole, int page, int off, int g) {
-        constexpr int PIECES = decltype(pieces)::value;
-        auto row_of = [&](int k) { return reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k)); };
-        if (T::F16) {
-            const uint32_t place = ptx::smem_u32(mine) + raw % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const int flat = i * 32 + lane;
-                const char* const from = row_of(flat / PIECES);
-                cp_async16(place + flat * 16, from ? from + u * PIECES * 16 + flat % PIECES * 16 : static_cast<const char*>(a.c.k), from != nullptr);
-            }
-            ++raw;
-        } else {
-            uint64_t* const empty = values ? &ctrl->v_empty[nv % T::V_STAGES] : &ctrl->k_empty[nk % T::K_STAGES];
-            const uint32_t parity = (values ? nv / T::V_STAGES : nk / T::K_STAGES) + 1;
-            // (what waits for a place may itself be waited for)
-            if (waiting && !__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(empty), parity & 1))) flush();
-            wait_bar(empty, parity, ctrl, a.status);
-            const uint32_t place = ptx::smem_u32(values ? room.v + nv % T::V_STAGES * T::V_UNIT : room.k + nk % T::K_STAGES * T::K_UNIT) + 32 * warp * 128;
-            if (whole) {
-                if (waiting) flush();
-                constexpr int SLABS = (PIECES + 7) / 8;
-                const uint32_t bar = ptx::smem_u32(values ? &ctrl->v_full[nv % T::V_STAGES] : &ctrl->k_full[nk % T::K_STAGES]);
-                if (lane == 0) ptx::mbar_arrive_expect_tx(bar, SLABS * 32 * 128);
-                __syncwarp();
-                const int first = lane / SLABS * a.box, x = lane % SLABS;      // of the warp's keys; slab
-                const int p = __shfl_sync(0xffffffffu, page, first & 31), o = __shfl_sync(0xffffffffu, off, first & 31);
-                if (first < 32)
-                    tma_load_4d(place + x * T::SLAB + first * 128, values ? mv : mk, bar, u * (PIECES * 8) + 64 * x, g, o, p);
-                if (values) ++nv;
-                else ++nk;
-                return;
-            }
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const int flat = i * 32 + lane, k = flat / PIECES, piece = flat % PIECES;      // 8 elements
-                const char* const from = row_of(k);
-                const uint32_t dst = place + (piece >> 3) * T::SLAB + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
-                cp_async16(dst, from ? from + u * PIECES * 16 + piece * 16 : static_cast<const char*>(a.c.k), from != nullptr);
-            }
-        }
-        cp_commit();
-        kinds = kinds << 1 | (values ? 1u : 0u), ++waiting;
-        if (values) ++nv;
-        else ++nk;
-        if (waiting > LAG) {
-            cp_wait<LAG>();
-            settle();
-        }
-    };
-    Seg s;
     for (;;) {
-        // (what is still under way is waited for before the warp waits for more work)
-        if (!__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(&ctrl->seg_full[segs % SEGS]), (segs / SEGS) & 1))) flush();
-        if (!next_seg(a, ctrl, segs, s, false)) break;
-        // keys that some row of the item sees; no others are read
-        const int from = first_key(a, s.pos, s.klen), to = end_key(a, s.pos + s.ntok - 1, s.klen);
-        auto page_of = [&](int j) {
-            const int key = KT * j + 32 * warp + lane;
-            return j < s.jb && key >= from && key < to ? max(a.table[s.k0 + key / a.c.page_size], -1) : INT_MIN;
-        };
-        // the pages of the next tiles' keys are looked up ahead: [0] the tile whose values come next, [2] the furthest
-        int page[4] = {page_of(s.ja), page_of(s.ja + 1), page_of(s.ja + 2), INT_MIN};
-        int base = s.ja;
-        loads_of<T>(a, s, [&](bool values, int j) {
-            if (any_aborted(ctrl)) return;
-            const int p = j == base ? page[0] : j == base + 1 ? page[1] : page[2];
-            const int key = KT * j + 32 * warp + lane;
+        if (more && iv == s.jb) {                           // a new segment (what is still under way is settled before the warp waits for one)
+            if (waiting == 0 || __all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(&ctrl->seg_full[segs % SEGS]), (segs / SEGS) & 1))) {
+                tiles += s.jb - s.ja;
+                more = next_seg(a, ctrl, segs, s, false);
+                if (!more && any_aborted(ctrl)) break;
+                if (more) {
+                    from = first_key(a, s.pos, s.klen), to = end_key(a, s.pos + s.ntok - 1, s.klen);
+                    ik = iv = s.ja;
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) page[i] = page_of(iv + i);
+                    if (iv == s.jb) continue;
+                }
+            }
+        }
+        const bool issue = more && iv < s.jb;
+        if (!issue && waiting == 0) break;
+        if (issue) {
+            // the order of use: keys of two tiles, then values of a tile, keys of the next but one
+            const bool values = !(ik < s.jb && ik < iv + 2);
+            const int j = values ? iv : ik, key = KT * j + 32 * warp + lane;
+            const int p = j == iv ? page[0] : page[1];
             const bool ok = p >= 0 && p < a.c.num_pages;
-            if (!values) {
+            if (!values && u == 0) {
                 const unsigned bits = __ballot_sync(0xffffffffu, ok || p == INT_MIN);
                 if (lane == 0) reinterpret_cast<uint32_t*>(&ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD])[warp] = bits;
                 if (!ok && p != INT_MIN) raise_bad_index(a.status);
             }
             const int off = key % a.c.page_size;
-            const bool whole = !T::F16 && a.maps && __all_sync(0xffffffffu, ok);
-            const char* row = nullptr;
-            if (ok)
-                row = values ? static_cast<const char*>(a.c.v) + (p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride) * ELEM
-                             : static_cast<const char*>(a.c.k) + (p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride) * ELEM;
-            if (values)
-                for (int u = 0; u < T::NVU; ++u) load(Pieces<T::VC * ELEM / 16>(), true, row, u, whole, p, off, s.g);
-            else
-                for (int u = 0; u < T::NKU; ++u) load(Pieces<T::KC * ELEM / 16>(), false, row, u, whole, p, off, s.g);
-            if (values) {      // on to the next tile
-                page[0] = page[1], page[1] = page[2], page[2] = page_of(j + 3);
-                base = j + 1;
+            const int pieces = (values ? T::VC : T::KC) * ELEM / 16;      // 16-byte pieces of a key in a unit
+            const char* row = nullptr;                      // of the lane's key
+            if (ok) {
+                const i64 at = values ? p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride
+                                      : p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride;
+                row = static_cast<const char*>(values ? a.c.v : a.c.k) + at * ELEM + u * pieces * 16;
             }
-        });
-        tiles += s.jb - s.ja;
+            uint32_t place;                                 // of the warp's 32 keys
+            uint64_t* full = nullptr;
+            bool boxes = false;
+            if (T::F16) {
+                place = ptx::smem_u32(mine) + raw % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
+            } else {
+                const uint32_t n = values ? nv : nk, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
+                wait_bar(values ? &ctrl->v_empty[st] : &ctrl->k_empty[st], n / stages + 1, ctrl, a.status);
+                place = ptx::smem_u32(values ? room.v + st * T::V_UNIT : room.k + st * T::K_UNIT) + 32 * warp * 128;
+                full = values ? &ctrl->v_full[st] : &ctrl->k_full[st];
+                boxes = a.maps && __all_sync(0xffffffffu, ok);
+            }
+            if (boxes) {
+                const int slabs = (pieces + 7) / 8;
+                if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(full), slabs * 32 * 128);
+                __syncwarp();
+                const int x = slabs == 2 ? lane & 1 : 0, first = (slabs == 2 ? lane >> 1 : lane) * a.box;      // slab; of the warp's keys
+                const int bp = __shfl_sync(0xffffffffu, p, first & 31), bo = __shfl_sync(0xffffffffu, off, first & 31);
+                if (first < 32)
+                    tma_load_4d(place + x * T::SLAB + first * 128, values ? mv : mk, ptx::smem_u32(full), u * pieces * 8 + 64 * x, s.g, bo, bp);
+            } else {
+#pragma unroll 4
+                for (int i = 0; i < pieces; ++i) {          // 32 keys' pieces, 32 at a time
+                    const int flat = i * 32 + lane, k = flat / pieces, piece = flat - k * pieces;
+                    const char* const src = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
+                    const uint32_t dst = T::F16 ? place + flat * 16 : place + (piece >> 3) * T::SLAB + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                    cp_async16(dst, src ? src + piece * 16 : static_cast<const char*>(a.c.k), src != nullptr);
+                }
+                cp_commit();
+                if (!T::F16) {
+                    cp_wait<0>();
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) arrive(full);
+                }
+            }
+            if (T::F16) kinds = kinds << 1 | (values ? 1u : 0u), ++waiting, ++raw;
+            if (values) ++nv;
+            else ++nk;
+            if (++u == (values ? T::NVU : T::NKU)) {
+                u = 0;
+                if (values) ++iv, page[0] = page[1], page[1] = page[2], page[2] = page_of(iv + 2);
+                else ++ik;
+            }
+        }
+        if (T::F16 && (waiting > LAG || !issue)) {          // the oldest one has come (or all have to): it is widened into its place
+            if (issue) cp_wait<LAG>();
+            else cp_wait<0>();
+            const bool values = (kinds >> (waiting - 1)) & 1;
+            // (the ones behind it, of the same kind, have been counted already)
+            const uint32_t newer = __popc(kinds & ((1u << (waiting - 1)) - 1)), later = values ? newer : waiting - 1 - newer;
+            const uint32_t n = (values ? nv : nk) - 1 - later, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
+            wait_bar(values ? &ctrl->v_empty[st] : &ctrl->k_empty[st], n / stages + 1, ctrl, a.status);
+            __syncwarp();
+            const uint8_t* const src = mine + (raw - waiting) % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
+            uint8_t* const place = values ? room.v + st * T::V_UNIT : room.k + st * T::K_UNIT;
+            const int pieces = (values ? T::VC : T::KC) / 16;
+#pragma unroll 4
+            for (int i = 0; i < pieces; ++i) {
+                const int flat = i * 32 + lane, key = flat / pieces, piece = flat - key * pieces;      // 16 elements
+                const uint4 x = *reinterpret_cast<const uint4*>(src + flat * 16);
+                uint32_t f[8];
+                e4m3_to_f16(x.x, f[0], f[1]), e4m3_to_f16(x.y, f[2], f[3]), e4m3_to_f16(x.z, f[4], f[5]), e4m3_to_f16(x.w, f[6], f[7]);
+                // (the second slab's lanes store their halves in the other order: eight lanes then meet every bank once)
+                const int c = (piece & 3) * 2, odd = piece >> 2 & 1;
+                uint8_t* const dst = place + (piece >> 2) * T::SLAB + (32 * warp + key) * 128;
+                const uint4 lo = make_uint4(f[0], f[1], f[2], f[3]), hi = make_uint4(f[4], f[5], f[6], f[7]);
+                *reinterpret_cast<uint4*>(dst + (((c + odd) ^ (key & 7)) << 4)) = odd ? hi : lo;
+                *reinterpret_cast<uint4*>(dst + (((c + 1 - odd) ^ (key & 7)) << 4)) = odd ? lo : hi;
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive(values ? &ctrl->v_full[st] : &ctrl->k_full[st]);
+            --waiting;
+        }
         if (any_aborted(ctrl)) break;
     }
-    if (!any_aborted(ctrl)) flush();
     cp_wait<0>();
     if (!T::F16 && lane == 0 && aborted(ctrl)) landed(ctrl->k_full, nk, T::K_STAGES), landed(ctrl->v_full, nv, T::V_STAGES);
     __syncwarp();
@@ -1260,9 +1222,11 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     ptx::grid_dep_wait();
     {   // the list's length: every warp adds up a stretch of entries
-        const i64 e0 = a.entries * warp / T::WARPS, e1 = a.entries * (warp + 1) / T::WARPS;
+        // (stretches of whole warps' entries)
+        const int stretch = stretch_of<T>(a), e0 = min(stretch * warp, a.entries), e1 = min(e0 + stretch, a.entries);
         i64 sum = 0;
-        for (i64 e = e0; e < e1; e += 32) {
+#pragma unroll 1
+        for (int e = e0; e < e1; e += 32) {
             Entry en = {};
             if (e + lane < e1) en = entry_of<T::PAGED>(a, e + lane, blockIdx.x == 0);
             sum += entry_cost<T::TILES>(a, en.qlen, en.klen);
