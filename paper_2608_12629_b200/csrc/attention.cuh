@@ -791,52 +791,54 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         float2 odd[4];                             // NaN once something is not finite
 #pragma unroll
         for (int k = 0; k < 4; ++k) odd[k] = make_float2(0.f, 0.f);
-        uint32_t o[2][32];
-        auto fetch = [&](int d, int b) {
-            if (n_mine) ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o[b]);
-        };
-        if (!n_mine) {
+        uint32_t oa[32], oc[32];                   // 32 columns; the next ones are on their way meanwhile
+        auto fetch = [&](uint32_t (&o)[32], int d) {
+            if (n_mine) {
+                ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o);
+            } else {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[0][k] = o[1][k] = 0u;
-        }
-        fetch(0, 0);
-#pragma unroll 1
-        for (int d0 = 0; d0 < D; d0 += 64) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int d = d0 + 32 * b;
-                if (b == 1 && d >= D) break;
-                ptx::tmem_ld_wait(o[b]);
-                if (d + 32 < D) fetch(d + 32, b ^ 1);
-                float (&f)[32] = reinterpret_cast<float (&)[32]>(o[b]);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) f[k] *= f0;
-                if (n_other) {
-                    uint32_t o1[32];
-                    ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
-                    ptx::tmem_ld_wait(o1);
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = fmaf(__uint_as_float(o1[k]), f1, f[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    check2(odd[(k >> 1) & 3], f[k], f[k + 1]);
-                    if (empty) f[k] = f[k + 1] = 0.f;
-                }
-                // (by way of shared memory, in whole sectors: no faster)
-                if (!valid) continue;
-                if (part_at >= 0) {
-                    float4* const to = reinterpret_cast<float4*>(part + static_cast<i64>(part_row) * D + d);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) to[k] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
-                } else {
-                    uint4* const to = reinterpret_cast<uint4*>(a.out + row * D + d);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        to[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]), pack_bf16(f[8 * k + 4], f[8 * k + 5]),
-                                           pack_bf16(f[8 * k + 6], f[8 * k + 7]));
-                }
+                for (int k = 0; k < 32; ++k) o[k] = 0u;
             }
+        };
+        auto finish = [&](uint32_t (&o)[32], int d) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
+            if (n_other) {
+                uint32_t o1[32];
+                ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
+                ptx::tmem_ld_wait(o1);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+                check2(odd[(k >> 1) & 3], __uint_as_float(o[k]), __uint_as_float(o[k + 1]));
+                if (empty) o[k] = o[k + 1] = 0u;
+            }
+            // (by way of shared memory, in whole sectors: no faster)
+            if (!valid) return;
+            if (part_at >= 0) {
+                uint4* const to = reinterpret_cast<uint4*>(part + static_cast<i64>(part_row) * D + d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) to[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                uint4* const to = reinterpret_cast<uint4*>(a.out + row * D + d);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) to[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            }
+        };
+        fetch(oa, 0);
+#pragma unroll 1
+        for (int d = 0; d < D; d += 64) {
+            ptx::tmem_ld_wait(oa);
+            if (d + 32 < D) fetch(oc, d + 32);
+            finish(oa, d);
+            if (d + 32 >= D) break;
+            ptx::tmem_ld_wait(oc);
+            if (d + 64 < D) fetch(oa, d + 64);
+            finish(oc, d + 32);
         }
         ptx::tc_fence_before();
         __syncwarp();
@@ -1190,7 +1192,8 @@ __device__ __forceinline__ void sums_warp(const Args& a, Ctrl* ctrl, uint32_t v_
 
 template <class T>
 __global__ void __launch_bounds__(T::THREADS, 1)
-attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Args a) {
+attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                 const __grid_constant__ Args a) {
     extern __shared__ uint8_t smem_raw[];
     Room room;
     room.q = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
