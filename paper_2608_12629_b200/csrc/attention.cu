@@ -54,6 +54,12 @@ int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_
     a.tokens = MT / a.heads;
     if (B > INT_MAX / 64 / (static_cast<i64>(a.Hkv) * a.runs)) return CAKE_ERR_SHAPE;
     a.entries = static_cast<int>(B) * a.Hkv * a.runs;
+    const uint32_t per = static_cast<uint32_t>(a.Hkv) * a.runs;      // e / per for e < 2^31: mulhi(e, ceil(2^(31 + k) / per)) >> (k - 1), 2^k >= per
+    uint32_t k = 0;
+    while ((1ull << k) < per) ++k;
+    a.per_mul = per == 1 ? 0 : static_cast<uint32_t>(((1ull << (31 + k)) + per - 1) / per);
+    a.per_shift = per == 1 ? 0 : k - 1;
+    a.share_mul = ~0ull / ctas_of(*di);
     a.negative = scale < 0.f;
     a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
     a.status = static_cast<int*>(ws);

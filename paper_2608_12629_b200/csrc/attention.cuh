@@ -16,8 +16,8 @@
 //   different rows that share each tile of keys (DUAL), or, where an item has no more than 128 rows,
 //   the same rows over every other tile of keys (ALT), joined at the end.
 //
-// Work is the list of all tiles of keys of all items (sequence, key-value head, block of rows), one after the other; CTA c of n
-// takes the c-th of n equal shares, whatever the lengths are, moved to the end of an item where that is near.  Items that several
+// Work is the list of all keys of all items (sequence, key-value head, block of rows), one after the other, with some for an item's
+// start and end; CTA c of n takes the c-th of n equal shares, whatever the lengths are, in whole tiles and moved to the end of an item where that is near.  Items that several
 // CTAs share are joined from parts in the workspace by a second kernel, in the order of the CTAs.
 //
 // Warps: two warpgroups of softmax rows, one that loads pages (paged caches only), one with a scheduler, a TMA and an MMA thread.
@@ -37,10 +37,9 @@ constexpr int MT = 128;                        // rows of a tile
 constexpr int MOST_CTAS = 148;                 // that the workspace has room for parts of (two each)
 constexpr int SEGS = 4;                        // segments of work that the scheduler is ahead
 constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags are kept
-constexpr int OVERHEAD = 4;                    // tiles of keys that an item's start and end cost
-constexpr int SNAP = 5;                        // a share's end within so many tiles of an item's is moved there (> OVERHEAD)
-constexpr int MIN_SHARE = 2;                   // tiles
-static_assert(SNAP > OVERHEAD, "a part has at least one tile of keys");
+constexpr int OVERHEAD = 576;                  // keys that an item's start and end cost (four tiles of them, and half of one that is not full)
+constexpr int SNAP = 2;                        // a share's end within fewer tiles of an item's is moved there
+constexpr int MIN_SHARE = OVERHEAD / 2;        // of a CTA, in keys
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
@@ -71,6 +70,8 @@ struct Args {
     i64 T, Tk, q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
     i64 table_stride, table_head_stride, lens_stride, lens_head_stride;
     int entries;                               // sequences * key-value heads * runs
+    uint32_t per_mul, per_shift;               // e / (heads * runs) = mulhi(e, per_mul) >> per_shift (per_mul 0: e)
+    uint64_t share_mul;                        // 2^64 / CTAs
     int Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
@@ -215,11 +216,11 @@ struct Entry {
     int qlen, klen, g, run;
 };
 template <bool PAGED>
-__device__ __noinline__ Entry entry_of(const Args& a, int e, bool report) {
+__device__ __forceinline__ Entry entry_of(const Args& a, int e, bool report) {
     Entry n;
     const int per = a.Hkv * a.runs;
-    const int b = e / per, r = e - b * per;
-    n.g = r / a.runs, n.run = r - n.g * a.runs;
+    const int b = a.per_mul ? static_cast<int>(__umulhi(e, a.per_mul) >> a.per_shift) : e, r = e - b * per;
+    n.g = a.runs == 1 ? r : r / a.runs, n.run = r - n.g * a.runs;
     const int s0 = a.starts[b], s1 = a.starts[b + 1];
     bool bad = s0 < 0 || s1 < s0 || s1 > a.T;
     n.q0 = s0, n.qlen = bad ? 0 : s1 - s0;
@@ -246,31 +247,22 @@ __device__ __forceinline__ void tiles_of(const Args& a, int pos, int n, int klen
 }
 template <int TILES>
 __device__ __forceinline__ int blocks_of(const Args& a, int qlen) { return (qlen + TILES * a.tokens - 1) / (TILES * a.tokens); }
+// Cost of the first n items of an entry, in keys: OVERHEAD + end - first key for each, where both grow by a block's tokens from item
+// to item (but for the last item's end, which is the sequence's): sums of arithmetic series, no loop
 template <int TILES>
-__device__ __noinline__ int cost_of(const Args& a, int qlen, int klen, int block) {
-    const int per = TILES * a.tokens, tok = block * per;
-    int ja, jb;
-    tiles_of(a, klen - qlen + tok, min(per, qlen - tok), klen, ja, jb);
-    return jb - ja + OVERHEAD;
-}
-// the cost of the lane's entry (lanes without one: qlen = 0); long ones are added up by the whole warp
-template <int TILES>
-__device__ __forceinline__ i64 entry_cost(const Args& a, int qlen, int klen) {
-    const int lane = threadIdx.x & 31;
-    const int blocks = blocks_of<TILES>(a, qlen);
-    i64 sum = 0;
-    if (blocks <= 4)
-#pragma unroll 1
-        for (int i = 0; i < blocks; ++i) sum += cost_of<TILES>(a, qlen, klen, i);
-    for (unsigned todo = __ballot_sync(0xffffffffu, blocks > 4); todo; todo &= todo - 1) {
-        const int who = __ffs(todo) - 1;
-        const int ql = __shfl_sync(0xffffffffu, qlen, who), kl = __shfl_sync(0xffffffffu, klen, who), n = __shfl_sync(0xffffffffu, blocks, who);
-        i64 s = 0;
-#pragma unroll 1
-        for (int i = lane; i < n; i += 32) s += cost_of<TILES>(a, ql, kl, i);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == who) sum = s;
+__device__ __noinline__ i64 cost_before(const Args& a, int qlen, int klen, int n) {
+    const int per = TILES * a.tokens, off = klen - qlen;
+    if (!a.causal) return static_cast<i64>(n) * (OVERHEAD + klen);
+    const int full = min(n, qlen / per);                    // items of a whole block of tokens
+    i64 sum = static_cast<i64>(n) * OVERHEAD + (n > full ? klen : 0);
+    const int i0 = off < 0 ? min(full, -off / per) : 0;     // those before see nothing
+    const i64 m = full - i0;
+    sum += m * off + per * (m * (i0 + 1 + full) / 2);       // off + (i + 1) per, i0 <= i < full
+    if (a.window > 0) {
+        const i64 gone = static_cast<i64>(off) - a.window + 1;      // first key of item i: gone + i per
+        const int i1 = gone < 0 ? static_cast<int>(min(static_cast<i64>(n), (-gone + per - 1) / per)) : 0;
+        const i64 k = n - i1;
+        sum -= k * gone + per * (k * (i1 + n - 1) / 2);
     }
     return sum;
 }
@@ -283,8 +275,11 @@ __device__ __forceinline__ i64 inclusive_scan(i64 v) {
     }
     return v;
 }
-// a share's end p tiles into an item of this cost, moved to the item's ends where they are near
-__device__ __forceinline__ int snap(int p, int cost) { return p <= SNAP ? 0 : cost - p <= SNAP ? cost : p; }
+// a share's end p keys into an item of n tiles, in tiles, moved to the item's ends where they are near
+__device__ __forceinline__ int snap(i64 p, int n) {
+    const int t = p <= OVERHEAD ? 0 : static_cast<int>(min(p - OVERHEAD, static_cast<i64>(INT_MAX))) / KT;
+    return t < SNAP ? 0 : n - t < SNAP ? n : t;
+}
 
 // the tiles of keys of a segment that its row tile t sees (DUAL), or all of them
 template <class T>
@@ -352,10 +347,12 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     // the stretches' sums, added up
     const i64 sums = inclusive_scan(lane < T::WARPS ? ctrl->sums[lane] : 0);
     const i64 total = __shfl_sync(all, sums, 31);
-    const int n = total < static_cast<i64>(MIN_SHARE) * gridDim.x ? max(static_cast<int>(total) / MIN_SHARE, 1) : static_cast<int>(gridDim.x);
-    const i64 whole = total / n;
-    const int over = static_cast<int>(total - whole * n);
-    auto begin_of = [&](int c) { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(n); };      // of CTA c's share: floor(total c / n)
+    // Shares: CTA c's begins at total * c / n, or a little before, for all CTAs alike
+    const bool many = total >= static_cast<i64>(MIN_SHARE) * gridDim.x;
+    const int n = many ? static_cast<int>(gridDim.x) : max(static_cast<int>(total) / MIN_SHARE, 1);
+    auto begin_of = [&](int c) {
+        return c >= n ? total : many ? static_cast<i64>(__umul64hi(total, a.share_mul * c)) : static_cast<i64>(static_cast<unsigned>(total) * c / n);
+    };
     const int cta = blockIdx.x;
     uint32_t count = 0, q_count[2] = {0, 0}, nk = 0;      // segments, loads of queries, units of keys so far
     const bool lead = ptx::elect_one();
@@ -391,30 +388,36 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
         for (int who = 32; who == 32 && e < e_end; e += who) {
             Entry one = {};
             if (e + lane < e_end) one = entry_of<T::PAGED>(a, e + lane, false);
-            who = find(entry_cost<TILES>(a, one.qlen, one.klen));
+            who = find(cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen)));
+            en.q0 = __shfl_sync(all, one.q0, who & 31), en.k0 = __shfl_sync(all, one.k0, who & 31);
+            en.qlen = __shfl_sync(all, one.qlen, who & 31), en.klen = __shfl_sync(all, one.klen, who & 31);
+            en.g = __shfl_sync(all, one.g, who & 31), en.run = __shfl_sync(all, one.run, who & 31);
         }
-        en = entry_of<T::PAGED>(a, e, false);
         int blocks = blocks_of<TILES>(a, en.qlen);
+        // its item
 #pragma unroll 1
-        for (int who = blocks > 1 ? 32 : 0; who == 32 && block < blocks; block += who)
-            who = find(block + lane < blocks ? cost_of<TILES>(a, en.qlen, en.klen, block + lane) : 0);
+        for (int step = blocks > 1 ? 1 << (31 - __clz(blocks - 1)) : 0; step; step >>= 1)
+            if (block + step < blocks && before + cost_before<TILES>(a, en.qlen, en.klen, block + step) <= x0) block += step;
+        if (block) before += cost_before<TILES>(a, en.qlen, en.klen, block);
         int start = -1;
+#pragma unroll 1
         while (x1 > before && block < blocks) {
             const int per = TILES * a.tokens, tok = block * per, ntok = min(per, en.qlen - tok);
             const int pos = en.klen - en.qlen + tok;
             int ja, jb;
             tiles_of(a, pos, ntok, en.klen, ja, jb);
-            const int cost = jb - ja + OVERHEAD;
-            if (start < 0) start = snap(static_cast<int>(x0 - before), cost);      // the share's first item
-            const int end = x1 >= before + cost ? cost : snap(static_cast<int>(x1 - before), cost);
-            if (start < end) {
+            const int tiles = jb - ja;
+            const i64 end_at = before + OVERHEAD + end_key(a, pos + ntok - 1, en.klen) - (a.window > 0 ? first_key(a, pos, en.klen) : 0);
+            if (start < 0) start = x0 > before ? snap(x0 - before, tiles) : 0;      // the share's first item
+            const bool to_end = x1 >= end_at;
+            const int end = to_end ? tiles : snap(x1 - before, tiles);
+            if (to_end ? start < tiles || start == 0 : start < end) {
                 Seg s;
                 s.tok = en.q0 + tok, s.k0 = en.k0, s.g = en.g;
                 s.head0 = en.g * a.G + en.run * a.heads, s.heads = min(a.heads, a.G - en.run * a.heads);
                 s.ntok = ntok, s.pos = pos, s.klen = en.klen;
-                s.ja = start ? ja + start - OVERHEAD : ja;
-                s.jb = end == cost ? jb : ja + end - OVERHEAD;
-                s.part = start == 0 && end == cost ? -1 : 2 * cta + (start == 0 ? 1 : 0);
+                s.ja = ja + start, s.jb = ja + end;
+                s.part = start == 0 && end == tiles ? -1 : 2 * cta + (start == 0 ? 1 : 0);
                 s.negative = a.negative;
                 if (T::F16 && a.c.k_scale && a.c.k_scale[en.g] < 0.f) s.negative ^= 1;
                 s.done = 0;
@@ -422,12 +425,12 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
                 if (lead && !aborted(ctrl)) load_queries_keys<T>(a, ctrl, room, mq, mk, s, q_count, nk);
                 __syncwarp();
                 if (any_aborted(ctrl)) break;
-                if (start == 0 && end < cost) {      // the CTAs behind this one have the rest
+                if (start == 0 && end < tiles) {      // the CTAs behind this one have the rest
                     int c1 = cta;
 #pragma unroll 1
                     for (int c = cta + 1; c < n; c += 32) {
-                        const i64 x = c + lane < n ? begin_of(c + lane) : total;
-                        const unsigned in = __ballot_sync(all, before + cost - x > SNAP);
+                        const i64 x = begin_of(c + lane);
+                        const unsigned in = __ballot_sync(all, c + lane < n && x < end_at && snap(x - before, tiles) < tiles);
                         c1 += __popc(in);
                         if (in != all) break;
                     }
@@ -435,11 +438,12 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
                     split.valid = 1;
                 }
             }
-            if (end < cost) break;
-            before += cost;
+            if (!to_end) break;
+            before = end_at;
             start = 0;
             if (++block == blocks) {
                 block = 0, blocks = 0;
+#pragma unroll 1
                 while (blocks == 0 && ++e < a.entries) {
                     en = entry_of<T::PAGED>(a, e, false);
                     blocks = blocks_of<TILES>(a, en.qlen);
@@ -636,12 +640,19 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 if (other && lane == 0) arrive(&ctrl->q_empty[0]);
             }
         }
+        const bool idle = !__any_sync(0xffffffffu, tok < a.tokens && my_tok < sp->ntok);      // a warp without a row: P may hold anything there
         float m = NEG_INF, l = 0.f;                // m: the maximum that is subtracted, without LIFT
         for (int i = 0; i < n_mine; ++i) {
             const int key0 = KT * (first + i * step);
             const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
             wait_bar(&ctrl->s_full[t], s_count, ctrl, a.status);
             ++s_count;
+            if (idle) {
+                if (o_count[pb]) wait_bar(&ctrl->o_done[pb], o_count[pb] - 1, ctrl, a.status);
+                ++o_count[pb];
+                if (lane == 0) arrive(&ctrl->s_free), arrive(&ctrl->p_ready[pb]);
+                continue;
+            }
             ptx::tc_fence_after();
             uint32_t x[4][32];
 #pragma unroll
@@ -1232,7 +1243,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (int e = e0; e < e1; e += 32) {
             Entry en = {};
             if (e + lane < e1) en = entry_of<T::PAGED>(a, e + lane, blockIdx.x == 0);
-            sum += entry_cost<T::TILES>(a, en.qlen, en.klen);
+            sum += cost_before<T::TILES>(a, en.qlen, en.klen, blocks_of<T::TILES>(a, en.qlen));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -1365,6 +1376,7 @@ attention_join_kernel(const Args a) {
 struct Maps {
     CUtensorMap q, k, v;
 };
+inline int ctas_of(const DeviceInfo& di) { return di.sm_count < MOST_CTAS ? di.sm_count : MOST_CTAS; }
 int launch_64(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
 int launch_96(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
 int launch_128(const Args& a, const Maps& m, int kind, const DeviceInfo& di, cudaStream_t s);
@@ -1387,7 +1399,7 @@ int launch(const Args& a, const Maps& m, const DeviceInfo& di, cudaStream_t s) {
         return allow_smem(attention_kernel<T>, SMEM);
     });
     if (!ok) return CAKE_ERR_CUDA;
-    const int ctas = di.sm_count < MOST_CTAS ? di.sm_count : MOST_CTAS;
+    const int ctas = ctas_of(di);
     if (launch_early(attention_kernel<T>, dim3(ctas), dim3(T::THREADS), SMEM, s, m.q, m.k, m.v, a) != cudaSuccess) return CAKE_ERR_CUDA;
     return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * JOIN_SLICES), dim3(32 * JOIN_WARPS), 0, s, a) == cudaSuccess
                ? CAKE_OK : CAKE_ERR_CUDA;
