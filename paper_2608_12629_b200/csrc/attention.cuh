@@ -38,7 +38,7 @@ constexpr int MOST_CTAS = 148;                 // that the workspace has room fo
 constexpr int SEGS = 4;                        // segments of work that the scheduler is ahead
 constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags are kept
 constexpr int OVERHEAD = 576;                  // keys that an item's start and end cost (four tiles of them, and half of one that is not full)
-constexpr int SNAP = 2;                        // a share's end within fewer tiles of an item's is moved there
+constexpr int SNAP = 4;                        // a share's end within fewer tiles of an item's is moved there
 constexpr int MIN_SHARE = OVERHEAD / 2;        // of a CTA, in keys
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 constexpr float LOG2E = 1.4426950408889634f;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void wait_more(uint32_t addr, uint32_t parity, Ctrl* 
 }
 __device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* ctrl, int* status) {
     const uint32_t addr = ptx::smem_u32(bar);
-    if (!ptx::mbar_try_wait(addr, parity & 1)) wait_more(addr, parity & 1, ctrl, status);
+    if (__builtin_expect(!ptx::mbar_try_wait(addr, parity & 1), 0)) wait_more(addr, parity & 1, ctrl, status);
 }
 __device__ __forceinline__ void arrive(uint64_t* bar) { ptx::mbar_arrive(ptx::smem_u32(bar)); }
 __device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flushed to zero
@@ -647,7 +647,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
             wait_bar(&ctrl->s_full[t], s_count, ctrl, a.status);
             ++s_count;
-            if (idle) {
+            if (__builtin_expect(idle, 0)) {
                 if (o_count[pb]) wait_bar(&ctrl->o_done[pb], o_count[pb] - 1, ctrl, a.status);
                 ++o_count[pb];
                 if (lane == 0) arrive(&ctrl->s_free), arrive(&ctrl->p_ready[pb]);
@@ -671,7 +671,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             }
             // Which rows look for their maximum: it is theirs alone to say, so that a row's bits do not depend on its neighbours
             bool search = m == NEG_INF;
-            if (masked) {
+            if (__builtin_expect(masked, 0)) {
                 const uint32_t seen[4] = {pages.x, pages.y, pages.z, pages.w};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -687,7 +687,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             float total;
 #pragma unroll 1                               // (one copy of this: the loops are about what the instruction caches hold)
             for (int pass = 0;; ++pass) {
-                if (__any_sync(0xffffffffu, search)) {
+                if (__builtin_expect(__any_sync(0xffffffffu, search), 0)) {
                     float top[4];
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
@@ -802,7 +802,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         float2 odd[4];                             // NaN once something is not finite
 #pragma unroll
         for (int k = 0; k < 4; ++k) odd[k] = make_float2(0.f, 0.f);
-        uint32_t oa[32], oc[32];                   // 32 columns; the next ones are on their way meanwhile
+        // (a short loop: an item's end is run once in a while, and to fetch its instructions is what costs it most; with the next columns on their way
+        // meanwhile, and twice the code, 8 packed prompts took 151 us for 141)
+        uint32_t oa[32];
         auto fetch = [&](uint32_t (&o)[32], int d) {
             if (n_mine) {
                 ptx::tmem_ld_x32(t_lane + O_COL + ob * KT + d, o);
@@ -814,7 +816,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         auto finish = [&](uint32_t (&o)[32], int d) {
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
-            if (n_other) {
+            if (__builtin_expect(n_other, 0)) {
                 uint32_t o1[32];
                 ptx::tmem_ld_x32(t_lane + O_COL + KT + d, o1);
                 ptx::tmem_ld_wait(o1);
@@ -840,16 +842,11 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 for (int k = 0; k < 4; ++k) to[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
             }
         };
-        fetch(oa, 0);
 #pragma unroll 1
-        for (int d = 0; d < D; d += 64) {
+        for (int d = 0; d < D; d += 32) {
+            fetch(oa, d);
             ptx::tmem_ld_wait(oa);
-            if (d + 32 < D) fetch(oc, d + 32);
             finish(oa, d);
-            if (d + 32 >= D) break;
-            ptx::tmem_ld_wait(oc);
-            if (d + 64 < D) fetch(oa, d + 64);
-            finish(oc, d + 32);
         }
         ptx::tc_fence_before();
         __syncwarp();
@@ -859,7 +856,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         }
         if (valid) {
             bool mended = false;
-            if (isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y)) && isfinite(l) && !empty) {
+            if (__builtin_expect(isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y)) && isfinite(l) && !empty, 0)) {
                 RowAt at;
                 const int klen = sp->klen, pos = sp->pos, ntok = sp->ntok;
                 at.row = row, at.g = g, at.part_row = part_row, at.part = part_at, at.base = sp->k0;

@@ -2,8 +2,9 @@
 //
 //   out[n][h] = bf16(cache[slot n][h] * scale[h])
 //
-// Bound by memory: a token's heads are read once and written once.  A thread moves runs of 8 (bf16) or 16 (e4m3) elements, 16 bytes a
-// load, four loads in flight.
+// Bound by memory: a token's heads are read once and written once.  A thread has one place in a token's row, 8 elements of a head (16 bytes
+// written, so that a warp's store covers whole sectors: 16 elements a thread, in two stores of half sectors, 128 us for 100,001 8-bit tokens), and
+// walks over tokens, several loads in flight.
 #include "serving.cuh"
 
 namespace cake {
@@ -13,77 +14,77 @@ int check_cache(const cake_paged_cache* c);   // kv_append.cu
 
 namespace {
 
-constexpr int READ_THREADS = 256, READ_BATCH = 4;
+constexpr int READ_THREADS = 256, RUN = 8;
 
 struct ReadArgs {
     cake_paged_cache c;
     const long long* slots;
     cake_bf16 *out_k, *out_v;
-    i64 N, stride, head_stride, units;      // units: of all tokens, in both matrices
-    int per_head, per_token;                // units of a head, of a token in one matrix
+    i64 N, stride, head_stride;
+    int per_head, units, tokens;            // runs of a head, of a token in both matrices; tokens of a block's step
     int* status;
 };
 
-template <bool E4M3>
+template <bool E4M3, int BATCH>
 __global__ void __launch_bounds__(READ_THREADS)
 kv_read_kernel(const ReadArgs a) {
-    constexpr int RUN = E4M3 ? 16 : 8, ELEM = E4M3 ? 1 : 2;
+    constexpr int ELEM = E4M3 ? 1 : 2;
+    // the thread's place: (matrix, head, run)
+    const int t = threadIdx.x / a.units, u = blockIdx.y * READ_THREADS + threadIdx.x - t * a.units;
+    if (u >= a.units || t >= a.tokens) return;
+    const int heads = u / a.per_head, d = (u - heads * a.per_head) * RUN;
+    const bool is_v = a.out_k == nullptr || heads >= a.c.Hkv;
+    const int h = a.out_k != nullptr && is_v ? heads - a.c.Hkv : heads;
+    const i64 page_stride = is_v ? a.c.v_page_stride : a.c.k_page_stride, token_stride = is_v ? a.c.v_token_stride : a.c.k_token_stride;
+    const char* const from = static_cast<const char*>(is_v ? a.c.v : a.c.k) + (h * (is_v ? a.c.v_head_stride : a.c.k_head_stride) + d) * ELEM;
+    cake_bf16* const to = (is_v ? a.out_v : a.out_k) + h * a.head_stride + d;
+    const float* const scales = E4M3 ? (is_v ? a.c.v_scale : a.c.k_scale) : nullptr;
     ptx::grid_dep_wait();
-    // unit i of a block's stretch: (token, matrix, head, run), the runs of a token's head in one matrix next to each other
-    const i64 first = static_cast<i64>(blockIdx.x) * (READ_THREADS * READ_BATCH) + threadIdx.x;
-    const int both = a.out_v && a.out_k ? 2 : 1;
-    uint4 got[READ_BATCH];
-    cake_bf16* to[READ_BATCH];
-    const float* scale[READ_BATCH];
+    const float scale = scales ? scales[h] : 1.f;
+    const i64 first = static_cast<i64>(blockIdx.x) * a.tokens * BATCH + t;
+    i64 slot[BATCH];
+    uint4 got[BATCH];
 #pragma unroll
-    for (int b = 0; b < READ_BATCH; ++b) {
-        const i64 i = first + b * READ_THREADS;
-        to[b] = nullptr, scale[b] = nullptr;
+    for (int b = 0; b < BATCH; ++b) {
+        const i64 n = first + b * a.tokens;
+        slot[b] = n < a.N ? a.slots[n] : -1;
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
         got[b] = make_uint4(0u, 0u, 0u, 0u);
-        if (i >= a.units) continue;
-        const int per = a.per_token * both;
-        const i64 n = (static_cast<unsigned long long>(i) >> 32) == 0 ? static_cast<unsigned>(i) / static_cast<unsigned>(per) : i / per;
-        int rest = static_cast<int>(i - n * per);
-        const bool is_v = both == 2 ? rest >= a.per_token : a.out_v != nullptr;
-        if (both == 2 && is_v) rest -= a.per_token;
-        const int h = rest / a.per_head, d = (rest - h * a.per_head) * RUN;
-        const i64 slot = a.slots[n];
-        const i64 page = (static_cast<unsigned long long>(slot) >> 32) == 0 ? static_cast<unsigned>(slot) / static_cast<unsigned>(a.c.page_size)
-                                                                            : slot / a.c.page_size;
-        to[b] = (is_v ? a.out_v : a.out_k) + n * a.stride + h * a.head_stride + d;
-        if (slot >= 0 && page < a.c.num_pages) {
-            const i64 off = slot - page * a.c.page_size;
-            const i64 at = is_v ? page * a.c.v_page_stride + off * a.c.v_token_stride + h * a.c.v_head_stride
-                                : page * a.c.k_page_stride + off * a.c.k_token_stride + h * a.c.k_head_stride;
-            got[b] = *reinterpret_cast<const uint4*>(static_cast<const char*>(is_v ? a.c.v : a.c.k) + (at + d) * ELEM);
+        // (32-bit division where it will do: the 64-bit one is a hundred instructions)
+        const i64 page = (static_cast<unsigned long long>(slot[b]) >> 32) == 0 ? static_cast<unsigned>(slot[b]) / static_cast<unsigned>(a.c.page_size)
+                                                                               : slot[b] / a.c.page_size;
+        if (slot[b] >= 0 && page < a.c.num_pages) {
+            const char* const at = from + (page * page_stride + (slot[b] - page * a.c.page_size) * token_stride) * ELEM;
             if (E4M3) {
-                const float* s = is_v ? a.c.v_scale : a.c.k_scale;
-                if (s) scale[b] = s + h;
+                const uint2 w = *reinterpret_cast<const uint2*>(at);
+                got[b].x = w.x, got[b].y = w.y;
+            } else {
+                got[b] = *reinterpret_cast<const uint4*>(at);
             }
-        } else if (slot >= 0) {
+        } else if (slot[b] >= 0) {
             raise_bad_index(a.status);
         }
     }
 #pragma unroll
-    for (int b = 0; b < READ_BATCH; ++b) {
-        if (!to[b]) continue;
+    for (int b = 0; b < BATCH; ++b) {
+        const i64 n = first + b * a.tokens;
+        if (n >= a.N) break;
         if (E4M3) {
-            const float s = scale[b] ? *scale[b] : 1.f;
-            const uint32_t w[4] = {got[b].x, got[b].y, got[b].z, got[b].w};
-            uint32_t p[8];
+            const uint32_t w[2] = {got[b].x, got[b].y};
+            uint32_t p[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const uint16_t pair = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
                 uint32_t f16;
                 asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f16) : "h"(pair));
                 const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&f16));
-                p[j] = pack_bf16(f.x * s, f.y * s);
+                p[j] = pack_bf16(f.x * scale, f.y * scale);
             }
-            reinterpret_cast<uint4*>(to[b])[0] = make_uint4(p[0], p[1], p[2], p[3]);
-            reinterpret_cast<uint4*>(to[b])[1] = make_uint4(p[4], p[5], p[6], p[7]);
-        } else {
-            *reinterpret_cast<uint4*>(to[b]) = got[b];
+            got[b] = make_uint4(p[0], p[1], p[2], p[3]);
         }
+        *reinterpret_cast<uint4*>(to + n * a.stride) = got[b];
     }
 }
 
@@ -113,13 +114,20 @@ extern "C" int cake_kv_read(const cake_paged_cache* cache, const long long* slot
     const bool e4m3 = cache->type == CAKE_KV_E4M3;
     ReadArgs a;
     a.c = *cache, a.slots = slots, a.out_k = out_k, a.out_v = out_v, a.N = N, a.stride = out_stride, a.head_stride = out_head_stride;
-    a.per_head = cache->D / (e4m3 ? 16 : 8);
-    if (a.per_head > INT_MAX / 2 / cache->Hkv) return CAKE_ERR_SHAPE;
-    a.per_token = a.per_head * cache->Hkv;
-    a.units = N * a.per_token * (out_k && out_v ? 2 : 1);
+    a.per_head = cache->D / RUN;
+    if (a.per_head > INT_MAX / 4 / cache->Hkv) return CAKE_ERR_SHAPE;
+    a.units = a.per_head * cache->Hkv * (out_k && out_v ? 2 : 1);
     a.status = static_cast<int*>(ws);
-    const i64 blocks = (a.units + READ_THREADS * READ_BATCH - 1) / (READ_THREADS * READ_BATCH);
-    if (blocks > INT_MAX) return CAKE_ERR_SHAPE;
-    return launch_early(e4m3 ? kv_read_kernel<true> : kv_read_kernel<false>, dim3(static_cast<unsigned>(blocks)), dim3(READ_THREADS), 0,
-                        reinterpret_cast<cudaStream_t>(stream), a) == cudaSuccess ? CAKE_OK : CAKE_ERR_CUDA;
+    const unsigned parts = static_cast<unsigned>((a.units + READ_THREADS - 1) / READ_THREADS);
+    if (parts > 65535) return CAKE_ERR_SHAPE;
+    a.tokens = a.units < READ_THREADS ? READ_THREADS / a.units : 1;
+    // Tokens to a thread: one while that leaves the SMs less than a few blocks each (latency: 777 tokens 3.4 us), else several, whose loads overlap
+    const i64 steps = (N + a.tokens - 1) / a.tokens;
+    const bool few = steps * parts < 8 * di.sm_count;
+    constexpr int BATCH = 8;
+    const i64 blocks = few ? steps : (steps + BATCH - 1) / BATCH;
+    void (*const kernel)(const ReadArgs) = e4m3 ? (few ? kv_read_kernel<true, 1> : kv_read_kernel<true, BATCH>)
+                                                : (few ? kv_read_kernel<false, 1> : kv_read_kernel<false, BATCH>);
+    return launch_early(kernel, dim3(static_cast<unsigned>(blocks), parts), dim3(READ_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), a) == cudaSuccess
+               ? CAKE_OK : CAKE_ERR_CUDA;
 }

@@ -300,7 +300,7 @@ extern "C" int cake_qk_norm_append(const cake_paged_cache* cache, const cake_bf1
             par = heads * lanes <= 512 ? heads : 512 / lanes;
             while (par * lanes % 32 != 0 && par * lanes < 512) ++par;      // (whole warps: shuffles name lanes of the head alone, but the rest is idle)
         } else {
-            const int target = 128, most = target / lanes;
+            const int target = T >= 2048 ? 32 : 128, most = target / lanes;
             par = (heads + 3) / 4 <= most ? (heads + 3) / 4 : most;
             tokens = target / (lanes * par) > 0 ? target / (lanes * par) : 1;
         }
