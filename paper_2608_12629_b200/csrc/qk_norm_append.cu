@@ -85,23 +85,23 @@ qk_norm_kernel(const NormArgs a) {
     if (!p.rotate_ok) return;
     const bool live = 16 * u < D;
     const int half = a.rot >> 1;
-    // the two runs of 8 elements; pairs (i, i + rot/2): the first rot/16 lanes have those that rotate into each other
+    // The two runs of 8 elements, neighbours in neighbouring lanes (runs of a lane beside each other would be loaded and stored in half sectors).
+    // Pairs (i, i + rot/2): the first rot/16 lanes have those that rotate into each other
     const bool opposite = !PAIRS && 16 * u < a.rot;
-    const int d0 = opposite ? 8 * u : 16 * u, d1 = opposite ? half + 8 * u : 16 * u + 8;
-    const bool turn0 = live && (PAIRS ? d0 < a.rot : opposite), turn1 = live && (PAIRS ? d1 < a.rot : opposite);
+    const int rest = PAIRS || opposite ? 0 : a.rot, v = u - (rest >> 4);
+    const int d0 = rest + 8 * v, d1 = d0 + (opposite ? half : (D - rest) >> 1);
+    const bool turn0 = live && (PAIRS ? d0 < a.rot : opposite), turn1 = live && PAIRS && d1 < a.rot;
     float cs[8], sn[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) cs[j] = 1.f, sn[j] = 0.f;
-    if (turn0) {
-        const float* row = a.cos_sin + static_cast<i64>(p.pos) * a.rot + 8 * u;      // pairs: 8 u of the rot/2 angles belong to element 16 u
-#pragma unroll
-        for (int j = 0; j < 8; j += 4) {
-            if (j == 4 && !turn1) break;
-            const float4 c = *reinterpret_cast<const float4*>(row + j), w = *reinterpret_cast<const float4*>(row + half + j);
-            cs[j] = c.x, cs[j + 1] = c.y, cs[j + 2] = c.z, cs[j + 3] = c.w;
-            sn[j] = w.x, sn[j + 1] = w.y, sn[j + 2] = w.z, sn[j + 3] = w.w;
-        }
-    }
+    const float* const angles = a.cos_sin + static_cast<i64>(p.pos) * a.rot;
+    auto angle4 = [&](int at, int j) {
+        const float4 c = *reinterpret_cast<const float4*>(angles + at), w = *reinterpret_cast<const float4*>(angles + half + at);
+        cs[j] = c.x, cs[j + 1] = c.y, cs[j + 2] = c.z, cs[j + 3] = c.w;
+        sn[j] = w.x, sn[j + 1] = w.y, sn[j + 2] = w.z, sn[j + 3] = w.w;
+    };
+    if (turn0) angle4(PAIRS ? d0 >> 1 : d0, 0);
+    if (PAIRS ? turn1 : turn0) angle4(PAIRS ? d1 >> 1 : d0 + 4, 4);
     constexpr uint32_t kOnes = 0x3f803f80u;
     uint4 wq[2], wk[2];
     wq[0] = wq[1] = wk[0] = wk[1] = make_uint4(kOnes, kOnes, kOnes, kOnes);
@@ -149,7 +149,7 @@ qk_norm_kernel(const NormArgs a) {
                 if (PAIRS) {
                     if (turn0)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) turn(f[2 * j], f[2 * j + 1], cs[j], sn[j]);      // (angle 0 where the second run does not turn)
+                        for (int j = 0; j < 8; ++j) turn(f[2 * j], f[2 * j + 1], cs[j], sn[j]);      // (an angle of 0 where the second run does not turn)
                 } else if (turn0) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) turn(f[j], f[8 + j], cs[j], sn[j]);
