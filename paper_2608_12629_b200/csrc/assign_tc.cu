@@ -1673,16 +1673,18 @@ int make_tmap_heads(CUtensorMap* m, const void* base, int D, int heads, i64 head
     return r == CUDA_SUCCESS ? CAKE_OK : CAKE_ERR_CUDA;
 }
 
-// bf16 [pages][tokens][heads][D] (D contiguous), strides in bytes, multiples of 16
-int make_tmap_pages(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride, int tokens, i64 token_stride, i64 pages, i64 page_stride, int box_tokens) {
+// bf16 or bytes [pages][tokens][heads][D] (D contiguous), strides in bytes, multiples of 16
+int make_tmap_pages(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride, int tokens, i64 token_stride, i64 pages, i64 page_stride,
+                    int columns, int box_tokens, bool bytes) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return CAKE_ERR_CUDA;
     cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(pages)};
     cuuint64_t strides[3] = {static_cast<cuuint64_t>(head_stride), static_cast<cuuint64_t>(token_stride), static_cast<cuuint64_t>(page_stride)};
-    cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(box_tokens), 1};
+    cuuint32_t box[4] = {static_cast<cuuint32_t>(columns), 1, static_cast<cuuint32_t>(box_tokens), 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    CUresult r = fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CAKE_OK : CAKE_ERR_CUDA;
 }
 

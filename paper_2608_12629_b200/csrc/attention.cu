@@ -20,11 +20,14 @@ int make_map(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride
     return make_tmap_heads(m, base, D, heads, head_stride * 2, tokens, stride * 2, box_heads, box_tokens);
 }
 
-int make_map_pages(CUtensorMap* m, const void* base, const cake_paged_cache& c, i64 head, i64 token, i64 page, int box) {
+// boxes of the columns that a unit of loads has (bf16: 64, swizzled; e4m3: all of the unit's) x `box` tokens of a page
+int make_map_pages(CUtensorMap* m, const void* base, const cake_paged_cache& c, i64 head, i64 token, i64 page, int columns, int box) {
     if (c.Hkv == 1) head = c.D;
+    if (c.page_size == 1) token = c.D;
     if (c.num_pages == 1) page = c.D;
     if (head < c.D || token < c.D || page < c.D) return CAKE_ERR_UNSUPPORTED;      // (strides of zero: expanded tensors)
-    return make_tmap_pages(m, base, c.D, c.Hkv, head * 2, c.page_size, token * 2, c.num_pages, page * 2, box);
+    const int size = c.type == CAKE_KV_BF16 ? 2 : 1;
+    return make_tmap_pages(m, base, c.D, c.Hkv, head * size, c.page_size, token * size, c.num_pages, page * size, columns, box, size == 1);
 }
 
 bool strides_ok(int D, i64 heads, i64 head_stride, i64 tokens, i64 stride) {
@@ -165,9 +168,11 @@ int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_st
     // Pages come in boxes where a warp's 32 keys are whole boxes of a page: 8, 16 or 32 tokens, or 32 of a page of several times that
     const cake_paged_cache& c = *cache;
     a.box = c.page_size < 32 ? c.page_size : 32;
-    a.maps = c.type == CAKE_KV_BF16 && (c.page_size % 32 == 0 || c.page_size == 16 || c.page_size == 8) &&
-             make_map_pages(&maps.k, c.k, c, c.k_head_stride, c.k_token_stride, c.k_page_stride, a.box) == CAKE_OK &&
-             make_map_pages(&maps.v, c.v, c, c.v_head_stride, c.v_token_stride, c.v_page_stride, a.box) == CAKE_OK;
+    const bool bytes = c.type == CAKE_KV_E4M3;
+    const int k_columns = bytes ? (c.D == 256 ? 64 : c.D) : 64, v_columns = bytes ? (c.D == 256 ? 128 : c.D) : 64;
+    a.maps = (c.page_size % 32 == 0 || c.page_size == 16 || c.page_size == 8) &&
+             make_map_pages(&maps.k, c.k, c, c.k_head_stride, c.k_token_stride, c.k_page_stride, k_columns, a.box) == CAKE_OK &&
+             make_map_pages(&maps.v, c.v, c, c.v_head_stride, c.v_token_stride, c.v_page_stride, v_columns, a.box) == CAKE_OK;
     if (!a.maps) maps.k = maps.v = maps.q;      // (not used)
     return launch_any(a, maps, cache->D, cache->type == CAKE_KV_E4M3 ? PAGED_E4M3 : PAGED_BF16, di, reinterpret_cast<cudaStream_t>(stream));
 }

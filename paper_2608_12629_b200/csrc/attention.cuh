@@ -76,7 +76,7 @@ struct Args {
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
     bool negative, causal;                     // sign of the scale
-    bool maps;                                 // paged bf16: mk and mv are maps of the pages, boxes of `box` tokens
+    bool maps;                                 // paged: mk and mv are maps of the pages, boxes of `box` tokens
     int box;
 };
 
@@ -129,6 +129,7 @@ struct __align__(16) Ctrl {
     uint64_t seg_full[SEGS], seg_empty[SEGS];
     uint64_t q_full[2], q_empty[2], q_conv[2];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t raw_full[4][3];                   // of a loading warp's places
     uint64_t s_full[2], p_ready[2], o_done[2], o_free[2], s_free, x_full, x_empty, drained[2];
     Seg seg[SEGS];
     i64 sums[16];
@@ -922,7 +923,7 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
     uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;           // segments, units of keys and of values, tiles so far
     // e4m3: units that were fetched into the ring and are not widened yet, oldest first: a bit for each says that it is of values
     constexpr int LAG = T::F16 ? T::RAW_STAGES - 1 : 0;
-    uint32_t waiting = 0, kinds = 0, raw = 0;               // raw: units that were fetched
+    uint32_t waiting = 0, kinds = 0, copied = 0, raw = 0;   // copied: a bit for each that came by 16-byte copies; raw: units that were fetched
     uint8_t* const mine = room.raw + warp * (T::RAW / 4);
     Seg s = {};
     int from = 0, to = 0, ik = 0, iv = 0, u = 0;            // keys that some row of the item sees; tiles whose keys, values come next; unit of the tile
@@ -972,22 +973,25 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
             uint64_t* full = nullptr;
             bool boxes = false;
             if (T::F16) {
-                place = ptx::smem_u32(mine) + raw % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
+                const uint32_t st = raw % (T::F16 ? T::RAW_STAGES : 1);
+                place = ptx::smem_u32(mine) + st * T::RAW;
+                full = &ctrl->raw_full[warp][st];
             } else {
                 const uint32_t n = values ? nv : nk, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
                 wait_bar(values ? &ctrl->v_empty[st] : &ctrl->k_empty[st], n / stages + 1, ctrl, a.status);
                 place = ptx::smem_u32(values ? room.v + st * T::V_UNIT : room.k + st * T::K_UNIT) + 32 * warp * 128;
                 full = values ? &ctrl->v_full[st] : &ctrl->k_full[st];
-                boxes = a.maps && __all_sync(0xffffffffu, ok);
             }
+            boxes = a.maps && __all_sync(0xffffffffu, ok);
             if (boxes) {
-                const int slabs = (pieces + 7) / 8;
-                if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(full), slabs * 32 * 128);
+                // (8-bit: rows of a unit as they are, one behind the other; else slabs of 64 columns)
+                const int slabs = T::F16 ? 1 : (pieces + 7) / 8, pitch = T::F16 ? pieces * 16 : 128;
+                if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(full), slabs * 32 * pitch);
                 __syncwarp();
                 const int x = slabs == 2 ? lane & 1 : 0, first = (slabs == 2 ? lane >> 1 : lane) * a.box;      // slab; of the warp's keys
                 const int bp = __shfl_sync(0xffffffffu, p, first & 31), bo = __shfl_sync(0xffffffffu, off, first & 31);
                 if (first < 32)
-                    tma_load_4d(place + x * T::SLAB + first * 128, values ? mv : mk, ptx::smem_u32(full), u * pieces * 8 + 64 * x, s.g, bo, bp);
+                    tma_load_4d(place + x * T::SLAB + first * pitch, values ? mv : mk, ptx::smem_u32(full), u * pieces * (16 / ELEM) + 64 * x, s.g, bo, bp);
             } else {
 #pragma unroll 4
                 for (int i = 0; i < pieces; ++i) {          // 32 keys' pieces, 32 at a time
@@ -1004,7 +1008,7 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
                     if (lane == 0) arrive(full);
                 }
             }
-            if (T::F16) kinds = kinds << 1 | (values ? 1u : 0u), ++waiting, ++raw;
+            if (T::F16) kinds = kinds << 1 | (values ? 1u : 0u), copied = copied << 1 | (boxes ? 0u : 1u), ++waiting, ++raw;
             if (values) ++nv;
             else ++nk;
             if (++u == (values ? T::NVU : T::NKU)) {
@@ -1014,9 +1018,18 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
             }
         }
         if (T::F16 && (waiting > LAG || !issue)) {          // the oldest one has come (or all have to): it is widened into its place
-            if (issue) cp_wait<LAG>();
-            else cp_wait<0>();
             const bool values = (kinds >> (waiting - 1)) & 1;
+            {
+                const uint32_t r = raw - waiting, st = r % (T::F16 ? T::RAW_STAGES : 1);
+                uint64_t* const bar = &ctrl->raw_full[warp][st];
+                if ((copied >> (waiting - 1)) & 1) {
+                    cp_wait<0>();
+                    __syncwarp();
+                    if (lane == 0) arrive(bar);             // (a parity names every other use of the place)
+                } else {
+                    wait_bar(bar, r / (T::F16 ? T::RAW_STAGES : 1), ctrl, a.status);
+                }
+            }
             // (the ones behind it, of the same kind, have been counted already)
             const uint32_t newer = __popc(kinds & ((1u << (waiting - 1)) - 1)), later = values ? newer : waiting - 1 - newer;
             const uint32_t n = (values ? nv : nk) - 1 - later, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
@@ -1046,7 +1059,10 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
         if (any_aborted(ctrl)) break;
     }
     cp_wait<0>();
-    if (!T::F16 && lane == 0 && aborted(ctrl)) landed(ctrl->k_full, nk, T::K_STAGES), landed(ctrl->v_full, nv, T::V_STAGES);
+    if (lane == 0 && aborted(ctrl)) {
+        if (T::F16) landed(ctrl->raw_full[warp], raw, T::F16 ? T::RAW_STAGES : 1);
+        else landed(ctrl->k_full, nk, T::K_STAGES), landed(ctrl->v_full, nv, T::V_STAGES);
+    }
     __syncwarp();
 }
 
@@ -1221,6 +1237,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         }
         for (int i = 0; i < T::K_STAGES; ++i) init(&ctrl->k_full[i], T::PAGED ? 4 : 1), init(&ctrl->k_empty[i], 1);
         for (int i = 0; i < T::V_STAGES; ++i) init(&ctrl->v_full[i], T::PAGED ? 4 : 1), init(&ctrl->v_empty[i], 1);
+        if (T::F16)
+            for (int i = 0; i < 12; ++i) init(&ctrl->raw_full[i / 3][i % 3], 1);
         init(&ctrl->x_full, 4), init(&ctrl->x_empty, 4), init(&ctrl->s_free, 4), init(&ctrl->drained[0], 1), init(&ctrl->drained[1], 1);
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();

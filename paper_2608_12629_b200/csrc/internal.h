@@ -78,8 +78,10 @@ int make_tmap_rows16(CUtensorMap* m, const void* base, i64 rows, int box_rows);
 int make_tmap_bytes(CUtensorMap* m, const void* base, i64 cols, i64 rows, i64 stride, int box_rows);
 // bf16 [tokens][heads][D], strides in bytes; box = 64 columns x box_heads heads x box_tokens tokens, 128-byte swizzle, zeros outside
 int make_tmap_heads(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride, i64 tokens, i64 stride, int box_heads, int box_tokens);
-// bf16 [pages][tokens][heads][D], any order of the outer three, strides in bytes; box = 64 columns x 1 head x box_tokens tokens of a page, 128-byte swizzle
-int make_tmap_pages(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride, int tokens, i64 token_stride, i64 pages, i64 page_stride, int box_tokens);
+// bf16 (or bytes) [pages][tokens][heads][D], any order of the outer three, strides in bytes, multiples of 16; box = `columns` x 1 head x box_tokens
+// tokens of a page, 128-byte swizzle (bytes: none)
+int make_tmap_pages(CUtensorMap* m, const void* base, int D, int heads, i64 head_stride, int tokens, i64 token_stride, i64 pages, i64 page_stride,
+                    int columns, int box_tokens, bool bytes);
 // Fused update (fuse_sums / fuse_counts / fuse_ctas all given, one problem, K <= 128, D <= 128 and room in shared
 // memory): the assign kernel also adds the rows of every tile to per-cluster sums on the tensor core.  On return
 // *fuse_ctas = n > 0 says that it did: fuse_sums then holds n partial sums of [128][round_up(D, 16)] floats (one per
