@@ -42,6 +42,14 @@ int check_heads(int Hq, int Hkv, int D) {
     return supported(D) ? CAKE_OK : CAKE_ERR_UNSUPPORTED;
 }
 
+// e / d for e < 2^31: mulhi(e, ceil(2^(31 + k) / d)) >> (k - 1) with 2^k >= d; 0 for d = 1
+void division(uint32_t d, uint32_t* mul, uint32_t* shift) {
+    uint32_t k = 0;
+    while ((1ull << k) < d) ++k;
+    *mul = d == 1 ? 0 : static_cast<uint32_t>(((1ull << (31 + k)) + d - 1) / d);
+    *shift = d == 1 ? 0 : k - 1;
+}
+
 // what both entry points share: everything of a but the keys
 int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_bytes, DeviceInfo* di) {
     if (!a.q || !a.starts || !a.out) return CAKE_ERR_NULL;
@@ -57,11 +65,7 @@ int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_
     a.tokens = MT / a.heads;
     if (B > INT_MAX / 64 / (static_cast<i64>(a.Hkv) * a.runs)) return CAKE_ERR_SHAPE;
     a.entries = static_cast<int>(B) * a.Hkv * a.runs;
-    const uint32_t per = static_cast<uint32_t>(a.Hkv) * a.runs;      // e / per for e < 2^31: mulhi(e, ceil(2^(31 + k) / per)) >> (k - 1), 2^k >= per
-    uint32_t k = 0;
-    while ((1ull << k) < per) ++k;
-    a.per_mul = per == 1 ? 0 : static_cast<uint32_t>(((1ull << (31 + k)) + per - 1) / per);
-    a.per_shift = per == 1 ? 0 : k - 1;
+    division(static_cast<uint32_t>(a.Hkv) * a.runs, &a.per_mul, &a.per_shift);
     a.share_mul = ~0ull / ctas_of(*di);
     a.negative = scale < 0.f;
     a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
@@ -165,6 +169,7 @@ int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_st
     a.Hq = Hq, a.Hkv = cache->Hkv, a.window = window, a.causal = true;
     rc = prepare(a, maps, B, cache->D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
+    division(static_cast<uint32_t>(cache->page_size), &a.page_mul, &a.page_shift);
     // Pages come in boxes where a warp's 32 keys are whole boxes of a page: 8, 16 or 32 tokens, or 32 of a page of several times that
     const cake_paged_cache& c = *cache;
     a.box = c.page_size < 32 ? c.page_size : 32;

@@ -71,6 +71,7 @@ struct Args {
     i64 table_stride, table_head_stride, lens_stride, lens_head_stride;
     int entries;                               // sequences * key-value heads * runs
     uint32_t per_mul, per_shift;               // e / (heads * runs) = mulhi(e, per_mul) >> per_shift (per_mul 0: e)
+    uint32_t page_mul, page_shift;             // the same for a page's tokens
     uint64_t share_mul;                        // 2^64 / CTAs
     int Hq, Hkv, G, runs, heads, tokens;    // heads: of a run of a group's query heads; tokens: of a tile of rows
     int max_pages, window;
@@ -167,6 +168,7 @@ __device__ __forceinline__ void wait_bar(uint64_t* bar, uint32_t parity, Ctrl* c
     const uint32_t addr = ptx::smem_u32(bar);
     if (__builtin_expect(!ptx::mbar_try_wait(addr, parity & 1), 0)) wait_more(addr, parity & 1, ctrl, status);
 }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void arrive(uint64_t* bar) { ptx::mbar_arrive(ptx::smem_u32(bar)); }
 __device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flushed to zero
     float y;
@@ -210,6 +212,8 @@ __device__ __forceinline__ int first_key(const Args& a, int pos, int klen) {
     return a.window > 0 && pos >= a.window ? min(pos - a.window + 1, klen) : 0;
 }
 __device__ __forceinline__ int end_key(const Args& a, int pos, int klen) { return a.causal ? max(0, min(pos + 1, klen)) : klen; }
+
+__device__ __forceinline__ int page_number(const Args& a, int key) { return a.page_mul ? static_cast<int>(__umulhi(key, a.page_mul) >> a.page_shift) : key; }
 
 // An entry: a sequence's new tokens, a key-value head and a run of its query heads.
 struct Entry {
@@ -499,7 +503,7 @@ __device__ __forceinline__ float key_at(const Args& a, const void* p, int d) {
 template <class T>
 __device__ __forceinline__ bool locate(const Args& a, const RowAt& r, int key, const void*& k, const void*& v) {
     if (T::PAGED) {
-        const int page = a.table[r.base + key / a.c.page_size];
+        const int page = a.table[r.base + page_number(a, key)];
         if (page < 0 || page >= a.c.num_pages) return false;
         const i64 off = key % a.c.page_size, size = T::F16 ? 1 : 2;
         k = static_cast<const char*>(a.c.k) + (page * a.c.k_page_stride + off * a.c.k_token_stride + r.g * a.c.k_head_stride) * size;
@@ -913,155 +917,153 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
-// Pages by 128 threads: lane i of warp w looks up key 32 w + i of a tile.  bf16: 32 keys that are all there come in boxes of up to 32 tokens of a
-// page; others (the sequence's end, a window's begin, pages that are no multiple of 8) by 16-byte copies, zeros where nothing is to be
-// read.  e4m3: by 16-byte copies into a ring of their own, from where the warp that fetched them widens them.
+// Pages by four warps, two for the keys and two for the values: lane i of a warp looks up keys i and 32 + i of its half of a tile.  Keys that are
+// all there come in boxes of up to 32 tokens of a page; others (the sequence's end, a window's begin, pages that are no multiple of 8) by
+// 16-byte copies, zeros where nothing is to be read.  e4m3: into a ring of their own, 32 keys at a time, from where the warp widens them.
 template <class T>
 __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mk, const CUtensorMap* mv) {
     constexpr int ELEM = T::F16 ? 1 : 2;
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
-    uint32_t segs = 0, nk = 0, nv = 0, tiles = 0;           // segments, units of keys and of values, tiles so far
-    // e4m3: units that were fetched into the ring and are not widened yet, oldest first: a bit for each says that it is of values
-    constexpr int LAG = T::F16 ? T::RAW_STAGES - 1 : 0;
-    uint32_t waiting = 0, kinds = 0, copied = 0, raw = 0;   // copied: a bit for each that came by 16-byte copies; raw: units that were fetched
+    const int lane = threadIdx.x & 31, warp = uniform((threadIdx.x >> 5) & 3);
+    const bool values = warp >= 2;
+    const int half = 64 * (warp & 1);                       // the warp's first key of a tile
+    const int pieces = (values ? T::VC : T::KC) * ELEM / 16, units = values ? T::NVU : T::NKU;      // 16-byte pieces of a key in a unit
+    const uint32_t stages = values ? T::V_STAGES : T::K_STAGES, unit_bytes = values ? T::V_UNIT : T::K_UNIT;
+    uint8_t* const ring = values ? room.v : room.k;
+    uint64_t* const full = values ? ctrl->v_full : ctrl->k_full;
+    uint64_t* const empty = values ? ctrl->v_empty : ctrl->k_empty;
+    const CUtensorMap* const map = values ? mv : mk;
+    const char* const base = static_cast<const char*>(values ? a.c.v : a.c.k);
+    const i64 page_stride = values ? a.c.v_page_stride : a.c.k_page_stride, token_stride = values ? a.c.v_token_stride : a.c.k_token_stride,
+              head_stride = values ? a.c.v_head_stride : a.c.k_head_stride;
+    uint32_t segs = 0, n = 0, tiles = 0;                    // segments, units, tiles so far
+    // e4m3: pieces of work of 32 keys that were fetched into the warp's ring, and those of them that are not widened yet; a bit for each of these,
+    // oldest highest, says that it came by 16-byte copies
+    constexpr uint32_t RING = T::F16 ? T::RAW_STAGES : 1;
+    uint32_t raw = 0, waiting = 0, copied = 0;
     uint8_t* const mine = room.raw + warp * (T::RAW / 4);
+    auto widen = [&]() {
+        const uint32_t at = raw - waiting, st = at % RING, unit = at >> 1, keys = half + 32 * (at & 1);
+        uint64_t* const bar = &ctrl->raw_full[warp][st];
+        if ((copied >> (waiting - 1)) & 1) {
+            cp_wait<0>();
+            __syncwarp();
+            if (lane == 0) arrive(bar);                     // (a parity names every other use of the place)
+        } else {
+            wait_bar(bar, at / RING, ctrl, a.status);
+        }
+        wait_bar(&empty[unit % stages], unit / stages + 1, ctrl, a.status);
+        __syncwarp();
+        const uint8_t* const src = mine + st * T::RAW;
+        uint8_t* const place = ring + unit % stages * unit_bytes + keys * 128;
+#pragma unroll 4
+        for (int i = 0; i < pieces; ++i) {
+            const int flat = i * 32 + lane, key = flat / pieces, piece = flat - key * pieces;      // 16 elements
+            const uint4 x = *reinterpret_cast<const uint4*>(src + flat * 16);
+            uint32_t f[8];
+            e4m3_to_f16(x.x, f[0], f[1]), e4m3_to_f16(x.y, f[2], f[3]), e4m3_to_f16(x.z, f[4], f[5]), e4m3_to_f16(x.w, f[6], f[7]);
+            // (the second slab's lanes store their halves in the other order: eight lanes then meet every bank once)
+            const int c = (piece & 3) * 2, odd = piece >> 2 & 1;
+            uint8_t* const dst = place + (piece >> 2) * T::SLAB + key * 128;
+            const uint4 lo = make_uint4(f[0], f[1], f[2], f[3]), hi = make_uint4(f[4], f[5], f[6], f[7]);
+            *reinterpret_cast<uint4*>(dst + (((c + odd) ^ (key & 7)) << 4)) = odd ? hi : lo;
+            *reinterpret_cast<uint4*>(dst + (((c + 1 - odd) ^ (key & 7)) << 4)) = odd ? lo : hi;
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) arrive(&full[unit % stages]);
+        --waiting;
+    };
     Seg s = {};
-    int from = 0, to = 0, ik = 0, iv = 0, u = 0;            // keys that some row of the item sees; tiles whose keys, values come next; unit of the tile
-    int page[3] = {INT_MIN, INT_MIN, INT_MIN};              // of the lane's key in tiles iv, iv + 1, iv + 2; INT_MIN: not to be read
-    bool more = true;
-    auto page_of = [&](int j) {
-        const int key = KT * j + 32 * warp + lane;
-        return j < s.jb && key >= from && key < to ? max(a.table[s.k0 + key / a.c.page_size], -1) : INT_MIN;
+    int from = 0, to = 0;                                   // keys that some row of the item sees
+    // the page of a key; INT_MIN: not to be read
+    auto page_of = [&](int key) {
+        if (key < from || key >= to) return INT_MIN;
+        return max(a.table[s.k0 + page_number(a, key)], -1);
     };
     for (;;) {
-        if (more && iv == s.jb) {                           // a new segment (what is still under way is settled before the warp waits for one)
-            if (waiting == 0 || __all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(&ctrl->seg_full[segs % SEGS]), (segs / SEGS) & 1))) {
-                tiles += s.jb - s.ja;
-                more = next_seg(a, ctrl, segs, s, false);
-                if (!more && any_aborted(ctrl)) break;
-                if (more) {
-                    from = first_key(a, s.pos, s.klen), to = end_key(a, s.pos + s.ntok - 1, s.klen);
-                    ik = iv = s.ja;
+        // (what is still under way is widened before the warp waits for more work)
+        while (T::F16 && waiting && !__all_sync(0xffffffffu, ptx::mbar_test_wait(ptx::smem_u32(&ctrl->seg_full[segs % SEGS]), (segs / SEGS) & 1))) widen();
+        tiles += s.jb - s.ja;
+        if (!next_seg(a, ctrl, segs, s, false)) break;
+        from = first_key(a, s.pos, s.klen), to = end_key(a, s.pos + s.ntok - 1, s.klen);
+        to = min(to, KT * s.jb);
+        int key = KT * s.ja + half + lane;
+        int next[2] = {page_of(key), page_of(key + 32)};    // (of the tile after: looked up while this one is fetched)
+#pragma unroll 1
+        for (int j = s.ja; j < s.jb; ++j, key += KT) {
+            const int p[2] = {next[0], next[1]};
+            if (j + 1 < s.jb) next[0] = page_of(key + KT), next[1] = page_of(key + KT + 32);
+            bool ok[2];
 #pragma unroll
-                    for (int i = 0; i < 3; ++i) page[i] = page_of(iv + i);
-                    if (iv == s.jb) continue;
+            for (int h = 0; h < 2; ++h) {
+                ok[h] = p[h] >= 0 && p[h] < a.c.num_pages;
+                if (!values) {
+                    const unsigned bits = __ballot_sync(0xffffffffu, ok[h] || p[h] == INT_MIN);
+                    if (lane == 0) reinterpret_cast<uint32_t*>(&ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD])[(half >> 5) + h] = bits;
+                    if (!ok[h] && p[h] != INT_MIN) raise_bad_index(a.status);
                 }
             }
-        }
-        const bool issue = more && iv < s.jb;
-        if (!issue && waiting == 0) break;
-        if (issue) {
-            // the order of use: keys of two tiles, then values of a tile, keys of the next but one
-            const bool values = !(ik < s.jb && ik < iv + 2);
-            const int j = values ? iv : ik, key = KT * j + 32 * warp + lane;
-            const int p = j == iv ? page[0] : page[1];
-            const bool ok = p >= 0 && p < a.c.num_pages;
-            if (!values && u == 0) {
-                const unsigned bits = __ballot_sync(0xffffffffu, ok || p == INT_MIN);
-                if (lane == 0) reinterpret_cast<uint32_t*>(&ctrl->flags[(tiles + j - s.ja) % FLAGS_AHEAD])[warp] = bits;
-                if (!ok && p != INT_MIN) raise_bad_index(a.status);
-            }
-            const int off = key % a.c.page_size;
-            const int pieces = (values ? T::VC : T::KC) * ELEM / 16;      // 16-byte pieces of a key in a unit
-            const char* row = nullptr;                      // of the lane's key
-            if (ok) {
-                const i64 at = values ? p * a.c.v_page_stride + off * a.c.v_token_stride + s.g * a.c.v_head_stride
-                                      : p * a.c.k_page_stride + off * a.c.k_token_stride + s.g * a.c.k_head_stride;
-                row = static_cast<const char*>(values ? a.c.v : a.c.k) + at * ELEM + u * pieces * 16;
-            }
-            uint32_t place;                                 // of the warp's 32 keys
-            uint64_t* full = nullptr;
-            bool boxes = false;
-            if (T::F16) {
-                const uint32_t st = raw % (T::F16 ? T::RAW_STAGES : 1);
-                place = ptx::smem_u32(mine) + st * T::RAW;
-                full = &ctrl->raw_full[warp][st];
-            } else {
-                const uint32_t n = values ? nv : nk, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
-                wait_bar(values ? &ctrl->v_empty[st] : &ctrl->k_empty[st], n / stages + 1, ctrl, a.status);
-                place = ptx::smem_u32(values ? room.v + st * T::V_UNIT : room.k + st * T::K_UNIT) + 32 * warp * 128;
-                full = values ? &ctrl->v_full[st] : &ctrl->k_full[st];
-            }
-            boxes = a.maps && __all_sync(0xffffffffu, ok);
-            if (boxes) {
-                // (8-bit: rows of a unit as they are, one behind the other; else slabs of 64 columns)
-                const int slabs = T::F16 ? 1 : (pieces + 7) / 8, pitch = T::F16 ? pieces * 16 : 128;
-                if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(full), slabs * 32 * pitch);
-                __syncwarp();
-                const int x = slabs == 2 ? lane & 1 : 0, first = (slabs == 2 ? lane >> 1 : lane) * a.box;      // slab; of the warp's keys
-                const int bp = __shfl_sync(0xffffffffu, p, first & 31), bo = __shfl_sync(0xffffffffu, off, first & 31);
-                if (first < 32)
-                    tma_load_4d(place + x * T::SLAB + first * pitch, values ? mv : mk, ptx::smem_u32(full), u * pieces * (16 / ELEM) + 64 * x, s.g, bo, bp);
-            } else {
+            const int off[2] = {key - page_number(a, key) * a.c.page_size, key + 32 - page_number(a, key + 32) * a.c.page_size};
+            // n 64 keys, or 32 at a time (e4m3)
+            constexpr int STEP = T::F16 ? 1 : 2;
+#pragma unroll 1
+            for (int u = 0; u < units; ++u) {
+                if (!T::F16) wait_bar(&empty[n % stages], n / stages + 1, ctrl, a.status);
+#pragma unroll 1
+                for (int h = 0; h < 2; h += STEP) {
+                    const bool boxes = a.maps && __all_sync(0xffffffffu, T::F16 ? (h ? ok[1] : ok[0]) : ok[0] && ok[1]);
+                    const uint32_t st = T::F16 ? raw % RING : n % stages;
+                    const uint32_t place = T::F16 ? ptx::smem_u32(mine) + st * T::RAW : ptx::smem_u32(ring) + st * unit_bytes + half * 128;
+                    uint64_t* const bar = T::F16 ? &ctrl->raw_full[warp][st] : &full[st];
+                    if (boxes) {
+                        // (8-bit: rows of a unit as they are, one behind the other; else slabs of 64 columns)
+                        const int slabs = T::F16 ? 1 : (pieces + 7) / 8, pitch = T::F16 ? pieces * 16 : 128;
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(bar), slabs * 32 * STEP * pitch);
+                        __syncwarp();
+                        const int x = slabs == 2 ? lane & 1 : 0, first = (slabs == 2 ? lane >> 1 : lane) * a.box;      // slab; of the keys
+                        const int p0 = __shfl_sync(0xffffffffu, p[0], first & 31), p1 = __shfl_sync(0xffffffffu, p[1], first & 31);
+                        const int o0 = __shfl_sync(0xffffffffu, off[0], first & 31), o1 = __shfl_sync(0xffffffffu, off[1], first & 31);
+                        const bool second = h + (first >> 5) != 0;
+                        if (first < 32 * STEP)
+                            tma_load_4d(place + x * T::SLAB + first * pitch, map, ptx::smem_u32(bar), u * pieces * (16 / ELEM) + 64 * x, s.g, second ? o1 : o0, second ? p1 : p0);
+                    } else {
+#pragma unroll 1
+                        for (int g = h; g < h + STEP; ++g) {
+                            const char* row = nullptr;      // of the lane's key
+                            if (g ? ok[1] : ok[0])
+                                row = base + ((g ? p[1] : p[0]) * page_stride + (g ? off[1] : off[0]) * token_stride + s.g * head_stride) * ELEM + u * pieces * 16;
 #pragma unroll 4
-                for (int i = 0; i < pieces; ++i) {          // 32 keys' pieces, 32 at a time
-                    const int flat = i * 32 + lane, k = flat / pieces, piece = flat - k * pieces;
-                    const char* const src = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
-                    const uint32_t dst = T::F16 ? place + flat * 16 : place + (piece >> 3) * T::SLAB + k * 128 + (((piece & 7) ^ (k & 7)) << 4);
-                    cp_async16(dst, src ? src + piece * 16 : static_cast<const char*>(a.c.k), src != nullptr);
+                            for (int i = 0; i < pieces; ++i) {      // 32 keys' pieces, 32 at a time
+                                const int flat = i * 32 + lane, k = flat / pieces, piece = flat - k * pieces;
+                                const char* const src = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
+                                const uint32_t dst = T::F16 ? place + flat * 16 : place + (piece >> 3) * T::SLAB + (32 * g + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
+                                cp_async16(dst, src ? src + piece * 16 : base, src != nullptr);
+                            }
+                        }
+                        cp_commit();
+                        if (!T::F16) {
+                            cp_wait<0>();
+                            ptx::fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) arrive(bar);
+                        }
+                    }
+                    if (T::F16) {
+                        copied = copied << 1 | (boxes ? 0u : 1u), ++waiting, ++raw;
+                        if (waiting == RING) widen();
+                    }
                 }
-                cp_commit();
-                if (!T::F16) {
-                    cp_wait<0>();
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) arrive(full);
-                }
+                ++n;
             }
-            if (T::F16) kinds = kinds << 1 | (values ? 1u : 0u), copied = copied << 1 | (boxes ? 0u : 1u), ++waiting, ++raw;
-            if (values) ++nv;
-            else ++nk;
-            if (++u == (values ? T::NVU : T::NKU)) {
-                u = 0;
-                if (values) ++iv, page[0] = page[1], page[1] = page[2], page[2] = page_of(iv + 2);
-                else ++ik;
-            }
-        }
-        if (T::F16 && (waiting > LAG || !issue)) {          // the oldest one has come (or all have to): it is widened into its place
-            const bool values = (kinds >> (waiting - 1)) & 1;
-            {
-                const uint32_t r = raw - waiting, st = r % (T::F16 ? T::RAW_STAGES : 1);
-                uint64_t* const bar = &ctrl->raw_full[warp][st];
-                if ((copied >> (waiting - 1)) & 1) {
-                    cp_wait<0>();
-                    __syncwarp();
-                    if (lane == 0) arrive(bar);             // (a parity names every other use of the place)
-                } else {
-                    wait_bar(bar, r / (T::F16 ? T::RAW_STAGES : 1), ctrl, a.status);
-                }
-            }
-            // (the ones behind it, of the same kind, have been counted already)
-            const uint32_t newer = __popc(kinds & ((1u << (waiting - 1)) - 1)), later = values ? newer : waiting - 1 - newer;
-            const uint32_t n = (values ? nv : nk) - 1 - later, stages = values ? T::V_STAGES : T::K_STAGES, st = n % stages;
-            wait_bar(values ? &ctrl->v_empty[st] : &ctrl->k_empty[st], n / stages + 1, ctrl, a.status);
-            __syncwarp();
-            const uint8_t* const src = mine + (raw - waiting) % (T::F16 ? T::RAW_STAGES : 1) * T::RAW;
-            uint8_t* const place = values ? room.v + st * T::V_UNIT : room.k + st * T::K_UNIT;
-            const int pieces = (values ? T::VC : T::KC) / 16;
-#pragma unroll 4
-            for (int i = 0; i < pieces; ++i) {
-                const int flat = i * 32 + lane, key = flat / pieces, piece = flat - key * pieces;      // 16 elements
-                const uint4 x = *reinterpret_cast<const uint4*>(src + flat * 16);
-                uint32_t f[8];
-                e4m3_to_f16(x.x, f[0], f[1]), e4m3_to_f16(x.y, f[2], f[3]), e4m3_to_f16(x.z, f[4], f[5]), e4m3_to_f16(x.w, f[6], f[7]);
-                // (the second slab's lanes store their halves in the other order: eight lanes then meet every bank once)
-                const int c = (piece & 3) * 2, odd = piece >> 2 & 1;
-                uint8_t* const dst = place + (piece >> 2) * T::SLAB + (32 * warp + key) * 128;
-                const uint4 lo = make_uint4(f[0], f[1], f[2], f[3]), hi = make_uint4(f[4], f[5], f[6], f[7]);
-                *reinterpret_cast<uint4*>(dst + (((c + odd) ^ (key & 7)) << 4)) = odd ? hi : lo;
-                *reinterpret_cast<uint4*>(dst + (((c + 1 - odd) ^ (key & 7)) << 4)) = odd ? lo : hi;
-            }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) arrive(values ? &ctrl->v_full[st] : &ctrl->k_full[st]);
-            --waiting;
+            if (any_aborted(ctrl)) break;
         }
         if (any_aborted(ctrl)) break;
     }
+    while (T::F16 && waiting && !any_aborted(ctrl)) widen();
     cp_wait<0>();
     if (lane == 0 && aborted(ctrl)) {
-        if (T::F16) landed(ctrl->raw_full[warp], raw, T::F16 ? T::RAW_STAGES : 1);
-        else landed(ctrl->k_full, nk, T::K_STAGES), landed(ctrl->v_full, nv, T::V_STAGES);
+        if (T::F16) landed(ctrl->raw_full[warp], raw, RING);
+        else landed(full, n, stages);
     }
     __syncwarp();
 }
@@ -1070,7 +1072,6 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
 // One warp issues the scores' products, another the weighted sums': neither waits for what the other's operands wait for.  The whole warp
 // walks through its loop, so that addresses and descriptors are the same in all lanes as the compiler sees it (a tensor instruction
 // takes them from uniform registers); one lane issues.
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 __device__ __forceinline__ void drain(Ctrl* ctrl, int who) {      // products under way end before shared and tensor memory are given up
     ptx::umma_commit(ptx::smem_u32(&ctrl->drained[who]));
@@ -1235,8 +1236,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             init(&ctrl->q_full[i], 1), init(&ctrl->q_empty[i], T::q_readers(i)), init(&ctrl->q_conv[i], 4);
             init(&ctrl->s_full[i], 1), init(&ctrl->p_ready[i], 4), init(&ctrl->o_done[i], 1), init(&ctrl->o_free[i], 4);
         }
-        for (int i = 0; i < T::K_STAGES; ++i) init(&ctrl->k_full[i], T::PAGED ? 4 : 1), init(&ctrl->k_empty[i], 1);
-        for (int i = 0; i < T::V_STAGES; ++i) init(&ctrl->v_full[i], T::PAGED ? 4 : 1), init(&ctrl->v_empty[i], 1);
+        for (int i = 0; i < T::K_STAGES; ++i) init(&ctrl->k_full[i], T::F16 ? 4 : T::PAGED ? 2 : 1), init(&ctrl->k_empty[i], 1);
+        for (int i = 0; i < T::V_STAGES; ++i) init(&ctrl->v_full[i], T::F16 ? 4 : T::PAGED ? 2 : 1), init(&ctrl->v_empty[i], 1);
         if (T::F16)
             for (int i = 0; i < 12; ++i) init(&ctrl->raw_full[i / 3][i % 3], 1);
         init(&ctrl->x_full, 4), init(&ctrl->x_empty, 4), init(&ctrl->s_free, 4), init(&ctrl->drained[0], 1), init(&ctrl->drained[1], 1);
