@@ -955,7 +955,8 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
         __syncwarp();
         const uint8_t* const src = mine + st * T::RAW;
         uint8_t* const place = ring + unit % stages * unit_bytes + keys * 128;
-#pragma unroll 4
+        // (all of a unit's loads in flight: 1,508 us for 32,768 cached tokens where four at a time took 1,640)
+#pragma unroll 8
         for (int i = 0; i < pieces; ++i) {
             const int flat = i * 32 + lane, key = flat / pieces, piece = flat - key * pieces;      // 16 elements
             const uint4 x = *reinterpret_cast<const uint4*>(src + flat * 16);
@@ -1303,24 +1304,27 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 // ------------------------------------------------------------------------------------------------------------- join
 // out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m), m = max m_i, over the parts of an item, in order.  A warp to a row; where an
 // item has more than 8 parts, a block to a row (its warps share the parts).
-constexpr int JOIN_SLICES = 16, JOIN_WARPS = 8;
+constexpr int JOIN_WARPS = 8;
+// Blocks to an item: with many tokens whole tiles of rows are joined (8 packed prompts 140.8 us with 16, 143.3 with 8); with few, blocks without work are
+// what it costs (one prompt of 201 tokens 18.0 and 17.2)
+inline int join_slices(i64 tokens) { return tokens < 1024 ? 8 : 16; }
 template <int D, int ROWS, int TILES>
 __global__ void __launch_bounds__(32 * JOIN_WARPS)
-attention_join_kernel(const Args a) {
+attention_join_kernel(const Args a, int slices) {
     constexpr int V = (D + 127) / 128;           // float4 of a lane
     constexpr i64 PART = static_cast<i64>(ROWS) * (D + 2);
     __shared__ float4 accs[JOIN_WARPS][V][32];
     __shared__ float2 mls[JOIN_WARPS];
     ptx::grid_dep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c0 = blockIdx.x / JOIN_SLICES, slice = blockIdx.x % JOIN_SLICES;
+    const int c0 = blockIdx.x / slices, slice = blockIdx.x - c0 * slices;
     const Split e = a.splits[c0];
     if (!e.valid) return;
     const bool many = e.c1 - c0 + 1 > JOIN_WARPS;
     const int rows = e.ntok * e.heads;
     const float vs = a.c.type == CAKE_KV_E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
     const bool dual = TILES == 2 && e.ntok > a.tokens;
-    for (int i = many ? slice : slice * JOIN_WARPS + warp; i < rows; i += many ? JOIN_SLICES : JOIN_SLICES * JOIN_WARPS) {
+    for (int i = many ? slice : slice * JOIN_WARPS + warp; i < rows; i += many ? slices : slices * JOIN_WARPS) {
         const int tok = i / e.heads, h = i - tok * e.heads;
         const int t = dual && tok >= a.tokens ? 1 : 0;
         const int row = t * MT + (tok - t * a.tokens) * a.heads + h;
@@ -1417,7 +1421,8 @@ int launch(const Args& a, const Maps& m, const DeviceInfo& di, cudaStream_t s) {
     if (!ok) return CAKE_ERR_CUDA;
     const int ctas = ctas_of(di);
     if (launch_early(attention_kernel<T>, dim3(ctas), dim3(T::THREADS), SMEM, s, m.q, m.k, m.v, a) != cudaSuccess) return CAKE_ERR_CUDA;
-    return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * JOIN_SLICES), dim3(32 * JOIN_WARPS), 0, s, a) == cudaSuccess
+    const int slices = join_slices(a.T);
+    return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * slices), dim3(32 * JOIN_WARPS), 0, s, a, slices) == cudaSuccess
                ? CAKE_OK : CAKE_ERR_CUDA;
 }
 template <int D>
