@@ -75,6 +75,14 @@ int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_
     return make_map(&maps.q, a.q, D, a.Hq, a.q_head_stride, a.T, a.q_stride, a.heads, a.tokens);
 }
 
+// Whether an item can have so many tiles of keys that its share may be cut (`most`: keys of a sequence).  If not, nothing has to be joined: one launch
+// (a prompt of 201 tokens 17.3 -> 14 us)
+bool may_cut(const Args& a, int D, i64 most) {
+    const i64 tokens = static_cast<i64>(D == 256 ? 1 : 2) * a.tokens;
+    const i64 tiles = a.window > 0 && a.window + tokens < most ? (a.window + tokens) / KT + 2 : (most + KT - 1) / KT;
+    return tiles >= 2 * SNAP;
+}
+
 int launch_any(const Args& a, const Maps& m, int D, int kind, const DeviceInfo& di, cudaStream_t s) {
     switch (D) {
         case 64: return launch_64(a, m, kind, di, s);
@@ -130,6 +138,7 @@ int cake_prompt_attention(const cake_bf16* q, long long q_stride, long long q_he
     a.Hq = Hq, a.Hkv = Hkv, a.window = window, a.causal = flags & CAKE_ATTENTION_CAUSAL;
     rc = prepare(a, maps, B, D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
+    a.cuts = may_cut(a, D, Tk);
     if (Tk == 0) {      // (no keys at all: nothing is loaded, any map will do)
         maps.k = maps.v = maps.q;
     } else {
@@ -169,15 +178,16 @@ int cake_paged_chunk(const cake_bf16* q, long long q_stride, long long q_head_st
     a.Hq = Hq, a.Hkv = cache->Hkv, a.window = window, a.causal = true;
     rc = prepare(a, maps, B, cache->D, scale, ws, ws_bytes, &di);
     if (rc != CAKE_OK) return rc;
+    a.cuts = may_cut(a, cache->D, static_cast<i64>(max_pages) * cache->page_size);
     division(static_cast<uint32_t>(cache->page_size), &a.page_mul, &a.page_shift);
     // Pages come in boxes where a warp's 32 keys are whole boxes of a page: 8, 16 or 32 tokens, or 32 of a page of several times that
     const cake_paged_cache& c = *cache;
     a.box = c.page_size < 32 ? c.page_size : 32;
     const bool bytes = c.type == CAKE_KV_E4M3;
-    const int k_columns = bytes ? (c.D == 256 ? 64 : c.D) : 64, v_columns = bytes ? (c.D == 256 ? 128 : c.D) : 64;
+    const int columns = bytes ? (c.D == 256 ? 128 : c.D) : 64;
     a.maps = (c.page_size % 32 == 0 || c.page_size == 16 || c.page_size == 8) &&
-             make_map_pages(&maps.k, c.k, c, c.k_head_stride, c.k_token_stride, c.k_page_stride, k_columns, a.box) == CAKE_OK &&
-             make_map_pages(&maps.v, c.v, c, c.v_head_stride, c.v_token_stride, c.v_page_stride, v_columns, a.box) == CAKE_OK;
+             make_map_pages(&maps.k, c.k, c, c.k_head_stride, c.k_token_stride, c.k_page_stride, columns, a.box) == CAKE_OK &&
+             make_map_pages(&maps.v, c.v, c, c.v_head_stride, c.v_token_stride, c.v_page_stride, columns, a.box) == CAKE_OK;
     if (!a.maps) maps.k = maps.v = maps.q;      // (not used)
     return launch_any(a, maps, cache->D, cache->type == CAKE_KV_E4M3 ? PAGED_E4M3 : PAGED_BF16, di, reinterpret_cast<cudaStream_t>(stream));
 }

@@ -77,6 +77,7 @@ struct Args {
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
     bool negative, causal;                     // sign of the scale
+    bool cuts;                                 // an item may be shared by CTAs
     bool maps;                                 // paged: mk and mv are maps of the pages, boxes of `box` tokens
     int box;
 };
@@ -97,10 +98,11 @@ struct Traits {
     static constexpr bool PAGED = KIND != PACKED, F16 = KIND == PAGED_E4M3;
     static constexpr int TILES = D == 256 ? 1 : 2;
     // Keys and values have a ring of places each (64 KiB), a tile of them comes in units of KC (VC) columns, in slabs of 64: 128-byte rows,
-    // 128-byte swizzle.  Heads of 256: smaller units of keys, so that the next tile's come in behind this one's products
+    // 128-byte swizzle.  Heads of 256: smaller units of keys, so that the next tile's come in behind this one's products (8-bit ones: a unit's start and
+    // end is most of what it costs to widen it)
     static constexpr uint32_t SLAB = MT * 128;
     static constexpr int SLABS = (D + 63) / 64;
-    static constexpr int KC = D == 256 ? 64 : D, VC = D == 256 ? 128 : D;
+    static constexpr int KC = D == 256 ? (F16 ? 128 : 64) : D, VC = D == 256 ? 128 : D;
     static constexpr int NKU = D / KC, NVU = D / VC;
     static constexpr int K_SLABS = (KC + 63) / 64, V_SLABS = (VC + 63) / 64;
     static constexpr uint32_t K_UNIT = K_SLABS * SLAB, V_UNIT = V_SLABS * SLAB;
@@ -927,6 +929,9 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
     const bool values = warp >= 2;
     const int half = 64 * (warp & 1);                       // the warp's first key of a tile
     const int pieces = (values ? T::VC : T::KC) * ELEM / 16, units = values ? T::NVU : T::NKU;      // 16-byte pieces of a key in a unit
+    // (units of two sizes: powers of two)
+    static_assert(T::KC == T::VC || (T::VC == 2 * T::KC && T::KC == 64), "");
+    auto over_pieces = [&](int i) { return T::KC == T::VC ? i / (T::KC * ELEM / 16) : i >> ((ELEM == 1 ? 2 : 3) + (values ? 1 : 0)); };
     const uint32_t stages = values ? T::V_STAGES : T::K_STAGES, unit_bytes = values ? T::V_UNIT : T::K_UNIT;
     uint8_t* const ring = values ? room.v : room.k;
     uint64_t* const full = values ? ctrl->v_full : ctrl->k_full;
@@ -958,7 +963,7 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
         // (all of a unit's loads in flight: 1,508 us for 32,768 cached tokens where four at a time took 1,640)
 #pragma unroll 8
         for (int i = 0; i < pieces; ++i) {
-            const int flat = i * 32 + lane, key = flat / pieces, piece = flat - key * pieces;      // 16 elements
+            const int flat = i * 32 + lane, key = over_pieces(flat), piece = flat - key * pieces;      // 16 elements
             const uint4 x = *reinterpret_cast<const uint4*>(src + flat * 16);
             uint32_t f[8];
             e4m3_to_f16(x.x, f[0], f[1]), e4m3_to_f16(x.y, f[2], f[3]), e4m3_to_f16(x.z, f[4], f[5]), e4m3_to_f16(x.w, f[6], f[7]);
@@ -1035,7 +1040,7 @@ __device__ __forceinline__ void load_pages(const Args& a, Ctrl* ctrl, const Room
                                 row = base + ((g ? p[1] : p[0]) * page_stride + (g ? off[1] : off[0]) * token_stride + s.g * head_stride) * ELEM + u * pieces * 16;
 #pragma unroll 4
                             for (int i = 0; i < pieces; ++i) {      // 32 keys' pieces, 32 at a time
-                                const int flat = i * 32 + lane, k = flat / pieces, piece = flat - k * pieces;
+                                const int flat = i * 32 + lane, k = over_pieces(flat), piece = flat - k * pieces;
                                 const char* const src = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), k));
                                 const uint32_t dst = T::F16 ? place + flat * 16 : place + (piece >> 3) * T::SLAB + (32 * g + k) * 128 + (((piece & 7) ^ (k & 7)) << 4);
                                 cp_async16(dst, src ? src + piece * 16 : base, src != nullptr);
@@ -1302,29 +1307,28 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------------------- join
-// out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m), m = max m_i, over the parts of an item, in order.  A warp to a row; where an
-// item has more than 8 parts, a block to a row (its warps share the parts).
-constexpr int JOIN_WARPS = 8;
-// Blocks to an item: with many tokens whole tiles of rows are joined (8 packed prompts 140.8 us with 16, 143.3 with 8); with few, blocks without work are
-// what it costs (one prompt of 201 tokens 18.0 and 17.2)
-inline int join_slices(i64 tokens) { return tokens < 1024 ? 8 : 16; }
+// out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m), m = max m_i, over the parts of an item, in order.  A warp to a row, or, for few rows of many
+// parts, a block to a row (its warps share the parts).
+constexpr int JOIN_WARPS = 8, JOIN_BATCH = 4, JOIN_SLICES = 16;      // SLICES: blocks to an item
 template <int D, int ROWS, int TILES>
 __global__ void __launch_bounds__(32 * JOIN_WARPS)
-attention_join_kernel(const Args a, int slices) {
+attention_join_kernel(const Args a) {
     constexpr int V = (D + 127) / 128;           // float4 of a lane
     constexpr i64 PART = static_cast<i64>(ROWS) * (D + 2);
     __shared__ float4 accs[JOIN_WARPS][V][32];
     __shared__ float2 mls[JOIN_WARPS];
     ptx::grid_dep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c0 = blockIdx.x / slices, slice = blockIdx.x - c0 * slices;
+    const int c0 = blockIdx.x / JOIN_SLICES, slice = blockIdx.x % JOIN_SLICES;
     const Split e = a.splits[c0];
     if (!e.valid) return;
-    const bool many = e.c1 - c0 + 1 > JOIN_WARPS;
-    const int rows = e.ntok * e.heads;
+    const int rows = e.ntok * e.heads, parts = e.c1 - c0 + 1;
+    // rounds of loads, one behind the other: a row to a warp, or to a block
+    const bool many = (rows + JOIN_SLICES - 1) / JOIN_SLICES * ((parts + JOIN_WARPS * JOIN_BATCH - 1) / (JOIN_WARPS * JOIN_BATCH) + 1) <
+                      (rows + JOIN_SLICES * JOIN_WARPS - 1) / (JOIN_SLICES * JOIN_WARPS) * ((parts + JOIN_BATCH - 1) / JOIN_BATCH);
     const float vs = a.c.type == CAKE_KV_E4M3 && a.c.v_scale ? a.c.v_scale[e.g] : 1.f;
     const bool dual = TILES == 2 && e.ntok > a.tokens;
-    for (int i = many ? slice : slice * JOIN_WARPS + warp; i < rows; i += many ? slices : slices * JOIN_WARPS) {
+    for (int i = many ? slice : slice * JOIN_WARPS + warp; i < rows; i += many ? JOIN_SLICES : JOIN_SLICES * JOIN_WARPS) {
         const int tok = i / e.heads, h = i - tok * e.heads;
         const int t = dual && tok >= a.tokens ? 1 : 0;
         const int row = t * MT + (tok - t * a.tokens) * a.heads + h;
@@ -1343,7 +1347,7 @@ attention_join_kernel(const Args a, int slices) {
             }
         };
         const int step = many ? JOIN_WARPS : 1;
-        constexpr int BATCH = 4;
+        constexpr int BATCH = JOIN_BATCH;
         for (int c = c0 + (many ? warp : 0); c <= e.c1; c += BATCH * step) {
             float4 u[BATCH][V];
             float2 ml[BATCH];
@@ -1421,8 +1425,8 @@ int launch(const Args& a, const Maps& m, const DeviceInfo& di, cudaStream_t s) {
     if (!ok) return CAKE_ERR_CUDA;
     const int ctas = ctas_of(di);
     if (launch_early(attention_kernel<T>, dim3(ctas), dim3(T::THREADS), SMEM, s, m.q, m.k, m.v, a) != cudaSuccess) return CAKE_ERR_CUDA;
-    const int slices = join_slices(a.T);
-    return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * slices), dim3(32 * JOIN_WARPS), 0, s, a, slices) == cudaSuccess
+    if (!a.cuts) return CAKE_OK;
+    return launch_early(attention_join_kernel<T::D, T::PART_ROWS, T::TILES>, dim3(ctas * JOIN_SLICES), dim3(32 * JOIN_WARPS), 0, s, a) == cudaSuccess
                ? CAKE_OK : CAKE_ERR_CUDA;
 }
 template <int D>
