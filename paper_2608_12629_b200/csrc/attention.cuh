@@ -648,7 +648,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             }
         }
         const bool idle = !__any_sync(0xffffffffu, tok < a.tokens && my_tok < sp->ntok);      // a warp without a row: P may hold anything there
-        float m = NEG_INF, l = 0.f;                // m: the maximum that is subtracted, without LIFT
+        // Rows that are none, or see nothing, have no maximum to look for: whatever their scores are (what lay in shared memory, for rows behind the
+        // queries' box), they do not hold up the others
+        const bool live = tok < a.tokens && my_tok < sp->ntok && k0 < k1;
+        float m = live ? NEG_INF : 0.f, l = 0.f;   // m: the maximum that is subtracted, without LIFT
         for (int i = 0; i < n_mine; ++i) {
             const int key0 = KT * (first + i * step);
             const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
@@ -744,7 +747,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 }
                 total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 // (the second time m is the maximum: no more than that can be done for scores so large that their differences are lost)
-                search = !search && total > LIMIT;
+                search = live && !search && total > LIMIT;
                 if (pass > 0 || !__any_sync(0xffffffffu, search)) break;
             }
             ++o_count[pb];
