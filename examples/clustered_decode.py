@@ -84,10 +84,10 @@ def main(tokens=4096, device="cuda:0", seed=0):
     cake.cake_kv_append(cache, k, v, slots[:tokens], position[:tokens], table, ws=ws)
 
     # clusters of each head's cached keys
-    flat = k_cache.view(-1, HKV, D)
+    by_head, _ = cake.cake_kv_read(cache, slots[:tokens], by_head=True, want_v=False, ws=ws)
     found = []
     for h in range(HKV):
-        keys = flat[slots[:tokens], h].contiguous()
+        keys = by_head[h]
         found.append(cake.cake_kmeans_lloyd(keys, inputs.sample_init(keys, CLUSTERS, seed + h), ITERS))
 
     # a decode step: the new token into the cache, its clusters, attention over their tokens and the most recent ones

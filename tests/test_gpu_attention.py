@@ -467,3 +467,39 @@ def test_no_tokens_and_refusals():
     for bad in (dict(page_table=table.long()), dict(q=qc.float())):
         with pytest.raises(TypeError):
             cake.cake_paged_chunk(**{**dict(q=qc, cache=cache, page_table=table, seq_lens=n, starts=starts_of([2])), **bad})
+
+
+@pytest.mark.parametrize("D,kv", [(64, "bf16"), (128, "bf16"), (256, "bf16"), (128, "e4m3"), (256, "e4m3")])
+@pytest.mark.parametrize("up", [True, False])
+def test_scores_that_grow_or_fall_along_the_sequence(D, kv, up):
+    """A maximum that rises by hundreds from tile to tile is followed (what went before then weighs nothing); one that falls is kept."""
+    new, lens = [70, 3], [1500, 900]
+    q, cache, table, n = paged(21, new, lens, 4, 2, D, 16, kv)
+    q.abs_().clamp_(min=0.05)
+    g = gen(22)
+    for b, L in enumerate(lens):
+        t = torch.arange(L, device=DEV)
+        where = (table[b, t // 16].long(), t % 16)
+        size = (t if up else L - t).float() / L * (400 if kv == "e4m3" else 40)
+        rows = size[:, None, None] * (0.9 + 0.1 * torch.rand(L, 2, D, generator=g, device=DEV))
+        if kv == "e4m3":
+            cache.k.view(torch.uint8)[where] = rows.to(E4M3).view(torch.uint8)
+        else:
+            cache.k[where] = rows.to(BF16)
+    out, lse = run_chunk(q, cache, table, n, new)
+    check_chunk(out, lse, q, cache, table, new, lens)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+def test_huge_scores_do_not_hang_and_follow_the_largest():
+    """Scores of 10^30 and more, whose differences 32 bits do not hold: the calls end, and rows with one largest key give its value."""
+    lens = [260]
+    q, k, v = packed(23, lens, lens, 2, 1, 64)
+    q[:] = 2.0 ** 60
+    k[:] = 0
+    k[7, 0, 0] = 2.0 ** 60
+    out, lse = run_packed(q, k, v, lens, lens)
+    assert torch.equal(out[7:], v[7].expand(253, 2, 64)) and torch.isfinite(out[:7]).all()
+    k[:] = torch.randn(260, 1, 64, device=DEV).bfloat16() * 2.0 ** 60
+    out, lse = run_packed(q, k, v, lens, lens)
+    assert out.shape == q.shape
