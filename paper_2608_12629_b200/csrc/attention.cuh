@@ -351,8 +351,17 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     constexpr int TILES = T::TILES;
     const int lane = threadIdx.x & 31;
     const unsigned all = 0xffffffffu;
-    // the stretches' sums, added up
-    const i64 sums = inclusive_scan(lane < T::WARPS ? ctrl->sums[lane] : 0);
+    // The costs, added up: of the warps' stretches, or of the entries where they are no more than lanes
+    const bool few = a.entries <= 32;
+    Entry one = {};
+    i64 mine = 0;
+    if (few) {
+        if (lane < a.entries) one = entry_of<T::PAGED>(a, lane, blockIdx.x == 0);
+        mine = cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen));
+    } else if (lane < T::WARPS) {
+        mine = ctrl->sums[lane];
+    }
+    const i64 sums = inclusive_scan(mine);
     const i64 total = __shfl_sync(all, sums, 31);
     // Shares: CTA c's begins at total * c / n, or a little before, for all CTAs alike
     const bool many = total >= static_cast<i64>(MIN_SHARE) * gridDim.x;
@@ -376,30 +385,26 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     Split split = {};
     if (cta < n && total > 0) {
         const i64 x0 = begin_of(cta), x1 = begin_of(cta + 1);
-        // the entry that x0 is in: its stretch first
+        // the entry that x0 is in (its stretch first)
         const unsigned behind = __ballot_sync(all, x0 < sums);
         const int w = __ffs(behind) - 1;
         i64 before = w > 0 ? __shfl_sync(all, sums, (w - 1) & 31) : 0;
-        const int stretch = stretch_of<T>(a), e_end = min(stretch * (w + 1), a.entries);
-        int e = stretch * w, block = 0;
-        Entry en = {};
-        // lanes look at 32 entries, then at 32 items of one, at a time
-        auto find = [&](i64 cost) {
-            const i64 upto = inclusive_scan(cost);
-            const unsigned hit = __ballot_sync(all, x0 < before + upto);
-            const int who = hit ? __ffs(hit) - 1 : 32;
-            before += __shfl_sync(all, hit ? upto - cost : upto, hit ? who : 31);
-            return who;
-        };
+        const int stretch = stretch_of<T>(a), e_end = few ? 0 : min(stretch * (w + 1), a.entries);
+        int e = few ? 0 : stretch * w, block = 0, who = few ? w : 32;
 #pragma unroll 1
-        for (int who = 32; who == 32 && e < e_end; e += who) {
-            Entry one = {};
+        for (; who == 32 && e < e_end; e += who) {      // 32 entries at a time
+            one = {};
             if (e + lane < e_end) one = entry_of<T::PAGED>(a, e + lane, false);
-            who = find(cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen)));
-            en.q0 = __shfl_sync(all, one.q0, who & 31), en.k0 = __shfl_sync(all, one.k0, who & 31);
-            en.qlen = __shfl_sync(all, one.qlen, who & 31), en.klen = __shfl_sync(all, one.klen, who & 31);
-            en.g = __shfl_sync(all, one.g, who & 31), en.run = __shfl_sync(all, one.run, who & 31);
+            const i64 cost = cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen)), upto = inclusive_scan(cost);
+            const unsigned hit = __ballot_sync(all, x0 < before + upto);
+            who = hit ? __ffs(hit) - 1 : 32;
+            before += __shfl_sync(all, hit ? upto - cost : upto, hit ? who : 31);
         }
+        if (few) e = w;
+        Entry en;
+        en.q0 = __shfl_sync(all, one.q0, who & 31), en.k0 = __shfl_sync(all, one.k0, who & 31);
+        en.qlen = __shfl_sync(all, one.qlen, who & 31), en.klen = __shfl_sync(all, one.klen, who & 31);
+        en.g = __shfl_sync(all, one.g, who & 31), en.run = __shfl_sync(all, one.run, who & 31);
         int blocks = blocks_of<TILES>(a, en.qlen);
         // its item
 #pragma unroll 1
@@ -1260,8 +1265,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         ptx::tmem_relinquish();
     }
     ptx::grid_dep_wait();
-    {   // the list's length: every warp adds up a stretch of entries
-        // (stretches of whole warps' entries)
+    if (a.entries > 32) {      // the list's length: every warp adds up a stretch of entries (of few, the scheduler does it all)
         const int stretch = stretch_of<T>(a), e0 = min(stretch * warp, a.entries), e1 = min(e0 + stretch, a.entries);
         i64 sum = 0;
 #pragma unroll 1
