@@ -162,10 +162,12 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
  * A token that sees nothing (or nothing that weighs anything) gives zeros, and -inf in out_lse.  Keys and values that a token does
  * not see do not touch its row, infinities and NaN among them (a row that meets such values beside its own is computed again, key by
  * key: slow, and right).  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are
- * rounded to bf16 for the product with the values (8-bit caches: to f16), their sum is not.  D: 64, 96, 128 or 256
+ * rounded to bf16 for the product with the values (8-bit caches: to f16, 11 bits down to 2^-21 of a row's heaviest, in steps of 2^-31
+ * of it below), their sum is not.  8-bit caches: queries are divided by a power of two per head and rounded to f16 (exact down to 2^-14 of the head's largest element).  D: 64, 96, 128 or 256
  * (CAKE_ERR_UNSUPPORTED otherwise).  q, k, v and out are 16-byte aligned and strides multiples of 8 elements, at least D
- * (CAKE_ERR_ALIGN, CAKE_ERR_SHAPE); the stride of a dimension of one element is not looked at.  Two launches.  The result depends
- * on the inputs and their sizes, not on timing.
+ * (CAKE_ERR_ALIGN, CAKE_ERR_SHAPE); the stride of a dimension of one element is not looked at.  One launch where no item
+ * can be shared by blocks (fewer than eight tiles of 128 keys: Tk, or the table's width, or the window), two otherwise.  The result depends on the
+ * inputs and their sizes, not on timing.
  */
 CAKE_API int cake_attention_workspace_bytes(int Hq, int Hkv, int D, size_t* out_bytes);
 /*

@@ -4,7 +4,9 @@
 //
 // Bound by memory: a token's heads are read once and written once.  A thread has one place in a token's row, 8 elements of a head (16 bytes
 // written, so that a warp's store covers whole sectors: 16 elements a thread, in two stores of half sectors, 128 us for 100,001 8-bit tokens), and
-// walks over tokens, several loads in flight.
+// walks over tokens, several loads in flight: eight (100,001 tokens with two 173 us, four 140, sixteen 122).
+//
+// Measured (one B200): 100,001 8-bit tokens of 8 heads of 128 120 us = 5.1 TB/s, 79 % of a copy's rate; one token 3.0 us, a launch's latency.
 #include "serving.cuh"
 
 namespace cake {

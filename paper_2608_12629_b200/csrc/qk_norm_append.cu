@@ -6,6 +6,10 @@
 // registers of D/16 neighbouring lanes, 16 elements each: two runs of 8 that rotate into each other, so that the only exchange
 // between lanes is the sum of squares (2 to 4 shuffles).  A thread keeps its place's cosines, sines and norm weights and walks over heads, four
 // at a time.  Sums, norm and rotation in 32 bits, one rounding at the store.
+//
+// Measured (one B200): 16 tokens of 32 + 2 x 8 heads of 128 3.1 us, a launch's latency; 16,001 tokens 83 us = 5.25 TB/s, 80 % of a copy's rate; 5,000 tokens of
+// 16 + 2 x 4 heads of 256 into an 8-bit cache 33 us.  Blocks of one warp: what a token needs before its heads (slot, position, angles, weights) is a chain
+// of loads, and many short blocks hide it better than few long ones (16,001 tokens: 81 us by one warp, 95 by two, 107 by four).
 #include "serving.cuh"
 
 namespace cake {
