@@ -8,6 +8,7 @@ namespace serving {
 namespace attn {
 namespace {
 
+static_assert(kHeaderBytes % 256 == 0, "parts are written by 32 bytes");
 constexpr size_t kSplitBytes = (MOST_CTAS * sizeof(Split) + 255) / 256 * 256;
 size_t part_floats(int D) { return static_cast<size_t>(D == 256 ? MT : 2 * MT) * (D + 2); }
 bool supported(int D) { return D == 64 || D == 96 || D == 128 || D == 256; }
@@ -68,6 +69,7 @@ int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_
     division(static_cast<uint32_t>(a.Hkv) * a.runs, &a.per_mul, &a.per_shift);
     a.share_mul = ~0ull / ctas_of(*di);
     a.negative = scale < 0.f;
+    a.wide = aligned(a.out, 32);
     a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
     a.status = static_cast<int*>(ws);
     a.splits = reinterpret_cast<Split*>(static_cast<char*>(ws) + kHeaderBytes);

@@ -51,7 +51,7 @@ constexpr int SEGS = 4;                        // segments of work that the sche
 constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags are kept
 constexpr int OVERHEAD = 576;                  // keys that an item's start and end cost (four tiles of them, and half of one that is not full)
 constexpr int SNAP = 4;                        // a share's end within fewer tiles of an item's is moved there
-constexpr int MIN_SHARE = OVERHEAD / 2;        // of a CTA, in keys
+constexpr int MIN_SHARE = OVERHEAD / 4;        // of a CTA, in keys
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
@@ -89,6 +89,7 @@ struct Args {
     int max_pages, window;
     float scale_log2;                          // |scale| log2 e
     bool negative, causal;                     // sign of the scale
+    bool wide;                                 // out is a multiple of 32 bytes
     bool cuts;                                 // an item may be shared by CTAs
     bool maps;                                 // paged: mk and mv are maps of the pages, boxes of `box` tokens
     int box;
@@ -217,6 +218,11 @@ __device__ __forceinline__ void check2(float2& s, float a, float b) {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {      // zeros where !ok
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void store32(void* to, const uint32_t (&o)[32], int k) {      // o[k .. k + 7], to a multiple of 32 bytes
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(o[k]), "r"(o[k + 1]), "r"(o[k + 2]), "r"(o[k + 3]), "r"(o[k + 4]), "r"(o[k + 5]), "r"(o[k + 6]), "r"(o[k + 7])
+                 : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -267,11 +273,17 @@ __device__ __forceinline__ void tiles_of(const Args& a, int pos, int n, int klen
 template <int TILES>
 __device__ __forceinline__ int blocks_of(const Args& a, int qlen) { return (qlen + TILES * a.tokens - 1) / (TILES * a.tokens); }
 // Cost of the first n items of an entry, in keys: OVERHEAD + end - first key for each, where both grow by a block's tokens from item
-// to item (but for the last item's end, which is the sequence's): sums of arithmetic series, no loop
-template <int TILES>
+// to item (but for the last item's end, which is the sequence's): sums of arithmetic series, no loop.  An item of one row tile, the last one it can be,
+// takes its keys two tiles at a time and costs half as much (1,630 clocks a tile of keys where two row tiles take 3,190; counted in full, a step of single
+// tokens and pieces of prompts took 263 us for 257); with 8-bit caches, whose tiles take as long to widen for one as for two, it does not
+template <class T>
+__device__ __forceinline__ bool is_cheap(const Args& a, int ntok) { return T::TILES == 2 && !T::F16 && ntok <= a.tokens; }
+template <class T>
 __device__ __noinline__ i64 cost_before(const Args& a, int qlen, int klen, int n) {
-    const int per = TILES * a.tokens, off = klen - qlen;
-    if (!a.causal) return static_cast<i64>(n) * (OVERHEAD + klen);
+    const int per = T::TILES * a.tokens, off = klen - qlen;
+    i64 less = 0;                                           // half of the last item's, if it is one row tile
+    if (n > 0 && is_cheap<T>(a, qlen - (n - 1) * per)) less = (OVERHEAD + static_cast<i64>(klen) - first_key(a, off + (n - 1) * per, klen) + 1) >> 1;
+    if (!a.causal) return static_cast<i64>(n) * (OVERHEAD + klen) - less;
     const int full = min(n, qlen / per);                    // items of a whole block of tokens
     i64 sum = static_cast<i64>(n) * OVERHEAD + (n > full ? klen : 0);
     const int i0 = off < 0 ? min(full, -off / per) : 0;     // those before see nothing
@@ -283,7 +295,7 @@ __device__ __noinline__ i64 cost_before(const Args& a, int qlen, int klen, int n
         const i64 k = n - i1;
         sum -= k * gone + per * (k * (i1 + n - 1) / 2);
     }
-    return sum;
+    return sum - less;
 }
 __device__ __forceinline__ i64 inclusive_scan(i64 v) {
     const int lane = threadIdx.x & 31;
@@ -294,8 +306,9 @@ __device__ __forceinline__ i64 inclusive_scan(i64 v) {
     }
     return v;
 }
-// a share's end p keys into an item of n tiles, in tiles, moved to the item's ends where they are near
-__device__ __forceinline__ int snap(i64 p, int n) {
+// a share's end p keys (of cost) into an item of n tiles, in tiles, moved to the item's ends where they are near
+__device__ __forceinline__ int snap(i64 p, int n, int cheap) {
+    p <<= cheap;
     const int t = p <= OVERHEAD ? 0 : static_cast<int>(min(p - OVERHEAD, static_cast<i64>(INT_MAX))) / KT;
     return t < SNAP ? 0 : n - t < SNAP ? n : t;
 }
@@ -369,7 +382,7 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
     i64 mine = 0;
     if (few) {
         if (lane < a.entries) one = entry_of<T::PAGED>(a, lane, blockIdx.x == 0);
-        mine = cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen));
+        mine = cost_before<T>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen));
     } else if (lane < T::WARPS) {
         mine = ctrl->sums[lane];
     }
@@ -407,7 +420,7 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
         for (; who == 32 && e < e_end; e += who) {      // 32 entries at a time
             one = {};
             if (e + lane < e_end) one = entry_of<T::PAGED>(a, e + lane, false);
-            const i64 cost = cost_before<TILES>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen)), upto = inclusive_scan(cost);
+            const i64 cost = cost_before<T>(a, one.qlen, one.klen, blocks_of<TILES>(a, one.qlen)), upto = inclusive_scan(cost);
             const unsigned hit = __ballot_sync(all, x0 < before + upto);
             who = hit ? __ffs(hit) - 1 : 32;
             before += __shfl_sync(all, hit ? upto - cost : upto, hit ? who : 31);
@@ -421,8 +434,8 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
         // its item
 #pragma unroll 1
         for (int step = blocks > 1 ? 1 << (31 - __clz(blocks - 1)) : 0; step; step >>= 1)
-            if (block + step < blocks && before + cost_before<TILES>(a, en.qlen, en.klen, block + step) <= x0) block += step;
-        if (block) before += cost_before<TILES>(a, en.qlen, en.klen, block);
+            if (block + step < blocks && before + cost_before<T>(a, en.qlen, en.klen, block + step) <= x0) block += step;
+        if (block) before += cost_before<T>(a, en.qlen, en.klen, block);
         int start = -1;
 #pragma unroll 1
         while (x1 > before && block < blocks) {
@@ -431,10 +444,11 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
             int ja, jb;
             tiles_of(a, pos, ntok, en.klen, ja, jb);
             const int tiles = jb - ja;
-            const i64 end_at = before + OVERHEAD + end_key(a, pos + ntok - 1, en.klen) - (a.window > 0 ? first_key(a, pos, en.klen) : 0);
-            if (start < 0) start = x0 > before ? snap(x0 - before, tiles) : 0;      // the share's first item
+            const int cheap = is_cheap<T>(a, ntok);
+            const i64 end_at = before + ((OVERHEAD + static_cast<i64>(end_key(a, pos + ntok - 1, en.klen)) - (a.window > 0 ? first_key(a, pos, en.klen) : 0)) >> cheap);
+            if (start < 0) start = x0 > before ? snap(x0 - before, tiles, cheap) : 0;      // the share's first item
             const bool to_end = x1 >= end_at;
-            const int end = to_end ? tiles : snap(x1 - before, tiles);
+            const int end = to_end ? tiles : snap(x1 - before, tiles, cheap);
             if (to_end ? start < tiles || start == 0 : start < end) {
                 Seg s;
                 s.tok = en.q0 + tok, s.k0 = en.k0, s.g = en.g;
@@ -454,7 +468,7 @@ __device__ __forceinline__ void schedule(const Args& a, Ctrl* ctrl, const Room& 
 #pragma unroll 1
                     for (int c = cta + 1; c < n; c += 32) {
                         const i64 x = begin_of(c + lane);
-                        const unsigned in = __ballot_sync(all, c + lane < n && x < end_at && snap(x - before, tiles) < tiles);
+                        const unsigned in = __ballot_sync(all, c + lane < n && x < end_at && snap(x - before, tiles, cheap) < tiles);
                         c1 += __popc(in);
                         if (in != all) break;
                     }
@@ -855,18 +869,22 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 check2(odd[(k >> 1) & 3], __uint_as_float(o[k]), __uint_as_float(o[k + 1]));
                 if (empty) o[k] = o[k + 1] = 0u;
             }
-            // (by way of shared memory, in whole sectors: no faster)
+            // (whole sectors: by halves, what is stored held up all that comes behind it in shared memory too; 8 packed prompts 143 us for 138)
             if (!valid) return;
             if (part_at >= 0) {
-                uint4* const to = reinterpret_cast<uint4*>(part + static_cast<i64>(part_row) * D + d);
+                float* const to = part + static_cast<i64>(part_row) * D + d;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) to[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                for (int k = 0; k < 4; ++k) store32(to + 8 * k, o, 8 * k);
             } else {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) o[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
-                uint4* const to = reinterpret_cast<uint4*>(a.out + row * D + d);
+                cake_bf16* const to = a.out + row * D + d;
+                if (a.wide) {
+                    store32(to, o, 0), store32(to + 16, o, 8);
+                } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) to[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(to)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                }
             }
         };
 #pragma unroll 1
@@ -1284,7 +1302,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (int e = e0; e < e1; e += 32) {
             Entry en = {};
             if (e + lane < e1) en = entry_of<T::PAGED>(a, e + lane, blockIdx.x == 0);
-            sum += cost_before<T::TILES>(a, en.qlen, en.klen, blocks_of<T::TILES>(a, en.qlen));
+            sum += cost_before<T>(a, en.qlen, en.klen, blocks_of<T::TILES>(a, en.qlen));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);

@@ -192,3 +192,33 @@ def test_host_threads_at_once():
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert not errors and all(torch.equal(x, want) for x in got)
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_outputs_at_every_allowed_alignment(D):
+    """out is 16-byte aligned: a buffer 16 bytes behind a multiple of 32 gets the same bits, and nothing beside it is touched."""
+    lens = [130, 2500, 7]
+    q, k, v = base.packed(5, lens, lens, 4, 2, D)
+    want, _ = base.run_packed(q, k, v, lens, lens)
+    room = torch.full((q.numel() + 32,), 7.0, dtype=BF16, device=DEV)
+    out = room[8:8 + q.numel()].view(sum(lens), 4, D)
+    assert out.data_ptr() % 32 == 16
+    cake.cake_prompt_attention(q, k, v, base.starts_of(lens), out=out)
+    assert torch.equal(out, want)
+    assert (room[:8] == 7).all() and (room[8 + q.numel():] == 7).all()
+
+
+def test_sequences_of_one_row_tile_beside_larger_ones():
+    """Items of one row tile count half when work is shared out: long rows of single tokens beside pieces of prompts, and prompts whose last
+    block is one tile, in windows and without."""
+    new, lens = [1, 900, 1, 65, 1, 32, 1], [3900, 2100, 5000, 65, 1, 4000, 129]
+    for window in (0, 777):
+        for kv in ("bf16", "e4m3"):
+            q, cache, table, n = base.paged(7, new, lens, 8, 2, 128, 16, kv)
+            out, lse = base.run_chunk(q, cache, table, n, new, window=window)
+            base.check_chunk(out, lse, q, cache, table, new, lens, window=window)
+        q, k, v = base.packed(8, new, lens, 8, 2, 64)
+        out, lse = base.run_packed(q, k, v, new, lens, window=window)
+        base.check_packed(out, lse, q, k, v, new, lens, window=window)
+    out, lse = base.run_packed(q, k, v, new, lens, causal=False)
+    base.check_packed(out, lse, q, k, v, new, lens, causal=False)
