@@ -201,6 +201,24 @@ def test_read(kv, D, Hkv, N, page):
     assert cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
 
 
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("N", [1, 50, 3000])
+def test_read_to_every_allowed_alignment(kv, N):
+    """Outputs are 16-byte aligned: 16 bytes behind a multiple of 32 they hold the same, and nothing beside them is touched."""
+    cache = cache_of(5, 40, 100, 3, 96, kv, filled=True)
+    slots = torch.randint(-1, 4000, (N,), device=DEV, generator=gen(N))
+    want = cake.cake_kv_read(cache, slots)
+    n = N * 3 * 96
+    for by_head in (False, True):
+        rooms = [torch.full((n + 32,), 7.0, dtype=BF16, device=DEV) for _ in range(2)]
+        outs = [r[8:8 + n].view((3, N, 96) if by_head else (N, 3, 96)) for r in rooms]
+        assert all(o.data_ptr() % 32 == 16 for o in outs)
+        cake.cake_kv_read(cache, slots, out_k=outs[0], out_v=outs[1], by_head=by_head)
+        for o, w, r in zip(outs, want, rooms):
+            assert torch.equal(o.transpose(0, 1) if by_head else o, w)
+            assert (r[:8] == 7).all() and (r[8 + n:] == 7).all()
+
+
 def test_read_of_values_that_are_not_finite_slots_out_of_range_and_refusals():
     cache = cache_of(1, 4, 16, 2, 64, "e4m3", filled=True)
     cache.k.view(torch.uint8)[1, 3] = 0x7f
