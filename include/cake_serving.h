@@ -157,7 +157,8 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
  *   q          [T][Hq][D] bf16, tokens q_stride apart, heads q_head_stride apart, in
  *   starts     [B + 1] int32, device, in: 0 <= starts[b] <= starts[b + 1] <= T; a sequence for which that does not hold is left out
  *              (device status CAKE_ERR_BAD_INDEX).  Tokens of no sequence are left as they were in out and out_lse
- *   out        [T][Hq][D] bf16 contiguous, out;   out_lse [T][Hq] fp32 contiguous, out, may be NULL: log of the sum of exponentials
+ *   out        [T][Hq][D] bf16 contiguous, out;   out_lse [T][Hq] fp32 contiguous, out, may be NULL: log of the sum of exponentials;
+ *              neither overlaps an input
  *   ws         at least cake_attention_workspace_bytes(Hq, Hkv, D) bytes: any number of sequences and tokens
  * A token that sees nothing (or nothing that weighs anything) gives zeros, and -inf in out_lse.  Keys and values that a token does
  * not see do not touch its row, infinities and NaN among them (a row that meets such values beside its own is computed again, key by

@@ -666,6 +666,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 c *= ctrl->q_scale[qt][r];
                 ++q_count[qt];
             }
+            c = fmaxf(c, 1.17549435e-38f);         // (scales of zero: a mask's infinity times it stays infinite)
             if (t == 1) {      // looks at every load of the first tile
                 bool other = !dual && used;
                 if (dual) {

@@ -222,3 +222,15 @@ def test_sequences_of_one_row_tile_beside_larger_ones():
         base.check_packed(out, lse, q, k, v, new, lens, window=window)
     out, lse = base.run_packed(q, k, v, new, lens, causal=False)
     base.check_packed(out, lse, q, k, v, new, lens, causal=False)
+
+
+def test_scales_of_zero_weigh_all_visible_keys_alike():
+    """A head whose keys' scale is zero has scores of zero: the mean of the values that a token sees, log of their number, masked keys left out."""
+    new, lens = [3, 140], [50, 300]
+    q, cache, table, n = base.paged(11, new, lens, 4, 2, 128, 16, "e4m3")
+    cache.k_scale[0] = 0.0
+    out, lse = base.run_chunk(q, cache, table, n, new, window=100)
+    base.check_chunk(out, lse, q, cache, table, new, lens, window=100)
+    q[5:40] *= 2.0 ** -125      # and queries next to nothing
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    base.check_chunk(out, lse, q, cache, table, new, lens)
