@@ -640,6 +640,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         const int ra = first, step = alt ? 2 : 1;
         if (alt) first += t;
         const int n_mine = first < rb ? (rb - first + step - 1) / step : 0;
+        const uint32_t flag0 = tiles + first - sp->ja;                      // its first tile among all that were loaded
         const int my_tok = (dual ? t * a.tokens : 0) + tok;                 // of the segment's tokens
         int k0, k1, inner0, inner1;                                         // the row sees [k0, k1), every row of the tile [inner0, inner1)
         {
@@ -708,7 +709,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             bool masked = key0 < inner0 || key0 + KT > inner1;
             uint4 pages = make_uint4(~0u, ~0u, ~0u, ~0u);
             if (T::PAGED) {
-                pages = ctrl->flags[(tiles + first + i * step - ra) % FLAGS_AHEAD];
+                pages = ctrl->flags[(flag0 + i * step) % FLAGS_AHEAD];
                 masked |= (pages.x & pages.y & pages.z & pages.w) != ~0u;
             }
             // Which rows look for their maximum: it is theirs alone to say, so that a row's bits do not depend on its neighbours

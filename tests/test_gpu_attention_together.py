@@ -234,3 +234,21 @@ def test_scales_of_zero_weigh_all_visible_keys_alike():
     q[5:40] *= 2.0 ** -125      # and queries next to nothing
     out, lse = base.run_chunk(q, cache, table, n, new)
     base.check_chunk(out, lse, q, cache, table, new, lens)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("window", [0, 150, 300])
+def test_pages_out_of_range_inside_windows_and_pieces(kv, window):
+    """The second row tile of an item may begin behind the first one's first tile of keys: it sees its own tiles' missing pages."""
+    page, new, lens = 16, [900, 70], [2000, 1500]
+    q, cache, table, n = base.paged(13, new, lens, 4, 1, 128, page, kv)
+    keep = torch.ones(2, 2000, dtype=torch.bool, device=DEV)
+    for b, entry in ((0, 69), (0, 75), (0, 90), (0, 117), (1, 81), (1, 92)):
+        table[b, entry] = -1
+        keep[b, entry * page:(entry + 1) * page] = False
+    ws = cake.alloc_attention_workspace(4, 1, 128, DEV)
+    out, lse = cake.cake_paged_chunk(q, cache, table, n, base.starts_of(new), want_lse=True, ws=ws, window=window)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_ERR_BAD_INDEX
+    table.clamp_(min=0)
+    base.check(out, lse, q, lambda b, g: tuple(torch.nan_to_num(x) for x in base.cached(cache, table, lens, b, g)), new, lens, 1, 128 ** -0.5, True, window,
+               f16=kv == "e4m3", keep=lambda b, g: keep[b, :lens[b]])
