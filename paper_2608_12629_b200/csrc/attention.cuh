@@ -350,20 +350,21 @@ __device__ __forceinline__ void load_queries_keys(const Args& a, Ctrl* ctrl, con
         for (int x = 0; x < T::SLABS; ++x)
             ptx::tma_load_3d(ptx::smem_u32(room.q) + t * T::Q_TILE + x * T::SLAB, mq, bar, 64 * x, s.head0, static_cast<int>(s.tok) + t * a.tokens);
     }
-    if (T::PAGED) return;
+    if constexpr (!T::PAGED) {
 #pragma unroll 1
-    for (int j = s.ja; j < s.jb; ++j)
+        for (int j = s.ja; j < s.jb; ++j)
 #pragma unroll 1
-        for (int u = 0; u < T::NKU; ++u, ++nk) {
-            const uint32_t st = nk % T::K_STAGES;
-            wait_bar(&ctrl->k_empty[st], nk / T::K_STAGES + 1, ctrl, a.status);
-            if (aborted(ctrl)) return;
-            const uint32_t bar = ptx::smem_u32(&ctrl->k_full[st]);
-            ptx::mbar_arrive_expect_tx(bar, T::K_UNIT);
+            for (int u = 0; u < T::NKU; ++u, ++nk) {
+                const uint32_t st = nk % T::K_STAGES;
+                wait_bar(&ctrl->k_empty[st], nk / T::K_STAGES + 1, ctrl, a.status);
+                if (aborted(ctrl)) return;
+                const uint32_t bar = ptx::smem_u32(&ctrl->k_full[st]);
+                ptx::mbar_arrive_expect_tx(bar, T::K_UNIT);
 #pragma unroll
-            for (int x = 0; x < T::K_SLABS; ++x)
-                ptx::tma_load_3d(ptx::smem_u32(room.k) + st * T::K_UNIT + x * T::SLAB, mk, bar, T::KC * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
-        }
+                for (int x = 0; x < T::K_SLABS; ++x)
+                    ptx::tma_load_3d(ptx::smem_u32(room.k) + st * T::K_UNIT + x * T::SLAB, mk, bar, T::KC * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+            }
+    }
 }
 // copies in flight land before the CTA gives up its shared memory (they have, unless a wait has expired)
 __device__ __forceinline__ void landed(uint64_t* bars, uint32_t n, uint32_t stages) {
