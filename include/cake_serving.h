@@ -160,6 +160,7 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
  *   out        [T][Hq][D] bf16 contiguous, out;   out_lse [T][Hq] fp32 contiguous, out, may be NULL: log of the sum of exponentials;
  *              neither overlaps an input
  *   ws         at least cake_attention_workspace_bytes(Hq, Hkv, D) bytes: any number of sequences and tokens
+ *   scale      any number; zero weighs all keys alike.  NaN (here, or in an 8-bit cache's k_scale) makes every row NaN that sees something
  * A token that sees nothing (or nothing that weighs anything) gives zeros, and -inf in out_lse.  Keys and values that a token does
  * not see do not touch its row, infinities and NaN among them (a row that meets such values beside its own is computed again, key by
  * key: slow, and right).  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are

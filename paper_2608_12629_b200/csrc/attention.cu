@@ -70,7 +70,7 @@ int prepare(Args& a, Maps& maps, i64 B, int D, float scale, void* ws, size_t ws_
     a.share_mul = ~0ull / ctas_of(*di);
     a.negative = scale < 0.f;
     a.wide = aligned(a.out, 32);
-    a.scale_log2 = fmaxf(fabsf(scale) * LOG2E, 7.888609052210118e-31f);      // (2^-100: a mask's infinity times it stays infinite)
+    a.scale_log2 = static_cast<float>(fabs(static_cast<double>(scale)) * 1.4426950408889634);
     a.status = static_cast<int*>(ws);
     a.splits = reinterpret_cast<Split*>(static_cast<char*>(ws) + kHeaderBytes);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeaderBytes + kSplitBytes);

@@ -53,7 +53,6 @@ constexpr int OVERHEAD = 576;                  // keys that an item's start and 
 constexpr int SNAP = 4;                        // a share's end within fewer tiles of an item's is moved there
 constexpr int MIN_SHARE = OVERHEAD / 4;        // of a CTA, in keys
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
 
@@ -189,6 +188,13 @@ __device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flus
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// What a row's scores are multiplied by: |scale| log2 e times its head's scale and what its queries were divided by (in 64 bits: the parts may leave 32 where
+// the product does not).  Never zero (of which a mask's infinity would make a NaN): 2^-149 leaves scores of zero in all that 2^x sees.  Not a number: the
+// row's end says so, and the mask stays a mask.
+__device__ __forceinline__ float factor_of(float scale_log2, float head, float queries) {
+    const float c = static_cast<float>(static_cast<double>(scale_log2) * fabsf(head) * queries);
+    return c > 0.f ? c : 1.4012985e-45f;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t d;
@@ -651,9 +657,8 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             inner0 = first_key(a, pos + min(sp->ntok, (dual ? (t + 1) * a.tokens : sp->ntok)) - 1, klen);
             inner1 = end_key(a, pos + (dual ? t * a.tokens : 0), klen);
         }
-        float c = a.scale_log2;
+        float c = factor_of(a.scale_log2, 1.f, 1.f);
         if (T::F16) {
-            if (a.c.k_scale) c *= fabsf(a.c.k_scale[sp->g]);
             const int qt = dual ? t : 0;
             const bool used = dual ? n_mine > 0 : sp->jb > sp->ja;
             if (used && (dual || t == 0)) {
@@ -665,10 +670,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             }
             if (used) {
                 wait_bar(&ctrl->q_conv[qt], q_count[qt], ctrl, a.status);
-                c *= ctrl->q_scale[qt][r];
+                c = factor_of(a.scale_log2, a.c.k_scale ? a.c.k_scale[sp->g] : 1.f, ctrl->q_scale[qt][r]);
                 ++q_count[qt];
             }
-            c = fmaxf(c, 1.17549435e-38f);         // (scales of zero: a mask's infinity times it stays infinite)
             if (t == 1) {      // looks at every load of the first tile
                 bool other = !dual && used;
                 if (dual) {
@@ -838,6 +842,8 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         const i64 row = (sp->tok + my_tok) * a.Hq + sp->head0 + h;
         const float sub = top == NEG_INF ? NEG_INF : top - LIFT;      // what was subtracted
         const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[g] : 1.f;
+        // (a scale that is no number: so are the rows that see anything)
+        if (isnan(a.scale_log2) || (T::F16 && a.c.k_scale && isnan(a.c.k_scale[g]))) l = l == 0.f ? 0.f : NAN;
         const bool empty = l == 0.f;               // sees nothing that weighs anything: zeros, whatever the values are
         const float inv = part_at >= 0 ? 1.f : vs / l;
         f0 *= inv, f1 *= inv;
