@@ -53,6 +53,7 @@ constexpr int OVERHEAD = 576;                  // keys that an item's start and 
 constexpr int SNAP = 4;                        // a share's end within fewer tiles of an item's is moved there
 constexpr int MIN_SHARE = OVERHEAD / 4;        // of a CTA, in keys
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
+constexpr float LEAST = 1.4012985e-45f;        // 2^-149
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
 
@@ -194,7 +195,7 @@ __device__ __forceinline__ float ex2(float x) {      // 2 ulp; below 2^-126 flus
 // row's end says so, and the mask stays a mask.
 __device__ __forceinline__ float factor_of(float scale_log2, float head, float queries) {
     const float c = static_cast<float>(static_cast<double>(scale_log2) * fabsf(head) * queries);
-    return c > 0.f ? c : 1.4012985e-45f;
+    return c > 0.f ? c : LEAST;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t d;
@@ -632,6 +633,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
     // rescaled: weights above 1 do no harm in 32 bits, nor rounded to bf16.  Weights in f16 (8-bit values, which widen to f16 exactly) lie LIFT higher, so
     // that 11 bits are held down to 2^-21 of the heaviest and steps of 2^-31 below; each is at most LIMIT, which f16 holds
     constexpr float LIFT = T::F16 ? 7.f : 0.f, LIMIT = T::F16 ? 65000.f : 1048576.f;
+    // x c - m in one rounding lies beside what m = x c was rounded by: half a step of m, which passes 2^x's range where m passes 2^30.  Scores that reach FAR, whose
+    // neighbours in 32 bits are two powers of two apart, are multiplied by the power of two that is not below c instead, which rounds nothing; what is
+    // beyond FAR stays beyond it, in the same order
+    constexpr float FAR = 16777216.f;
     const int lane = threadIdx.x & 31, r = threadIdx.x & 127;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(r & 96) << 16);
     const int tok = r / a.heads;
@@ -657,7 +662,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             inner0 = first_key(a, pos + min(sp->ntok, (dual ? (t + 1) * a.tokens : sp->ntok)) - 1, klen);
             inner1 = end_key(a, pos + (dual ? t * a.tokens : 0), klen);
         }
-        float c = factor_of(a.scale_log2, 1.f, 1.f);
+        float c = a.scale_log2 > 0.f ? a.scale_log2 : LEAST;
         if (T::F16) {
             const int qt = dual ? t : 0;
             const bool used = dual ? n_mine > 0 : sp->jb > sp->ja;
@@ -690,6 +695,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
         // queries' box), they do not hold up the others
         const bool live = tok < a.tokens && my_tok < sp->ntok && k0 < k1;
         float m = live ? NEG_INF : 0.f, l = 0.f;   // m: the maximum that is subtracted, without LIFT
+        const float c_near = c, c_far = __uint_as_float(min((__float_as_uint(c) + 0x7fffffu) & 0xff800000u, 0x7f000000u));      // c: the one of m
         for (int i = 0; i < n_mine; ++i) {
             const int key0 = KT * (first + i * step);
             const int pb = T::TILES == 2 ? t : i & 1;      // place of the weights
@@ -744,10 +750,12 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                         for (int k = 1; k < 31; k += 2) top[w] = ptx::fmax3(top[w], __uint_as_float(x[w][k]), __uint_as_float(x[w][k + 1]));
                         top[w] = fmaxf(top[w], __uint_as_float(x[w][31]));
                     }
-                    const float up = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                    top[0] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    const float near = top[0] * c_near, up = fabsf(near) < FAR ? near : top[0] * c_far;
                     const bool higher = search && up > m;
                     const float f = higher ? ex2(m - up) : 1.f;
                     if (higher) m = up;
+                    c = fabsf(m) < FAR ? c_near : c_far;
                     l *= f;
                     if (i > 0) {
                         const int ob = T::TILES == 2 ? t : 0, last = T::TILES == 2 ? t : pb ^ 1;      // the product before has to be complete
@@ -831,6 +839,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             o_count[1] += n_other;
             wait_bar(&ctrl->o_done[1], o_count[1] - 1, ctrl, a.status);
         }
+        if (fabsf(top) >= FAR && top != NEG_INF) top = top / c_far * c_near;
         const int ob = T::TILES == 2 ? t : 0;
         if (n_mine) {
             const int last = T::TILES == 2 ? t : (n_mine - 1) & 1;

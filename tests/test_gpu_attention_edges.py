@@ -1,4 +1,4 @@
-"""Attention of many tokens at the edges of its range, against a plain implementation in 64 bits: scales that are no numbers or next to nothing.
+"""Attention of many tokens at the edges of its range, against a plain implementation in 64 bits: scales that are no numbers or next to nothing, scores beyond all bounds.
 
 Tolerances: those of test_gpu_attention.py, whose reference and bounds this file uses."""
 import math
@@ -73,3 +73,69 @@ def test_scales_of_an_8_bit_cache_whose_product_leaves_32_bits_on_the_way():
     assert torch.isfinite(q).all()
     out, lse = base.run_chunk(q, cache, table, n, new, scale=2.0 ** -69)
     base.check_chunk(out, lse, q, cache, table, new, lens, scale=2.0 ** -69)
+
+
+# -------------------------------------------------------------------------------------------------------- large scores
+def check_largest(out, lse, q, keys_values, new, lens, Hkv, scale, top):
+    """Scores so far apart that all but a row's largest weigh nothing.  Where the largest leads the next by more than their roundings, (D + 3) 2^-23 of sum |q k|, and
+    another 200 for the weights, the row is its value (its weight and the output rounded), and lse its score; where not, it lies between the values and the lse within
+    that much of it."""
+    T, Hq, D = q.shape
+    G, at, clear = Hq // Hkv, 0, 0
+    for b, n in enumerate(new):
+        for g in range(Hkv):
+            k, v = (t.double() for t in keys_values(b, g))
+            rows = q[at:at + n, g * G:(g + 1) * G].double()
+            hide = ~base.visible(n, lens[b], True, 0)[:, None, :].expand(n, G, lens[b])
+            x = (torch.einsum("igd,td->igt", rows, k) * scale).masked_fill(hide, -math.inf)
+            err = (D + 3) * base.U * (torch.einsum("igd,td->igt", rows.abs(), k.abs()) * abs(scale)).masked_fill(hide, 0).amax(2)
+            assert float(x.amax()) > top
+            best, where = x.max(2)
+            next_best = x.scatter(2, where[..., None], -math.inf).amax(2)
+            lead = best - next_best > 2 * err + 200
+            got, got_lse = out[at:at + n, g * G:(g + 1) * G].double(), lse[at:at + n, g * G:(g + 1) * G].double()
+            assert ((got - v[where]).abs() <= 2.01 * 2.0 ** -8 * v[where].abs())[lead].all()
+            assert (got.abs() <= 1.01 * v.abs().max()).all()
+            assert ((got_lse - best).abs() <= err + 2 * base.U * best.abs() + 10).all()
+            clear += int(lead.sum())
+        at += n
+    assert clear > T * Hq // 2
+
+
+@pytest.mark.parametrize("power", [11, 13, 30, 58])
+@pytest.mark.parametrize("D,lens", [(64, [260, 5]), (96, [130]), (128, [2500]), (256, [1300, 40])])
+def test_scores_far_beyond_what_their_differences_leave_in_32_bits(D, lens, power):
+    """Scores of 2^23 to 2^118: their maximum's rounding alone would pass the range of an exponential."""
+    q, k, v = base.packed(D, lens, lens, 4, 2, D)
+    q, k = q * 2.0 ** power, k * 2.0 ** power
+    out, lse = base.run_packed(q, k, v, lens, lens)
+    at = [0, lens[0], sum(lens)]
+    check_largest(out, lse, q, lambda b, g: (k[at[b]:at[b + 1], g], v[at[b]:at[b + 1], g]), lens, lens, 2, D ** -0.5, 2.0 ** (2 * power))
+    # most of a row's keys and then the others as they are: its scores come into the range again, the other way round they leave it
+    for part in (slice(0, sum(lens) // 2), slice(sum(lens) // 2, None)):
+        k2 = k.clone()
+        k2[part] = k2[part] * 2.0 ** -power
+        out, lse = base.run_packed(q, k2, v, lens, lens)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all() and (out.abs() <= 1.01 * v.abs().max()).all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("D,new,lens", [(128, [200, 3], [300, 4000]), (256, [9], [1500])])
+def test_scores_beyond_over_pages(kv, D, new, lens):
+    q, cache, table, n = base.paged(5, new, lens, 4, 2, D, 16, kv)
+    q *= 2.0 ** 60
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    check_largest(out, lse, q, lambda b, g: base.cached(cache, table, lens, b, g), new, lens, 2, D ** -0.5, 2.0 ** 60)
+
+
+def test_ordinary_rows_beside_rows_of_large_scores():
+    """A row's bits do not depend on its neighbours, whose scores take another way."""
+    lens = [300, 2000]
+    q, k, v = base.packed(6, lens, lens, 4, 2, 128)
+    want, want_lse = base.run_packed(q, k, v, lens, lens)
+    q2 = q.clone()
+    q2[::3] *= 2.0 ** 80
+    q2[1::6, 1] *= -2.0 ** 40
+    out, lse = base.run_packed(q2, k, v, lens, lens)
+    same = (q2 == q).all(2)
+    assert torch.equal(out[same], want[same]) and torch.equal(lse[same], want_lse[same]) and torch.isfinite(out).all() and torch.isfinite(lse).all()
