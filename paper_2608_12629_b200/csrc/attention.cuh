@@ -267,6 +267,7 @@ __device__ __forceinline__ Entry entry_of(const Args& a, int e, bool report) {
         const bool wrong = k0 < 0 || k1 < k0 || k1 > a.Tk;
         bad |= wrong;
         n.k0 = wrong ? 0 : k0, n.klen = wrong ? 0 : k1 - k0;
+        if (wrong) n.qlen = 0;
     }
     if (bad && report) raise_bad_index(a.status);
     return n;

@@ -139,3 +139,43 @@ def test_ordinary_rows_beside_rows_of_large_scores():
     out, lse = base.run_packed(q2, k, v, lens, lens)
     same = (q2 == q).all(2)
     assert torch.equal(out[same], want[same]) and torch.equal(lse[same], want_lse[same]) and torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+# ------------------------------------------------------------------------------------------------------------- ranges
+@pytest.mark.parametrize("k_starts", [[0, 50, 40, 90], [0, 50, -1, 90], [0, 50, 100, 90], None])
+def test_sequences_whose_keys_are_out_of_range_are_left_out(k_starts):
+    """Their tokens stay as they were; the others' are theirs.  k_starts None: 90 keys for 120 tokens, which the last sequence's pass."""
+    g = base.gen(3)
+    new, D = [40, 30, 50], 64
+    q, k, v = base.normal(g, 120, 4, D, std=1.2), base.normal(g, 90, 2, D, std=1.2), base.normal(g, 90, 2, D)
+    ks = None if k_starts is None else torch.tensor(k_starts, dtype=torch.int32, device=DEV)
+    out, lse = torch.full_like(q, 7.0), torch.full((120, 4), 5.0, device=DEV)
+    ws = cake.alloc_attention_workspace(4, 2, D, DEV)
+    cake.cake_prompt_attention(q, k, v, base.starts_of(new), ks, out=out, out_lse=lse, ws=ws)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_ERR_BAD_INDEX
+    at = k_starts or [0, 40, 70, 120]
+    a = 0
+    for b, n in enumerate(new):
+        k0, k1 = at[b], at[b + 1]
+        if 0 <= k0 <= k1 <= 90:
+            base.check_packed(out[a:a + n], lse[a:a + n], q[a:a + n], k[k0:k1], v[k0:k1], [n], [k1 - k0])
+        else:
+            assert (out[a:a + n] == 7).all() and (lse[a:a + n] == 5).all()
+        a += n
+
+
+def test_lengths_beyond_the_table_and_sequences_beside_those_that_are_left_out():
+    """A length beyond the table is cut to it: 48 tokens; sequences beside one whose starts are out of range are theirs."""
+    q, cache, table, n = base.paged(2, [5, 5], [48, 40], 4, 2, 64, 16, "bf16")
+    ws = cake.alloc_attention_workspace(4, 2, 64, DEV)
+    n[0] = 1000
+    out, lse = cake.cake_paged_chunk(q, cache, table, n, base.starts_of([5, 5]), want_lse=True, ws=ws)
+    assert cake.cake_kmeans_device_status(ws) == cake.CAKE_ERR_BAD_INDEX
+    base.check_chunk(out, lse, q, cache, table, [5, 5], [48, 40])
+    for starts, kept in (([-1, 5, 10], 1), ([6, 5, 10], 1), ([0, 5, 4], 0), ([0, 5, 11], 0)):
+        out, lse = torch.full_like(q, 3.0), torch.full((10, 4), 2.0, device=DEV)
+        n[0] = 48
+        cake.cake_paged_chunk(q, cache, table, n, torch.tensor(starts, dtype=torch.int32, device=DEV), out=out, out_lse=lse, ws=ws)
+        mine, other = slice(5 * kept, 5 * kept + 5), slice(5 - 5 * kept, 10 - 5 * kept)
+        assert (out[other] == 3).all() and (lse[other] == 2).all()
+        base.check_chunk(out[mine], lse[mine], q[mine], cache, table[kept:kept + 1], [5], [[48, 40][kept]])
