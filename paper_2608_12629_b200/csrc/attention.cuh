@@ -52,7 +52,7 @@ constexpr int FLAGS_AHEAD = 16;                // tiles of keys whose page flags
 constexpr int OVERHEAD = 576;                  // keys that an item's start and end cost (four tiles of them, and half of one that is not full)
 constexpr int SNAP = 4;                        // a share's end within fewer tiles of an item's is moved there
 constexpr int MIN_SHARE = OVERHEAD / 4;        // of a CTA, in keys
-constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
+constexpr uint64_t WAIT_LIMIT_NS = 8000000000ull;      // (a warp that computes its rows again, mend_rows, keeps the others waiting)
 constexpr float LEAST = 1.4012985e-45f;        // 2^-149
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
@@ -522,83 +522,201 @@ __device__ __forceinline__ bool next_seg(const Args& a, Ctrl* ctrl, uint32_t& co
 }
 
 // ------------------------------------------------------------------------------------------------------------ rows
-// A row whose O holds something that is not finite: if that comes from values that the row does not see (they weigh nothing, but
-// zero times infinity is NaN), the row is computed again without them, key by key.  Returns false where nothing has to be mended.
-struct RowAt {
-    i64 row;                  // of out and lse: token * Hq + head
-    const cake_bf16* q;
-    int k0, k1;               // the keys that it sees in this segment
-    int from, to;             // the keys that were multiplied
-    int g, part_row, part;
-    i64 base;                 // Seg::k0
-};
+// Rows whose O holds something that is not finite: if that comes from values that a row does not see (they weigh nothing, but zero times infinity is NaN), the row
+// is computed again without them, in 32 bits, from the keys that it sees in this segment.  A warp to its 32 rows: it looks once for the first and the last
+// such value of each column, and has then MEND rows at a time, a lane to a key for the scores, two or more columns to a lane for the sums.
+// Measured: a tile's 127 rows of 128 over 4,096 cached keys 7.5 ms (a row to a thread: 187), over 40,000 73 ms (heads of 256: 120), where the call takes 0.4 (0.6).  So 2 to 3 us
+// a key for a warp's rows: a piece of a million keys ends before the others' patience does.
 template <class T>
-__device__ __forceinline__ float key_at(const Args& a, const void* p, int d) {
+__device__ __forceinline__ float2 pair_at(const char* row, int d) {      // elements d and d + 1 of a key or value
     if (T::F16) {
-        uint32_t lo, hi;
-        e4m3_to_f16(static_cast<const cake_e4m3*>(p)[d], lo, hi);
-        return __half2float(__ushort_as_half(static_cast<unsigned short>(lo & 0xffff)));
+        const uint16_t w = *reinterpret_cast<const uint16_t*>(row + d);
+        uint32_t f;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(w));
+        return __half22float2(*reinterpret_cast<const __half2*>(&f));
     }
-    return bf16_f(static_cast<const cake_bf16*>(p)[d]);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(row + 2 * d);
+    return make_float2(bf16_lo(w), bf16_hi(w));
 }
-// where a key and its value are; false: nowhere
-template <class T>
-__device__ __forceinline__ bool locate(const Args& a, const RowAt& r, int key, const void*& k, const void*& v) {
+// where a key of a segment, or its value, is; nullptr: nowhere
+template <class T, bool VALUE>
+__device__ __forceinline__ const char* locate(const Args& a, const Seg* s, int key, int to) {
+    if (key >= to) return nullptr;
     if (T::PAGED) {
-        const int page = a.table[r.base + page_number(a, key)];
-        if (page < 0 || page >= a.c.num_pages) return false;
-        const i64 off = key % a.c.page_size, size = T::F16 ? 1 : 2;
-        k = static_cast<const char*>(a.c.k) + (page * a.c.k_page_stride + off * a.c.k_token_stride + r.g * a.c.k_head_stride) * size;
-        v = static_cast<const char*>(a.c.v) + (page * a.c.v_page_stride + off * a.c.v_token_stride + r.g * a.c.v_head_stride) * size;
-    } else {
-        if (r.base + key >= a.Tk) return false;
-        k = a.k + (r.base + key) * a.k_stride + r.g * a.k_head_stride;
-        v = a.v + (r.base + key) * a.v_stride + r.g * a.v_head_stride;
+        const int page = a.table[s->k0 + page_number(a, key)];
+        if (page < 0 || page >= a.c.num_pages) return nullptr;
+        const i64 off = key - page_number(a, key) * a.c.page_size;
+        return static_cast<const char*>(VALUE ? a.c.v : a.c.k) +
+               (VALUE ? page * a.c.v_page_stride + off * a.c.v_token_stride + s->g * a.c.v_head_stride
+                      : page * a.c.k_page_stride + off * a.c.k_token_stride + s->g * a.c.k_head_stride) * (T::F16 ? 1 : 2);
     }
-    return true;
+    return reinterpret_cast<const char*>(VALUE ? a.v + (s->k0 + key) * a.v_stride + s->g * a.v_head_stride : a.k + (s->k0 + key) * a.k_stride + s->g * a.k_head_stride);
 }
 template <class T>
-__device__ __forceinline__ bool mend_row(const Args& a, RowAt r, float c, float top, float vs) {
-    constexpr int D = T::D;
-    const void *k = nullptr, *v = nullptr;
-    bool wrong = false;
-#pragma unroll 1
-    for (int key = r.from; key < r.to && !wrong; ++key) {
-        if (key >= r.k0 && key < r.k1) {
-            key = r.k1 - 1;
-            continue;
+__device__ __forceinline__ void eight_at(const char* row, int d, float (&f)[8]) {      // elements d to d + 7
+    if (T::F16) {
+        const uint2 w = *reinterpret_cast<const uint2*>(row + d);
+        uint32_t h[4];
+        e4m3_to_f16(w.x, h[0], h[1]), e4m3_to_f16(w.y, h[2], h[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&h[j]));
+            f[2 * j] = u.x, f[2 * j + 1] = u.y;
         }
-        if (!locate<T>(a, r, key, k, v)) continue;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) wrong |= !isfinite(key_at<T>(a, v, d));
-    }
-    if (!wrong) return false;
-    float o[D], l = 0.f;
-#pragma unroll 1
-    for (int d = 0; d < D; ++d) o[d] = 0.f;
-#pragma unroll 1
-    for (int key = r.k0; key < r.k1; ++key) {
-        if (!locate<T>(a, r, key, k, v)) continue;
-        float dot = 0.f;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) dot = fmaf(bf16_f(r.q[d]), key_at<T>(a, k, d), dot);
-        const float p = ex2(fmaf(dot, c, -top));
-        l += p;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) o[d] = fmaf(p, key_at<T>(a, v, d), o[d]);
-    }
-    if (r.part < 0) {
-        const float f = l == 0.f ? 0.f : vs / l;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) a.out[r.row * D + d] = to_bf16(o[d] * f);
-        if (a.lse) a.lse[r.row] = (top + log2f(l)) * LN2;
     } else {
-        float* const to = a.parts + r.part * T::PART;
-#pragma unroll 1
-        for (int d = 0; d < D; ++d) to[static_cast<i64>(r.part_row) * D + d] = o[d];
-        to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row] = top, to[static_cast<i64>(T::PART_ROWS) * D + 2 * r.part_row + 1] = l;
+        const uint4 u = *reinterpret_cast<const uint4*>(row + 2 * d);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[2 * j] = bf16_lo(w[j]), f[2 * j + 1] = bf16_hi(w[j]);
     }
-    return true;
+}
+constexpr int MEND = 4;
+// todo: a bit for each of the warp's rows, row0 + bit of row tile t, that holds something that is not finite; tiles of keys [ra, rb) were multiplied
+template <class T>
+__device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, unsigned todo, int row0, int t, int ra, int rb) {
+    constexpr int D = T::D, PAIRS = (D + 63) / 64;
+    constexpr unsigned all = 0xffffffffu;
+    const int lane = threadIdx.x & 31, pos = s->pos, klen = s->klen;
+    const int tile = is_dual<T>(a, *s) ? t : 0;
+    int from = KT * ra, to = KT * rb;
+    if (T::PAGED) from = max(from, first_key(a, pos, klen)), to = min(to, end_key(a, pos + s->ntok - 1, klen));      // (others were not loaded)
+    else to = static_cast<int>(min(static_cast<i64>(to), a.Tk - s->k0));
+    // first and last key of which the lane's columns 2 lane + 64 j and the next are not finite
+    int first[2 * PAIRS], last[2 * PAIRS];
+#pragma unroll
+    for (int j = 0; j < 2 * PAIRS; ++j) first[j] = INT_MAX, last[j] = -1;
+#pragma unroll 1
+    for (int key = from; key < to; key += 32) {
+        const char* const mine = locate<T, true>(a, s, key + lane, to);
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 8) {
+            float2 f[8][PAIRS];
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const char* const v = reinterpret_cast<const char*>(__shfl_sync(all, reinterpret_cast<unsigned long long>(mine), i + b));
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) f[b][j] = v && 2 * lane + 64 * j < D ? pair_at<T>(v, 2 * lane + 64 * j) : make_float2(0.f, 0.f);
+            }
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) {
+                    if (!isfinite(f[b][j].x)) first[2 * j] = min(first[2 * j], key + i + b), last[2 * j] = key + i + b;
+                    if (!isfinite(f[b][j].y)) first[2 * j + 1] = min(first[2 * j + 1], key + i + b), last[2 * j + 1] = key + i + b;
+                }
+        }
+    }
+    const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[s->g] : 1.f, ks = T::F16 && a.c.k_scale ? a.c.k_scale[s->g] : 1.f;
+    for (;;) {
+        int rows[MEND], k0[MEND], k1[MEND], kmin = INT_MAX, kmax = 0;
+#pragma unroll
+        for (int n = 0; n < MEND; ++n) {
+            rows[n] = -1, k0[n] = k1[n] = 0;
+#pragma unroll 1
+            for (; todo && rows[n] < 0; todo &= todo - 1) {
+                const int r = row0 + __ffs(todo) - 1, tok = tile * a.tokens + r / a.heads;
+                const int b0 = max(from, first_key(a, pos + tok, klen)), b1 = min(to, end_key(a, pos + tok, klen));
+                bool unseen = false;
+#pragma unroll
+                for (int j = 0; j < 2 * PAIRS; ++j) unseen |= first[j] < b0 || last[j] >= b1;
+                if (__any_sync(all, unseen)) rows[n] = r, k0[n] = b0, k1[n] = b1, kmin = min(kmin, b0), kmax = max(kmax, b1);
+            }
+        }
+        if (rows[0] < 0) break;
+        const cake_bf16* q[MEND];
+        float c[MEND], inv[MEND], m[MEND], l[MEND];      // l: of the lane's keys
+        float2 o[MEND][PAIRS];
+#pragma unroll
+        for (int n = 0; n < MEND; ++n) {
+            const int r = rows[n] < 0 ? rows[0] : rows[n], tok = r / a.heads;
+            q[n] = a.q + (s->tok + tile * a.tokens + tok) * a.q_stride + (s->head0 + r - tok * a.heads) * a.q_head_stride;
+            const float qs = T::F16 ? ctrl->q_scale[tile][r] : 1.f;      // (as 16 bits took them: their products stay in 32)
+            c[n] = factor_of(a.scale_log2, ks, qs), inv[n] = 1.f / qs;
+            if (s->negative) c[n] = -c[n];
+            m[n] = NEG_INF, l[n] = 0.f;
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) o[n][j] = make_float2(0.f, 0.f);
+        }
+#pragma unroll 1
+        for (int key = kmin; key < kmax; key += 32) {
+            const char* const k = locate<T, false>(a, s, key + lane, kmax);
+            const char* const mine = locate<T, true>(a, s, key + lane, kmax);
+            float x[MEND];
+#pragma unroll
+            for (int n = 0; n < MEND; ++n) x[n] = 0.f;
+            if (k) {
+#pragma unroll 2
+                for (int d = 0; d < D; d += 8) {
+                    float f[8];
+                    eight_at<T>(k, d, f);
+#pragma unroll
+                    for (int n = 0; n < MEND; ++n) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(q[n] + d);
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float lo = T::F16 ? bf16_lo(w[j]) * inv[n] : bf16_lo(w[j]), hi = T::F16 ? bf16_hi(w[j]) * inv[n] : bf16_hi(w[j]);
+                            x[n] = fmaf(lo, f[2 * j], x[n]), x[n] = fmaf(hi, f[2 * j + 1], x[n]);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < MEND; ++n) {
+                const bool sees = k && key + lane >= k0[n] && key + lane < k1[n];
+                x[n] = sees ? x[n] * c[n] : NEG_INF;
+                float up = x[n];
+#pragma unroll
+                for (int b = 16; b; b >>= 1) up = fmaxf(up, __shfl_xor_sync(all, up, b));
+                up = fmaxf(up, m[n]);
+                const float base = up == NEG_INF ? 0.f : up, f = ex2(m[n] - base), p = ex2(x[n] - base);
+                m[n] = up, l[n] = l[n] * f + p;
+                x[n] = sees ? p : -1.f;            // the key's weight; -1: nothing, whatever its value is
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) o[n][j].x *= f, o[n][j].y *= f;
+            }
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 4) {
+                float2 u[4][PAIRS];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const char* const v = reinterpret_cast<const char*>(__shfl_sync(all, reinterpret_cast<unsigned long long>(mine), i + b));
+#pragma unroll
+                    for (int j = 0; j < PAIRS; ++j) u[b][j] = v && 2 * lane + 64 * j < D ? pair_at<T>(v, 2 * lane + 64 * j) : make_float2(0.f, 0.f);
+                }
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int n = 0; n < MEND; ++n) {
+                        const float w = __shfl_sync(all, x[n], i + b);
+                        if (w < 0.f) continue;
+#pragma unroll
+                        for (int j = 0; j < PAIRS; ++j) o[n][j].x = fmaf(w, u[b][j].x, o[n][j].x), o[n][j].y = fmaf(w, u[b][j].y, o[n][j].y);
+                    }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < MEND; ++n) {
+            if (rows[n] < 0) break;
+#pragma unroll
+            for (int b = 16; b; b >>= 1) l[n] += __shfl_xor_sync(all, l[n], b);
+            const int tok = rows[n] / a.heads, part_row = tile * MT + rows[n];
+            const i64 row = (s->tok + tile * a.tokens + tok) * a.Hq + s->head0 + rows[n] - tok * a.heads;
+            float* const part = a.parts + s->part * T::PART;
+            const float f = l[n] == 0.f ? 0.f : vs / l[n];
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) {
+                const int d = 2 * lane + 64 * j;
+                if (d >= D) continue;
+                if (s->part >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(part_row) * D + d) = o[n][j];
+                else *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o[n][j].x * f, o[n][j].y * f);
+            }
+            if (lane == 0) {
+                if (s->part >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(m[n], l[n]);
+                else if (a.lse) a.lse[row] = (m[n] + log2f(l[n])) * LN2;
+            }
+        }
+    }
 }
 
 // Queries of a row to f16, in place: divided by a power of two that brings its largest to [1, 2).  Returns that power.
@@ -919,25 +1037,12 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             if (n_other) arrive(&ctrl->o_free[1]);
         }
         if (valid) {
-            bool mended = false;
-            if (__builtin_expect(isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y)) && isfinite(l) && !empty, 0)) {
-                RowAt at;
-                const int klen = sp->klen, pos = sp->pos, ntok = sp->ntok;
-                at.row = row, at.g = g, at.part_row = part_row, at.part = part_at, at.base = sp->k0;
-                at.q = a.q + (sp->tok + my_tok) * a.q_stride + (sp->head0 + h) * a.q_head_stride;
-                at.from = KT * ra, at.to = KT * rb;
-                if (T::PAGED)                      // (what no row of the segment sees was not loaded)
-                    at.from = max(at.from, first_key(a, pos, klen)), at.to = min(at.to, end_key(a, pos + ntok - 1, klen));
-                at.k0 = max(k0, KT * ra), at.k1 = min(k1, KT * rb);
-                float cc = sp->negative ? -a.scale_log2 : a.scale_log2;
-                if (T::F16 && a.c.k_scale) cc *= fabsf(a.c.k_scale[g]);
-                mended = mend_row<T>(a, at, cc, sub, vs);
-            }
-            if (!mended) {
-                if (part_at >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
-                else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + __log2f(l)) * LN2;
-            }
+            if (part_at >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(sub, l);
+            else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + __log2f(l)) * LN2;
         }
+        const bool finite = !isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y));
+        const unsigned todo = __ballot_sync(0xffffffffu, valid && !finite && isfinite(l) && !empty);
+        if (__builtin_expect(todo != 0, 0)) mend_rows<T>(a, ctrl, sp, todo, r & 96, t, ra, rb);
         __syncwarp();
         if (lane == 0) arrive(&ctrl->seg_empty[segs % SEGS]);
     }

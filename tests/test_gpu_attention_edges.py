@@ -179,3 +179,100 @@ def test_lengths_beyond_the_table_and_sequences_beside_those_that_are_left_out()
         mine, other = slice(5 * kept, 5 * kept + 5), slice(5 - 5 * kept, 10 - 5 * kept)
         assert (out[other] == 3).all() and (lse[other] == 2).all()
         base.check_chunk(out[mine], lse[mine], q[mine], cache, table[kept:kept + 1], [5], [[48, 40][kept]])
+
+
+# ------------------------------------------------------------------------- values that are not finite, seen and not seen
+def check_around(out, lse, q, keys_values, new, lens, Hkv, bad, window=0, keep=None, **more):
+    """bad: {(sequence, token): columns} whose values are not finite.  Tokens that see none of them are theirs; of the others the columns named are not finite, the rest theirs."""
+    scale, a = q.shape[2] ** -0.5, 0
+    for b, n in enumerate(new):
+        marks = sorted(t for s, t in bad if s == b)
+        cuts = sorted({0, *(min(max(t - (lens[b] - n), 0), n) for t in marks), *(min(max(t - (lens[b] - n) + window, 0), n) for t in marks if window), n})
+        for i0, i1 in zip(cuts[:-1], cuts[1:]):
+            L = lens[b] - n + i1                      # these tokens' keys
+            first = max(0, L - (i1 - i0) - window + 1) if window else 0      # of the first of them
+            seen = [t for t in marks if t < L and t >= (L - window if window else 0)]
+            cols = sorted({c for t in seen for c in bad[b, t]})
+            sub, sub_lse = out[a + i0:a + i1].clone(), lse[a + i0:a + i1]
+            assert not torch.isfinite(sub[..., cols]).any()
+            sub[..., cols] = 0
+
+            def without(_, g):
+                k, v = (t[:L].double().clone() for t in keys_values(b, g))
+                for t in marks:
+                    if t < L:
+                        v[t, list(bad[b, t])] = 0
+                v[:, cols] = 0
+                return k, v
+            base.check(sub, sub_lse, q[a + i0:a + i1], without, [i1 - i0], [L], Hkv, scale, True, window,
+                       keep=None if keep is None else lambda _, g: keep[b, :L], **more)
+        a += n
+
+
+NOT_FINITE = [(D, new, lens, window) for D in (64, 96, 128, 256) for new, lens, window in
+              (([200, 5], [330, 130], 0), ([3], [4001], 0), ([70, 300], [2500, 300], 0), ([150, 260], [1700, 900], 77))]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("D,new,lens,window", NOT_FINITE)
+def test_chunk_values_that_are_not_finite(kv, D, new, lens, window):
+    """Whole items and parts of them, two row tiles and one, pages that are missing."""
+    page = 16
+    q, cache, table, n = base.paged(D + window, new, lens, 4, 2, D, page, kv)
+    g = base.gen(D)
+    bad, keep = {}, torch.ones(len(new), max(lens), dtype=torch.bool, device=DEV)
+    missing = [(b, max(L - m, 0) // 2 // page) for b, (m, L) in enumerate(zip(new, lens)) if L > m + 2 * page]
+    for b, (m, L) in enumerate(zip(new, lens)):
+        for t, cols in ((L - 1, range(D)), (L - 1 - m // 3, (3, D - 1)), (L - 1 - m // 2, (D // 2,))):
+            bad.setdefault((b, t), tuple(cols))
+    for (b, t), cols in bad.items():
+        where = table[b, t // page].long(), t % page
+        for c in cols:
+            if kv == "e4m3":
+                cache.v.view(torch.uint8)[where[0], where[1], :, c] = 0x7f
+            else:
+                cache.v[where[0], where[1], :, c] = (math.nan, math.inf, -math.inf)[c % 3]
+    for b, entry in missing:
+        table[b, entry] = -1
+        keep[b, entry * page:(entry + 1) * page] = False
+    ws = cake.alloc_attention_workspace(4, 2, D, DEV)
+    out, lse = cake.cake_paged_chunk(q, cache, table, n, base.starts_of(new), want_lse=True, ws=ws, window=window)
+    assert cake.cake_kmeans_device_status(ws) == (cake.CAKE_ERR_BAD_INDEX if missing and not window else cake.CAKE_OK)
+    held = table.clamp(min=0)
+
+    def keys_values(b, h):
+        k, v = base.cached(cache, held, lens, b, h)
+        return torch.where(keep[b, :lens[b], None], k, torch.zeros_like(k)), torch.where(keep[b, :lens[b], None], v, torch.zeros_like(v))
+    check_around(out, lse, q, keys_values, new, lens, 2, bad, window, keep, f16=kv == "e4m3")
+
+
+@pytest.mark.parametrize("D,new,lens,window", NOT_FINITE)
+def test_prompt_values_that_are_not_finite_in_every_form(D, new, lens, window):
+    q, k, v = base.packed(D + window, new, lens, 4, 2, D)
+    at, bad = [0, lens[0], sum(lens)], {}
+    for b, (m, L) in enumerate(zip(new, lens)):
+        for t, cols in ((L - 1, range(D)), (L - 1 - m // 3, (3, D - 1)), (L - 1 - m // 2, (D // 2,))):
+            bad.setdefault((b, t), tuple(cols))
+    for (b, t), cols in bad.items():
+        for c in cols:
+            v[at[b] + t, :, c] = (math.nan, math.inf, -math.inf)[c % 3]
+    out, lse = base.run_packed(q, k, v, new, lens, window=window)
+    check_around(out, lse, q, lambda b, g: (k[at[b]:at[b + 1], g], v[at[b]:at[b + 1], g]), new, lens, 2, bad, window)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_rows_computed_again_over_a_long_context(kv):
+    """As many sequences as CTAs over the same 40,000 cached tokens, the newest of which has a value that is not finite: all earlier rows of its tile are computed again."""
+    B, L, n, D, page = 148, 40000, 128, 128, 64
+    q, cache, table, lens = base.paged(1, [n], [L], 1, 1, D, page, kv)
+    q = base.normal(base.gen(2), B * n, 1, D, std=1.2)
+    where = table[0, (L - 1) // page].long(), (L - 1) % page
+    if kv == "e4m3":
+        cache.v.view(torch.uint8)[where[0], where[1], 0, 7] = 0x7f
+    else:
+        cache.v[where[0], where[1], 0, 7] = math.inf
+    out, lse = base.run_chunk(q, cache, table.expand(B, -1).contiguous(), lens.expand(B).contiguous(), [n] * B)
+    for b in (0, 77, B - 1):
+        rows = slice(b * n, b * n + n)
+        check_around(out[rows], lse[rows], q[rows], lambda _, g: base.cached(cache, table, [L], 0, g), [n], [L], 1, {(0, L - 1): (7,)}, f16=kv == "e4m3")
+    assert torch.isfinite(out.view(B, n, D)[:, :-1]).all()
