@@ -144,7 +144,7 @@ struct Traits {
 struct __align__(16) Ctrl {
     uint64_t seg_full[SEGS], seg_empty[SEGS];
     uint64_t q_full[2], q_empty[2], q_conv[2];
-    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_end;
     uint64_t raw_full[4][3];                   // of a loading warp's places
     uint64_t s_full[2], p_ready[2], o_done[2], o_free[2], s_free, x_full, x_empty, drained[2];
     Seg seg[SEGS];
@@ -580,7 +580,7 @@ __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, 
     const int tile = is_dual<T>(a, *s) ? t : 0;
     int from = KT * ra, to = KT * rb;
     if (T::PAGED) from = max(from, first_key(a, pos, klen)), to = min(to, end_key(a, pos + s->ntok - 1, klen));      // (others were not loaded)
-    else to = static_cast<int>(min(static_cast<i64>(to), a.Tk - s->k0));
+    else to = min(to, klen);                       // (zeros were put behind the sequence)
     // first and last key of which the lane's columns 2 lane + 64 j and the next are not finite
     int first[2 * PAIRS], last[2 * PAIRS];
 #pragma unroll
@@ -1049,30 +1049,58 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
 }
 
 // ------------------------------------------------------------------------------------------------------------ loads
-// Values of packed prompts: one thread
+// Values of packed prompts: one warp.
+template <class T>
+__device__ __forceinline__ void load_unit(uint32_t place, const CUtensorMap* mv, uint64_t* full, int column, int g, int key) {
+    const uint32_t bar = ptx::smem_u32(full);
+    ptx::mbar_arrive_expect_tx(bar, T::V_UNIT);
+#pragma unroll
+    for (int x = 0; x < T::V_SLABS; ++x) ptx::tma_load_3d(place + x * T::SLAB, mv, bar, column + 64 * x, g, key);
+}
+// What lies behind a sequence in its last tile is another's or nobody's: zeros in its place, of which no weight of zero makes a NaN
+template <class T>
+__device__ __noinline__ void load_end(Ctrl* ctrl, int* status, uint8_t* place, const CUtensorMap* mv, uint64_t* full, uint32_t ends, int column, int g, int key, int kept) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) load_unit<T>(ptx::smem_u32(place), mv, &ctrl->v_end, column, g, key);
+    __syncwarp();
+    wait_bar(&ctrl->v_end, ends, ctrl, status);
+#pragma unroll 1
+    for (int x = 0; x < T::V_SLABS; ++x)
+#pragma unroll 4
+        for (int at = kept * 128 + lane * 16; at < KT * 128; at += 512) *reinterpret_cast<uint4*>(place + x * T::SLAB + at) = make_uint4(0u, 0u, 0u, 0u);
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) arrive(full);
+}
 template <class T>
 __device__ __forceinline__ void load_values(const Args& a, Ctrl* ctrl, const Room& room, const CUtensorMap* mv) {
-    uint32_t segs = 0, nv = 0;
+    const bool lead = ptx::elect_one();
+    uint32_t segs = 0, nv = 0, ends = 0;                    // segments, units, units that a sequence ends in
     Seg s;
-    while (next_seg(a, ctrl, segs, s, true)) {
+    while (next_seg(a, ctrl, segs, s, false)) {
+        const int klen = uniform(s.klen);
 #pragma unroll 1
-        for (int j = s.ja; j < s.jb; ++j)
+        for (int j = s.ja; j < s.jb; ++j) {
 #pragma unroll 1
             for (int u = 0; u < T::NVU; ++u, ++nv) {
                 const uint32_t st = nv % T::V_STAGES;
                 wait_bar(&ctrl->v_empty[st], nv / T::V_STAGES + 1, ctrl, a.status);
-                if (aborted(ctrl)) {
-                    landed(ctrl->v_full, nv, T::V_STAGES);
-                    return;
-                }
-                const uint32_t bar = ptx::smem_u32(&ctrl->v_full[st]);
-                ptx::mbar_arrive_expect_tx(bar, T::V_UNIT);
-#pragma unroll
-                for (int x = 0; x < T::V_SLABS; ++x)
-                    ptx::tma_load_3d(ptx::smem_u32(room.v) + st * T::V_UNIT + x * T::SLAB, mv, bar, T::VC * u + 64 * x, s.g, static_cast<int>(s.k0) + KT * j);
+                if (any_aborted(ctrl)) break;
+                uint8_t* const place = room.v + st * T::V_UNIT;
+                const int key = static_cast<int>(s.k0) + KT * j;
+                if (__builtin_expect(klen < KT * (j + 1), 0)) load_end<T>(ctrl, a.status, place, mv, &ctrl->v_full[st], ends++, T::VC * u, s.g, key, klen - KT * j);
+                else if (lead) load_unit<T>(ptx::smem_u32(place), mv, &ctrl->v_full[st], T::VC * u, s.g, key);
+                __syncwarp();
             }
+            if (any_aborted(ctrl)) break;
+        }
+        if (any_aborted(ctrl)) break;
     }
-    if (aborted(ctrl)) landed(ctrl->v_full, nv, T::V_STAGES);
+    if (lead && aborted(ctrl)) {
+        landed(ctrl->v_full, nv, T::V_STAGES);
+        landed(&ctrl->v_end, ends, 1);
+    }
+    __syncwarp();
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w) {
@@ -1408,7 +1436,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (int i = 0; i < T::V_STAGES; ++i) init(&ctrl->v_full[i], T::F16 ? 4 : T::PAGED ? 2 : 1), init(&ctrl->v_empty[i], 1);
         if (T::F16)
             for (int i = 0; i < 12; ++i) init(&ctrl->raw_full[i / 3][i % 3], 1);
-        init(&ctrl->x_full, 4), init(&ctrl->x_empty, 4), init(&ctrl->s_free, 4), init(&ctrl->drained[0], 1), init(&ctrl->drained[1], 1);
+        init(&ctrl->v_end, 1), init(&ctrl->x_full, 4), init(&ctrl->x_empty, 4), init(&ctrl->s_free, 4), init(&ctrl->drained[0], 1), init(&ctrl->drained[1], 1);
         ctrl->abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&mq);
@@ -1442,8 +1470,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         if (warp == T::WARP_SCHED) {
             schedule<T>(a, ctrl, room, &mq, &mk);
         } else if (warp == T::WARP_VALUES) {
-            if (!T::PAGED && ptx::elect_one()) load_values<T>(a, ctrl, room, &mv);
-            __syncwarp();
+            if (!T::PAGED) load_values<T>(a, ctrl, room, &mv);
         } else if (warp == T::WARP_MMA) {
             scores_warp<T>(a, ctrl, ptx::smem_u32(room.q), ptx::smem_u32(room.k), tmem);
         } else {

@@ -276,3 +276,30 @@ def test_rows_computed_again_over_a_long_context(kv):
         rows = slice(b * n, b * n + n)
         check_around(out[rows], lse[rows], q[rows], lambda _, g: base.cached(cache, table, [L], 0, g), [n], [L], 1, {(0, L - 1): (7,)}, f16=kv == "e4m3")
     assert torch.isfinite(out.view(B, n, D)[:, :-1]).all()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 50)])
+def test_what_lies_behind_a_sequence_does_not_matter(D, causal, window):
+    """Padding, and a neighbour's values: NaN there gives the same bits.  Sequences whose last tile holds one key, nearly all, all; several tiles, cut items."""
+    for lens in ([1, 130, 127, 128, 2, 255], [1500]):
+        q, k, v = base.packed(D, lens, lens, 4, 2, D, extra=140)
+        out, lse = base.run_packed(q, k, v, lens, lens, causal, window)
+        k2, v2 = k.clone(), v.clone()
+        k2[sum(lens):], v2[sum(lens):] = math.nan, math.inf
+        again, lse2 = base.run_packed(q, k2, v2, lens, lens, causal, window)
+        n = sum(lens)
+        assert torch.equal(again[:n], out[:n]) and torch.equal(lse2[:n], lse[:n])
+        at = 0
+        for i, m in enumerate(lens):                  # every other sequence is not finite
+            if i % 2:
+                k2[at:at + m], v2[at:at + m] = math.nan, math.nan
+            at += m
+        again, lse2 = base.run_packed(q, k2, v2, lens, lens, causal, window)
+        at = 0
+        for i, m in enumerate(lens):
+            if i % 2 == 0:
+                assert torch.equal(again[at:at + m], out[at:at + m]) and torch.equal(lse2[at:at + m], lse[at:at + m])
+            else:
+                assert torch.isnan(again[at:at + m]).all()
+            at += m
