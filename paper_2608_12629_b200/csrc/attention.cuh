@@ -522,11 +522,13 @@ __device__ __forceinline__ bool next_seg(const Args& a, Ctrl* ctrl, uint32_t& co
 }
 
 // ------------------------------------------------------------------------------------------------------------ rows
-// Rows whose O holds something that is not finite: if that comes from values that a row does not see (they weigh nothing, but zero times infinity is NaN), the row
-// is computed again without them, in 32 bits, from the keys that it sees in this segment.  A warp to its 32 rows: it looks once for the first and the last
-// such value of each column, and has then MEND rows at a time, a lane to a key for the scores, two or more columns to a lane for the sums.
+// Rows whose O holds something that is not finite.  It may come from values that a row does not see (they weigh nothing, but zero times infinity is NaN), or from
+// finite ones whose weighted sum passes 32 bits (weights reach 2^20): the row is then computed again, in 32 bits, from the keys that it sees in this segment, with
+// weights of at most 2^-DOWN.  Where it comes from infinities and NaN that the row sees it is right as it is.  A warp to its 32 rows: it looks once for the first and the
+// last such value of each column, and has then MEND rows at a time, a lane to a key for the scores, two or more columns to a lane for the sums.
 // Measured: a tile's 127 rows of 128 over 4,096 cached keys 7.5 ms (a row to a thread: 187), over 40,000 73 ms (heads of 256: 120), where the call takes 0.4 (0.6).  So 2 to 3 us
 // a key for a warp's rows: a piece of a million keys ends before the others' patience does.
+__device__ __forceinline__ float2 as_pair(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
 template <class T>
 __device__ __forceinline__ float2 pair_at(const char* row, int d) {      // elements d and d + 1 of a key or value
     if (T::F16) {
@@ -535,8 +537,7 @@ __device__ __forceinline__ float2 pair_at(const char* row, int d) {      // elem
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(w));
         return __half22float2(*reinterpret_cast<const __half2*>(&f));
     }
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(row + 2 * d);
-    return make_float2(bf16_lo(w), bf16_hi(w));
+    return as_pair(*reinterpret_cast<const uint32_t*>(row + 2 * d));
 }
 // where a key of a segment, or its value, is; nullptr: nowhere
 template <class T, bool VALUE>
@@ -570,12 +571,13 @@ __device__ __forceinline__ void eight_at(const char* row, int d, float (&f)[8]) 
         for (int j = 0; j < 4; ++j) f[2 * j] = bf16_lo(w[j]), f[2 * j + 1] = bf16_hi(w[j]);
     }
 }
-constexpr int MEND = 4;
+constexpr int MEND = 4, DOWN = 40;
 // todo: a bit for each of the warp's rows, row0 + bit of row tile t, that holds something that is not finite; tiles of keys [ra, rb) were multiplied
 template <class T>
 __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, unsigned todo, int row0, int t, int ra, int rb) {
     constexpr int D = T::D, PAIRS = (D + 63) / 64;
     constexpr unsigned all = 0xffffffffu;
+    constexpr float kDown = 1.f / (1ull << DOWN);
     const int lane = threadIdx.x & 31, pos = s->pos, klen = s->klen;
     const int tile = is_dual<T>(a, *s) ? t : 0;
     int from = KT * ra, to = KT * rb;
@@ -607,6 +609,12 @@ __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, 
         }
     }
     const float vs = T::F16 && a.c.v_scale ? a.c.v_scale[s->g] : 1.f, ks = T::F16 && a.c.k_scale ? a.c.k_scale[s->g] : 1.f;
+    float* const part = a.parts + s->part * T::PART;
+    auto out_row = [&](int r) {
+        const int tok = r / a.heads;
+        return (s->tok + tile * a.tokens + tok) * a.Hq + s->head0 + r - tok * a.heads;
+    };
+    __syncwarp();                                           // (rows that others of the warp have stored)
     for (;;) {
         int rows[MEND], k0[MEND], k1[MEND], kmin = INT_MAX, kmax = 0;
 #pragma unroll
@@ -616,10 +624,18 @@ __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, 
             for (; todo && rows[n] < 0; todo &= todo - 1) {
                 const int r = row0 + __ffs(todo) - 1, tok = tile * a.tokens + r / a.heads;
                 const int b0 = max(from, first_key(a, pos + tok, klen)), b1 = min(to, end_key(a, pos + tok, klen));
-                bool unseen = false;
+                bool again = false;
 #pragma unroll
-                for (int j = 0; j < 2 * PAIRS; ++j) unseen |= first[j] < b0 || last[j] >= b1;
-                if (__any_sync(all, unseen)) rows[n] = r, k0[n] = b0, k1[n] = b1, kmin = min(kmin, b0), kmax = max(kmax, b1);
+                for (int j = 0; j < PAIRS; ++j) {
+                    const int d = 2 * lane + 64 * j;
+                    if (d >= D) continue;
+                    const float2 f = s->part >= 0 ? *reinterpret_cast<const float2*>(part + static_cast<i64>(tile * MT + r) * D + d)
+                                                  : as_pair(*reinterpret_cast<const uint32_t*>(a.out + out_row(r) * D + d));
+                    // (last is -1 where there are none)
+                    again |= first[2 * j] < b0 || last[2 * j] >= b1 || (last[2 * j] < 0 && !isfinite(f.x));
+                    again |= first[2 * j + 1] < b0 || last[2 * j + 1] >= b1 || (last[2 * j + 1] < 0 && !isfinite(f.y));
+                }
+                if (__any_sync(all, again)) rows[n] = r, k0[n] = b0, k1[n] = b1, kmin = min(kmin, b0), kmax = max(kmax, b1);
             }
         }
         if (rows[0] < 0) break;
@@ -671,7 +687,7 @@ __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, 
                 up = fmaxf(up, m[n]);
                 const float base = up == NEG_INF ? 0.f : up, f = ex2(m[n] - base), p = ex2(x[n] - base);
                 m[n] = up, l[n] = l[n] * f + p;
-                x[n] = sees ? p : -1.f;            // the key's weight; -1: nothing, whatever its value is
+                x[n] = sees ? p * kDown : -1.f;    // the key's weight; -1: nothing, whatever its value is
 #pragma unroll
                 for (int j = 0; j < PAIRS; ++j) o[n][j].x *= f, o[n][j].y *= f;
             }
@@ -700,19 +716,18 @@ __device__ __noinline__ void mend_rows(const Args& a, Ctrl* ctrl, const Seg* s, 
             if (rows[n] < 0) break;
 #pragma unroll
             for (int b = 16; b; b >>= 1) l[n] += __shfl_xor_sync(all, l[n], b);
-            const int tok = rows[n] / a.heads, part_row = tile * MT + rows[n];
-            const i64 row = (s->tok + tile * a.tokens + tok) * a.Hq + s->head0 + rows[n] - tok * a.heads;
-            float* const part = a.parts + s->part * T::PART;
+            const int part_row = tile * MT + rows[n];
+            const i64 row = out_row(rows[n]);
             const float f = l[n] == 0.f ? 0.f : vs / l[n];
 #pragma unroll
             for (int j = 0; j < PAIRS; ++j) {
                 const int d = 2 * lane + 64 * j;
                 if (d >= D) continue;
                 if (s->part >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(part_row) * D + d) = o[n][j];
-                else *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o[n][j].x * f, o[n][j].y * f);
+                else *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o[n][j].x * f * (1.f / kDown), o[n][j].y * f * (1.f / kDown));
             }
             if (lane == 0) {
-                if (s->part >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(m[n], l[n]);
+                if (s->part >= 0) *reinterpret_cast<float2*>(part + static_cast<i64>(T::PART_ROWS) * D + 2 * part_row) = make_float2(m[n] + DOWN, l[n] * kDown);
                 else if (a.lse) a.lse[row] = (m[n] + log2f(l[n])) * LN2;
             }
         }
@@ -1496,7 +1511,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 
 // ------------------------------------------------------------------------------------------------------------- join
 // out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m), m = max m_i, over the parts of an item, in order.  A warp to a row, or, for few rows of many
-// parts, a block to a row (its warps share the parts).
+// parts, a block to a row (its warps share the parts).  Sums lie 2^8 lower (MOST_CTAS parts at most), so that those of finite parts are finite.
+static_assert(MOST_CTAS <= 256, "");
 constexpr int JOIN_WARPS = 8, JOIN_BATCH = 4, JOIN_SLICES = 16;      // SLICES: blocks to an item
 template <int D, int ROWS, int TILES>
 __global__ void __launch_bounds__(32 * JOIN_WARPS)
@@ -1524,9 +1540,9 @@ attention_join_kernel(const Args a) {
         float4 acc[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](float pm, float pl, const float4 (&u)[V]) {
+        auto add = [&](float pm, float pl, const float4 (&u)[V], float down) {
             const float up = fmaxf(m, pm), from = up == NEG_INF ? 0.f : up;
-            const float f = ex2(m - from), g = ex2(pm - from);
+            const float f = ex2(m - from), g = ex2(pm - from) * down;
             m = up, l = l * f + pl * g;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -1554,7 +1570,7 @@ attention_join_kernel(const Args a) {
                 }
             }
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) add(ml[b].x, ml[b].y, u[b]);
+            for (int b = 0; b < BATCH; ++b) add(ml[b].x, ml[b].y, u[b], 1.f / 256.f);
         }
         if (many) {
             __syncthreads();
@@ -1567,7 +1583,7 @@ attention_join_kernel(const Args a) {
                 float4 u[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) u[v] = accs[w][v][lane];
-                add(mls[w].x, mls[w].y, u);
+                add(mls[w].x, mls[w].y, u, 1.f);
             }
         }
         const float f = l == 0.f ? 0.f : vs / l;
@@ -1580,7 +1596,7 @@ attention_join_kernel(const Args a) {
             cake_bf16* const to = a.out + out_row * D + d;
             *reinterpret_cast<uint2*>(to) = w;
         }
-        if (a.lse && lane == 0) a.lse[out_row] = l == 0.f ? NEG_INF : (m + log2f(l)) * LN2;
+        if (a.lse && lane == 0) a.lse[out_row] = l == 0.f ? NEG_INF : (m + log2f(l * 256.f)) * LN2;
     }
 }
 

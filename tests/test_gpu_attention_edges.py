@@ -303,3 +303,36 @@ def test_what_lies_behind_a_sequence_does_not_matter(D, causal, window):
             else:
                 assert torch.isnan(again[at:at + m]).all()
             at += m
+
+
+# ------------------------------------------------------------------------------------------------------- large values
+def large(g, *shape):
+    """Finite bf16 values of up to 3.3e38, half of them above 2^126."""
+    return (base.normal(g, *shape, dtype=torch.float32) * 2.0 ** 127).clamp(-3.3e38, 3.3e38).to(BF16)
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("new,lens,window", [([300, 5], [300, 5], 0), ([3], [4001], 0), ([2500], [2500], 0), ([300], [1700], 150)])
+def test_finite_values_whose_sums_pass_32_bits(D, new, lens, window):
+    """Their average does not: rows of whole items, of parts, and of parts that are joined."""
+    q, k, v = base.packed(D + window, new, lens, 4, 2, D)
+    v = large(base.gen(D), *v.shape)
+    k[: lens[0] // 2] *= 0.1                          # (later keys' weights pass the first tile's by far)
+    out, lse = base.run_packed(q, k, v, new, lens, window=window)
+    base.check_packed(out, lse, q, k, v, new, lens, window=window)
+    v[:, 1] *= 2.0 ** -9                              # beside a head whose sums do not, until its weights do
+    out, lse = base.run_packed(q, k, v, new, lens, window=window)
+    base.check_packed(out, lse, q, k, v, new, lens, window=window)
+
+
+def test_finite_values_whose_sums_pass_32_bits_over_pages():
+    new, lens = [200, 3], [330, 3000]
+    q, cache, table, n = base.paged(3, new, lens, 4, 2, 128, 16, "bf16")
+    cache.v.copy_(torch.where(torch.isfinite(cache.v), large(base.gen(4), *cache.v.shape), cache.v))
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    base.check_chunk(out, lse, q, cache, table, new, lens)
+    # and an infinity that some see: its column is theirs, the others are averages
+    where = table[0, 320 // 16].long(), 0
+    cache.v[where[0], where[1], :, 5] = math.inf
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    check_around(out, lse, q, lambda b, g: base.cached(cache, table, lens, b, g), new, lens, 2, {(0, 320): (5,)})
