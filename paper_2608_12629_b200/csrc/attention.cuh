@@ -764,9 +764,12 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
     constexpr int D = T::D;
     // What is subtracted from a row's scores, m, is the maximum of the first tile in which it sees anything; it is raised to the maximum so far
     // only when a tile's weights add up to more than LIMIT.  So the maximum of most tiles is never looked for, and O is hardly ever
-    // rescaled: weights above 1 do no harm in 32 bits, nor rounded to bf16.  Weights in f16 (8-bit values, which widen to f16 exactly) lie LIFT higher, so
-    // that 11 bits are held down to 2^-21 of the heaviest and steps of 2^-31 below; each is at most LIMIT, which f16 holds
-    constexpr float LIFT = T::F16 ? 7.f : 0.f, LIMIT = T::F16 ? 65000.f : 1048576.f;
+    // rescaled: weights above 1 do no harm in 32 bits, nor rounded to bf16.  Weights in f16 (8-bit values, which widen to f16 exactly) lie LIFT higher, the heaviest at 2^11 or
+    // above, so that 11 bits are held down to 2^-25 of it and steps of 2^-35 below.  A tile of which a quarter's weights add up to more than f16 holds is looked
+    // at, and m is raised where one of them passes 2^(LIFT + ROOM); so that this is rare, every row looks for its maximum at its 2nd, 5th, 17th, ... tile too.  (2 x 32,768
+    // keys, scores of a spread of up to 1.8: 1,669 us; without those looks 1,812 - 1,858; raised whenever a larger one is found, 512 tokens over 2 x 8,192: 417 us for 350;
+    // heaviest at 2^7, 11 bits down to 2^-21: 1,637 and 349)
+    constexpr float LIFT = T::F16 ? 11.f : 0.f, ROOM = T::F16 ? 4.875f : 0.f, LIMIT = T::F16 ? 60000.f : 1048576.f;
     // x c - m in one rounding lies beside what m = x c was rounded by: half a step of m, which passes 2^x's range where m passes 2^30.  Scores that reach FAR, whose
     // neighbours in 32 bits are two powers of two apart, are multiplied by the power of two that is not below c instead, which rounds nothing; what is
     // beyond FAR stays beyond it, in the same order
@@ -859,6 +862,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             }
             // Which rows look for their maximum: it is theirs alone to say, so that a row's bits do not depend on its neighbours
             bool search = m == NEG_INF;
+            if (T::F16) search |= live && i > 0 && (i & (i - 1)) == 0 && (i & 0x55555555) != 0;
             if (__builtin_expect(masked, 0)) {
                 const uint32_t seen[4] = {pages.x, pages.y, pages.z, pages.w};
 #pragma unroll
@@ -886,7 +890,8 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                     }
                     top[0] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                     const float near = top[0] * c_near, up = fabsf(near) < FAR ? near : top[0] * c_far;
-                    const bool higher = search && up > m;
+                    const bool higher = search && up > (pass > 0 ? m + ROOM : m);
+                    if (T::F16 && pass > 0 && !__any_sync(0xffffffffu, higher)) break;
                     const float f = higher ? ex2(m - up) : 1.f;
                     if (higher) m = up;
                     c = fabsf(m) < FAR ? c_near : c_far;
@@ -927,7 +932,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                 }
                 total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 // (the second time m is the maximum: no more than that can be done for scores so large that their differences are lost)
-                search = live && !search && total > LIMIT;
+                search = live && !search && (T::F16 ? fmaxf(ptx::fmax3(sum[0].x, sum[0].y, sum[1].x), sum[1].y) : total) > LIMIT;
                 if (pass > 0 || !__any_sync(0xffffffffu, search)) break;
             }
             ++o_count[pb];

@@ -336,3 +336,53 @@ def test_finite_values_whose_sums_pass_32_bits_over_pages():
     cache.v[where[0], where[1], :, 5] = math.inf
     out, lse = base.run_chunk(q, cache, table, n, new)
     check_around(out, lse, q, lambda b, g: base.cached(cache, table, lens, b, g), new, lens, 2, {(0, 320): (5,)})
+
+
+# ------------------------------------------------------------------------------------------ light weights, 8-bit caches
+@pytest.mark.parametrize("D,new,lens", [(64, 1, 300), (128, 200, 330), (128, 3, 4001), (256, 40, 1500)])
+@pytest.mark.parametrize("where", [5, 0.6, -1])
+@pytest.mark.parametrize("light", [0.5, 0.0, -1.0])
+def test_light_keys_of_an_8_bit_cache(D, new, lens, where, light):
+    """One key has all of the weight and values of zero; what is left are keys of 2^-28 to 2^-31 of it, all alike.  Weights hold 11 bits down to 2^-25 of the heaviest, steps of 2^-35 below:
+    half a step, 2^-36, for each key, as for a decode."""
+    where = int(where * lens) if 0 < where < 1 else where % lens
+    new = min(new, lens - where)                      # (all of its tokens see the heavy key)
+    q, cache, table, n = base.paged(2, [new], [lens], 2, 1, D, 16, "e4m3")
+    g = base.gen(D)
+    q.zero_()
+    q[:, 0, 0], q[:, 1, 0] = 1.0, 0.5
+    k = torch.zeros(lens, 1, D, device=DEV)
+    k[:, 0, 0] = light
+    k[where, 0, 0] = 20.0
+    v = 1 + torch.rand(lens, 1, D, generator=g, device=DEV)
+    v[where] = 0
+    t = torch.arange(lens, device=DEV)
+    at = table[0, t // 16].long(), t % 16
+    cache.k.view(torch.uint8)[at], cache.v.view(torch.uint8)[at] = k.to(E4M3).view(torch.uint8), v.to(E4M3).view(torch.uint8)
+    cache.k_scale.fill_(1.0)
+    cache.v_scale.fill_(1.0)
+    out, lse = base.run_chunk(q, cache, table, n, [new], scale=1.0)
+    ref, _ = cake.cake_paged_decode(q[-1:].contiguous(), cache, table, n, scale=1.0)
+    kk, vv = base.cached(cache, table, [lens], 0, 0)
+    want, want_lse, most, delta, _ = base.reference(q, kk, vv, 1.0, base.visible(new, lens, True, 0))
+    for got, rows in ((out, slice(0, new)), (ref, slice(new - 1, new))):
+        bound = (2.0 ** -11 + 2 * delta[rows] + 2 * (40 + lens / 128) * base.U)[..., None] * most[rows] + 1.01 * 2.0 ** -8 * want[rows].abs() + 1.01 * 2.0 ** -36 * vv.sum(0)
+        err = (got.double() - want[rows]).abs()
+        assert (err <= bound).all(), f"worst {float((err / bound).max()):.3g} bounds"
+    assert ((lse.double() - want_lse).abs() <= delta + (40 + lens / 128) * base.U + 2.0 ** -22 + 2 * base.U * want_lse.abs()).all()
+
+
+@pytest.mark.parametrize("D,new,lens", [(64, [40], [3000]), (128, [300, 5], [900, 2000]), (256, [20], [1500])])
+@pytest.mark.parametrize("std", [0.0, 0.05, 0.4, 8.0])
+def test_flat_and_steep_rows_of_an_8_bit_cache(D, new, lens, std):
+    """Weights that are all alike add up to more than f16 holds although none passes it; scores that grow from tile to tile do pass it, by little and by much."""
+    q, cache, table, n = base.paged(7, new, lens, 4, 2, D, 16, "e4m3", std=std)
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    base.check_chunk(out, lse, q, cache, table, new, lens)
+    q.fill_(0.25)
+    for b, L in enumerate(lens):
+        t = torch.arange(L, device=DEV)
+        rows = ((t // 64).float() * (1 + std) * 8 / D / 0.25 / 0.02)[:, None, None].expand(L, 2, D)
+        cache.k.view(torch.uint8)[table[b, t // 16].long(), t % 16] = rows.clamp(max=448).to(E4M3).contiguous().view(torch.uint8)
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    base.check_chunk(out, lse, q, cache, table, new, lens)
