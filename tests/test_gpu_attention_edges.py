@@ -386,3 +386,37 @@ def test_flat_and_steep_rows_of_an_8_bit_cache(D, new, lens, std):
         cache.k.view(torch.uint8)[table[b, t // 16].long(), t % 16] = rows.clamp(max=448).to(E4M3).contiguous().view(torch.uint8)
     out, lse = base.run_chunk(q, cache, table, n, new)
     base.check_chunk(out, lse, q, cache, table, new, lens)
+
+
+# ------------------------------------------------------------------------------------------- as they are used together
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_pieces_of_prompts_over_an_8_bit_cache(D):
+    """Norm, append and attention piece by piece: every piece against the cache's own contents in 64 bits, so that what 8 bits cost the keys and values is no excuse."""
+    g = base.gen(D)
+    Hq, Hkv, page, lens = 4, 2, 16, [700, 233]
+    rows = base.normal(g, sum(lens), Hq + 2 * Hkv, D)
+    weight = (1 + 0.2 * base.normal(g, 2, D).float()).to(BF16)
+    pages = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(pages), device=DEV, generator=g).int()
+    table = torch.full((2, max(pages)), -1, dtype=torch.int32, device=DEV)
+    table[0, :pages[0]], table[1, :pages[1]] = order[:pages[0]], order[pages[0]:]
+    store = [torch.zeros(sum(pages), page, Hkv, D, device=DEV).to(E4M3) for _ in range(2)]
+    cache = cake.PagedCache(*store, torch.tensor([0.02, 0.03], device=DEV), torch.tensor([0.01, 0.02], device=DEV))
+    ws = cake.alloc_attention_workspace(Hq, Hkv, D, DEV)
+    done = [0, 0]
+    for piece in ([300, 0], [1, 100], [200, 1], [0, 132], [199, 0]):
+        at = torch.cat([torch.arange(d, d + n, device=DEV) for d, n in zip(done, piece)])
+        owner = torch.repeat_interleave(torch.arange(2, device=DEV), torch.tensor(piece, device=DEV))
+        slots = table[owner, at // page].long() * page + at % page
+        x = rows[at + owner * lens[0]]
+        q, _ = cake.cake_qk_norm_append(cache, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], slots, weight[0], weight[1], ws=ws)
+        done = [d + n for d, n in zip(done, piece)]
+        n = torch.tensor(done, dtype=torch.int32, device=DEV)
+        out, lse = cake.cake_paged_chunk(q, cache, table, n, base.starts_of(piece), want_lse=True, ws=ws)
+        base.check_chunk(out, lse, q, cache, table.clamp(min=0), piece, done)
+        k, v = cake.cake_kv_read(cache, slots, ws=ws)      # what was appended is what was attended to
+        for b in range(2):
+            mine = owner == b
+            want = [torch.stack([base.cached(cache, table.clamp(min=0), done, b, h)[i] for h in range(Hkv)], 1)[at[mine]].to(BF16) for i in range(2)]
+            assert torch.equal(k[mine], want[0]) and torch.equal(v[mine], want[1])
+    assert done == lens and cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
