@@ -220,7 +220,7 @@ __device__ __forceinline__ void reg_dep(uint32_t (&r)[32]) {
         : "memory");
 }
 
-// 32 lanes x 32 (16) consecutive columns from registers, and the wait for all stores of this thread
+// 32 lanes x 16 consecutive columns from registers, and the wait for all stores of this thread
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "

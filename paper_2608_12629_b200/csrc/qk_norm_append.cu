@@ -298,7 +298,11 @@ extern "C" int cake_qk_norm_append(const cake_paged_cache* cache, const cake_bf1
     if (wide) {
         const int lanes = D == 64 ? 4 : D == 256 ? 16 : 8;
         const int heads = Hq + 2 * cache->Hkv;
-        // Few tokens: a head to a group of lanes (latency).  More: four heads to a group, whose loads overlap and share the token's angles and weights
+        // Few tokens: a head to a group of lanes (latency).  More: four heads to a group, whose loads overlap and share the token's angles and weights, in blocks of
+        // 128 threads and, where those are plenty, of a single warp.  32 + 2 * 8 heads of 128, bf16 cache, us by a head to a group, 128 threads and a warp: 128 tokens 2.7,
+        // 3.5 and 6.8; 192 4.4, 3.7 and 6.7; 512 12, 5.6 and 9.1; 1,024 22, 10.6 and 10.4; 1,500 32, 13.2 and 11.7; 2,048 42, 16.4 and 13.1; 4,096 82, 30 and 24; 16,001 310,
+        // 104 and 80 (16 + 2 * 4 heads of 256 and 64 + 2 * 8 of 128 into 8-bit caches change places at the same sizes).  8 + 2 * 2 heads of 64: 512 2.5, 3.7 and 3.7;
+        // 1,500 4.6, 3.9 and 4.0; 16,001 40, 17.8 and 20.7
         int par, tokens = 1;
         if (T <= 128) {
             par = heads * lanes <= 512 ? heads : 512 / lanes;
