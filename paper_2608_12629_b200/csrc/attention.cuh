@@ -1061,7 +1061,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
             else if (a.lse) a.lse[row] = empty ? NEG_INF : (sub + __log2f(l)) * LN2;
         }
         const bool finite = !isnan((odd[0].x + odd[0].y) + (odd[1].x + odd[1].y) + (odd[2].x + odd[2].y) + (odd[3].x + odd[3].y));
-        const unsigned todo = __ballot_sync(0xffffffffu, valid && !finite && isfinite(l) && !empty);
+        const unsigned todo = __ballot_sync(0xffffffffu, valid && !finite && isfinite(l) && isfinite(vs) && !empty);
         if (__builtin_expect(todo != 0, 0)) mend_rows<T>(a, ctrl, sp, todo, r & 96, t, ra, rb);
         __syncwarp();
         if (lane == 0) arrive(&ctrl->seg_empty[segs % SEGS]);

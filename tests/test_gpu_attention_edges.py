@@ -420,3 +420,14 @@ def test_pieces_of_prompts_over_an_8_bit_cache(D):
             want = [torch.stack([base.cached(cache, table.clamp(min=0), done, b, h)[i] for h in range(Hkv)], 1)[at[mine]].to(BF16) for i in range(2)]
             assert torch.equal(k[mine], want[0]) and torch.equal(v[mine], want[1])
     assert done == lens and cake.cake_kmeans_device_status(ws) == cake.CAKE_OK
+
+
+def test_scales_of_values_that_are_no_numbers():
+    """They reach every row of their head that sees something, and no other head's; the rows are not computed again for it."""
+    new, lens = [5, 200, 4], [3, 1500, 300]
+    q, cache, table, n = base.paged(5, new, lens, 4, 2, 128, 16, "e4m3")
+    want, want_lse = base.run_chunk(q, cache, table, n, new)
+    cache.v_scale[1] = math.nan
+    out, lse = base.run_chunk(q, cache, table, n, new)
+    assert torch.equal(out[:, :2], want[:, :2]) and torch.equal(lse, want_lse)
+    assert (out[:2] == 0).all() and torch.isnan(out[2:, 2:]).all()      # (the first two tokens see nothing)
