@@ -923,7 +923,8 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Ctrl* ctrl, const Ro
                         u = ex2(u), v = ex2(v);
                         add2(sum[k & 1], u, v);
                         // Weights are rounded to 16 bits for the tensor core (bf16: half a step of 2^-8, about what the output's own
-                        // rounding is; it is the operand type that the values have), their sum is that of the unrounded ones
+                        // rounding is; it is the operand type that the values have, and a second term for the rest would be a second product and has
+                        // no room in tensor memory), their sum is that of the unrounded ones
                         p[k] = T::F16 ? pack_f16(u, v) : pack_bf16(u, v);
                     }
                     // the product that read the place of the weights before is complete (looked at every time: a parity names every other one)
