@@ -164,7 +164,8 @@ CAKE_API int cake_paged_decode(const cake_bf16* q, long long q_stride, long long
  * A token that sees nothing (or nothing that weighs anything) gives zeros, and -inf in out_lse.  Keys and values that a token does
  * not see do not touch its row, infinities and NaN among them (a row that meets such values in a tile of 128 keys beside its own is computed
  * again from its keys: right, and slow, 2 to 3 us a key for 32 such rows; beyond about a million keys that one block has of them the wait for it may
- * run out: device status CAKE_ERR_TIMEOUT).  A row whose weighted sum of finite values passes 32 bits is computed again likewise.  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are
+ * run out: device status CAKE_ERR_TIMEOUT).  A row whose weighted sum of finite values passes 32 bits is computed again likewise.
+ * An infinite value that a token sees may give NaN instead of infinity.  Scores, their maximum and sum, and the weighted sum of values are held in 32 bits.  The weights are
  * rounded to bf16 for the product with the values (8-bit caches: to f16, 11 bits down to 2^-25 of a row's heaviest, in steps of 2^-35
  * of it below), their sum is not.  8-bit caches: queries are divided by a power of two per head and rounded to f16 (exact down to 2^-14 of the head's largest element).  D: 64, 96, 128 or 256
  * (CAKE_ERR_UNSUPPORTED otherwise).  q, k, v and out are 16-byte aligned and strides multiples of 8 elements, at least D
