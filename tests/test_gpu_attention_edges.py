@@ -1,4 +1,5 @@
-"""Attention of many tokens at the edges of its range, against a plain implementation in 64 bits: scales that are no numbers or next to nothing, scores beyond all bounds.
+"""Attention of many tokens at the edges of its range, against a plain implementation in 64 bits: scales that are no numbers or next to nothing, scores and values
+beyond what 32 bits add up, values that are not finite and not seen, ranges out of bounds, the lightest weights of 8-bit caches, pieces of prompts as they are used.
 
 Tolerances: those of test_gpu_attention.py, whose reference and bounds this file uses."""
 import math
